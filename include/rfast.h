@@ -452,6 +452,68 @@ int rfast_ls_gradient_static(const float* d_feat, const float* d_target, const f
                              float* d_grad, int32_t rows, int32_t n_features, float l2,
                              void* cuda_stream, char* err, size_t err_len);
 
+/* ---- operators of a training step ------------------------------------------------------------
+ * No counterpart in the paper: they stand beside rfast_ls_gradient_static for callers that keep
+ * their own parameters, gradients and activations on the device.  Conventions of all of them:
+ * addresses named d_*, and every address inside the lists below, are DEVICE addresses of the device
+ * that is current at the call (RFAST_EINVAL for host memory or another device's where that
+ * is seen: the first tensor of each list and every single address are looked up); arrays OF
+ * addresses and sizes are HOST arrays, read before the call returns.  Work is enqueued on
+ * cuda_stream (cudaStream_t as void*; NULL: legacy default stream) and the call returns
+ * without waiting; nothing is allocated, nothing is kept from one call for the next, and every call
+ * may be captured into a CUDA graph (the addresses and scalars are then those of the
+ * recorded call).  err (may be NULL) receives the message of a failure.  A workspace belongs to one call
+ * at a time: calls that may overlap on the GPU -- other streams, graphs replayed side by side --
+ * need one each.  Results do not depend on timing: the same inputs give the same bits. */
+enum { RFAST_TYPE_F32 = 0, RFAST_TYPE_BF16 = 1, RFAST_TYPE_F16 = 2 };
+
+/* 2-norm over all values of all gradient tensors, and the factor that clips it:
+ *     norm = sqrt(sum g^2),   scale = max_norm / max(norm, max_norm)
+ * Sums are held in 64 bits, so that neither large nor tiny gradients leave the range of the sum.  A NaN
+ * makes both NaN; an infinite gradient gives norm = inf, scale = 0.  No values: norm = 0, scale = 1.
+ *   numel [n_tensors] values per tensor (0 allowed), grad [n_tensors] addresses, aligned to their
+ *   type only; d_norm, d_scale: one float each, either may be NULL (max_norm is then not read
+ *   without d_scale); workspace: RFAST_GRAD_NORM_WORKSPACE bytes of DEVICE memory, aligned to 8. */
+#define RFAST_GRAD_NORM_WORKSPACE 16384
+int rfast_grad_norm(int32_t n_tensors, int32_t grad_type, const int64_t* numel, const void* const* grad,
+                    float max_norm, float* d_norm, float* d_scale, void* workspace, size_t workspace_bytes,
+                    void* cuda_stream, char* err, size_t err_len);
+
+/* One AdamW step, in place, over many tensors (one launch for up to 480 of them):
+ *     g' = scale g                          scale = *d_grad_scale, 1 without it
+ *     m  = beta1 m + (1 - beta1) g'
+ *     v  = beta2 v + (1 - beta2) g'^2
+ *     p  = p (1 - lr weight_decay) - lr m / (1 - beta1^t) / (sqrt(v / (1 - beta2^t)) + eps)
+ * in 32 bits; p is rounded once to its type.
+ * state_bits = 32: m and v are fp32.
+ * state_bits = 8:  m holds e4m3 codes of the first moment, v e4m3 codes of sqrt(v) (half the range in
+ *   octaves, so that its small values keep their digits), one byte per value.  A block is RFAST_ADAMW_BLOCK
+ *   consecutive values of a tensor, the last one shorter; its scale is max(largest magnitude / 448, 2^-100)
+ *   in fp32, m_scale and v_scale hold ceil(numel / RFAST_ADAMW_BLOCK) of them per tensor, and a
+ *   value is code * scale.  Codes are nearest values, ties to even; a positive sqrt(v) keeps at least the
+ *   smallest positive code, so that no first moment meets a denominator of eps alone.  All bytes zero
+ *   are moments of zero.  A NaN or infinite gradient leaves its whole block's moments NaN or infinite.
+ * Tensors may not overlap one another.  Addresses are aligned to their type only; tensors whose
+ * addresses are aligned to four values are read and written in quads. */
+#define RFAST_ADAMW_BLOCK 256
+typedef struct rfast_adamw {
+    int32_t n_tensors;
+    int32_t param_type, grad_type;     /* RFAST_TYPE_* */
+    int32_t state_bits;                /* 32 or 8 */
+    const int64_t*     numel;          /* [n_tensors], 0 allowed */
+    void* const*       param;
+    const void* const* grad;
+    void* const*       m;              /* fp32 or 8-bit codes */
+    void* const*       v;
+    float* const*      m_scale;        /* 8-bit moments only */
+    float* const*      v_scale;
+    double  lr, beta1, beta2, eps, weight_decay;   /* beta in [0, 1), eps >= 2^-126 */
+    int64_t step;                      /* t >= 1, the number of this step */
+    const int64_t* d_step;             /* DEVICE: t is read from here instead (a step recorded into a graph), or NULL */
+    const float*   d_grad_scale;       /* DEVICE: factor on the gradients, or NULL */
+} rfast_adamw;
+int rfast_adamw_step(const rfast_adamw* a, void* cuda_stream, char* err, size_t err_len);
+
 void        rfast_destroy(rfast_ctx* ctx);
 const char* rfast_last_error(const rfast_ctx* ctx);   /* ctx may be NULL: last create error */
 const char* rfast_version(void);

@@ -61,6 +61,19 @@ class _Schedule(C.Structure):
                 ("alpha_round", C.c_void_p)]
 
 
+TYPE_IDS = {"f32": 0, "bf16": 1, "f16": 2}
+GRAD_NORM_WORKSPACE = 16384
+ADAMW_BLOCK = 256
+
+
+class _AdamW(C.Structure):
+    _fields_ = [("n_tensors", C.c_int32), ("param_type", C.c_int32), ("grad_type", C.c_int32), ("state_bits", C.c_int32),
+                ("numel", C.c_void_p), ("param", C.c_void_p), ("grad", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p),
+                ("m_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("weight_decay", C.c_double),
+                ("step", C.c_int64), ("d_step", C.c_void_p), ("d_grad_scale", C.c_void_p)]
+
+
 _lib = None
 
 
@@ -105,6 +118,9 @@ def lib():
         L.rfast_write_packet.argtypes = [C.c_void_p, C.c_int, C.c_int32, C.c_int32, C.c_void_p, C.c_size_t]
         L.rfast_ls_gradient_static.argtypes = [C.c_void_p] * 4 + [C.c_int32, C.c_int32, C.c_float,
                                                C.c_void_p, C.c_char_p, C.c_size_t]
+        L.rfast_grad_norm.argtypes = [C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_float, C.c_void_p, C.c_void_p,
+                                      C.c_void_p, C.c_size_t, C.c_void_p, C.c_char_p, C.c_size_t]
+        L.rfast_adamw_step.argtypes = [C.POINTER(_AdamW), C.c_void_p, C.c_char_p, C.c_size_t]
         _lib = L
     return _lib
 
@@ -381,6 +397,63 @@ def rfast_ls_gradient_static(d_feat: int, d_target: int, d_x: int, d_grad: int, 
                                         C.c_void_p(cuda_stream), err, 256)
     if rc != OK:
         raise RFastError(rc, err.value.decode())
+
+
+def _type(name):
+    if name not in TYPE_IDS:
+        raise ValueError(f"unknown type {name!r}: one of {', '.join(TYPE_IDS)}")
+    return TYPE_IDS[name]
+
+
+def _list(values, n=None, what="list"):
+    """Sizes or device addresses of a list of tensors as a host array of 64-bit integers."""
+    a = np.ascontiguousarray(values, dtype=np.int64)
+    if a.ndim != 1 or (n is not None and len(a) != n):
+        raise ValueError(f"{what} must hold one entry per tensor")
+    return a
+
+
+def _op(rc, err):
+    if rc != OK:
+        raise RFastError(rc, err.value.decode())
+
+
+def rfast_grad_norm(grad, numel, max_norm: float, d_norm: int, d_scale: int, workspace: int, workspace_bytes: int,
+                    grad_type: str = "f32", cuda_stream: int = 0) -> None:
+    """2-norm over all gradient tensors into *d_norm and the factor max_norm / max(norm, max_norm) into
+    *d_scale (DEVICE addresses of one fp32 value each, 0 for none).  grad: DEVICE addresses of the
+    tensors, numel their sizes (sequences or integer arrays); workspace: the DEVICE address of
+    GRAD_NORM_WORKSPACE bytes that no other running call uses.  Enqueued on cuda_stream."""
+    n = _list(numel, None, "numel")
+    g = _list(grad, len(n), "grad")
+    err = C.create_string_buffer(256)
+    _op(lib().rfast_grad_norm(len(n), _type(grad_type), n.ctypes.data, g.ctypes.data, max_norm, d_norm or None, d_scale or None,
+                              workspace or None, workspace_bytes, cuda_stream or None, err, 256), err)
+
+
+def rfast_adamw_step(param, grad, m, v, numel, step: int = 0, lr: float = 1e-3, beta1: float = 0.9, beta2: float = 0.999,
+                     eps: float = 1e-8, weight_decay: float = 1e-2, m_scale=None, v_scale=None, param_type: str = "f32",
+                     grad_type: str = "f32", d_step: int = 0, d_grad_scale: int = 0, cuda_stream: int = 0) -> None:
+    """One AdamW step, in place, over many tensors: param, grad, m, v are their DEVICE addresses, numel
+    their sizes (sequences or integer arrays).  Moments are fp32; with m_scale and v_scale they are 8-bit
+    codes with one fp32 scale per ADAMW_BLOCK values of a tensor.  step counts from 1; d_step: DEVICE
+    address of an int64 that holds it instead; d_grad_scale: DEVICE address of an fp32 factor on the
+    gradients (rfast_grad_norm writes one).  Enqueued on cuda_stream."""
+    n = _list(numel, None, "numel")
+    k = len(n)
+    lists = [_list(a, k, name) for a, name in ((param, "param"), (grad, "grad"), (m, "m"), (v, "v"))]
+    if (m_scale is None) != (v_scale is None):
+        raise ValueError("8-bit moments need both m_scale and v_scale")
+    bits = 32
+    scales = [None, None]
+    if m_scale is not None:
+        bits = 8
+        lists += [_list(m_scale, k, "m_scale"), _list(v_scale, k, "v_scale")]
+        scales = [a.ctypes.data for a in lists[4:]]
+    args = _AdamW(k, _type(param_type), _type(grad_type), bits, n.ctypes.data, *[a.ctypes.data for a in lists[:4]], *scales,
+                  lr, beta1, beta2, eps, weight_decay, step, d_step or None, d_grad_scale or None)
+    err = C.create_string_buffer(256)
+    _op(lib().rfast_adamw_step(C.byref(args), cuda_stream or None, err, 256), err)
 
 
 class Engine:

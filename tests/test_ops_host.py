@@ -1,0 +1,111 @@
+"""Refusals of the training-step operators.  Every one of them is decided on the host before any
+device is looked at, so these run without a GPU; the addresses are never followed."""
+
+from __future__ import annotations
+
+import numpy as np
+import pytest
+
+A = 1 << 20          # an address nobody reads
+
+
+def _refused(text, call, *a, **kw):
+    from paper_2307_11617_b200.binding import EINVAL, RFastError
+    with pytest.raises(RFastError) as ei:
+        call(*a, **kw)
+    assert ei.value.code == EINVAL and text in str(ei.value), ei.value
+
+
+def _adamw(**kw):
+    import paper_2307_11617_b200 as pkg
+    n = kw.pop("numel", [5, 7])
+    base = dict(param=[A, A], grad=[A, A], m=[A, A], v=[A, A], numel=n, step=1)
+    base.update(kw)
+    pkg.rfast_adamw_step(**base)
+
+
+@pytest.mark.parametrize("text,kw", [
+    ("step counts from 1", dict(step=0)),
+    ("beta1 and beta2", dict(beta1=1.0)),
+    ("beta1 and beta2", dict(beta2=float("nan"))),
+    ("beta1 and beta2", dict(beta2=-0.1)),
+    ("eps must be", dict(eps=0.0)),
+    ("eps must be", dict(eps=1e-60)),
+    ("eps must be", dict(eps=float("nan"))),
+    ("lr and weight_decay", dict(lr=float("inf"))),
+    ("lr and weight_decay", dict(weight_decay=float("nan"))),
+    ("numel of tensor 1", dict(numel=[5, -1])),
+    ("numel of tensor 0", dict(numel=[1 << 41, 3])),
+    ("tensor 1 has a null address", dict(grad=[A, 0])),
+    ("tensor 0 has a null address", dict(m=[0, A])),
+    ("tensor 0 has a null address", dict(m_scale=[0, A], v_scale=[A, A])),
+    ("not aligned", dict(param=[A + 2, A])),
+    ("not aligned", dict(param=[A + 1, A], param_type="bf16")),
+    ("not aligned", dict(v=[A, A + 1])),
+    ("not aligned", dict(m_scale=[A, A + 2], v_scale=[A, A])),
+])
+def test_adamw_refuses(rfast_lib, text, kw):
+    _refused(text, _adamw, **kw)
+
+
+def test_adamw_c_entry_refuses(rfast_lib):
+    """What the binding cannot be made to pass."""
+    import ctypes as C
+    from paper_2307_11617_b200 import binding as B
+    err = C.create_string_buffer(256)
+    assert B.lib().rfast_adamw_step(None, None, err, 256) == B.EINVAL and b"null arguments" in err.value
+    assert B.lib().rfast_adamw_step(None, None, None, 0) == B.EINVAL
+    one = np.ones(1, np.int64)
+    a = B._AdamW(1, 0, 0, 32, one.ctypes.data, one.ctypes.data, one.ctypes.data, one.ctypes.data, None, None, None, 1e-3, 0.9, 0.99, 1e-8, 0, 1, None, None)
+    assert B.lib().rfast_adamw_step(C.byref(a), None, err, 256) == B.EINVAL and b"null array" in err.value
+    for field, value, text in (("state_bits", 16, b"state_bits"), ("param_type", 7, b"unknown type"), ("grad_type", -1, b"unknown type"),
+                               ("n_tensors", -1, b"n_tensors")):
+        a = B._AdamW(1, 0, 0, 32, *[one.ctypes.data] * 5, None, None, 1e-3, 0.9, 0.99, 1e-8, 0, 1, None, None)
+        setattr(a, field, value)
+        assert B.lib().rfast_adamw_step(C.byref(a), None, err, 256) == B.EINVAL and text in err.value, err.value
+
+
+def test_adamw_nothing_to_do_needs_no_device(rfast_lib):
+    import paper_2307_11617_b200 as pkg
+    pkg.rfast_adamw_step([], [], [], [], [], step=1)
+    pkg.rfast_adamw_step([0], [0], [0], [0], [0], step=1)          # an empty tensor has no address
+
+
+def test_lists_of_unlike_length_are_refused(rfast_lib):
+    import paper_2307_11617_b200 as pkg
+    with pytest.raises(ValueError):
+        pkg.rfast_adamw_step([A], [A, A], [A], [A], [3], step=1)
+    with pytest.raises(ValueError):
+        pkg.rfast_adamw_step([A], [A], [A], [A], [3], step=1, m_scale=[A])
+    with pytest.raises(ValueError):
+        pkg.rfast_adamw_step([A], [A], [A], [A], [3], step=1, param_type="f64")
+    with pytest.raises(ValueError):
+        pkg.rfast_grad_norm([A], [3, 4], 1.0, A, A, A, 16384)
+
+
+@pytest.mark.parametrize("text,kw", [
+    ("neither", dict(d_norm=0, d_scale=0)),
+    ("max_norm", dict(max_norm=0.0)),
+    ("max_norm", dict(max_norm=float("nan"))),
+    ("workspace must be given", dict(workspace=0)),
+    ("aligned to 8", dict(workspace=A + 4)),
+    ("workspace needs", dict(workspace_bytes=8)),
+    ("output is not aligned", dict(d_norm=A + 2)),
+    ("numel of tensor 0", dict(numel=[-2, 1])),
+    ("tensor 1 has a null address", dict(grad=[A, 0])),
+    ("address of tensor 1", dict(grad=[A, A + 1], grad_type="f16")),
+])
+def test_grad_norm_refuses(rfast_lib, text, kw):
+    import paper_2307_11617_b200 as pkg
+    base = dict(grad=[A, A], numel=[5, 7], max_norm=1.0, d_norm=A, d_scale=A, workspace=A, workspace_bytes=pkg.GRAD_NORM_WORKSPACE)
+    base.update(kw)
+    _refused(text, pkg.rfast_grad_norm, **base)
+
+
+def test_constants_of_the_binding_are_the_headers(rfast_lib, repo_root):
+    import os
+    import re
+    from paper_2307_11617_b200 import binding as B
+    text = open(os.path.join(repo_root, "include", "rfast.h")).read()
+    assert int(re.search(r"#define RFAST_GRAD_NORM_WORKSPACE (\d+)", text).group(1)) == B.GRAD_NORM_WORKSPACE
+    assert int(re.search(r"#define RFAST_ADAMW_BLOCK (\d+)", text).group(1)) == B.ADAMW_BLOCK
