@@ -6,9 +6,10 @@
 // call), tensors are cut into chunks, and a thread block finds its tensor by bisection in the
 // table's running chunk counts.
 //
-// Elements are taken in quads: lane l of a warp holds quads l and l + 32 of a block of 256
-// values, so that a request covers 512, 256 or 128 contiguous bytes for 4-, 2- and 1-byte types
-// and a block's largest value is one warp reduction away.
+// A warp takes a block of 256 values at a time.  Where the tensor's addresses allow it, lane l holds
+// quads l and l + 32 of the block, so that a request covers 512, 256 or 128 contiguous bytes for
+// 4-, 2- and 1-byte types; in ragged last blocks and misaligned tensors it holds values l + 32 j.
+// Either way the block's largest value is one warp reduction away.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -17,6 +18,7 @@
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
+#include <type_traits>
 
 #include "ops.h"
 
@@ -27,7 +29,7 @@ namespace {
 constexpr int kThreadsOp = 256;
 constexpr int kWarps = kThreadsOp / 32;
 
-// ---- typed quads ------------------------------------------------------------------------------
+// ---- types ------------------------------------------------------------------------------------
 __device__ __forceinline__ float to_f32(float v) { return v; }
 __device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
 __device__ __forceinline__ float to_f32(__half v) { return __half2float(v); }
@@ -38,73 +40,43 @@ template <> __device__ __forceinline__ __half from_f32<__half>(float v) { return
 
 template <class T> struct Raw4 { typedef uint2 type; };          // four 16-bit values
 template <> struct Raw4<float> { typedef float4 type; };
+template <> struct Raw4<uint8_t> { typedef uint32_t type; };     // four codes
 
-__device__ __forceinline__ float4 unpack4(float4 r, const float*) { return r; }
-__device__ __forceinline__ float4 unpack4(uint2 r, const __nv_bfloat16*) {
-    return make_float4(__uint_as_float(r.x << 16), __uint_as_float(r.x & 0xffff0000u),
-                       __uint_as_float(r.y << 16), __uint_as_float(r.y & 0xffff0000u));
+__device__ __forceinline__ void unpack2(uint32_t r, const __nv_bfloat16*, float* v) {
+    v[0] = __uint_as_float(r << 16);
+    v[1] = __uint_as_float(r & 0xffff0000u);
 }
-__device__ __forceinline__ float4 unpack4(uint2 r, const __half*) {
-    const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&r.x));
-    const float2 b = __half22float2(*reinterpret_cast<const __half2*>(&r.y));
-    return make_float4(a.x, a.y, b.x, b.y);
+__device__ __forceinline__ void unpack2(uint32_t r, const __half*, float* v) {
+    const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&r));
+    v[0] = a.x; v[1] = a.y;
 }
-
-// Values i .. i+3 of a tensor of n; `wide`: the tensor's address allows quad accesses.
+__device__ __forceinline__ void unpack4(float4 r, const float*, float* v) { v[0] = r.x; v[1] = r.y; v[2] = r.z; v[3] = r.w; }
 template <class T>
-__device__ __forceinline__ float4 load4(const T* t, int64_t i, int64_t n, bool wide) {
-    if (wide && i + 4 <= n) {
-        typedef typename Raw4<T>::type R;
-        return unpack4(__ldcs(reinterpret_cast<const R*>(t + i)), t);
-    }
-    float v[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] = i + k < n ? to_f32(t[i + k]) : 0.f;
-    return make_float4(v[0], v[1], v[2], v[3]);
-}
+__device__ __forceinline__ void unpack4(uint2 r, const T* t, float* v) { unpack2(r.x, t, v); unpack2(r.y, t, v + 2); }
 
-__device__ __forceinline__ void store_raw4(float* t, float4 v) { __stcs(reinterpret_cast<float4*>(t), v); }
-__device__ __forceinline__ void store_raw4(__nv_bfloat16* t, float4 v) {
-    const __nv_bfloat162 a = __floats2bfloat162_rn(v.x, v.y), b = __floats2bfloat162_rn(v.z, v.w);
+__device__ __forceinline__ void store4(float* t, const float* v) { __stcs(reinterpret_cast<float4*>(t), make_float4(v[0], v[1], v[2], v[3])); }
+__device__ __forceinline__ void store4(__nv_bfloat16* t, const float* v) {
+    const __nv_bfloat162 a = __floats2bfloat162_rn(v[0], v[1]), b = __floats2bfloat162_rn(v[2], v[3]);
     __stcs(reinterpret_cast<uint2*>(t), make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b)));
 }
-__device__ __forceinline__ void store_raw4(__half* t, float4 v) {
-    const __half2 a = __floats2half2_rn(v.x, v.y), b = __floats2half2_rn(v.z, v.w);
+__device__ __forceinline__ void store4(__half* t, const float* v) {
+    const __half2 a = __floats2half2_rn(v[0], v[1]), b = __floats2half2_rn(v[2], v[3]);
     __stcs(reinterpret_cast<uint2*>(t), make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b)));
-}
-template <class T>
-__device__ __forceinline__ void store4(T* t, int64_t i, int64_t n, bool wide, float4 v) {
-    if (wide && i + 4 <= n) { store_raw4(t + i, v); return; }
-    const float a[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int k = 0; k < 4; ++k) if (i + k < n) t[i + k] = from_f32<T>(a[k]);
 }
 
 // ---- 8-bit codes: e4m3, four to a word ----------------------------------------------------------
-__device__ __forceinline__ float4 decode4(uint32_t c) {
+__device__ __forceinline__ void decode4(uint32_t c, float* v) {
     uint32_t lo, hi;
     asm("{\n.reg .b16 a, b;\nmov.b32 {a, b}, %2;\ncvt.rn.f16x2.e4m3x2 %0, a;\ncvt.rn.f16x2.e4m3x2 %1, b;\n}" : "=r"(lo), "=r"(hi) : "r"(c));
     const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&lo)), y = __half22float2(*reinterpret_cast<const __half2*>(&hi));
-    return make_float4(x.x, x.y, y.x, y.y);
+    v[0] = x.x; v[1] = x.y; v[2] = y.x; v[3] = y.y;
 }
 // nearest, ties to even, beyond the largest value: the largest value
-__device__ __forceinline__ uint32_t encode4(float4 v) {
+__device__ __forceinline__ uint32_t encode4(const float* v) {
     uint32_t c;
     asm("{\n.reg .b16 a, b;\ncvt.rn.satfinite.e4m3x2.f32 a, %2, %1;\ncvt.rn.satfinite.e4m3x2.f32 b, %4, %3;\nmov.b32 %0, {a, b};\n}"
-        : "=r"(c) : "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w));
+        : "=r"(c) : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]));
     return c;
-}
-__device__ __forceinline__ uint32_t load_codes(const uint8_t* t, int64_t i, int64_t n, bool wide) {
-    if (wide && i + 4 <= n) return __ldcs(reinterpret_cast<const uint32_t*>(t + i));
-    uint32_t c = 0;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) if (i + k < n) c |= (uint32_t)t[i + k] << (8 * k);
-    return c;
-}
-__device__ __forceinline__ void store_codes(uint8_t* t, int64_t i, int64_t n, bool wide, uint32_t c) {
-    if (wide && i + 4 <= n) { __stcs(reinterpret_cast<uint32_t*>(t + i), c); return; }
-#pragma unroll
-    for (int k = 0; k < 4; ++k) if (i + k < n) t[i + k] = (uint8_t)(c >> (8 * k));
 }
 
 // maxima that a NaN goes through
@@ -118,26 +90,22 @@ __device__ __forceinline__ float warp_max_nan(float v) {
     asm volatile("redux.sync.max.NaN.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
     return r;
 }
-__device__ __forceinline__ float max4_abs(float4 v) {
-    return max_nan(max_nan(fabsf(v.x), fabsf(v.y)), max_nan(fabsf(v.z), fabsf(v.w)));
-}
-
 // Scale of a block from its largest value.  The floor keeps 1 / scale finite; blocks that small
 // (all below 2^-91) just use fewer codes.
 __device__ __forceinline__ float block_scale(float top) {
     return max_nan(__fmul_rn(top, (float)(1.0 / 448.0)), 7.888609052210118e-31f);   // 2^-100
 }
-
-// ---- one value ------------------------------------------------------------------------------------
-// Products and sums are rounded one by one (no fused multiply-add), so that the value an 8-bit code
-// is chosen from does not depend on how the compiler contracts the expression.
-__device__ __forceinline__ void moments(const AdamCoef& c, float g, float& m, float& v) {
-    m = __fadd_rn(__fmul_rn(m, c.beta1), __fmul_rn(g, c.omb1));
-    v = __fadd_rn(__fmul_rn(v, c.beta2), __fmul_rn(__fmul_rn(g, g), c.omb2));
+// 1 ulp; below the least normal number 0
+__device__ __forceinline__ float root_of(float v) {
+    float r;
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
 }
-// x (1 - lr wd) - step * m / (r * root + eps); the quotient to 2 ulp is far below the rounding of x
-__device__ __forceinline__ float updated(const AdamCoef& c, float p, float m, float r) {
-    return p * c.keep - c.step * __fdividef(m, fmaf(r, c.root, c.eps));
+// 1 ulp; the denominators are at least eps, a normal number
+__device__ __forceinline__ float inverse_of(float v) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
 }
 
 struct TensorView {
@@ -149,86 +117,180 @@ struct TensorView {
     bool wide;
 };
 
-// U blocks of 256 values from block b0 on, by one warp; every load is in flight before the first use.
-template <class PT, class GT, bool S8, int U>
-__device__ __forceinline__ void adamw_blocks(const TensorView& t, const AdamCoef& c, float gscale, int64_t b0, int lane) {
-    float4 p[U][2], g[U][2], m[U][2], v[U][2];
-    uint32_t cm[U][2], cv[U][2];
-    float sm[U], sv[U];
+// Factors of a step that do not change from value to value.
+struct StepFactors {
+    float b1, g1;        // m = b1 m + g1 g
+    float b2, g2;        // 32-bit moments: v = b2 v + (g2 g)^2; 8-bit moments: v = (b2 r)^2 + (g2 g)^2
+    float root, eps, keep, step;
+};
+template <bool S8>
+__device__ __forceinline__ StepFactors factors(const AdamCoef& c, float gscale) {
+    return {c.beta1, gscale * c.omb1, S8 ? c.root_beta2 : c.beta2, gscale * c.root_omb2, c.root, c.eps, c.keep, c.step};
+}
+
+// Eight values: moments and parameter after the step.  8-bit moments come as codes with their block's
+// scales and leave as the first moment and the root of the second.
+template <bool S8>
+__device__ __forceinline__ void advance(const StepFactors& f, float sm, float sv, float (&p)[8], const float (&g)[8], float (&m)[8], float (&v)[8]) {
+    const float bm = S8 ? sm * f.b1 : f.b1, bv = S8 ? sv * f.b2 : f.b2;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int64_t i0 = (b0 + u) * kAdamBlock + lane * 4;
-        sm[u] = sv[u] = 0.f;
-        if (S8 && (b0 + u) * kAdamBlock < t.n) { sm[u] = t.ms[b0 + u]; sv[u] = t.vs[b0 + u]; }
+    for (int k = 0; k < 8; ++k) {
+        const float h = f.g2 * g[k];
+        m[k] = fmaf(f.g1, g[k], bm * m[k]);
+        float r;
+        if (S8) {
+            const float q = bv * v[k];
+            r = root_of(fmaf(q, q, h * h));
+            v[k] = r;
+        } else {
+            v[k] = fmaf(bv, v[k], h * h);
+            r = root_of(v[k]);
+        }
+        p[k] = fmaf(-f.step, m[k] * inverse_of(fmaf(r, f.root, f.eps)), p[k] * f.keep);
+    }
+}
+
+// Scales and codes of a block's moments, eight values in every lane.  A positive root keeps a positive
+// code: a first moment that survives its rounding must not meet a denominator of eps alone.
+__device__ __forceinline__ void to_codes(const float (&m)[8], const float (&r)[8], float& sm, float& sv, float (&cm)[8], float (&cv)[8]) {
+    float tm = fabsf(m[0]), tv = r[0];
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const int64_t i = i0 + k * 128;
-            g[u][k] = load4((const GT*)t.g, i, t.n, t.wide);
-            p[u][k] = load4((const PT*)t.p, i, t.n, t.wide);
-            if (S8) {
-                cm[u][k] = load_codes((const uint8_t*)t.m, i, t.n, t.wide);
-                cv[u][k] = load_codes((const uint8_t*)t.v, i, t.n, t.wide);
-            } else {
-                m[u][k] = load4((const float*)t.m, i, t.n, t.wide);
-                v[u][k] = load4((const float*)t.v, i, t.n, t.wide);
-            }
+    for (int k = 1; k < 8; ++k) { tm = max_nan(tm, fabsf(m[k])); tv = max_nan(tv, r[k]); }
+    sm = block_scale(warp_max_nan(tm));
+    sv = block_scale(warp_max_nan(tv));
+    const float im = __frcp_rn(sm), iv = __frcp_rn(sv);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        cm[k] = m[k] * im;
+        const float q = r[k] * iv;
+        cv[k] = r[k] > 0.f ? max_nan(q, 0.001953125f) : q;      // 2^-9
+    }
+}
+
+// A block as it lies in memory, two quads of every stream per lane.
+template <class PT, class GT, class MT>
+struct RawBlock {
+    typename Raw4<PT>::type p[2];
+    typename Raw4<GT>::type g[2];
+    typename Raw4<MT>::type m[2], v[2];
+    float sm, sv;
+};
+template <class PT, class GT, class MT, bool S8>
+__device__ __forceinline__ void fetch(RawBlock<PT, GT, MT>& r, const TensorView& t, int64_t b, int lane) {
+    const int64_t i = b * kAdamBlock + lane * 4;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        r.g[k] = __ldcs(reinterpret_cast<const typename Raw4<GT>::type*>((const GT*)t.g + i + k * 128));
+        r.p[k] = __ldcs(reinterpret_cast<const typename Raw4<PT>::type*>((const PT*)t.p + i + k * 128));
+        r.m[k] = __ldcs(reinterpret_cast<const typename Raw4<MT>::type*>((const MT*)t.m + i + k * 128));
+        r.v[k] = __ldcs(reinterpret_cast<const typename Raw4<MT>::type*>((const MT*)t.v + i + k * 128));
+    }
+    if (S8) { r.sm = t.ms[b]; r.sv = t.vs[b]; }
+}
+template <class PT, class GT, class MT, bool S8>
+__device__ __forceinline__ void finish(const RawBlock<PT, GT, MT>& r, const TensorView& t, const StepFactors& f, int64_t b, int lane) {
+    const int64_t i = b * kAdamBlock + lane * 4;
+    float p[8], g[8], m[8], v[8];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        unpack4(r.g[k], (const GT*)nullptr, g + 4 * k);
+        unpack4(r.p[k], (const PT*)nullptr, p + 4 * k);
+        if constexpr (S8) {
+            decode4(r.m[k], m + 4 * k);
+            decode4(r.v[k], v + 4 * k);
+        } else {
+            unpack4(r.m[k], (const float*)nullptr, m + 4 * k);
+            unpack4(r.v[k], (const float*)nullptr, v + 4 * k);
         }
     }
+    advance<S8>(f, r.sm, r.sv, p, g, m, v);
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        if ((b0 + u) * kAdamBlock >= t.n) return;                  // the same for the whole warp
-        const int64_t i0 = (b0 + u) * kAdamBlock + lane * 4;
-        float4 r[2];
+    for (int k = 0; k < 2; ++k) store4((PT*)t.p + i + k * 128, p + 4 * k);
+    if constexpr (S8) {
+        float sm, sv, cm[8], cv[8];
+        to_codes(m, v, sm, sv, cm, cv);
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-            if (S8) {
-                const float4 a = decode4(cm[u][k]), b = decode4(cv[u][k]);
-                m[u][k] = make_float4(__fmul_rn(a.x, sm[u]), __fmul_rn(a.y, sm[u]), __fmul_rn(a.z, sm[u]), __fmul_rn(a.w, sm[u]));
-                const float4 o = make_float4(__fmul_rn(b.x, sv[u]), __fmul_rn(b.y, sv[u]), __fmul_rn(b.z, sv[u]), __fmul_rn(b.w, sv[u]));
-                v[u][k] = make_float4(__fmul_rn(o.x, o.x), __fmul_rn(o.y, o.y), __fmul_rn(o.z, o.z), __fmul_rn(o.w, o.w));
-            }
-            const float4 q = make_float4(__fmul_rn(g[u][k].x, gscale), __fmul_rn(g[u][k].y, gscale), __fmul_rn(g[u][k].z, gscale), __fmul_rn(g[u][k].w, gscale));
-            moments(c, q.x, m[u][k].x, v[u][k].x);
-            moments(c, q.y, m[u][k].y, v[u][k].y);
-            moments(c, q.z, m[u][k].z, v[u][k].z);
-            moments(c, q.w, m[u][k].w, v[u][k].w);
-            r[k] = make_float4(__fsqrt_rn(v[u][k].x), __fsqrt_rn(v[u][k].y), __fsqrt_rn(v[u][k].z), __fsqrt_rn(v[u][k].w));
-            const float4 x = p[u][k];
-            store4((PT*)t.p, i0 + k * 128, t.n, t.wide,
-                   make_float4(updated(c, x.x, m[u][k].x, r[k].x), updated(c, x.y, m[u][k].y, r[k].y),
-                               updated(c, x.z, m[u][k].z, r[k].z), updated(c, x.w, m[u][k].w, r[k].w)));
-            if (!S8) {
-                store4((float*)t.m, i0 + k * 128, t.n, t.wide, m[u][k]);
-                store4((float*)t.v, i0 + k * 128, t.n, t.wide, v[u][k]);
-            }
+            __stcs(reinterpret_cast<uint32_t*>((uint8_t*)t.m + i + k * 128), encode4(cm + 4 * k));
+            __stcs(reinterpret_cast<uint32_t*>((uint8_t*)t.v + i + k * 128), encode4(cv + 4 * k));
         }
-        if (S8) {
-            // values beyond the tensor's end were loaded as zeros and stay zero: they raise no maximum
-            const float tm = block_scale(warp_max_nan(max_nan(max4_abs(m[u][0]), max4_abs(m[u][1]))));
-            const float tv = block_scale(warp_max_nan(max_nan(max4_abs(r[0]), max4_abs(r[1]))));
-            const float im = __frcp_rn(tm), iv = __frcp_rn(tv);
+        if (lane == 0) { t.ms[b] = sm; t.vs[b] = sv; }
+    } else {
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const float4 a = m[u][k];
-                store_codes((uint8_t*)t.m, i0 + k * 128, t.n, t.wide,
-                            encode4(make_float4(__fmul_rn(a.x, im), __fmul_rn(a.y, im), __fmul_rn(a.z, im), __fmul_rn(a.w, im))));
-                // a positive root keeps a positive code: a first moment that survives its rounding must
-                // not meet a denominator of eps alone
-                float w[4] = {r[k].x, r[k].y, r[k].z, r[k].w};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float q = __fmul_rn(w[j], iv);
-                    w[j] = w[j] > 0.f && q < 0.001953125f ? 0.001953125f : q;     // 2^-9
-                }
-                store_codes((uint8_t*)t.v, i0 + k * 128, t.n, t.wide, encode4(make_float4(w[0], w[1], w[2], w[3])));
-            }
-            if (lane == 0) { t.ms[b0 + u] = tm; t.vs[b0 + u] = tv; }
+        for (int k = 0; k < 2; ++k) {
+            store4((float*)t.m + i + k * 128, m + 4 * k);
+            store4((float*)t.v + i + k * 128, v + 4 * k);
         }
     }
 }
 
-constexpr int kAdamU = 2;                                   // blocks of 256 in flight per warp
-constexpr int kAdamChunk = kWarps * kAdamU;                 // blocks per thread block
+// A block that ends early or whose tensor is misaligned, value by value.  Values beyond the end
+// count as zeros: they raise no maximum.
+template <class PT, class GT, class MT, bool S8>
+__device__ __forceinline__ void block_by_values(const TensorView& t, const StepFactors& f, int64_t b, int lane) {
+    const int64_t i = b * kAdamBlock + lane;
+    float p[8], g[8], m[8], v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const int64_t j = i + 32 * k;
+        const bool in = j < t.n;
+        p[k] = in ? to_f32(((const PT*)t.p)[j]) : 0.f;
+        g[k] = in ? to_f32(((const GT*)t.g)[j]) : 0.f;
+        if constexpr (S8) {
+            float q[4];
+            const uint32_t c = in ? (uint32_t)((const uint8_t*)t.m)[j] | (uint32_t)((const uint8_t*)t.v)[j] << 8 : 0u;
+            decode4(c, q);
+            m[k] = q[0]; v[k] = q[1];
+        } else {
+            m[k] = in ? ((const float*)t.m)[j] : 0.f;
+            v[k] = in ? ((const float*)t.v)[j] : 0.f;
+        }
+    }
+    advance<S8>(f, S8 ? t.ms[b] : 0.f, S8 ? t.vs[b] : 0.f, p, g, m, v);
+    float sm, sv, cm[8], cv[8];
+    if constexpr (S8) to_codes(m, v, sm, sv, cm, cv);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const int64_t j = i + 32 * k;
+        if (j >= t.n) break;
+        ((PT*)t.p)[j] = from_f32<PT>(p[k]);
+        if constexpr (S8) {
+            const float q[4] = {cm[k], cv[k], 0.f, 0.f};
+            const uint32_t c = encode4(q);
+            ((uint8_t*)t.m)[j] = (uint8_t)c;
+            ((uint8_t*)t.v)[j] = (uint8_t)(c >> 8);
+        } else {
+            ((float*)t.m)[j] = m[k];
+            ((float*)t.v)[j] = v[k];
+        }
+    }
+    if constexpr (S8) if (lane == 0) { t.ms[b] = sm; t.vs[b] = sv; }
+}
+
+constexpr int kAdamRun = 4;                                 // blocks of 256 values per warp
+constexpr int kAdamChunk = kWarps * kAdamRun;               // blocks per thread block
+
+// The chunk of blocks [c0, c0 + kAdamChunk) of a tensor, by one thread block: warp w takes blocks w,
+// w + 8, ...; a block is fetched while the one before it is worked on.
+template <class PT, class GT, bool S8>
+__device__ __forceinline__ void adamw_chunk(const TensorView& t, const StepFactors& f, int64_t c0) {
+    typedef typename std::conditional<S8, uint8_t, float>::type MT;
+    const int lane = threadIdx.x & 31;
+    const int64_t b0 = c0 + (threadIdx.x >> 5);
+    const int64_t full = t.wide ? t.n / kAdamBlock : 0;     // blocks that quads cover
+    RawBlock<PT, GT, MT> raw[2];
+    if (b0 < full) fetch<PT, GT, MT, S8>(raw[0], t, b0, lane);
+#pragma unroll
+    for (int u = 0; u < kAdamRun; ++u) {
+        const int64_t b = b0 + u * kWarps;
+        if (u + 1 < kAdamRun && b + kWarps < full) fetch<PT, GT, MT, S8>(raw[(u + 1) & 1], t, b + kWarps, lane);
+        if (b < full) finish<PT, GT, MT, S8>(raw[u & 1], t, f, b, lane);
+    }
+    if ((c0 + kAdamChunk) <= full) return;
+#pragma unroll 1
+    for (int64_t b = b0; b < c0 + kAdamChunk && b * kAdamBlock < t.n; b += kWarps)
+        if (b >= full) block_by_values<PT, GT, MT, S8>(t, f, b, lane);
+}
 
 template <int T>
 struct AdamTable {
@@ -259,7 +321,7 @@ __device__ __forceinline__ int find_tensor(const int* first, int count, int b) {
 }
 
 template <class PT, class GT, bool S8, int T>
-__global__ void __launch_bounds__(kThreadsOp)
+__global__ void __launch_bounds__(kThreadsOp, S8 ? 3 : 2)
 k_adamw(const __grid_constant__ AdamTable<T> a) {
     AdamCoef c = a.c;
     if (a.d_step) {
@@ -278,13 +340,12 @@ k_adamw(const __grid_constant__ AdamTable<T> a) {
     TensorView t{a.p[k], a.g[k], a.m[k], a.v[k], nullptr, nullptr, a.n[k], true};
     if (S8) { t.ms = a.ms[k]; t.vs = a.vs[k]; }
     if (t.n < 0) { t.n = -1 - t.n; t.wide = false; }
-    const int64_t b0 = (int64_t)(blockIdx.x - a.first[k]) * kAdamChunk + (threadIdx.x >> 5) * kAdamU;
-    if (b0 * kAdamBlock < t.n) adamw_blocks<PT, GT, S8, kAdamU>(t, c, gscale, b0, threadIdx.x & 31);
+    adamw_chunk<PT, GT, S8>(t, factors<S8>(c, gscale), (int64_t)(blockIdx.x - a.first[k]) * kAdamChunk);
 }
 
 // The engine's rows.  grid = (chunks of a row, events)
 template <bool S8>
-__global__ void __launch_bounds__(kThreadsOp)
+__global__ void __launch_bounds__(kThreadsOp, S8 ? 3 : 2)
 k_adamw_rows(AdamRows r, AdamCoef c) {
     const EvDesc e = r.ev[blockIdx.y];
     const float2 f = r.factor[e.stamp - 1];
@@ -298,13 +359,12 @@ k_adamw_rows(AdamRows r, AdamCoef c) {
     } else {
         t.m = (float*)r.m + row; t.v = (float*)r.v + row;
     }
-    const int64_t b0 = (int64_t)blockIdx.x * kAdamChunk + (threadIdx.x >> 5) * kAdamU;
-    if (b0 * kAdamBlock < t.n) adamw_blocks<float, float, S8, kAdamU>(t, c, 1.f, b0, threadIdx.x & 31);
+    adamw_chunk<float, float, S8>(t, factors<S8>(c, 1.f), (int64_t)blockIdx.x * kAdamChunk);
 }
 
 // ---- gradient norm ----------------------------------------------------------------------------------
-constexpr int kNormU = 4;                                   // quads of a thread in flight
-constexpr int kNormChunk = kThreadsOp * 4 * kNormU;         // values per chunk
+constexpr int kNormU = 4;                                   // 16-byte loads of a thread in flight
+constexpr int kNormBytes = kThreadsOp * 16 * kNormU;        // bytes of a chunk
 constexpr int kNormParts = RFAST_GRAD_NORM_WORKSPACE / 8;   // partial sums that the workspace holds
 constexpr int kNormGrid = 148 * 6;
 
@@ -319,15 +379,24 @@ struct NormTable {
 
 // Sum of the squares of eight values.  In 32 bits the squares of values beyond 1e19 overflow and
 // those below 1e-19 lose digits; such groups (and those of zeros) are summed in 64 bits.
-__device__ __forceinline__ double square_sum(float4 a, float4 b) {
-    float s = a.x * a.x;
-    s = fmaf(a.y, a.y, s); s = fmaf(a.z, a.z, s); s = fmaf(a.w, a.w, s);
-    s = fmaf(b.x, b.x, s); s = fmaf(b.y, b.y, s); s = fmaf(b.z, b.z, s); s = fmaf(b.w, b.w, s);
+__device__ __forceinline__ double square_sum(const float (&v)[8]) {
+    float s = v[0] * v[0];
+#pragma unroll
+    for (int k = 1; k < 8; ++k) s = fmaf(v[k], v[k], s);
     if (s > 1e-25f && s < 1e37f) return (double)s;
-    const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
     double d = 0.0;
+#pragma unroll
     for (int k = 0; k < 8; ++k) d = fma((double)v[k], (double)v[k], d);
     return d;
+}
+__device__ __forceinline__ void unpack_pair(uint4 a, uint4 b, const float*, float (&x)[8], float (&)[8]) {   // 8 values, the rest unused
+    x[0] = __uint_as_float(a.x); x[1] = __uint_as_float(a.y); x[2] = __uint_as_float(a.z); x[3] = __uint_as_float(a.w);
+    x[4] = __uint_as_float(b.x); x[5] = __uint_as_float(b.y); x[6] = __uint_as_float(b.z); x[7] = __uint_as_float(b.w);
+}
+template <class T>
+__device__ __forceinline__ void unpack_pair(uint4 a, uint4 b, const T* t, float (&x)[8], float (&y)[8]) {
+    unpack2(a.x, t, x); unpack2(a.y, t, x + 2); unpack2(a.z, t, x + 4); unpack2(a.w, t, x + 6);
+    unpack2(b.x, t, y); unpack2(b.y, t, y + 2); unpack2(b.z, t, y + 4); unpack2(b.w, t, y + 6);
 }
 
 __device__ __forceinline__ double block_sum(double v, double* sh) {      // fixed tree; the result in thread 0
@@ -362,12 +431,29 @@ k_grad_norm(const __grid_constant__ NormTable<T> a) {
         const bool wide = n >= 0;
         if (!wide) n = -1 - n;
         const GT* g = (const GT*)a.g[k];
-        const int64_t i0 = (ch - a.first[k]) * kNormChunk + threadIdx.x * 4;
-        float4 q[kNormU];
+        constexpr int kPer = kNormBytes / (int)sizeof(GT);  // values of a chunk
+        const int64_t i0 = (ch - a.first[k]) * kPer;
+        if (wide && i0 + kPer <= n) {
+            const uint4* src = reinterpret_cast<const uint4*>(g + i0) + threadIdx.x;
+            uint4 q[kNormU];
 #pragma unroll
-        for (int u = 0; u < kNormU; ++u) q[u] = load4(g, i0 + (int64_t)u * kThreadsOp * 4, n, wide);
+            for (int u = 0; u < kNormU; ++u) q[u] = __ldcs(src + u * kThreadsOp);
 #pragma unroll
-        for (int u = 0; u < kNormU; u += 2) sum += square_sum(q[u], q[u + 1]);
+            for (int u = 0; u < kNormU; u += 2) {
+                float x[8], y[8];
+                unpack_pair(q[u], q[u + 1], (const GT*)nullptr, x, y);
+                sum += square_sum(x);
+                if (sizeof(GT) == 2) sum += square_sum(y);
+            }
+        } else {                                            // the end of a tensor, or a misaligned one
+            const int64_t end = i0 + kPer < n ? i0 + kPer : n;
+            for (int64_t i = i0 + threadIdx.x; i < end; i += 8 * kThreadsOp) {
+                float x[8];
+#pragma unroll
+                for (int u = 0; u < 8; ++u) x[u] = i + u * kThreadsOp < end ? to_f32(g[i + u * kThreadsOp]) : 0.f;
+                sum += square_sum(x);
+            }
+        }
     }
     const double s = block_sum(sum, sh);
     if (threadIdx.x == 0) a.part[blockIdx.x] = s;
@@ -458,9 +544,10 @@ cudaError_t norm_span(const int64_t* numel, const void* const* grad, int k0, int
         const int64_t n = numel[k];
         if (n == 0) continue;
         t.g[q] = grad[k];
-        t.n[q] = (uintptr_t)grad[k] % (4 * sizeof(GT)) == 0 ? n : -1 - n;
+        t.n[q] = (uintptr_t)grad[k] % 16 == 0 ? n : -1 - n;
         t.first[q] = chunks;
-        chunks += (n + kNormChunk - 1) / kNormChunk;
+        const int64_t per = kNormBytes / (int64_t)sizeof(GT);
+        chunks += (n + per - 1) / per;
         ++q;
     }
     *blocks_out = 0;
@@ -513,7 +600,7 @@ int check_device_pointer(const void* p, const char* what, char* err, size_t err_
 AdamCoef adamw_coef(double lr, double beta1, double beta2, double eps, double weight_decay, int64_t t) {
     AdamCoef c;
     c.beta1 = (float)beta1; c.omb1 = (float)(1.0 - beta1);
-    c.beta2 = (float)beta2; c.omb2 = (float)(1.0 - beta2);
+    c.beta2 = (float)beta2; c.root_beta2 = (float)std::sqrt(beta2); c.root_omb2 = (float)std::sqrt(1.0 - beta2);
     c.eps = (float)eps; c.keep = (float)(1.0 - lr * weight_decay);
     c.step = (float)(lr / (1.0 - std::pow(beta1, (double)t)));
     c.root = (float)(1.0 / std::sqrt(1.0 - std::pow(beta2, (double)t)));

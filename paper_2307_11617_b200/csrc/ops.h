@@ -17,7 +17,8 @@ constexpr int kAdamBlock = RFAST_ADAMW_BLOCK;    // values that share a scale of
 
 // Scalars of one AdamW step, formed on the host in 64 bits and rounded once.
 struct AdamCoef {
-    float beta1, omb1, beta2, omb2;    // omb = 1 - beta
+    float beta1, omb1, beta2;          // omb = 1 - beta
+    float root_beta2, root_omb2;       // square roots of beta2 and 1 - beta2
     float eps, keep;                   // keep = 1 - lr * weight_decay
     float step;                        // lr / (1 - beta1^t)
     float root;                        // 1 / sqrt(1 - beta2^t)
