@@ -491,10 +491,10 @@ int rfast_grad_norm(int32_t n_tensors, int32_t grad_type, const int64_t* numel, 
  *   consecutive values of a tensor, the last one shorter; its scale is max(largest magnitude / 448, 2^-100)
  *   in fp32, m_scale and v_scale hold ceil(numel / RFAST_ADAMW_BLOCK) of them per tensor, and a
  *   value is code * scale.  Codes are nearest values, ties to even; a positive sqrt(v) keeps at least the
- *   smallest positive code, so that no first moment meets a denominator of eps alone.  All bytes zero
- *   are moments of zero.  A NaN or infinite gradient leaves its whole block's moments NaN or infinite.
- * Tensors may not overlap one another.  Addresses are aligned to their type only; tensors whose
- * addresses are aligned to four values are read and written in quads. */
+ *   smallest positive code, so that no first moment meets a denominator of eps alone (second moments
+ *   below 2^-126 count as zero).  All bytes zero are moments of zero.  A NaN or infinite gradient leaves its whole block's moments NaN or infinite.
+ * Tensors may not overlap one another.  Addresses need to be aligned to their type only; tensors whose
+ * addresses are all multiples of 16 bytes are the fast ones. */
 #define RFAST_ADAMW_BLOCK 256
 typedef struct rfast_adamw {
     int32_t n_tensors;
