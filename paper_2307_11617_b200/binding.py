@@ -413,6 +413,13 @@ def _list(values, n=None, what="list"):
     return a
 
 
+def _host(a):
+    """Address of a non-empty host array's data (None for an empty one); a.ctypes.data takes three times as long."""
+    if not a.size:
+        return None
+    return C.addressof(C.c_char.from_buffer(a)) if a.flags.writeable else a.ctypes.data
+
+
 def _op(rc, err):
     if rc != OK:
         raise RFastError(rc, err.value.decode())
@@ -427,7 +434,7 @@ def rfast_grad_norm(grad, numel, max_norm: float, d_norm: int, d_scale: int, wor
     n = _list(numel, None, "numel")
     g = _list(grad, len(n), "grad")
     err = C.create_string_buffer(256)
-    _op(lib().rfast_grad_norm(len(n), _type(grad_type), n.ctypes.data, g.ctypes.data, max_norm, d_norm or None, d_scale or None,
+    _op(lib().rfast_grad_norm(len(n), _type(grad_type), _host(n), _host(g), max_norm, d_norm or None, d_scale or None,
                               workspace or None, workspace_bytes, cuda_stream or None, err, 256), err)
 
 
@@ -449,8 +456,8 @@ def rfast_adamw_step(param, grad, m, v, numel, step: int = 0, lr: float = 1e-3, 
     if m_scale is not None:
         bits = 8
         lists += [_list(m_scale, k, "m_scale"), _list(v_scale, k, "v_scale")]
-        scales = [a.ctypes.data for a in lists[4:]]
-    args = _AdamW(k, _type(param_type), _type(grad_type), bits, n.ctypes.data, *[a.ctypes.data for a in lists[:4]], *scales,
+        scales = [_host(a) for a in lists[4:]]
+    args = _AdamW(k, _type(param_type), _type(grad_type), bits, _host(n), *[_host(a) for a in lists[:4]], *scales,
                   lr, beta1, beta2, eps, weight_decay, step, d_step or None, d_grad_scale or None)
     err = C.create_string_buffer(256)
     _op(lib().rfast_adamw_step(C.byref(args), cuda_stream or None, err, 256), err)
