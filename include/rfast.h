@@ -514,6 +514,45 @@ typedef struct rfast_adamw {
 } rfast_adamw;
 int rfast_adamw_step(const rfast_adamw* a, void* cuda_stream, char* err, size_t err_len);
 
+/* Group norm with an activation, channels last.  x is [samples][positions][channels] (positions: height
+ * x width, or 1 for the rows of a hidden layer); the channels form `groups` groups of neighbours, and
+ * for every sample and group, over its M = positions * channels / groups values,
+ *     mean = sum x / M,  rstd = 1 / sqrt(sum (x - mean)^2 / M + eps)
+ *     h = (x - mean) rstd,  u = gamma h + beta,  y = act(u)
+ *     act: u | max(u, 0) | u / (1 + exp(-u))
+ * gamma and beta are fp32 [samples / samples_per_set][channels]: samples_per_set consecutive samples
+ * share a row (all of them: one layer; a worker's rows: one layer per worker).  mean and rstd are
+ * written, fp32 [samples][groups]; the backward pass wants them.  Sums and statistics are held in
+ * 32 bits, y is rounded once to its type; variances come from deviations, not from a difference
+ * of squares.  A NaN or infinity leaves NaN in its sample's group and nowhere else.
+ * Strides are those of a sample and of a position, in elements (two numbers; NULL: contiguous);
+ * channels are neighbours.  Read operands may overlap themselves (a stride of 0 repeats), written
+ * ones may not; y may be x, dx may be x or dy, with the same strides.  Addresses and strides in
+ * multiples of 16 bytes are the fast ones.  A group may have 8192 channels at most.
+ *
+ * Backward, from dy and the forward pass's x, mean, rstd (act'(0) = 0 for max(u, 0)):
+ *     du = dy act'(u);  dbeta = sum du, dgamma = sum du h over the samples of a set (fp32)
+ *     dx = rstd (gamma du - sum(gamma du) / M - h sum(gamma du h) / M)
+ * workspace: rfast_group_norm_workspace(shape, 1) bytes of DEVICE memory, aligned to 4 (the forward
+ * pass needs rfast_group_norm_workspace(shape, 0), which may be 0); its size depends on the shape
+ * alone.  No positions: nothing is normalised, dgamma and dbeta are zero. */
+enum { RFAST_ACT_NONE = 0, RFAST_ACT_RELU = 1, RFAST_ACT_SILU = 2 };
+typedef struct rfast_gn_shape {
+    int64_t samples, positions;
+    int32_t channels, groups;
+    int64_t samples_per_set;
+    int32_t type;                      /* RFAST_TYPE_*, of x, y, dy and dx */
+    int32_t act;                       /* RFAST_ACT_* */
+} rfast_gn_shape;
+int64_t rfast_group_norm_workspace(const rfast_gn_shape* shape, int backward);   /* bytes, or a negative status */
+int rfast_group_norm(const rfast_gn_shape* shape, const void* d_x, const int64_t* x_strides, const float* d_gamma,
+                     const float* d_beta, float eps, void* d_y, const int64_t* y_strides, float* d_mean, float* d_rstd,
+                     void* workspace, size_t workspace_bytes, void* cuda_stream, char* err, size_t err_len);
+int rfast_group_norm_backward(const rfast_gn_shape* shape, const void* d_dy, const int64_t* dy_strides, const void* d_x,
+                              const int64_t* x_strides, const float* d_gamma, const float* d_beta, const float* d_mean,
+                              const float* d_rstd, void* d_dx, const int64_t* dx_strides, float* d_dgamma, float* d_dbeta,
+                              void* workspace, size_t workspace_bytes, void* cuda_stream, char* err, size_t err_len);
+
 void        rfast_destroy(rfast_ctx* ctx);
 const char* rfast_last_error(const rfast_ctx* ctx);   /* ctx may be NULL: last create error */
 const char* rfast_version(void);

@@ -62,6 +62,7 @@ class _Schedule(C.Structure):
 
 
 TYPE_IDS = {"f32": 0, "bf16": 1, "f16": 2}
+ACT_IDS = {"none": 0, "relu": 1, "silu": 2}
 GRAD_NORM_WORKSPACE = 16384
 ADAMW_BLOCK = 256
 
@@ -72,6 +73,11 @@ class _AdamW(C.Structure):
                 ("m_scale", C.c_void_p), ("v_scale", C.c_void_p),
                 ("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("weight_decay", C.c_double),
                 ("step", C.c_int64), ("d_step", C.c_void_p), ("d_grad_scale", C.c_void_p)]
+
+
+class _GnShape(C.Structure):
+    _fields_ = [("samples", C.c_int64), ("positions", C.c_int64), ("channels", C.c_int32), ("groups", C.c_int32),
+                ("samples_per_set", C.c_int64), ("type", C.c_int32), ("act", C.c_int32)]
 
 
 _lib = None
@@ -120,6 +126,11 @@ def lib():
                                                C.c_void_p, C.c_char_p, C.c_size_t]
         L.rfast_grad_norm.argtypes = [C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_float, C.c_void_p, C.c_void_p,
                                       C.c_void_p, C.c_size_t, C.c_void_p, C.c_char_p, C.c_size_t]
+        L.rfast_group_norm_workspace.argtypes = [C.POINTER(_GnShape), C.c_int]
+        L.rfast_group_norm_workspace.restype = C.c_int64
+        L.rfast_group_norm.argtypes = [C.POINTER(_GnShape), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_float, C.c_void_p, C.c_void_p,
+                                       C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p, C.c_char_p, C.c_size_t]
+        L.rfast_group_norm_backward.argtypes = [C.POINTER(_GnShape)] + [C.c_void_p] * 13 + [C.c_size_t, C.c_void_p, C.c_char_p, C.c_size_t]
         L.rfast_adamw_step.argtypes = [C.POINTER(_AdamW), C.c_void_p, C.c_char_p, C.c_size_t]
         _lib = L
     return _lib
@@ -461,6 +472,53 @@ def rfast_adamw_step(param, grad, m, v, numel, step: int = 0, lr: float = 1e-3, 
                   lr, beta1, beta2, eps, weight_decay, step, d_step or None, d_grad_scale or None)
     err = C.create_string_buffer(256)
     _op(lib().rfast_adamw_step(C.byref(args), cuda_stream or None, err, 256), err)
+
+
+def _gn_shape(samples, positions, channels, groups, samples_per_set, type, act):
+    if act not in ACT_IDS:
+        raise ValueError(f"unknown activation {act!r}: one of {', '.join(ACT_IDS)}")
+    return _GnShape(samples, positions, channels, groups, max(samples, 1) if samples_per_set is None else samples_per_set, _type(type), ACT_IDS[act])
+
+
+def _strides(s):
+    return None if s is None else (C.c_int64 * 2)(*s)
+
+
+def rfast_group_norm_workspace(samples: int, positions: int, channels: int, groups: int, samples_per_set=None, type: str = "f32",
+                               act: str = "none", backward: bool = False) -> int:
+    """Bytes of DEVICE workspace that a call of this shape needs."""
+    need = lib().rfast_group_norm_workspace(C.byref(_gn_shape(samples, positions, channels, groups, samples_per_set, type, act)), 1 if backward else 0)
+    if need < 0:
+        raise RFastError(int(need), "rfast_group_norm_workspace: the shape is not valid")
+    return int(need)
+
+
+def rfast_group_norm(x: int, gamma: int, beta: int, y: int, mean: int, rstd: int, samples: int, positions: int, channels: int, groups: int,
+                     samples_per_set=None, eps: float = 1e-5, act: str = "none", type: str = "f32", x_strides=None, y_strides=None,
+                     workspace: int = 0, workspace_bytes: int = 0, cuda_stream: int = 0) -> None:
+    """Group norm with an activation, channels last: y = act(gamma (x - mean) rstd + beta) over x
+    [samples][positions][channels].  All addresses are DEVICE addresses; x and y have `type`, gamma, beta
+    [samples / samples_per_set][channels] and the results mean, rstd [samples][groups] are fp32
+    (samples_per_set None: one row for all samples).  Strides: (sample, position) in elements, None for
+    contiguous.  Enqueued on cuda_stream."""
+    shape = _gn_shape(samples, positions, channels, groups, samples_per_set, type, act)
+    err = C.create_string_buffer(256)
+    _op(lib().rfast_group_norm(C.byref(shape), x or None, _strides(x_strides), gamma or None, beta or None, eps, y or None, _strides(y_strides),
+                               mean or None, rstd or None, workspace or None, workspace_bytes, cuda_stream or None, err, 256), err)
+
+
+def rfast_group_norm_backward(dy: int, x: int, gamma: int, beta: int, mean: int, rstd: int, dx: int, dgamma: int, dbeta: int, samples: int,
+                              positions: int, channels: int, groups: int, samples_per_set=None, act: str = "none", type: str = "f32",
+                              dy_strides=None, x_strides=None, dx_strides=None, workspace: int = 0, workspace_bytes: int = 0,
+                              cuda_stream: int = 0) -> None:
+    """Gradients of rfast_group_norm: dx (of `type`), dgamma and dbeta (fp32, one row per set) from dy and
+    the forward pass's x, mean and rstd.  workspace: rfast_group_norm_workspace(..., backward=True) bytes
+    that no other running call uses.  Enqueued on cuda_stream."""
+    shape = _gn_shape(samples, positions, channels, groups, samples_per_set, type, act)
+    err = C.create_string_buffer(256)
+    _op(lib().rfast_group_norm_backward(C.byref(shape), dy or None, _strides(dy_strides), x or None, _strides(x_strides), gamma or None, beta or None,
+                                        mean or None, rstd or None, dx or None, _strides(dx_strides), dgamma or None, dbeta or None,
+                                        workspace or None, workspace_bytes, cuda_stream or None, err, 256), err)
 
 
 class Engine:

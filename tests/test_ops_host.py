@@ -109,3 +109,92 @@ def test_constants_of_the_binding_are_the_headers(rfast_lib, repo_root):
     text = open(os.path.join(repo_root, "include", "rfast.h")).read()
     assert int(re.search(r"#define RFAST_GRAD_NORM_WORKSPACE (\d+)", text).group(1)) == B.GRAD_NORM_WORKSPACE
     assert int(re.search(r"#define RFAST_ADAMW_BLOCK (\d+)", text).group(1)) == B.ADAMW_BLOCK
+
+
+# ---- group norm --------------------------------------------------------------------------------------
+SHAPE = dict(samples=4, positions=6, channels=12, groups=3)
+
+
+@pytest.mark.parametrize("text,kw", [
+    ("samples and positions", dict(samples=-1)),
+    ("samples and positions", dict(positions=1 << 31)),
+    ("multiple of groups", dict(groups=5)),
+    ("multiple of groups", dict(groups=0)),
+    ("multiple of groups", dict(channels=0)),
+    ("8192 channels", dict(channels=8193, groups=1)),
+    ("2^24 channels", dict(channels=1 << 25, groups=1 << 25)),
+    ("multiple of samples_per_set", dict(samples_per_set=3)),
+    ("multiple of samples_per_set", dict(samples_per_set=0)),
+])
+def test_group_norm_refuses_shapes(rfast_lib, text, kw):
+    import paper_2307_11617_b200 as pkg
+    from paper_2307_11617_b200.binding import EINVAL, RFastError
+    shape = {**SHAPE, **kw}
+    _refused(text, pkg.rfast_group_norm, A, A, A, A, A, A, **shape)
+    _refused(text, pkg.rfast_group_norm_backward, A, A, A, A, A, A, A, A, A, workspace=A, workspace_bytes=1 << 30, **shape)
+    with pytest.raises(RFastError) as ei:
+        pkg.rfast_group_norm_workspace(backward=True, **shape)
+    assert ei.value.code == EINVAL
+
+
+@pytest.mark.parametrize("text,kw", [
+    ("eps must be", dict(eps=0.0)), ("eps must be", dict(eps=float("nan"))), ("eps must be", dict(eps=-1.0)),
+    ("x is null", dict(x=0)), ("beta is null", dict(beta=0)), ("rstd is null", dict(rstd=0)),
+    ("x is not aligned", dict(x=A + 2)), ("y is not aligned", dict(y=A + 1, type="bf16")), ("gamma is not aligned", dict(gamma=A + 2, type="bf16")),
+    ("stride of x is negative", dict(x_strides=(72, -12))), ("strides of y", dict(y_strides=(72, 11))),
+    ("strides of y", dict(y_strides=(71, 12))), ("strides of y", dict(y_strides=(12, 47))), ("strides of y", dict(y_strides=(0, 12))),
+])
+def test_group_norm_refuses_operands(rfast_lib, text, kw):
+    import paper_2307_11617_b200 as pkg
+    _refused(text, pkg.rfast_group_norm, **{**dict(x=A, gamma=A, beta=A, y=A, mean=A, rstd=A), **SHAPE, **kw})
+
+
+@pytest.mark.parametrize("text,kw", [
+    ("dy is null", dict(dy=0)), ("dgamma is null", dict(dgamma=0)), ("mean is null", dict(mean=0)), ("dx is not aligned", dict(dx=A + 2)),
+    ("workspace needs", dict(workspace_bytes=0)), ("workspace needs", dict(workspace=0)), ("workspace needs", dict(workspace=A + 2)),
+    ("strides of dx", dict(dx_strides=(60, 12))), ("stride of dy is negative", dict(dy_strides=(-72, 12))),
+])
+def test_group_norm_backward_refuses_operands(rfast_lib, text, kw):
+    import paper_2307_11617_b200 as pkg
+    base = dict(dy=A, x=A, gamma=A, beta=A, mean=A, rstd=A, dx=A, dgamma=A, dbeta=A, workspace=A, workspace_bytes=1 << 30)
+    _refused(text, pkg.rfast_group_norm_backward, **{**base, **SHAPE, **kw})
+
+
+def test_group_norm_of_nothing_needs_no_device(rfast_lib):
+    import paper_2307_11617_b200 as pkg
+    pkg.rfast_group_norm(0, 0, 0, 0, 0, 0, **{**SHAPE, "samples": 0})
+    pkg.rfast_group_norm(0, 0, 0, 0, 0, 0, **{**SHAPE, "positions": 0})
+    pkg.rfast_group_norm_backward(0, 0, 0, 0, 0, 0, 0, 0, 0, **{**SHAPE, "samples": 0})
+    assert pkg.rfast_group_norm_workspace(**SHAPE) == 0
+    assert pkg.rfast_group_norm_workspace(backward=True, **SHAPE) > 0
+
+
+def test_unknown_names_are_refused(rfast_lib):
+    import paper_2307_11617_b200 as pkg
+    with pytest.raises(ValueError):
+        pkg.rfast_group_norm(A, A, A, A, A, A, act="gelu", **SHAPE)
+    with pytest.raises(ValueError):
+        pkg.rfast_group_norm(A, A, A, A, A, A, type="f64", **SHAPE)
+
+
+def test_group_norm_gradient_formula_against_differences():
+    """The backward formula that the GPU tests compare with, against central differences of the forward one."""
+    from group_norm_reference import backward, forward
+    rng = np.random.default_rng(0)
+    n, s, c, g, sets = 4, 5, 6, 3, 2
+    for act in ("none", "relu", "silu"):
+        x, dy = rng.standard_normal((n, s, c)), rng.standard_normal((n, s, c))
+        gamma, beta = 1 + 0.3 * rng.standard_normal((sets, c)), 0.3 * rng.standard_normal((sets, c))
+        y, mean, rstd, _ = forward(x, gamma, beta, g, 1e-3, act)
+        dx, dgamma, dbeta = backward(dy, x, gamma, beta, mean, rstd, g, act)[:3]
+        f = lambda *a: (dy * forward(*a, g, 1e-3, act)[0]).sum()  # noqa: E731
+        for got, k in ((dx, 0), (dgamma, 1), (dbeta, 2)):
+            args = [x, gamma, beta]
+            for at in np.ndindex(*args[k].shape):
+                h = np.zeros_like(args[k])
+                h[at] = 1e-6
+                up, down = [a.copy() for a in args], [a.copy() for a in args]
+                up[k] += h
+                down[k] -= h
+                # differences of step 1e-6 carry 1e-6^2 of curvature and 1e-16 / 1e-6 of rounding
+                assert abs((f(*up) - f(*down)) / 2e-6 - got[at]) < 1e-7 * (1 + abs(got[at])) * 10, (act, k, at)
