@@ -31,24 +31,16 @@ namespace {
 
 constexpr int kT = 256;                                    // threads per block
 
-__device__ __forceinline__ float to_f32(float v) { return v; }
-__device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
-__device__ __forceinline__ float to_f32(__half v) { return __half2float(v); }
-__device__ __forceinline__ void from_f32(float* t, float v) { *t = v; }
-__device__ __forceinline__ void from_f32(__nv_bfloat16* t, float v) { *t = __float2bfloat16_rn(v); }
-__device__ __forceinline__ void from_f32(__half* t, float v) { *t = __float2half_rn(v); }
-
 template <int BYTES> struct Word;
 template <> struct Word<16> { typedef uint4 type; };
 template <> struct Word<4> { typedef uint32_t type; };
 template <> struct Word<2> { typedef uint16_t type; };
 
-// V neighbouring channels of one position
+// V neighbouring channels of one position, as they lie in memory
 template <class T, int V>
 struct Vec {
     typedef typename Word<(int)sizeof(T) * V>::type W;
-    union { W w; T e[V]; };
-    __device__ __forceinline__ Vec() {}
+    W w;
 };
 template <class T, int V>
 __device__ __forceinline__ Vec<T, V> load_vec(const T* p) {
@@ -56,12 +48,51 @@ __device__ __forceinline__ Vec<T, V> load_vec(const T* p) {
     v.w = *reinterpret_cast<const typename Vec<T, V>::W*>(p);
     return v;
 }
-template <class T, int V>
-__device__ __forceinline__ void store_vec(T* p, const float (&f)[V]) {
-    Vec<T, V> v;
-#pragma unroll
-    for (int k = 0; k < V; ++k) from_f32(&v.e[k], f[k]);
-    __stcs(reinterpret_cast<typename Vec<T, V>::W*>(p), v.w);
+__device__ __forceinline__ void widen2(uint32_t r, const __nv_bfloat16*, float* f) {
+    f[0] = __uint_as_float(r << 16);
+    f[1] = __uint_as_float(r & 0xffff0000u);
+}
+__device__ __forceinline__ void widen2(uint32_t r, const __half*, float* f) {
+    const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&r));
+    f[0] = a.x; f[1] = a.y;
+}
+__device__ __forceinline__ void widen(Vec<float, 4> v, float (&f)[4]) {
+    f[0] = __uint_as_float(v.w.x); f[1] = __uint_as_float(v.w.y); f[2] = __uint_as_float(v.w.z); f[3] = __uint_as_float(v.w.w);
+}
+__device__ __forceinline__ void widen(Vec<float, 1> v, float (&f)[1]) { f[0] = __uint_as_float(v.w); }
+template <class T>
+__device__ __forceinline__ void widen(Vec<T, 8> v, float (&f)[8]) {
+    const T* t = nullptr;
+    widen2(v.w.x, t, f); widen2(v.w.y, t, f + 2); widen2(v.w.z, t, f + 4); widen2(v.w.w, t, f + 6);
+}
+template <class T>
+__device__ __forceinline__ void widen(Vec<T, 2> v, float (&f)[2]) { widen2(v.w, (const T*)nullptr, f); }
+template <class T>
+__device__ __forceinline__ void widen(Vec<T, 1> v, float (&f)[1]) {
+    float t[2];
+    widen2((uint32_t)v.w, (const T*)nullptr, t);
+    f[0] = t[0];
+}
+__device__ __forceinline__ uint32_t narrow2(const float* f, const __nv_bfloat16*) {
+    const __nv_bfloat162 a = __floats2bfloat162_rn(f[0], f[1]);
+    return *reinterpret_cast<const uint32_t*>(&a);
+}
+__device__ __forceinline__ uint32_t narrow2(const float* f, const __half*) {
+    const __half2 a = __floats2half2_rn(f[0], f[1]);
+    return *reinterpret_cast<const uint32_t*>(&a);
+}
+__device__ __forceinline__ void store_vec(float* p, const float (&f)[4]) { __stcs(reinterpret_cast<float4*>(p), make_float4(f[0], f[1], f[2], f[3])); }
+__device__ __forceinline__ void store_vec(float* p, const float (&f)[1]) { __stcs(p, f[0]); }
+template <class T>
+__device__ __forceinline__ void store_vec(T* p, const float (&f)[8]) {
+    __stcs(reinterpret_cast<uint4*>(p), make_uint4(narrow2(f, p), narrow2(f + 2, p), narrow2(f + 4, p), narrow2(f + 6, p)));
+}
+template <class T>
+__device__ __forceinline__ void store_vec(T* p, const float (&f)[2]) { __stcs(reinterpret_cast<uint32_t*>(p), narrow2(f, p)); }
+template <class T>
+__device__ __forceinline__ void store_vec(T* p, const float (&f)[1]) {
+    const float t[2] = {f[0], 0.f};
+    __stcs(reinterpret_cast<unsigned short*>(p), (unsigned short)narrow2(t, p));
 }
 template <int BYTES>
 __device__ __forceinline__ void copy_async(void* dst, const void* src) {
@@ -71,8 +102,30 @@ __device__ __forceinline__ void copy_async(void* dst, const void* src) {
 }
 __device__ __forceinline__ void copies_landed() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
-// 1 / (1 + exp(-u)): the exponential's argument is rounded once, so the result is good to about 2^-23
-__device__ __forceinline__ float sigmoid_of(float u) { return __fdividef(1.f, 1.f + __expf(-u)); }
+// 1 / (1 + exp(-u)).  2^t and the reciprocal are the hardware's (2 ulp and 1 ulp), t is rounded once: the result is good
+// to about 2^-23.  u = -inf gives 0.
+__device__ __forceinline__ float sigmoid_of(float u) {
+    float e, q;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(u * -1.4426950408889634f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(q) : "f"(1.f + e));
+    return q;
+}
+
+// Rows 0 .. cnt of a thread, R at a time: all loads of a batch go out before the first row is worked on (a
+// store in between would hold later loads back, the operands being allowed to coincide).
+template <int R, class Row, class Load, class Use>
+__device__ __forceinline__ void walk(int cnt, Load load, Use use) {
+    int r = 0;
+    for (; r + R <= cnt; r += R) {
+        Row q[R];
+#pragma unroll
+        for (int k = 0; k < R; ++k) q[k] = load(r + k);
+#pragma unroll
+        for (int k = 0; k < R; ++k) use(q[k], r + k);
+    }
+#pragma unroll 1
+    for (; r < cnt; ++r) use(load(r), r);
+}
 
 // ---- geometry, chosen on the host -------------------------------------------------------------------
 struct GnShape {
@@ -104,6 +157,7 @@ struct GnArgs {
     void* out;                         // y, dx
     int64_t xn, xs, dn, ds, on, os;    // strides of a sample and of a position, in elements
     const float *gamma, *beta;
+    bool quads;                        // their addresses and stride allow 16-byte loads
     int64_t affine_stride;
     const int* set_row;                // row of gamma / beta of a set, or null: the set itself
     int set_row_stride;
@@ -132,6 +186,37 @@ __device__ __forceinline__ Seat seat_of(const GnPlan& p) {
     return s;
 }
 
+// scale or shift of V neighbouring channels
+template <int V>
+__device__ __forceinline__ void affine_of(const float* p, bool quads, float (&f)[V]) {
+    if constexpr (V % 4 == 0) {
+        if (quads) {
+#pragma unroll
+            for (int k = 0; k < V; k += 4) {
+                const float4 q = *reinterpret_cast<const float4*>(p + k);
+                f[k] = q.x; f[k + 1] = q.y; f[k + 2] = q.z; f[k + 3] = q.w;
+            }
+            return;
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < V; ++k) f[k] = p[k];
+}
+// groups of V neighbouring channels from channel c on: one (WHOLE) or one per channel
+template <int V, bool WHOLE>
+__device__ __forceinline__ void groups_of(int c, int cg, int (&g)[WHOLE ? 1 : V]) {
+    int q = c / cg;
+    g[0] = q;
+    if constexpr (!WHOLE) {
+        int rest = c - q * cg;
+#pragma unroll
+        for (int v = 1; v < V; ++v) {
+            if (++rest == cg) { rest = 0; ++q; }
+            g[v] = q;
+        }
+    }
+}
+
 // Sum over L neighbouring lanes (L a power of two), all lanes of the warp taking part.
 __device__ __forceinline__ float team_sum(float v, int L) {
     for (int o = L >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
@@ -145,18 +230,18 @@ __device__ __forceinline__ int team_size(int entries) {
 
 // ---- forward --------------------------------------------------------------------------------------
 // grid = (items * cluster, slabs), clusters along x
-template <class T, int V, bool BUF>
-__global__ void __launch_bounds__(kT)
+template <class T, int V, bool WHOLE, bool BUF>
+__global__ void __launch_bounds__(kT, BUF && WHOLE ? 4 : 3)
 k_gn_forward(const __grid_constant__ GnArgs a) {
     extern __shared__ __align__(16) uint8_t smem[];
     typedef Vec<T, V> X;
     const GnShape& s = a.s;
     const GnPlan& p = a.p;
-    const bool whole = s.Cg % V == 0;                       // an access stays inside a group
+    constexpr int kBatch = 4, kGv = WHOLE ? 1 : V, kAcc = WHOLE ? (V < 4 ? V : 4) : V;
     X* buf = reinterpret_cast<X*>(smem);
-    // per thread (whole) or per thread and channel: count, mean, sum of squared deviations
+    // per thread (WHOLE: an access stays inside a group) or per thread and channel: count, mean, sum of squared deviations
     float* e_n = reinterpret_cast<float*>(smem + p.buf);
-    const int width = whole ? 1 : V;
+    constexpr int width = kGv;
     float* e_mean = e_n + kT;
     float* e_m2 = e_mean + kT * width;
     float* bins = e_m2 + kT * width;                        // [ns * gs][3], then [ns * gs][2] final
@@ -188,61 +273,64 @@ k_gn_forward(const __grid_constant__ GnArgs a) {
     float t_n = 0.f, t_mean = 0.f, t_m2 = 0.f;
     for (int j = 0; j < p.cj; ++j) {
         const int cv = me.txi + j * kT;
-        float first[V], s1[V], s2[V];
+        float first[kGv], s1[kAcc], s2[kAcc];
 #pragma unroll
-        for (int v = 0; v < V; ++v) first[v] = s1[v] = s2[v] = 0.f;
+        for (int v = 0; v < kAcc; ++v) s1[v] = s2[v] = 0.f;
+#pragma unroll
+        for (int v = 0; v < kGv; ++v) first[v] = 0.f;
         if (cnt > 0 && cv < cols) {
             const T* at = x + cv * V;
             const X* bt = buf + j * p.rpt * kT + threadIdx.x;
-            const X q0 = BUF ? bt[0] : load_vec<T, V>(at);
+            auto load = [&](int r) { return BUF ? bt[r * kT] : load_vec<T, V>(at + r * step); };
+            {
+                float f[V];
+                widen(load(0), f);
 #pragma unroll
-            for (int v = 0; v < V; ++v) first[v] = to_f32(q0.e[v]);
-#pragma unroll 4
-            for (int r = 1; r < cnt; ++r) {
-                const X q = BUF ? bt[r * kT] : load_vec<T, V>(at + r * step);
+                for (int v = 0; v < kGv; ++v) first[v] = f[v];
+            }
+            walk<kBatch, X>(cnt, load, [&](const X& q, int) {     // a first value counts as a deviation of 0
+                float f[V];
+                widen(q, f);
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
-                    const float d = to_f32(q.e[v]) - first[v];
-                    s1[v] += d;
-                    s2[v] = fmaf(d, d, s2[v]);
+                    const float d = f[v] - first[WHOLE ? 0 : v];
+                    s1[v % kAcc] += d;
+                    s2[v % kAcc] = fmaf(d, d, s2[v % kAcc]);
                 }
-            }
-            const float inv = 1.f / (float)cnt;
-            float avg = 0.f;
+            });
+            if (WHOLE) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
+                for (int v = 1; v < kAcc; ++v) { s1[0] += s1[v]; s2[0] += s2[v]; }
+            }
+            const float nn = (float)cnt * (WHOLE ? V : 1), inv = 1.f / nn;
+#pragma unroll
+            for (int v = 0; v < kGv; ++v) {
                 const float d = s1[v] * inv;
                 s2[v] = fmaxf(fmaf(-s1[v], d, s2[v]), 0.f) + (s2[v] - s2[v]);    // the second term is a NaN where there was one
-                first[v] += d;                              // now the channel's mean
+                first[v] += d;                              // now the mean
             }
-            if (whole) {
-#pragma unroll
-                for (int v = 1; v < V; ++v) avg += first[v] - first[0];
-                avg = fmaf(avg, 1.f / V, first[0]);
-                float m2 = 0.f;
-#pragma unroll
-                for (int v = 0; v < V; ++v) { const float d = first[v] - avg; m2 = fmaf(d * d, (float)cnt, m2 + s2[v]); }
-                const float nn = (float)cnt * V, d = avg - t_mean, tot = t_n + nn;
+            if (WHOLE && t_n > 0.f) {                       // a further pass over a wide group
+                const float d = first[0] - t_mean, tot = t_n + nn;
                 t_mean += d * (nn / tot);
-                t_m2 += m2 + d * d * (t_n * nn / tot);
+                t_m2 += s2[0] + d * d * (t_n * nn / tot);
                 t_n = tot;
             } else {
-                t_n = (float)cnt;
+                t_mean = first[0]; t_m2 = s2[0]; t_n = nn;
             }
         }
-        if (!whole) {                                       // a slab of several groups is never wider than the block
+        if (!WHOLE) {                                       // a slab of several groups is never wider than the block
             if (me.on && cv < cols) {
 #pragma unroll
-                for (int v = 0; v < V; ++v) { e_mean[threadIdx.x * V + v] = first[v]; e_m2[threadIdx.x * V + v] = s2[v]; }
+                for (int v = 0; v < kGv; ++v) { e_mean[threadIdx.x * V + v] = first[v]; e_m2[threadIdx.x * V + v] = s2[v]; }
             }
         }
     }
     e_n[threadIdx.x] = t_n;
-    if (whole) { e_mean[threadIdx.x] = t_mean; e_m2[threadIdx.x] = t_m2; }
+    if (WHOLE) { e_mean[threadIdx.x] = t_mean; e_m2[threadIdx.x] = t_m2; }
     __syncthreads();
     // the groups' sums over this block, a team of lanes per group
     {
-        const int unit = whole ? min(s.Cg / V, p.tx) : s.Cg;   // entries of a group in one row of threads
+        const int unit = WHOLE ? min(s.Cg / V, p.tx) : s.Cg;   // entries of a group in one row of threads
         const int entries = unit * p.tr, L = team_size(entries), lane = threadIdx.x & (L - 1);
         for (int b0 = 0; b0 < nb; b0 += kT / L) {
             const int b = b0 + threadIdx.x / L;
@@ -253,7 +341,7 @@ k_gn_forward(const __grid_constant__ GnArgs a) {
             float cn = 0.f, cm = 0.f;
             for (int q = lane; in && q < entries; q += L) {
                 const int row = q / unit, t = (sl * p.tr + row) * p.tx, u = g * unit + (q - row * unit);
-                const float k = e_n[t + (whole ? u : u / V)];
+                const float k = e_n[t + (WHOLE ? u : u / V)];
                 cn += k;
                 if (k > 0.f) cm = fmaf(k, e_mean[t * width + u] - ref, cm);
             }
@@ -263,7 +351,7 @@ k_gn_forward(const __grid_constant__ GnArgs a) {
             float m2 = 0.f;
             for (int q = lane; in && q < entries; q += L) {
                 const int row = q / unit, t = (sl * p.tr + row) * p.tx, u = g * unit + (q - row * unit);
-                const float k = e_n[t + (whole ? u : u / V)];
+                const float k = e_n[t + (WHOLE ? u : u / V)];
                 if (k > 0.f) {
                     const float d = e_mean[t * width + u] - mean;
                     m2 += fmaf(k * d, d, e_m2[t * width + u]);
@@ -313,59 +401,74 @@ k_gn_forward(const __grid_constant__ GnArgs a) {
         for (int j = 0; j < p.cj; ++j) {
             const int cv = me.txi + j * kT;
             if (cv >= cols) break;
-            float mean[V], mul[V], add[V];
+            float mean[kGv], mul[V], add[V];
+            int g[kGv];
+            groups_of<V, WHOLE>(cv * V, s.Cg, g);
+            affine_of<V>(gam + cv * V, a.quads, mul);
+            affine_of<V>(bet + cv * V, a.quads, add);
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const int c = cv * V + v, b = me.sl * gs + c / s.Cg;
-                mean[v] = fin[2 * b];
-                mul[v] = gam[c] * fin[2 * b + 1];
-                add[v] = bet[c];
+            for (int v = 0; v < kGv; ++v) {
+                const float* f = fin + 2 * (me.sl * gs + g[v]);
+                mean[v] = f[0];
+                if (WHOLE) {
+#pragma unroll
+                    for (int u = 0; u < V; ++u) mul[u] *= f[1];
+                } else {
+                    mul[v] *= f[1];
+                }
             }
             const T* at = x + cv * V;
             const X* bt = buf + j * p.rpt * kT + threadIdx.x;
-#pragma unroll 4
-            for (int r = 0; r < cnt; ++r) {
-                const X q = BUF ? bt[r * kT] : load_vec<T, V>(at + r * step);
+            auto load = [&](int r) { return BUF ? bt[r * kT] : load_vec<T, V>(at + r * step); };
+            walk<kBatch, X>(cnt, load, [&](const X& q, int r) {
                 float o[V];
+                widen(q, o);
 #pragma unroll
-                for (int v = 0; v < V; ++v) o[v] = fmaf(to_f32(q.e[v]) - mean[v], mul[v], add[v]);
-                if (s.act == RFAST_ACT_RELU) {
-#pragma unroll
-                    for (int v = 0; v < V; ++v) o[v] = o[v] < 0.f ? 0.f : o[v];       // a NaN stays one
-                } else if (s.act == RFAST_ACT_SILU) {
+                for (int v = 0; v < V; ++v) o[v] = fmaf(o[v] - mean[WHOLE ? 0 : v], mul[v], add[v]);
+                if (s.act == RFAST_ACT_SILU) {
 #pragma unroll
                     for (int v = 0; v < V; ++v) o[v] *= sigmoid_of(o[v]);
+                } else if (s.act == RFAST_ACT_RELU) {
+#pragma unroll
+                    for (int v = 0; v < V; ++v) o[v] = o[v] < 0.f ? 0.f : o[v];       // a NaN stays one
                 }
-                store_vec<T, V>(y + r * ostep + cv * V, o);
-            }
+                store_vec(y + r * ostep + cv * V, o);
+            });
         }
     }
     if (p.cluster > 1) cg::this_cluster().barrier_wait();      // nobody reads this block's sums any more
 }
 
 // ---- backward -------------------------------------------------------------------------------------
-// d act(u) / du times dy
-__device__ __forceinline__ float through(int act, float dy, float u) {
-    if (act == RFAST_ACT_RELU) return u > 0.f ? dy : 0.f;
+// dy act'(u)
+template <int V>
+__device__ __forceinline__ void through(int act, const float (&u)[V], float (&dy)[V]) {
     if (act == RFAST_ACT_SILU) {
-        const float q = sigmoid_of(u);
-        return dy * (q * fmaf(u, 1.f - q, 1.f));
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const float q = sigmoid_of(u[v]);
+            dy[v] *= fmaf(q, fmaf(-q, u[v], u[v]), q);       // q (1 + u (1 - q))
+        }
+    } else if (act == RFAST_ACT_RELU) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) dy[v] = u[v] > 0.f ? dy[v] : 0.f;
     }
-    return dy;
 }
+template <class X> struct Pair { X x, d; };
 
 // With du = dy act'(u), h = (x - mean) rstd, and over the M values of a group
 //     one = sum gamma du / M, two = sum gamma du h / M:   dx = rstd (gamma du - one - two h);
 // per channel dbeta = sum du, dgamma = sum du h over the samples of a set.  A cluster takes every
 // `parts`-th item of a set and keeps the channels' sums of its items in shared memory.
 // grid = (parts * cluster, slabs, sets)
-template <class T, int V, bool BUF>
-__global__ void __launch_bounds__(kT)
+template <class T, int V, bool WHOLE, bool BUF>
+__global__ void __launch_bounds__(kT, BUF && WHOLE ? 3 : 2)
 k_gn_backward(const __grid_constant__ GnArgs a) {
     extern __shared__ __align__(16) uint8_t smem[];
     typedef Vec<T, V> X;
     const GnShape& s = a.s;
     const GnPlan& p = a.p;
+    constexpr int kBatch = BUF ? 2 : 4, kGv = WHOLE ? 1 : V;
     X* bufx = reinterpret_cast<X*>(smem);
     X* bufd = reinterpret_cast<X*>(smem + p.buf / 2);
     float* ent = reinterpret_cast<float*>(smem + p.buf);     // [2][kT * V]: du, du h of a thread's channels
@@ -373,7 +476,7 @@ k_gn_backward(const __grid_constant__ GnArgs a) {
     const int gs = min(p.gs, s.G - (int)blockIdx.y * p.gs); // the last slab may be narrower
     const int W = gs * s.Cg, nb = p.ns * gs;
     const int wide = min(p.W, kT * V);                       // channels of one pass over the width
-    float* sums = col + (p.tr > 1 ? 2 * p.ns * wide : 0);    // [nb][2] this block's, then [nb][2] the cluster's
+    float* sums = col + (p.tr > 1 ? 2 * max(kT, p.ns * wide) : 0);    // [nb][2] this block's, then [nb][2] the cluster's
     float* tot = sums + 2 * nb;
     float* acc = tot + 2 * nb;                               // [2][W]: dbeta, dgamma of the block's items
 
@@ -413,32 +516,49 @@ k_gn_backward(const __grid_constant__ GnArgs a) {
 #pragma unroll
             for (int v = 0; v < V; ++v) s_du[v] = s_dh[v] = 0.f;
             if (cnt > 0 && cv < cols) {
-                float mean[V], rs[V], ga[V], be[V];
+                float mean[kGv], rs[kGv], mul[V], add[V];    // u = (x - mean) mul + add
+                int g[kGv];
+                groups_of<V, WHOLE>(c0 + cv * V, s.Cg, g);
+                affine_of<V>(gam + cv * V, a.quads, mul);
+                affine_of<V>(bet + cv * V, a.quads, add);
 #pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    const int c = cv * V + v;
-                    const int64_t g = n * s.G + (c0 + c) / s.Cg;
-                    mean[v] = a.mean[g]; rs[v] = a.rstd[g]; ga[v] = gam[c]; be[v] = bet[c];
-                }
+                for (int v = 0; v < kGv; ++v) { mean[v] = a.mean[n * s.G + g[v]]; rs[v] = a.rstd[n * s.G + g[v]]; }
+#pragma unroll
+                for (int v = 0; v < V; ++v) mul[v] *= rs[WHOLE ? 0 : v];
                 const X* bx = bufx + j * p.rpt * kT + threadIdx.x;
                 const X* bd = bufd + j * p.rpt * kT + threadIdx.x;
-#pragma unroll 2
-                for (int r = 0; r < cnt; ++r) {
-                    const X q = BUF ? bx[r * kT] : load_vec<T, V>(x + r * xstep + cv * V);
-                    const X d = BUF ? bd[r * kT] : load_vec<T, V>(dy + r * dstep + cv * V);
+                auto load = [&](int r) {
+                    Pair<X> q;
+                    q.x = BUF ? bx[r * kT] : load_vec<T, V>(x + r * xstep + cv * V);
+                    q.d = BUF ? bd[r * kT] : load_vec<T, V>(dy + r * dstep + cv * V);
+                    return q;
+                };
+                walk<kBatch, Pair<X>>(cnt, load, [&](const Pair<X>& q, int) {
+                    float d[V], du[V], u[V];
+                    widen(q.x, d);
+                    widen(q.d, du);
 #pragma unroll
-                    for (int v = 0; v < V; ++v) {
-                        const float h = (to_f32(q.e[v]) - mean[v]) * rs[v];
-                        const float du = through(s.act, to_f32(d.e[v]), fmaf(h, ga[v], be[v]));
-                        s_du[v] += du;
-                        s_dh[v] = fmaf(du, h, s_dh[v]);
-                    }
-                }
+                    for (int v = 0; v < V; ++v) { d[v] -= mean[WHOLE ? 0 : v]; u[v] = fmaf(d[v], mul[v], add[v]); }
+                    through(s.act, u, du);
+#pragma unroll
+                    for (int v = 0; v < V; ++v) { s_du[v] += du[v]; s_dh[v] = fmaf(du[v], d[v], s_dh[v]); }
+                });
+#pragma unroll
+                for (int v = 0; v < V; ++v) s_dh[v] *= rs[WHOLE ? 0 : v];     // h = (x - mean) rstd
             }
             // [row of threads][channel of this pass]
             if (me.on) {
 #pragma unroll
-                for (int v = 0; v < V; ++v) { ent[threadIdx.x * V + v] = s_du[v]; ent[kT * V + threadIdx.x * V + v] = s_dh[v]; }
+                for (int v = 0; v < V; v += (V >= 4 ? 4 : 1)) {
+                    float *e0 = ent + threadIdx.x * V + v, *e1 = e0 + kT * V;
+                    if constexpr (V >= 4) {
+                        *reinterpret_cast<float4*>(e0) = make_float4(s_du[v], s_du[v + 1], s_du[v + 2], s_du[v + 3]);
+                        *reinterpret_cast<float4*>(e1) = make_float4(s_dh[v], s_dh[v + 1], s_dh[v + 2], s_dh[v + 3]);
+                    } else {
+                        *e0 = s_du[v];
+                        *e1 = s_dh[v];
+                    }
+                }
             }
             __syncthreads();
             const int pw = min(p.tx * V, W - j * kT * V);  // channels of this pass
@@ -446,27 +566,30 @@ k_gn_backward(const __grid_constant__ GnArgs a) {
             const float *q0 = ent, *q1 = ent + kT * V;
             int qp = pitch;                                  // floats between a sample's rows
             if (p.tr > 1) {
-                // down the rows of threads: `ways` threads per channel, then their sums, in fixed order
-                const int nc = p.ns * pw;
-                int ways = 1;
-                while (ways * 2 * nc <= kT && ways * 2 <= p.tr && ways < 32) ways *= 2;
-                for (int b0 = 0; b0 < nc; b0 += kT / ways) {
-                    const int k = b0 + threadIdx.x / ways, w = threadIdx.x & (ways - 1);
+                // down the rows of threads, `ways` threads per channel, then their sums, in fixed order
+                const int nc = p.ns * pw, ways = nc >= kT ? 1 : min(kT / nc, p.tr);
+                float *c0s = col, *c1s = col + (kT > p.ns * wide ? kT : p.ns * wide);
+                for (int i = threadIdx.x; i < nc * ways; i += kT) {
+                    const int w = i / nc, k = i - w * nc, sl = k / pw;
                     float u0 = 0.f, u1 = 0.f;
-                    if (k < nc) {
-                        const int sl = k / pw, c = k - sl * pw;
-                        for (int r = w; r < p.tr; r += ways) {
-                            const int at = (sl * p.tr + r) * pitch + c;
-                            u0 += q0[at];
-                            u1 += q1[at];
-                        }
+                    for (int at = (sl * p.tr + w) * pitch + (k - sl * pw), r = w; r < p.tr; r += ways, at += ways * pitch) {
+                        u0 += q0[at];
+                        u1 += q1[at];
                     }
-                    u0 = team_sum(u0, ways);
-                    u1 = team_sum(u1, ways);
-                    if (k < nc && w == 0) { col[k] = u0; col[p.ns * wide + k] = u1; }
+                    c0s[i] = u0;
+                    c1s[i] = u1;
                 }
                 __syncthreads();
-                q0 = col; q1 = col + p.ns * wide; qp = pw;
+                if (ways > 1) {
+                    if ((int)threadIdx.x < nc) {             // nc < kT: one channel per thread
+                        float u0 = c0s[threadIdx.x], u1 = c1s[threadIdx.x];
+                        for (int w = 1; w < ways; ++w) { u0 += c0s[w * nc + threadIdx.x]; u1 += c1s[w * nc + threadIdx.x]; }
+                        c0s[threadIdx.x] = u0;
+                        c1s[threadIdx.x] = u1;
+                    }
+                    __syncthreads();
+                }
+                q0 = c0s; q1 = c1s; qp = pw;
             }
             // dbeta, dgamma of this item's samples
             for (int c = threadIdx.x; c < pw; c += kT) {
@@ -511,30 +634,44 @@ k_gn_backward(const __grid_constant__ GnArgs a) {
             for (int j = 0; j < p.cj; ++j) {
                 const int cv = me.txi + j * kT;
                 if (cv >= cols) break;
-                float mean[V], rs[V], ga[V], be[V], one[V], two[V];
+                float mean[kGv], k1[kGv], k2[kGv], mul[V], add[V];   // dx = mul du - k1 - (x - mean) k2
+                int g[kGv];
+                groups_of<V, WHOLE>(cv * V, s.Cg, g);
+                affine_of<V>(gam + cv * V, a.quads, mul);
+                affine_of<V>(bet + cv * V, a.quads, add);
 #pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    const int c = cv * V + v, b = me.sl * gs + c / s.Cg;
-                    const int64_t g = n * s.G + (c0 + c) / s.Cg;
-                    mean[v] = a.mean[g]; rs[v] = a.rstd[g]; ga[v] = gam[c]; be[v] = bet[c];
-                    one[v] = sg[2 * b] * inv_m;
-                    two[v] = sg[2 * b + 1] * inv_m;
+                for (int v = 0; v < kGv; ++v) {
+                    const int64_t at = n * s.G + blockIdx.y * p.gs + g[v];
+                    const float rs = a.rstd[at], *q = sg + 2 * (me.sl * gs + g[v]);
+                    mean[v] = a.mean[at];
+                    k1[v] = rs * (q[0] * inv_m);
+                    k2[v] = rs * rs * (q[1] * inv_m);
+                    if (WHOLE) {
+#pragma unroll
+                        for (int u = 0; u < V; ++u) mul[u] *= rs;
+                    } else {
+                        mul[v] *= rs;
+                    }
                 }
                 const X* bx = bufx + j * p.rpt * kT + threadIdx.x;
                 const X* bd = bufd + j * p.rpt * kT + threadIdx.x;
-#pragma unroll 2
-                for (int r = 0; r < cnt; ++r) {
-                    const X q = BUF ? bx[r * kT] : load_vec<T, V>(x + r * xstep + cv * V);
-                    const X d = BUF ? bd[r * kT] : load_vec<T, V>(dy + r * dstep + cv * V);
-                    float o[V];
+                auto load = [&](int r) {
+                    Pair<X> q;
+                    q.x = BUF ? bx[r * kT] : load_vec<T, V>(x + r * xstep + cv * V);
+                    q.d = BUF ? bd[r * kT] : load_vec<T, V>(dy + r * dstep + cv * V);
+                    return q;
+                };
+                walk<kBatch, Pair<X>>(cnt, load, [&](const Pair<X>& q, int r) {
+                    float d[V], du[V], u[V];
+                    widen(q.x, d);
+                    widen(q.d, du);
 #pragma unroll
-                    for (int v = 0; v < V; ++v) {
-                        const float h = (to_f32(q.e[v]) - mean[v]) * rs[v];
-                        const float du = through(s.act, to_f32(d.e[v]), fmaf(h, ga[v], be[v]));
-                        o[v] = rs[v] * (fmaf(ga[v], du, -one[v]) - h * two[v]);
-                    }
-                    store_vec<T, V>(dx + r * ostep + cv * V, o);
-                }
+                    for (int v = 0; v < V; ++v) { d[v] -= mean[WHOLE ? 0 : v]; u[v] = fmaf(d[v], mul[v], add[v]); }
+                    through(s.act, u, du);
+#pragma unroll
+                    for (int v = 0; v < V; ++v) du[v] = fmaf(du[v], mul[v], fmaf(-d[v], k2[WHOLE ? 0 : v], -k1[WHOLE ? 0 : v]));
+                    store_vec(dx + r * ostep + cv * V, du);
+                });
             }
         }
         if (p.cluster == 1) __syncthreads();                 // `sums` may be filled again
@@ -597,7 +734,7 @@ size_t plan_smem(const GnShape& s, const GnPlan& p, bool backward) {
         return p.buf + sizeof(float) * (kT + 2 * kT * width + 5 * nb);
     }
     const size_t wide = p.W < kT * p.V ? p.W : kT * p.V;
-    return p.buf + sizeof(float) * (2 * (size_t)kT * p.V + (p.tr > 1 ? 2 * p.ns * wide : 0) + 4 * nb + 2 * (size_t)p.W);
+    return p.buf + sizeof(float) * (2 * (size_t)kT * p.V + (p.tr > 1 ? 2 * (p.ns * wide > kT ? p.ns * wide : (size_t)kT) : 0) + 4 * nb + 2 * (size_t)p.W);
 }
 
 // vmax: channels per access that addresses and strides allow (a power of two, times the type at most 16 bytes)
@@ -677,16 +814,23 @@ cudaError_t launch_plan(K kernel, dim3 grid, const GnArgs& a, cudaStream_t st) {
     return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 
+template <class T, int V, bool WHOLE>
+cudaError_t launch_whole(const GnArgs& a, bool backward, dim3 grid, cudaStream_t st) {
+    if constexpr (sizeof(T) * V >= 4) {
+        if (a.p.buffered) return backward ? launch_plan(k_gn_backward<T, V, WHOLE, true>, grid, a, st) : launch_plan(k_gn_forward<T, V, WHOLE, true>, grid, a, st);
+    }
+    return backward ? launch_plan(k_gn_backward<T, V, WHOLE, false>, grid, a, st) : launch_plan(k_gn_forward<T, V, WHOLE, false>, grid, a, st);
+}
 template <class T, int V>
 cudaError_t launch_gn(const GnArgs& a, bool backward, cudaStream_t st) {
     const dim3 grid((unsigned)((backward ? a.p.parts : a.p.items) * a.p.cluster), a.p.slabs, backward ? (unsigned)(a.s.N / a.s.per_set) : 1);
-    if constexpr (sizeof(T) * V >= 4) {
-        if (a.p.buffered) return backward ? launch_plan(k_gn_backward<T, V, true>, grid, a, st) : launch_plan(k_gn_forward<T, V, true>, grid, a, st);
-    }
-    return backward ? launch_plan(k_gn_backward<T, V, false>, grid, a, st) : launch_plan(k_gn_forward<T, V, false>, grid, a, st);
+    if (a.s.Cg % V == 0) return launch_whole<T, V, true>(a, backward, grid, st);
+    if constexpr (V > 1) return launch_whole<T, V, false>(a, backward, grid, st);
+    return cudaErrorInvalidValue;
 }
 
-cudaError_t launch_typed(const GnArgs& a, int type, bool backward, cudaStream_t st) {
+cudaError_t launch_typed(GnArgs& a, int type, bool backward, cudaStream_t st) {
+    a.quads = !((uintptr_t)a.gamma % 16 || (uintptr_t)a.beta % 16 || a.affine_stride % 4);
     switch (type) {
         case RFAST_TYPE_F32: return a.p.V == 4 ? launch_gn<float, 4>(a, backward, st) : launch_gn<float, 1>(a, backward, st);
         case RFAST_TYPE_BF16:
