@@ -500,7 +500,8 @@ def rfast_group_norm(x: int, gamma: int, beta: int, y: int, mean: int, rstd: int
     [samples][positions][channels].  All addresses are DEVICE addresses; x and y have `type`, gamma, beta
     [samples / samples_per_set][channels] and the results mean, rstd [samples][groups] are fp32
     (samples_per_set None: one row for all samples).  Strides: (sample, position) in elements, None for
-    contiguous.  Enqueued on cuda_stream."""
+    contiguous.  workspace: rfast_group_norm_workspace(...) bytes that no other running call uses.
+    Enqueued on cuda_stream."""
     shape = _gn_shape(samples, positions, channels, groups, samples_per_set, type, act)
     err = C.create_string_buffer(256)
     _op(lib().rfast_group_norm(C.byref(shape), x or None, _strides(x_strides), gamma or None, beta or None, eps, y or None, _strides(y_strides),

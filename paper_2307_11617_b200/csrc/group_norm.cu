@@ -1,19 +1,21 @@
 // Group norm with an activation, channels last, forward and backward (see rfast_group_norm in rfast.h
 // for the formulas).
 //
-// Work item: a sample (or several, where a sample has few positions) x a slab of channels, the
-// smallest run of whole groups that is at least 128 bytes wide.  A thread keeps its column of V
-// neighbouring channels and walks down the positions, so that all that belongs to a channel -- sums,
-// scale, shift -- sits in its registers.  An item is taken by a cluster of 1 to 16 thread blocks that split
-// the positions and exchange the groups' sums through distributed shared memory.  Every value crosses
-// HBM once: what a thread has read for the sums waits in shared memory (asynchronous copies that
-// only this thread reads back, so no barrier guards them) or, for items too large for that, is read
-// again out of L2, where the cluster has just put it.
+// A thread keeps its column of V neighbouring channels and walks down the positions, so that all that belongs to a
+// channel -- sums, scale, shift -- sits in its registers.  A thread block's columns make up a slab, the smallest run
+// of whole groups that is at least 128 bytes wide.  There are two ways through a sample's slab:
+//   - one thread block takes it whole (or several samples' where they have few positions).  What a thread has read for the
+//     sums waits in shared memory: asynchronous copies that only this thread reads back, so no barrier guards them;
+//   - slabs that are too large for that, or too few to fill the GPU, are cut into chunks of positions: one launch for the
+//     chunks' sums, one that merges them and goes over the values again.  Samples are taken in batches that the L2
+//     cache holds, the second launch starting from the end, so that its reads are served there.
+// The sums of a slab could also meet inside a cluster of thread blocks that keep the slab in their shared memory.  Built and
+// measured: loading, summing and writing then follow one another on the whole GPU, and 32 x 3136 x 256 bf16 took 37 us
+// forward and 122 us backward.
 //
 // Variances do not come from a difference of two large sums: a thread sums deviations from the first value it
 // sees in each channel, and its mean and sum of squared deviations are merged with the others' by the parallel
 // form of the two-pass formula (Chan, Golub, LeVeque).
-#include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -22,8 +24,6 @@
 #include <cstdio>
 
 #include "ops.h"
-
-namespace cg = cooperative_groups;
 
 namespace rfast {
 
@@ -48,51 +48,65 @@ __device__ __forceinline__ Vec<T, V> load_vec(const T* p) {
     v.w = *reinterpret_cast<const typename Vec<T, V>::W*>(p);
     return v;
 }
-__device__ __forceinline__ void widen2(uint32_t r, const __nv_bfloat16*, float* f) {
-    f[0] = __uint_as_float(r << 16);
-    f[1] = __uint_as_float(r & 0xffff0000u);
-}
-__device__ __forceinline__ void widen2(uint32_t r, const __half*, float* f) {
+// Two fp32 values side by side: one instruction adds or multiplies both.
+struct F2 { uint64_t v; };
+__device__ __forceinline__ F2 pair(float a, float b) { F2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ F2 both(float a) { return pair(a, a); }
+__device__ __forceinline__ void split(F2 p, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p.v)); }
+__device__ __forceinline__ F2 operator+(F2 a, F2 b) { F2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
+__device__ __forceinline__ F2 operator*(F2 a, F2 b) { F2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) { F2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v)); return r; }
+
+// pairs of V channels; a single channel has a zero beside it
+template <int V> constexpr int kPairs = (V + 1) / 2;
+
+__device__ __forceinline__ F2 widen2(uint32_t r, const __nv_bfloat16*) { return pair(__uint_as_float(r << 16), __uint_as_float(r & 0xffff0000u)); }
+__device__ __forceinline__ F2 widen2(uint32_t r, const __half*) {
     const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&r));
-    f[0] = a.x; f[1] = a.y;
+    return pair(a.x, a.y);
 }
-__device__ __forceinline__ void widen(Vec<float, 4> v, float (&f)[4]) {
-    f[0] = __uint_as_float(v.w.x); f[1] = __uint_as_float(v.w.y); f[2] = __uint_as_float(v.w.z); f[3] = __uint_as_float(v.w.w);
+__device__ __forceinline__ void widen(Vec<float, 4> v, F2 (&f)[2]) {
+    f[0] = pair(__uint_as_float(v.w.x), __uint_as_float(v.w.y));
+    f[1] = pair(__uint_as_float(v.w.z), __uint_as_float(v.w.w));
 }
-__device__ __forceinline__ void widen(Vec<float, 1> v, float (&f)[1]) { f[0] = __uint_as_float(v.w); }
+__device__ __forceinline__ void widen(Vec<float, 1> v, F2 (&f)[1]) { f[0] = pair(__uint_as_float(v.w), 0.f); }
 template <class T>
-__device__ __forceinline__ void widen(Vec<T, 8> v, float (&f)[8]) {
+__device__ __forceinline__ void widen(Vec<T, 8> v, F2 (&f)[4]) {
     const T* t = nullptr;
-    widen2(v.w.x, t, f); widen2(v.w.y, t, f + 2); widen2(v.w.z, t, f + 4); widen2(v.w.w, t, f + 6);
+    f[0] = widen2(v.w.x, t); f[1] = widen2(v.w.y, t); f[2] = widen2(v.w.z, t); f[3] = widen2(v.w.w, t);
 }
 template <class T>
-__device__ __forceinline__ void widen(Vec<T, 2> v, float (&f)[2]) { widen2(v.w, (const T*)nullptr, f); }
+__device__ __forceinline__ void widen(Vec<T, 2> v, F2 (&f)[1]) { f[0] = widen2(v.w, (const T*)nullptr); }
 template <class T>
-__device__ __forceinline__ void widen(Vec<T, 1> v, float (&f)[1]) {
-    float t[2];
-    widen2((uint32_t)v.w, (const T*)nullptr, t);
-    f[0] = t[0];
+__device__ __forceinline__ void widen(Vec<T, 1> v, F2 (&f)[1]) { f[0] = widen2((uint32_t)v.w, (const T*)nullptr); }
+__device__ __forceinline__ uint32_t narrow2(F2 f, const __nv_bfloat16*) {
+    float a, b;
+    split(f, a, b);
+    const __nv_bfloat162 r = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&r);
 }
-__device__ __forceinline__ uint32_t narrow2(const float* f, const __nv_bfloat16*) {
-    const __nv_bfloat162 a = __floats2bfloat162_rn(f[0], f[1]);
-    return *reinterpret_cast<const uint32_t*>(&a);
+__device__ __forceinline__ uint32_t narrow2(F2 f, const __half*) {
+    float a, b;
+    split(f, a, b);
+    const __half2 r = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&r);
 }
-__device__ __forceinline__ uint32_t narrow2(const float* f, const __half*) {
-    const __half2 a = __floats2half2_rn(f[0], f[1]);
-    return *reinterpret_cast<const uint32_t*>(&a);
-}
-__device__ __forceinline__ void store_vec(float* p, const float (&f)[4]) { __stcs(reinterpret_cast<float4*>(p), make_float4(f[0], f[1], f[2], f[3])); }
-__device__ __forceinline__ void store_vec(float* p, const float (&f)[1]) { __stcs(p, f[0]); }
-template <class T>
-__device__ __forceinline__ void store_vec(T* p, const float (&f)[8]) {
-    __stcs(reinterpret_cast<uint4*>(p), make_uint4(narrow2(f, p), narrow2(f + 2, p), narrow2(f + 4, p), narrow2(f + 6, p)));
-}
-template <class T>
-__device__ __forceinline__ void store_vec(T* p, const float (&f)[2]) { __stcs(reinterpret_cast<uint32_t*>(p), narrow2(f, p)); }
-template <class T>
-__device__ __forceinline__ void store_vec(T* p, const float (&f)[1]) {
-    const float t[2] = {f[0], 0.f};
-    __stcs(reinterpret_cast<unsigned short*>(p), (unsigned short)narrow2(t, p));
+// V is the number of channels, the pairs holding that many
+template <int V, class T>
+__device__ __forceinline__ void store_vec(T* p, const F2 (&f)[kPairs<V>]) {
+    if constexpr (sizeof(T) == 4) {
+        float q[2 * kPairs<V>];
+#pragma unroll
+        for (int k = 0; k < kPairs<V>; ++k) split(f[k], q[2 * k], q[2 * k + 1]);
+        if constexpr (V == 4) __stcs(reinterpret_cast<float4*>(p), make_float4(q[0], q[1], q[2], q[3]));
+        else __stcs(p, q[0]);
+    } else if constexpr (V == 8) {
+        __stcs(reinterpret_cast<uint4*>(p), make_uint4(narrow2(f[0], p), narrow2(f[1], p), narrow2(f[2], p), narrow2(f[3], p)));
+    } else if constexpr (V == 2) {
+        __stcs(reinterpret_cast<uint32_t*>(p), narrow2(f[0], p));
+    } else {
+        __stcs(reinterpret_cast<unsigned short*>(p), (unsigned short)narrow2(f[0], p));
+    }
 }
 template <int BYTES>
 __device__ __forceinline__ void copy_async(void* dst, const void* src) {
@@ -100,31 +114,45 @@ __device__ __forceinline__ void copy_async(void* dst, const void* src) {
     if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(d), "l"(src) : "memory");
     else asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(d), "l"(src) : "memory");
 }
-__device__ __forceinline__ void copies_landed() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// until at most `left` of the youngest groups are on their way
+__device__ __forceinline__ void copies_wait(int left) {
+    switch (left) {
+        case 0: asm volatile("cp.async.wait_group 0;" ::: "memory"); break;
+        case 1: asm volatile("cp.async.wait_group 1;" ::: "memory"); break;
+        case 2: asm volatile("cp.async.wait_group 2;" ::: "memory"); break;
+        default: asm volatile("cp.async.wait_group 3;" ::: "memory"); break;
+    }
+}
 
 // 1 / (1 + exp(-u)).  2^t and the reciprocal are the hardware's (2 ulp and 1 ulp), t is rounded once: the result is good
 // to about 2^-23.  u = -inf gives 0.
-__device__ __forceinline__ float sigmoid_of(float u) {
-    float e, q;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(u * -1.4426950408889634f));
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(q) : "f"(1.f + e));
-    return q;
+__device__ __forceinline__ F2 sigmoid2(F2 u) {
+    float a, b;
+    split(u * both(-1.4426950408889634f), a, b);
+    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(a));
+    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(b));
+    split(pair(a, b) + both(1.f), a, b);
+    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(a));
+    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(b));
+    return pair(a, b);
 }
 
-// Rows 0 .. cnt of a thread, R at a time: all loads of a batch go out before the first row is worked on (a
-// store in between would hold later loads back, the operands being allowed to coincide).
+// cnt rows of a thread, R at a time: all loads of a batch go out before the first row is worked on (a store in
+// between would hold later loads back, the operands being allowed to coincide).
 template <int R, class Row, class Load, class Use>
 __device__ __forceinline__ void walk(int cnt, Load load, Use use) {
     int r = 0;
+#pragma unroll 1
     for (; r + R <= cnt; r += R) {
         Row q[R];
 #pragma unroll
-        for (int k = 0; k < R; ++k) q[k] = load(r + k);
+        for (int k = 0; k < R; ++k) q[k] = load();
 #pragma unroll
-        for (int k = 0; k < R; ++k) use(q[k], r + k);
+        for (int k = 0; k < R; ++k) use(q[k]);
     }
 #pragma unroll 1
-    for (; r < cnt; ++r) use(load(r), r);
+    for (; r < cnt; ++r) { Row q = load(); use(q); }
 }
 
 // ---- geometry, chosen on the host -------------------------------------------------------------------
@@ -140,13 +168,13 @@ struct GnPlan {
     int W, gs, slabs;                  // channels and groups of a slab
     int tx, cj;                        // threads across the slab, passes over its width
     int tr, ns;                        // threads down the positions of a sample, samples per item
-    int cluster;                       // thread blocks per item
+    int chunks;                        // thread blocks per sample and slab; 1: one launch does it all
     int64_t rows;                      // positions per thread block
-    int rpt;                           // positions per thread
+    int rpt;                           // positions per thread (buffered)
     bool buffered;                     // what was read waits in shared memory
-    int64_t items;                     // items per set (forward: over all samples)
-    int64_t parts;                     // backward: thread blocks (clusters) that share a set's items
-    size_t buf, smem;                  // bytes: the buffer, all
+    int64_t items;                     // one launch: items per set (forward: over all samples)
+    int64_t parts;                     // one launch, backward: thread blocks that share a set's items
+    size_t buf;                        // bytes of the buffer
 };
 
 struct GnArgs {
@@ -163,8 +191,15 @@ struct GnArgs {
     int set_row_stride;
     float *mean, *rstd;                // [N][G]: out (forward), in (backward)
     float *dgamma, *dbeta;             // backward: where the sums of a set go
-    float* part;                       // backward: [sets][parts * cluster][2][C] when a set has several blocks
+    float2* gpart;                     // chunks: [N][G][chunks] mean and squared deviations, or the two sums of the backward pass
+    float* part;                       // backward: rows of [2][C], du and du h summed; a row per thread block of a set or per
+                                       // sample and chunk
+    int64_t n0, n1;                    // chunks: samples of this launch
 };
+
+// A thread block's task: everything in one launch (what it reads kept in shared memory, or read twice where that is too small
+// or accesses are too narrow), the chunks' sums, or what follows from them.
+enum { kWhole = 0, kSums = 1, kApply = 2, kReread = 3 };
 
 __device__ __forceinline__ const float* affine_row(const GnArgs& a, const float* base, int64_t set) {
     const int64_t row = a.set_row ? (int64_t)a.set_row[set * a.set_row_stride] : set;
@@ -174,33 +209,41 @@ __device__ __forceinline__ const float* affine_row(const GnArgs& a, const float*
 // What a thread is in its block: column, sample of the item, first position; the same for both directions.
 struct Seat {
     int txi, sl, rr;                   // column of threads, sample within the item, row of the sample's threads
+    int64_t r0;                        // first position
+    int have;                          // positions of the thread block
+    int rows;                          // positions of this thread where its sample exists
     bool on;
 };
-__device__ __forceinline__ Seat seat_of(const GnPlan& p) {
+__device__ __forceinline__ Seat seat_of(const GnShape& g, const GnPlan& p, unsigned chunk) {
     Seat s;
-    const int tyi = threadIdx.x / p.tx;
+    const unsigned tyi = threadIdx.x / (unsigned)p.tx;
     s.txi = threadIdx.x - tyi * p.tx;
-    s.sl = tyi / p.tr;
+    s.sl = p.ns == 1 ? (tyi < (unsigned)p.tr ? 0 : 1) : tyi / (unsigned)p.tr;
     s.rr = tyi - s.sl * p.tr;
     s.on = s.sl < p.ns;
+    s.r0 = (int64_t)chunk * p.rows + s.rr;
+    const int64_t left = g.S - (int64_t)chunk * p.rows;     // fits 32 bits: there are fewer than 2^31 positions
+    s.have = (int)(left < p.rows ? (left < 0 ? 0 : left) : p.rows);
+    s.rows = s.on && s.rr < s.have ? (int)(((unsigned)(s.have - s.rr) + p.tr - 1) / (unsigned)p.tr) : 0;
     return s;
 }
 
 // scale or shift of V neighbouring channels
 template <int V>
-__device__ __forceinline__ void affine_of(const float* p, bool quads, float (&f)[V]) {
+__device__ __forceinline__ void affine_of(const float* p, bool quads, F2 (&f)[kPairs<V>]) {
     if constexpr (V % 4 == 0) {
         if (quads) {
 #pragma unroll
             for (int k = 0; k < V; k += 4) {
                 const float4 q = *reinterpret_cast<const float4*>(p + k);
-                f[k] = q.x; f[k + 1] = q.y; f[k + 2] = q.z; f[k + 3] = q.w;
+                f[k / 2] = pair(q.x, q.y);
+                f[k / 2 + 1] = pair(q.z, q.w);
             }
             return;
         }
     }
 #pragma unroll
-    for (int k = 0; k < V; ++k) f[k] = p[k];
+    for (int k = 0; k < V; k += 2) f[k / 2] = pair(p[k], k + 1 < V ? p[k + 1] : 0.f);
 }
 // groups of V neighbouring channels from channel c on: one (WHOLE) or one per channel
 template <int V, bool WHOLE>
@@ -229,113 +272,157 @@ __device__ __forceinline__ int team_size(int entries) {
 }
 
 // ---- forward --------------------------------------------------------------------------------------
-// grid = (items * cluster, slabs), clusters along x
-template <class T, int V, bool WHOLE, bool BUF>
-__global__ void __launch_bounds__(kT, BUF && WHOLE ? 4 : 3)
+// kWhole, kReread: grid = (items, slabs).  kSums, kApply: grid = (samples of the launch * chunks, slabs); kApply runs back to front.
+template <class T, int V, bool WHOLE, int TASK>
+__global__ void __launch_bounds__(kT, WHOLE ? 4 : 3)
 k_gn_forward(const __grid_constant__ GnArgs a) {
     extern __shared__ __align__(16) uint8_t smem[];
     typedef Vec<T, V> X;
     const GnShape& s = a.s;
     const GnPlan& p = a.p;
-    constexpr int kBatch = 4, kGv = WHOLE ? 1 : V, kAcc = WHOLE ? (V < 4 ? V : 4) : V;
+    constexpr bool BUF = TASK == kWhole, kOne = TASK == kWhole || TASK == kReread;
+    constexpr int kBatch = TASK == kSums ? 8 : 4, kP = kPairs<V>, kGv = WHOLE ? 1 : V, kGp = WHOLE ? 1 : kP, kAcc = WHOLE ? (kP < 2 ? 1 : 2) : kP;
     X* buf = reinterpret_cast<X*>(smem);
     // per thread (WHOLE: an access stays inside a group) or per thread and channel: count, mean, sum of squared deviations
+    constexpr int width = kGv, kEnt = TASK == kApply ? 0 : kT;
     float* e_n = reinterpret_cast<float*>(smem + p.buf);
-    constexpr int width = kGv;
-    float* e_mean = e_n + kT;
-    float* e_m2 = e_mean + kT * width;
-    float* bins = e_m2 + kT * width;                        // [ns * gs][3], then [ns * gs][2] final
+    float* e_mean = e_n + kEnt;
+    float* e_m2 = e_mean + kEnt * width;
     const int gs = min(p.gs, s.G - (int)blockIdx.y * p.gs); // the last slab may be narrower
     const int nb = p.ns * gs;
-    float* fin = bins + 3 * nb;
+    float2* fin = reinterpret_cast<float2*>(e_m2 + kEnt * width);      // [nb] mean, rstd
 
-    const int rank = p.cluster > 1 ? blockIdx.x % p.cluster : 0;
-    const int64_t item = blockIdx.x / p.cluster;
-    const Seat me = seat_of(p);
-    const int64_t n = item * p.ns + me.sl;
-    const bool on = me.on && n < s.N;
-    const int64_t r0 = (int64_t)rank * p.rows + me.rr;
-    const int64_t r1 = min(s.S, (int64_t)(rank + 1) * p.rows);
-    const int cnt = on && r0 < r1 ? (int)((r1 - r0 + p.tr - 1) / p.tr) : 0;
+    if (TASK == kSums) asm volatile("griddepcontrol.launch_dependents;");
+    unsigned item = TASK == kApply ? gridDim.x - 1 - blockIdx.x : blockIdx.x, chunk = 0;
+    if (!kOne) {
+        const unsigned q = item / (unsigned)p.chunks;
+        chunk = item - q * p.chunks;
+        item = q;
+    }
+    const Seat me = seat_of(s, p, chunk);
+    const int64_t nf = kOne ? (int64_t)item * p.ns : a.n0 + item, n = nf + me.sl;    // first sample of the block, this thread's
+    const int cnt = n < s.N ? me.rows : 0;
     const int c0 = blockIdx.y * p.W, cols = gs * s.Cg / V;
-    const T* x = (const T*)a.x + n * a.xn + r0 * a.xs + c0;
+    const T* x = (const T*)a.x + n * a.xn + me.r0 * a.xs + c0;
     const int64_t step = (int64_t)p.tr * a.xs;
 
-    if (BUF) {
+    if constexpr (TASK != kApply) {
+        // what is read comes in up to four lots of rows; the first is worked on while the others are on their way
+        const int lot = BUF ? (cnt + 3) / 4 : cnt;
+        if (BUF) {
+            for (int j = 0; j < p.cj; ++j) {
+                const int cv = me.txi + j * kT;
+                if (cv < cols) {
+                    const T* at = x + cv * V;
+                    X* to = buf + j * p.rpt * kT + threadIdx.x;
+                    int r = 0;
+                    for (int k = 0; k < 4; ++k) {
+                        for (const int end = min(cnt, r + lot); r < end; ++r, at += step, to += kT) copy_async<sizeof(X)>(to, at);
+                        if (p.cj == 1) copies_commit();
+                    }
+                }
+            }
+            if (p.cj > 1) { copies_commit(); copies_wait(0); }
+        }
+        // count, mean and squared deviations of what this thread holds
+        float t_n = 0.f, t_mean = 0.f, t_m2 = 0.f;
         for (int j = 0; j < p.cj; ++j) {
             const int cv = me.txi + j * kT;
-            if (cv < cols)
-                for (int r = 0; r < cnt; ++r) copy_async<sizeof(X)>(buf + (j * p.rpt + r) * kT + threadIdx.x, x + r * step + cv * V);
-        }
-        copies_landed();
-    }
-    // count, mean and squared deviations of what this thread holds
-    float t_n = 0.f, t_mean = 0.f, t_m2 = 0.f;
-    for (int j = 0; j < p.cj; ++j) {
-        const int cv = me.txi + j * kT;
-        float first[kGv], s1[kAcc], s2[kAcc];
+            F2 first[kGp], s1[kAcc], s2[kAcc];               // the first value, negated
 #pragma unroll
-        for (int v = 0; v < kAcc; ++v) s1[v] = s2[v] = 0.f;
+            for (int v = 0; v < kAcc; ++v) s1[v] = s2[v] = both(0.f);
 #pragma unroll
-        for (int v = 0; v < kGv; ++v) first[v] = 0.f;
-        if (cnt > 0 && cv < cols) {
-            const T* at = x + cv * V;
-            const X* bt = buf + j * p.rpt * kT + threadIdx.x;
-            auto load = [&](int r) { return BUF ? bt[r * kT] : load_vec<T, V>(at + r * step); };
-            {
-                float f[V];
-                widen(load(0), f);
+            for (int v = 0; v < kGp; ++v) first[v] = both(0.f);
+            float mean[2 * kGp], m2[2 * kGp];
 #pragma unroll
-                for (int v = 0; v < kGv; ++v) first[v] = f[v];
-            }
-            walk<kBatch, X>(cnt, load, [&](const X& q, int) {     // a first value counts as a deviation of 0
-                float f[V];
-                widen(q, f);
+            for (int v = 0; v < 2 * kGp; ++v) mean[v] = m2[v] = 0.f;
+            if (cnt > 0 && cv < cols) {
+                const T* at = x + cv * V;
+                const X* bt = buf + j * p.rpt * kT + threadIdx.x;
+                auto load = [&]() {
+                    if (BUF) { const X q = *bt; bt += kT; return q; }
+                    const X q = load_vec<T, V>(at);
+                    at += step;
+                    return q;
+                };
+                if (BUF && p.cj == 1) copies_wait(3);
+                {
+                    F2 f[kP];
+                    widen(BUF ? *bt : load_vec<T, V>(at), f);
 #pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    const float d = f[v] - first[WHOLE ? 0 : v];
-                    s1[v % kAcc] += d;
-                    s2[v % kAcc] = fmaf(d, d, s2[v % kAcc]);
+                    for (int v = 0; v < kGp; ++v) {
+                        float lo, hi;
+                        split(f[v], lo, hi);
+                        mean[2 * v] = lo;
+                        mean[2 * v + 1] = WHOLE ? lo : hi;
+                        first[v] = pair(-lo, WHOLE ? -lo : -hi);
+                    }
                 }
-            });
-            if (WHOLE) {
+                auto use = [&](const X& q) {                 // a first value counts as a deviation of 0
+                    F2 f[kP];
+                    widen(q, f);
 #pragma unroll
-                for (int v = 1; v < kAcc; ++v) { s1[0] += s1[v]; s2[0] += s2[v]; }
-            }
-            const float nn = (float)cnt * (WHOLE ? V : 1), inv = 1.f / nn;
+                    for (int v = 0; v < kP; ++v) {
+                        const F2 d = f[v] + first[WHOLE ? 0 : v];
+                        s1[v % kAcc] = s1[v % kAcc] + d;
+                        s2[v % kAcc] = fma2(d, d, s2[v % kAcc]);
+                    }
+                };
+                if (BUF && p.cj == 1) {
+                    for (int k = 0, r = 0; k < 4; ++k, r += lot) {
+                        if (k) copies_wait(3 - k);
+                        walk<kBatch, X>(min(cnt - r, lot), load, use);
+                    }
+                } else {
+                    walk<kBatch, X>(cnt, load, use);
+                }
+                if (WHOLE) {
+                    if (kAcc == 2) { s1[0] = s1[0] + s1[kAcc - 1]; s2[0] = s2[0] + s2[kAcc - 1]; }
+                    float lo, hi;
+                    split(s1[0], lo, hi);
+                    s1[0] = both(V > 1 ? lo + hi : lo);
+                    split(s2[0], lo, hi);
+                    s2[0] = both(V > 1 ? lo + hi : lo);
+                }
+                const float nn = (float)cnt * (WHOLE ? V : 1), inv = 1.f / nn;
 #pragma unroll
-            for (int v = 0; v < kGv; ++v) {
-                const float d = s1[v] * inv;
-                s2[v] = fmaxf(fmaf(-s1[v], d, s2[v]), 0.f) + (s2[v] - s2[v]);    // the second term is a NaN where there was one
-                first[v] += d;                              // now the mean
+                for (int v = 0; v < kGp; ++v) {
+                    float a1[2], a2[2];
+                    split(s1[v], a1[0], a1[1]);
+                    split(s2[v], a2[0], a2[1]);
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const float d = a1[k] * inv;
+                        m2[2 * v + k] = fmaxf(fmaf(-a1[k], d, a2[k]), 0.f) + (a2[k] - a2[k]);   // the second term is a NaN where there was one
+                        mean[2 * v + k] += d;
+                    }
+                }
+                if (WHOLE && t_n > 0.f) {                    // a further pass over a wide group
+                    const float d = mean[0] - t_mean, tot = t_n + nn;
+                    t_mean += d * (nn / tot);
+                    t_m2 += m2[0] + d * d * (t_n * nn / tot);
+                    t_n = tot;
+                } else {
+                    t_mean = mean[0]; t_m2 = m2[0]; t_n = nn;
+                }
             }
-            if (WHOLE && t_n > 0.f) {                       // a further pass over a wide group
-                const float d = first[0] - t_mean, tot = t_n + nn;
-                t_mean += d * (nn / tot);
-                t_m2 += s2[0] + d * d * (t_n * nn / tot);
-                t_n = tot;
-            } else {
-                t_mean = first[0]; t_m2 = s2[0]; t_n = nn;
+            if (!WHOLE) {                                    // a slab of several groups is never wider than the block
+                if (me.on && cv < cols) {
+#pragma unroll
+                    for (int v = 0; v < kGv; ++v) { e_mean[threadIdx.x * V + v] = mean[v]; e_m2[threadIdx.x * V + v] = m2[v]; }
+                }
             }
         }
-        if (!WHOLE) {                                       // a slab of several groups is never wider than the block
-            if (me.on && cv < cols) {
-#pragma unroll
-                for (int v = 0; v < kGv; ++v) { e_mean[threadIdx.x * V + v] = first[v]; e_m2[threadIdx.x * V + v] = s2[v]; }
-            }
-        }
-    }
-    e_n[threadIdx.x] = t_n;
-    if (WHOLE) { e_mean[threadIdx.x] = t_mean; e_m2[threadIdx.x] = t_m2; }
-    __syncthreads();
-    // the groups' sums over this block, a team of lanes per group
-    {
-        const int unit = WHOLE ? min(s.Cg / V, p.tx) : s.Cg;   // entries of a group in one row of threads
+        e_n[threadIdx.x] = t_n;
+        if (WHOLE) { e_mean[threadIdx.x] = t_mean; e_m2[threadIdx.x] = t_m2; }
+        __syncthreads();
+        // the groups' sums over this block, a team of lanes per group
+        const int unit = WHOLE ? min(s.Cg / V, p.tx) : s.Cg;    // entries of a group in one row of threads
         const int entries = unit * p.tr, L = team_size(entries), lane = threadIdx.x & (L - 1);
         for (int b0 = 0; b0 < nb; b0 += kT / L) {
             const int b = b0 + threadIdx.x / L;
             const bool in = b < nb;
-            const int sl = in ? b / gs : 0, g = in ? b - sl * gs : 0;
+            const int sl = in && p.ns > 1 ? b / gs : 0, g = in ? b - sl * gs : 0;
             // means are summed as differences from one of them: a flat group has exactly its level
             const float ref = in ? e_mean[sl * p.tr * p.tx * width + g * unit] : 0.f;
             float cn = 0.f, cm = 0.f;
@@ -358,357 +445,485 @@ k_gn_forward(const __grid_constant__ GnArgs a) {
                 }
             }
             m2 = team_sum(m2, L);
-            if (in && lane == 0) { bins[3 * b] = cn; bins[3 * b + 1] = mean; bins[3 * b + 2] = m2; }
-        }
-    }
-    if (p.cluster > 1) cg::this_cluster().sync(); else __syncthreads();
-    for (int b = threadIdx.x; b < nb; b += kT) {
-        float mean = bins[3 * b + 1], m2 = bins[3 * b + 2];
-        if (p.cluster > 1) {                                // every block of the cluster adds up the same, in the same order
-            cg::cluster_group cl = cg::this_cluster();
-            const float ref = cl.map_shared_rank(bins, 0)[3 * b + 1];
-            float cn = 0.f, cm = 0.f;
-            for (int r = 0; r < p.cluster; ++r) {
-                const float* o = cl.map_shared_rank(bins, r) + 3 * b;
-                if (o[0] > 0.f) { cn += o[0]; cm = fmaf(o[0], o[1] - ref, cm); }
-            }
-            mean = ref + cm / cn;
-            m2 = 0.f;
-            for (int r = 0; r < p.cluster; ++r) {
-                const float* o = cl.map_shared_rank(bins, r) + 3 * b;
-                if (o[0] > 0.f) { const float d = o[1] - mean; m2 += fmaf(o[0] * d, d, o[2]); }
-            }
-        }
-        const float rstd = rsqrtf(m2 / ((float)s.S * (float)s.Cg) + s.eps);
-        fin[2 * b] = mean;
-        fin[2 * b + 1] = rstd;
-        const int sl = b / gs;
-        const int64_t nn = item * p.ns + sl;
-        if (rank == 0 && nn < s.N) {
-            const int64_t at = nn * s.G + blockIdx.y * p.gs + (b - sl * gs);
-            a.mean[at] = mean;
-            a.rstd[at] = rstd;
-        }
-    }
-    if (p.cluster > 1) cg::this_cluster().barrier_arrive();    // this block has read what it needs of the others
-    __syncthreads();
-    if (cnt > 0) {
-        const int64_t set = n / s.per_set;
-        const float* gam = affine_row(a, a.gamma, set) + c0;
-        const float* bet = affine_row(a, a.beta, set) + c0;
-        T* y = (T*)a.out + n * a.on + r0 * a.os + c0;
-        const int64_t ostep = (int64_t)p.tr * a.os;
-        for (int j = 0; j < p.cj; ++j) {
-            const int cv = me.txi + j * kT;
-            if (cv >= cols) break;
-            float mean[kGv], mul[V], add[V];
-            int g[kGv];
-            groups_of<V, WHOLE>(cv * V, s.Cg, g);
-            affine_of<V>(gam + cv * V, a.quads, mul);
-            affine_of<V>(bet + cv * V, a.quads, add);
-#pragma unroll
-            for (int v = 0; v < kGv; ++v) {
-                const float* f = fin + 2 * (me.sl * gs + g[v]);
-                mean[v] = f[0];
-                if (WHOLE) {
-#pragma unroll
-                    for (int u = 0; u < V; ++u) mul[u] *= f[1];
+            if (in && lane == 0) {
+                const int64_t at = (nf + sl) * s.G + blockIdx.y * p.gs + g;
+                if (TASK == kSums) {
+                    a.gpart[at * p.chunks + chunk] = make_float2(mean, m2);
                 } else {
-                    mul[v] *= f[1];
+                    const float rstd = rsqrtf(m2 / ((float)s.S * (float)s.Cg) + s.eps);
+                    fin[b] = make_float2(mean, rstd);
+                    if (nf + sl < s.N) { a.mean[at] = mean; a.rstd[at] = rstd; }
                 }
             }
-            const T* at = x + cv * V;
-            const X* bt = buf + j * p.rpt * kT + threadIdx.x;
-            auto load = [&](int r) { return BUF ? bt[r * kT] : load_vec<T, V>(at + r * step); };
-            walk<kBatch, X>(cnt, load, [&](const X& q, int r) {
-                float o[V];
-                widen(q, o);
-#pragma unroll
-                for (int v = 0; v < V; ++v) o[v] = fmaf(o[v] - mean[WHOLE ? 0 : v], mul[v], add[v]);
-                if (s.act == RFAST_ACT_SILU) {
-#pragma unroll
-                    for (int v = 0; v < V; ++v) o[v] *= sigmoid_of(o[v]);
-                } else if (s.act == RFAST_ACT_RELU) {
-#pragma unroll
-                    for (int v = 0; v < V; ++v) o[v] = o[v] < 0.f ? 0.f : o[v];       // a NaN stays one
-                }
-                store_vec(y + r * ostep + cv * V, o);
-            });
+        }
+        if (TASK == kSums) return;
+    } else {
+        // merge the chunks, a team of lanes per group; all chunks but the last hold p.rows positions
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        const int L = team_size(p.chunks), lane = threadIdx.x & (L - 1);
+        const float full = (float)p.rows * (float)s.Cg, last = (float)(s.S - (int64_t)(p.chunks - 1) * p.rows) * (float)s.Cg;
+        const float all = (float)s.S * (float)s.Cg;
+        for (int b0 = 0; b0 < gs; b0 += kT / L) {
+            const int g = b0 + threadIdx.x / L;
+            const bool in = g < gs;
+            const int64_t at = nf * s.G + blockIdx.y * p.gs + g;
+            const float2* q = a.gpart + at * p.chunks;
+            const float ref = in ? q[0].x : 0.f;
+            float cm = 0.f, m2 = 0.f;
+            for (int k = lane; in && k < p.chunks; k += L) cm = fmaf(k + 1 < p.chunks ? full : last, q[k].x - ref, cm);
+            const float mean = ref + team_sum(cm, L) / all;
+            for (int k = lane; in && k < p.chunks; k += L) {
+                const float2 v = q[k];
+                const float d = v.x - mean;
+                m2 += fmaf((k + 1 < p.chunks ? full : last) * d, d, v.y);
+            }
+            m2 = team_sum(m2, L);
+            if (in && lane == 0) {
+                const float rstd = rsqrtf(m2 / all + s.eps);
+                fin[g] = make_float2(mean, rstd);
+                if (chunk == 0) { a.mean[at] = mean; a.rstd[at] = rstd; }
+            }
         }
     }
-    if (p.cluster > 1) cg::this_cluster().barrier_wait();      // nobody reads this block's sums any more
+    __syncthreads();
+    if (cnt == 0) return;
+    const int64_t set = (unsigned)n / (unsigned)s.per_set;      // both below 2^31
+    const float* gam = affine_row(a, a.gamma, set) + c0;
+    const float* bet = affine_row(a, a.beta, set) + c0;
+    T* y = (T*)a.out + n * a.on + me.r0 * a.os + c0;
+    const int64_t ostep = (int64_t)p.tr * a.os;
+    for (int j = 0; j < p.cj; ++j) {
+        const int cv = me.txi + j * kT;
+        if (cv >= cols) break;
+        F2 mean[kGp], mul[kP], add[kP];                     // the mean, negated
+        int g[kGv];
+        groups_of<V, WHOLE>(cv * V, s.Cg, g);
+        affine_of<V>(gam + cv * V, a.quads, mul);
+        affine_of<V>(bet + cv * V, a.quads, add);
+        const float2* f = fin + me.sl * gs;
+        if (WHOLE) {
+            const float2 q = f[g[0]];
+            mean[0] = both(-q.x);
+#pragma unroll
+            for (int v = 0; v < kP; ++v) mul[v] = mul[v] * both(q.y);
+        } else {
+#pragma unroll
+            for (int v = 0; v < kP; ++v) {
+                const float2 q = f[g[2 * v]], r = f[g[(2 * v + 1) % kGv]];
+                mean[v] = pair(-q.x, -r.x);
+                mul[v] = mul[v] * pair(q.y, r.y);
+            }
+        }
+        const T* at = x + cv * V;
+        const X* bt = buf + j * p.rpt * kT + threadIdx.x;
+        T* to = y + cv * V;
+        auto load = [&]() {
+            if (BUF) { const X q = *bt; bt += kT; return q; }
+            const X q = load_vec<T, V>(at);
+            at += step;
+            return q;
+        };
+        walk<kBatch, X>(cnt, load, [&](const X& q) {
+            F2 o[kP];
+            widen(q, o);
+#pragma unroll
+            for (int v = 0; v < kP; ++v) o[v] = fma2(o[v] + mean[WHOLE ? 0 : v], mul[v], add[v]);
+            if (s.act == RFAST_ACT_SILU) {
+#pragma unroll
+                for (int v = 0; v < kP; ++v) o[v] = o[v] * sigmoid2(o[v]);
+            } else if (s.act == RFAST_ACT_RELU) {
+#pragma unroll
+                for (int v = 0; v < kP; ++v) {
+                    float lo, hi;
+                    split(o[v], lo, hi);
+                    o[v] = pair(lo < 0.f ? 0.f : lo, hi < 0.f ? 0.f : hi);       // a NaN stays one
+                }
+            }
+            store_vec<V>(to, o);
+            to += ostep;
+        });
+    }
 }
 
 // ---- backward -------------------------------------------------------------------------------------
 // dy act'(u)
-template <int V>
-__device__ __forceinline__ void through(int act, const float (&u)[V], float (&dy)[V]) {
+__device__ __forceinline__ F2 through(int act, F2 u, F2 dy) {
     if (act == RFAST_ACT_SILU) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const float q = sigmoid_of(u[v]);
-            dy[v] *= fmaf(q, fmaf(-q, u[v], u[v]), q);       // q (1 + u (1 - q))
-        }
-    } else if (act == RFAST_ACT_RELU) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) dy[v] = u[v] > 0.f ? dy[v] : 0.f;
+        const F2 q = sigmoid2(u);
+        float a, b;
+        split(q, a, b);
+        return dy * fma2(q, fma2(pair(-a, -b), u, u), q);    // q (1 + u (1 - q))
     }
+    if (act == RFAST_ACT_RELU) {
+        float a, b, c, d;
+        split(u, a, b);
+        split(dy, c, d);
+        return pair(a > 0.f ? c : 0.f, b > 0.f ? d : 0.f);
+    }
+    return dy;
 }
 template <class X> struct Pair { X x, d; };
+// A thread's fp32 values of a row, kept between the passes: 16 bytes (or 8) per thread and plane, so that a warp's
+// accesses spread over all banks.
+template <int P> struct alignas(P >= 2 ? 16 : 8) Plane { F2 f[P >= 2 ? 2 : 1]; };
+template <int P> constexpr int kPlanes = P >= 4 ? P / 2 : 1;
+template <int P>
+__device__ __forceinline__ void put(Plane<P>* at, const F2 (&f)[P]) {
+#pragma unroll
+    for (int k = 0; k < kPlanes<P>; ++k) {
+        Plane<P> q;
+#pragma unroll
+        for (int v = 0; v < (P >= 2 ? 2 : 1); ++v) q.f[v] = f[2 * k + v];
+        at[k * kT] = q;
+    }
+}
+template <int P>
+__device__ __forceinline__ void get(const Plane<P>* at, F2 (&f)[P]) {
+#pragma unroll
+    for (int k = 0; k < kPlanes<P>; ++k) {
+        const Plane<P> q = at[k * kT];
+#pragma unroll
+        for (int v = 0; v < (P >= 2 ? 2 : 1); ++v) f[2 * k + v] = q.f[v];
+    }
+}
 
 // With du = dy act'(u), h = (x - mean) rstd, and over the M values of a group
 //     one = sum gamma du / M, two = sum gamma du h / M:   dx = rstd (gamma du - one - two h);
-// per channel dbeta = sum du, dgamma = sum du h over the samples of a set.  A cluster takes every
-// `parts`-th item of a set and keeps the channels' sums of its items in shared memory.
-// grid = (parts * cluster, slabs, sets)
-template <class T, int V, bool WHOLE, bool BUF>
-__global__ void __launch_bounds__(kT, BUF && WHOLE ? 3 : 2)
+// per channel dbeta = sum du, dgamma = sum du h over the samples of a set.
+// kWhole, kReread: grid = (parts, slabs, sets); a block takes every `parts`-th item of a set, keeps the channels' sums of its items in
+// shared memory and, buffered, du in fp32 in the place of dy, so that the second pass has no exponentials.
+// kSums, kApply: grid = (samples of the launch * chunks, slabs); kApply runs back to front.
+template <class T, int V, bool WHOLE, int TASK>
+__global__ void __launch_bounds__(kT, WHOLE && TASK == kSums ? 3 : 2)
 k_gn_backward(const __grid_constant__ GnArgs a) {
     extern __shared__ __align__(16) uint8_t smem[];
     typedef Vec<T, V> X;
     const GnShape& s = a.s;
     const GnPlan& p = a.p;
-    constexpr int kBatch = BUF ? 2 : 4, kGv = WHOLE ? 1 : V;
+    constexpr bool BUF = TASK == kWhole, kOne = TASK == kWhole || TASK == kReread;
+    constexpr int kBatch = TASK == kApply ? 4 : 2, kP = kPairs<V>, kGv = WHOLE ? 1 : V, kGp = WHOLE ? 1 : kP;
+    typedef Plane<kP> K;
+    constexpr int kRow = kPlanes<kP> * kT;                   // planes of a row, one after the other
     X* bufx = reinterpret_cast<X*>(smem);
-    X* bufd = reinterpret_cast<X*>(smem + p.buf / 2);
-    float* ent = reinterpret_cast<float*>(smem + p.buf);     // [2][kT * V]: du, du h of a thread's channels
-    float* col = ent + 2 * kT * V;                           // [2][ns * width of a pass]: the same, summed down the positions
+    K* bufd = reinterpret_cast<K*>(smem + (size_t)p.rpt * p.cj * kT * sizeof(X));      // dy in the first plane, then du
     const int gs = min(p.gs, s.G - (int)blockIdx.y * p.gs); // the last slab may be narrower
     const int W = gs * s.Cg, nb = p.ns * gs;
     const int wide = min(p.W, kT * V);                       // channels of one pass over the width
-    float* sums = col + (p.tr > 1 ? 2 * max(kT, p.ns * wide) : 0);    // [nb][2] this block's, then [nb][2] the cluster's
-    float* tot = sums + 2 * nb;
-    float* acc = tot + 2 * nb;                               // [2][W]: dbeta, dgamma of the block's items
+    const int across = p.tr > 1 ? max(kT, p.ns * wide) : 0;
+    float* ent = reinterpret_cast<float*>(smem + p.buf);     // [2][kT * V]: du, du h of a thread's channels
+    float* col = ent + (TASK == kApply ? 0 : 2 * kT * V);    // [2][across]: the same, summed down the positions
+    float2* sums = reinterpret_cast<float2*>(col + (TASK == kApply ? 0 : 2 * across));     // [nb] the groups' two sums
+    float* acc = reinterpret_cast<float*>(sums + nb);        // [2][W]: dbeta, dgamma of the block's items
 
-    const int rank = p.cluster > 1 ? blockIdx.x % p.cluster : 0;
-    const int64_t set = blockIdx.z;
-    const Seat me = seat_of(p);
-    const int64_t r0 = (int64_t)rank * p.rows + me.rr;
-    const int64_t r1 = min(s.S, (int64_t)(rank + 1) * p.rows);
+    if (TASK == kSums) asm volatile("griddepcontrol.launch_dependents;");
+    unsigned lead = TASK == kApply ? gridDim.x - 1 - blockIdx.x : blockIdx.x, chunk = 0;
+    if (!kOne) {
+        const unsigned q = lead / (unsigned)p.chunks;
+        chunk = lead - q * p.chunks;
+        lead = q;
+    }
+    const Seat me = seat_of(s, p, chunk);
+    const int64_t set = kOne ? (int64_t)blockIdx.z : (int64_t)((unsigned)(a.n0 + lead) / (unsigned)s.per_set);
     const int c0 = blockIdx.y * p.W, cols = W / V;
     const float* gam = affine_row(a, a.gamma, set) + c0;
     const float* bet = affine_row(a, a.beta, set) + c0;
     const int64_t xstep = (int64_t)p.tr * a.xs, dstep = (int64_t)p.tr * a.ds, ostep = (int64_t)p.tr * a.os;
     const float inv_m = 1.f / ((float)s.S * (float)s.Cg);
-    for (int c = threadIdx.x; c < 2 * p.W; c += kT) acc[c] = 0.f;
+    if (TASK != kApply)
+        for (int c = threadIdx.x; c < 2 * p.W; c += kT) acc[c] = 0.f;
 
-    for (int64_t item = blockIdx.x / p.cluster; item < p.items; item += p.parts) {
-        const int64_t in_set = item * p.ns + me.sl, n = set * s.per_set + in_set;
-        const bool on = me.on && in_set < s.per_set;
-        const int cnt = on && r0 < r1 ? (int)((r1 - r0 + p.tr - 1) / p.tr) : 0;
-        const T* x = (const T*)a.x + n * a.xn + r0 * a.xs + c0;
-        const T* dy = (const T*)a.dy + n * a.dn + r0 * a.ds + c0;
-        if (BUF) {
+    const int64_t last_item = kOne ? p.items : (int64_t)lead + 1;
+    for (int64_t item = lead; item < last_item; item += p.parts) {
+        const int64_t in_set = item * p.ns + me.sl, n = kOne ? set * s.per_set + in_set : a.n0 + lead;
+        const int cnt = !kOne || in_set < s.per_set ? me.rows : 0;
+        const T* x = (const T*)a.x + n * a.xn + me.r0 * a.xs + c0;
+        const T* dy = (const T*)a.dy + n * a.dn + me.r0 * a.ds + c0;
+        if constexpr (TASK != kApply) {
+            const int lot = BUF ? (cnt + 3) / 4 : cnt;       // rows of a group of copies
+            if (BUF) {
+                for (int j = 0; j < p.cj; ++j) {
+                    const int cv = me.txi + j * kT;
+                    if (cv < cols) {
+                        const T *ax = x + cv * V, *ad = dy + cv * V;
+                        X* tx = bufx + j * p.rpt * kT + threadIdx.x;
+                        K* td = bufd + j * p.rpt * kRow + threadIdx.x;
+                        int r = 0;
+                        for (int k = 0; k < 4; ++k) {
+                            for (const int end = min(cnt, r + lot); r < end; ++r, ax += xstep, ad += dstep, tx += kT, td += kRow) {
+                                copy_async<sizeof(X)>(tx, ax);
+                                copy_async<sizeof(X)>(td, ad);
+                            }
+                            if (p.cj == 1) copies_commit();
+                        }
+                    }
+                }
+                if (p.cj > 1) { copies_commit(); copies_wait(0); }
+            }
+            for (int b = threadIdx.x; b < nb; b += kT) sums[b] = make_float2(0.f, 0.f);
             for (int j = 0; j < p.cj; ++j) {
                 const int cv = me.txi + j * kT;
-                if (cv < cols)
-                    for (int r = 0; r < cnt; ++r) {
-                        copy_async<sizeof(X)>(bufx + (j * p.rpt + r) * kT + threadIdx.x, x + r * xstep + cv * V);
-                        copy_async<sizeof(X)>(bufd + (j * p.rpt + r) * kT + threadIdx.x, dy + r * dstep + cv * V);
+                F2 s_du[kP], s_dh[kP];
+#pragma unroll
+                for (int v = 0; v < kP; ++v) s_du[v] = s_dh[v] = both(0.f);
+                if (cnt > 0 && cv < cols) {
+                    F2 mean[kGp], rs[kGp], mul[kP], add[kP]; // u = (x - mean) mul + add; the mean, negated
+                    int g[kGv];
+                    groups_of<V, WHOLE>(c0 + cv * V, s.Cg, g);
+                    affine_of<V>(gam + cv * V, a.quads, mul);
+                    affine_of<V>(bet + cv * V, a.quads, add);
+                    const float *pm = a.mean + n * s.G, *pr = a.rstd + n * s.G;
+#pragma unroll
+                    for (int v = 0; v < kGp; ++v) {
+                        const int g0 = g[WHOLE ? 0 : 2 * v], g1 = g[WHOLE ? 0 : (2 * v + 1) % kGv];
+                        mean[v] = pair(-pm[g0], -pm[g1]);
+                        rs[v] = pair(pr[g0], pr[g1]);
                     }
-            }
-            copies_landed();
-        }
-        for (int b = threadIdx.x; b < 2 * nb; b += kT) sums[b] = 0.f;
-        for (int j = 0; j < p.cj; ++j) {
-            const int cv = me.txi + j * kT;
-            float s_du[V], s_dh[V];
 #pragma unroll
-            for (int v = 0; v < V; ++v) s_du[v] = s_dh[v] = 0.f;
-            if (cnt > 0 && cv < cols) {
-                float mean[kGv], rs[kGv], mul[V], add[V];    // u = (x - mean) mul + add
-                int g[kGv];
-                groups_of<V, WHOLE>(c0 + cv * V, s.Cg, g);
-                affine_of<V>(gam + cv * V, a.quads, mul);
-                affine_of<V>(bet + cv * V, a.quads, add);
+                    for (int v = 0; v < kP; ++v) mul[v] = mul[v] * rs[WHOLE ? 0 : v];
+                    const X* bx = bufx + j * p.rpt * kT + threadIdx.x;
+                    K* bd = bufd + j * p.rpt * kRow + threadIdx.x;
+                    K* keep = bd;
+                    const T *ax = x + cv * V, *ad = dy + cv * V;
+                    auto load = [&]() {
+                        Pair<X> q;
+                        if (BUF) {
+                            q.x = *bx;
+                            q.d = *reinterpret_cast<const X*>(bd);
+                            bx += kT; bd += kRow;
+                        } else {
+                            q.x = load_vec<T, V>(ax);
+                            q.d = load_vec<T, V>(ad);
+                            ax += xstep; ad += dstep;
+                        }
+                        return q;
+                    };
+                    auto use = [&](const Pair<X>& q) {
+                        F2 d[kP], du[kP];
+                        widen(q.x, d);
+                        widen(q.d, du);
 #pragma unroll
-                for (int v = 0; v < kGv; ++v) { mean[v] = a.mean[n * s.G + g[v]]; rs[v] = a.rstd[n * s.G + g[v]]; }
-#pragma unroll
-                for (int v = 0; v < V; ++v) mul[v] *= rs[WHOLE ? 0 : v];
-                const X* bx = bufx + j * p.rpt * kT + threadIdx.x;
-                const X* bd = bufd + j * p.rpt * kT + threadIdx.x;
-                auto load = [&](int r) {
-                    Pair<X> q;
-                    q.x = BUF ? bx[r * kT] : load_vec<T, V>(x + r * xstep + cv * V);
-                    q.d = BUF ? bd[r * kT] : load_vec<T, V>(dy + r * dstep + cv * V);
-                    return q;
-                };
-                walk<kBatch, Pair<X>>(cnt, load, [&](const Pair<X>& q, int) {
-                    float d[V], du[V], u[V];
-                    widen(q.x, d);
-                    widen(q.d, du);
-#pragma unroll
-                    for (int v = 0; v < V; ++v) { d[v] -= mean[WHOLE ? 0 : v]; u[v] = fmaf(d[v], mul[v], add[v]); }
-                    through(s.act, u, du);
-#pragma unroll
-                    for (int v = 0; v < V; ++v) { s_du[v] += du[v]; s_dh[v] = fmaf(du[v], d[v], s_dh[v]); }
-                });
-#pragma unroll
-                for (int v = 0; v < V; ++v) s_dh[v] *= rs[WHOLE ? 0 : v];     // h = (x - mean) rstd
-            }
-            // [row of threads][channel of this pass]
-            if (me.on) {
-#pragma unroll
-                for (int v = 0; v < V; v += (V >= 4 ? 4 : 1)) {
-                    float *e0 = ent + threadIdx.x * V + v, *e1 = e0 + kT * V;
-                    if constexpr (V >= 4) {
-                        *reinterpret_cast<float4*>(e0) = make_float4(s_du[v], s_du[v + 1], s_du[v + 2], s_du[v + 3]);
-                        *reinterpret_cast<float4*>(e1) = make_float4(s_dh[v], s_dh[v + 1], s_dh[v + 2], s_dh[v + 3]);
+                        for (int v = 0; v < kP; ++v) {
+                            d[v] = d[v] + mean[WHOLE ? 0 : v];
+                            du[v] = through(s.act, fma2(d[v], mul[v], add[v]), du[v]);
+                            s_du[v] = s_du[v] + du[v];
+                            s_dh[v] = fma2(du[v], d[v], s_dh[v]);
+                        }
+                        if (BUF) { put<kP>(keep, du); keep += kRow; }
+                    };
+                    if (BUF && p.cj == 1) {
+                        for (int k = 0, r = 0; k < 4; ++k, r += lot) {
+                            copies_wait(3 - k);
+                            walk<kBatch, Pair<X>>(min(cnt - r, lot), load, use);
+                        }
                     } else {
-                        *e0 = s_du[v];
-                        *e1 = s_dh[v];
+                        walk<kBatch, Pair<X>>(cnt, load, use);
                     }
+#pragma unroll
+                    for (int v = 0; v < kP; ++v) s_dh[v] = s_dh[v] * rs[WHOLE ? 0 : v];     // h = (x - mean) rstd
                 }
-            }
-            __syncthreads();
-            const int pw = min(p.tx * V, W - j * kT * V);  // channels of this pass
-            const int pitch = p.tx * V;
-            const float *q0 = ent, *q1 = ent + kT * V;
-            int qp = pitch;                                  // floats between a sample's rows
-            if (p.tr > 1) {
-                // down the rows of threads, `ways` threads per channel, then their sums, in fixed order
-                const int nc = p.ns * pw, ways = nc >= kT ? 1 : min(kT / nc, p.tr);
-                float *c0s = col, *c1s = col + (kT > p.ns * wide ? kT : p.ns * wide);
-                for (int i = threadIdx.x; i < nc * ways; i += kT) {
-                    const int w = i / nc, k = i - w * nc, sl = k / pw;
-                    float u0 = 0.f, u1 = 0.f;
-                    for (int at = (sl * p.tr + w) * pitch + (k - sl * pw), r = w; r < p.tr; r += ways, at += ways * pitch) {
-                        u0 += q0[at];
-                        u1 += q1[at];
+                // [row of threads][channel of this pass]
+                if (me.on) {
+                    float *e0 = ent + threadIdx.x * V, *e1 = e0 + kT * V;
+                    if constexpr (V == 1) {
+                        float z;
+                        split(s_du[0], *e0, z);
+                        split(s_dh[0], *e1, z);
+                    } else {
+#pragma unroll
+                        for (int v = 0; v < kP; v += (kP >= 2 ? 2 : 1)) {
+                            K k0, k1;
+#pragma unroll
+                            for (int u = 0; u < (kP >= 2 ? 2 : 1); ++u) { k0.f[u] = s_du[v + u]; k1.f[u] = s_dh[v + u]; }
+                            *reinterpret_cast<K*>(e0 + 2 * v) = k0;
+                            *reinterpret_cast<K*>(e1 + 2 * v) = k1;
+                        }
                     }
-                    c0s[i] = u0;
-                    c1s[i] = u1;
                 }
                 __syncthreads();
-                if (ways > 1) {
-                    if ((int)threadIdx.x < nc) {             // nc < kT: one channel per thread
-                        float u0 = c0s[threadIdx.x], u1 = c1s[threadIdx.x];
-                        for (int w = 1; w < ways; ++w) { u0 += c0s[w * nc + threadIdx.x]; u1 += c1s[w * nc + threadIdx.x]; }
-                        c0s[threadIdx.x] = u0;
-                        c1s[threadIdx.x] = u1;
+                const int pw = min(p.tx * V, W - j * kT * V);    // channels of this pass
+                const int pitch = p.tx * V;
+                const float *q0 = ent, *q1 = ent + kT * V;
+                int qp = pitch;                              // floats between a sample's rows
+                if (p.tr > 1) {
+                    // down the rows of threads, `ways` threads per channel, then their sums, in fixed order
+                    const int nc = p.ns * pw, ways = nc >= kT ? 1 : min(kT / nc, p.tr);
+                    float *c0s = col, *c1s = col + across;
+                    for (int i = threadIdx.x; i < nc * ways; i += kT) {
+                        const int w = i / nc, k = i - w * nc, sl = k / pw;
+                        float u0 = 0.f, u1 = 0.f;
+                        for (int at = (sl * p.tr + w) * pitch + (k - sl * pw), r = w; r < p.tr; r += ways, at += ways * pitch) {
+                            u0 += q0[at];
+                            u1 += q1[at];
+                        }
+                        c0s[i] = u0;
+                        c1s[i] = u1;
                     }
                     __syncthreads();
-                }
-                q0 = c0s; q1 = c1s; qp = pw;
-            }
-            // dbeta, dgamma of this item's samples
-            for (int c = threadIdx.x; c < pw; c += kT) {
-                float u0 = 0.f, u1 = 0.f;
-                for (int sl = 0; sl < p.ns; ++sl) { u0 += q0[sl * qp + c]; u1 += q1[sl * qp + c]; }
-                acc[j * kT * V + c] += u0;
-                acc[p.W + j * kT * V + c] += u1;
-            }
-            // the groups' sums, a team of lanes per group
-            const int unit = min(s.Cg, pw), L = team_size(unit), lane = threadIdx.x & (L - 1);
-            for (int b0 = 0; b0 < nb; b0 += kT / L) {
-                const int b = b0 + threadIdx.x / L;
-                float u0 = 0.f, u1 = 0.f;
-                if (b < nb) {
-                    const int sl = b / gs, g = b - sl * gs;
-                    for (int q = lane; q < unit; q += L) {
-                        const int c = g * unit + q;
-                        const float ga = gam[j * kT * V + c];
-                        u0 = fmaf(ga, q0[sl * qp + c], u0);
-                        u1 = fmaf(ga, q1[sl * qp + c], u1);
+                    if (ways > 1) {
+                        if ((int)threadIdx.x < nc) {         // nc < kT: one channel per thread
+                            float u0 = c0s[threadIdx.x], u1 = c1s[threadIdx.x];
+                            for (int w = 1; w < ways; ++w) { u0 += c0s[w * nc + threadIdx.x]; u1 += c1s[w * nc + threadIdx.x]; }
+                            c0s[threadIdx.x] = u0;
+                            c1s[threadIdx.x] = u1;
+                        }
+                        __syncthreads();
                     }
+                    q0 = c0s; q1 = c1s; qp = pw;
+                }
+                // dbeta, dgamma of this item's samples
+                for (int c = threadIdx.x; c < pw; c += kT) {
+                    float u0 = 0.f, u1 = 0.f;
+                    for (int sl = 0; sl < p.ns; ++sl) { u0 += q0[sl * qp + c]; u1 += q1[sl * qp + c]; }
+                    acc[j * kT * V + c] += u0;
+                    acc[p.W + j * kT * V + c] += u1;
+                }
+                // the groups' sums, a team of lanes per group
+                const int unit = min(s.Cg, pw), L = team_size(unit), lane = threadIdx.x & (L - 1);
+                for (int b0 = 0; b0 < nb; b0 += kT / L) {
+                    const int b = b0 + threadIdx.x / L;
+                    float u0 = 0.f, u1 = 0.f;
+                    if (b < nb) {
+                        const int sl = p.ns > 1 ? b / gs : 0, g = b - sl * gs;
+                        for (int q = lane; q < unit; q += L) {
+                            const int c = g * unit + q;
+                            const float ga = gam[j * kT * V + c];
+                            u0 = fmaf(ga, q0[sl * qp + c], u0);
+                            u1 = fmaf(ga, q1[sl * qp + c], u1);
+                        }
+                    }
+                    u0 = team_sum(u0, L);
+                    u1 = team_sum(u1, L);
+                    if (b < nb && lane == 0) { sums[b].x += u0; sums[b].y += u1; }
+                }
+                __syncthreads();                             // before the next pass or item fills `ent`
+            }
+            if (TASK == kSums) {
+                for (int g = threadIdx.x; g < gs; g += kT) a.gpart[(n * s.G + blockIdx.y * p.gs + g) * p.chunks + chunk] = sums[g];
+                break;
+            }
+        } else {
+            // merge the chunks, a team of lanes per group
+            asm volatile("griddepcontrol.wait;" ::: "memory");
+            const int L = team_size(p.chunks), lane = threadIdx.x & (L - 1);
+            for (int b0 = 0; b0 < gs; b0 += kT / L) {
+                const int g = b0 + threadIdx.x / L;
+                float u0 = 0.f, u1 = 0.f;
+                if (g < gs) {
+                    const float2* q = a.gpart + (n * s.G + blockIdx.y * p.gs + g) * p.chunks;
+                    for (int k = lane; k < p.chunks; k += L) { const float2 v = q[k]; u0 += v.x; u1 += v.y; }
                 }
                 u0 = team_sum(u0, L);
                 u1 = team_sum(u1, L);
-                if (b < nb && lane == 0) { sums[2 * b] += u0; sums[2 * b + 1] += u1; }
+                if (g < gs && lane == 0) sums[g] = make_float2(u0, u1);
             }
-            __syncthreads();                                 // before the next pass or item fills `ent`
+            __syncthreads();
         }
-        if (p.cluster > 1) {
-            cg::cluster_group cl = cg::this_cluster();
-            cl.sync();
-            for (int b = threadIdx.x; b < 2 * nb; b += kT) {
-                float u = 0.f;
-                for (int r = 0; r < p.cluster; ++r) u += cl.map_shared_rank(sums, r)[b];
-                tot[b] = u;
-            }
-            cl.sync();                                       // `sums` may be filled again, `tot` stands
-        }
-        const float* sg = p.cluster > 1 ? tot : sums;
         if (cnt > 0) {
-            T* dx = (T*)a.out + n * a.on + r0 * a.os + c0;
+            T* dx = (T*)a.out + n * a.on + me.r0 * a.os + c0;
             for (int j = 0; j < p.cj; ++j) {
                 const int cv = me.txi + j * kT;
                 if (cv >= cols) break;
-                float mean[kGv], k1[kGv], k2[kGv], mul[V], add[V];   // dx = mul du - k1 - (x - mean) k2
+                F2 mean[kGp], k1[kGp], k2[kGp], mul[kP], add[kP];   // dx = mul du - k1 - (x - mean) k2; all but mul and add negated
                 int g[kGv];
                 groups_of<V, WHOLE>(cv * V, s.Cg, g);
                 affine_of<V>(gam + cv * V, a.quads, mul);
-                affine_of<V>(bet + cv * V, a.quads, add);
+                if (!BUF) affine_of<V>(bet + cv * V, a.quads, add);
+                const float *pm = a.mean + n * s.G + blockIdx.y * p.gs, *pr = a.rstd + n * s.G + blockIdx.y * p.gs;
+                const float2* q = sums + me.sl * gs;
 #pragma unroll
-                for (int v = 0; v < kGv; ++v) {
-                    const int64_t at = n * s.G + blockIdx.y * p.gs + g[v];
-                    const float rs = a.rstd[at], *q = sg + 2 * (me.sl * gs + g[v]);
-                    mean[v] = a.mean[at];
-                    k1[v] = rs * (q[0] * inv_m);
-                    k2[v] = rs * rs * (q[1] * inv_m);
-                    if (WHOLE) {
+                for (int v = 0; v < kGp; ++v) {
+                    const int g0 = g[WHOLE ? 0 : 2 * v], g1 = g[WHOLE ? 0 : (2 * v + 1) % kGv];
+                    const F2 rs = pair(pr[g0], pr[g1]);
+                    mean[v] = pair(-pm[g0], -pm[g1]);
+                    k1[v] = rs * pair(-inv_m * q[g0].x, -inv_m * q[g1].x);
+                    k2[v] = rs * rs * pair(-inv_m * q[g0].y, -inv_m * q[g1].y);
+                    if (!WHOLE) mul[v] = mul[v] * rs;
+                    else {
 #pragma unroll
-                        for (int u = 0; u < V; ++u) mul[u] *= rs;
-                    } else {
-                        mul[v] *= rs;
+                        for (int u = 0; u < kP; ++u) mul[u] = mul[u] * rs;
                     }
                 }
                 const X* bx = bufx + j * p.rpt * kT + threadIdx.x;
-                const X* bd = bufd + j * p.rpt * kT + threadIdx.x;
-                auto load = [&](int r) {
-                    Pair<X> q;
-                    q.x = BUF ? bx[r * kT] : load_vec<T, V>(x + r * xstep + cv * V);
-                    q.d = BUF ? bd[r * kT] : load_vec<T, V>(dy + r * dstep + cv * V);
-                    return q;
+                const K* bd = bufd + j * p.rpt * kRow + threadIdx.x;
+                const T *ax = x + cv * V, *ad = dy + cv * V;
+                T* to = dx + cv * V;
+                auto last = [&](F2 (&d)[kP], F2 (&du)[kP]) {  // d: x - mean
+#pragma unroll
+                    for (int v = 0; v < kP; ++v) du[v] = fma2(du[v], mul[v], fma2(d[v], k2[WHOLE ? 0 : v], k1[WHOLE ? 0 : v]));
+                    store_vec<V>(to, du);
+                    to += ostep;
                 };
-                walk<kBatch, Pair<X>>(cnt, load, [&](const Pair<X>& q, int r) {
-                    float d[V], du[V], u[V];
-                    widen(q.x, d);
-                    widen(q.d, du);
+                if constexpr (BUF) {
+                    struct Held { X x; F2 d[kP]; };
+                    walk<kBatch, Held>(cnt, [&]() { Held h; h.x = *bx; get<kP>(bd, h.d); bx += kT; bd += kRow; return h; }, [&](Held& h) {
+                        F2 d[kP];
+                        widen(h.x, d);
 #pragma unroll
-                    for (int v = 0; v < V; ++v) { d[v] -= mean[WHOLE ? 0 : v]; u[v] = fmaf(d[v], mul[v], add[v]); }
-                    through(s.act, u, du);
+                        for (int v = 0; v < kP; ++v) d[v] = d[v] + mean[WHOLE ? 0 : v];
+                        last(d, h.d);
+                    });
+                } else {
+                    walk<kBatch, Pair<X>>(cnt, [&]() {
+                        Pair<X> h;
+                        h.x = load_vec<T, V>(ax);
+                        h.d = load_vec<T, V>(ad);
+                        ax += xstep; ad += dstep;
+                        return h;
+                    }, [&](const Pair<X>& h) {
+                        F2 d[kP], du[kP];
+                        widen(h.x, d);
+                        widen(h.d, du);
 #pragma unroll
-                    for (int v = 0; v < V; ++v) du[v] = fmaf(du[v], mul[v], fmaf(-d[v], k2[WHOLE ? 0 : v], -k1[WHOLE ? 0 : v]));
-                    store_vec(dx + r * ostep + cv * V, du);
-                });
+                        for (int v = 0; v < kP; ++v) {
+                            d[v] = d[v] + mean[WHOLE ? 0 : v];
+                            du[v] = through(s.act, fma2(d[v], mul[v], add[v]), du[v]);
+                        }
+                        last(d, du);
+                    });
+                }
             }
         }
-        if (p.cluster == 1) __syncthreads();                 // `sums` may be filled again
+        if (TASK == kApply) return;
+        __syncthreads();                                     // `sums` may be filled again
     }
-    if (p.parts * p.cluster == 1) {
-        for (int c = threadIdx.x; c < W; c += kT) {
-            a.dbeta[set * s.C + c0 + c] = acc[c];
-            a.dgamma[set * s.C + c0 + c] = acc[p.W + c];
+    if constexpr (TASK != kApply) {
+        float *to0, *to1;                                    // dbeta, dgamma
+        if (kOne && p.parts == 1) {
+            to0 = a.dbeta + set * s.C + c0;
+            to1 = a.dgamma + set * s.C + c0;
+        } else {
+            const int64_t row = kOne ? set * p.parts + blockIdx.x : (a.n0 + lead) * p.chunks + chunk;
+            to0 = a.part + row * 2 * s.C + c0;
+            to1 = to0 + s.C;
         }
-    } else {
-        float* row = a.part + ((set * p.parts * p.cluster + blockIdx.x) * 2) * s.C + c0;
         for (int c = threadIdx.x; c < W; c += kT) {
-            row[c] = acc[c];
-            row[s.C + c] = acc[p.W + c];
+            to0[c] = acc[c];
+            to1[c] = acc[p.W + c];
         }
     }
 }
 
-// dgamma, dbeta of a set from its blocks' sums, in the order of the blocks, eight at a time, in 64 bits.
-// grid = (channels / 32, sets), 256 threads
-__global__ void __launch_bounds__(kT)
-k_gn_affine(const float* __restrict__ part, int rows, int C, float* __restrict__ dgamma, float* __restrict__ dbeta) {
-    __shared__ double sh[2][8][32];
-    const int c = blockIdx.x * 32 + (threadIdx.x & 31), w = threadIdx.x >> 5;
+// dgamma, dbeta of a set from its rows of sums, in a fixed order, in 64 bits.  grid = (channels / 32, sets), 1024 threads
+constexpr int kAffineWarps = 32;
+__global__ void __launch_bounds__(32 * kAffineWarps)
+k_gn_affine(const float* __restrict__ part, int64_t rows, int C, float* __restrict__ dgamma, float* __restrict__ dbeta) {
+    __shared__ double sh[2][kAffineWarps][32];
+    const int lane = threadIdx.x & 31, c = blockIdx.x * 32 + lane, w = threadIdx.x >> 5;
     const float* base = part + (int64_t)blockIdx.y * rows * 2 * C + c;
     double b = 0.0, g = 0.0;
-    if (c < C)
-        for (int r = w; r < rows; r += 8) {
-            b += (double)base[(int64_t)r * 2 * C];
-            g += (double)base[(int64_t)r * 2 * C + C];
+    if (c < C) {
+#pragma unroll 4
+        for (int64_t r = w; r < rows; r += kAffineWarps) {
+            b += (double)base[r * 2 * C];
+            g += (double)base[r * 2 * C + C];
         }
-    sh[0][w][threadIdx.x & 31] = b;
-    sh[1][w][threadIdx.x & 31] = g;
+    }
+    sh[0][w][lane] = b;
+    sh[1][w][lane] = g;
     __syncthreads();
     if (w < 2 && c < C) {
         double u = 0.0;
-        for (int k = 0; k < 8; ++k) u += sh[w][k][threadIdx.x & 31];
+        for (int k = 0; k < kAffineWarps; ++k) u += sh[w][k][lane];
         (w ? dgamma : dbeta)[(int64_t)blockIdx.y * C + c] = (float)u;
     }
 }
@@ -716,116 +931,150 @@ k_gn_affine(const float* __restrict__ part, int rows, int C, float* __restrict__
 // ---- host side ------------------------------------------------------------------------------------
 constexpr int kSms = 148;
 constexpr int kMaxGroupChannels = 8192;                     // a block keeps two sums for every channel of a group
-constexpr size_t kBufMost = 200 * 1024, kBufGood = 64 * 1024;
+constexpr int kMaxChunks = 512;
+constexpr size_t kMostSmem = 220 * 1024;
+constexpr int64_t kBatchBytes = (int64_t)64 << 20;          // of the samples between a launch for the sums and the one after it: half of L2
 
-// Blocks that may share a set's sums: bounds the workspace, whatever the plan.
-int64_t part_rows(const GnShape& s) {
-    const int64_t sets = s.N / s.per_set;
-    int64_t cap = 1024 / sets;
-    cap = cap < 16 ? 16 : cap > 256 ? 256 : cap;
-    const int64_t most = s.per_set * (s.S < 64 ? 1 : 16);
-    return cap < most ? cap : most;
+// Chunks of a sample's slab, a function of the shape alone (the workspace follows from it); 1: one launch.
+int chunks_of(const GnShape& s, int esize, bool backward) {
+    int64_t width = (int64_t)s.Cg * esize;                  // bytes of a slab, roughly
+    if (width < 128) width = (128 + width - 1) / width * width;
+    if (width > (int64_t)s.C * esize) width = (int64_t)s.C * esize;
+    const int64_t item = s.S * width, items = s.N * (((int64_t)s.C * esize + width - 1) / width);
+    // one launch while a slab fits the buffer (backward: x and du in fp32) and either fills the GPU or is read in about a microsecond
+    const int64_t most = backward ? 32 * 1024 : 64 * 1024;
+    if (s.S < 64 || (item <= most && (items >= kSms || item <= 16 * 1024))) return 1;
+    int64_t chunks = (item + 32 * 1024 - 1) / (32 * 1024);
+    if (items * chunks < 4 * kSms) chunks = (4 * kSms + items - 1) / items;
+    if (chunks > item / (8 * 1024)) chunks = item / (8 * 1024);
+    if (chunks > s.S / 32) chunks = s.S / 32;
+    return (int)(chunks < 2 ? 2 : chunks > kMaxChunks ? kMaxChunks : chunks);
 }
 
-size_t plan_smem(const GnShape& s, const GnPlan& p, bool backward) {
+// One launch: blocks that share a set's sums at most.
+int64_t part_rows(const GnShape& s) {
+    const int64_t sets = s.N / s.per_set;
+    int64_t cap = 2048 / sets;
+    cap = cap < 16 ? 16 : cap > 256 ? 256 : cap;
+    return cap < s.per_set ? cap : s.per_set;
+}
+
+// Bytes of the workspace: the groups' partial sums, then the channels' rows.
+size_t group_bytes(const GnShape& s, int chunks) { return chunks > 1 ? (size_t)s.N * s.G * chunks * sizeof(float2) : 0; }
+size_t row_bytes(const GnShape& s, int chunks) {
+    return (size_t)(chunks > 1 ? s.N * chunks : s.N / s.per_set * part_rows(s)) * 2 * s.C * sizeof(float);
+}
+
+size_t smem_bytes(const GnShape& s, const GnPlan& p, bool backward, int task) {
     const size_t nb = (size_t)p.ns * p.gs;
     if (!backward) {
         const size_t width = s.Cg % p.V == 0 ? 1 : p.V;
-        return p.buf + sizeof(float) * (kT + 2 * kT * width + 5 * nb);
+        return p.buf + (task == kApply ? 0 : sizeof(float) * (kT + 2 * kT * width)) + sizeof(float2) * nb;
     }
     const size_t wide = p.W < kT * p.V ? p.W : kT * p.V;
-    return p.buf + sizeof(float) * (2 * (size_t)kT * p.V + (p.tr > 1 ? 2 * (p.ns * wide > kT ? p.ns * wide : (size_t)kT) : 0) + 4 * nb + 2 * (size_t)p.W);
+    const size_t across = p.tr > 1 ? (p.ns * wide > kT ? p.ns * wide : (size_t)kT) : 0;
+    if (task == kApply) return sizeof(float2) * nb;
+    return p.buf + sizeof(float) * (2 * (size_t)kT * p.V + 2 * across + 2 * (size_t)p.W) + sizeof(float2) * nb;
 }
 
 // vmax: channels per access that addresses and strides allow (a power of two, times the type at most 16 bytes)
 GnPlan make_plan(const GnShape& s, int esize, int vmax, bool backward) {
-    GnPlan best{};
+    GnPlan p{};
     int V = vmax;
     // an access may straddle narrow groups, but a slab has to hold whole accesses
     const bool broad = s.Cg * esize >= 128;
     if (broad) { while (s.Cg % V) V /= 2; } else { while (s.C % V) V /= 2; }
     if (V * esize == 8) V /= 2;                             // accesses of 16, 4 or 2 bytes
-    const int64_t batch = backward ? s.per_set : s.N, sets = backward ? s.N / s.per_set : 1;
-    const int streams = backward ? 2 : 1;
-    for (int target = 128; target >= 32; target /= 2) {
-        GnPlan p{};
-        p.V = V;
-        p.gs = broad ? 1 : s.G;
-        if (!broad)
-            for (int gs = 1; gs < s.G; ++gs)
-                if (gs * s.Cg % V == 0 && gs * s.Cg * esize >= target) { p.gs = gs; break; }
-        p.W = p.gs * s.Cg;
-        p.slabs = (s.G + p.gs - 1) / p.gs;
-        const int cols = p.W / V;
-        p.tx = cols < kT ? cols : kT;
-        p.cj = (cols + kT - 1) / kT;
-        const int ty = kT / p.tx;
-        // thread blocks per item: enough of them to fill the SMs twice, each with at least a row per thread,
-        // and with what it reads in 64 KB of shared memory if that can be had
-        p.cluster = 1;
-        auto shape_of = [&](int cl) {
-            p.cluster = cl;
-            p.rows = (s.S + cl - 1) / cl;
-            p.tr = (int)(p.rows < ty ? p.rows : ty);
-            p.ns = 1;
-            if (cl == 1) {
-                int64_t ns = ty / p.tr;
-                if (ns > batch) ns = batch;
-                p.ns = (int)ns;
-            }
-            const int64_t rpt = (p.rows + p.tr - 1) / p.tr;
-            const int64_t bytes = rpt * p.cj * kT * V * esize * streams;
-            p.items = (batch + p.ns - 1) / p.ns;
-            p.buffered = V * esize >= 4 && bytes <= (int64_t)kBufMost;
-            p.rpt = p.buffered ? (int)rpt : 0;
-            p.buf = p.buffered ? (size_t)bytes : 0;
-            return p.items * sets * p.slabs * cl;
-        };
-        int64_t blocks = shape_of(1);
-        while (p.cluster < 16 && s.S >= 64 && p.rows > 2 * ty &&
-               (blocks < 2 * kSms || !p.buffered || p.buf > kBufGood)) blocks = shape_of(p.cluster * 2);
-        p.smem = plan_smem(s, p, backward);
-        if (p.buffered && p.smem > 220 * 1024) { p.buffered = false; p.buf = 0; p.rpt = 0; p.smem = plan_smem(s, p, backward); }
-        p.parts = 1;
-        if (backward) {
-            int64_t most = part_rows(s) / p.cluster;
-            if (most < 1) most = 1;
-            p.parts = p.items < most ? p.items : most;
-        }
-        if (target == 128) best = p;
-        else if (p.slabs > best.slabs) best = p;
-        if (blocks >= kSms || broad) break;                 // narrower slabs only where thread blocks are few
+    const int64_t batch = backward ? s.per_set : s.N;
+    p.V = V;
+    p.gs = broad ? 1 : s.G;
+    if (!broad)
+        for (int gs = 1; gs < s.G; ++gs)
+            if (gs * s.Cg % V == 0 && gs * s.Cg * esize >= 128) { p.gs = gs; break; }
+    p.W = p.gs * s.Cg;
+    p.slabs = (s.G + p.gs - 1) / p.gs;
+    const int cols = p.W / V;
+    p.tx = cols < kT ? cols : kT;
+    p.cj = (cols + kT - 1) / kT;
+    const int ty = kT / p.tx;
+    p.chunks = chunks_of(s, esize, backward);
+    p.rows = (s.S + p.chunks - 1) / p.chunks;
+    p.chunks = (int)((s.S + p.rows - 1) / p.rows);          // none is empty
+    p.tr = (int)(p.rows < ty ? p.rows : ty);
+    p.ns = 1;
+    p.parts = 1;
+    if (p.chunks > 1) return p;
+    int64_t ns = ty / p.tr;
+    p.ns = (int)(ns > batch ? batch : ns);
+    p.items = (batch + p.ns - 1) / p.ns;
+    if (backward) {
+        const int64_t most = part_rows(s);
+        p.parts = p.items < most ? p.items : most;
     }
-    return best;
+    if (V * esize >= 4) {
+        const int64_t rpt = (p.rows + p.tr - 1) / p.tr;
+        GnPlan q = p;
+        q.buffered = true;
+        q.buf = (size_t)(rpt * p.cj * kT * (V * esize + (backward ? 8 * ((V + 1) / 2) : 0)));   // x, and du in pairs
+        q.rpt = (int)rpt;
+        if (smem_bytes(s, q, backward, kWhole) <= kMostSmem) return q;
+    }
+    return p;
 }
 
 template <class K>
-cudaError_t launch_plan(K kernel, dim3 grid, const GnArgs& a, cudaStream_t st) {
-    cudaError_t e = cudaSuccess;
-    if (a.p.smem > 48 * 1024) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)a.p.smem);
-    if (e == cudaSuccess && a.p.cluster > 8) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-    if (e != cudaSuccess) return e;
+cudaError_t launch_task(K kernel, dim3 grid, const GnArgs& a, size_t smem, bool follows, cudaStream_t st) {
+    if (smem > 48 * 1024) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return e;
+    }
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = grid; cfg.blockDim = dim3(kT); cfg.dynamicSmemBytes = a.p.smem; cfg.stream = st;
-    cudaLaunchAttribute at{};
-    at.id = cudaLaunchAttributeClusterDimension;
-    at.val.clusterDim.x = a.p.cluster; at.val.clusterDim.y = 1; at.val.clusterDim.z = 1;
-    cfg.attrs = &at; cfg.numAttrs = a.p.cluster > 1 ? 1 : 0;
+    cfg.gridDim = grid; cfg.blockDim = dim3(kT); cfg.dynamicSmemBytes = smem; cfg.stream = st;
+    cudaLaunchAttribute at{};                               // the launch after the sums is on its way while they are formed
+    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &at; cfg.numAttrs = follows ? 1 : 0;
     return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 
 template <class T, int V, bool WHOLE>
-cudaError_t launch_whole(const GnArgs& a, bool backward, dim3 grid, cudaStream_t st) {
-    if constexpr (sizeof(T) * V >= 4) {
-        if (a.p.buffered) return backward ? launch_plan(k_gn_backward<T, V, WHOLE, true>, grid, a, st) : launch_plan(k_gn_forward<T, V, WHOLE, true>, grid, a, st);
+cudaError_t launch_whole(GnArgs& a, bool backward, cudaStream_t st) {
+    const GnPlan& p = a.p;
+    auto smem = [&](int task) { return smem_bytes(a.s, p, backward, task); };
+    if (p.chunks == 1) {
+        const dim3 grid((unsigned)(backward ? p.parts : p.items), p.slabs, backward ? (unsigned)(a.s.N / a.s.per_set) : 1);
+        if constexpr (sizeof(T) * V >= 4) {
+            if (p.buffered) return backward ? launch_task(k_gn_backward<T, V, WHOLE, kWhole>, grid, a, smem(kWhole), false, st)
+                                            : launch_task(k_gn_forward<T, V, WHOLE, kWhole>, grid, a, smem(kWhole), false, st);
+        }
+        return backward ? launch_task(k_gn_backward<T, V, WHOLE, kReread>, grid, a, smem(kReread), false, st)
+                        : launch_task(k_gn_forward<T, V, WHOLE, kReread>, grid, a, smem(kReread), false, st);
     }
-    return backward ? launch_plan(k_gn_backward<T, V, WHOLE, false>, grid, a, st) : launch_plan(k_gn_forward<T, V, WHOLE, false>, grid, a, st);
+    const int64_t bytes = a.s.S * a.s.C * (int64_t)sizeof(T) * (backward ? 2 : 1);
+    int64_t per = kBatchBytes / bytes;
+    if (per < 1) per = 1;
+    if (per * p.chunks > 0x7fffffff) per = 0x7fffffff / p.chunks;
+    // batches as equal as possible
+    const int64_t batches = (a.s.N + per - 1) / per;
+    per = (a.s.N + batches - 1) / batches;
+    cudaError_t e = cudaSuccess;
+    for (a.n0 = 0; a.n0 < a.s.N && e == cudaSuccess; a.n0 = a.n1) {
+        a.n1 = a.n0 + per < a.s.N ? a.n0 + per : a.s.N;
+        const dim3 grid((unsigned)((a.n1 - a.n0) * p.chunks), p.slabs, 1);
+        if (backward) {
+            e = launch_task(k_gn_backward<T, V, WHOLE, kSums>, grid, a, smem(kSums), false, st);
+            if (e == cudaSuccess) e = launch_task(k_gn_backward<T, V, WHOLE, kApply>, grid, a, smem(kApply), true, st);
+        } else {
+            e = launch_task(k_gn_forward<T, V, WHOLE, kSums>, grid, a, smem(kSums), false, st);
+            if (e == cudaSuccess) e = launch_task(k_gn_forward<T, V, WHOLE, kApply>, grid, a, smem(kApply), true, st);
+        }
+    }
+    return e;
 }
 template <class T, int V>
-cudaError_t launch_gn(const GnArgs& a, bool backward, cudaStream_t st) {
-    const dim3 grid((unsigned)((backward ? a.p.parts : a.p.items) * a.p.cluster), a.p.slabs, backward ? (unsigned)(a.s.N / a.s.per_set) : 1);
-    if (a.s.Cg % V == 0) return launch_whole<T, V, true>(a, backward, grid, st);
-    if constexpr (V > 1) return launch_whole<T, V, false>(a, backward, grid, st);
+cudaError_t launch_gn(GnArgs& a, bool backward, cudaStream_t st) {
+    if (a.s.Cg % V == 0) return launch_whole<T, V, true>(a, backward, st);
+    if constexpr (V > 1) return launch_whole<T, V, false>(a, backward, st);
     return cudaErrorInvalidValue;
 }
 
@@ -879,6 +1128,14 @@ int strides_of(const int64_t* given, const GnShape& s, int64_t* sn, int64_t* ss,
     return RFAST_OK;
 }
 
+int check_workspace(const rfast_gn_shape* g, int backward, const void* workspace, size_t bytes, const char* me, char* err, size_t err_len) {
+    const int64_t need = rfast_group_norm_workspace(g, backward);
+    if (need == 0) return RFAST_OK;
+    if (!workspace || (uintptr_t)workspace % 8 || (int64_t)bytes < need)
+        return op_fail(err, err_len, RFAST_EINVAL, "%s: the workspace needs %lld bytes, aligned to 8", me, (long long)need);
+    return check_device_pointer(workspace, "workspace", err, err_len);
+}
+
 // Whether two of the N x S rows of C values share one (rows that interleave in other ways than one stride
 // inside the other count as overlapping).
 bool overlaps(const GnShape& s, int64_t sn, int64_t ss) {
@@ -899,16 +1156,16 @@ using namespace rfast;
 extern "C" int64_t rfast_group_norm_workspace(const rfast_gn_shape* g, int backward) {
     const int rc = check_shape(g, "rfast_group_norm_workspace", nullptr, 0);
     if (rc != RFAST_OK) return rc;
-    if (!backward || g->samples == 0) return 0;
+    if (g->samples == 0 || g->positions == 0) return 0;
     const GnShape s = shape_from(g, 1.f);
-    return (s.N / s.per_set) * part_rows(s) * 2 * s.C * (int64_t)sizeof(float);
+    const int chunks = chunks_of(s, type_bytes(g->type), backward != 0);
+    return (int64_t)(group_bytes(s, chunks) + (backward ? row_bytes(s, chunks) : 0));
 }
 
 extern "C" int rfast_group_norm(const rfast_gn_shape* g, const void* d_x, const int64_t* x_strides, const float* d_gamma, const float* d_beta, float eps,
                                 void* d_y, const int64_t* y_strides, float* d_mean, float* d_rstd, void* workspace, size_t workspace_bytes,
                                 void* cuda_stream, char* err, size_t err_len) {
     const char* const me = "rfast_group_norm";
-    (void)workspace; (void)workspace_bytes;                 // none needed so far
     GN_TRY(check_shape(g, me, err, err_len));
     if (!(eps >= 1.17549435e-38f) || !std::isfinite(eps)) return op_fail(err, err_len, RFAST_EINVAL, "%s: eps must be at least 2^-126", me);
     GnArgs a{};
@@ -924,11 +1181,13 @@ extern "C" int rfast_group_norm(const rfast_gn_shape* g, const void* d_x, const 
         if (!ptrs[k]) return op_fail(err, err_len, RFAST_EINVAL, "%s: %s is null", me, names[k]);
         if ((uintptr_t)ptrs[k] % (k == 0 || k == 3 ? es : 4)) return op_fail(err, err_len, RFAST_EINVAL, "%s: %s is not aligned to its type", me, names[k]);
     }
+    GN_TRY(check_workspace(g, 0, workspace, workspace_bytes, me, err, err_len));
     for (int k = 0; k < 6; ++k) GN_TRY(check_device_pointer(ptrs[k], names[k], err, err_len));
     a.x = d_x; a.out = d_y; a.gamma = d_gamma; a.beta = d_beta; a.affine_stride = a.s.C; a.mean = d_mean; a.rstd = d_rstd;
     const int vx = allowed(d_x, a.xn, a.xs, es), vy = allowed(d_y, a.on, a.os, es);
     a.p = make_plan(a.s, es, vx < vy ? vx : vy, false);
-    if (a.p.items * a.p.cluster > 0x7fffffff || a.p.slabs > 65535) return op_fail(err, err_len, RFAST_EINVAL, "%s: too many samples or groups", me);
+    a.gpart = (float2*)workspace;
+    if (a.p.slabs > 65535) return op_fail(err, err_len, RFAST_EINVAL, "%s: too many samples or groups", me);
     const cudaError_t e = launch_typed(a, g->type, false, (cudaStream_t)cuda_stream);
     if (e != cudaSuccess) return op_fail(err, err_len, RFAST_ECUDA, "%s: kernel launch: %s", me, cudaGetErrorString(e));
     return RFAST_OK;
@@ -956,12 +1215,7 @@ extern "C" int rfast_group_norm_backward(const rfast_gn_shape* g, const void* d_
         if (!ptrs[k]) return op_fail(err, err_len, RFAST_EINVAL, "%s: %s is null", me, names[k]);
         if ((uintptr_t)ptrs[k] % (k >= 6 ? es : 4)) return op_fail(err, err_len, RFAST_EINVAL, "%s: %s is not aligned to its type", me, names[k]);
     }
-    if (a.s.S > 0) {
-        const int64_t need = rfast_group_norm_workspace(g, 1);
-        if (!workspace || (uintptr_t)workspace % 4 || (int64_t)workspace_bytes < need)
-            return op_fail(err, err_len, RFAST_EINVAL, "%s: the workspace needs %lld bytes, aligned to 4", me, (long long)need);
-        GN_TRY(check_device_pointer(workspace, "workspace", err, err_len));
-    }
+    if (a.s.S > 0) GN_TRY(check_workspace(g, 1, workspace, workspace_bytes, me, err, err_len));
     for (int k = 0; k < count; ++k) GN_TRY(check_device_pointer(ptrs[k], names[k], err, err_len));
     cudaStream_t st = (cudaStream_t)cuda_stream;
     cudaError_t e;
@@ -972,7 +1226,9 @@ extern "C" int rfast_group_norm_backward(const rfast_gn_shape* g, const void* d_
     }
     a.x = d_x; a.dy = d_dy; a.out = d_dx; a.gamma = d_gamma; a.beta = d_beta; a.affine_stride = a.s.C;
     a.mean = const_cast<float*>(d_mean); a.rstd = const_cast<float*>(d_rstd);
-    a.dgamma = d_dgamma; a.dbeta = d_dbeta; a.part = (float*)workspace;
+    a.dgamma = d_dgamma; a.dbeta = d_dbeta;
+    a.gpart = (float2*)workspace;
+    a.part = (float*)((char*)workspace + group_bytes(a.s, chunks_of(a.s, es, true)));
     int v = allowed(d_x, a.xn, a.xs, es);
     const int v2 = allowed(d_dy, a.dn, a.ds, es), v3 = allowed(d_dx, a.on, a.os, es);
     v = v < v2 ? v : v2;
@@ -980,8 +1236,9 @@ extern "C" int rfast_group_norm_backward(const rfast_gn_shape* g, const void* d_
     a.p = make_plan(a.s, es, v, true);
     if (a.p.slabs > 65535 || sets > 65535) return op_fail(err, err_len, RFAST_EINVAL, "%s: too many groups or sets", me);
     e = launch_typed(a, g->type, true, st);
-    if (e == cudaSuccess && a.p.parts * a.p.cluster > 1) {
-        k_gn_affine<<<dim3((a.s.C + 31) / 32, (unsigned)sets), kT, 0, st>>>(a.part, (int)(a.p.parts * a.p.cluster), a.s.C, d_dgamma, d_dbeta);
+    if (e == cudaSuccess && (a.p.chunks > 1 || a.p.parts > 1)) {
+        const int64_t rows = a.p.chunks > 1 ? a.s.per_set * a.p.chunks : a.p.parts;
+        k_gn_affine<<<dim3((a.s.C + 31) / 32, (unsigned)sets), 32 * kAffineWarps, 0, st>>>(a.part, rows, a.s.C, d_dgamma, d_dbeta);
         e = cudaGetLastError();
     }
     if (e != cudaSuccess) return op_fail(err, err_len, RFAST_ECUDA, "%s: kernel launch: %s", me, cudaGetErrorString(e));

@@ -38,14 +38,18 @@ SHAPES = {
     "ragged slab": (2, 19, 200, 25, 1),
     "prime groups": (2, 5, 309, 103, 1),
     "twenty a group": (2, 301, 40, 2, 1),
-    "cluster": (1, 5001, 128, 32, 1),
-    "cluster of wide groups": (2, 4000, 256, 2, 1),
+    "long": (1, 5001, 128, 32, 1),
+    "long, wide groups": (2, 4000, 256, 2, 1),
+    "long, sets": (4, 1300, 64, 4, 2),
+    "many of middle length": (200, 81, 64, 8, 4),
     "wide group": (2, 3, 8192, 1, 1),
     "wide odd group": (2, 9, 4097, 1, 2),
-    "too long to keep": (1, 40_003, 64, 8, 1),
+    "wide group, too large to keep": (2, 20, 8192, 1, 2),
+    "very long": (1, 40_003, 64, 8, 1),
+    "very long, wide odd group": (1, 700, 4097, 1, 1),
     "seventeen positions": (9, 17, 64, 4, 3),
 }
-LONG = ("too long to keep",)
+LONG = ("very long", "very long, wide odd group")
 
 
 def _torch():
@@ -85,9 +89,12 @@ class _Case:
         x = self.x if x is None else x
         y = self.room() if out is None else out
         stats = torch.full((2, self.n, self.g), 7.0, device="cuda")
+        need = pkg.rfast_group_norm_workspace(**self.shape(act))
+        work = torch.full((need,), 255, dtype=torch.uint8, device="cuda")         # NaNs: only what was written may be read
         torch.cuda.synchronize()
         pkg.rfast_group_norm(x.data_ptr(), self.gamma.data_ptr(), self.beta.data_ptr(), y.data_ptr(), stats[0].data_ptr(), stats[1].data_ptr(), eps=EPS,
-                             x_strides=x.stride()[:2], y_strides=y.stride()[:2], cuda_stream=stream, **self.shape(act))
+                             x_strides=x.stride()[:2], y_strides=y.stride()[:2], workspace=work.data_ptr(), workspace_bytes=need, cuda_stream=stream,
+                             **self.shape(act))
         torch.cuda.synchronize()
         return y, stats[0], stats[1]
 
@@ -193,7 +200,7 @@ def test_group_norm_and_its_gradients(rfast_lib, shape, kind, act):
 
 @pytest.mark.parametrize("pad,lead", [(8, 0), (8, 8), (2, 0), (3, 0), (0, 1), (5, 3)])
 @pytest.mark.parametrize("kind", ["f32", "bf16"])
-@pytest.mark.parametrize("shape", ["odd", "ten a group", "hidden layer", "cluster", "seventeen positions"])
+@pytest.mark.parametrize("shape", ["odd", "ten a group", "hidden layer", "long", "seventeen positions"])
 def test_strides_and_alignment(rfast_lib, shape, kind, pad, lead):
     """Operands inside wider tensors, from any address: what lies around the results stays."""
     c = _Case(SHAPES[shape], kind, seed=2, pad=pad, lead=lead)
@@ -205,7 +212,7 @@ def test_strides_and_alignment(rfast_lib, shape, kind, pad, lead):
     assert _outside_stands(back[0])
 
 
-@pytest.mark.parametrize("shape", ["hidden layer", "ten a group", "cluster", "too long to keep", "wide odd group"])
+@pytest.mark.parametrize("shape", ["hidden layer", "ten a group", "long", "very long", "wide odd group"])
 def test_in_place_and_repeated_runs_give_the_same_bits(rfast_lib, shape):
     torch, _ = _torch()
     c = _Case(SHAPES[shape], "bf16", seed=3)
@@ -240,7 +247,7 @@ def test_positions_of_another_order_and_repeated_ones(rfast_lib):
 
 
 @pytest.mark.parametrize("bad", [np.nan, np.inf, -np.inf])
-@pytest.mark.parametrize("shape", ["ten a group", "hidden layer", "cluster"])
+@pytest.mark.parametrize("shape", ["ten a group", "hidden layer", "long"])
 def test_bad_values_stay_in_their_group(rfast_lib, shape, bad):
     c = _Case(SHAPES[shape], "f32", seed=6)
     good = [_np(t) for t in c.forward("silu")]
@@ -283,7 +290,7 @@ def test_recorded_passes_and_side_by_side(rfast_lib):
     """Both passes captured and replayed; two graphs with a workspace each replayed on two streams."""
     import paper_2307_11617_b200 as pkg
     torch, _ = _torch()
-    cases = [_Case(SHAPES["ten a group"], "f16", seed=k) for k in (11, 12)]
+    cases = [_Case(SHAPES[name], "f16", seed=k) for k, name in ((11, "ten a group"), (12, "ten a group"), (13, "long"), (14, "long"))]
     want, graphs, outs, streams = [], [], [], []
     for c in cases:
         f = c.forward("silu")
@@ -291,15 +298,15 @@ def test_recorded_passes_and_side_by_side(rfast_lib):
         stream = torch.cuda.Stream()
         y, dx = c.room(), c.room()
         stats, da = torch.zeros(2, c.n, c.g, device="cuda"), torch.zeros(2, c.sets, c.c, device="cuda")
-        need = pkg.rfast_group_norm_workspace(backward=True, **c.shape("silu"))
-        work = torch.empty(need, dtype=torch.uint8, device="cuda")
+        first, need = (pkg.rfast_group_norm_workspace(backward=b, **c.shape("silu")) for b in (False, True))
+        work = torch.empty(first + need, dtype=torch.uint8, device="cuda")
         graph = torch.cuda.CUDAGraph()
         torch.cuda.synchronize()
         with torch.cuda.graph(graph, stream=stream):
             pkg.rfast_group_norm(c.x.data_ptr(), c.gamma.data_ptr(), c.beta.data_ptr(), y.data_ptr(), stats[0].data_ptr(), stats[1].data_ptr(), eps=EPS,
-                                 cuda_stream=stream.cuda_stream, **c.shape("silu"))
+                                 workspace=work.data_ptr(), workspace_bytes=first, cuda_stream=stream.cuda_stream, **c.shape("silu"))
             pkg.rfast_group_norm_backward(c.dy.data_ptr(), c.x.data_ptr(), c.gamma.data_ptr(), c.beta.data_ptr(), stats[0].data_ptr(),
-                                          stats[1].data_ptr(), dx.data_ptr(), da[0].data_ptr(), da[1].data_ptr(), workspace=work.data_ptr(),
+                                          stats[1].data_ptr(), dx.data_ptr(), da[0].data_ptr(), da[1].data_ptr(), workspace=work.data_ptr() + first,
                                           workspace_bytes=need, cuda_stream=stream.cuda_stream, **c.shape("silu"))
         graphs.append(graph)
         outs.append([y, stats[0], stats[1], dx, da[0], da[1], work])

@@ -151,7 +151,7 @@ def test_group_norm_refuses_operands(rfast_lib, text, kw):
 
 @pytest.mark.parametrize("text,kw", [
     ("dy is null", dict(dy=0)), ("dgamma is null", dict(dgamma=0)), ("mean is null", dict(mean=0)), ("dx is not aligned", dict(dx=A + 2)),
-    ("workspace needs", dict(workspace_bytes=0)), ("workspace needs", dict(workspace=0)), ("workspace needs", dict(workspace=A + 2)),
+    ("workspace needs", dict(workspace_bytes=0)), ("workspace needs", dict(workspace=0)), ("workspace needs", dict(workspace=A + 4)),
     ("strides of dx", dict(dx_strides=(60, 12))), ("stride of dy is negative", dict(dy_strides=(-72, 12))),
 ])
 def test_group_norm_backward_refuses_operands(rfast_lib, text, kw):
