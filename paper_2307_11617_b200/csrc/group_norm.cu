@@ -139,23 +139,56 @@ __device__ __forceinline__ F2 sigmoid2(F2 u) {
 }
 
 // cnt rows of a thread, R at a time: all loads of a batch go out before the first row is worked on (a store in
-// between would hold later loads back, the operands being allowed to coincide).
-template <int R, class Row, class Load, class Use>
+// between would hold later loads back, the operands being allowed to coincide).  AHEAD: from memory, and the next batch's loads go
+// out before this one's work, so that two batches cover the latency.
+template <int R, bool AHEAD, class Row, class Load, class Use>
 __device__ __forceinline__ void walk(int cnt, Load load, Use use) {
     int r = 0;
+    if constexpr (AHEAD) {
+        Row q[R], n[R];
+        if (cnt >= R) {
+#pragma unroll
+            for (int k = 0; k < R; ++k) q[k] = load();
+        }
 #pragma unroll 1
-    for (; r + R <= cnt; r += R) {
-        Row q[R];
+        for (; r + R <= cnt; r += R) {
+            if (r + 2 * R <= cnt) {
 #pragma unroll
-        for (int k = 0; k < R; ++k) q[k] = load();
+                for (int k = 0; k < R; ++k) n[k] = load();
+            }
 #pragma unroll
-        for (int k = 0; k < R; ++k) use(q[k]);
+            for (int k = 0; k < R; ++k) use(q[k]);
+#pragma unroll
+            for (int k = 0; k < R; ++k) q[k] = n[k];
+        }
+        // the rest, fewer than R: together
+#pragma unroll
+        for (int k = 0; k < R - 1; ++k) if (r + k < cnt) q[k] = load();
+#pragma unroll
+        for (int k = 0; k < R - 1; ++k) if (r + k < cnt) use(q[k]);
+    } else {
+#pragma unroll 1
+        for (; r + R <= cnt; r += R) {
+            Row q[R];
+#pragma unroll
+            for (int k = 0; k < R; ++k) q[k] = load();
+#pragma unroll
+            for (int k = 0; k < R; ++k) use(q[k]);
+        }
+#pragma unroll 1
+        for (; r < cnt; ++r) { Row q = load(); use(q); }
     }
-#pragma unroll 1
-    for (; r < cnt; ++r) { Row q = load(); use(q); }
 }
 
 // ---- geometry, chosen on the host -------------------------------------------------------------------
+// Quotients of numbers below 2^16 by a divisor that the host knows: one multiplication.  m = floor(2^32 / d) + 1 overshoots
+// 2^32 / d by at most 1, so the product's high word is exact while n d < 2^32.
+struct Divisor {
+    uint32_t m;                        // 0: d = 1
+    int d;
+    __host__ void set(int64_t v) { d = (int)v; m = v == 1 ? 0u : (uint32_t)(((uint64_t)1 << 32) / (uint64_t)v + 1); }
+    __device__ __forceinline__ unsigned of(unsigned n) const { return m ? __umulhi(n, m) : n; }
+};
 struct GnShape {
     int64_t N, S;                      // samples, positions
     int C, G, Cg;                      // channels, groups, channels per group
@@ -170,6 +203,8 @@ struct GnPlan {
     int tr, ns;                        // threads down the positions of a sample, samples per item
     int chunks;                        // thread blocks per sample and slab; 1: one launch does it all
     int64_t rows;                      // positions per thread block
+    int each, more, each_end, more_end;    // per thread: `each` of them, the first `more` rows of threads one more; in the last chunk
+    Divisor by_tx, by_tr, by_gs, by_cg, by_unit;    // by_unit: entries of a group in one row of threads
     int rpt;                           // positions per thread (buffered)
     bool buffered;                     // what was read waits in shared memory
     int64_t items;                     // one launch: items per set (forward: over all samples)
@@ -210,21 +245,19 @@ __device__ __forceinline__ const float* affine_row(const GnArgs& a, const float*
 struct Seat {
     int txi, sl, rr;                   // column of threads, sample within the item, row of the sample's threads
     int64_t r0;                        // first position
-    int have;                          // positions of the thread block
     int rows;                          // positions of this thread where its sample exists
     bool on;
 };
 __device__ __forceinline__ Seat seat_of(const GnShape& g, const GnPlan& p, unsigned chunk) {
     Seat s;
-    const unsigned tyi = threadIdx.x / (unsigned)p.tx;
+    const unsigned tyi = p.by_tx.of(threadIdx.x);
     s.txi = threadIdx.x - tyi * p.tx;
-    s.sl = p.ns == 1 ? (tyi < (unsigned)p.tr ? 0 : 1) : tyi / (unsigned)p.tr;
+    s.sl = p.by_tr.of(tyi);
     s.rr = tyi - s.sl * p.tr;
     s.on = s.sl < p.ns;
     s.r0 = (int64_t)chunk * p.rows + s.rr;
-    const int64_t left = g.S - (int64_t)chunk * p.rows;     // fits 32 bits: there are fewer than 2^31 positions
-    s.have = (int)(left < p.rows ? (left < 0 ? 0 : left) : p.rows);
-    s.rows = s.on && s.rr < s.have ? (int)(((unsigned)(s.have - s.rr) + p.tr - 1) / (unsigned)p.tr) : 0;
+    const bool end = chunk + 1 == (unsigned)p.chunks;
+    s.rows = s.on ? (end ? p.each_end : p.each) + (s.rr < (end ? p.more_end : p.more) ? 1 : 0) : 0;
     return s;
 }
 
@@ -247,8 +280,9 @@ __device__ __forceinline__ void affine_of(const float* p, bool quads, F2 (&f)[kP
 }
 // groups of V neighbouring channels from channel c on: one (WHOLE) or one per channel
 template <int V, bool WHOLE>
-__device__ __forceinline__ void groups_of(int c, int cg, int (&g)[WHOLE ? 1 : V]) {
-    int q = c / cg;
+__device__ __forceinline__ void groups_of(int c, const Divisor& by_cg, int (&g)[WHOLE ? 1 : V]) {
+    const int cg = by_cg.d;
+    int q = by_cg.of(c);
     g[0] = q;
     if constexpr (!WHOLE) {
         int rest = c - q * cg;
@@ -272,16 +306,16 @@ __device__ __forceinline__ int team_size(int entries) {
 }
 
 // ---- forward --------------------------------------------------------------------------------------
-// kWhole, kReread: grid = (items, slabs).  kSums, kApply: grid = (samples of the launch * chunks, slabs); kApply runs back to front.
+// kWhole, kReread: grid = (items, slabs).  kSums, kApply: grid = (chunks, slabs, samples of the launch); kApply runs back to front.
 template <class T, int V, bool WHOLE, int TASK>
-__global__ void __launch_bounds__(kT, WHOLE ? 4 : 3)
+__global__ void __launch_bounds__(kT, WHOLE && TASK == kWhole ? 4 : 3)
 k_gn_forward(const __grid_constant__ GnArgs a) {
     extern __shared__ __align__(16) uint8_t smem[];
     typedef Vec<T, V> X;
     const GnShape& s = a.s;
     const GnPlan& p = a.p;
     constexpr bool BUF = TASK == kWhole, kOne = TASK == kWhole || TASK == kReread;
-    constexpr int kBatch = TASK == kSums ? 8 : 4, kP = kPairs<V>, kGv = WHOLE ? 1 : V, kGp = WHOLE ? 1 : kP, kAcc = WHOLE ? (kP < 2 ? 1 : 2) : kP;
+    constexpr int kBatch = 4, kP = kPairs<V>, kGv = WHOLE ? 1 : V, kGp = WHOLE ? 1 : kP, kAcc = WHOLE ? (kP < 2 ? 1 : 2) : kP;
     X* buf = reinterpret_cast<X*>(smem);
     // per thread (WHOLE: an access stays inside a group) or per thread and channel: count, mean, sum of squared deviations
     constexpr int width = kGv, kEnt = TASK == kApply ? 0 : kT;
@@ -289,16 +323,12 @@ k_gn_forward(const __grid_constant__ GnArgs a) {
     float* e_mean = e_n + kEnt;
     float* e_m2 = e_mean + kEnt * width;
     const int gs = min(p.gs, s.G - (int)blockIdx.y * p.gs); // the last slab may be narrower
-    const int nb = p.ns * gs;
+    const int nb = p.ns * p.gs;
     float2* fin = reinterpret_cast<float2*>(e_m2 + kEnt * width);      // [nb] mean, rstd
 
     if (TASK == kSums) asm volatile("griddepcontrol.launch_dependents;");
-    unsigned item = TASK == kApply ? gridDim.x - 1 - blockIdx.x : blockIdx.x, chunk = 0;
-    if (!kOne) {
-        const unsigned q = item / (unsigned)p.chunks;
-        chunk = item - q * p.chunks;
-        item = q;
-    }
+    const unsigned item = kOne ? blockIdx.x : TASK == kApply ? gridDim.z - 1 - blockIdx.z : blockIdx.z;
+    const unsigned chunk = kOne ? 0u : TASK == kApply ? gridDim.x - 1 - blockIdx.x : blockIdx.x;
     const Seat me = seat_of(s, p, chunk);
     const int64_t nf = kOne ? (int64_t)item * p.ns : a.n0 + item, n = nf + me.sl;    // first sample of the block, this thread's
     const int cnt = n < s.N ? me.rows : 0;
@@ -371,10 +401,10 @@ k_gn_forward(const __grid_constant__ GnArgs a) {
                 if (BUF && p.cj == 1) {
                     for (int k = 0, r = 0; k < 4; ++k, r += lot) {
                         if (k) copies_wait(3 - k);
-                        walk<kBatch, X>(min(cnt - r, lot), load, use);
+                        walk<kBatch, !BUF, X>(min(cnt - r, lot), load, use);
                     }
                 } else {
-                    walk<kBatch, X>(cnt, load, use);
+                    walk<kBatch, !BUF, X>(cnt, load, use);
                 }
                 if (WHOLE) {
                     if (kAcc == 2) { s1[0] = s1[0] + s1[kAcc - 1]; s2[0] = s2[0] + s2[kAcc - 1]; }
@@ -384,7 +414,7 @@ k_gn_forward(const __grid_constant__ GnArgs a) {
                     split(s2[0], lo, hi);
                     s2[0] = both(V > 1 ? lo + hi : lo);
                 }
-                const float nn = (float)cnt * (WHOLE ? V : 1), inv = 1.f / nn;
+                const float nn = (float)cnt * (WHOLE ? V : 1), inv = __frcp_rn(nn);
 #pragma unroll
                 for (int v = 0; v < kGp; ++v) {
                     float a1[2], a2[2];
@@ -421,13 +451,13 @@ k_gn_forward(const __grid_constant__ GnArgs a) {
         const int entries = unit * p.tr, L = team_size(entries), lane = threadIdx.x & (L - 1);
         for (int b0 = 0; b0 < nb; b0 += kT / L) {
             const int b = b0 + threadIdx.x / L;
-            const bool in = b < nb;
-            const int sl = in && p.ns > 1 ? b / gs : 0, g = in ? b - sl * gs : 0;
+            const int sl = p.ns > 1 ? (int)p.by_gs.of(b) : 0, g = b - sl * p.gs;
+            const bool in = b < nb && g < gs;
             // means are summed as differences from one of them: a flat group has exactly its level
             const float ref = in ? e_mean[sl * p.tr * p.tx * width + g * unit] : 0.f;
             float cn = 0.f, cm = 0.f;
             for (int q = lane; in && q < entries; q += L) {
-                const int row = q / unit, t = (sl * p.tr + row) * p.tx, u = g * unit + (q - row * unit);
+                const int row = p.by_unit.of(q), t = (sl * p.tr + row) * p.tx, u = g * unit + (q - row * unit);
                 const float k = e_n[t + (WHOLE ? u : u / V)];
                 cn += k;
                 if (k > 0.f) cm = fmaf(k, e_mean[t * width + u] - ref, cm);
@@ -437,7 +467,7 @@ k_gn_forward(const __grid_constant__ GnArgs a) {
             const float mean = cn > 0.f ? ref + cm / cn : 0.f;
             float m2 = 0.f;
             for (int q = lane; in && q < entries; q += L) {
-                const int row = q / unit, t = (sl * p.tr + row) * p.tx, u = g * unit + (q - row * unit);
+                const int row = p.by_unit.of(q), t = (sl * p.tr + row) * p.tx, u = g * unit + (q - row * unit);
                 const float k = e_n[t + (WHOLE ? u : u / V)];
                 if (k > 0.f) {
                     const float d = e_mean[t * width + u] - mean;
@@ -497,10 +527,10 @@ k_gn_forward(const __grid_constant__ GnArgs a) {
         if (cv >= cols) break;
         F2 mean[kGp], mul[kP], add[kP];                     // the mean, negated
         int g[kGv];
-        groups_of<V, WHOLE>(cv * V, s.Cg, g);
+        groups_of<V, WHOLE>(cv * V, p.by_cg, g);
         affine_of<V>(gam + cv * V, a.quads, mul);
         affine_of<V>(bet + cv * V, a.quads, add);
-        const float2* f = fin + me.sl * gs;
+        const float2* f = fin + me.sl * p.gs;
         if (WHOLE) {
             const float2 q = f[g[0]];
             mean[0] = both(-q.x);
@@ -523,7 +553,7 @@ k_gn_forward(const __grid_constant__ GnArgs a) {
             at += step;
             return q;
         };
-        walk<kBatch, X>(cnt, load, [&](const X& q) {
+        walk<kBatch, !BUF, X>(cnt, load, [&](const X& q) {
             F2 o[kP];
             widen(q, o);
 #pragma unroll
@@ -587,27 +617,57 @@ __device__ __forceinline__ void get(const Plane<P>* at, F2 (&f)[P]) {
     }
 }
 
+// dgamma, dbeta of 32 channels of a set from the set's rows of sums, by a thread block, in a fixed order, in 64 bits.
+__device__ __forceinline__ void affine_sums(const float* part, int64_t rows, int C, int64_t set, int c32, float* dgamma, float* dbeta) {
+    __shared__ double sh[2][kT / 32][32];
+    const int lane = threadIdx.x & 31, c = c32 * 32 + lane, w = threadIdx.x >> 5;
+    const float* base = part + set * rows * 2 * C + c;
+    double b = 0.0, g = 0.0;
+    if (c < C) {
+#pragma unroll 4
+        for (int64_t r = w; r < rows; r += kT / 32) {
+            b += (double)base[r * 2 * C];
+            g += (double)base[r * 2 * C + C];
+        }
+    }
+    __syncthreads();                                         // a block may have several turns
+    sh[0][w][lane] = b;
+    sh[1][w][lane] = g;
+    __syncthreads();
+    if (w < 2 && c < C) {
+        double u = 0.0;
+        for (int k = 0; k < kT / 32; ++k) u += sh[w][k][lane];
+        (w ? dgamma : dbeta)[set * C + c] = (float)u;
+    }
+}
+// grid = (channels / 32, sets)
+__global__ void __launch_bounds__(kT)
+k_gn_affine(const float* __restrict__ part, int64_t rows, int C, float* __restrict__ dgamma, float* __restrict__ dbeta) {
+    affine_sums(part, rows, C, blockIdx.y, blockIdx.x, dgamma, dbeta);
+}
+
 // With du = dy act'(u), h = (x - mean) rstd, and over the M values of a group
 //     one = sum gamma du / M, two = sum gamma du h / M:   dx = rstd (gamma du - one - two h);
 // per channel dbeta = sum du, dgamma = sum du h over the samples of a set.
 // kWhole, kReread: grid = (parts, slabs, sets); a block takes every `parts`-th item of a set, keeps the channels' sums of its items in
 // shared memory and, buffered, du in fp32 in the place of dy, so that the second pass has no exponentials.
-// kSums, kApply: grid = (samples of the launch * chunks, slabs); kApply runs back to front.
+// kSums, kApply: grid = (chunks, slabs, samples of the launch); kApply runs back to front, its last launch with one slab more, whose
+// blocks form dgamma and dbeta meanwhile.
 template <class T, int V, bool WHOLE, int TASK>
-__global__ void __launch_bounds__(kT, WHOLE && TASK == kSums ? 3 : 2)
+__global__ void __launch_bounds__(kT, 2)
 k_gn_backward(const __grid_constant__ GnArgs a) {
     extern __shared__ __align__(16) uint8_t smem[];
     typedef Vec<T, V> X;
     const GnShape& s = a.s;
     const GnPlan& p = a.p;
     constexpr bool BUF = TASK == kWhole, kOne = TASK == kWhole || TASK == kReread;
-    constexpr int kBatch = TASK == kApply ? 4 : 2, kP = kPairs<V>, kGv = WHOLE ? 1 : V, kGp = WHOLE ? 1 : kP;
+    constexpr int kBatch = BUF ? 2 : 3, kP = kPairs<V>, kGv = WHOLE ? 1 : V, kGp = WHOLE ? 1 : kP;
     typedef Plane<kP> K;
     constexpr int kRow = kPlanes<kP> * kT;                   // planes of a row, one after the other
     X* bufx = reinterpret_cast<X*>(smem);
     K* bufd = reinterpret_cast<K*>(smem + (size_t)p.rpt * p.cj * kT * sizeof(X));      // dy in the first plane, then du
     const int gs = min(p.gs, s.G - (int)blockIdx.y * p.gs); // the last slab may be narrower
-    const int W = gs * s.Cg, nb = p.ns * gs;
+    const int W = gs * s.Cg, nb = p.ns * p.gs;
     const int wide = min(p.W, kT * V);                       // channels of one pass over the width
     const int across = p.tr > 1 ? max(kT, p.ns * wide) : 0;
     float* ent = reinterpret_cast<float*>(smem + p.buf);     // [2][kT * V]: du, du h of a thread's channels
@@ -615,13 +675,17 @@ k_gn_backward(const __grid_constant__ GnArgs a) {
     float2* sums = reinterpret_cast<float2*>(col + (TASK == kApply ? 0 : 2 * across));     // [nb] the groups' two sums
     float* acc = reinterpret_cast<float*>(sums + nb);        // [2][W]: dbeta, dgamma of the block's items
 
-    if (TASK == kSums) asm volatile("griddepcontrol.launch_dependents;");
-    unsigned lead = TASK == kApply ? gridDim.x - 1 - blockIdx.x : blockIdx.x, chunk = 0;
-    if (!kOne) {
-        const unsigned q = lead / (unsigned)p.chunks;
-        chunk = lead - q * p.chunks;
-        lead = q;
+    if (TASK == kApply && blockIdx.y == (unsigned)p.slabs) {
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        const int64_t rows = s.per_set * p.chunks;
+        const unsigned tiles = (s.C + 31) / 32, sets = (unsigned)s.N / (unsigned)s.per_set;
+        for (int64_t t = blockIdx.x + (int64_t)blockIdx.z * gridDim.x; t < (int64_t)tiles * sets; t += (int64_t)gridDim.x * gridDim.z)
+            affine_sums(a.part, rows, s.C, t / tiles, (int)(t % tiles), a.dgamma, a.dbeta);
+        return;
     }
+    if (TASK == kSums) asm volatile("griddepcontrol.launch_dependents;");
+    const unsigned lead = kOne ? blockIdx.x : TASK == kApply ? gridDim.z - 1 - blockIdx.z : blockIdx.z;
+    const unsigned chunk = kOne ? 0u : TASK == kApply ? gridDim.x - 1 - blockIdx.x : blockIdx.x;
     const Seat me = seat_of(s, p, chunk);
     const int64_t set = kOne ? (int64_t)blockIdx.z : (int64_t)((unsigned)(a.n0 + lead) / (unsigned)s.per_set);
     const int c0 = blockIdx.y * p.W, cols = W / V;
@@ -668,10 +732,10 @@ k_gn_backward(const __grid_constant__ GnArgs a) {
                 if (cnt > 0 && cv < cols) {
                     F2 mean[kGp], rs[kGp], mul[kP], add[kP]; // u = (x - mean) mul + add; the mean, negated
                     int g[kGv];
-                    groups_of<V, WHOLE>(c0 + cv * V, s.Cg, g);
+                    groups_of<V, WHOLE>(cv * V, p.by_cg, g);
                     affine_of<V>(gam + cv * V, a.quads, mul);
                     affine_of<V>(bet + cv * V, a.quads, add);
-                    const float *pm = a.mean + n * s.G, *pr = a.rstd + n * s.G;
+                    const float *pm = a.mean + n * s.G + blockIdx.y * p.gs, *pr = a.rstd + n * s.G + blockIdx.y * p.gs;
 #pragma unroll
                     for (int v = 0; v < kGp; ++v) {
                         const int g0 = g[WHOLE ? 0 : 2 * v], g1 = g[WHOLE ? 0 : (2 * v + 1) % kGv];
@@ -713,10 +777,10 @@ k_gn_backward(const __grid_constant__ GnArgs a) {
                     if (BUF && p.cj == 1) {
                         for (int k = 0, r = 0; k < 4; ++k, r += lot) {
                             copies_wait(3 - k);
-                            walk<kBatch, Pair<X>>(min(cnt - r, lot), load, use);
+                            walk<kBatch, !BUF, Pair<X>>(min(cnt - r, lot), load, use);
                         }
                     } else {
-                        walk<kBatch, Pair<X>>(cnt, load, use);
+                        walk<kBatch, !BUF, Pair<X>>(cnt, load, use);
                     }
 #pragma unroll
                     for (int v = 0; v < kP; ++v) s_dh[v] = s_dh[v] * rs[WHOLE ? 0 : v];     // h = (x - mean) rstd
@@ -782,8 +846,9 @@ k_gn_backward(const __grid_constant__ GnArgs a) {
                 for (int b0 = 0; b0 < nb; b0 += kT / L) {
                     const int b = b0 + threadIdx.x / L;
                     float u0 = 0.f, u1 = 0.f;
-                    if (b < nb) {
-                        const int sl = p.ns > 1 ? b / gs : 0, g = b - sl * gs;
+                    const int sl = p.ns > 1 ? (int)p.by_gs.of(b) : 0, g = b - sl * p.gs;
+                    const bool in = b < nb && g < gs;
+                    if (in) {
                         for (int q = lane; q < unit; q += L) {
                             const int c = g * unit + q;
                             const float ga = gam[j * kT * V + c];
@@ -793,7 +858,7 @@ k_gn_backward(const __grid_constant__ GnArgs a) {
                     }
                     u0 = team_sum(u0, L);
                     u1 = team_sum(u1, L);
-                    if (b < nb && lane == 0) { sums[b].x += u0; sums[b].y += u1; }
+                    if (in && lane == 0) { sums[b].x += u0; sums[b].y += u1; }
                 }
                 __syncthreads();                             // before the next pass or item fills `ent`
             }
@@ -825,11 +890,11 @@ k_gn_backward(const __grid_constant__ GnArgs a) {
                 if (cv >= cols) break;
                 F2 mean[kGp], k1[kGp], k2[kGp], mul[kP], add[kP];   // dx = mul du - k1 - (x - mean) k2; all but mul and add negated
                 int g[kGv];
-                groups_of<V, WHOLE>(cv * V, s.Cg, g);
+                groups_of<V, WHOLE>(cv * V, p.by_cg, g);
                 affine_of<V>(gam + cv * V, a.quads, mul);
                 if (!BUF) affine_of<V>(bet + cv * V, a.quads, add);
                 const float *pm = a.mean + n * s.G + blockIdx.y * p.gs, *pr = a.rstd + n * s.G + blockIdx.y * p.gs;
-                const float2* q = sums + me.sl * gs;
+                const float2* q = sums + me.sl * p.gs;
 #pragma unroll
                 for (int v = 0; v < kGp; ++v) {
                     const int g0 = g[WHOLE ? 0 : 2 * v], g1 = g[WHOLE ? 0 : (2 * v + 1) % kGv];
@@ -855,7 +920,7 @@ k_gn_backward(const __grid_constant__ GnArgs a) {
                 };
                 if constexpr (BUF) {
                     struct Held { X x; F2 d[kP]; };
-                    walk<kBatch, Held>(cnt, [&]() { Held h; h.x = *bx; get<kP>(bd, h.d); bx += kT; bd += kRow; return h; }, [&](Held& h) {
+                    walk<kBatch, false, Held>(cnt, [&]() { Held h; h.x = *bx; get<kP>(bd, h.d); bx += kT; bd += kRow; return h; }, [&](Held& h) {
                         F2 d[kP];
                         widen(h.x, d);
 #pragma unroll
@@ -863,7 +928,7 @@ k_gn_backward(const __grid_constant__ GnArgs a) {
                         last(d, h.d);
                     });
                 } else {
-                    walk<kBatch, Pair<X>>(cnt, [&]() {
+                    walk<kBatch, !BUF, Pair<X>>(cnt, [&]() {
                         Pair<X> h;
                         h.x = load_vec<T, V>(ax);
                         h.d = load_vec<T, V>(ad);
@@ -903,37 +968,21 @@ k_gn_backward(const __grid_constant__ GnArgs a) {
     }
 }
 
-// dgamma, dbeta of a set from its rows of sums, in a fixed order, in 64 bits.  grid = (channels / 32, sets), 1024 threads
-constexpr int kAffineWarps = 32;
-__global__ void __launch_bounds__(32 * kAffineWarps)
-k_gn_affine(const float* __restrict__ part, int64_t rows, int C, float* __restrict__ dgamma, float* __restrict__ dbeta) {
-    __shared__ double sh[2][kAffineWarps][32];
-    const int lane = threadIdx.x & 31, c = blockIdx.x * 32 + lane, w = threadIdx.x >> 5;
-    const float* base = part + (int64_t)blockIdx.y * rows * 2 * C + c;
-    double b = 0.0, g = 0.0;
-    if (c < C) {
-#pragma unroll 4
-        for (int64_t r = w; r < rows; r += kAffineWarps) {
-            b += (double)base[r * 2 * C];
-            g += (double)base[r * 2 * C + C];
-        }
-    }
-    sh[0][w][lane] = b;
-    sh[1][w][lane] = g;
-    __syncthreads();
-    if (w < 2 && c < C) {
-        double u = 0.0;
-        for (int k = 0; k < kAffineWarps; ++k) u += sh[w][k][lane];
-        (w ? dgamma : dbeta)[(int64_t)blockIdx.y * C + c] = (float)u;
-    }
-}
-
 // ---- host side ------------------------------------------------------------------------------------
 constexpr int kSms = 148;
 constexpr int kMaxGroupChannels = 8192;                     // a block keeps two sums for every channel of a group
 constexpr int kMaxChunks = 512;
 constexpr size_t kMostSmem = 220 * 1024;
 constexpr int64_t kBatchBytes = (int64_t)64 << 20;          // of the samples between a launch for the sums and the one after it: half of L2
+
+// Samples between a launch for the sums and the one after it: as many as half the L2 cache holds, in batches as equal as possible.
+int64_t batch_of(const GnShape& s, int esize, bool backward) {
+    int64_t per = kBatchBytes / (s.S * s.C * esize * (backward ? 2 : 1));
+    if (per < 1) per = 1;
+    if (per > 65535) per = 65535;
+    const int64_t batches = (s.N + per - 1) / per;
+    return (s.N + batches - 1) / batches;
+}
 
 // Chunks of a sample's slab, a function of the shape alone (the workspace follows from it); 1: one launch.
 int chunks_of(const GnShape& s, int esize, bool backward) {
@@ -944,8 +993,9 @@ int chunks_of(const GnShape& s, int esize, bool backward) {
     // one launch while a slab fits the buffer (backward: x and du in fp32) and either fills the GPU or is read in about a microsecond
     const int64_t most = backward ? 32 * 1024 : 64 * 1024;
     if (s.S < 64 || (item <= most && (items >= kSms || item <= 16 * 1024))) return 1;
-    int64_t chunks = (item + 32 * 1024 - 1) / (32 * 1024);
-    if (items * chunks < 4 * kSms) chunks = (4 * kSms + items - 1) / items;
+    // one thread block on every third (backward: half) of an SM at a time: what a thread sets up serves all its positions
+    const int64_t at_once = items / s.N * batch_of(s, esize, backward);
+    int64_t chunks = (backward ? 2 : 3) * kSms / at_once;
     if (chunks > item / (8 * 1024)) chunks = item / (8 * 1024);
     if (chunks > s.S / 32) chunks = s.S / 32;
     return (int)(chunks < 2 ? 2 : chunks > kMaxChunks ? kMaxChunks : chunks);
@@ -1003,6 +1053,11 @@ GnPlan make_plan(const GnShape& s, int esize, int vmax, bool backward) {
     p.tr = (int)(p.rows < ty ? p.rows : ty);
     p.ns = 1;
     p.parts = 1;
+    const int64_t end = s.S - (p.chunks - 1) * p.rows;
+    p.each = (int)(p.rows / p.tr); p.more = (int)(p.rows % p.tr);
+    p.each_end = (int)(end / p.tr); p.more_end = (int)(end % p.tr);
+    const int unit = s.Cg % V == 0 ? s.Cg / V : s.Cg;
+    p.by_tx.set(p.tx); p.by_tr.set(p.tr); p.by_gs.set(p.gs); p.by_cg.set(s.Cg); p.by_unit.set(unit < p.tx || s.Cg % V ? unit : p.tx);
     if (p.chunks > 1) return p;
     int64_t ns = ty / p.tr;
     p.ns = (int)(ns > batch ? batch : ns);
@@ -1050,20 +1105,15 @@ cudaError_t launch_whole(GnArgs& a, bool backward, cudaStream_t st) {
         return backward ? launch_task(k_gn_backward<T, V, WHOLE, kReread>, grid, a, smem(kReread), false, st)
                         : launch_task(k_gn_forward<T, V, WHOLE, kReread>, grid, a, smem(kReread), false, st);
     }
-    const int64_t bytes = a.s.S * a.s.C * (int64_t)sizeof(T) * (backward ? 2 : 1);
-    int64_t per = kBatchBytes / bytes;
-    if (per < 1) per = 1;
-    if (per * p.chunks > 0x7fffffff) per = 0x7fffffff / p.chunks;
-    // batches as equal as possible
-    const int64_t batches = (a.s.N + per - 1) / per;
-    per = (a.s.N + batches - 1) / batches;
+    const int64_t per = batch_of(a.s, (int)sizeof(T), backward);
     cudaError_t e = cudaSuccess;
     for (a.n0 = 0; a.n0 < a.s.N && e == cudaSuccess; a.n0 = a.n1) {
         a.n1 = a.n0 + per < a.s.N ? a.n0 + per : a.s.N;
-        const dim3 grid((unsigned)((a.n1 - a.n0) * p.chunks), p.slabs, 1);
+        const dim3 grid(p.chunks, p.slabs, (unsigned)(a.n1 - a.n0));
         if (backward) {
             e = launch_task(k_gn_backward<T, V, WHOLE, kSums>, grid, a, smem(kSums), false, st);
-            if (e == cudaSuccess) e = launch_task(k_gn_backward<T, V, WHOLE, kApply>, grid, a, smem(kApply), true, st);
+            const dim3 more(grid.x, p.slabs + (a.n1 == a.s.N ? 1 : 0), grid.z);
+            if (e == cudaSuccess) e = launch_task(k_gn_backward<T, V, WHOLE, kApply>, more, a, smem(kApply), true, st);
         } else {
             e = launch_task(k_gn_forward<T, V, WHOLE, kSums>, grid, a, smem(kSums), false, st);
             if (e == cudaSuccess) e = launch_task(k_gn_forward<T, V, WHOLE, kApply>, grid, a, smem(kApply), true, st);
@@ -1234,11 +1284,10 @@ extern "C" int rfast_group_norm_backward(const rfast_gn_shape* g, const void* d_
     v = v < v2 ? v : v2;
     v = v < v3 ? v : v3;
     a.p = make_plan(a.s, es, v, true);
-    if (a.p.slabs > 65535 || sets > 65535) return op_fail(err, err_len, RFAST_EINVAL, "%s: too many groups or sets", me);
+    if (a.p.slabs > 65534 || sets > 65535) return op_fail(err, err_len, RFAST_EINVAL, "%s: too many groups or sets", me);
     e = launch_typed(a, g->type, true, st);
-    if (e == cudaSuccess && (a.p.chunks > 1 || a.p.parts > 1)) {
-        const int64_t rows = a.p.chunks > 1 ? a.s.per_set * a.p.chunks : a.p.parts;
-        k_gn_affine<<<dim3((a.s.C + 31) / 32, (unsigned)sets), 32 * kAffineWarps, 0, st>>>(a.part, rows, a.s.C, d_dgamma, d_dbeta);
+    if (e == cudaSuccess && a.p.chunks == 1 && a.p.parts > 1) {
+        k_gn_affine<<<dim3((a.s.C + 31) / 32, (unsigned)sets), kT, 0, st>>>(a.part, a.p.parts, a.s.C, d_dgamma, d_dbeta);
         e = cudaGetLastError();
     }
     if (e != cudaSuccess) return op_fail(err, err_len, RFAST_ECUDA, "%s: kernel launch: %s", me, cudaGetErrorString(e));

@@ -36,6 +36,7 @@ SHAPES = {
     "three a group": (2, 50, 96, 32, 1),
     "ten a group": (2, 330, 320, 32, 2),
     "ragged slab": (2, 19, 200, 25, 1),
+    "ragged slab, few positions": (7, 3, 200, 25, 1),
     "prime groups": (2, 5, 309, 103, 1),
     "twenty a group": (2, 301, 40, 2, 1),
     "long": (1, 5001, 128, 32, 1),
