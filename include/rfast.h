@@ -533,7 +533,7 @@ int rfast_adamw_step(const rfast_adamw* a, void* cuda_stream, char* err, size_t 
  * Backward, from dy and the forward pass's x, mean, rstd (act'(0) = 0 for max(u, 0)):
  *     du = dy act'(u);  dbeta = sum du, dgamma = sum du h over the samples of a set (fp32)
  *     dx = rstd (gamma du - sum(gamma du) / M - h sum(gamma du h) / M)
- * workspace: rfast_group_norm_workspace(shape, backward) bytes of DEVICE memory, aligned to 8 (0 for
+ * workspace: rfast_group_norm_workspace(shape, backward) bytes of DEVICE memory, aligned to 16 (0 for
  * many shapes: it may then be NULL); its size depends on the shape alone.  No positions: nothing is normalised, dgamma and dbeta are zero. */
 enum { RFAST_ACT_NONE = 0, RFAST_ACT_RELU = 1, RFAST_ACT_SILU = 2 };
 typedef struct rfast_gn_shape {

@@ -6,9 +6,11 @@
 // of whole groups that is at least 128 bytes wide.  There are two ways through a sample's slab:
 //   - one thread block takes it whole (or several samples' where they have few positions).  What a thread has read for the
 //     sums waits in shared memory: asynchronous copies that only this thread reads back, so no barrier guards them;
-//   - slabs that are too large for that, or too few to fill the GPU, are cut into chunks of positions: one launch for the
-//     chunks' sums, one that merges them and goes over the values again.  Samples are taken in batches that the L2
-//     cache holds, the second launch starting from the end, so that its reads are served there.
+//   - slabs that are too large for that, or too few to fill the GPU, are laid end to end, all their positions in one row,
+//     and the row is cut into as many equal spans as thread blocks run at a time: one launch for the sums of each slab's part
+//     in a span, one that merges them and goes over the values again.  Every SM has the same work, and what a thread
+//     sets up serves as many positions as can be.  Samples are taken in batches that the L2 cache holds, the second
+//     launch starting from the end, so that its reads are served there.
 // The sums of a slab could also meet inside a cluster of thread blocks that keep the slab in their shared memory.  Built and
 // measured: loading, summing and writing then follow one another on the whole GPU, and 32 x 3136 x 256 bf16 took 37 us
 // forward and 122 us backward.
@@ -125,60 +127,69 @@ __device__ __forceinline__ void copies_wait(int left) {
     }
 }
 
-// 1 / (1 + exp(-u)).  2^t and the reciprocal are the hardware's (2 ulp and 1 ulp), t is rounded once: the result is good
-// to about 2^-23.  u = -inf gives 0.
+// 1 / (1 + exp(-u)) of a pair.  2^t and the reciprocal are the hardware's (2 ulp and 1 ulp), t and the products are rounded
+// once each: the result is good to about 2^-22.  The special function unit, with a result every other cycle where the
+// adders have eight, is what bounds a pass with this in it, so one reciprocal, of the product of both denominators, serves
+// two values (3 instead of 4 of its operations per pair).  To keep the product in range exp(-u) stops growing at 2^60: below
+// u = -41 the result is 2^-60.
 __device__ __forceinline__ F2 sigmoid2(F2 u) {
     float a, b;
     split(u * both(-1.4426950408889634f), a, b);
+    asm("min.NaN.f32 %0, %0, %1;" : "+f"(a) : "f"(60.f));
+    asm("min.NaN.f32 %0, %0, %1;" : "+f"(b) : "f"(60.f));
     asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(a));
     asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(b));
     split(pair(a, b) + both(1.f), a, b);
-    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(a));
-    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(b));
-    return pair(a, b);
+    float r = a * b;
+    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(r));
+    return pair(b, a) * both(r);
 }
 
-// cnt rows of a thread, R at a time: all loads of a batch go out before the first row is worked on (a store in
-// between would hold later loads back, the operands being allowed to coincide).  AHEAD: from memory, and the next batch's loads go
-// out before this one's work, so that two batches cover the latency.
-template <int R, bool AHEAD, class Row, class Load, class Use>
+// cnt rows of a thread out of shared memory, R at a time: all loads of a batch go out before the first row is worked on.
+template <int R, class Row, class Load, class Use>
 __device__ __forceinline__ void walk(int cnt, Load load, Use use) {
     int r = 0;
-    if constexpr (AHEAD) {
-        Row q[R], n[R];
-        if (cnt >= R) {
-#pragma unroll
-            for (int k = 0; k < R; ++k) q[k] = load();
-        }
 #pragma unroll 1
-        for (; r + R <= cnt; r += R) {
-            if (r + 2 * R <= cnt) {
+    for (; r + R <= cnt; r += R) {
+        Row q[R];
 #pragma unroll
-                for (int k = 0; k < R; ++k) n[k] = load();
-            }
+        for (int k = 0; k < R; ++k) q[k] = load();
+#pragma unroll
+        for (int k = 0; k < R; ++k) use(q[k]);
+    }
+#pragma unroll 1
+    for (; r < cnt; ++r) { Row q = load(); use(q); }
+}
+// The same out of memory: a batch's loads go out before the batch ahead of it is worked on (its stores would hold them back,
+// the operands being allowed to coincide), the first batch's as early as the caller likes.
+template <int R, class Row> struct Ahead {
+    Row q[R];
+    template <class Load> __device__ __forceinline__ void begin(int cnt, Load& load) {
+#pragma unroll
+        for (int k = 0; k < R; ++k) if (k < cnt) q[k] = load();
+    }
+    template <class Load, class Use> __device__ __forceinline__ void run(int cnt, Load& load, Use use) {
+        int r = 0;
+#pragma unroll 1
+        for (; r + 2 * R <= cnt; r += R) {
+            Row n[R];
+#pragma unroll
+            for (int k = 0; k < R; ++k) n[k] = load();
 #pragma unroll
             for (int k = 0; k < R; ++k) use(q[k]);
 #pragma unroll
             for (int k = 0; k < R; ++k) q[k] = n[k];
         }
-        // the rest, fewer than R: together
+        const int left = cnt - r;                            // fewer than 2 R; the first R of them are here
+        Row n[R - 1];
 #pragma unroll
-        for (int k = 0; k < R - 1; ++k) if (r + k < cnt) q[k] = load();
+        for (int k = 0; k < R - 1; ++k) if (R + k < left) n[k] = load();
 #pragma unroll
-        for (int k = 0; k < R - 1; ++k) if (r + k < cnt) use(q[k]);
-    } else {
-#pragma unroll 1
-        for (; r + R <= cnt; r += R) {
-            Row q[R];
+        for (int k = 0; k < R; ++k) if (k < left) use(q[k]);
 #pragma unroll
-            for (int k = 0; k < R; ++k) q[k] = load();
-#pragma unroll
-            for (int k = 0; k < R; ++k) use(q[k]);
-        }
-#pragma unroll 1
-        for (; r < cnt; ++r) { Row q = load(); use(q); }
+        for (int k = 0; k < R - 1; ++k) if (R + k < left) use(n[k]);
     }
-}
+};
 
 // ---- geometry, chosen on the host -------------------------------------------------------------------
 // Quotients of numbers below 2^16 by a divisor that the host knows: one multiplication.  m = floor(2^32 / d) + 1 overshoots
@@ -201,9 +212,12 @@ struct GnPlan {
     int W, gs, slabs;                  // channels and groups of a slab
     int tx, cj;                        // threads across the slab, passes over its width
     int tr, ns;                        // threads down the positions of a sample, samples per item
-    int chunks;                        // thread blocks per sample and slab; 1: one launch does it all
-    int64_t rows;                      // positions per thread block
-    int each, more, each_end, more_end;    // per thread: `each` of them, the first `more` rows of threads one more; in the last chunk
+    bool spans;                        // two launches over spans; otherwise one, a thread block taking whole slabs
+    int64_t per;                       // positions in a span
+    int64_t total;                     // positions of all slabs of a launch
+    int pieces;                        // spans that a slab can lie in, at most
+    int blocks;                        // spans, at most
+    int each, more;                    // one launch: positions per thread, the first `more` rows of threads one more
     Divisor by_tx, by_tr, by_gs, by_cg, by_unit;    // by_unit: entries of a group in one row of threads
     int rpt;                           // positions per thread (buffered)
     bool buffered;                     // what was read waits in shared memory
@@ -226,14 +240,14 @@ struct GnArgs {
     int set_row_stride;
     float *mean, *rstd;                // [N][G]: out (forward), in (backward)
     float *dgamma, *dbeta;             // backward: where the sums of a set go
-    float2* gpart;                     // chunks: [N][G][chunks] mean and squared deviations, or the two sums of the backward pass
+    float4* gpart;                     // spans: [N][G][pieces] count, mean and squared deviations, or the two sums of the backward pass
     float* part;                       // backward: rows of [2][C], du and du h summed; a row per thread block of a set or per
-                                       // sample and chunk
-    int64_t n0, n1;                    // chunks: samples of this launch
+                                       // sample and piece
+    int64_t n0;                        // spans: first sample of this launch
 };
 
 // A thread block's task: everything in one launch (what it reads kept in shared memory, or read twice where that is too small
-// or accesses are too narrow), the chunks' sums, or what follows from them.
+// or accesses are too narrow), the sums over a span, or what follows from them.
 enum { kWhole = 0, kSums = 1, kApply = 2, kReread = 3 };
 
 __device__ __forceinline__ const float* affine_row(const GnArgs& a, const float* base, int64_t set) {
@@ -244,22 +258,43 @@ __device__ __forceinline__ const float* affine_row(const GnArgs& a, const float*
 // What a thread is in its block: column, sample of the item, first position; the same for both directions.
 struct Seat {
     int txi, sl, rr;                   // column of threads, sample within the item, row of the sample's threads
-    int64_t r0;                        // first position
-    int rows;                          // positions of this thread where its sample exists
+    int rows;                          // one launch: positions of this thread
     bool on;
 };
-__device__ __forceinline__ Seat seat_of(const GnShape& g, const GnPlan& p, unsigned chunk) {
+__device__ __forceinline__ Seat seat_of(const GnPlan& p) {
     Seat s;
     const unsigned tyi = p.by_tx.of(threadIdx.x);
     s.txi = threadIdx.x - tyi * p.tx;
     s.sl = p.by_tr.of(tyi);
     s.rr = tyi - s.sl * p.tr;
     s.on = s.sl < p.ns;
-    s.r0 = (int64_t)chunk * p.rows + s.rr;
-    const bool end = chunk + 1 == (unsigned)p.chunks;
-    s.rows = s.on ? (end ? p.each_end : p.each) + (s.rr < (end ? p.more_end : p.more) ? 1 : 0) : 0;
+    s.rows = s.on ? p.each + (s.rr < p.more ? 1 : 0) : 0;
     return s;
 }
+
+// The part of a slab that a span holds.  Slabs lie end to end, those of a sample next to one another.
+struct Part {
+    int64_t n;                         // sample
+    int slab;
+    int64_t from;                      // positions [from, from + count)
+    int count;
+    int piece, pieces;                 // which of the slab's parts this is, and how many it has
+};
+__device__ __forceinline__ Part part_at(const GnArgs& a, int64_t at, int64_t end, int64_t span) {
+    Part q;
+    const int64_t item = (int64_t)((uint64_t)at / (uint64_t)a.s.S);
+    q.from = at - item * a.s.S;
+    const int64_t left = a.s.S - q.from;
+    q.count = (int)(left < end - at ? left : end - at);
+    const unsigned n = (unsigned)item / (unsigned)a.p.slabs;     // a launch has fewer than 2^31 slabs
+    q.slab = (int)(item - (int64_t)n * a.p.slabs);
+    q.n = a.n0 + n;
+    const int64_t first = (int64_t)((uint64_t)(at - q.from) / (uint64_t)a.p.per), last = (int64_t)((uint64_t)(at - q.from + a.s.S - 1) / (uint64_t)a.p.per);
+    q.piece = (int)(span - first);
+    q.pieces = (int)(last - first) + 1;
+    return q;
+}
+__device__ __forceinline__ int rows_of(int count, int rr, int tr) { return rr < count ? (int)((unsigned)(count - rr - 1) / (unsigned)tr) + 1 : 0; }
 
 // scale or shift of V neighbouring channels
 template <int V>
@@ -306,7 +341,7 @@ __device__ __forceinline__ int team_size(int entries) {
 }
 
 // ---- forward --------------------------------------------------------------------------------------
-// kWhole, kReread: grid = (items, slabs).  kSums, kApply: grid = (chunks, slabs, samples of the launch); kApply runs back to front.
+// kWhole, kReread: grid = (items, slabs).  kSums, kApply: grid = spans; kApply takes them back to front.
 template <class T, int V, bool WHOLE, int TASK>
 __global__ void __launch_bounds__(kT, WHOLE && TASK == kWhole ? 4 : 3)
 k_gn_forward(const __grid_constant__ GnArgs a) {
@@ -322,256 +357,273 @@ k_gn_forward(const __grid_constant__ GnArgs a) {
     float* e_n = reinterpret_cast<float*>(smem + p.buf);
     float* e_mean = e_n + kEnt;
     float* e_m2 = e_mean + kEnt * width;
-    const int gs = min(p.gs, s.G - (int)blockIdx.y * p.gs); // the last slab may be narrower
     const int nb = p.ns * p.gs;
     float2* fin = reinterpret_cast<float2*>(e_m2 + kEnt * width);      // [nb] mean, rstd
-
+    const Seat me = seat_of(p);
+    const int64_t step = (int64_t)p.tr * a.xs, ostep = (int64_t)p.tr * a.os;
     if (TASK == kSums) asm volatile("griddepcontrol.launch_dependents;");
-    const unsigned item = kOne ? blockIdx.x : TASK == kApply ? gridDim.z - 1 - blockIdx.z : blockIdx.z;
-    const unsigned chunk = kOne ? 0u : TASK == kApply ? gridDim.x - 1 - blockIdx.x : blockIdx.x;
-    const Seat me = seat_of(s, p, chunk);
-    const int64_t nf = kOne ? (int64_t)item * p.ns : a.n0 + item, n = nf + me.sl;    // first sample of the block, this thread's
-    const int cnt = n < s.N ? me.rows : 0;
-    const int c0 = blockIdx.y * p.W, cols = gs * s.Cg / V;
-    const T* x = (const T*)a.x + n * a.xn + me.r0 * a.xs + c0;
-    const int64_t step = (int64_t)p.tr * a.xs;
+    bool waited = false;
 
-    if constexpr (TASK != kApply) {
-        // what is read comes in up to four lots of rows; the first is worked on while the others are on their way
-        const int lot = BUF ? (cnt + 3) / 4 : cnt;
-        if (BUF) {
+    const int64_t span = TASK == kApply ? gridDim.x - 1 - blockIdx.x : blockIdx.x;
+    int64_t at = kOne ? 0 : span * p.per;
+    const int64_t end = kOne ? 1 : min(at + p.per, p.total);
+    while (at < end) {
+        Part part;
+        if (kOne) {
+            part.n = (int64_t)blockIdx.x * p.ns; part.slab = blockIdx.y; part.from = 0;
+            at = end;
+        } else {
+            part = part_at(a, at, end, span);
+            at += part.count;
+        }
+        const int slab = part.slab, gs = min(p.gs, s.G - slab * p.gs);      // the last slab may be narrower
+        const int64_t n = part.n + me.sl, r0 = part.from + me.rr;            // this thread's sample and first position
+        const int cnt = kOne ? (n < s.N ? me.rows : 0) : me.on ? rows_of(part.count, me.rr, p.tr) : 0;
+        const int c0 = slab * p.W, cols = gs * s.Cg / V;
+        const T* x = (const T*)a.x + n * a.xn + r0 * a.xs + c0;
+        const T* px = x + me.txi * V;                        // of the pass over the width that is under way
+        auto load = [&]() { const X q = load_vec<T, V>(px); px += step; return q; };
+        Ahead<kBatch, X> rows;
+
+        if constexpr (TASK != kApply) {
+            // what is read comes in up to four lots of rows; the first is worked on while the others are on their way
+            const int lot = BUF ? (cnt + 3) / 4 : cnt;
+            if (BUF) {
+                for (int j = 0; j < p.cj; ++j) {
+                    const int cv = me.txi + j * kT;
+                    if (cv < cols) {
+                        const T* from = x + cv * V;
+                        X* to = buf + j * p.rpt * kT + threadIdx.x;
+                        int r = 0;
+                        for (int k = 0; k < 4; ++k) {
+                            for (const int stop = min(cnt, r + lot); r < stop; ++r, from += step, to += kT) copy_async<sizeof(X)>(to, from);
+                            if (p.cj == 1) copies_commit();
+                        }
+                    }
+                }
+                if (p.cj > 1) { copies_commit(); copies_wait(0); }
+            }
+            // count, mean and squared deviations of what this thread holds
+            float t_n = 0.f, t_mean = 0.f, t_m2 = 0.f;
             for (int j = 0; j < p.cj; ++j) {
                 const int cv = me.txi + j * kT;
-                if (cv < cols) {
-                    const T* at = x + cv * V;
-                    X* to = buf + j * p.rpt * kT + threadIdx.x;
-                    int r = 0;
-                    for (int k = 0; k < 4; ++k) {
-                        for (const int end = min(cnt, r + lot); r < end; ++r, at += step, to += kT) copy_async<sizeof(X)>(to, at);
-                        if (p.cj == 1) copies_commit();
+                F2 first[kGp], s1[kAcc], s2[kAcc];           // the first value, negated
+#pragma unroll
+                for (int v = 0; v < kAcc; ++v) s1[v] = s2[v] = both(0.f);
+                float mean[2 * kGp], m2[2 * kGp];
+#pragma unroll
+                for (int v = 0; v < 2 * kGp; ++v) mean[v] = m2[v] = 0.f;
+                if (cnt > 0 && cv < cols) {
+                    const X* bt = buf + j * p.rpt * kT + threadIdx.x;
+                    X x0;
+                    if constexpr (BUF) {
+                        if (p.cj == 1) copies_wait(3);
+                        x0 = *bt;
+                    } else {
+                        px = x + cv * V;
+                        rows.begin(cnt, load);
+                        x0 = rows.q[0];
                     }
-                }
-            }
-            if (p.cj > 1) { copies_commit(); copies_wait(0); }
-        }
-        // count, mean and squared deviations of what this thread holds
-        float t_n = 0.f, t_mean = 0.f, t_m2 = 0.f;
-        for (int j = 0; j < p.cj; ++j) {
-            const int cv = me.txi + j * kT;
-            F2 first[kGp], s1[kAcc], s2[kAcc];               // the first value, negated
+                    {
+                        F2 f[kP];
+                        widen(x0, f);
 #pragma unroll
-            for (int v = 0; v < kAcc; ++v) s1[v] = s2[v] = both(0.f);
+                        for (int v = 0; v < kGp; ++v) {
+                            float lo, hi;
+                            split(f[v], lo, hi);
+                            mean[2 * v] = lo;
+                            mean[2 * v + 1] = WHOLE ? lo : hi;
+                            first[v] = pair(-lo, WHOLE ? -lo : -hi);
+                        }
+                    }
+                    auto use = [&](const X& q) {             // a first value counts as a deviation of 0
+                        F2 f[kP];
+                        widen(q, f);
 #pragma unroll
-            for (int v = 0; v < kGp; ++v) first[v] = both(0.f);
-            float mean[2 * kGp], m2[2 * kGp];
-#pragma unroll
-            for (int v = 0; v < 2 * kGp; ++v) mean[v] = m2[v] = 0.f;
-            if (cnt > 0 && cv < cols) {
-                const T* at = x + cv * V;
-                const X* bt = buf + j * p.rpt * kT + threadIdx.x;
-                auto load = [&]() {
-                    if (BUF) { const X q = *bt; bt += kT; return q; }
-                    const X q = load_vec<T, V>(at);
-                    at += step;
-                    return q;
-                };
-                if (BUF && p.cj == 1) copies_wait(3);
-                {
-                    F2 f[kP];
-                    widen(BUF ? *bt : load_vec<T, V>(at), f);
+                        for (int v = 0; v < kP; ++v) {
+                            const F2 d = f[v] + first[WHOLE ? 0 : v];
+                            s1[v % kAcc] = s1[v % kAcc] + d;
+                            s2[v % kAcc] = fma2(d, d, s2[v % kAcc]);
+                        }
+                    };
+                    if constexpr (BUF) {
+                        auto held = [&]() { const X q = *bt; bt += kT; return q; };
+                        if (p.cj == 1) {
+                            for (int k = 0, r = 0; k < 4; ++k, r += lot) {
+                                if (k) copies_wait(3 - k);
+                                walk<kBatch, X>(min(cnt - r, lot), held, use);
+                            }
+                        } else {
+                            walk<kBatch, X>(cnt, held, use);
+                        }
+                    } else {
+                        rows.run(cnt, load, use);
+                    }
+                    if (WHOLE) {
+                        if (kAcc == 2) { s1[0] = s1[0] + s1[kAcc - 1]; s2[0] = s2[0] + s2[kAcc - 1]; }
+                        float lo, hi;
+                        split(s1[0], lo, hi);
+                        s1[0] = both(V > 1 ? lo + hi : lo);
+                        split(s2[0], lo, hi);
+                        s2[0] = both(V > 1 ? lo + hi : lo);
+                    }
+                    const float nn = (float)cnt * (WHOLE ? V : 1), inv = __frcp_rn(nn);
 #pragma unroll
                     for (int v = 0; v < kGp; ++v) {
-                        float lo, hi;
-                        split(f[v], lo, hi);
-                        mean[2 * v] = lo;
-                        mean[2 * v + 1] = WHOLE ? lo : hi;
-                        first[v] = pair(-lo, WHOLE ? -lo : -hi);
+                        float a1[2], a2[2];
+                        split(s1[v], a1[0], a1[1]);
+                        split(s2[v], a2[0], a2[1]);
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            const float d = a1[k] * inv;
+                            m2[2 * v + k] = fmaxf(fmaf(-a1[k], d, a2[k]), 0.f) + (a2[k] - a2[k]);   // the second term is a NaN where there was one
+                            mean[2 * v + k] += d;
+                        }
+                    }
+                    if (WHOLE && t_n > 0.f) {                // a further pass over a wide group
+                        const float d = mean[0] - t_mean, tot = t_n + nn;
+                        t_mean += d * (nn / tot);
+                        t_m2 += m2[0] + d * d * (t_n * nn / tot);
+                        t_n = tot;
+                    } else {
+                        t_mean = mean[0]; t_m2 = m2[0]; t_n = nn;
                     }
                 }
-                auto use = [&](const X& q) {                 // a first value counts as a deviation of 0
-                    F2 f[kP];
-                    widen(q, f);
+                if (!WHOLE) {                                // a slab of several groups is never wider than the block
+                    if (me.on && cv < cols) {
+#pragma unroll
+                        for (int v = 0; v < kGv; ++v) { e_mean[threadIdx.x * V + v] = mean[v]; e_m2[threadIdx.x * V + v] = m2[v]; }
+                    }
+                }
+            }
+            e_n[threadIdx.x] = t_n;
+            if (WHOLE) { e_mean[threadIdx.x] = t_mean; e_m2[threadIdx.x] = t_m2; }
+            __syncthreads();
+            // the groups' sums over this block, a team of lanes per group
+            const int unit = WHOLE ? min(s.Cg / V, p.tx) : s.Cg;    // entries of a group in one row of threads
+            const int entries = unit * p.tr, L = team_size(entries), lane = threadIdx.x & (L - 1);
+            for (int b0 = 0; b0 < nb; b0 += kT / L) {
+                const int b = b0 + threadIdx.x / L;
+                const int sl = p.ns > 1 ? (int)p.by_gs.of(b) : 0, g = b - sl * p.gs;
+                const bool in = b < nb && g < gs;
+                // means are summed as differences from one of them: a flat group has exactly its level
+                const float ref = in ? e_mean[sl * p.tr * p.tx * width + g * unit] : 0.f;
+                float cn = 0.f, cm = 0.f;
+                for (int q = lane; in && q < entries; q += L) {
+                    const int row = p.by_unit.of(q), t = (sl * p.tr + row) * p.tx, u = g * unit + (q - row * unit);
+                    const float k = e_n[t + (WHOLE ? u : u / V)];
+                    cn += k;
+                    if (k > 0.f) cm = fmaf(k, e_mean[t * width + u] - ref, cm);
+                }
+                cn = team_sum(cn, L);
+                cm = team_sum(cm, L);
+                const float mean = cn > 0.f ? ref + cm / cn : 0.f;
+                float m2 = 0.f;
+                for (int q = lane; in && q < entries; q += L) {
+                    const int row = p.by_unit.of(q), t = (sl * p.tr + row) * p.tx, u = g * unit + (q - row * unit);
+                    const float k = e_n[t + (WHOLE ? u : u / V)];
+                    if (k > 0.f) {
+                        const float d = e_mean[t * width + u] - mean;
+                        m2 += fmaf(k * d, d, e_m2[t * width + u]);
+                    }
+                }
+                m2 = team_sum(m2, L);
+                if (in && lane == 0) {
+                    const int64_t to = (part.n + sl) * s.G + slab * p.gs + g;
+                    if (TASK == kSums) {
+                        a.gpart[to * p.pieces + part.piece] = make_float4(cn, mean, m2, 0.f);
+                    } else {
+                        const float rstd = rsqrtf(m2 / ((float)s.S * (float)s.Cg) + s.eps);
+                        fin[b] = make_float2(mean, rstd);
+                        if (part.n + sl < s.N) { a.mean[to] = mean; a.rstd[to] = rstd; }
+                    }
+                }
+            }
+            if (TASK == kSums) {
+                if (at < end) __syncthreads();               // the entries may be filled again
+                continue;
+            }
+        } else {
+            if (cnt > 0 && me.txi < cols) rows.begin(cnt, load);     // on their way while the sums are merged
+            if (!waited) { asm volatile("griddepcontrol.wait;" ::: "memory"); waited = true; }
+            // a team of lanes per group
+            const int L = team_size(part.pieces), lane = threadIdx.x & (L - 1);
+            const float all = (float)s.S * (float)s.Cg;
+            for (int b0 = 0; b0 < gs; b0 += kT / L) {
+                const int g = b0 + threadIdx.x / L;
+                const bool in = g < gs;
+                const int64_t to = part.n * s.G + slab * p.gs + g;
+                const float4* q = a.gpart + to * p.pieces;
+                const float4 mine = in && lane < part.pieces ? q[lane] : make_float4(0.f, 0.f, 0.f, 0.f);
+                const float ref = __shfl_sync(0xffffffffu, mine.y, threadIdx.x & 31 & ~(L - 1));
+                float cm = mine.x * (mine.x > 0.f ? mine.y - ref : 0.f);
+                for (int k = lane + L; in && k < part.pieces; k += L) { const float4 v = q[k]; cm = fmaf(v.x, v.y - ref, cm); }
+                const float mean = ref + team_sum(cm, L) / all;
+                float d = mine.y - mean, m2 = mine.x > 0.f ? fmaf(mine.x * d, d, mine.z) : 0.f;
+                for (int k = lane + L; in && k < part.pieces; k += L) { const float4 v = q[k]; d = v.y - mean; m2 += fmaf(v.x * d, d, v.z); }
+                m2 = team_sum(m2, L);
+                if (in && lane == 0) {
+                    const float rstd = rsqrtf(m2 / all + s.eps);
+                    fin[g] = make_float2(mean, rstd);
+                    if (part.piece == 0) { a.mean[to] = mean; a.rstd[to] = rstd; }
+                }
+            }
+        }
+        __syncthreads();
+        if (cnt > 0) {
+            const int64_t set = (unsigned)n / (unsigned)s.per_set;      // both below 2^31
+            const float* gam = affine_row(a, a.gamma, set) + c0;
+            const float* bet = affine_row(a, a.beta, set) + c0;
+            T* y = (T*)a.out + n * a.on + r0 * a.os + c0;
+            for (int j = 0; j < p.cj; ++j) {
+                const int cv = me.txi + j * kT;
+                if (cv >= cols) break;
+                if (!BUF && (kOne || j > 0)) { px = x + cv * V; rows.begin(cnt, load); }
+                F2 mean[kGp], mul[kP], add[kP];              // the mean, negated
+                int g[kGv];
+                groups_of<V, WHOLE>(cv * V, p.by_cg, g);
+                affine_of<V>(gam + cv * V, a.quads, mul);
+                affine_of<V>(bet + cv * V, a.quads, add);
+                const float2* f = fin + me.sl * p.gs;
+                if (WHOLE) {
+                    const float2 q = f[g[0]];
+                    mean[0] = both(-q.x);
+#pragma unroll
+                    for (int v = 0; v < kP; ++v) mul[v] = mul[v] * both(q.y);
+                } else {
 #pragma unroll
                     for (int v = 0; v < kP; ++v) {
-                        const F2 d = f[v] + first[WHOLE ? 0 : v];
-                        s1[v % kAcc] = s1[v % kAcc] + d;
-                        s2[v % kAcc] = fma2(d, d, s2[v % kAcc]);
+                        const float2 q = f[g[2 * v]], r = f[g[(2 * v + 1) % kGv]];
+                        mean[v] = pair(-q.x, -r.x);
+                        mul[v] = mul[v] * pair(q.y, r.y);
                     }
+                }
+                const X* bt = buf + j * p.rpt * kT + threadIdx.x;
+                T* to = y + cv * V;
+                auto use = [&](const X& q) {
+                    F2 o[kP];
+                    widen(q, o);
+#pragma unroll
+                    for (int v = 0; v < kP; ++v) o[v] = fma2(o[v] + mean[WHOLE ? 0 : v], mul[v], add[v]);
+                    if (s.act == RFAST_ACT_SILU) {
+#pragma unroll
+                        for (int v = 0; v < kP; ++v) o[v] = o[v] * sigmoid2(o[v]);
+                    } else if (s.act == RFAST_ACT_RELU) {
+#pragma unroll
+                        for (int v = 0; v < kP; ++v) {
+                            float lo, hi;
+                            split(o[v], lo, hi);
+                            o[v] = pair(lo < 0.f ? 0.f : lo, hi < 0.f ? 0.f : hi);       // a NaN stays one
+                        }
+                    }
+                    store_vec<V>(to, o);
+                    to += ostep;
                 };
-                if (BUF && p.cj == 1) {
-                    for (int k = 0, r = 0; k < 4; ++k, r += lot) {
-                        if (k) copies_wait(3 - k);
-                        walk<kBatch, !BUF, X>(min(cnt - r, lot), load, use);
-                    }
-                } else {
-                    walk<kBatch, !BUF, X>(cnt, load, use);
-                }
-                if (WHOLE) {
-                    if (kAcc == 2) { s1[0] = s1[0] + s1[kAcc - 1]; s2[0] = s2[0] + s2[kAcc - 1]; }
-                    float lo, hi;
-                    split(s1[0], lo, hi);
-                    s1[0] = both(V > 1 ? lo + hi : lo);
-                    split(s2[0], lo, hi);
-                    s2[0] = both(V > 1 ? lo + hi : lo);
-                }
-                const float nn = (float)cnt * (WHOLE ? V : 1), inv = __frcp_rn(nn);
-#pragma unroll
-                for (int v = 0; v < kGp; ++v) {
-                    float a1[2], a2[2];
-                    split(s1[v], a1[0], a1[1]);
-                    split(s2[v], a2[0], a2[1]);
-#pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        const float d = a1[k] * inv;
-                        m2[2 * v + k] = fmaxf(fmaf(-a1[k], d, a2[k]), 0.f) + (a2[k] - a2[k]);   // the second term is a NaN where there was one
-                        mean[2 * v + k] += d;
-                    }
-                }
-                if (WHOLE && t_n > 0.f) {                    // a further pass over a wide group
-                    const float d = mean[0] - t_mean, tot = t_n + nn;
-                    t_mean += d * (nn / tot);
-                    t_m2 += m2[0] + d * d * (t_n * nn / tot);
-                    t_n = tot;
-                } else {
-                    t_mean = mean[0]; t_m2 = m2[0]; t_n = nn;
-                }
-            }
-            if (!WHOLE) {                                    // a slab of several groups is never wider than the block
-                if (me.on && cv < cols) {
-#pragma unroll
-                    for (int v = 0; v < kGv; ++v) { e_mean[threadIdx.x * V + v] = mean[v]; e_m2[threadIdx.x * V + v] = m2[v]; }
-                }
+                if constexpr (BUF) walk<kBatch, X>(cnt, [&]() { const X q = *bt; bt += kT; return q; }, use);
+                else rows.run(cnt, load, use);
             }
         }
-        e_n[threadIdx.x] = t_n;
-        if (WHOLE) { e_mean[threadIdx.x] = t_mean; e_m2[threadIdx.x] = t_m2; }
-        __syncthreads();
-        // the groups' sums over this block, a team of lanes per group
-        const int unit = WHOLE ? min(s.Cg / V, p.tx) : s.Cg;    // entries of a group in one row of threads
-        const int entries = unit * p.tr, L = team_size(entries), lane = threadIdx.x & (L - 1);
-        for (int b0 = 0; b0 < nb; b0 += kT / L) {
-            const int b = b0 + threadIdx.x / L;
-            const int sl = p.ns > 1 ? (int)p.by_gs.of(b) : 0, g = b - sl * p.gs;
-            const bool in = b < nb && g < gs;
-            // means are summed as differences from one of them: a flat group has exactly its level
-            const float ref = in ? e_mean[sl * p.tr * p.tx * width + g * unit] : 0.f;
-            float cn = 0.f, cm = 0.f;
-            for (int q = lane; in && q < entries; q += L) {
-                const int row = p.by_unit.of(q), t = (sl * p.tr + row) * p.tx, u = g * unit + (q - row * unit);
-                const float k = e_n[t + (WHOLE ? u : u / V)];
-                cn += k;
-                if (k > 0.f) cm = fmaf(k, e_mean[t * width + u] - ref, cm);
-            }
-            cn = team_sum(cn, L);
-            cm = team_sum(cm, L);
-            const float mean = cn > 0.f ? ref + cm / cn : 0.f;
-            float m2 = 0.f;
-            for (int q = lane; in && q < entries; q += L) {
-                const int row = p.by_unit.of(q), t = (sl * p.tr + row) * p.tx, u = g * unit + (q - row * unit);
-                const float k = e_n[t + (WHOLE ? u : u / V)];
-                if (k > 0.f) {
-                    const float d = e_mean[t * width + u] - mean;
-                    m2 += fmaf(k * d, d, e_m2[t * width + u]);
-                }
-            }
-            m2 = team_sum(m2, L);
-            if (in && lane == 0) {
-                const int64_t at = (nf + sl) * s.G + blockIdx.y * p.gs + g;
-                if (TASK == kSums) {
-                    a.gpart[at * p.chunks + chunk] = make_float2(mean, m2);
-                } else {
-                    const float rstd = rsqrtf(m2 / ((float)s.S * (float)s.Cg) + s.eps);
-                    fin[b] = make_float2(mean, rstd);
-                    if (nf + sl < s.N) { a.mean[at] = mean; a.rstd[at] = rstd; }
-                }
-            }
-        }
-        if (TASK == kSums) return;
-    } else {
-        // merge the chunks, a team of lanes per group; all chunks but the last hold p.rows positions
-        asm volatile("griddepcontrol.wait;" ::: "memory");
-        const int L = team_size(p.chunks), lane = threadIdx.x & (L - 1);
-        const float full = (float)p.rows * (float)s.Cg, last = (float)(s.S - (int64_t)(p.chunks - 1) * p.rows) * (float)s.Cg;
-        const float all = (float)s.S * (float)s.Cg;
-        for (int b0 = 0; b0 < gs; b0 += kT / L) {
-            const int g = b0 + threadIdx.x / L;
-            const bool in = g < gs;
-            const int64_t at = nf * s.G + blockIdx.y * p.gs + g;
-            const float2* q = a.gpart + at * p.chunks;
-            const float ref = in ? q[0].x : 0.f;
-            float cm = 0.f, m2 = 0.f;
-            for (int k = lane; in && k < p.chunks; k += L) cm = fmaf(k + 1 < p.chunks ? full : last, q[k].x - ref, cm);
-            const float mean = ref + team_sum(cm, L) / all;
-            for (int k = lane; in && k < p.chunks; k += L) {
-                const float2 v = q[k];
-                const float d = v.x - mean;
-                m2 += fmaf((k + 1 < p.chunks ? full : last) * d, d, v.y);
-            }
-            m2 = team_sum(m2, L);
-            if (in && lane == 0) {
-                const float rstd = rsqrtf(m2 / all + s.eps);
-                fin[g] = make_float2(mean, rstd);
-                if (chunk == 0) { a.mean[at] = mean; a.rstd[at] = rstd; }
-            }
-        }
-    }
-    __syncthreads();
-    if (cnt == 0) return;
-    const int64_t set = (unsigned)n / (unsigned)s.per_set;      // both below 2^31
-    const float* gam = affine_row(a, a.gamma, set) + c0;
-    const float* bet = affine_row(a, a.beta, set) + c0;
-    T* y = (T*)a.out + n * a.on + me.r0 * a.os + c0;
-    const int64_t ostep = (int64_t)p.tr * a.os;
-    for (int j = 0; j < p.cj; ++j) {
-        const int cv = me.txi + j * kT;
-        if (cv >= cols) break;
-        F2 mean[kGp], mul[kP], add[kP];                     // the mean, negated
-        int g[kGv];
-        groups_of<V, WHOLE>(cv * V, p.by_cg, g);
-        affine_of<V>(gam + cv * V, a.quads, mul);
-        affine_of<V>(bet + cv * V, a.quads, add);
-        const float2* f = fin + me.sl * p.gs;
-        if (WHOLE) {
-            const float2 q = f[g[0]];
-            mean[0] = both(-q.x);
-#pragma unroll
-            for (int v = 0; v < kP; ++v) mul[v] = mul[v] * both(q.y);
-        } else {
-#pragma unroll
-            for (int v = 0; v < kP; ++v) {
-                const float2 q = f[g[2 * v]], r = f[g[(2 * v + 1) % kGv]];
-                mean[v] = pair(-q.x, -r.x);
-                mul[v] = mul[v] * pair(q.y, r.y);
-            }
-        }
-        const T* at = x + cv * V;
-        const X* bt = buf + j * p.rpt * kT + threadIdx.x;
-        T* to = y + cv * V;
-        auto load = [&]() {
-            if (BUF) { const X q = *bt; bt += kT; return q; }
-            const X q = load_vec<T, V>(at);
-            at += step;
-            return q;
-        };
-        walk<kBatch, !BUF, X>(cnt, load, [&](const X& q) {
-            F2 o[kP];
-            widen(q, o);
-#pragma unroll
-            for (int v = 0; v < kP; ++v) o[v] = fma2(o[v] + mean[WHOLE ? 0 : v], mul[v], add[v]);
-            if (s.act == RFAST_ACT_SILU) {
-#pragma unroll
-                for (int v = 0; v < kP; ++v) o[v] = o[v] * sigmoid2(o[v]);
-            } else if (s.act == RFAST_ACT_RELU) {
-#pragma unroll
-                for (int v = 0; v < kP; ++v) {
-                    float lo, hi;
-                    split(o[v], lo, hi);
-                    o[v] = pair(lo < 0.f ? 0.f : lo, hi < 0.f ? 0.f : hi);       // a NaN stays one
-                }
-            }
-            store_vec<V>(to, o);
-            to += ostep;
-        });
+        if (at < end) __syncthreads();                       // `fin` may be filled again
     }
 }
 
@@ -651,8 +703,8 @@ k_gn_affine(const float* __restrict__ part, int64_t rows, int C, float* __restri
 // per channel dbeta = sum du, dgamma = sum du h over the samples of a set.
 // kWhole, kReread: grid = (parts, slabs, sets); a block takes every `parts`-th item of a set, keeps the channels' sums of its items in
 // shared memory and, buffered, du in fp32 in the place of dy, so that the second pass has no exponentials.
-// kSums, kApply: grid = (chunks, slabs, samples of the launch); kApply runs back to front, its last launch with one slab more, whose
-// blocks form dgamma and dbeta meanwhile.
+// kSums, kApply: grid = spans; kApply takes them back to front, its last launch with some blocks more, which form dgamma and dbeta
+// meanwhile.
 template <class T, int V, bool WHOLE, int TASK>
 __global__ void __launch_bounds__(kT, 2)
 k_gn_backward(const __grid_constant__ GnArgs a) {
@@ -666,8 +718,7 @@ k_gn_backward(const __grid_constant__ GnArgs a) {
     constexpr int kRow = kPlanes<kP> * kT;                   // planes of a row, one after the other
     X* bufx = reinterpret_cast<X*>(smem);
     K* bufd = reinterpret_cast<K*>(smem + (size_t)p.rpt * p.cj * kT * sizeof(X));      // dy in the first plane, then du
-    const int gs = min(p.gs, s.G - (int)blockIdx.y * p.gs); // the last slab may be narrower
-    const int W = gs * s.Cg, nb = p.ns * p.gs;
+    const int nb = p.ns * p.gs;
     const int wide = min(p.W, kT * V);                       // channels of one pass over the width
     const int across = p.tr > 1 ? max(kT, p.ns * wide) : 0;
     float* ent = reinterpret_cast<float*>(smem + p.buf);     // [2][kT * V]: du, du h of a thread's channels
@@ -675,33 +726,56 @@ k_gn_backward(const __grid_constant__ GnArgs a) {
     float2* sums = reinterpret_cast<float2*>(col + (TASK == kApply ? 0 : 2 * across));     // [nb] the groups' two sums
     float* acc = reinterpret_cast<float*>(sums + nb);        // [2][W]: dbeta, dgamma of the block's items
 
-    if (TASK == kApply && blockIdx.y == (unsigned)p.slabs) {
+    if (TASK == kApply && blockIdx.x >= (unsigned)p.blocks) {
         asm volatile("griddepcontrol.wait;" ::: "memory");
-        const int64_t rows = s.per_set * p.chunks;
+        const int64_t rows = s.per_set * p.pieces;
         const unsigned tiles = (s.C + 31) / 32, sets = (unsigned)s.N / (unsigned)s.per_set;
-        for (int64_t t = blockIdx.x + (int64_t)blockIdx.z * gridDim.x; t < (int64_t)tiles * sets; t += (int64_t)gridDim.x * gridDim.z)
+        for (unsigned t = blockIdx.x - p.blocks; t < tiles * sets; t += gridDim.x - p.blocks)
             affine_sums(a.part, rows, s.C, t / tiles, (int)(t % tiles), a.dgamma, a.dbeta);
         return;
     }
     if (TASK == kSums) asm volatile("griddepcontrol.launch_dependents;");
-    const unsigned lead = kOne ? blockIdx.x : TASK == kApply ? gridDim.z - 1 - blockIdx.z : blockIdx.z;
-    const unsigned chunk = kOne ? 0u : TASK == kApply ? gridDim.x - 1 - blockIdx.x : blockIdx.x;
-    const Seat me = seat_of(s, p, chunk);
-    const int64_t set = kOne ? (int64_t)blockIdx.z : (int64_t)((unsigned)(a.n0 + lead) / (unsigned)s.per_set);
-    const int c0 = blockIdx.y * p.W, cols = W / V;
-    const float* gam = affine_row(a, a.gamma, set) + c0;
-    const float* bet = affine_row(a, a.beta, set) + c0;
+    bool waited = false;
+    const Seat me = seat_of(p);
     const int64_t xstep = (int64_t)p.tr * a.xs, dstep = (int64_t)p.tr * a.ds, ostep = (int64_t)p.tr * a.os;
     const float inv_m = 1.f / ((float)s.S * (float)s.Cg);
     if (TASK != kApply)
         for (int c = threadIdx.x; c < 2 * p.W; c += kT) acc[c] = 0.f;
 
-    const int64_t last_item = kOne ? p.items : (int64_t)lead + 1;
-    for (int64_t item = lead; item < last_item; item += p.parts) {
-        const int64_t in_set = item * p.ns + me.sl, n = kOne ? set * s.per_set + in_set : a.n0 + lead;
-        const int cnt = !kOne || in_set < s.per_set ? me.rows : 0;
-        const T* x = (const T*)a.x + n * a.xn + me.r0 * a.xs + c0;
-        const T* dy = (const T*)a.dy + n * a.dn + me.r0 * a.ds + c0;
+    const int64_t span = TASK == kApply ? p.blocks - 1 - (int)blockIdx.x : blockIdx.x;
+    int64_t at = kOne ? blockIdx.x : span * p.per;           // one launch: items; otherwise positions
+    const int64_t end = kOne ? p.items : min(at + p.per, p.total);
+    while (at < end) {
+        Part part;
+        int64_t in_set = 0;                                  // one launch: this thread's sample within its set
+        if (kOne) {
+            part.slab = blockIdx.y; part.from = 0;
+            in_set = at * p.ns + me.sl;
+            part.n = (int64_t)blockIdx.z * s.per_set + in_set;
+            at += p.parts;
+        } else {
+            part = part_at(a, at, end, span);
+            at += part.count;
+        }
+        const int slab = part.slab, gs = min(p.gs, s.G - slab * p.gs), W = gs * s.Cg;      // the last slab may be narrower
+        const int64_t n = part.n, r0 = part.from + me.rr;     // this thread's sample and first position
+        const int64_t set = kOne ? (int64_t)blockIdx.z : (int64_t)((unsigned)n / (unsigned)s.per_set);
+        const int c0 = slab * p.W, cols = W / V;
+        const float* gam = affine_row(a, a.gamma, set) + c0;
+        const float* bet = affine_row(a, a.beta, set) + c0;
+        const int cnt = kOne ? (in_set < s.per_set ? me.rows : 0) : me.on ? rows_of(part.count, me.rr, p.tr) : 0;
+        const T* x = (const T*)a.x + n * a.xn + r0 * a.xs + c0;
+        const T* dy = (const T*)a.dy + n * a.dn + r0 * a.ds + c0;
+        const T *px = x + me.txi * V, *pd = dy + me.txi * V;  // of the pass over the width that is under way
+        auto load = [&]() {
+            Pair<X> q;
+            q.x = load_vec<T, V>(px);
+            q.d = load_vec<T, V>(pd);
+            px += xstep; pd += dstep;
+            return q;
+        };
+        Ahead<kBatch, Pair<X>> rows;
+        if constexpr (!BUF) { if (cnt > 0 && me.txi < cols) rows.begin(cnt, load); }       // on their way before anything else
         if constexpr (TASK != kApply) {
             const int lot = BUF ? (cnt + 3) / 4 : cnt;       // rows of a group of copies
             if (BUF) {
@@ -713,7 +787,7 @@ k_gn_backward(const __grid_constant__ GnArgs a) {
                         K* td = bufd + j * p.rpt * kRow + threadIdx.x;
                         int r = 0;
                         for (int k = 0; k < 4; ++k) {
-                            for (const int end = min(cnt, r + lot); r < end; ++r, ax += xstep, ad += dstep, tx += kT, td += kRow) {
+                            for (const int stop = min(cnt, r + lot); r < stop; ++r, ax += xstep, ad += dstep, tx += kT, td += kRow) {
                                 copy_async<sizeof(X)>(tx, ax);
                                 copy_async<sizeof(X)>(td, ad);
                             }
@@ -735,7 +809,7 @@ k_gn_backward(const __grid_constant__ GnArgs a) {
                     groups_of<V, WHOLE>(cv * V, p.by_cg, g);
                     affine_of<V>(gam + cv * V, a.quads, mul);
                     affine_of<V>(bet + cv * V, a.quads, add);
-                    const float *pm = a.mean + n * s.G + blockIdx.y * p.gs, *pr = a.rstd + n * s.G + blockIdx.y * p.gs;
+                    const float *pm = a.mean + n * s.G + slab * p.gs, *pr = a.rstd + n * s.G + slab * p.gs;
 #pragma unroll
                     for (int v = 0; v < kGp; ++v) {
                         const int g0 = g[WHOLE ? 0 : 2 * v], g1 = g[WHOLE ? 0 : (2 * v + 1) % kGv];
@@ -747,18 +821,11 @@ k_gn_backward(const __grid_constant__ GnArgs a) {
                     const X* bx = bufx + j * p.rpt * kT + threadIdx.x;
                     K* bd = bufd + j * p.rpt * kRow + threadIdx.x;
                     K* keep = bd;
-                    const T *ax = x + cv * V, *ad = dy + cv * V;
-                    auto load = [&]() {
+                    auto held = [&]() {
                         Pair<X> q;
-                        if (BUF) {
-                            q.x = *bx;
-                            q.d = *reinterpret_cast<const X*>(bd);
-                            bx += kT; bd += kRow;
-                        } else {
-                            q.x = load_vec<T, V>(ax);
-                            q.d = load_vec<T, V>(ad);
-                            ax += xstep; ad += dstep;
-                        }
+                        q.x = *bx;
+                        q.d = *reinterpret_cast<const X*>(bd);
+                        bx += kT; bd += kRow;
                         return q;
                     };
                     auto use = [&](const Pair<X>& q) {
@@ -774,13 +841,18 @@ k_gn_backward(const __grid_constant__ GnArgs a) {
                         }
                         if (BUF) { put<kP>(keep, du); keep += kRow; }
                     };
-                    if (BUF && p.cj == 1) {
-                        for (int k = 0, r = 0; k < 4; ++k, r += lot) {
-                            copies_wait(3 - k);
-                            walk<kBatch, !BUF, Pair<X>>(min(cnt - r, lot), load, use);
+                    if constexpr (BUF) {
+                        if (p.cj == 1) {
+                            for (int k = 0, r = 0; k < 4; ++k, r += lot) {
+                                copies_wait(3 - k);
+                                walk<kBatch, Pair<X>>(min(cnt - r, lot), held, use);
+                            }
+                        } else {
+                            walk<kBatch, Pair<X>>(cnt, held, use);
                         }
                     } else {
-                        walk<kBatch, !BUF, Pair<X>>(cnt, load, use);
+                        if (j > 0) { px = x + cv * V; pd = dy + cv * V; rows.begin(cnt, load); }
+                        rows.run(cnt, load, use);
                     }
 #pragma unroll
                     for (int v = 0; v < kP; ++v) s_dh[v] = s_dh[v] * rs[WHOLE ? 0 : v];     // h = (x - mean) rstd
@@ -863,19 +935,35 @@ k_gn_backward(const __grid_constant__ GnArgs a) {
                 __syncthreads();                             // before the next pass or item fills `ent`
             }
             if (TASK == kSums) {
-                for (int g = threadIdx.x; g < gs; g += kT) a.gpart[(n * s.G + blockIdx.y * p.gs + g) * p.chunks + chunk] = sums[g];
-                break;
+                for (int g = threadIdx.x; g < gs; g += kT) {
+                    const float2 q = sums[g];
+                    a.gpart[(n * s.G + slab * p.gs + g) * p.pieces + part.piece] = make_float4(q.x, q.y, 0.f, 0.f);
+                }
+                // the channels' sums: a row per piece, rows of pieces that the slab does not have are zeros
+                float* to = a.part + (n * p.pieces + part.piece) * 2 * s.C + c0;
+                for (int c = threadIdx.x; c < W; c += kT) {
+                    to[c] = acc[c];
+                    to[s.C + c] = acc[p.W + c];
+                }
+                __syncthreads();
+                for (int c = threadIdx.x; c < 2 * p.W; c += kT) acc[c] = 0.f;
+                if (part.piece + 1 == part.pieces)
+                    for (int k = part.pieces; k < p.pieces; ++k) {
+                        to = a.part + (n * p.pieces + k) * 2 * s.C + c0;
+                        for (int c = threadIdx.x; c < W; c += kT) to[c] = to[s.C + c] = 0.f;
+                    }
+                continue;
             }
         } else {
-            // merge the chunks, a team of lanes per group
-            asm volatile("griddepcontrol.wait;" ::: "memory");
-            const int L = team_size(p.chunks), lane = threadIdx.x & (L - 1);
+            if (!waited) { asm volatile("griddepcontrol.wait;" ::: "memory"); waited = true; }
+            // merge the pieces, a team of lanes per group
+            const int L = team_size(part.pieces), lane = threadIdx.x & (L - 1);
             for (int b0 = 0; b0 < gs; b0 += kT / L) {
                 const int g = b0 + threadIdx.x / L;
                 float u0 = 0.f, u1 = 0.f;
                 if (g < gs) {
-                    const float2* q = a.gpart + (n * s.G + blockIdx.y * p.gs + g) * p.chunks;
-                    for (int k = lane; k < p.chunks; k += L) { const float2 v = q[k]; u0 += v.x; u1 += v.y; }
+                    const float4* q = a.gpart + (n * s.G + slab * p.gs + g) * p.pieces;
+                    for (int k = lane; k < part.pieces; k += L) { const float4 v = q[k]; u0 += v.x; u1 += v.y; }
                 }
                 u0 = team_sum(u0, L);
                 u1 = team_sum(u1, L);
@@ -884,16 +972,17 @@ k_gn_backward(const __grid_constant__ GnArgs a) {
             __syncthreads();
         }
         if (cnt > 0) {
-            T* dx = (T*)a.out + n * a.on + me.r0 * a.os + c0;
+            T* dx = (T*)a.out + n * a.on + r0 * a.os + c0;
             for (int j = 0; j < p.cj; ++j) {
                 const int cv = me.txi + j * kT;
                 if (cv >= cols) break;
+                if (!BUF && (kOne || j > 0)) { px = x + cv * V; pd = dy + cv * V; rows.begin(cnt, load); }
                 F2 mean[kGp], k1[kGp], k2[kGp], mul[kP], add[kP];   // dx = mul du - k1 - (x - mean) k2; all but mul and add negated
                 int g[kGv];
                 groups_of<V, WHOLE>(cv * V, p.by_cg, g);
                 affine_of<V>(gam + cv * V, a.quads, mul);
                 if (!BUF) affine_of<V>(bet + cv * V, a.quads, add);
-                const float *pm = a.mean + n * s.G + blockIdx.y * p.gs, *pr = a.rstd + n * s.G + blockIdx.y * p.gs;
+                const float *pm = a.mean + n * s.G + slab * p.gs, *pr = a.rstd + n * s.G + slab * p.gs;
                 const float2* q = sums + me.sl * p.gs;
 #pragma unroll
                 for (int v = 0; v < kGp; ++v) {
@@ -910,7 +999,6 @@ k_gn_backward(const __grid_constant__ GnArgs a) {
                 }
                 const X* bx = bufx + j * p.rpt * kT + threadIdx.x;
                 const K* bd = bufd + j * p.rpt * kRow + threadIdx.x;
-                const T *ax = x + cv * V, *ad = dy + cv * V;
                 T* to = dx + cv * V;
                 auto last = [&](F2 (&d)[kP], F2 (&du)[kP]) {  // d: x - mean
 #pragma unroll
@@ -920,7 +1008,7 @@ k_gn_backward(const __grid_constant__ GnArgs a) {
                 };
                 if constexpr (BUF) {
                     struct Held { X x; F2 d[kP]; };
-                    walk<kBatch, false, Held>(cnt, [&]() { Held h; h.x = *bx; get<kP>(bd, h.d); bx += kT; bd += kRow; return h; }, [&](Held& h) {
+                    walk<kBatch, Held>(cnt, [&]() { Held h; h.x = *bx; get<kP>(bd, h.d); bx += kT; bd += kRow; return h; }, [&](Held& h) {
                         F2 d[kP];
                         widen(h.x, d);
 #pragma unroll
@@ -928,13 +1016,7 @@ k_gn_backward(const __grid_constant__ GnArgs a) {
                         last(d, h.d);
                     });
                 } else {
-                    walk<kBatch, !BUF, Pair<X>>(cnt, [&]() {
-                        Pair<X> h;
-                        h.x = load_vec<T, V>(ax);
-                        h.d = load_vec<T, V>(ad);
-                        ax += xstep; ad += dstep;
-                        return h;
-                    }, [&](const Pair<X>& h) {
+                    rows.run(cnt, load, [&](const Pair<X>& h) {
                         F2 d[kP], du[kP];
                         widen(h.x, d);
                         widen(h.d, du);
@@ -948,17 +1030,17 @@ k_gn_backward(const __grid_constant__ GnArgs a) {
                 }
             }
         }
-        if (TASK == kApply) return;
         __syncthreads();                                     // `sums` may be filled again
     }
-    if constexpr (TASK != kApply) {
+    if constexpr (kOne) {
+        const int slab = blockIdx.y, c0 = slab * p.W, W = min(p.gs, s.G - slab * p.gs) * s.Cg;
+        const int64_t set = blockIdx.z;
         float *to0, *to1;                                    // dbeta, dgamma
-        if (kOne && p.parts == 1) {
+        if (p.parts == 1) {
             to0 = a.dbeta + set * s.C + c0;
             to1 = a.dgamma + set * s.C + c0;
         } else {
-            const int64_t row = kOne ? set * p.parts + blockIdx.x : (a.n0 + lead) * p.chunks + chunk;
-            to0 = a.part + row * 2 * s.C + c0;
+            to0 = a.part + (set * p.parts + blockIdx.x) * 2 * s.C + c0;
             to1 = to0 + s.C;
         }
         for (int c = threadIdx.x; c < W; c += kT) {
@@ -971,7 +1053,7 @@ k_gn_backward(const __grid_constant__ GnArgs a) {
 // ---- host side ------------------------------------------------------------------------------------
 constexpr int kSms = 148;
 constexpr int kMaxGroupChannels = 8192;                     // a block keeps two sums for every channel of a group
-constexpr int kMaxChunks = 512;
+constexpr int kAffineBlocks = 16;                           // that form dgamma and dbeta beside the last launch over spans
 constexpr size_t kMostSmem = 220 * 1024;
 constexpr int64_t kBatchBytes = (int64_t)64 << 20;          // of the samples between a launch for the sums and the one after it: half of L2
 
@@ -984,21 +1066,26 @@ int64_t batch_of(const GnShape& s, int esize, bool backward) {
     return (s.N + batches - 1) / batches;
 }
 
-// Chunks of a sample's slab, a function of the shape alone (the workspace follows from it); 1: one launch.
-int chunks_of(const GnShape& s, int esize, bool backward) {
-    int64_t width = (int64_t)s.Cg * esize;                  // bytes of a slab, roughly
-    if (width < 128) width = (128 + width - 1) / width * width;
-    if (width > (int64_t)s.C * esize) width = (int64_t)s.C * esize;
-    const int64_t item = s.S * width, items = s.N * (((int64_t)s.C * esize + width - 1) / width);
-    // one launch while a slab fits the buffer (backward: x and du in fp32) and either fills the GPU or is read in about a microsecond
-    const int64_t most = backward ? 32 * 1024 : 64 * 1024;
-    if (s.S < 64 || (item <= most && (items >= kSms || item <= 16 * 1024))) return 1;
-    // one thread block on every third (backward: half) of an SM at a time: what a thread sets up serves all its positions
-    const int64_t at_once = items / s.N * batch_of(s, esize, backward);
-    int64_t chunks = (backward ? 2 : 3) * kSms / at_once;
-    if (chunks > item / (8 * 1024)) chunks = item / (8 * 1024);
-    if (chunks > s.S / 32) chunks = s.S / 32;
-    return (int)(chunks < 2 ? 2 : chunks > kMaxChunks ? kMaxChunks : chunks);
+// Whether slabs of W channels go through spans: where they do not fit the buffer (backward: x and du in fp32), or are fewer than the
+// SMs and take longer than a microsecond or two to read.
+bool in_spans(const GnShape& s, int esize, int W, int slabs, bool backward) {
+    const int64_t item = s.S * W * esize, items = s.N * slabs;
+    return s.S >= 64 && (item > (backward ? 32 * 1024 : 64 * 1024) || (items < kSms && item > 16 * 1024));
+}
+// Spans of a launch over `items` slabs: one for every thread block that runs at a time, of 32 positions and 8 KB at least.  `pieces`: spans
+// that a slab can lie in.
+void cut_spans(GnPlan& p, const GnShape& s, int esize, bool backward, int64_t items) {
+    p.total = items * s.S;
+    const int at_a_time = (backward ? 2 : 3) * kSms - kAffineBlocks;
+    int64_t per = (p.total + at_a_time - 1) / at_a_time;
+    const int64_t least = (8 * 1024 + p.W * esize - 1) / (p.W * esize);
+    if (per < least) per = least;
+    if (per < 32) per = 32;
+    if (per > p.total) per = p.total;
+    if (per > 0x7fffffff) per = 0x7fffffff;
+    p.per = per;
+    p.blocks = (int)((p.total + per - 1) / per);
+    p.pieces = (int)((s.S + per - 2) / per) + 1;
 }
 
 // One launch: blocks that share a set's sums at most.
@@ -1007,12 +1094,6 @@ int64_t part_rows(const GnShape& s) {
     int64_t cap = 2048 / sets;
     cap = cap < 16 ? 16 : cap > 256 ? 256 : cap;
     return cap < s.per_set ? cap : s.per_set;
-}
-
-// Bytes of the workspace: the groups' partial sums, then the channels' rows.
-size_t group_bytes(const GnShape& s, int chunks) { return chunks > 1 ? (size_t)s.N * s.G * chunks * sizeof(float2) : 0; }
-size_t row_bytes(const GnShape& s, int chunks) {
-    return (size_t)(chunks > 1 ? s.N * chunks : s.N / s.per_set * part_rows(s)) * 2 * s.C * sizeof(float);
 }
 
 size_t smem_bytes(const GnShape& s, const GnPlan& p, bool backward, int task) {
@@ -1035,7 +1116,6 @@ GnPlan make_plan(const GnShape& s, int esize, int vmax, bool backward) {
     const bool broad = s.Cg * esize >= 128;
     if (broad) { while (s.Cg % V) V /= 2; } else { while (s.C % V) V /= 2; }
     if (V * esize == 8) V /= 2;                             // accesses of 16, 4 or 2 bytes
-    const int64_t batch = backward ? s.per_set : s.N;
     p.V = V;
     p.gs = broad ? 1 : s.G;
     if (!broad)
@@ -1047,19 +1127,19 @@ GnPlan make_plan(const GnShape& s, int esize, int vmax, bool backward) {
     p.tx = cols < kT ? cols : kT;
     p.cj = (cols + kT - 1) / kT;
     const int ty = kT / p.tx;
-    p.chunks = chunks_of(s, esize, backward);
-    p.rows = (s.S + p.chunks - 1) / p.chunks;
-    p.chunks = (int)((s.S + p.rows - 1) / p.rows);          // none is empty
-    p.tr = (int)(p.rows < ty ? p.rows : ty);
+    p.tr = (int)(s.S < ty ? s.S : ty);
     p.ns = 1;
     p.parts = 1;
-    const int64_t end = s.S - (p.chunks - 1) * p.rows;
-    p.each = (int)(p.rows / p.tr); p.more = (int)(p.rows % p.tr);
-    p.each_end = (int)(end / p.tr); p.more_end = (int)(end % p.tr);
     const int unit = s.Cg % V == 0 ? s.Cg / V : s.Cg;
     p.by_tx.set(p.tx); p.by_tr.set(p.tr); p.by_gs.set(p.gs); p.by_cg.set(s.Cg); p.by_unit.set(unit < p.tx || s.Cg % V ? unit : p.tx);
-    if (p.chunks > 1) return p;
-    int64_t ns = ty / p.tr;
+    p.spans = in_spans(s, esize, p.W, p.slabs, backward);
+    if (p.spans) {
+        cut_spans(p, s, esize, backward, batch_of(s, esize, backward) * p.slabs);
+        return p;
+    }
+    p.each = (int)(s.S / p.tr); p.more = (int)(s.S % p.tr);
+    const int64_t batch = backward ? s.per_set : s.N;
+    const int64_t ns = ty / p.tr;
     p.ns = (int)(ns > batch ? batch : ns);
     p.items = (batch + p.ns - 1) / p.ns;
     if (backward) {
@@ -1067,7 +1147,7 @@ GnPlan make_plan(const GnShape& s, int esize, int vmax, bool backward) {
         p.parts = p.items < most ? p.items : most;
     }
     if (V * esize >= 4) {
-        const int64_t rpt = (p.rows + p.tr - 1) / p.tr;
+        const int64_t rpt = (s.S + p.tr - 1) / p.tr;
         GnPlan q = p;
         q.buffered = true;
         q.buf = (size_t)(rpt * p.cj * kT * (V * esize + (backward ? 8 * ((V + 1) / 2) : 0)));   // x, and du in pairs
@@ -1075,6 +1155,20 @@ GnPlan make_plan(const GnShape& s, int esize, int vmax, bool backward) {
         if (smem_bytes(s, q, backward, kWhole) <= kMostSmem) return q;
     }
     return p;
+}
+
+// Bytes of the workspace for a plan: the groups' partial sums, then the channels' rows.
+size_t group_bytes(const GnShape& s, const GnPlan& p) { return p.spans ? (size_t)s.N * s.G * p.pieces * sizeof(float4) : 0; }
+size_t row_bytes(const GnShape& s, const GnPlan& p) { return (size_t)(p.spans ? s.N * p.pieces : s.N / s.per_set * part_rows(s)) * 2 * s.C * sizeof(float); }
+// The most that any plan of the shape takes, whatever addresses and strides allow.
+size_t workspace_bytes_of(const GnShape& s, int esize, bool backward) {
+    size_t most = 0;
+    for (int v = 1; v * esize <= 16; v *= 2) {
+        const GnPlan p = make_plan(s, esize, v, backward);
+        const size_t b = group_bytes(s, p) + (backward ? row_bytes(s, p) : 0);
+        if (b > most) most = b;
+    }
+    return most;
 }
 
 template <class K>
@@ -1096,7 +1190,7 @@ template <class T, int V, bool WHOLE>
 cudaError_t launch_whole(GnArgs& a, bool backward, cudaStream_t st) {
     const GnPlan& p = a.p;
     auto smem = [&](int task) { return smem_bytes(a.s, p, backward, task); };
-    if (p.chunks == 1) {
+    if (!p.spans) {
         const dim3 grid((unsigned)(backward ? p.parts : p.items), p.slabs, backward ? (unsigned)(a.s.N / a.s.per_set) : 1);
         if constexpr (sizeof(T) * V >= 4) {
             if (p.buffered) return backward ? launch_task(k_gn_backward<T, V, WHOLE, kWhole>, grid, a, smem(kWhole), false, st)
@@ -1105,18 +1199,19 @@ cudaError_t launch_whole(GnArgs& a, bool backward, cudaStream_t st) {
         return backward ? launch_task(k_gn_backward<T, V, WHOLE, kReread>, grid, a, smem(kReread), false, st)
                         : launch_task(k_gn_forward<T, V, WHOLE, kReread>, grid, a, smem(kReread), false, st);
     }
-    const int64_t per = batch_of(a.s, (int)sizeof(T), backward);
+    const int64_t batch = batch_of(a.s, (int)sizeof(T), backward);
     cudaError_t e = cudaSuccess;
-    for (a.n0 = 0; a.n0 < a.s.N && e == cudaSuccess; a.n0 = a.n1) {
-        a.n1 = a.n0 + per < a.s.N ? a.n0 + per : a.s.N;
-        const dim3 grid(p.chunks, p.slabs, (unsigned)(a.n1 - a.n0));
+    for (a.n0 = 0; a.n0 < a.s.N && e == cudaSuccess; a.n0 += batch) {
+        const int64_t left = a.s.N - a.n0, count = left < batch ? left : batch;
+        a.p.total = count * p.slabs * a.s.S;                 // the last batch may be smaller; its spans keep their length
+        a.p.blocks = (int)((a.p.total + p.per - 1) / p.per);
+        const dim3 grid(a.p.blocks), next(a.p.blocks + (backward && count == left ? kAffineBlocks : 0));
         if (backward) {
             e = launch_task(k_gn_backward<T, V, WHOLE, kSums>, grid, a, smem(kSums), false, st);
-            const dim3 more(grid.x, p.slabs + (a.n1 == a.s.N ? 1 : 0), grid.z);
-            if (e == cudaSuccess) e = launch_task(k_gn_backward<T, V, WHOLE, kApply>, more, a, smem(kApply), true, st);
+            if (e == cudaSuccess) e = launch_task(k_gn_backward<T, V, WHOLE, kApply>, next, a, smem(kApply), true, st);
         } else {
             e = launch_task(k_gn_forward<T, V, WHOLE, kSums>, grid, a, smem(kSums), false, st);
-            if (e == cudaSuccess) e = launch_task(k_gn_forward<T, V, WHOLE, kApply>, grid, a, smem(kApply), true, st);
+            if (e == cudaSuccess) e = launch_task(k_gn_forward<T, V, WHOLE, kApply>, next, a, smem(kApply), true, st);
         }
     }
     return e;
@@ -1181,8 +1276,8 @@ int strides_of(const int64_t* given, const GnShape& s, int64_t* sn, int64_t* ss,
 int check_workspace(const rfast_gn_shape* g, int backward, const void* workspace, size_t bytes, const char* me, char* err, size_t err_len) {
     const int64_t need = rfast_group_norm_workspace(g, backward);
     if (need == 0) return RFAST_OK;
-    if (!workspace || (uintptr_t)workspace % 8 || (int64_t)bytes < need)
-        return op_fail(err, err_len, RFAST_EINVAL, "%s: the workspace needs %lld bytes, aligned to 8", me, (long long)need);
+    if (!workspace || (uintptr_t)workspace % 16 || (int64_t)bytes < need)
+        return op_fail(err, err_len, RFAST_EINVAL, "%s: the workspace needs %lld bytes, aligned to 16", me, (long long)need);
     return check_device_pointer(workspace, "workspace", err, err_len);
 }
 
@@ -1208,8 +1303,7 @@ extern "C" int64_t rfast_group_norm_workspace(const rfast_gn_shape* g, int backw
     if (rc != RFAST_OK) return rc;
     if (g->samples == 0 || g->positions == 0) return 0;
     const GnShape s = shape_from(g, 1.f);
-    const int chunks = chunks_of(s, type_bytes(g->type), backward != 0);
-    return (int64_t)(group_bytes(s, chunks) + (backward ? row_bytes(s, chunks) : 0));
+    return (int64_t)workspace_bytes_of(s, type_bytes(g->type), backward != 0);
 }
 
 extern "C" int rfast_group_norm(const rfast_gn_shape* g, const void* d_x, const int64_t* x_strides, const float* d_gamma, const float* d_beta, float eps,
@@ -1236,7 +1330,7 @@ extern "C" int rfast_group_norm(const rfast_gn_shape* g, const void* d_x, const 
     a.x = d_x; a.out = d_y; a.gamma = d_gamma; a.beta = d_beta; a.affine_stride = a.s.C; a.mean = d_mean; a.rstd = d_rstd;
     const int vx = allowed(d_x, a.xn, a.xs, es), vy = allowed(d_y, a.on, a.os, es);
     a.p = make_plan(a.s, es, vx < vy ? vx : vy, false);
-    a.gpart = (float2*)workspace;
+    a.gpart = (float4*)workspace;
     if (a.p.slabs > 65535) return op_fail(err, err_len, RFAST_EINVAL, "%s: too many samples or groups", me);
     const cudaError_t e = launch_typed(a, g->type, false, (cudaStream_t)cuda_stream);
     if (e != cudaSuccess) return op_fail(err, err_len, RFAST_ECUDA, "%s: kernel launch: %s", me, cudaGetErrorString(e));
@@ -1277,16 +1371,16 @@ extern "C" int rfast_group_norm_backward(const rfast_gn_shape* g, const void* d_
     a.x = d_x; a.dy = d_dy; a.out = d_dx; a.gamma = d_gamma; a.beta = d_beta; a.affine_stride = a.s.C;
     a.mean = const_cast<float*>(d_mean); a.rstd = const_cast<float*>(d_rstd);
     a.dgamma = d_dgamma; a.dbeta = d_dbeta;
-    a.gpart = (float2*)workspace;
-    a.part = (float*)((char*)workspace + group_bytes(a.s, chunks_of(a.s, es, true)));
     int v = allowed(d_x, a.xn, a.xs, es);
     const int v2 = allowed(d_dy, a.dn, a.ds, es), v3 = allowed(d_dx, a.on, a.os, es);
     v = v < v2 ? v : v2;
     v = v < v3 ? v : v3;
     a.p = make_plan(a.s, es, v, true);
+    a.gpart = (float4*)workspace;
+    a.part = (float*)((char*)workspace + group_bytes(a.s, a.p));
     if (a.p.slabs > 65534 || sets > 65535) return op_fail(err, err_len, RFAST_EINVAL, "%s: too many groups or sets", me);
     e = launch_typed(a, g->type, true, st);
-    if (e == cudaSuccess && a.p.chunks == 1 && a.p.parts > 1) {
+    if (e == cudaSuccess && !a.p.spans && a.p.parts > 1) {
         k_gn_affine<<<dim3((a.s.C + 31) / 32, (unsigned)sets), kT, 0, st>>>(a.part, a.p.parts, a.s.C, d_dgamma, d_dbeta);
         e = cudaGetLastError();
     }
