@@ -24,6 +24,7 @@
 
 #include <cmath>
 #include <cstdio>
+#include <type_traits>
 
 #include "ops.h"
 
@@ -32,6 +33,7 @@ namespace rfast {
 namespace {
 
 constexpr int kT = 256;                                    // threads per block
+constexpr int kRingPairs = 4;                              // pairs of rows that a thread's ring holds
 
 template <int BYTES> struct Word;
 template <> struct Word<16> { typedef uint4 type; };
@@ -127,6 +129,8 @@ __device__ __forceinline__ void copies_wait(int left) {
     }
 }
 
+template <int LEFT> __device__ __forceinline__ void copies_pending() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
+
 // 1 / (1 + exp(-u)) of a pair.  2^t and the reciprocal are the hardware's (2 ulp and 1 ulp), t and the products are rounded
 // once each: the result is good to about 2^-22.  The special function unit, with a result every other cycle where the
 // adders have eight, is what bounds a pass with this in it, so one reciprocal, of the product of both denominators, serves
@@ -160,7 +164,37 @@ __device__ __forceinline__ void walk(int cnt, Load load, Use use) {
 #pragma unroll 1
     for (; r < cnt; ++r) { Row q = load(); use(q); }
 }
-// The same out of memory: a batch's loads go out before the batch ahead of it is worked on (its stores would hold them back,
+// The same out of memory, through a ring of 2 PAIRS slots in shared memory that only this thread uses: `fetch(slot)` starts the
+// asynchronous copies of the next row into a slot, `held(slot)` reads one.  What is on its way costs no registers, so there can be
+// enough of it: rows fetched ahead into registers left 40 to 50 KB on their way in an SM, and 4 TB/s.
+template <int PAIRS> struct Ring {
+    int in, sent;
+    template <class Fetch> __device__ __forceinline__ void send(int cnt, Fetch& fetch) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+            if (sent < cnt) { fetch(in); in = in + 1 == 2 * PAIRS ? 0 : in + 1; ++sent; }
+        copies_commit();
+    }
+    template <class Fetch> __device__ __forceinline__ void begin(int cnt, Fetch& fetch) {
+        in = sent = 0;
+        for (int k = 0; k < PAIRS - 1; ++k) send(cnt, fetch);
+    }
+    template <class Row, class Fetch, class Held, class Use> __device__ __forceinline__ void run(int cnt, Fetch& fetch, Held held, Use use) {
+        int out = 0;
+#pragma unroll 1
+        for (int r = 0; r < cnt; r += 2) {
+            send(cnt, fetch);
+            copies_pending<PAIRS - 1>();
+            Row q[2];
+            q[0] = held(out);
+            q[1] = held(out + 1);                            // past the last row: what lay there, unused
+            out = out + 2 == 2 * PAIRS ? 0 : out + 2;
+            use(q[0]);
+            if (r + 1 < cnt) use(q[1]);
+        }
+    }
+};
+// Where accesses are too narrow for copies: a batch's loads go out before the batch ahead of it is worked on (its stores would hold them back,
 // the operands being allowed to coincide), the first batch's as early as the caller likes.
 template <int R, class Row> struct Ahead {
     Row q[R];
@@ -343,7 +377,7 @@ __device__ __forceinline__ int team_size(int entries) {
 // ---- forward --------------------------------------------------------------------------------------
 // kWhole, kReread: grid = (items, slabs).  kSums, kApply: grid = spans; kApply takes them back to front.
 template <class T, int V, bool WHOLE, int TASK>
-__global__ void __launch_bounds__(kT, WHOLE && TASK == kWhole ? 4 : 3)
+__global__ void __launch_bounds__(kT, WHOLE ? 4 : 3)
 k_gn_forward(const __grid_constant__ GnArgs a) {
     extern __shared__ __align__(16) uint8_t smem[];
     typedef Vec<T, V> X;
@@ -354,6 +388,9 @@ k_gn_forward(const __grid_constant__ GnArgs a) {
     X* buf = reinterpret_cast<X*>(smem);
     // per thread (WHOLE: an access stays inside a group) or per thread and channel: count, mean, sum of squared deviations
     constexpr int width = kGv, kEnt = TASK == kApply ? 0 : kT;
+    constexpr bool RING = !BUF && sizeof(X) >= 4;
+    constexpr int kPairsAhead = kRingPairs;
+    X* ring = buf + threadIdx.x;
     float* e_n = reinterpret_cast<float*>(smem + p.buf);
     float* e_mean = e_n + kEnt;
     float* e_m2 = e_mean + kEnt * width;
@@ -383,7 +420,10 @@ k_gn_forward(const __grid_constant__ GnArgs a) {
         const T* x = (const T*)a.x + n * a.xn + r0 * a.xs + c0;
         const T* px = x + me.txi * V;                        // of the pass over the width that is under way
         auto load = [&]() { const X q = load_vec<T, V>(px); px += step; return q; };
-        Ahead<kBatch, X> rows;
+        auto fetch = [&](int slot) { copy_async<sizeof(X)>(ring + slot * kT, px); px += step; };
+        auto waiting = [&](int slot) { return ring[slot * kT]; };
+        typename std::conditional<RING, Ring<kPairsAhead>, Ahead<kBatch, X>>::type rows;
+        auto begin = [&]() { if constexpr (RING) rows.begin(cnt, fetch); else rows.begin(cnt, load); };
 
         if constexpr (TASK != kApply) {
             // what is read comes in up to four lots of rows; the first is worked on while the others are on their way
@@ -421,8 +461,8 @@ k_gn_forward(const __grid_constant__ GnArgs a) {
                         x0 = *bt;
                     } else {
                         px = x + cv * V;
-                        rows.begin(cnt, load);
-                        x0 = rows.q[0];
+                        x0 = load_vec<T, V>(px);
+                        begin();
                     }
                     {
                         F2 f[kP];
@@ -456,6 +496,8 @@ k_gn_forward(const __grid_constant__ GnArgs a) {
                         } else {
                             walk<kBatch, X>(cnt, held, use);
                         }
+                    } else if constexpr (RING) {
+                        rows.template run<X>(cnt, fetch, waiting, use);
                     } else {
                         rows.run(cnt, load, use);
                     }
@@ -544,7 +586,7 @@ k_gn_forward(const __grid_constant__ GnArgs a) {
                 continue;
             }
         } else {
-            if (cnt > 0 && me.txi < cols) rows.begin(cnt, load);     // on their way while the sums are merged
+            if (cnt > 0 && me.txi < cols) begin();           // on their way while the sums are merged
             if (!waited) { asm volatile("griddepcontrol.wait;" ::: "memory"); waited = true; }
             // a team of lanes per group
             const int L = team_size(part.pieces), lane = threadIdx.x & (L - 1);
@@ -578,7 +620,7 @@ k_gn_forward(const __grid_constant__ GnArgs a) {
             for (int j = 0; j < p.cj; ++j) {
                 const int cv = me.txi + j * kT;
                 if (cv >= cols) break;
-                if (!BUF && (kOne || j > 0)) { px = x + cv * V; rows.begin(cnt, load); }
+                if constexpr (!BUF) { if (kOne || j > 0) { px = x + cv * V; begin(); } }
                 F2 mean[kGp], mul[kP], add[kP];              // the mean, negated
                 int g[kGv];
                 groups_of<V, WHOLE>(cv * V, p.by_cg, g);
@@ -620,6 +662,7 @@ k_gn_forward(const __grid_constant__ GnArgs a) {
                     to += ostep;
                 };
                 if constexpr (BUF) walk<kBatch, X>(cnt, [&]() { const X q = *bt; bt += kT; return q; }, use);
+                else if constexpr (RING) rows.template run<X>(cnt, fetch, waiting, use);
                 else rows.run(cnt, load, use);
             }
         }
@@ -706,7 +749,7 @@ k_gn_affine(const float* __restrict__ part, int64_t rows, int C, float* __restri
 // kSums, kApply: grid = spans; kApply takes them back to front, its last launch with some blocks more, which form dgamma and dbeta
 // meanwhile.
 template <class T, int V, bool WHOLE, int TASK>
-__global__ void __launch_bounds__(kT, 2)
+__global__ void __launch_bounds__(kT, WHOLE && (TASK == kSums || TASK == kApply) ? 3 : 2)
 k_gn_backward(const __grid_constant__ GnArgs a) {
     extern __shared__ __align__(16) uint8_t smem[];
     typedef Vec<T, V> X;
@@ -718,6 +761,9 @@ k_gn_backward(const __grid_constant__ GnArgs a) {
     constexpr int kRow = kPlanes<kP> * kT;                   // planes of a row, one after the other
     X* bufx = reinterpret_cast<X*>(smem);
     K* bufd = reinterpret_cast<K*>(smem + (size_t)p.rpt * p.cj * kT * sizeof(X));      // dy in the first plane, then du
+    constexpr bool RING = !BUF && sizeof(X) >= 4;
+    constexpr int kPairsAhead = kRingPairs;
+    X* ring = bufx + threadIdx.x;                            // slots of x and dy
     const int nb = p.ns * p.gs;
     const int wide = min(p.W, kT * V);                       // channels of one pass over the width
     const int across = p.tr > 1 ? max(kT, p.ns * wide) : 0;
@@ -774,8 +820,15 @@ k_gn_backward(const __grid_constant__ GnArgs a) {
             px += xstep; pd += dstep;
             return q;
         };
-        Ahead<kBatch, Pair<X>> rows;
-        if constexpr (!BUF) { if (cnt > 0 && me.txi < cols) rows.begin(cnt, load); }       // on their way before anything else
+        auto fetch = [&](int slot) {
+            copy_async<sizeof(X)>(ring + 2 * slot * kT, px);
+            copy_async<sizeof(X)>(ring + (2 * slot + 1) * kT, pd);
+            px += xstep; pd += dstep;
+        };
+        auto waiting = [&](int slot) { Pair<X> q; q.x = ring[2 * slot * kT]; q.d = ring[(2 * slot + 1) * kT]; return q; };
+        typename std::conditional<RING, Ring<kPairsAhead>, Ahead<kBatch, Pair<X>>>::type rows;
+        auto begin = [&]() { if constexpr (RING) rows.begin(cnt, fetch); else rows.begin(cnt, load); };
+        if constexpr (!BUF) { if (cnt > 0 && me.txi < cols) begin(); }       // on their way before anything else
         if constexpr (TASK != kApply) {
             const int lot = BUF ? (cnt + 3) / 4 : cnt;       // rows of a group of copies
             if (BUF) {
@@ -851,8 +904,9 @@ k_gn_backward(const __grid_constant__ GnArgs a) {
                             walk<kBatch, Pair<X>>(cnt, held, use);
                         }
                     } else {
-                        if (j > 0) { px = x + cv * V; pd = dy + cv * V; rows.begin(cnt, load); }
-                        rows.run(cnt, load, use);
+                        if (j > 0) { px = x + cv * V; pd = dy + cv * V; begin(); }
+                        if constexpr (RING) rows.template run<Pair<X>>(cnt, fetch, waiting, use);
+                        else rows.run(cnt, load, use);
                     }
 #pragma unroll
                     for (int v = 0; v < kP; ++v) s_dh[v] = s_dh[v] * rs[WHOLE ? 0 : v];     // h = (x - mean) rstd
@@ -976,7 +1030,7 @@ k_gn_backward(const __grid_constant__ GnArgs a) {
             for (int j = 0; j < p.cj; ++j) {
                 const int cv = me.txi + j * kT;
                 if (cv >= cols) break;
-                if (!BUF && (kOne || j > 0)) { px = x + cv * V; pd = dy + cv * V; rows.begin(cnt, load); }
+                if constexpr (!BUF) { if (kOne || j > 0) { px = x + cv * V; pd = dy + cv * V; begin(); } }
                 F2 mean[kGp], k1[kGp], k2[kGp], mul[kP], add[kP];   // dx = mul du - k1 - (x - mean) k2; all but mul and add negated
                 int g[kGv];
                 groups_of<V, WHOLE>(cv * V, p.by_cg, g);
@@ -1016,7 +1070,7 @@ k_gn_backward(const __grid_constant__ GnArgs a) {
                         last(d, h.d);
                     });
                 } else {
-                    rows.run(cnt, load, [&](const Pair<X>& h) {
+                    auto use = [&](const Pair<X>& h) {
                         F2 d[kP], du[kP];
                         widen(h.x, d);
                         widen(h.d, du);
@@ -1026,7 +1080,9 @@ k_gn_backward(const __grid_constant__ GnArgs a) {
                             du[v] = through(s.act, fma2(d[v], mul[v], add[v]), du[v]);
                         }
                         last(d, du);
-                    });
+                    };
+                    if constexpr (RING) rows.template run<Pair<X>>(cnt, fetch, waiting, use);
+                    else rows.run(cnt, load, use);
                 }
             }
         }
@@ -1076,7 +1132,7 @@ bool in_spans(const GnShape& s, int esize, int W, int slabs, bool backward) {
 // that a slab can lie in.
 void cut_spans(GnPlan& p, const GnShape& s, int esize, bool backward, int64_t items) {
     p.total = items * s.S;
-    const int at_a_time = (backward ? 2 : 3) * kSms - kAffineBlocks;
+    const int at_a_time = (backward ? 3 : 4) * kSms - kAffineBlocks;
     int64_t per = (p.total + at_a_time - 1) / at_a_time;
     const int64_t least = (8 * 1024 + p.W * esize - 1) / (p.W * esize);
     if (per < least) per = least;
@@ -1096,6 +1152,9 @@ int64_t part_rows(const GnShape& s) {
     return cap < s.per_set ? cap : s.per_set;
 }
 
+// the rings of a plan that is not buffered (accesses of four bytes and more)
+size_t ring_bytes(int V, int esize, bool backward) { return V * esize >= 4 ? (size_t)2 * kRingPairs * kT * V * esize * (backward ? 2 : 1) : 0; }
+
 size_t smem_bytes(const GnShape& s, const GnPlan& p, bool backward, int task) {
     const size_t nb = (size_t)p.ns * p.gs;
     if (!backward) {
@@ -1104,7 +1163,7 @@ size_t smem_bytes(const GnShape& s, const GnPlan& p, bool backward, int task) {
     }
     const size_t wide = p.W < kT * p.V ? p.W : kT * p.V;
     const size_t across = p.tr > 1 ? (p.ns * wide > kT ? p.ns * wide : (size_t)kT) : 0;
-    if (task == kApply) return sizeof(float2) * nb;
+    if (task == kApply) return p.buf + sizeof(float2) * nb;
     return p.buf + sizeof(float) * (2 * (size_t)kT * p.V + 2 * across + 2 * (size_t)p.W) + sizeof(float2) * nb;
 }
 
@@ -1132,6 +1191,7 @@ GnPlan make_plan(const GnShape& s, int esize, int vmax, bool backward) {
     p.parts = 1;
     const int unit = s.Cg % V == 0 ? s.Cg / V : s.Cg;
     p.by_tx.set(p.tx); p.by_tr.set(p.tr); p.by_gs.set(p.gs); p.by_cg.set(s.Cg); p.by_unit.set(unit < p.tx || s.Cg % V ? unit : p.tx);
+    p.buf = ring_bytes(V, esize, backward);
     p.spans = in_spans(s, esize, p.W, p.slabs, backward);
     if (p.spans) {
         cut_spans(p, s, esize, backward, batch_of(s, esize, backward) * p.slabs);
