@@ -6,11 +6,11 @@
 // of whole groups that is at least 128 bytes wide.  There are two ways through a sample's slab:
 //   - one thread block takes it whole (or several samples' where they have few positions).  What a thread has read for the
 //     sums waits in shared memory: asynchronous copies that only this thread reads back, so no barrier guards them;
-//   - slabs that are too large for that, or too few to fill the GPU, are laid end to end, all their positions in one row,
-//     and the row is cut into as many equal spans as thread blocks run at a time: one launch for the sums of each slab's part
-//     in a span, one that merges them and goes over the values again.  Every SM has the same work, and what a thread
-//     sets up serves as many positions as can be.  Samples are taken in batches that the L2 cache holds, the second
-//     launch starting from the end, so that its reads are served there.
+//   - slabs that are too large for that, or too few to fill the GPU, are cut into equal chunks of positions, as many as thread
+//     blocks run at a time: one launch for the chunks' sums, one that merges them and goes over the values again, from the
+//     end, so that the L2 cache serves what it still holds.  (Spans of equal length over slabs laid end to end, which give
+//     every SM the same work, were slower: a block whose span holds the end of a slab and the start of the next sets up
+//     and sums up twice, 5 us each, and the launch waits for it: 36 against 25 us for 32 x 3136 x 256 bf16.)
 // The sums of a slab could also meet inside a cluster of thread blocks that keep the slab in their shared memory.  Built and
 // measured: loading, summing and writing then follow one another on the whole GPU, and 32 x 3136 x 256 bf16 took 37 us
 // forward and 122 us backward.
@@ -33,7 +33,7 @@ namespace rfast {
 namespace {
 
 constexpr int kT = 256;                                    // threads per block
-constexpr int kRingPairs = 4;                              // pairs of rows that a thread's ring holds
+constexpr int kRingPairs = 3;                              // pairs of rows that a thread's ring holds
 
 template <int BYTES> struct Word;
 template <> struct Word<16> { typedef uint4 type; };
@@ -246,11 +246,8 @@ struct GnPlan {
     int W, gs, slabs;                  // channels and groups of a slab
     int tx, cj;                        // threads across the slab, passes over its width
     int tr, ns;                        // threads down the positions of a sample, samples per item
-    bool spans;                        // two launches over spans; otherwise one, a thread block taking whole slabs
-    int64_t per;                       // positions in a span
-    int64_t total;                     // positions of all slabs of a launch
-    int pieces;                        // spans that a slab can lie in, at most
-    int blocks;                        // spans, at most
+    int chunks;                        // of a slab's positions; 0: one launch, a thread block taking whole slabs
+    int rows;                          // positions of a chunk
     int each, more;                    // one launch: positions per thread, the first `more` rows of threads one more
     Divisor by_tx, by_tr, by_gs, by_cg, by_unit;    // by_unit: entries of a group in one row of threads
     int rpt;                           // positions per thread (buffered)
@@ -274,14 +271,14 @@ struct GnArgs {
     int set_row_stride;
     float *mean, *rstd;                // [N][G]: out (forward), in (backward)
     float *dgamma, *dbeta;             // backward: where the sums of a set go
-    float4* gpart;                     // spans: [N][G][pieces] count, mean and squared deviations, or the two sums of the backward pass
+    float4* gpart;                     // chunks: [N][G][chunks] count, mean and squared deviations, or the two sums of the backward pass
     float* part;                       // backward: rows of [2][C], du and du h summed; a row per thread block of a set or per
-                                       // sample and piece
-    int64_t n0;                        // spans: first sample of this launch
+                                       // sample and chunk
+    int64_t n0;                        // chunks: first sample of this launch
 };
 
 // A thread block's task: everything in one launch (what it reads kept in shared memory, or read twice where that is too small
-// or accesses are too narrow), the sums over a span, or what follows from them.
+// or accesses are too narrow), the sums over a chunk, or what follows from them.
 enum { kWhole = 0, kSums = 1, kApply = 2, kReread = 3 };
 
 __device__ __forceinline__ const float* affine_row(const GnArgs& a, const float* base, int64_t set) {
@@ -306,26 +303,24 @@ __device__ __forceinline__ Seat seat_of(const GnPlan& p) {
     return s;
 }
 
-// The part of a slab that a span holds.  Slabs lie end to end, those of a sample next to one another.
+// What a thread block has before it: all positions of a slab, or a chunk of them.
 struct Part {
-    int64_t n;                         // sample
+    int64_t n;                         // (first) sample
     int slab;
-    int64_t from;                      // positions [from, from + count)
+    int64_t from;                      // chunks: positions [from, from + count)
     int count;
-    int piece, pieces;                 // which of the slab's parts this is, and how many it has
+    int piece;                         // which chunk
 };
-__device__ __forceinline__ Part part_at(const GnArgs& a, int64_t at, int64_t end, int64_t span) {
+// Chunks come on x, slabs on y, samples on z; BACK: from the end.
+template <bool BACK>
+__device__ __forceinline__ Part part_of(const GnArgs& a) {
     Part q;
-    const int64_t item = (int64_t)((uint64_t)at / (uint64_t)a.s.S);
-    q.from = at - item * a.s.S;
+    q.piece = BACK ? a.p.chunks - 1 - (int)blockIdx.x : blockIdx.x;
+    q.slab = blockIdx.y;
+    q.n = a.n0 + (BACK ? gridDim.z - 1 - blockIdx.z : blockIdx.z);
+    q.from = (int64_t)q.piece * a.p.rows;
     const int64_t left = a.s.S - q.from;
-    q.count = (int)(left < end - at ? left : end - at);
-    const unsigned n = (unsigned)item / (unsigned)a.p.slabs;     // a launch has fewer than 2^31 slabs
-    q.slab = (int)(item - (int64_t)n * a.p.slabs);
-    q.n = a.n0 + n;
-    const int64_t first = (int64_t)((uint64_t)(at - q.from) / (uint64_t)a.p.per), last = (int64_t)((uint64_t)(at - q.from + a.s.S - 1) / (uint64_t)a.p.per);
-    q.piece = (int)(span - first);
-    q.pieces = (int)(last - first) + 1;
+    q.count = left < a.p.rows ? (int)left : a.p.rows;
     return q;
 }
 __device__ __forceinline__ int rows_of(int count, int rr, int tr) { return rr < count ? (int)((unsigned)(count - rr - 1) / (unsigned)tr) + 1 : 0; }
@@ -375,7 +370,7 @@ __device__ __forceinline__ int team_size(int entries) {
 }
 
 // ---- forward --------------------------------------------------------------------------------------
-// kWhole, kReread: grid = (items, slabs).  kSums, kApply: grid = spans; kApply takes them back to front.
+// kWhole, kReread: grid = (items, slabs).  kSums, kApply: grid = (chunks, slabs, samples of the launch).
 template <class T, int V, bool WHOLE, int TASK>
 __global__ void __launch_bounds__(kT, WHOLE ? 4 : 3)
 k_gn_forward(const __grid_constant__ GnArgs a) {
@@ -399,20 +394,10 @@ k_gn_forward(const __grid_constant__ GnArgs a) {
     const Seat me = seat_of(p);
     const int64_t step = (int64_t)p.tr * a.xs, ostep = (int64_t)p.tr * a.os;
     if (TASK == kSums) asm volatile("griddepcontrol.launch_dependents;");
-    bool waited = false;
-
-    const int64_t span = TASK == kApply ? gridDim.x - 1 - blockIdx.x : blockIdx.x;
-    int64_t at = kOne ? 0 : span * p.per;
-    const int64_t end = kOne ? 1 : min(at + p.per, p.total);
-    while (at < end) {
+    {
         Part part;
-        if (kOne) {
-            part.n = (int64_t)blockIdx.x * p.ns; part.slab = blockIdx.y; part.from = 0;
-            at = end;
-        } else {
-            part = part_at(a, at, end, span);
-            at += part.count;
-        }
+        if (kOne) { part.n = (int64_t)blockIdx.x * p.ns; part.slab = blockIdx.y; part.from = 0; part.piece = 0; }
+        else part = part_of<TASK == kApply>(a);
         const int slab = part.slab, gs = min(p.gs, s.G - slab * p.gs);      // the last slab may be narrower
         const int64_t n = part.n + me.sl, r0 = part.from + me.rr;            // this thread's sample and first position
         const int cnt = kOne ? (n < s.N ? me.rows : 0) : me.on ? rows_of(part.count, me.rr, p.tr) : 0;
@@ -573,7 +558,7 @@ k_gn_forward(const __grid_constant__ GnArgs a) {
                 if (in && lane == 0) {
                     const int64_t to = (part.n + sl) * s.G + slab * p.gs + g;
                     if (TASK == kSums) {
-                        a.gpart[to * p.pieces + part.piece] = make_float4(cn, mean, m2, 0.f);
+                        a.gpart[to * p.chunks + part.piece] = make_float4(cn, mean, m2, 0.f);
                     } else {
                         const float rstd = rsqrtf(m2 / ((float)s.S * (float)s.Cg) + s.eps);
                         fin[b] = make_float2(mean, rstd);
@@ -581,28 +566,25 @@ k_gn_forward(const __grid_constant__ GnArgs a) {
                     }
                 }
             }
-            if (TASK == kSums) {
-                if (at < end) __syncthreads();               // the entries may be filled again
-                continue;
-            }
+            if (TASK == kSums) return;
         } else {
             if (cnt > 0 && me.txi < cols) begin();           // on their way while the sums are merged
-            if (!waited) { asm volatile("griddepcontrol.wait;" ::: "memory"); waited = true; }
+            asm volatile("griddepcontrol.wait;" ::: "memory");
             // a team of lanes per group
-            const int L = team_size(part.pieces), lane = threadIdx.x & (L - 1);
+            const int L = team_size(p.chunks), lane = threadIdx.x & (L - 1);
             const float all = (float)s.S * (float)s.Cg;
             for (int b0 = 0; b0 < gs; b0 += kT / L) {
                 const int g = b0 + threadIdx.x / L;
                 const bool in = g < gs;
                 const int64_t to = part.n * s.G + slab * p.gs + g;
-                const float4* q = a.gpart + to * p.pieces;
-                const float4 mine = in && lane < part.pieces ? q[lane] : make_float4(0.f, 0.f, 0.f, 0.f);
+                const float4* q = a.gpart + to * p.chunks;
+                const float4 mine = in && lane < p.chunks ? q[lane] : make_float4(0.f, 0.f, 0.f, 0.f);
                 const float ref = __shfl_sync(0xffffffffu, mine.y, threadIdx.x & 31 & ~(L - 1));
                 float cm = mine.x * (mine.x > 0.f ? mine.y - ref : 0.f);
-                for (int k = lane + L; in && k < part.pieces; k += L) { const float4 v = q[k]; cm = fmaf(v.x, v.y - ref, cm); }
+                for (int k = lane + L; in && k < p.chunks; k += L) { const float4 v = q[k]; cm = fmaf(v.x, v.y - ref, cm); }
                 const float mean = ref + team_sum(cm, L) / all;
                 float d = mine.y - mean, m2 = mine.x > 0.f ? fmaf(mine.x * d, d, mine.z) : 0.f;
-                for (int k = lane + L; in && k < part.pieces; k += L) { const float4 v = q[k]; d = v.y - mean; m2 += fmaf(v.x * d, d, v.z); }
+                for (int k = lane + L; in && k < p.chunks; k += L) { const float4 v = q[k]; d = v.y - mean; m2 += fmaf(v.x * d, d, v.z); }
                 m2 = team_sum(m2, L);
                 if (in && lane == 0) {
                     const float rstd = rsqrtf(m2 / all + s.eps);
@@ -666,7 +648,6 @@ k_gn_forward(const __grid_constant__ GnArgs a) {
                 else rows.run(cnt, load, use);
             }
         }
-        if (at < end) __syncthreads();                       // `fin` may be filled again
     }
 }
 
@@ -746,7 +727,7 @@ k_gn_affine(const float* __restrict__ part, int64_t rows, int C, float* __restri
 // per channel dbeta = sum du, dgamma = sum du h over the samples of a set.
 // kWhole, kReread: grid = (parts, slabs, sets); a block takes every `parts`-th item of a set, keeps the channels' sums of its items in
 // shared memory and, buffered, du in fp32 in the place of dy, so that the second pass has no exponentials.
-// kSums, kApply: grid = spans; kApply takes them back to front, its last launch with some blocks more, which form dgamma and dbeta
+// kSums, kApply: grid = (chunks, slabs, samples of the launch), the last kApply with one slab more, whose blocks form dgamma and dbeta
 // meanwhile.
 template <class T, int V, bool WHOLE, int TASK>
 __global__ void __launch_bounds__(kT, WHOLE && (TASK == kSums || TASK == kApply) ? 3 : 2)
@@ -772,36 +753,30 @@ k_gn_backward(const __grid_constant__ GnArgs a) {
     float2* sums = reinterpret_cast<float2*>(col + (TASK == kApply ? 0 : 2 * across));     // [nb] the groups' two sums
     float* acc = reinterpret_cast<float*>(sums + nb);        // [2][W]: dbeta, dgamma of the block's items
 
-    if (TASK == kApply && blockIdx.x >= (unsigned)p.blocks) {
+    if (TASK == kApply && blockIdx.y == (unsigned)p.slabs) {
         asm volatile("griddepcontrol.wait;" ::: "memory");
-        const int64_t rows = s.per_set * p.pieces;
+        const int64_t rows = s.per_set * p.chunks;
         const unsigned tiles = (s.C + 31) / 32, sets = (unsigned)s.N / (unsigned)s.per_set;
-        for (unsigned t = blockIdx.x - p.blocks; t < tiles * sets; t += gridDim.x - p.blocks)
+        for (unsigned t = blockIdx.x + blockIdx.z * gridDim.x; t < tiles * sets; t += gridDim.x * gridDim.z)
             affine_sums(a.part, rows, s.C, t / tiles, (int)(t % tiles), a.dgamma, a.dbeta);
         return;
     }
     if (TASK == kSums) asm volatile("griddepcontrol.launch_dependents;");
-    bool waited = false;
     const Seat me = seat_of(p);
     const int64_t xstep = (int64_t)p.tr * a.xs, dstep = (int64_t)p.tr * a.ds, ostep = (int64_t)p.tr * a.os;
     const float inv_m = 1.f / ((float)s.S * (float)s.Cg);
     if (TASK != kApply)
         for (int c = threadIdx.x; c < 2 * p.W; c += kT) acc[c] = 0.f;
 
-    const int64_t span = TASK == kApply ? p.blocks - 1 - (int)blockIdx.x : blockIdx.x;
-    int64_t at = kOne ? blockIdx.x : span * p.per;           // one launch: items; otherwise positions
-    const int64_t end = kOne ? p.items : min(at + p.per, p.total);
-    while (at < end) {
+    for (int64_t item = kOne ? blockIdx.x : 0; item < (kOne ? p.items : 1); item += kOne ? p.parts : 1) {
         Part part;
         int64_t in_set = 0;                                  // one launch: this thread's sample within its set
         if (kOne) {
-            part.slab = blockIdx.y; part.from = 0;
-            in_set = at * p.ns + me.sl;
+            part.slab = blockIdx.y; part.from = 0; part.piece = 0;
+            in_set = item * p.ns + me.sl;
             part.n = (int64_t)blockIdx.z * s.per_set + in_set;
-            at += p.parts;
         } else {
-            part = part_at(a, at, end, span);
-            at += part.count;
+            part = part_of<TASK == kApply>(a);
         }
         const int slab = part.slab, gs = min(p.gs, s.G - slab * p.gs), W = gs * s.Cg;      // the last slab may be narrower
         const int64_t n = part.n, r0 = part.from + me.rr;     // this thread's sample and first position
@@ -939,7 +914,7 @@ k_gn_backward(const __grid_constant__ GnArgs a) {
                     const int nc = p.ns * pw, ways = nc >= kT ? 1 : min(kT / nc, p.tr);
                     float *c0s = col, *c1s = col + across;
                     for (int i = threadIdx.x; i < nc * ways; i += kT) {
-                        const int w = i / nc, k = i - w * nc, sl = k / pw;
+                        const int w = ways > 1 ? (unsigned)i / (unsigned)nc : 0, k = i - w * nc, sl = p.ns > 1 ? (unsigned)k / (unsigned)pw : 0;
                         float u0 = 0.f, u1 = 0.f;
                         for (int at = (sl * p.tr + w) * pitch + (k - sl * pw), r = w; r < p.tr; r += ways, at += ways * pitch) {
                             u0 += q0[at];
@@ -991,33 +966,25 @@ k_gn_backward(const __grid_constant__ GnArgs a) {
             if (TASK == kSums) {
                 for (int g = threadIdx.x; g < gs; g += kT) {
                     const float2 q = sums[g];
-                    a.gpart[(n * s.G + slab * p.gs + g) * p.pieces + part.piece] = make_float4(q.x, q.y, 0.f, 0.f);
+                    a.gpart[(n * s.G + slab * p.gs + g) * p.chunks + part.piece] = make_float4(q.x, q.y, 0.f, 0.f);
                 }
-                // the channels' sums: a row per piece, rows of pieces that the slab does not have are zeros
-                float* to = a.part + (n * p.pieces + part.piece) * 2 * s.C + c0;
+                float* to = a.part + (n * p.chunks + part.piece) * 2 * s.C + c0;        // the channels' sums
                 for (int c = threadIdx.x; c < W; c += kT) {
                     to[c] = acc[c];
                     to[s.C + c] = acc[p.W + c];
                 }
-                __syncthreads();
-                for (int c = threadIdx.x; c < 2 * p.W; c += kT) acc[c] = 0.f;
-                if (part.piece + 1 == part.pieces)
-                    for (int k = part.pieces; k < p.pieces; ++k) {
-                        to = a.part + (n * p.pieces + k) * 2 * s.C + c0;
-                        for (int c = threadIdx.x; c < W; c += kT) to[c] = to[s.C + c] = 0.f;
-                    }
-                continue;
+                return;
             }
         } else {
-            if (!waited) { asm volatile("griddepcontrol.wait;" ::: "memory"); waited = true; }
-            // merge the pieces, a team of lanes per group
-            const int L = team_size(part.pieces), lane = threadIdx.x & (L - 1);
+            asm volatile("griddepcontrol.wait;" ::: "memory");
+            // merge the chunks, a team of lanes per group
+            const int L = team_size(p.chunks), lane = threadIdx.x & (L - 1);
             for (int b0 = 0; b0 < gs; b0 += kT / L) {
                 const int g = b0 + threadIdx.x / L;
                 float u0 = 0.f, u1 = 0.f;
                 if (g < gs) {
-                    const float4* q = a.gpart + (n * s.G + slab * p.gs + g) * p.pieces;
-                    for (int k = lane; k < part.pieces; k += L) { const float4 v = q[k]; u0 += v.x; u1 += v.y; }
+                    const float4* q = a.gpart + (n * s.G + slab * p.gs + g) * p.chunks;
+                    for (int k = lane; k < p.chunks; k += L) { const float4 v = q[k]; u0 += v.x; u1 += v.y; }
                 }
                 u0 = team_sum(u0, L);
                 u1 = team_sum(u1, L);
@@ -1086,6 +1053,7 @@ k_gn_backward(const __grid_constant__ GnArgs a) {
                 }
             }
         }
+        if (!kOne) return;
         __syncthreads();                                     // `sums` may be filled again
     }
     if constexpr (kOne) {
@@ -1109,39 +1077,19 @@ k_gn_backward(const __grid_constant__ GnArgs a) {
 // ---- host side ------------------------------------------------------------------------------------
 constexpr int kSms = 148;
 constexpr int kMaxGroupChannels = 8192;                     // a block keeps two sums for every channel of a group
-constexpr int kAffineBlocks = 16;                           // that form dgamma and dbeta beside the last launch over spans
 constexpr size_t kMostSmem = 220 * 1024;
-constexpr int64_t kBatchBytes = (int64_t)64 << 20;          // of the samples between a launch for the sums and the one after it: half of L2
-
-// Samples between a launch for the sums and the one after it: as many as half the L2 cache holds, in batches as equal as possible.
-int64_t batch_of(const GnShape& s, int esize, bool backward) {
-    int64_t per = kBatchBytes / (s.S * s.C * esize * (backward ? 2 : 1));
-    if (per < 1) per = 1;
-    if (per > 65535) per = 65535;
-    const int64_t batches = (s.N + per - 1) / per;
-    return (s.N + batches - 1) / batches;
-}
-
-// Whether slabs of W channels go through spans: where they do not fit the buffer (backward: x and du in fp32), or are fewer than the
-// SMs and take longer than a microsecond or two to read.
-bool in_spans(const GnShape& s, int esize, int W, int slabs, bool backward) {
+// Into how many chunks the positions of slabs of W channels are cut; 0: not at all.  They are where a slab does not fit the buffer
+// (backward: x and du in fp32), or where there are fewer than SMs and each takes longer than a microsecond or two to read.  There
+// are as many as thread blocks run at a time, of 32 positions and 8 KB at least.
+int chunks_of(const GnShape& s, int esize, int W, int slabs, bool whole, bool backward) {
     const int64_t item = s.S * W * esize, items = s.N * slabs;
-    return s.S >= 64 && (item > (backward ? 32 * 1024 : 64 * 1024) || (items < kSms && item > 16 * 1024));
-}
-// Spans of a launch over `items` slabs: one for every thread block that runs at a time, of 32 positions and 8 KB at least.  `pieces`: spans
-// that a slab can lie in.
-void cut_spans(GnPlan& p, const GnShape& s, int esize, bool backward, int64_t items) {
-    p.total = items * s.S;
-    const int at_a_time = (backward ? 3 : 4) * kSms - kAffineBlocks;
-    int64_t per = (p.total + at_a_time - 1) / at_a_time;
-    const int64_t least = (8 * 1024 + p.W * esize - 1) / (p.W * esize);
-    if (per < least) per = least;
-    if (per < 32) per = 32;
-    if (per > p.total) per = p.total;
-    if (per > 0x7fffffff) per = 0x7fffffff;
-    p.per = per;
-    p.blocks = (int)((p.total + per - 1) / per);
-    p.pieces = (int)((s.S + per - 2) / per) + 1;
+    if (s.S < 64 || (item <= (backward ? 32 * 1024 : 64 * 1024) && (items >= kSms || item <= 16 * 1024))) return 0;
+    const int64_t at_a_time = (backward ? whole ? 3 : 2 : whole ? 4 : 3) * kSms;
+    int64_t chunks = at_a_time / items;
+    if (chunks > item / (8 * 1024)) chunks = item / (8 * 1024);
+    if (chunks > s.S / 32) chunks = s.S / 32;
+    const int64_t least = (s.S + 0x3fffffff) / 0x40000000;   // a chunk's positions are counted in 32 bits
+    return (int)(chunks < least ? least : chunks);
 }
 
 // One launch: blocks that share a set's sums at most.
@@ -1192,9 +1140,10 @@ GnPlan make_plan(const GnShape& s, int esize, int vmax, bool backward) {
     const int unit = s.Cg % V == 0 ? s.Cg / V : s.Cg;
     p.by_tx.set(p.tx); p.by_tr.set(p.tr); p.by_gs.set(p.gs); p.by_cg.set(s.Cg); p.by_unit.set(unit < p.tx || s.Cg % V ? unit : p.tx);
     p.buf = ring_bytes(V, esize, backward);
-    p.spans = in_spans(s, esize, p.W, p.slabs, backward);
-    if (p.spans) {
-        cut_spans(p, s, esize, backward, batch_of(s, esize, backward) * p.slabs);
+    p.chunks = chunks_of(s, esize, p.W, p.slabs, s.Cg % V == 0, backward);
+    if (p.chunks) {
+        p.rows = (int)((s.S + p.chunks - 1) / p.chunks);
+        p.chunks = (int)((s.S + p.rows - 1) / p.rows);      // none is empty
         return p;
     }
     p.each = (int)(s.S / p.tr); p.more = (int)(s.S % p.tr);
@@ -1218,8 +1167,8 @@ GnPlan make_plan(const GnShape& s, int esize, int vmax, bool backward) {
 }
 
 // Bytes of the workspace for a plan: the groups' partial sums, then the channels' rows.
-size_t group_bytes(const GnShape& s, const GnPlan& p) { return p.spans ? (size_t)s.N * s.G * p.pieces * sizeof(float4) : 0; }
-size_t row_bytes(const GnShape& s, const GnPlan& p) { return (size_t)(p.spans ? s.N * p.pieces : s.N / s.per_set * part_rows(s)) * 2 * s.C * sizeof(float); }
+size_t group_bytes(const GnShape& s, const GnPlan& p) { return p.chunks ? (size_t)s.N * s.G * p.chunks * sizeof(float4) : 0; }
+size_t row_bytes(const GnShape& s, const GnPlan& p) { return (size_t)(p.chunks ? s.N * p.chunks : s.N / s.per_set * part_rows(s)) * 2 * s.C * sizeof(float); }
 // The most that any plan of the shape takes, whatever addresses and strides allow.
 size_t workspace_bytes_of(const GnShape& s, int esize, bool backward) {
     size_t most = 0;
@@ -1250,7 +1199,7 @@ template <class T, int V, bool WHOLE>
 cudaError_t launch_whole(GnArgs& a, bool backward, cudaStream_t st) {
     const GnPlan& p = a.p;
     auto smem = [&](int task) { return smem_bytes(a.s, p, backward, task); };
-    if (!p.spans) {
+    if (!p.chunks) {
         const dim3 grid((unsigned)(backward ? p.parts : p.items), p.slabs, backward ? (unsigned)(a.s.N / a.s.per_set) : 1);
         if constexpr (sizeof(T) * V >= 4) {
             if (p.buffered) return backward ? launch_task(k_gn_backward<T, V, WHOLE, kWhole>, grid, a, smem(kWhole), false, st)
@@ -1259,19 +1208,16 @@ cudaError_t launch_whole(GnArgs& a, bool backward, cudaStream_t st) {
         return backward ? launch_task(k_gn_backward<T, V, WHOLE, kReread>, grid, a, smem(kReread), false, st)
                         : launch_task(k_gn_forward<T, V, WHOLE, kReread>, grid, a, smem(kReread), false, st);
     }
-    const int64_t batch = batch_of(a.s, (int)sizeof(T), backward);
     cudaError_t e = cudaSuccess;
-    for (a.n0 = 0; a.n0 < a.s.N && e == cudaSuccess; a.n0 += batch) {
-        const int64_t left = a.s.N - a.n0, count = left < batch ? left : batch;
-        a.p.total = count * p.slabs * a.s.S;                 // the last batch may be smaller; its spans keep their length
-        a.p.blocks = (int)((a.p.total + p.per - 1) / p.per);
-        const dim3 grid(a.p.blocks), next(a.p.blocks + (backward && count == left ? kAffineBlocks : 0));
+    for (a.n0 = 0; a.n0 < a.s.N && e == cudaSuccess; a.n0 += 65535) {
+        const int64_t left = a.s.N - a.n0;
+        const dim3 grid(p.chunks, p.slabs, (unsigned)(left < 65535 ? left : 65535)), next(grid.x, grid.y + (backward && left <= 65535 ? 1 : 0), grid.z);
         if (backward) {
             e = launch_task(k_gn_backward<T, V, WHOLE, kSums>, grid, a, smem(kSums), false, st);
             if (e == cudaSuccess) e = launch_task(k_gn_backward<T, V, WHOLE, kApply>, next, a, smem(kApply), true, st);
         } else {
             e = launch_task(k_gn_forward<T, V, WHOLE, kSums>, grid, a, smem(kSums), false, st);
-            if (e == cudaSuccess) e = launch_task(k_gn_forward<T, V, WHOLE, kApply>, next, a, smem(kApply), true, st);
+            if (e == cudaSuccess) e = launch_task(k_gn_forward<T, V, WHOLE, kApply>, grid, a, smem(kApply), true, st);
         }
     }
     return e;
@@ -1440,7 +1386,7 @@ extern "C" int rfast_group_norm_backward(const rfast_gn_shape* g, const void* d_
     a.part = (float*)((char*)workspace + group_bytes(a.s, a.p));
     if (a.p.slabs > 65534 || sets > 65535) return op_fail(err, err_len, RFAST_EINVAL, "%s: too many groups or sets", me);
     e = launch_typed(a, g->type, true, st);
-    if (e == cudaSuccess && !a.p.spans && a.p.parts > 1) {
+    if (e == cudaSuccess && !a.p.chunks && a.p.parts > 1) {
         k_gn_affine<<<dim3((a.s.C + 31) / 32, (unsigned)sets), kT, 0, st>>>(a.part, a.p.parts, a.s.C, d_dgamma, d_dbeta);
         e = cudaGetLastError();
     }
