@@ -33,6 +33,11 @@ SHAPES = {
     "odd": (3, 7, 15, 5, 3),
     "hidden layer": (96, 1, 512, 16, 12),
     "hidden layer, one set": (200, 1, 384, 8, 1),
+    "hidden layer, many rows": (3001, 1, 256, 8, 1),
+    "hidden layer, twenty a group": (70, 1, 120, 6, 2),
+    "hidden layer, wide groups": (33, 1, 1000, 2, 3),
+    "hidden layer, one row a set": (6, 1, 64, 2, 6),
+    "hidden layer, narrow groups": (130, 1, 72, 9, 2),
     "three a group": (2, 50, 96, 32, 1),
     "ten a group": (2, 330, 320, 32, 2),
     "ragged slab": (2, 19, 200, 25, 1),
