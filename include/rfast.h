@@ -61,7 +61,9 @@ typedef struct rfast_graph {
  *   SOFTMAX          x = [W (C x F, row c = class c) | bias (C)], cross-entropy
  *   MLP              x = [W1 (H x F) | b1 (H) | W2 (C x H) | b2 (C)], hidden = relu(W1 a + b1),
  *                    cross-entropy; operands of the matrix products are rounded to bf16
- *                    (round-to-nearest-even from fp32), accumulation in fp32
+ *                    (round-to-nearest-even from fp32), accumulation in fp32.  With norm_groups > 0
+ *                    x = [... | gamma (H) | beta (H)] and hidden = act(group norm(W1 a + b1)), the hidden
+ *                    units of each sampled row in norm_groups groups of neighbours (see rfast_group_norm)
  *   LOGISTIC_SPARSE  f_i(x) = 1/B sum_k log(1 + exp(-y_k a_k.x)), y in {-1,+1}, a_k sparse */
 enum {
     RFAST_MODEL_QUAD_DIAG       = 0,
@@ -105,7 +107,19 @@ typedef struct rfast_problem {
                               /* RFAST_TRACKER_RUNNING_SUMS: rho_ji and rho~_ij as Algorithm 1 prints  */
                               /* them; RFAST_TRACKER_BUCKETS: the edge masses of the augmented system   */
                               /* (Appendix F), see below                                               */
+    int32_t     norm_groups;  /* MLP: groups of the hidden layer's norm, a divisor of n_hidden; 0 = no norm and relu */
+    int32_t     norm_act;     /* MLP with a norm: RFAST_ACT_*                                              */
+    double      norm_eps;     /* MLP with a norm: >= 2^-126                                                */
+    int32_t     descent;      /* RFAST_DESCENT_*: the local step S1                                        */
+    double      beta1, beta2, adam_eps, weight_decay;   /* RFAST_DESCENT_ADAMW*, as in rfast_adamw          */
 } rfast_problem;
+
+/* The local step S1.  PLAIN: v_i = x_i - gamma^t z_i as Algorithm 1 prints it.  ADAMW, ADAMW8: v_i is x_i after
+ * one AdamW step (see rfast_adamw_step: moments in 32 or in 8 bits) with the tracker z_i in the role of the
+ * gradient, gamma^t as lr and the worker's own count t_i + 1 as t -- gradient tracking with adaptive momentum.
+ * The moments are private to a worker: packets, mixing and tracking stay as they are, so Lemma 3 holds.
+ * Not for the element-wise objective, whose remembered gradient is recomputed from x. */
+enum { RFAST_DESCENT_PLAIN = 0, RFAST_DESCENT_ADAMW = 1, RFAST_DESCENT_ADAMW8 = 2 };
 
 /* RFAST_TRACKER_BUCKETS.  S2b consumes rho_ij^{tau_new} - rho~_ij = the sum of a_ij z^{t+1/2}_j over
  * the sender's local iterations tau_prev < t <= tau_new: the mass that is on the edge, the quantity
@@ -168,6 +182,8 @@ enum {
     RFAST_STATE_TAU_V        = 13, /* int32 [|E_R|]    tau_v per G_R edge after the rounds run so far   */
                                    /*       (the stamp the receiver mixed in at its last activation)    */
     RFAST_STATE_TAU_RHO      = 14, /* int32 [|E_C|]    tau_rho per G_C edge after the rounds run so far */
+    RFAST_STATE_ADAM_M       = 15, /* float [n][p]     RFAST_DESCENT_ADAMW*: first and second moments    */
+    RFAST_STATE_ADAM_V       = 16, /* float [n][p]     (8-bit moments: the values they stand for)         */
     /* other names for the same views */
     RFAST_STATE_ACT_COUNTS           = RFAST_STATE_T_LOCAL,      /* activations per node = t_i          */
     RFAST_STATE_COMPILED_STAMPS_V    = RFAST_STATE_USED_TAU_V,
@@ -275,6 +291,7 @@ int rfast_seek(rfast_ctx* ctx, int32_t round);
  *                   the consumed version kept alive: where tau_rho = t_j it is the same row as
  *                   RHO_LATEST, so write RHO_BUF before RHO_LATEST
  *   V_LATEST        rows flagged by RFAST_STATE_V_HELD; other rows are ignored
+ *   ADAM_M, ADAM_V  32-bit moments of all n rows (RFAST_ESTATE for 8-bit ones: a checkpoint carries those)
  * Packets in flight that are neither the latest nor the buffered version of their edge are
  * written with rfast_write_packet.  Integer views cannot be written (RFAST_EINVAL): they
  * follow from the schedule and the round, see rfast_seek. */
@@ -385,7 +402,7 @@ int     rfast_checkpoint_load(rfast_ctx* ctx, const void* src, size_t bytes);
  *   out[6] the merit function of the non-convex analysis (Section V-B),
  *          M_F(x) = || grad F(xbar) ||^2 + || x - 1 xbar^T ||^2 = out[5]^2 + out[0]^2 (NaN where out[5] is)
  *   out[7] F(xbar) = sum_i f_i(xbar), the objective of eq. (1) at the mean iterate over every row
- *          of every shard (the loss curve of the experiments in Section VI); NaN for a softmax
+ *          of every shard (the loss curve of the experiments in Section VI), without weight decay; NaN for a softmax
  *          objective with more than 32 classes
  * n_out is 5 (the first five only), 7 or 8; RFAST_EINVAL otherwise.  out is a caller-owned HOST
  * array of doubles. */

@@ -8,7 +8,8 @@ to loss by central finite differences, and loss is the textbook definition writt
 Parameter layouts (x is one flat vector of length p):
   least_squares    x = coefficients [F]
   softmax          x = [W (C x F, row c = class c) | bias (C)]
-  mlp              x = [W1 (H x F) | b1 (H) | W2 (C x H) | b2 (C)],  hidden = relu(W1 a + b1)
+  mlp              x = [W1 (H x F) | b1 (H) | W2 (C x H) | b2 (C)],  hidden = relu(W1 a + b1); with a group norm
+                   x = [... | gamma (H) | beta (H)],  hidden = act(gamma (pre - mean) / std + beta)
   logistic_sparse  x = coefficients [p], labels in {-1,+1}, features in CSR
   quad_diag        f_i(x) = 0.5 * || d_i * (x - b_i) ||^2  (element-wise)
 """
@@ -106,7 +107,8 @@ class MLP:
     with the n_classes-wide output layer are a few columns thin, not GEMM work, and stay in
     full precision, as do sums, biases, ReLU, softmax and all accumulation."""
 
-    def __init__(self, feat, label, n_hidden, n_classes, l2=0.0, round_inputs=True):
+    def __init__(self, feat, label, n_hidden, n_classes, l2=0.0, round_inputs=True, norm_groups=0, norm_act="relu", norm_eps=1e-5):
+        self.groups, self.act, self.eps = norm_groups, norm_act, norm_eps
         self.A, self.lab = feat, label
         self.F, self.H, self.C = feat.shape[2], n_hidden, n_classes
         self.l2 = l2
@@ -117,7 +119,28 @@ class MLP:
         o1 = H * F
         o2 = o1 + H
         o3 = o2 + C * H
-        return x[:o1].reshape(H, F), x[o1:o2], x[o2:o3].reshape(C, H), x[o3:]
+        return x[:o1].reshape(H, F), x[o1:o2], x[o2:o3].reshape(C, H), x[o3:o3 + C]
+
+    def _norm(self, pre, x):
+        """Group norm of the rows of pre: normalised rows, 1 / std per row and group, value before the activation."""
+        H = self.H
+        gamma, beta = x[-2 * H:-H], x[-H:]
+        q = pre.reshape(len(pre), self.groups, -1)
+        d = q - q.mean(axis=2, keepdims=True)
+        rstd = 1.0 / np.sqrt((d * d).mean(axis=2, keepdims=True) + self.eps)
+        hat = (d * rstd).reshape(len(pre), H)
+        return hat, rstd, hat * gamma + beta
+
+    def _act(self, u):
+        return np.maximum(u, 0.0) if self.act == "relu" else u / (1.0 + np.exp(-u)) if self.act == "silu" else u
+
+    def _slope(self, u):
+        if self.act == "relu":
+            return (u > 0.0).astype(np.float64)
+        if self.act == "silu":
+            s = 1.0 / (1.0 + np.exp(-u))
+            return s * (1.0 + u * (1.0 - s))
+        return np.ones_like(u)
 
     def _forward(self, i, x, idx):
         q = self.q
@@ -125,7 +148,7 @@ class MLP:
         lab = self.lab[i][idx]
         W1, b1, W2, b2 = self._split(x)
         pre = A @ q(W1).T + b1
-        h = np.maximum(pre, 0.0)
+        h = self._act(self._norm(pre, x)[2]) if self.groups else np.maximum(pre, 0.0)
         logits = h @ W2.T + b2
         return A, lab, pre, h, logits
 
@@ -144,10 +167,19 @@ class MLP:
         gW2 = dlog.T @ h                          #                            [C, H]
         gb2 = dlog.sum(axis=0)
         dh = dlog @ W2                            #                            [B, H]
-        dpre = dh * (pre > 0.0)
+        extra = []
+        if self.groups:
+            hat, rstd, u = self._norm(pre, x)
+            du = dh * self._slope(u)
+            extra = [(du * hat).sum(axis=0), du.sum(axis=0)]
+            s = (du * x[-2 * self.H:-self.H]).reshape(len(pre), self.groups, -1)
+            hq = hat.reshape(s.shape)
+            dpre = (rstd * (s - s.mean(axis=2, keepdims=True) - hq * (s * hq).mean(axis=2, keepdims=True))).reshape(pre.shape)
+        else:
+            dpre = dh * (pre > 0.0)
         gW1 = q(dpre).T @ A                       # A already rounded          [H, F]
         gb1 = dpre.sum(axis=0)
-        return np.concatenate([gW1.ravel(), gb1, gW2.ravel(), gb2]) + self.l2 * x
+        return np.concatenate([gW1.ravel(), gb1, gW2.ravel(), gb2] + extra) + self.l2 * x
 
 
 class LogisticSparse:
@@ -189,7 +221,8 @@ def make_model(wl, **kw):
     if m == "softmax":
         return Softmax(d["feat"], d["label"], wl.dims["n_classes"], wl.l2)
     if m == "mlp":
-        return MLP(d["feat"], d["label"], wl.dims["n_hidden"], wl.dims["n_classes"], wl.l2, **kw)
+        norm = {k: wl.dims[k] for k in ("norm_groups", "norm_act", "norm_eps") if k in wl.dims}
+        return MLP(d["feat"], d["label"], wl.dims["n_hidden"], wl.dims["n_classes"], wl.l2, **norm, **kw)
     if m == "logistic_sparse":
         return LogisticSparse(d["sp_rowptr"], d["sp_col"], d["sp_val"], d["label"], wl.rows, wl.l2)
     raise KeyError(m)

@@ -45,15 +45,37 @@ def _out_lists(n, rowptr, col):
     return out
 
 
+_E4M3 = np.array([(f / 8.0) * 2.0 ** -6 if e == 0 else (1 + f / 8.0) * 2.0 ** (e - 7) for e in range(16) for f in range(8) if not (e == 15 and f == 7)])
+
+
+def _held8(v, least):
+    """What 8-bit codes of v stand for: e4m3 values in units of max / 448 of each block of 256, nearest, ties to even;
+    `least`: the smallest code of a positive value."""
+    out = np.empty_like(v)
+    for b in range(0, len(v), 256):
+        q = v[b:b + 256]
+        scale = max(np.abs(q).max() / 448.0, 2.0 ** -100)
+        a = np.abs(q) / scale
+        a = np.where((a > 0) & (a < least), least, a)
+        hi = np.searchsorted(_E4M3, a).clip(1, len(_E4M3) - 1)
+        lo = hi - 1
+        up = a - _E4M3[lo] > _E4M3[hi] - a
+        tie = a - _E4M3[lo] == _E4M3[hi] - a
+        k = np.where(tie, np.where(lo % 2 == 0, lo, hi), np.where(up, hi, lo))
+        out[b:b + 256] = np.sign(q) * _E4M3[k] * scale
+    return out
+
+
 class RFastOracle:
     """State of all n nodes plus the packets in flight."""
 
     def __init__(self, n, p, alpha, G_R, G_C, grad, x0=None, dtype=np.float64,
-                 increments_only=False):
+                 increments_only=False, descent=None):
         """G_R, G_C: objects with rowptr, col, w, diag (receiver-CSR; w[e] = M[receiver, col[e]]).
         grad(i, x, idx) -> stochastic gradient of f_i at x on sample rows idx (or None).
         increments_only=True builds the *wrong* tracker used as a negative control: it sends
-        the increment a_ji z^{t+1/2} instead of the running sum, so dropped mass is lost."""
+        the increment a_ji z^{t+1/2} instead of the running sum, so dropped mass is lost.
+        descent: None for S1 as printed, or the AdamW step's constants (see _adamw)."""
         self.n, self.p, self.alpha, self.dtype = n, p, alpha, dtype
         self.R, self.C = G_R, G_C
         self.grad = grad
@@ -83,6 +105,8 @@ class RFastOracle:
         self.inbox_rho = [[] for _ in range(EC)]
         self.round = 0
         self.activations = 0
+        self.descent = descent
+        self.m, self.s = [zero] * n, [zero] * n
         # integer artefacts, in event order then in-edge (CSR) order
         self.used_tau_v = []
         self.used_tau_rho = []
@@ -122,7 +146,7 @@ class RFastOracle:
         R, C, alpha = self.R, self.C, self.alpha
         self._deliver(i, r)
         # (S1) local descent
-        v = self.x[i] - alpha * self.z[i]
+        v = self.x[i] - alpha * self.z[i] if self.descent is None else self._adamw(i, alpha)
         # (S2a) consensus mix over N_i^in(W)
         x_new = R.diag[i] * v
         for e in range(int(R.rowptr[i]), int(R.rowptr[i + 1])):
@@ -156,6 +180,19 @@ class RFastOracle:
             self.rho_tilde[e] = self.rho_recv[e]
         self.x[i], self.z[i], self.g[i], self.v_latest[i] = x_new, z_new, g_new, v
         self.activations += 1
+
+    def _adamw(self, i, lr):
+        """S1 as an AdamW step with the tracker as its gradient; moments in 64 bits, or ("adamw8") in 8 bits with a
+        scale for each block of 256, the second moment as its root."""
+        d = self.descent
+        b1, b2, t = d.get("beta1", 0.9), d.get("beta2", 0.999), self.t[i] + 1
+        m = b1 * self.m[i] + (1 - b1) * self.z[i]
+        s = b2 * self.s[i] + (1 - b2) * self.z[i] ** 2
+        v = self.x[i] * (1 - lr * d.get("weight_decay", 0.0)) - lr * (m / (1 - b1 ** t)) / (np.sqrt(s / (1 - b2 ** t)) + d.get("eps", 1e-8))
+        if d["kind"] == "adamw8":
+            m, s = _held8(m, 0.0), _held8(np.sqrt(s), 2.0 ** -9) ** 2
+        self.m[i], self.s[i] = m, s
+        return v
 
     # -- views -----------------------------------------------------------------------------
     def X(self):
@@ -225,6 +262,7 @@ def run_schedule(orc: RFastOracle, sch, K=None, after_round=None):
 
 def from_workload(wl, grad, dtype=np.float64, **kw):
     """Oracle for a workload object (fields n, p, alpha, G_R, G_C, x0) and a gradient callable."""
+    kw.setdefault("descent", getattr(wl, "descent", None))
     return RFastOracle(wl.n, wl.p, wl.alpha, wl.G_R, wl.G_C, grad, wl.x0, dtype=dtype, **kw)
 
 

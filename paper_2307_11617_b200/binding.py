@@ -27,7 +27,9 @@ Q_ROUND, Q_EVENTS_TOTAL, Q_EVENTS_RUN, Q_LAUNCHES, Q_BYTES_RUN, Q_V_SLOTS, Q_RHO
 Q_DEVICE_BYTES, Q_N_USED_TAU_V, Q_N_USED_TAU_RHO, Q_BYTES_TOTAL = 7, 8, 9, 10
 Q_METHOD_BYTES_RUN, Q_METHOD_BYTES_TOTAL = 11, 12
 STATE_V_LATEST, STATE_V_HELD, STATE_TAU_V, STATE_TAU_RHO = 11, 12, 13, 14
-_FLOAT_VIEWS = (STATE_X, STATE_Y, STATE_G_LAST, STATE_RHO_LATEST, STATE_RHO_BUF, STATE_V_LATEST)
+STATE_ADAM_M, STATE_ADAM_V = 15, 16
+_FLOAT_VIEWS = (STATE_X, STATE_Y, STATE_G_LAST, STATE_RHO_LATEST, STATE_RHO_BUF, STATE_V_LATEST, STATE_ADAM_M, STATE_ADAM_V)
+DESCENT_IDS = {"plain": 0, "adamw": 1, "adamw8": 2}
 NOT_HELD = 1
 GRAPH_R, GRAPH_C = 0, 1
 
@@ -51,7 +53,9 @@ class _Problem(C.Structure):
                 ("quad_d", C.c_void_p), ("quad_b", C.c_void_p), ("feat", C.c_void_p),
                 ("target", C.c_void_p), ("label", C.c_void_p), ("sp_rowptr", C.c_void_p),
                 ("sp_col", C.c_void_p), ("sp_val", C.c_void_p), ("x0", C.c_void_p),
-                ("compensated", C.c_int32), ("tracker", C.c_int32)]
+                ("compensated", C.c_int32), ("tracker", C.c_int32),
+                ("norm_groups", C.c_int32), ("norm_act", C.c_int32), ("norm_eps", C.c_double), ("descent", C.c_int32),
+                ("beta1", C.c_double), ("beta2", C.c_double), ("adam_eps", C.c_double), ("weight_decay", C.c_double)]
 
 
 class _Schedule(C.Structure):
@@ -164,6 +168,13 @@ def _problem(wl, keep):
     P.n_features = int(dims.get("n_features", 0))
     P.n_classes = int(dims.get("n_classes", 0))
     P.n_hidden = int(dims.get("n_hidden", 0))
+    P.norm_groups = int(dims.get("norm_groups", 0))             # group norm in the MLP's hidden layer
+    P.norm_act = ACT_IDS[dims.get("norm_act", "relu")]
+    P.norm_eps = float(dims.get("norm_eps", 1e-5))
+    descent = getattr(wl, "descent", None) or {}                # {"kind": "adamw" | "adamw8", "beta1": ..., ...}
+    P.descent = DESCENT_IDS[descent.get("kind", "plain")]
+    P.beta1, P.beta2 = float(descent.get("beta1", 0.9)), float(descent.get("beta2", 0.999))
+    P.adam_eps, P.weight_decay = float(descent.get("eps", 1e-8)), float(descent.get("weight_decay", 0.0))
     data = getattr(wl, "data", {}) or {}
     spec = {"quad_d": ("d", np.float32), "quad_b": ("b", np.float32), "feat": ("feat", np.float32),
             "target": ("target", np.float32), "label": ("label", np.int32),
@@ -558,7 +569,7 @@ class Engine:
                  STATE_RHO_LATEST: (self.n_edges_c, p), STATE_RHO_BUF: (self.n_edges_c, p),
                  STATE_T_LOCAL: (n,), STATE_TAU_V_END: (self.n_edges_r,),
                  STATE_TAU_RHO_END: (self.n_edges_c,), STATE_ROUND: (1,),
-                 STATE_V_LATEST: (n, p), STATE_V_HELD: (n,), STATE_TAU_V: (self.n_edges_r,),
+                 STATE_V_LATEST: (n, p), STATE_V_HELD: (n,), STATE_ADAM_M: (n, p), STATE_ADAM_V: (n, p), STATE_TAU_V: (self.n_edges_r,),
                  STATE_TAU_RHO: (self.n_edges_c,)}.get(which)
         if which == STATE_USED_TAU_V:
             shape = (self.query(Q_N_USED_TAU_V),)

@@ -12,6 +12,7 @@
 
 #include "kernels.cuh"
 #include "logit_fused.cuh"
+#include "ops.h"
 #include "persist.cuh"
 #include "rfast_internal.h"
 
@@ -20,7 +21,7 @@ using namespace rfast;
 namespace rfast {
 // MLP gradient (tensor-core path), defined in grad_mlp.cu
 struct MlpPlan;
-int  mlp_plan_create(int n, int rows, int F, int H, int C, int B, int64_t stride, int max_events,
+int  mlp_plan_create(int n, int rows, int F, int H, int C, int B, int norm_groups, int norm_act, float norm_eps, int64_t stride, int max_events,
                      const float* d_feat, const __nv_bfloat16* xb, const float* x, float* gbuf, cudaStream_t st,
                      MlpPlan** out, size_t* dev_bytes, std::string& err);
 int  mlp_plan_status(MlpPlan* plan, cudaStream_t st);
@@ -142,6 +143,16 @@ struct rfast_ctx {
     double* d_diag_rowloss = nullptr;
     float* d_diag_x = nullptr;  double* d_diag_acc = nullptr;  EvDesc* d_diag_ev = nullptr;  int* d_diag_bidx = nullptr;
     MlpPlan* mlp = nullptr;
+    int norm_groups = 0, norm_act = 0;  double norm_eps = 0;      // group norm in the MLP's hidden layer
+    // AdamW in the place of S1: moments of every node, factors of the bias correction by local stamp
+    int descent = RFAST_DESCENT_PLAIN;
+    double beta1 = 0, beta2 = 0, adam_eps = 0, weight_decay = 0;
+    void *adam_m = nullptr, *adam_v = nullptr;
+    float *adam_ms = nullptr, *adam_vs = nullptr;                 // 8-bit moments: a scale per block, [n][adam_blocks]
+    float2* d_adam_factor = nullptr;
+    int64_t adam_blocks() const { return (p + kAdamBlock - 1) / kAdamBlock; }
+    size_t adam_bytes() const { return (size_t)n * stride * (descent == RFAST_DESCENT_ADAMW8 ? 1 : sizeof(float)); }
+    size_t adam_scale_bytes() const { return descent == RFAST_DESCENT_ADAMW8 ? (size_t)n * adam_blocks() * sizeof(float) : 0; }
     // compiled schedule
     bool has_sched = false;
     Compiled comp;
@@ -263,12 +274,13 @@ void free_schedule(rfast_ctx* c, bool recycle = false) {
     c->d_ev = c->d_init_ev = nullptr;
     c->vbuf = c->rbuf = c->scratch = nullptr;
     c->d_diag_idx = nullptr; c->d_diag_part = nullptr; c->d_xbar = nullptr; c->d_diag_res = nullptr;
+    c->d_adam_factor = nullptr;
     c->d_act_ptr = nullptr; c->d_alpha_round = nullptr; c->d_bar = nullptr; c->d_pstatus = nullptr;
     c->persist_ok = false;
     c->has_sched = false;
 }
 
-ModelTraffic traffic_of(int model, bool compensated, bool one_pass = false) {
+ModelTraffic traffic_of(int model, bool compensated, bool one_pass = false, int descent = RFAST_DESCENT_PLAIN) {
     ModelTraffic mt;
     mt.elementwise = (model == RFAST_MODEL_QUAD_DIAG);
     mt.data_streams = (mt.elementwise ? 2 : 0) + (compensated ? 2 : 0);
@@ -278,6 +290,11 @@ ModelTraffic traffic_of(int model, bool compensated, bool one_pass = false) {
     mt.grad_track_streams = (model == RFAST_MODEL_LOGISTIC_SPARSE ? 4 : 5) + (mt.elementwise ? 0 : (compensated ? 2 : 0));
     mt.method_streams = 2;    // element-wise: d and b, the remembered gradient recomputed; others: g_old read, g_new written
     if (one_pass) mt.grad_track_streams = 2 + (compensated ? 2 : 0);   // nothing is read twice
+    // AdamW in a pass of its own: x and z read, x written, both moments read and written (8-bit moments: 4 bytes in all)
+    if (descent != RFAST_DESCENT_PLAIN) {
+        mt.grad_track_streams += descent == RFAST_DESCENT_ADAMW8 ? 4 : 7;
+        mt.method_streams += descent == RFAST_DESCENT_ADAMW8 ? 1 : 4;
+    }
     return mt;
 }
 
@@ -287,6 +304,20 @@ int validate_problem(const rfast_problem* p, std::string& err) {
     if (p->n <= 0 || p->n > 65535) return bad("n must be in [1, 65535]");
     if (p->p <= 0) return bad("p must be positive");
     if (!(p->alpha == p->alpha)) return bad("alpha is NaN");
+    if (p->descent != RFAST_DESCENT_PLAIN) {
+        if (p->descent != RFAST_DESCENT_ADAMW && p->descent != RFAST_DESCENT_ADAMW8) return bad("unknown descent");
+        if (p->model == RFAST_MODEL_QUAD_DIAG) return bad("QUAD_DIAG recomputes its remembered gradient from x and takes the plain descent only");
+        if (!(p->beta1 >= 0 && p->beta1 < 1) || !(p->beta2 >= 0 && p->beta2 < 1)) return bad("beta1 and beta2 must be in [0, 1)");
+        if (!((float)p->adam_eps >= 1.17549435e-38f) || !std::isfinite((float)p->adam_eps)) return bad("adam_eps must be at least 2^-126");
+        if (!std::isfinite(p->weight_decay)) return bad("weight_decay must be finite");
+    }
+    if (p->norm_groups != 0) {
+        if (p->model != RFAST_MODEL_MLP) return bad("only the MLP has a hidden layer to normalise");
+        if (p->norm_groups < 0 || p->n_hidden <= 0 || p->n_hidden % p->norm_groups) return bad("norm_groups must divide n_hidden");
+        if (p->n_hidden / p->norm_groups > 8192) return bad("a group of the norm may have 8192 hidden units at most");
+        if (p->norm_act != RFAST_ACT_NONE && p->norm_act != RFAST_ACT_RELU && p->norm_act != RFAST_ACT_SILU) return bad("unknown norm_act");
+        if (!((float)p->norm_eps >= 1.17549435e-38f) || !std::isfinite((float)p->norm_eps)) return bad("norm_eps must be at least 2^-126");
+    }
     switch (p->model) {
         case RFAST_MODEL_QUAD_DIAG:
             if (!p->quad_d || !p->quad_b) return bad("QUAD_DIAG needs quad_d and quad_b");
@@ -306,8 +337,9 @@ int validate_problem(const rfast_problem* p, std::string& err) {
             break;
         case RFAST_MODEL_MLP:
             if (!p->feat || !p->label || p->rows <= 0 || p->batch <= 0) return bad("MLP needs feat, label, rows, batch");
-            if (p->p != (int64_t)p->n_hidden * p->n_features + p->n_hidden + (int64_t)p->n_classes * p->n_hidden + p->n_classes)
-                return bad("MLP needs p = H*F + H + C*H + C");
+            if (p->p != (int64_t)p->n_hidden * p->n_features + p->n_hidden + (int64_t)p->n_classes * p->n_hidden + p->n_classes +
+                            (p->norm_groups > 0 ? 2 * (int64_t)p->n_hidden : 0))
+                return bad(p->norm_groups > 0 ? "MLP with a norm needs p = H*F + H + C*H + C + 2*H" : "MLP needs p = H*F + H + C*H + C");
             break;
         case RFAST_MODEL_LOGISTIC_SPARSE:
             if (!p->sp_rowptr || !p->sp_col || !p->sp_val || !p->label || p->rows <= 0 || p->batch <= 0)
@@ -503,6 +535,14 @@ int reset_state(rfast_ctx* ctx) {
     else CK(cudaMemsetAsync(ctx->x, 0, plane, ctx->stream));
     const int n4 = (int)(ctx->stride / 4);
     if (ctx->zc) CK(cudaMemsetAsync(ctx->zc, 0, plane, ctx->stream));
+    if (ctx->adam_m) {                                        // all bytes zero are moments of zero
+        CK(cudaMemsetAsync(ctx->adam_m, 0, ctx->adam_bytes(), ctx->stream));
+        CK(cudaMemsetAsync(ctx->adam_v, 0, ctx->adam_bytes(), ctx->stream));
+        if (ctx->adam_ms) {
+            CK(cudaMemsetAsync(ctx->adam_ms, 0, ctx->adam_scale_bytes(), ctx->stream));
+            CK(cudaMemsetAsync(ctx->adam_vs, 0, ctx->adam_scale_bytes(), ctx->stream));
+        }
+    }
     if (ctx->model == RFAST_MODEL_QUAD_DIAG) {
         k_quad_grad<<<dim3((n4 + kThreads - 1) / kThreads, ctx->n), kThreads, 0, ctx->stream>>>(
             ctx->x, ctx->quad_d, ctx->quad_b, ctx->z, ctx->stride, n4);
@@ -546,7 +586,7 @@ void rfast_destroy(rfast_ctx* c) {
     if (c->snap_done) cudaEventDestroy(c->snap_done);
     if (c->mlp) mlp_plan_destroy(c->mlp);
     void* ptrs[] = {c->x, c->z, c->zc, c->gbuf, c->x0, c->quad_d, c->quad_b, c->feat, c->target, c->label,
-                    c->sp_ptr, c->sp_tile_ptr, c->sp_col, c->sp_val, c->xb, c->row_tmp,
+                    c->sp_ptr, c->sp_tile_ptr, c->sp_col, c->sp_val, c->xb, c->row_tmp, c->adam_m, c->adam_v, c->adam_ms, c->adam_vs,
                     c->d_diag_rowloss, c->d_diag_x, c->d_diag_acc, c->d_diag_ev, c->d_diag_bidx, c->snap_x, c->snap_y};
     for (void* q : ptrs) if (q) cudaFree(q);
     delete c;
@@ -572,6 +612,9 @@ int rfast_create(const rfast_problem* prob, void* cuda_stream, rfast_ctx** out) 
     ctx->compensated = prob->compensated != 0;
     ctx->rho2 = prob->compensated >= 2;
     ctx->buckets = prob->tracker == RFAST_TRACKER_BUCKETS;
+    ctx->descent = prob->descent;
+    ctx->beta1 = prob->beta1; ctx->beta2 = prob->beta2; ctx->adam_eps = prob->adam_eps; ctx->weight_decay = prob->weight_decay;
+    ctx->norm_groups = prob->norm_groups; ctx->norm_act = prob->norm_act; ctx->norm_eps = prob->norm_eps;
     ctx->stride = (prob->p + 31) / 32 * 32;
     if (ctx->stride / 4 > 0x7fffffff) return set_err(ctx, RFAST_EINVAL, "p too large");
     if ((rc = build_host_graph(prob->G_R, ctx->n, true, ctx->R, err)) != RFAST_OK) return set_err(ctx, rc, "G_R: " + err);
@@ -656,10 +699,18 @@ int rfast_create(const rfast_problem* prob, void* cuda_stream, rfast_ctx** out) 
         CK(dev_alloc(ctx, &ctx->xb, plane));
         CK(cudaMemsetAsync(ctx->xb, 0, plane * sizeof(__nv_bfloat16), ctx->stream));
         size_t mb = 0;
-        rc = mlp_plan_create(ctx->n, ctx->rows, ctx->F, ctx->H, ctx->C, ctx->batch, ctx->stride, ctx->n,
+        rc = mlp_plan_create(ctx->n, ctx->rows, ctx->F, ctx->H, ctx->C, ctx->batch, ctx->norm_groups, ctx->norm_act, (float)ctx->norm_eps, ctx->stride, ctx->n,
                              ctx->feat, ctx->xb, ctx->x, ctx->gbuf, ctx->stream, &ctx->mlp, &mb, err);
         if (rc != RFAST_OK) return set_err(ctx, rc, err);
         ctx->dev_bytes += mb;
+    }
+    if (ctx->descent != RFAST_DESCENT_PLAIN) {
+        CK(dev_alloc(ctx, (uint8_t**)&ctx->adam_m, ctx->adam_bytes()));
+        CK(dev_alloc(ctx, (uint8_t**)&ctx->adam_v, ctx->adam_bytes()));
+        if (ctx->descent == RFAST_DESCENT_ADAMW8) {
+            CK(dev_alloc(ctx, &ctx->adam_ms, (size_t)ctx->n * ctx->adam_blocks()));
+            CK(dev_alloc(ctx, &ctx->adam_vs, (size_t)ctx->n * ctx->adam_blocks()));
+        }
     }
     CK(cudaStreamSynchronize(ctx->stream));    // the caller's arrays may go away now
     plan_logit_fused(ctx, 0);
@@ -775,8 +826,19 @@ static int install_schedule(rfast_ctx* ctx, const rfast_schedule* s, Compiled&& 
     CK(dev_alloc(ctx, &ctx->d_bar, 1, true));
     CK(dev_alloc(ctx, &ctx->d_pstatus, 1, true));
     CK(cudaMemsetAsync(ctx->d_pstatus, 0, sizeof(int), ctx->stream));
+    if (ctx->descent != RFAST_DESCENT_PLAIN) {                // bias corrections by local stamp, formed in 64 bits
+        int most = 0;
+        for (int t : c.t_end) most = std::max(most, t);
+        std::vector<float2> factor((size_t)most);
+        for (int t = 1; t <= most; ++t) {
+            const AdamCoef k = adamw_coef(1.0, ctx->beta1, ctx->beta2, ctx->adam_eps, 0.0, t);
+            factor[t - 1] = make_float2(k.step, k.root);
+        }
+        if ((rc = upload(ctx, &ctx->d_adam_factor, factor))) return rc;
+    }
     ctx->persist_ok = false;
-    if ((ctx->model == RFAST_MODEL_LEAST_SQUARES || ctx->model == RFAST_MODEL_SOFTMAX) &&
+    // (a span of rounds in one kernel has the plain descent built in)
+    if (ctx->descent == RFAST_DESCENT_PLAIN && (ctx->model == RFAST_MODEL_LEAST_SQUARES || ctx->model == RFAST_MODEL_SOFTMAX) &&
         (size_t)ctx->n * ctx->stride * sizeof(float) <= ((size_t)8 << 20) && persist_smem(ctx) <= 200 * 1024) {
         int dev = 0, coop = 0, sms = 0, occ = 0;
         cudaGetDevice(&dev);
@@ -817,7 +879,7 @@ int rfast_load_schedule(rfast_ctx* ctx, const rfast_schedule* s) try {
     const bool one_pass = ctx->model == RFAST_MODEL_LOGISTIC_SPARSE && ctx->opt_fused && ctx->fused_cluster > 0;
     std::vector<int> holds;
     if (ctx->opt_open_end && s && s->K >= 0) holds.push_back(s->K);
-    int rc = compile_schedule(ctx->R, ctx->Cg, s, ctx->batch, ctx->rows, traffic_of(ctx->model, ctx->compensated, one_pass), ctx->buckets, comp, err, &holds);
+    int rc = compile_schedule(ctx->R, ctx->Cg, s, ctx->batch, ctx->rows, traffic_of(ctx->model, ctx->compensated, one_pass, ctx->descent), ctx->buckets, comp, err, &holds);
     if (rc != RFAST_OK) return set_err(ctx, rc, err);
     ctx->holds = holds;
     ctx->raw.reset();
@@ -844,7 +906,7 @@ int rfast_append_schedule(rfast_ctx* ctx, const rfast_schedule* more) try {
     Compiled comp;
     std::string err;
     const bool one_pass = ctx->model == RFAST_MODEL_LOGISTIC_SPARSE && ctx->opt_fused && ctx->fused_cluster > 0;
-    int rc = compile_schedule(ctx->R, ctx->Cg, &all, ctx->batch, ctx->rows, traffic_of(ctx->model, ctx->compensated, one_pass), ctx->buckets, comp, err, &holds);
+    int rc = compile_schedule(ctx->R, ctx->Cg, &all, ctx->batch, ctx->rows, traffic_of(ctx->model, ctx->compensated, one_pass, ctx->descent), ctx->buckets, comp, err, &holds);
     if (rc != RFAST_OK) return set_err(ctx, rc, err);
     // nothing of the rounds already loaded may have moved: same rows, same descriptors
     if (!prefix_same(ctx->comp, comp))
@@ -883,6 +945,17 @@ static int issue_rounds(rfast_ctx* ctx, int r0, int r1) {
         if (nev == 0) continue;
         a.ev = ctx->d_ev + c.act_ptr[r];
         if (!ctx->alpha_round.empty()) a.alpha = ctx->alpha_round[r];
+        if (ctx->descent != RFAST_DESCENT_PLAIN) {
+            // S1 in a pass of its own: x becomes v, and the kernels below mix what they take for x - 0 z
+            const float lr = ctx->alpha_round.empty() ? ctx->alpha : ctx->alpha_round[r];
+            AdamRows w{};
+            w.ev = a.ev; w.x = ctx->x; w.z = ctx->z; w.m = ctx->adam_m; w.v = ctx->adam_v; w.m_scale = ctx->adam_ms; w.v_scale = ctx->adam_vs;
+            w.p = ctx->p; w.stride = ctx->stride; w.scale_stride = ctx->adam_blocks(); w.factor = ctx->d_adam_factor; w.lr = lr;
+            CK(adamw_rows_launch(w, adamw_coef(lr, ctx->beta1, ctx->beta2, ctx->adam_eps, ctx->weight_decay, 1),
+                                 ctx->descent == RFAST_DESCENT_ADAMW8 ? 8 : 32, nev, ctx->stream));
+            ctx->launches += 1;
+            a.alpha = 0.f;
+        }
         if (ctx->model == RFAST_MODEL_QUAD_DIAG) {
             if (ctx->compensated) k_fused_quad<1, true><<<tile_grid(a.n4, 1, nev), kThreads, 0, ctx->stream>>>(a, ctx->quad_d, ctx->quad_b);
             else k_fused_quad<1, false><<<tile_grid(a.n4, 1, nev), kThreads, 0, ctx->stream>>>(a, ctx->quad_d, ctx->quad_b);
@@ -967,7 +1040,8 @@ int rfast_run(rfast_ctx* ctx, int32_t rounds, int sync) {
         for (auto& gc : ctx->graph_chunks) cudaGraphExecDestroy(gc.exec);
         ctx->graph_chunks.clear();
         ctx->graph_r0 = ctx->graph_r1 = -1;
-        const int per_round = ctx->model == RFAST_MODEL_QUAD_DIAG ? 1 : ctx->model == RFAST_MODEL_MLP ? 6 : 4;
+        const int per_round = (ctx->model == RFAST_MODEL_QUAD_DIAG ? 1 : ctx->model == RFAST_MODEL_MLP ? ctx->norm_groups > 0 ? 11 : 6 : 4) +
+                              (ctx->descent != RFAST_DESCENT_PLAIN ? 1 : 0);
         const int chunk_rounds = (int)std::max<int64_t>(2, kChunkLaunches / per_round);
         for (int ra = r0; ra < r1; ra += chunk_rounds) {
             const int rb = std::min(r1, ra + chunk_rounds);
@@ -1247,7 +1321,9 @@ int rfast_read_state(rfast_ctx* ctx, int which, void* dst, size_t bytes) try {
         if (bytes != idx.size() * (size_t)ctx->p * sizeof(float)) return set_err(ctx, RFAST_EINVAL, "read_state: size mismatch");
         return rows_by_index(ctx, pool, idx, dst, false);
     };
-    const bool is_float = which <= RFAST_STATE_RHO_BUF || which == RFAST_STATE_V_LATEST;
+    const bool moment = which == RFAST_STATE_ADAM_M || which == RFAST_STATE_ADAM_V;
+    if (moment && ctx->descent == RFAST_DESCENT_PLAIN) return set_err(ctx, RFAST_ESTATE, "read_state: the plain descent keeps no moments");
+    const bool is_float = which <= RFAST_STATE_RHO_BUF || which == RFAST_STATE_V_LATEST || moment;
     if (is_float) {
         int rc = check_device_status(ctx);
         if (rc != RFAST_OK) return rc;
@@ -1256,6 +1332,31 @@ int rfast_read_state(rfast_ctx* ctx, int which, void* dst, size_t bytes) try {
         case RFAST_STATE_X: return rows_out(ctx->x, n);
         case RFAST_STATE_Y: return rows_out(ctx->z, n);
         case RFAST_STATE_ROUND: return ints(&ctx->round, 1);
+        case RFAST_STATE_ADAM_M:
+        case RFAST_STATE_ADAM_V: {
+            const bool first = which == RFAST_STATE_ADAM_M;
+            const void* src = first ? ctx->adam_m : ctx->adam_v;
+            if (ctx->descent == RFAST_DESCENT_ADAMW) return rows_out((const float*)src, n);
+            if (bytes != (size_t)n * ctx->p * sizeof(float)) return set_err(ctx, RFAST_EINVAL, "read_state: size mismatch");
+            // e4m3 codes and a scale per block; the second moment's codes are those of its root
+            std::vector<uint8_t> code((size_t)n * ctx->stride);
+            std::vector<float> scale((size_t)n * ctx->adam_blocks());
+            CK(cudaMemcpyAsync(code.data(), src, code.size(), cudaMemcpyDeviceToHost, ctx->stream));
+            CK(cudaMemcpyAsync(scale.data(), first ? ctx->adam_ms : ctx->adam_vs, scale.size() * sizeof(float), cudaMemcpyDeviceToHost, ctx->stream));
+            CK(cudaStreamSynchronize(ctx->stream));
+            float value[256];
+            for (int k = 0; k < 256; ++k) {
+                const int e = (k >> 3) & 15, f = k & 7;
+                const float mag = e == 15 && f == 7 ? std::nanf("") : e == 0 ? std::ldexp((float)f, -9) : std::ldexp((float)(8 + f), e - 10);
+                value[k] = k & 128 ? -mag : mag;
+            }
+            for (int i = 0; i < n; ++i)
+                for (int64_t c = 0; c < ctx->p; ++c) {
+                    const float q = value[code[(size_t)i * ctx->stride + c]] * scale[(size_t)i * ctx->adam_blocks() + c / kAdamBlock];
+                    ((float*)dst)[(size_t)i * ctx->p + c] = first ? q : q * q;
+                }
+            return RFAST_OK;
+        }
         default: break;
     }
     if (!ctx->has_sched) return set_err(ctx, RFAST_ESTATE, "no schedule loaded");
@@ -1330,6 +1431,14 @@ int rfast_write_state(rfast_ctx* ctx, int which, const void* src, size_t bytes) 
             if (ctx->zc) CK(cudaMemsetAsync(ctx->zc, 0, (size_t)n * ctx->stride * sizeof(float), ctx->stream));
             CK(cudaStreamSynchronize(ctx->stream));
             return RFAST_OK;
+        case RFAST_STATE_ADAM_M:
+        case RFAST_STATE_ADAM_V:
+            if (ctx->descent != RFAST_DESCENT_ADAMW)
+                return set_err(ctx, RFAST_ESTATE, ctx->descent == RFAST_DESCENT_PLAIN ? "write_state: the plain descent keeps no moments"
+                                                                                      : "write_state: 8-bit moments are carried by checkpoints only");
+            if ((rc = rows_in((float*)(which == RFAST_STATE_ADAM_M ? ctx->adam_m : ctx->adam_v))) != RFAST_OK) return rc;
+            CK(cudaStreamSynchronize(ctx->stream));
+            return RFAST_OK;
         default: break;
     }
     if (!ctx->has_sched) return set_err(ctx, RFAST_ESTATE, "no schedule loaded");
@@ -1370,7 +1479,7 @@ static int compile_host_impl(const rfast_problem* prob, const rfast_schedule* s,
     if ((rc = build_host_graph(prob->G_C, prob->n, false, C, err)) != RFAST_OK) return done(rc);
     if ((rc = check_roots(R, C, prob->root, err)) != RFAST_OK) return done(rc);
     Compiled c;
-    if ((rc = compile_schedule(R, C, s, prob->batch, prob->rows, traffic_of(prob->model, prob->compensated != 0),
+    if ((rc = compile_schedule(R, C, s, prob->batch, prob->rows, traffic_of(prob->model, prob->compensated != 0, false, prob->descent),
                                prob->tracker == RFAST_TRACKER_BUCKETS, c, err)) != RFAST_OK) return done(rc);
     if (used_tau_v) std::copy(c.used_tau_v.begin(), c.used_tau_v.end(), used_tau_v);
     if (used_tau_rho) std::copy(c.used_tau_rho.begin(), c.used_tau_rho.end(), used_tau_rho);
@@ -1421,7 +1530,7 @@ int rfast_compile_append_check(const rfast_problem* prob, const rfast_schedule* 
     if ((rc = build_host_graph(prob->G_R, prob->n, true, R, err)) != RFAST_OK) return done(rc);
     if ((rc = build_host_graph(prob->G_C, prob->n, false, C, err)) != RFAST_OK) return done(rc);
     if ((rc = check_roots(R, C, prob->root, err)) != RFAST_OK) return done(rc);
-    const ModelTraffic mt = traffic_of(prob->model, prob->compensated != 0);
+    const ModelTraffic mt = traffic_of(prob->model, prob->compensated != 0, false, prob->descent);
     const bool buckets = prob->tracker == RFAST_TRACKER_BUCKETS;
     Compiled c1, c2, whole;
     std::vector<int> holds;
@@ -1474,6 +1583,14 @@ std::vector<std::pair<void*, size_t>> state_buffers(rfast_ctx* c) {
     if (c->zc) v.push_back({c->zc, plane});
     if (c->gbuf) v.push_back({c->gbuf, 2 * plane});
     if (c->xb) v.push_back({c->xb, plane / 2});
+    if (c->adam_m) {
+        v.push_back({c->adam_m, c->adam_bytes()});
+        v.push_back({c->adam_v, c->adam_bytes()});
+    }
+    if (c->adam_ms) {
+        v.push_back({c->adam_ms, c->adam_scale_bytes()});
+        v.push_back({c->adam_vs, c->adam_scale_bytes()});
+    }
     v.push_back({c->vbuf, (size_t)c->comp.n_v_slots * c->stride * sizeof(float)});
     v.push_back({c->rbuf, (size_t)c->comp.n_rho_slots * c->stride * sizeof(float) * (c->rho2 ? 2 : 1)});
     return v;
@@ -1485,7 +1602,7 @@ CkptHeader make_header(rfast_ctx* c) {
     h.p = c->p; h.stride = c->stride; h.n_events = c->comp.n_events;
     h.n = c->n; h.model = c->model; h.compensated = c->compensated + (c->rho2 ? 1 : 0); h.K = c->comp.K;
     h.n_v_slots = c->comp.n_v_slots; h.n_rho_slots = c->comp.n_rho_slots; h.round = c->round;
-    h.pad = c->buckets ? 1 : 0;
+    h.pad = (c->buckets ? 1 : 0) | c->descent << 1 | c->norm_groups << 3;
     return h;
 }
 
@@ -1670,7 +1787,7 @@ int rfast_diagnostics(rfast_ctx* ctx, double* out, int32_t n_out) try {
             k_diag_loss_softmax<<<grid, 256, 0, ctx->stream>>>(ctx->feat, ctx->label, ctx->d_xbar, ctx->d_diag_rowloss, ctx->rows, ctx->F, ctx->C);
         else if (ctx->model == RFAST_MODEL_MLP)
             k_diag_loss_mlp<<<grid, 256, 8 * (size_t)ctx->H * sizeof(double), ctx->stream>>>(ctx->feat, ctx->label, ctx->d_xbar, ctx->d_diag_rowloss,
-                                                                                             ctx->rows, ctx->F, ctx->H, ctx->C);
+                                                                                             ctx->rows, ctx->F, ctx->H, ctx->C, ctx->norm_groups, ctx->norm_act, ctx->norm_eps);
         else
             k_diag_loss_logistic<<<grid, 256, 0, ctx->stream>>>(ctx->sp_ptr, ctx->sp_col, ctx->sp_val, ctx->label, ctx->d_xbar, ctx->d_diag_rowloss, ctx->rows);
         CK(cudaGetLastError());

@@ -13,6 +13,11 @@
 // in fp32 on the CUDA cores: the logits as per-slab shares in the forward kernel's epilogue,
 // while h is still in shared memory, the rest in the backward kernel.
 //
+// With a group norm in the hidden layer, h = act(gamma (pre - mean) rstd + beta), the statistics of a row need all
+// its hidden units, which the slabs share out: the forward kernel then leaves pre, the group norm operator makes h of it
+// in a pass of its own, the logits follow from h, the backward kernel leaves dh, and the operator's backward pass
+// gives dpre, dgamma and dbeta.
+//
 // Every wait on an mbarrier is bounded: when it runs out the CTA records a code in a status
 // word, leaves its loops, frees its tensor memory and returns.
 #include <cuda.h>
@@ -22,6 +27,7 @@
 #include <cstdio>
 #include <string>
 
+#include "ops.h"
 #include "rfast_internal.h"
 
 namespace rfast {
@@ -164,6 +170,13 @@ struct MlpPlan {
     __nv_bfloat16 *featb = nullptr, *Ab = nullptr, *AbT = nullptr, *dpqT = nullptr;
     float* hf = nullptr;               // [ev][B][H] hidden activations
     float* share = nullptr;            // [ev][H / 128][B][16] logit shares of the slabs, zero beyond C
+    // group norm in the hidden layer (norm_groups > 0): hf then holds pre
+    int norm_groups = 0, norm_act = 0;
+    float norm_eps = 0;
+    float *hn = nullptr, *dh = nullptr;            // [ev][B][H] the layer's output; its gradient, then pre's
+    float *mean = nullptr, *rstd = nullptr;        // [ev][B][groups]
+    float* daff = nullptr;                         // [2][ev][H] dgamma, dbeta
+    void* norm_work = nullptr;
     int* status = nullptr;
     CUtensorMap tmW1, tmA, tmD, tmAT, tmX, tmG;
 };
@@ -226,8 +239,9 @@ k_mlp_gather(const EvDesc* __restrict__ evs, const int* __restrict__ batch_idx,
 // h[k][j] W2[c][j]: h is still on chip when the product ends (it is staged in the operand
 // stages, which are free by then), so the output layer costs no second pass over h.  The shares
 // of the H / 128 slabs are added, in slab order, by the backward kernel.
+// NORM: hf gets pre itself and there are no shares.
 // grid = (H / 128, events), 320 threads; dynamic shared memory kFwdSmem
-template <int CQ>
+template <int CQ, bool NORM>
 __global__ void __launch_bounds__(kFwdThreads, 2)
 k_mlp_fwd(const __grid_constant__ CUtensorMap tmW1, const __grid_constant__ CUtensorMap tmA,
           const EvDesc* __restrict__ evs, const float* __restrict__ x, int64_t stride,
@@ -299,7 +313,7 @@ k_mlp_fwd(const __grid_constant__ CUtensorMap tmW1, const __grid_constant__ CUte
         else { atomicExch(status, kErrMma); bad = 1; __threadfence_block(); mbar_arrive(&acc_full); }
     } else if (warp >= 2) {                                // ---- epilogue: TMEM -> relu -> hf and shared memory
         // while the product runs: the W2 columns of the slab (rows C .. CP-1 zero) and the bias
-        for (int o = wt; o < CP * kMTile; o += kFwdWorkers) {
+        for (int o = wt; !NORM && o < CP * kMTile; o += kFwdWorkers) {
             const int c = o >> 7, j = o & (kMTile - 1);
             w2s[c * kHsPitch + j] = c < C ? x[row + oW2 + (int64_t)c * H + h0 + j] : 0.f;
         }
@@ -318,16 +332,16 @@ k_mlp_fwd(const __grid_constant__ CUtensorMap tmW1, const __grid_constant__ CUte
                 tmem_ld16(tacc + ((uint32_t)(q * 32) << 16) + colh * 32 + c0, v);
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const float hval = fmaxf(v[i] + b1, 0.f);
+                    const float hval = NORM ? v[i] + b1 : fmaxf(v[i] + b1, 0.f);
                     out[(int64_t)(colh * 32 + c0 + i) * H] = hval;
-                    hs[(colh * 32 + c0 + i) * kHsPitch + jl] = hval;
+                    if (!NORM) hs[(colh * 32 + c0 + i) * kHsPitch + jl] = hval;
                 }
             }
         }
     }
     tc_fence_before();
     __syncthreads();                                       // h and the W2 columns are in shared memory
-    if (warp >= 2 && bad == 0) {                           // ---- the slab's share of the logits
+    if (!NORM && warp >= 2 && bad == 0) {                  // ---- the slab's share of the logits
         // Register tile of 4 rows x CQ classes per thread over a quarter of the hidden units: every
         // value read from shared memory feeds 4 (W2) or CQ (h) products, a third of the reads of
         // one row per thread.  Lane bits: jq = quarter of the units (interleaved: float4 4t + jq),
@@ -381,12 +395,13 @@ k_mlp_fwd(const __grid_constant__ CUtensorMap tmW1, const __grid_constant__ CUte
 // gb1, dpre and its bf16 transpose for the second big product; the first slab also sums gb2.
 // A thread owns one hidden unit and a quarter of the batch; the four partial sums are added in
 // a fixed order.  CQ = ceil(C / 4): the class dimension is processed in quads, zero beyond C.
+// NORM: dh goes to dhout [ev][B][H] as it is; gb1 and the transpose follow from dpre later (k_mlp_norm_out).
 // grid = (H / 64, events), 256 threads
-template <int CQ>
+template <int CQ, bool NORM>
 __global__ void __launch_bounds__(256)
 k_mlp_back(const EvDesc* __restrict__ evs, const int* __restrict__ batch_idx, const int* __restrict__ label,
            const float* __restrict__ x, int64_t stride, const float* __restrict__ hf,
-           const float* __restrict__ share, int R, __nv_bfloat16* __restrict__ dpqT,
+           const float* __restrict__ share, int R, __nv_bfloat16* __restrict__ dpqT, float* __restrict__ dhout,
            float* __restrict__ gbuf, int64_t gplane, int rows, int F, int H, int C, float l2) {
     constexpr int CP = CQ * 4, kSlab = 64, kQuarter = kBatch / 4;
     __shared__ float4 dl[kBatch][4];                       // [B][16]
@@ -465,6 +480,7 @@ k_mlp_back(const EvDesc* __restrict__ evs, const int* __restrict__ batch_idx, co
             float dh = 0.f;
 #pragma unroll
             for (int c = 0; c < CP; ++c) dh = fmaf(d[c], w2[c], dh);
+            if (NORM) dhout[((int64_t)ev * kBatch + k) * H + j] = dh;
             const float dp = hv[k0 + kk] > 0.f ? dh : 0.f;
             gb1 += dp;
             const uint32_t b = (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(dp));
@@ -472,19 +488,77 @@ k_mlp_back(const EvDesc* __restrict__ evs, const int* __restrict__ batch_idx, co
 #pragma unroll
             for (int c = 0; c < CP; ++c) gw2[c] = fmaf(d[c], hv[k0 + kk], gw2[c]);
         }
-        *reinterpret_cast<uint4*>(drow + k0) = make_uint4(pk[0], pk[1], pk[2], pk[3]);
+        if (!NORM) *reinterpret_cast<uint4*>(drow + k0) = make_uint4(pk[0], pk[1], pk[2], pk[3]);
     }
 #pragma unroll
     for (int c = 0; c < CP; ++c) part[kq][jl][c] = gw2[c];
     part[kq][jl][CP] = gb1;
     __syncthreads();
     // (C + 1) x 64 outputs, consecutive threads on consecutive hidden units
-    for (int o = threadIdx.x; o < (C + 1) * kSlab; o += 256) {
+    for (int o = threadIdx.x; o < (NORM ? C : C + 1) * kSlab; o += 256) {
         const int c = o >> 6, jj = o & (kSlab - 1);        // c == C: gb1
         const int pc = c < C ? c : CP;
         const float tot = ((part[0][jj][pc] + part[1][jj][pc]) + part[2][jj][pc]) + part[3][jj][pc];
         const int64_t at = c < C ? oW2 + (int64_t)c * H + blockIdx.x * kSlab + jj : (int64_t)H * F + blockIdx.x * kSlab + jj;
         g[at] = l2 != 0.f ? tot + l2 * x[row + at] : tot;
+    }
+}
+
+// The logits of a normalised hidden layer, one warp per sampled row, laid out as a single slab's shares.  The 20 KB of W2 come
+// out of L1 and L2; the rows of h are read once.  grid = (B / 8, events), 256 threads
+template <int CQ>
+__global__ void __launch_bounds__(256)
+k_mlp_logits(const EvDesc* __restrict__ evs, const float* __restrict__ x, int64_t stride, const float* __restrict__ hn,
+             float* __restrict__ share, int F, int H, int C) {
+    constexpr int CP = CQ * 4;
+    const int ev = blockIdx.y, k = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    const float* W2 = x + (int64_t)evs[ev].node * stride + (int64_t)H * F + H;
+    const float* h = hn + ((int64_t)ev * kBatch + k) * H;
+    float acc[CP];
+#pragma unroll
+    for (int c = 0; c < CP; ++c) acc[c] = 0.f;
+    for (int j = lane; j < H; j += 32) {
+        const float hv = h[j];
+#pragma unroll
+        for (int c = 0; c < CP; ++c) if (c < C) acc[c] = fmaf(hv, W2[(int64_t)c * H + j], acc[c]);
+    }
+    float mine = 0.f;                                      // lane c keeps class c
+#pragma unroll
+    for (int c = 0; c < CP; ++c) {
+        const float v = warp_sum(acc[c]);
+        if (lane == c) mine = v;
+    }
+    if (lane < 16) share[((int64_t)ev * kBatch + k) * 16 + lane] = mine;
+}
+
+// What the group norm's backward pass leaves goes where the gradient and the second big product want it: dpre [ev][B][H]
+// transposed to bf16, its sum over the batch (gb1, rows in ascending order), dgamma and dbeta.
+// grid = (H / 64, events), 256 threads
+__global__ void __launch_bounds__(256)
+k_mlp_norm_out(const EvDesc* __restrict__ evs, const float* __restrict__ x, int64_t stride, const float* __restrict__ dpre,
+               const float* __restrict__ dgamma, const float* __restrict__ dbeta, __nv_bfloat16* __restrict__ dpqT,
+               float* __restrict__ gbuf, int64_t gplane, int F, int H, int C, float l2) {
+    __shared__ float tile[kBatch][kBatch + 1];             // [row][hidden unit of the slab]
+    const int ev = blockIdx.y, j0 = blockIdx.x * 64;
+    const EvDesc e = evs[ev];
+    const int64_t row = (int64_t)e.node * stride;
+    float* g = gbuf + (int64_t)(e.g_par ^ 1) * gplane + row;
+    const float* d = dpre + (int64_t)ev * kBatch * H + j0;
+    for (int o = threadIdx.x; o < kBatch * 64; o += 256) tile[o >> 6][o & 63] = d[(int64_t)(o >> 6) * H + (o & 63)];
+    __syncthreads();
+    for (int o = threadIdx.x; o < 64 * (kBatch / 2); o += 256) {           // pairs of rows, side by side in the transpose
+        const int j = o >> 5, k = (o & 31) * 2;
+        const __nv_bfloat162 v = __floats2bfloat162_rn(tile[k][j], tile[k + 1][j]);
+        reinterpret_cast<__nv_bfloat162*>(dpqT + ((int64_t)ev * H + j0 + j) * kBatch)[k / 2] = v;
+    }
+    if (threadIdx.x < 192) {
+        const int j = threadIdx.x & 63, what = threadIdx.x >> 6;            // gb1, dgamma, dbeta
+        const int64_t oN = (int64_t)H * F + H + (int64_t)C * H + C;
+        float v = 0.f;
+        if (what == 0) for (int k = 0; k < kBatch; ++k) v += tile[k][j];
+        else v = (what == 1 ? dgamma : dbeta)[(int64_t)ev * H + j0 + j];
+        const int64_t at = (what == 0 ? (int64_t)H * F : oN + (int64_t)(what - 1) * H) + j0 + j;
+        g[at] = l2 != 0.f ? v + l2 * x[row + at] : v;
     }
 }
 
@@ -650,7 +724,7 @@ constexpr size_t kDw1Smem = 2 * (size_t)kMTile * kKBlock * 2 + 4 * 2 * (32 * 16 
 
 }  // namespace
 
-int mlp_plan_create(int n, int rows, int F, int H, int C, int B, int64_t stride, int max_events,
+int mlp_plan_create(int n, int rows, int F, int H, int C, int B, int norm_groups, int norm_act, float norm_eps, int64_t stride, int max_events,
                     const float* d_feat, const __nv_bfloat16* xb, const float* x, float* gbuf, cudaStream_t st,
                     MlpPlan** out, size_t* dev_bytes, std::string& err) {
     *out = nullptr;
@@ -677,6 +751,16 @@ int mlp_plan_create(int n, int rows, int F, int H, int C, int B, int64_t stride,
               cudaMalloc((void**)&p->hf, (size_t)max_events * kBatch * H * sizeof(float)) == cudaSuccess &&
               cudaMalloc((void**)&p->share, (size_t)max_events * (H / kMTile) * kBatch * 16 * sizeof(float)) == cudaSuccess &&
               cudaMalloc((void**)&p->status, sizeof(int)) == cudaSuccess;
+    size_t norm_bytes = 0;
+    if (ok && norm_groups > 0) {
+        p->norm_groups = norm_groups; p->norm_act = norm_act; p->norm_eps = norm_eps;
+        const size_t act = (size_t)max_events * kBatch * H * sizeof(float), stats = (size_t)max_events * kBatch * norm_groups * sizeof(float);
+        const size_t aff = (size_t)2 * max_events * H * sizeof(float), work = norm_rows_workspace(max_events, kBatch, H);
+        ok = cudaMalloc((void**)&p->hn, act) == cudaSuccess && cudaMalloc((void**)&p->dh, act) == cudaSuccess &&
+             cudaMalloc((void**)&p->mean, stats) == cudaSuccess && cudaMalloc((void**)&p->rstd, stats) == cudaSuccess &&
+             cudaMalloc((void**)&p->daff, aff) == cudaSuccess && cudaMalloc(&p->norm_work, work) == cudaSuccess;
+        norm_bytes = 2 * act + 2 * stats + aff + work;
+    }
     if (!ok) { mlp_plan_destroy(p); err = "MLP: device allocation failed"; return RFAST_ENOMEM; }
     cudaMemsetAsync(p->status, 0, sizeof(int), st);
     k_to_bf16<<<(unsigned)((nfeat + 255) / 256), 256, 0, st>>>(d_feat, p->featb, (int64_t)nfeat);
@@ -704,24 +788,25 @@ int mlp_plan_create(int n, int rows, int F, int H, int C, int B, int64_t stride,
             return RFAST_ECUDA;
         }
     }
-    if (cudaFuncSetAttribute(k_mlp_fwd<1>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kFwdSmem) != cudaSuccess ||
-        cudaFuncSetAttribute(k_mlp_fwd<2>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kFwdSmem) != cudaSuccess ||
-        cudaFuncSetAttribute(k_mlp_fwd<3>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kFwdSmem) != cudaSuccess ||
-        cudaFuncSetAttribute(k_mlp_fwd<4>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kFwdSmem) != cudaSuccess ||
+    const void* fwd[] = {(const void*)k_mlp_fwd<1, false>, (const void*)k_mlp_fwd<2, false>, (const void*)k_mlp_fwd<3, false>,
+                         (const void*)k_mlp_fwd<4, false>, (const void*)k_mlp_fwd<1, true>};
+    bool room = true;
+    for (const void* f : fwd) room = room && cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kFwdSmem) == cudaSuccess;
+    if (!room ||
         cudaFuncSetAttribute(k_mlp_dw1, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kDw1Smem) != cudaSuccess) {
         mlp_plan_destroy(p);
         err = "MLP: cannot reserve shared memory";
         return RFAST_ECUDA;
     }
     *out = p;
-    *dev_bytes = total + sizeof(int) + (size_t)max_events * kBatch * H * sizeof(float) +
+    *dev_bytes = total + norm_bytes + sizeof(int) + (size_t)max_events * kBatch * H * sizeof(float) +
                  (size_t)max_events * (H / kMTile) * kBatch * 16 * sizeof(float);
     return RFAST_OK;
 }
 
 void mlp_plan_destroy(MlpPlan* p) {
     if (!p) return;
-    void* ptrs[] = {p->featb, p->Ab, p->AbT, p->hf, p->share, p->dpqT, p->status};
+    void* ptrs[] = {p->featb, p->Ab, p->AbT, p->hf, p->share, p->dpqT, p->status, p->hn, p->dh, p->mean, p->rstd, p->daff, p->norm_work};
     for (void* q : ptrs) if (q) cudaFree(q);
     delete p;
 }
@@ -730,13 +815,39 @@ int mlp_grad_launch(MlpPlan* p, const GradArgs& g, const __nv_bfloat16* xb, cons
                     int n_events, cudaStream_t st, int64_t* launches, std::string& err) {
     if (!p || n_events > p->maxev) { err = "MLP: too many events for the plan"; return RFAST_EINVAL; }
     k_mlp_gather<<<dim3(p->Fp / kKBlock, n_events), 256, 0, st>>>(g.ev, g.batch_idx, p->featb, p->Ab, p->AbT, p->rows, p->F, p->Fp);
-    {
-        const int R = p->H / kMTile;
-        const dim3 gf(R, n_events), gb(p->H / 64, n_events);
+    const int R = p->H / kMTile;
+    const dim3 gf(R, n_events), gb(p->H / 64, n_events);
+    if (p->norm_groups > 0) {
+        k_mlp_fwd<1, true><<<gf, kFwdThreads, kFwdSmem, st>>>(p->tmW1, p->tmA, g.ev, g.x, g.stride, p->hf, p->share, p->F, p->H, p->C,
+                                                              p->Fp / kKBlock, p->status);
+        const int64_t oN = (int64_t)p->H * p->F + p->H + (int64_t)p->C * p->H + p->C;
+        NormRows nr{};
+        nr.ev = g.ev; nr.n_events = n_events; nr.batch = kBatch; nr.hidden = p->H; nr.groups = p->norm_groups; nr.act = p->norm_act;
+        nr.eps = p->norm_eps; nr.gamma = g.x + oN; nr.beta = g.x + oN + p->H; nr.stride = g.stride;
+        nr.x = p->hf; nr.out = p->hn; nr.mean = p->mean; nr.rstd = p->rstd;
+        nr.dgamma = p->daff; nr.dbeta = p->daff + (int64_t)p->maxev * p->H; nr.workspace = p->norm_work;
+        cudaError_t e = norm_rows_launch(nr, false, st, launches);
 #define RFAST_MID(CQ)                                                                                              \
-    k_mlp_fwd<CQ><<<gf, kFwdThreads, kFwdSmem, st>>>(p->tmW1, p->tmA, g.ev, g.x, g.stride, p->hf, p->share, p->F, \
+    k_mlp_logits<CQ><<<dim3(kBatch / 8, n_events), 256, 0, st>>>(g.ev, g.x, g.stride, p->hn, p->share, p->F, p->H, p->C); \
+    k_mlp_back<CQ, true><<<gb, 256, 0, st>>>(g.ev, g.batch_idx, label, g.x, g.stride, p->hn, p->share, 1, p->dpqT, p->dh, \
+                                             g.gbuf, g.gplane, p->rows, p->F, p->H, p->C, g.l2)
+        switch ((p->C + 3) / 4) {
+            case 1: RFAST_MID(1); break;
+            case 2: RFAST_MID(2); break;
+            case 3: RFAST_MID(3); break;
+            default: RFAST_MID(4); break;
+        }
+#undef RFAST_MID
+        nr.dy = p->dh; nr.out = p->dh;
+        if (e == cudaSuccess) e = norm_rows_launch(nr, true, st, launches);
+        if (e != cudaSuccess) { err = std::string("MLP: group norm: ") + cudaGetErrorString(e); return RFAST_ECUDA; }
+        k_mlp_norm_out<<<gb, 256, 0, st>>>(g.ev, g.x, g.stride, p->dh, nr.dgamma, nr.dbeta, p->dpqT, g.gbuf, g.gplane, p->F, p->H, p->C, g.l2);
+        *launches += 2;                                    // the logits and this one; the others are counted below
+    } else {
+#define RFAST_MID(CQ)                                                                                              \
+    k_mlp_fwd<CQ, false><<<gf, kFwdThreads, kFwdSmem, st>>>(p->tmW1, p->tmA, g.ev, g.x, g.stride, p->hf, p->share, p->F, \
                                                      p->H, p->C, p->Fp / kKBlock, p->status);                      \
-    k_mlp_back<CQ><<<gb, 256, 0, st>>>(g.ev, g.batch_idx, label, g.x, g.stride, p->hf, p->share, R, p->dpqT,      \
+    k_mlp_back<CQ, false><<<gb, 256, 0, st>>>(g.ev, g.batch_idx, label, g.x, g.stride, p->hf, p->share, R, p->dpqT, nullptr, \
                                        g.gbuf, g.gplane, p->rows, p->F, p->H, p->C, g.l2)
         switch ((p->C + 3) / 4) {
             case 1: RFAST_MID(1); break;

@@ -1560,6 +1560,31 @@ bool overlaps(const GnShape& s, int64_t sn, int64_t ss) {
 
 }  // namespace
 
+// Partial sums of the channels: as many rows as a set's samples at most.
+size_t norm_rows_workspace(int max_events, int batch, int hidden) { return (size_t)max_events * batch * 2 * hidden * sizeof(float); }
+
+cudaError_t norm_rows_launch(const NormRows& r, bool backward, cudaStream_t st, int64_t* launches) {
+    GnArgs a{};
+    a.s.N = (int64_t)r.n_events * r.batch; a.s.S = 1; a.s.C = r.hidden; a.s.G = r.groups; a.s.Cg = r.hidden / r.groups;
+    a.s.per_set = r.batch; a.s.eps = r.eps; a.s.act = r.act;
+    a.x = r.x; a.dy = r.dy; a.out = r.out;
+    a.xn = a.xs = a.dn = a.ds = a.on = a.os = r.hidden;
+    a.gamma = r.gamma; a.beta = r.beta; a.affine_stride = r.stride;
+    a.set_row = &r.ev->node;                                // a device address: it is not read here
+    a.set_row_stride = (int)(sizeof(EvDesc) / sizeof(int));
+    a.mean = r.mean; a.rstd = r.rstd; a.dgamma = r.dgamma; a.dbeta = r.dbeta;
+    a.p = make_plan(a.s, 4, allowed(r.x, a.xn, a.xs, 4), backward);
+    a.part = (float*)r.workspace;
+    cudaError_t e = launch_typed(a, RFAST_TYPE_F32, backward, st);
+    *launches += 1;
+    if (e == cudaSuccess && backward && a.p.parts > 1) {
+        k_gn_affine<<<dim3((r.hidden + 31) / 32, r.n_events), kT, 0, st>>>(a.part, a.p.parts, r.hidden, r.dgamma, r.dbeta);
+        e = cudaGetLastError();
+        *launches += 1;
+    }
+    return e;
+}
+
 }  // namespace rfast
 
 using namespace rfast;

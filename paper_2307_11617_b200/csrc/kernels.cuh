@@ -945,10 +945,11 @@ k_diag_loss_logistic(const int64_t* __restrict__ sp_ptr, const int* __restrict__
     if (lane == 0) rowloss[r] = m > 0 ? log1p(exp(-m)) : -m + log1p(exp(m));
 }
 //   MLP: x = [W1 (H x F) | b1 (H) | W2 (C x H) | b2 (C)]; the operands of A W1^T rounded to bf16 (the
-//   matrix product the tensor cores take), everything else as it is; dynamic shared memory: 8 * H doubles
+//   matrix product the tensor cores take), everything else as it is; dynamic shared memory: 8 * H doubles.
+//   groups > 0: x = [... | gamma (H) | beta (H)], group norm and activation in the place of relu
 __global__ void __launch_bounds__(256)
 k_diag_loss_mlp(const float* __restrict__ feat, const int* __restrict__ label, const float* __restrict__ xbar,
-                double* __restrict__ rowloss, int rows, int F, int H, int C) {
+                double* __restrict__ rowloss, int rows, int F, int H, int C, int groups, int act, double eps) {
     extern __shared__ double hs_all[];
     const int w = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int k = blockIdx.x * 8 + w;
@@ -962,7 +963,23 @@ k_diag_loss_mlp(const float* __restrict__ feat, const int* __restrict__ label, c
         for (int f = lane; f < F; f += 32)
             s += (double)__bfloat162float(__float2bfloat16_rn(W1[(int64_t)j * F + f])) * (double)__bfloat162float(__float2bfloat16_rn(a[f]));
         for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-        if (lane == 0) hs[j] = fmax(s + (double)b1[j], 0.0);
+        if (lane == 0) hs[j] = groups > 0 ? s + (double)b1[j] : fmax(s + (double)b1[j], 0.0);
+    }
+    __syncwarp();
+    const int per = groups > 0 ? H / groups : H;
+    const float *gamma = b2 + C, *beta = gamma + H;
+    for (int q = 0; q < groups; ++q) {
+        double m = 0, v = 0;
+        for (int j = lane; j < per; j += 32) m += hs[q * per + j];
+        for (int o = 16; o > 0; o >>= 1) m += __shfl_xor_sync(0xffffffffu, m, o);
+        m /= per;
+        for (int j = lane; j < per; j += 32) v += (hs[q * per + j] - m) * (hs[q * per + j] - m);
+        for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        const double rstd = 1.0 / sqrt(v / per + eps);
+        for (int j = lane; j < per; j += 32) {
+            const double u = (hs[q * per + j] - m) * rstd * (double)gamma[q * per + j] + (double)beta[q * per + j];
+            hs[q * per + j] = act == RFAST_ACT_RELU ? fmax(u, 0.0) : act == RFAST_ACT_SILU ? u / (1.0 + exp(-u)) : u;
+        }
     }
     __syncwarp();
     const int lab = label[r];

@@ -39,6 +39,23 @@ struct AdamRows {
 };
 cudaError_t adamw_rows_launch(const AdamRows& r, const AdamCoef& c, int state_bits, int n_events, cudaStream_t st);
 
+// The engine's hidden layers: rows [n_events][batch][hidden] fp32, event e with the scale and shift of its node.
+struct NormRows {
+    const EvDesc* ev;
+    int n_events, batch, hidden, groups, act;
+    float eps;
+    const float *gamma, *beta;         // of node 0; a node's are node * stride further on
+    int64_t stride;
+    const float* x;                    // before the norm
+    float* out;                        // forward: the layer's output; backward: the gradient of x
+    const float* dy;                   // backward (may be `out`)
+    float *mean, *rstd;                // [n_events * batch][groups]
+    float *dgamma, *dbeta;             // backward: [n_events][hidden]
+    void* workspace;                   // norm_rows_workspace() bytes
+};
+size_t norm_rows_workspace(int max_events, int batch, int hidden);
+cudaError_t norm_rows_launch(const NormRows& r, bool backward, cudaStream_t st, int64_t* launches);
+
 // Sets err and returns RFAST_EINVAL / RFAST_ECUDA unless `p` is memory of the current device.
 int check_device_pointer(const void* p, const char* what, char* err, size_t err_len);
 int op_fail(char* err, size_t err_len, int code, const char* fmt, ...);

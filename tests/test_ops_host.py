@@ -198,3 +198,77 @@ def test_group_norm_gradient_formula_against_differences():
                 down[k] -= h
                 # differences of step 1e-6 carry 1e-6^2 of curvature and 1e-16 / 1e-6 of rounding
                 assert abs((f(*up) - f(*down)) / 2e-6 - got[at]) < 1e-7 * (1 + abs(got[at])) * 10, (act, k, at)
+
+
+# ---- the engine's options -----------------------------------------------------------------------------
+@pytest.mark.parametrize("name,ov,text", [
+    ("quad_tree64", dict(p=16, K=2, descent={"kind": "adamw"}), "plain descent only"),
+    ("softmax_exp16", dict(n=4, F=8, C=3, rows=8, K=2, batch=2, descent={"kind": "adamw", "beta1": 1.0}), "beta1 and beta2"),
+    ("softmax_exp16", dict(n=4, F=8, C=3, rows=8, K=2, batch=2, descent={"kind": "adamw8", "eps": 0.0}), "adam_eps"),
+    ("softmax_exp16", dict(n=4, F=8, C=3, rows=8, K=2, batch=2, descent={"kind": "adamw8", "weight_decay": float("inf")}), "weight_decay"),
+    ("mlp_tree64", dict(n=3, F=16, H=128, C=3, rows=64, K=2, batch=64, norm_groups=3), "divide n_hidden"),
+])
+def test_engine_refuses_options(rfast_lib, name, ov, text):
+    import paper_2307_11617_b200 as pkg
+    from paper_2307_11617_b200.binding import EINVAL
+    from workloads import build_config
+    wl = build_config(name, seed=0, **ov)
+    with pytest.raises(pkg.RFastError) as ei:
+        pkg.Engine(wl)
+    assert ei.value.code == EINVAL and text in str(ei.value)
+
+
+def test_only_the_mlp_has_a_norm(rfast_lib):
+    import paper_2307_11617_b200 as pkg
+    from workloads import build_config
+    wl = build_config("softmax_exp16", seed=0, n=4, F=8, C=3, rows=8, K=2, batch=2)
+    wl.dims["norm_groups"] = 1
+    with pytest.raises(pkg.RFastError) as ei:
+        pkg.Engine(wl)
+    assert "hidden layer" in str(ei.value)
+
+
+@pytest.mark.parametrize("act", ["none", "relu", "silu"])
+@pytest.mark.parametrize("groups", [1, 3, 6])
+def test_oracle_normalised_mlp_gradient_against_differences(groups, act):
+    from oracle.models import MLP
+    rng = np.random.default_rng(groups)
+    F, H, C = 4, 6, 3
+    feat, lab = rng.standard_normal((1, 5, F)), rng.integers(0, C, (1, 5))
+    m = MLP(feat, lab, H, C, l2=0.1, round_inputs=False, norm_groups=groups, norm_act=act, norm_eps=1e-3)
+    x = rng.standard_normal(H * F + H + C * H + C + 2 * H)
+    idx = np.arange(5)
+    g = m.grad(0, x, idx)
+    for k in range(len(x)):
+        e = np.zeros_like(x)
+        e[k] = 1e-6
+        diff = (m.loss(0, x + e, idx) - m.loss(0, x - e, idx)) / 2e-6
+        # curvature 1e-12 and rounding 1e-16 / 1e-6, the loss's third derivative up to 1e3
+        assert abs(diff - g[k]) <= 1e-7 * (1 + abs(g[k])), k
+
+
+def test_oracle_adamw_step_is_the_definition():
+    """Two steps of one worker without neighbours, moments in 64 and in 8 bits, written out."""
+    from oracle.rfast_oracle import RFastOracle, _held8
+    from workloads import graph_from_edges
+    rng = np.random.default_rng(1)
+    p, lr = 700, 0.01
+    for kind in ("adamw", "adamw8"):
+        d = {"kind": kind, "beta1": 0.8, "beta2": 0.95, "eps": 1e-6, "weight_decay": 0.1}
+        orc = RFastOracle(1, p, lr, graph_from_edges(1, [], "row"), graph_from_edges(1, [], "col"), lambda i, x, idx: 3.0 * x, np.ones((1, p)), descent=d)
+        orc.init_gradients()
+        z = rng.standard_normal(p)
+        orc.z[0] = z.copy()
+        m, s, x = np.zeros(p), np.zeros(p), np.ones(p)
+        for t in (1, 2):
+            zt = orc.z[0].copy()
+            m, s = 0.8 * m + 0.2 * zt, 0.95 * s + 0.05 * zt * zt
+            x = x - lr * 0.1 * x - lr * (m / (1 - 0.8 ** t)) / (np.sqrt(s / (1 - 0.95 ** t)) + 1e-6)
+            orc.activate(0, t - 1, [], [], None)
+            assert np.allclose(orc.x[0], x, rtol=1e-12)
+            if kind == "adamw8":
+                mq, sq = _held8(m, 0.0), _held8(np.sqrt(s), 2.0 ** -9) ** 2
+                assert np.all(np.abs(mq - m) <= 2.0 ** -4 * np.maximum(np.abs(m), np.abs(mq)) + np.abs(m).max() * 2.0 ** -10 / 448)
+                m, s = mq, sq
+            assert np.allclose(orc.m[0], m, rtol=1e-12) and np.allclose(orc.s[0], s, rtol=1e-12)      # roundings of 64 bits
+            m, s = orc.m[0], orc.s[0]

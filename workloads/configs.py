@@ -52,6 +52,8 @@ class Workload:
                                     # tracker, 2 two-float tracker and running sums
     tracker: int = 0                # how the engine keeps the mass on the G_C edges: 0 running sums
                                     # (Algorithm 1 as printed), 1 one row per consumption ("buckets")
+    descent: dict | None = None     # the local step S1: None plain, {"kind": "adamw" or "adamw8", "beta1", "beta2", "eps",
+                                    # "weight_decay"} an AdamW step with the tracker as its gradient
 
     def __post_init__(self):
         # scalars are handed to every consumer as the fp32-representable value
@@ -84,11 +86,12 @@ def _gaussian_mixture(n, rows, F, C, classes_per_node, rng, scale):
 
 def build_config(name: str, seed: int = 0, **ov) -> Workload:
     """ov overrides: n, p, rows, K, F (features), H (hidden), C (classes), batch, drop,
-    max_delay, alpha, nnz (per sparse row), compensated, tracker."""
+    max_delay, alpha, nnz (per sparse row), compensated, tracker, descent; MLP: norm_groups, norm_act."""
     builders = {"ls_ring4": _ls_ring, "softmax_exp16": _softmax_exp, "mlp_tree64": _mlp_tree,
                 "quad_tree64": _quad_tree, "logistic_tree1024": _logistic_tree}
     wl = builders[name](seed, ov)
     wl.tracker = int(ov.get("tracker", 0))
+    wl.descent = ov.get("descent")
     return wl
 
 
@@ -148,12 +151,17 @@ def _mlp_tree(seed, ov):
     w1 = (rd.standard_normal(H * F) * np.sqrt(2.0 / F)).astype(np.float32)
     w2 = (rd.standard_normal(C * H) * np.sqrt(2.0 / H)).astype(np.float32)
     x_init = np.concatenate([w1, np.zeros(H, np.float32), w2, np.zeros(C, np.float32)])
+    dims = {"n_features": F, "n_hidden": H, "n_classes": C}
+    if ov.get("norm_groups", 0):                        # group norm in the hidden layer: its scale and shift at the end of x
+        x_init = np.concatenate([x_init, np.ones(H, np.float32), np.zeros(H, np.float32)])
+        p += 2 * H
+        dims.update(norm_groups=ov["norm_groups"], norm_act=ov.get("norm_act", "relu"), norm_eps=1e-5)
     x0 = np.broadcast_to(x_init, (n, p)).copy()
     act = activation_durations(
         n, K, lambda i, t: max(1, int(np.rint(np.exp(rs.standard_normal())))))
     sch = make_schedule(G_R, G_C, act, drop, max_delay, rs, batch=B, rows_per_node=rows)
     return Workload("mlp_tree64", n, p, 0, alpha, G_R, G_C, MODEL_MLP, B, l2, rows,
-                    dims={"n_features": F, "n_hidden": H, "n_classes": C},
+                    dims=dims,
                     data={"feat": feat, "label": label}, x0=x0, schedule=sch,
                     meta={"K": K, "drop": drop, "max_delay": max_delay})
 
