@@ -621,7 +621,7 @@ cudaError_t pick_param(const AdamTable<T>& a, int pt, int gt, int bits, cudaStre
 }
 
 // A table of T entries is copied into every launch; few tensors take the small one.
-constexpr int kFew = 24, kMany = 480;
+constexpr int kFew = 64, kMany = 480;
 
 // Blocks of 256 values per warp: as long as every SM gets several rounds of thread blocks, longer runs
 // pay the look-up in the table and the first, exposed fetch less often.

@@ -180,9 +180,27 @@ template <int PAIRS> struct Ring {
         for (int k = 0; k < PAIRS - 1; ++k) send(cnt, fetch);
     }
     template <class Row, class Fetch, class Held, class Use> __device__ __forceinline__ void run(int cnt, Fetch& fetch, Held held, Use use) {
-        int out = 0;
+        int out = 0, r = 0;
+        // while all that a turn of the ring fetches and uses exists, its slots are constants
+        constexpr int kTurn = 2 * PAIRS;
 #pragma unroll 1
-        for (int r = 0; r < cnt; r += 2) {
+        for (; r + kTurn + 2 * (PAIRS - 1) <= cnt; r += kTurn) {
+#pragma unroll
+            for (int p = 0; p < PAIRS; ++p) {
+                fetch((2 * p + 2 * (PAIRS - 1)) % kTurn);
+                fetch((2 * p + 2 * (PAIRS - 1) + 1) % kTurn);
+                copies_commit();
+                copies_pending<PAIRS - 1>();
+                Row q[2];
+                q[0] = held(2 * p);
+                q[1] = held(2 * p + 1);
+                use(q[0]);
+                use(q[1]);
+            }
+            sent += kTurn;
+        }
+#pragma unroll 1
+        for (; r < cnt; r += 2) {
             send(cnt, fetch);
             copies_pending<PAIRS - 1>();
             Row q[2];
