@@ -20,6 +20,7 @@
 #include <cstdio>
 #include <cstring>
 #include <type_traits>
+#include <utility>
 
 #include "ops.h"
 
@@ -576,12 +577,14 @@ __global__ void __cluster_dims__(kOneCtas, 1, 1) __launch_bounds__(kOneThreads)
 k_grad_norm_one(const __grid_constant__ NormTable<T> a, float max_norm, float* norm, float* scale) {
     __shared__ double sh[kOneThreads / 32], all[kOneCtas];
     cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
+    auto begun = cluster.barrier_arrive();
     double sum = 0.0;
     const int64_t chunks = a.first[a.count];
     int k = a.count - 1;
     for (int64_t ch = chunks - 1 - blockIdx.x * (kOneThreads / kThreadsOp) - threadIdx.x / kThreadsOp; ch >= 0; ch -= kOneTeams)
         sum += norm_chunk<GT, T>(a, ch, k, threadIdx.x % kThreadsOp);
     const double s = block_sum<kOneThreads>(sum, sh);
+    cluster.barrier_wait(std::move(begun));                 // the first block has begun: its shared memory is there
     if (threadIdx.x == 0) cluster.map_shared_rank(all, 0)[blockIdx.x] = s;
     cluster.sync();
     if (blockIdx.x == 0 && threadIdx.x == 0) {
