@@ -316,7 +316,7 @@ int64_t rfast_query(rfast_ctx* ctx, int what);
 
 /* Execution options.  The first two never change results: every path produces the same bits.
  *   RFAST_OPT_PERSISTENT  0 (default): one kernel per phase of a round.  1: problems whose state
- *                         fits L2 (least squares, softmax regression) run a span of rounds as
+ *                         fits L2 (least squares, softmax regression; plain descent) run a span of rounds as
  *                         ONE cooperative persistent kernel with grid barriers between the
  *                         phases of a round.  Every barrier wait is bounded; if one runs out
  *                         the kernel returns and the next synchronising call reports
@@ -509,9 +509,11 @@ int rfast_grad_norm(int32_t n_tensors, int32_t grad_type, const int64_t* numel, 
  *   in fp32, m_scale and v_scale hold ceil(numel / RFAST_ADAMW_BLOCK) of them per tensor, and a
  *   value is code * scale.  Codes are nearest values, ties to even; a positive sqrt(v) keeps at least the
  *   smallest positive code, so that no first moment meets a denominator of eps alone (second moments
- *   below 2^-126 count as zero).  All bytes zero are moments of zero.  A NaN or infinite gradient leaves its whole block's moments NaN or infinite.
+ *   below 2^-126 count as zero).  All bytes zero are moments of zero.  A NaN or infinite gradient leaves
+ *   its whole block's moments NaN or infinite.
  * Tensors may not overlap one another.  Addresses need to be aligned to their type only; tensors whose
- * addresses are all multiples of 16 bytes are the fast ones. */
+ * addresses are all multiples of 16 bytes are the fast ones.  A *d_step below 1 is not seen by the call: it
+ * leaves NaN or infinite parameters. */
 #define RFAST_ADAMW_BLOCK 256
 typedef struct rfast_adamw {
     int32_t n_tensors;
@@ -541,17 +543,22 @@ int rfast_adamw_step(const rfast_adamw* a, void* cuda_stream, char* err, size_t 
  * share a row (all of them: one layer; a worker's rows: one layer per worker).  mean and rstd are
  * written, fp32 [samples][groups]; the backward pass wants them.  Sums and statistics are held in
  * 32 bits, y is rounded once to its type; variances come from deviations, not from a difference
- * of squares.  A NaN or infinity leaves NaN in its sample's group and nowhere else.
+ * of squares.  A NaN or infinity in x leaves NaN in its sample's group and nowhere else (backward: and
+ * in dgamma and dbeta of the channels that it reaches).
  * Strides are those of a sample and of a position, in elements (two numbers; NULL: contiguous);
  * channels are neighbours.  Read operands may overlap themselves (a stride of 0 repeats), written
  * ones may not; y may be x, dx may be x or dy, with the same strides.  Addresses and strides in
- * multiples of 16 bytes are the fast ones.  A group may have 8192 channels at most.
+ * multiples of 16 bytes are the fast ones; no other operands may overlap.  A group may have 8192
+ * channels at most, there may be 2^24 channels, and 65535 runs of neighbouring groups that are at
+ * least 128 bytes wide each.
  *
  * Backward, from dy and the forward pass's x, mean, rstd (act'(0) = 0 for max(u, 0)):
  *     du = dy act'(u);  dbeta = sum du, dgamma = sum du h over the samples of a set (fp32)
  *     dx = rstd (gamma du - sum(gamma du) / M - h sum(gamma du h) / M)
+ * Sums are held in 32 bits, those over thread blocks in 64.  At most 65535 sets, 65534 runs of groups.
  * workspace: rfast_group_norm_workspace(shape, backward) bytes of DEVICE memory, aligned to 16 (0 for
- * many shapes: it may then be NULL); its size depends on the shape alone.  No positions: nothing is normalised, dgamma and dbeta are zero. */
+ * many shapes: it may then be NULL); its size depends on the shape alone.  No positions: nothing is
+ * normalised, dgamma and dbeta are zero. */
 enum { RFAST_ACT_NONE = 0, RFAST_ACT_RELU = 1, RFAST_ACT_SILU = 2 };
 typedef struct rfast_gn_shape {
     int64_t samples, positions;

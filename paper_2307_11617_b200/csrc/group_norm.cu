@@ -135,19 +135,22 @@ template <int LEFT> __device__ __forceinline__ void copies_pending() { asm volat
 // once each: the result is good to about 2^-22.  The special function unit, with a result every other cycle where the
 // adders have eight, is what bounds a pass with this in it, so one reciprocal, of the product of both denominators, serves
 // two values (3 instead of 4 of its operations per pair).  To keep the product in range exp(-u) stops growing at 2^60: below
-// u = -41 the result is 2^-60.
-__device__ __forceinline__ F2 sigmoid2(F2 u) {
+// u = -41 the result is 2^-60.  A NaN gives 2^-60 as well: it must not reach its neighbour through the product, and the caller
+// multiplies by u.  e: exp(-u)
+__device__ __forceinline__ F2 sigmoid2(F2 u, F2& e) {
     float a, b;
     split(u * both(-1.4426950408889634f), a, b);
-    asm("min.NaN.f32 %0, %0, %1;" : "+f"(a) : "f"(60.f));
-    asm("min.NaN.f32 %0, %0, %1;" : "+f"(b) : "f"(60.f));
+    asm("min.f32 %0, %0, %1;" : "+f"(a) : "f"(60.f));
+    asm("min.f32 %0, %0, %1;" : "+f"(b) : "f"(60.f));
     asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(a));
     asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(b));
-    split(pair(a, b) + both(1.f), a, b);
+    e = pair(a, b);
+    split(e + both(1.f), a, b);
     float r = a * b;
     asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(r));
     return pair(b, a) * both(r);
 }
+__device__ __forceinline__ F2 silu2(F2 u) { F2 e; return u * sigmoid2(u, e); }
 
 // cnt rows of a thread out of shared memory, R at a time: all loads of a batch go out before the first row is worked on.
 template <int R, class Row, class Load, class Use>
@@ -649,7 +652,7 @@ k_gn_forward(const __grid_constant__ GnArgs a) {
                     for (int v = 0; v < kP; ++v) o[v] = fma2(o[v] + mean[WHOLE ? 0 : v], mul[v], add[v]);
                     if (s.act == RFAST_ACT_SILU) {
 #pragma unroll
-                        for (int v = 0; v < kP; ++v) o[v] = o[v] * sigmoid2(o[v]);
+                        for (int v = 0; v < kP; ++v) o[v] = silu2(o[v]);
                     } else if (s.act == RFAST_ACT_RELU) {
 #pragma unroll
                         for (int v = 0; v < kP; ++v) {
@@ -673,10 +676,9 @@ k_gn_forward(const __grid_constant__ GnArgs a) {
 // dy act'(u)
 __device__ __forceinline__ F2 through(int act, F2 u, F2 dy) {
     if (act == RFAST_ACT_SILU) {
-        const F2 q = sigmoid2(u);
-        float a, b;
-        split(q, a, b);
-        return dy * fma2(q, fma2(pair(-a, -b), u, u), q);    // q (1 + u (1 - q))
+        F2 e;
+        const F2 q = sigmoid2(u, e);
+        return dy * fma2(q, q * e * u, q);                   // q (1 + u (1 - q)); q e has the digits that 1 - q loses at large u
     }
     if (act == RFAST_ACT_RELU) {
         float a, b, c, d;
@@ -1186,7 +1188,7 @@ k_gn_rows_forward(const __grid_constant__ GnArgs a, const __grid_constant__ RowP
                 for (int v = 0; v < kP; ++v) o[v] = fma2(d[k][v], mul[k][v] * both(rstd), add[k][v]);
                 if (s.act == RFAST_ACT_SILU) {
 #pragma unroll
-                    for (int v = 0; v < kP; ++v) o[v] = o[v] * sigmoid2(o[v]);
+                    for (int v = 0; v < kP; ++v) o[v] = silu2(o[v]);
                 } else if (s.act == RFAST_ACT_RELU) {
 #pragma unroll
                     for (int v = 0; v < kP; ++v) {
@@ -1416,8 +1418,8 @@ size_t workspace_bytes_of(const GnShape& s, int esize, bool backward) {
 
 template <class K>
 cudaError_t launch_task(K kernel, dim3 grid, const GnArgs& a, size_t smem, bool follows, cudaStream_t st) {
-    if (smem > 48 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (smem > 48 * 1024) {                                 // a limit; the same for every call, so that threads may launch side by side
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMostSmem);
         if (e != cudaSuccess) return e;
     }
     cudaLaunchConfig_t cfg{};
@@ -1461,7 +1463,7 @@ cudaError_t launch_rows(GnArgs& a, bool backward, cudaStream_t st) {
     }
     const size_t smem = (size_t)2 * r.sp * r.gt * s.Cg * sizeof(float);
     if (smem > 48 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(k_gn_rows_backward<T, V, K>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        const cudaError_t e = cudaFuncSetAttribute(k_gn_rows_backward<T, V, K>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMostSmem);
         if (e != cudaSuccess) return e;
     }
     k_gn_rows_backward<T, V, K><<<dim3(r.parts, r.slabs, (unsigned)sets), kT, smem, st>>>(a, r);

@@ -253,9 +253,10 @@ def test_positions_of_another_order_and_repeated_ones(rfast_lib):
 
 
 @pytest.mark.parametrize("bad", [np.nan, np.inf, -np.inf])
-@pytest.mark.parametrize("shape", ["ten a group", "hidden layer", "long"])
-def test_bad_values_stay_in_their_group(rfast_lib, shape, bad):
-    c = _Case(SHAPES[shape], "f32", seed=6)
+@pytest.mark.parametrize("shape,kind", [("ten a group", "f32"), ("hidden layer", "f32"), ("long", "f32"), ("one channel a group", "bf16"),
+                                        ("three a group", "bf16"), ("prime groups", "f16")])
+def test_bad_values_stay_in_their_group(rfast_lib, shape, kind, bad):
+    c = _Case(SHAPES[shape], kind, seed=6)
     good = [_np(t) for t in c.forward("silu")]
     n, s, ch = c.n - 1, c.s // 2, c.c // 2
     c.x[n, s, ch] = bad
@@ -269,6 +270,31 @@ def test_bad_values_stay_in_their_group(rfast_lib, shape, bad):
     rows[n, g] = True
     for a, b in ((good[1], hurt[1]), (good[2], hurt[2])):
         assert np.array_equal(a[~rows], b[~rows]) and not np.isfinite(b[rows]).any()
+
+
+@pytest.mark.parametrize("shape", ["one channel a group", "ten a group", "hidden layer", "long", "seventeen positions"])
+def test_a_bad_shift_stays_in_its_channel(rfast_lib, shape):
+    """A NaN in one channel's beta reaches that channel's values alone, forward and backward."""
+    c = _Case(SHAPES[shape], "bf16", seed=16)
+    good = [_np(t) for t in c.forward("silu")]
+    ch = c.c // 2
+    c.beta[0, ch] = np.nan
+    hurt = [_np(t) for t in c.forward("silu")]
+    hit = np.zeros(good[0].shape, bool)
+    hit[:c.n // c.sets, :, ch] = True
+    assert np.array_equal(good[0][~hit], hurt[0][~hit]) and np.isnan(hurt[0][hit]).all()
+    assert np.array_equal(good[1], hurt[1]) and np.array_equal(good[2], hurt[2])
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", ["ten a group", "hidden layer", "long", "seventeen positions", "wide odd group"])
+def test_slopes_far_from_zero(rfast_lib, shape, kind):
+    """Values of hundreds before the activation: its slope there is 1 or 0, however large they are."""
+    c = _Case(SHAPES[shape], kind, seed=17)
+    c.gamma *= 100.0
+    got = c.forward("silu")
+    _check_forward(c, "silu", got)
+    _check_backward(c, "silu", got[1], got[2], c.backward("silu", got[1], got[2]))
 
 
 def test_far_levels_and_flat_groups(rfast_lib):
@@ -324,6 +350,31 @@ def test_recorded_passes_and_side_by_side(rfast_lib):
     torch.cuda.synchronize()
     for w, o in zip(want, outs):
         assert all(torch.equal(a, b) for a, b in zip(w, o))
+
+
+def test_calls_of_two_threads(rfast_lib):
+    """Threads that launch one kernel with buffers of different sizes do not disturb each other."""
+    import threading
+    torch, _ = _torch()
+    cases = [_Case((160, s, 64, 1, 1), "f32", seed=30 + s) for s in (200, 255)]
+    want = [[t.clone() for t in c.forward("silu")] for c in cases]
+    torch.cuda.synchronize()
+    failed = []
+
+    def many(c, w):
+        try:
+            for _ in range(200):
+                got = c.forward("silu")
+                if not all(torch.equal(a, b) for a, b in zip(got, w)):
+                    raise AssertionError("values differ")
+        except Exception as e:  # noqa: BLE001
+            failed.append(e)
+    threads = [threading.Thread(target=many, args=a) for a in zip(cases, want)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failed, failed[0]
 
 
 def test_no_positions_and_foreign_addresses(rfast_lib):
