@@ -8,12 +8,15 @@
 //     sums waits in shared memory: asynchronous copies that only this thread reads back, so no barrier guards them;
 //   - slabs that are too large for that, or too few to fill the GPU, are cut into equal chunks of positions, as many as thread
 //     blocks run at a time: one launch for the chunks' sums, one that merges them and goes over the values again, from the
-//     end, so that the L2 cache serves what it still holds.  (Spans of equal length over slabs laid end to end, which give
-//     every SM the same work, were slower: a block whose span holds the end of a slab and the start of the next sets up
-//     and sums up twice, 5 us each, and the launch waits for it: 36 against 25 us for 32 x 3136 x 256 bf16.)
-// The sums of a slab could also meet inside a cluster of thread blocks that keep the slab in their shared memory.  Built and
-// measured: loading, summing and writing then follow one another on the whole GPU, and 32 x 3136 x 256 bf16 took 37 us
-// forward and 122 us backward.
+//     last position to the first, so that the L2 cache serves what it still holds (32 x 3136 x 256 bf16 backward, x and dy
+//     103 MB: the second launch reads 48 MB from memory, in the order of the first 87 MB).
+// Measured and dropped, all for 32 x 3136 x 256 bf16 and against 31 us forward and 48 us backward:
+//   - spans of equal length over slabs laid end to end, which give every SM the same work: a block whose span holds the end
+//     of a slab and the start of the next sets up and sums up twice, and the launch waits for it (36 and 84 us);
+//   - a cluster of thread blocks that keep a slab in their shared memory and merge its sums there: loading, summing and
+//     writing then follow one another on the whole GPU (37 and 122 us);
+//   - wider slabs: 256 bytes 31 and 52 us, 512 bytes 32 and 52 us (2 x 16384 x 320 f16: 17 us at 128 bytes, 23 and 34 us);
+//   - smaller chunks, half as many again: 35 and 57 us.
 //
 // Variances do not come from a difference of two large sums: a thread sums deviations from the first value it
 // sees in each channel, and its mean and sum of squared deviations are merged with the others' by the parallel
@@ -169,7 +172,8 @@ __device__ __forceinline__ void walk(int cnt, Load load, Use use) {
 }
 // The same out of memory, through a ring of 2 PAIRS slots in shared memory that only this thread uses: `fetch(slot)` starts the
 // asynchronous copies of the next row into a slot, `held(slot)` reads one.  What is on its way costs no registers, so there can be
-// enough of it: rows fetched ahead into registers left 40 to 50 KB on their way in an SM, and 4 TB/s.
+// enough of it: rows fetched ahead into registers left 40 to 50 KB on their way in an SM, and 4 TB/s.  (Two pairs: backward 50 us in the
+// place of 48; four: forward 31.2 in the place of 30.8 us, see the kernels for the shape.)
 template <int PAIRS> struct Ring {
     int in, sent;
     template <class Fetch> __device__ __forceinline__ void send(int cnt, Fetch& fetch) {
@@ -392,8 +396,13 @@ __device__ __forceinline__ int team_size(int entries) {
 
 // ---- forward --------------------------------------------------------------------------------------
 // kWhole, kReread: grid = (items, slabs).  kSums, kApply: grid = (chunks, slabs, samples of the launch).
+// 32 x 3136 x 256 bf16 with u / (1 + exp(-u)): 31 us, 3.3 TB/s of x read and y written once; 26 us without an activation.  The
+// sums take 11 us of it whether x comes from memory or from the L2 cache, the second launch 20 us: its 51 MB of writes
+// alone take 14 us (a plain fill does), the special function unit is busy for 9 us, and what is in the way is that all blocks
+// merge and set up at the same time.  Registers for two blocks per SM, four where a group's channels fill accesses (2 x 16384 x
+// 320 f16, ten channels a group: 17.0 us with two, 18.6 us with three; 32 x 3136 x 256 bf16: 31.4 us with two, 30.8 us with four).
 template <class T, int V, bool WHOLE, int TASK>
-__global__ void __launch_bounds__(kT, WHOLE ? 4 : 3)
+__global__ void __launch_bounds__(kT, WHOLE ? 4 : 2)
 k_gn_forward(const __grid_constant__ GnArgs a) {
     extern __shared__ __align__(16) uint8_t smem[];
     typedef Vec<T, V> X;
@@ -413,15 +422,17 @@ k_gn_forward(const __grid_constant__ GnArgs a) {
     const int nb = p.ns * p.gs;
     float2* fin = reinterpret_cast<float2*>(e_m2 + kEnt * width);      // [nb] mean, rstd
     const Seat me = seat_of(p);
-    const int64_t step = (int64_t)p.tr * a.xs, ostep = (int64_t)p.tr * a.os;
+    const int64_t rows_on = TASK == kApply ? -p.tr : p.tr;   // from row to row of a thread
+    const int64_t step = rows_on * a.xs, ostep = rows_on * a.os;
     if (TASK == kSums) asm volatile("griddepcontrol.launch_dependents;");
     {
         Part part;
         if (kOne) { part.n = (int64_t)blockIdx.x * p.ns; part.slab = blockIdx.y; part.from = 0; part.piece = 0; }
         else part = part_of<TASK == kApply>(a);
         const int slab = part.slab, gs = min(p.gs, s.G - slab * p.gs);      // the last slab may be narrower
-        const int64_t n = part.n + me.sl, r0 = part.from + me.rr;            // this thread's sample and first position
+        const int64_t n = part.n + me.sl;                    // this thread's sample, positions and the first of them
         const int cnt = kOne ? (n < s.N ? me.rows : 0) : me.on ? rows_of(part.count, me.rr, p.tr) : 0;
+        const int64_t r0 = part.from + me.rr + (TASK == kApply ? (cnt - 1) * (int64_t)p.tr : 0);
         const int c0 = slab * p.W, cols = gs * s.Cg / V;
         const T* x = (const T*)a.x + n * a.xn + r0 * a.xs + c0;
         const T* px = x + me.txi * V;                        // of the pass over the width that is under way
@@ -749,8 +760,11 @@ k_gn_affine(const float* __restrict__ part, int64_t rows, int C, float* __restri
 // shared memory and, buffered, du in fp32 in the place of dy, so that the second pass has no exponentials.
 // kSums, kApply: grid = (chunks, slabs, samples of the launch), the last kApply with one slab more, whose blocks form dgamma and dbeta
 // meanwhile.
+// 32 x 3136 x 256 bf16: 48 us, 3.2 TB/s of x and dy read and dx written once.  Bound by the arithmetic of a row (about 100
+// instructions for 8 channels) and its latency: the sums take as long with half of x and dy in the L2 cache.  So registers for two
+// blocks per SM, in which two rows' work interleaves: 48 us against 51 us with three.
 template <class T, int V, bool WHOLE, int TASK>
-__global__ void __launch_bounds__(kT, WHOLE && (TASK == kSums || TASK == kApply) ? 3 : 2)
+__global__ void __launch_bounds__(kT, 2)
 k_gn_backward(const __grid_constant__ GnArgs a) {
     extern __shared__ __align__(16) uint8_t smem[];
     typedef Vec<T, V> X;
@@ -783,7 +797,8 @@ k_gn_backward(const __grid_constant__ GnArgs a) {
     }
     if (TASK == kSums) asm volatile("griddepcontrol.launch_dependents;");
     const Seat me = seat_of(p);
-    const int64_t xstep = (int64_t)p.tr * a.xs, dstep = (int64_t)p.tr * a.ds, ostep = (int64_t)p.tr * a.os;
+    const int64_t rows_on = TASK == kApply ? -p.tr : p.tr;   // from row to row of a thread
+    const int64_t xstep = rows_on * a.xs, dstep = rows_on * a.ds, ostep = rows_on * a.os;
     const float inv_m = 1.f / ((float)s.S * (float)s.Cg);
     if (TASK != kApply)
         for (int c = threadIdx.x; c < 2 * p.W; c += kT) acc[c] = 0.f;
@@ -799,12 +814,13 @@ k_gn_backward(const __grid_constant__ GnArgs a) {
             part = part_of<TASK == kApply>(a);
         }
         const int slab = part.slab, gs = min(p.gs, s.G - slab * p.gs), W = gs * s.Cg;      // the last slab may be narrower
-        const int64_t n = part.n, r0 = part.from + me.rr;     // this thread's sample and first position
+        const int64_t n = part.n;                             // this thread's sample
         const int64_t set = kOne ? (int64_t)blockIdx.z : (int64_t)((unsigned)n / (unsigned)s.per_set);
         const int c0 = slab * p.W, cols = W / V;
         const float* gam = affine_row(a, a.gamma, set) + c0;
         const float* bet = affine_row(a, a.beta, set) + c0;
         const int cnt = kOne ? (in_set < s.per_set ? me.rows : 0) : me.on ? rows_of(part.count, me.rr, p.tr) : 0;
+        const int64_t r0 = part.from + me.rr + (TASK == kApply ? (cnt - 1) * (int64_t)p.tr : 0);      // its first position
         const T* x = (const T*)a.x + n * a.xn + r0 * a.xs + c0;
         const T* dy = (const T*)a.dy + n * a.dn + r0 * a.ds + c0;
         const T *px = x + me.txi * V, *pd = dy + me.txi * V;  // of the pass over the width that is under way
@@ -1320,7 +1336,7 @@ constexpr size_t kMostSmem = 220 * 1024;
 int chunks_of(const GnShape& s, int esize, int W, int slabs, bool whole, bool backward) {
     const int64_t item = s.S * W * esize, items = s.N * slabs;
     if (s.S < 64 || (item <= (backward ? 32 * 1024 : 64 * 1024) && (items >= kSms || item <= 16 * 1024))) return 0;
-    const int64_t at_a_time = (backward ? whole ? 3 : 2 : whole ? 4 : 3) * kSms;
+    const int64_t at_a_time = (backward ? 2 : whole ? 4 : 2) * kSms;
     int64_t chunks = at_a_time / items;
     if (chunks > item / (8 * 1024)) chunks = item / (8 * 1024);
     if (chunks > s.S / 32) chunks = s.S / 32;
