@@ -1112,13 +1112,24 @@ k_gn_backward(const __grid_constant__ GnArgs a) {
 
 // ---- one position per sample ----------------------------------------------------------------------
 // The rows of a hidden layer: a team of lanes takes a sample's group, K accesses per lane, and everything that belongs to
-// it stays in their registers; no barrier until the channels' sums of the backward pass are added up at the very end.  The general
-// path, whose blocks hold 32 samples and meet at five barriers for them, took 15.3 us forward and 39 us backward for 4096 x 512 fp32
-// in 16 groups.
-// A block has teams for `gt` neighbouring groups (128 bytes and more) of `sp` samples and walks down the samples.
+// it stays in their registers; no barrier until the channels' sums of the backward pass are added up at the very end.
+// A block has teams for `gt` neighbouring groups (128 bytes and more) of `sp` samples and walks down the samples; in the
+// forward pass neighbouring ones, so that it reads a set's scale and shift once (every block taking every 592nd row of teams:
+// 4096 x 2048 fp32, 64 sets, 44 us in the place of 15).
+// A lane holds 8 channels, 4 accesses where a team of 32 lanes with 8 each does not cover the group.  4096 x 512 fp32 in 16
+// groups, 64 sets: 6.8 us forward, 7.5 us backward; the general path, whose blocks hold 32 samples and meet at five barriers for
+// them, takes 15 and 39 us.  32768 x 512, the same sets' size: 43 and 51 us, 3.1 and 4.0 TB/s, bound by the loads that the blocks
+// have on their way.  16-bit loads of the backward pass go out two turns ahead and registers are for two blocks of an SM
+// (32768 x 512 bf16, one set: 31 us; one turn and three blocks: 44 us); forward a second turn ahead gains nothing.  With 4
+// channels per lane 4096 x 512 fp32 takes 7.2 and 7.7 us; with 16 of 16-bit types the registers spill (bf16 backward 13 us
+// in the place of 7).
+// 4096 x 2048 fp32 in 4 groups: 15.5 us, 4.3 TB/s, and 32 us backward, 3.2 TB/s; the general path takes 60 and 146 us.
+constexpr int kRowChannels = 8;
+template <int V, int K, bool BACKWARD> constexpr int kRowBlocks = BACKWARD ? K * V <= kRowChannels ? 2 : 1 : K == 1 ? 4 : K == 2 ? 3 : 2;
 struct RowPlan {
     int L, gt, sp, slabs;              // lanes of a team, groups and samples of a block, blocks across the groups
     int parts;                         // blocks down the samples (backward: of a set)
+    int turns;                         // forward: of a block
     Divisor by_gt;
 };
 
@@ -1141,7 +1152,7 @@ struct RowSeat {
 
 // grid = (parts, slabs); all lanes of a warp go through every turn, the shuffles being the warp's
 template <class T, int V, int K>
-__global__ void __launch_bounds__(kT, K == 1 ? 4 : 1)
+__global__ void __launch_bounds__(kT, kRowBlocks<V, K, false>)
 k_gn_rows_forward(const __grid_constant__ GnArgs a, const __grid_constant__ RowPlan r) {
     const GnShape& s = a.s;
     typedef Vec<T, V> X;
@@ -1151,17 +1162,18 @@ k_gn_rows_forward(const __grid_constant__ GnArgs a, const __grid_constant__ RowP
     F2 mul[K][kP], add[K][kP];
     int64_t set = -1;
     X q[K], next[K];
-    const int64_t jump = (int64_t)gridDim.x * r.sp, n0 = (int64_t)blockIdx.x * r.sp + me.sp;
+    // neighbouring samples, whose sets are few
+    const int64_t jump = r.sp, from = (int64_t)blockIdx.x * r.turns * r.sp, stop = min(s.N, from + (int64_t)r.turns * r.sp);
     auto load = [&](int64_t n, X (&to)[K]) {
 #pragma unroll
         for (int k = 0; k < K; ++k)
-            if (k < me.left && n < s.N) to[k] = load_vec<T, V>((const T*)a.x + n * a.xn + me.c + (int64_t)k * r.L * V);
+            if (k < me.left && n < stop) to[k] = load_vec<T, V>((const T*)a.x + n * a.xn + me.c + (int64_t)k * r.L * V);
     };
-    load(n0, q);
-    for (int64_t base = (int64_t)blockIdx.x * r.sp; base < s.N; base += jump) {
+    load(from + me.sp, q);
+    for (int64_t base = from; base < stop; base += jump) {
         const int64_t n = base + me.sp;
         load(n + jump, next);
-        const int left = n < s.N ? me.left : 0;
+        const int left = n < stop ? me.left : 0;
         if (left && (int64_t)((unsigned)n / (unsigned)s.per_set) != set) {
             set = (unsigned)n / (unsigned)s.per_set;
             const float *gam = affine_row(a, a.gamma, set) + me.c, *bet = affine_row(a, a.beta, set) + me.c;
@@ -1221,7 +1233,7 @@ k_gn_rows_forward(const __grid_constant__ GnArgs a, const __grid_constant__ RowP
 
 // grid = (parts, slabs, sets); dynamic shared memory: [2][kT * K * V] floats
 template <class T, int V, int K>
-__global__ void __launch_bounds__(kT, K == 1 ? 3 : 1)
+__global__ void __launch_bounds__(kT, kRowBlocks<V, K, true>)
 k_gn_rows_backward(const __grid_constant__ GnArgs a, const __grid_constant__ RowPlan r) {
     extern __shared__ __align__(16) uint8_t smem[];
     const GnShape& s = a.s;
@@ -1232,8 +1244,9 @@ k_gn_rows_backward(const __grid_constant__ GnArgs a, const __grid_constant__ Row
     const float *gam = affine_row(a, a.gamma, set) + me.c, *bet = affine_row(a, a.beta, set) + me.c;
     const float inv = -1.f / (float)s.Cg;
     F2 ga[K][kP], be[K][kP], s_du[K][kP], s_dh[K][kP];
-    Pair<X> q[K], next[K];
-    float mean = 0.f, rs = 0.f, mean_next = 0.f, rs_next = 0.f;
+    constexpr int kAhead = K == 1 ? 2 : 1;                 // turns whose values are on their way while a lane works on one
+    Pair<X> q[kAhead + 1][K];                                // this turn's values, then the following ones'
+    float means[kAhead + 1], rstds[kAhead + 1];
     const int64_t jump = (int64_t)gridDim.x * r.sp, end = (set + 1) * s.per_set;
     auto load = [&](int64_t n, Pair<X> (&to)[K], float& m, float& t) {
         if (n < end && me.left) {
@@ -1248,7 +1261,10 @@ k_gn_rows_backward(const __grid_constant__ GnArgs a, const __grid_constant__ Row
         }
     };
     const int64_t first = set * s.per_set + (int64_t)blockIdx.x * r.sp;
-    load(first + me.sp, q, mean, rs);
+#pragma unroll
+    for (int t = 0; t <= kAhead; ++t) means[t] = rstds[t] = 0.f;
+#pragma unroll
+    for (int t = 0; t < kAhead; ++t) load(first + me.sp + t * jump, q[t], means[t], rstds[t]);
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         if (k < me.left) { affine_of<V>(gam + k * r.L * V, a.quads, ga[k]); affine_of<V>(bet + k * r.L * V, a.quads, be[k]); }
@@ -1257,14 +1273,15 @@ k_gn_rows_backward(const __grid_constant__ GnArgs a, const __grid_constant__ Row
     }
     for (int64_t base = first; base < end; base += jump) {
         const int64_t n = base + me.sp;
-        load(n + jump, next, mean_next, rs_next);
+        load(n + kAhead * jump, q[kAhead], means[kAhead], rstds[kAhead]);
         const int left = n < end ? me.left : 0;
+        const float mean = means[0], rs = rstds[0];
         F2 h[K][kP], du[K][kP], one = both(0.f), two = both(0.f);
 #pragma unroll
         for (int k = 0; k < K; ++k)
             if (k < left) {
-                widen(q[k].x, h[k]);
-                widen(q[k].d, du[k]);
+                widen(q[0][k].x, h[k]);
+                widen(q[0][k].d, du[k]);
 #pragma unroll
                 for (int v = 0; v < kP; ++v) {
                     h[k][v] = (h[k][v] + both(-mean)) * both(rs);
@@ -1290,9 +1307,12 @@ k_gn_rows_backward(const __grid_constant__ GnArgs a, const __grid_constant__ Row
                 store_vec<V>((T*)a.out + n * a.on + me.c + (int64_t)k * r.L * V, o);
             }
 #pragma unroll
-        for (int k = 0; k < K; ++k) q[k] = next[k];
-        mean = mean_next;
-        rs = rs_next;
+        for (int t = 0; t < kAhead; ++t) {
+#pragma unroll
+            for (int k = 0; k < K; ++k) q[t][k] = q[t + 1][k];
+            means[t] = means[t + 1];
+            rstds[t] = rstds[t + 1];
+        }
     }
     // the channels' sums of the block's teams: [sample's row of teams][group of the block][channel]
     float* sh0 = reinterpret_cast<float*>(smem);
@@ -1461,7 +1481,7 @@ cudaError_t launch_rows(GnArgs& a, bool backward, cudaStream_t st) {
     r.gt = 1;
     while (r.gt < teams && r.gt < s.G && r.gt * s.Cg * (int)sizeof(T) < 128) r.gt *= 2;
     // more groups and fewer samples per block while blocks are more than run at a time: a block's set-up then serves more turns
-    const int at_a_time = (K == 1 ? backward ? 3 : 4 : 1) * kSms;
+    const int at_a_time = (backward ? kRowBlocks<V, K, true> : kRowBlocks<V, K, false>) * kSms;
     auto slabs = [&](int gt) { return (s.G + gt - 1) / gt; };
     while (r.gt * 2 <= teams && r.gt < s.G && (int64_t)slabs(r.gt) * (backward ? sets : 1) > at_a_time) r.gt *= 2;
     r.slabs = slabs(r.gt);
@@ -1472,6 +1492,10 @@ cudaError_t launch_rows(GnArgs& a, bool backward, cudaStream_t st) {
     if (parts > turns) parts = turns;
     if (backward && parts > part_rows(s)) parts = part_rows(s);
     r.parts = parts < 1 ? 1 : (int)parts;
+    if (!backward) {
+        r.turns = (int)((turns + r.parts - 1) / r.parts);
+        r.parts = (int)((turns + r.turns - 1) / r.turns);
+    }
     r.by_gt.set(r.gt);
     if (!backward) {
         k_gn_rows_forward<T, V, K><<<dim3(r.parts, r.slabs), kT, 0, st>>>(a, r);
@@ -1520,7 +1544,7 @@ template <class T, int V>
 cudaError_t launch_gn(GnArgs& a, bool backward, cudaStream_t st) {
     if constexpr (V * sizeof(T) == 16) {
         if (in_rows(a.s, V, (int)sizeof(T)))
-            return a.s.Cg / V <= 32 ? launch_rows<T, V, 1>(a, backward, st) : launch_rows<T, V, 4>(a, backward, st);
+            return a.s.Cg <= 32 * kRowChannels ? launch_rows<T, V, kRowChannels / V>(a, backward, st) : launch_rows<T, V, 4>(a, backward, st);
     }
     if (a.s.Cg % V == 0) return launch_whole<T, V, true>(a, backward, st);
     if constexpr (V > 1) return launch_whole<T, V, false>(a, backward, st);
