@@ -367,6 +367,28 @@ def test_offsets_beyond_32_bits(rfast_lib, shape):
     assert all(torch.equal(p, q) for p, q in zip(near, far))
 
 
+def test_more_samples_than_a_grid_holds(rfast_lib):
+    """Pieces of more than 65535 samples go out in several launches; samples on both sides of the border and the sums over all."""
+    torch, _ = _torch()
+    n, s, ch, g = 65538, 520, 64, 4
+    c = _Case((4, s, ch, g, 1), "bf16", seed=41)
+    c.n = n
+    torch.manual_seed(5)
+    c.x, c.dy = (torch.randn(n, s, ch, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    y = torch.empty_like(c.x)
+    got = c.forward("relu", out=y)
+    few = [0, 65534, 65535, 65537]
+    small = _Case((4, s, ch, g, 1), "bf16", seed=41)
+    small.gamma, small.beta, small.x, small.dy = c.gamma, c.beta, c.x[few], c.dy[few]
+    _check_forward(small, "relu", [t[few] for t in got])
+    back = c.backward("none", got[1], got[2], out=y)
+    ref = small.backward("none", got[1][few].contiguous(), got[2][few].contiguous())
+    _check_backward(small, "none", got[1][few], got[2][few], (back[0][few], ref[1], ref[2]))
+    total, size = (sum(f(c.dy[k:k + 4096].double()).sum((0, 1)) for k in range(0, n, 4096)) for f in (lambda t: t, torch.abs))
+    # a thread block adds up a sample's positions in fp32, all else in 64 bits
+    assert bool(((back[2][0].double() - total).abs() <= (s + 64) * U * size + U * total.abs()).all())
+
+
 def test_calls_of_two_threads(rfast_lib):
     """Threads that launch one kernel with buffers of different sizes do not disturb each other."""
     import threading
