@@ -43,6 +43,10 @@ SHAPES = {
     "ragged slab": (2, 19, 200, 25, 1),
     "ragged slab, few positions": (7, 3, 200, 25, 1),
     "prime groups": (2, 5, 309, 103, 1),
+    "ragged slab, many samples": (40, 19, 200, 25, 2),
+    "three a group, many samples": (40, 70, 96, 32, 1),
+    "prime groups, many samples": (33, 5, 309, 103, 1),
+    "ragged slab, many long samples": (36, 1100, 200, 25, 1),
     "twenty a group": (2, 301, 40, 2, 1),
     "long": (1, 5001, 128, 32, 1),
     "long, wide groups": (2, 4000, 256, 2, 1),
@@ -55,7 +59,7 @@ SHAPES = {
     "very long, wide odd group": (1, 700, 4097, 1, 1),
     "seventeen positions": (9, 17, 64, 4, 3),
 }
-LONG = ("very long", "very long, wide odd group")
+LONG = ("very long", "very long, wide odd group", "ragged slab, many long samples")
 
 
 def _torch():
