@@ -23,6 +23,7 @@
 #include <utility>
 
 #include "ops.h"
+#include "pairs.cuh"
 
 namespace rfast {
 
@@ -121,34 +122,58 @@ struct TensorView {
 
 // Factors of a step that do not change from value to value.
 struct StepFactors {
-    float b1, g1;        // m = b1 m + g1 g
-    float b2, g2;        // 32-bit moments: v = b2 v + (g2 g)^2; 8-bit moments: v = (b2 r)^2 + (g2 g)^2
+    float scale;         // of the gradients
+    float b1, g1;        // 32-bit moments: m = b1 m + g1 g, the scale within g1; 8-bit moments: m = b1 m + g1 (scale g)
+    float b2, g2;        // 32-bit moments: v = b2 v + (g2 g)^2, likewise; 8-bit moments: v = (b2 r)^2 + (g2 scale g)^2
     float root, eps, keep, step;
 };
 template <bool S8>
 __device__ __forceinline__ StepFactors factors(const AdamCoef& c, float gscale) {
-    return {c.beta1, gscale * c.omb1, S8 ? c.root_beta2 : c.beta2, gscale * c.root_omb2, c.root, c.eps, c.keep, c.step};
+    if (S8) return {gscale, c.beta1, c.omb1, c.root_beta2, c.root_omb2, c.root, c.eps, c.keep, c.step};
+    return {1.f, c.beta1, gscale * c.omb1, c.beta2, gscale * c.root_omb2, c.root, c.eps, c.keep, c.step};
 }
 
-// Eight values: moments and parameter after the step.  8-bit moments come as codes with their block's
-// scales and leave as the first moment and the root of the second.
-template <bool S8>
-__device__ __forceinline__ void advance(const StepFactors& f, float sm, float sv, float (&p)[8], const float (&g)[8], float (&m)[8], float (&v)[8]) {
-    const float bm = S8 ? sm * f.b1 : f.b1, bv = S8 ? sv * f.b2 : f.b2;
+// Eight values with 32-bit moments: moments and parameter after the step.
+__device__ __forceinline__ void advance(const StepFactors& f, float (&p)[8], const float (&g)[8], float (&m)[8], float (&v)[8]) {
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
         const float h = f.g2 * g[k];
-        m[k] = fmaf(f.g1, g[k], bm * m[k]);
-        float r;
-        if (S8) {
-            const float q = bv * v[k];
-            r = root_of(fmaf(q, q, h * h));
-            v[k] = r;
-        } else {
-            v[k] = fmaf(bv, v[k], h * h);
-            r = root_of(v[k]);
-        }
+        m[k] = fmaf(f.g1, g[k], f.b1 * m[k]);
+        v[k] = fmaf(f.b2, v[k], h * h);
+        const float r = root_of(v[k]);
         p[k] = fmaf(-f.step, m[k] * inverse_of(fmaf(r, f.root, f.eps)), p[k] * f.keep);
+    }
+}
+
+// 8-bit moments come as codes with their block's scales and leave as the first moment and the root of the second.
+//
+// First moments.  Value, products and sum are rounded one after the other, as the formula has them: the sum decides between two
+// codes, and formed in fewer roundings it falls on the other side of a border in other places than a plain evaluation does
+// (26M values: some 30 codes, each off by 2^-4 of itself).  The scaled gradients are left in g.
+__device__ __forceinline__ void first_moments8(const StepFactors& f, float sm, float (&g)[8], float (&m)[8]) {
+#pragma unroll
+    for (int k = 0; k < 8; k += 2) {
+        const F2 s = pair(g[k], g[k + 1]) * both(f.scale);
+        split(s, g[k], g[k + 1]);
+        float a[2], b[2];
+        split(pair(m[k], m[k + 1]) * both(sm) * both(f.b1), a[0], a[1]);
+        split(s * both(f.g1), b[0], b[1]);
+        m[k] = __fadd_rn(a[0], b[0]);                       // (a sum of pairs would be merged with the product before it)
+        m[k + 1] = __fadd_rn(a[1], b[1]);
+    }
+}
+__device__ __forceinline__ void advance8(const StepFactors& f, float sm, float sv, float (&p)[8], float (&g)[8], float (&m)[8], float (&v)[8]) {
+    const float bv = sv * f.b2;
+    first_moments8(f, sm, g, m);
+#pragma unroll
+    for (int k = 0; k < 8; k += 2) {
+        const F2 q = pair(v[k], v[k + 1]) * both(bv), h = pair(g[k], g[k + 1]) * both(f.g2);
+        split(fma2(q, q, h * h), v[k], v[k + 1]);
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        v[k] = root_of(v[k]);
+        p[k] = fmaf(-f.step, m[k] * inverse_of(fmaf(v[k], f.root, f.eps)), p[k] * f.keep);
     }
 }
 
@@ -204,7 +229,8 @@ __device__ __forceinline__ void finish(const RawBlock<PT, GT, MT>& r, const Tens
             unpack4(r.v[k], (const float*)nullptr, v + 4 * k);
         }
     }
-    advance<S8>(f, r.sm, r.sv, p, g, m, v);
+    if constexpr (S8) advance8(f, r.sm, r.sv, p, g, m, v);
+    else advance(f, p, g, m, v);
 #pragma unroll
     for (int k = 0; k < 2; ++k) store4((PT*)t.p + i + k * 128, p + 4 * k);
     if constexpr (S8) {
@@ -247,7 +273,8 @@ __device__ __forceinline__ void block_by_values(const TensorView& t, const StepF
             v[k] = in ? ((const float*)t.v)[j] : 0.f;
         }
     }
-    advance<S8>(f, S8 ? t.ms[b] : 0.f, S8 ? t.vs[b] : 0.f, p, g, m, v);
+    if constexpr (S8) advance8(f, t.ms[b], t.vs[b], p, g, m, v);
+    else advance(f, p, g, m, v);
     float sm, sv, cm[8], cv[8];
     if constexpr (S8) to_codes(m, v, sm, sv, cm, cv);
 #pragma unroll

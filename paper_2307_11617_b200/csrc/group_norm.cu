@@ -30,6 +30,7 @@
 #include <type_traits>
 
 #include "ops.h"
+#include "pairs.cuh"
 
 namespace rfast {
 
@@ -55,14 +56,6 @@ __device__ __forceinline__ Vec<T, V> load_vec(const T* p) {
     v.w = *reinterpret_cast<const typename Vec<T, V>::W*>(p);
     return v;
 }
-// Two fp32 values side by side: one instruction adds or multiplies both.
-struct F2 { uint64_t v; };
-__device__ __forceinline__ F2 pair(float a, float b) { F2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b)); return r; }
-__device__ __forceinline__ F2 both(float a) { return pair(a, a); }
-__device__ __forceinline__ void split(F2 p, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p.v)); }
-__device__ __forceinline__ F2 operator+(F2 a, F2 b) { F2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
-__device__ __forceinline__ F2 operator*(F2 a, F2 b) { F2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
-__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) { F2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v)); return r; }
 
 // pairs of V channels; a single channel has a zero beside it
 template <int V> constexpr int kPairs = (V + 1) / 2;

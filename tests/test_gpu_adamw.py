@@ -400,3 +400,34 @@ def test_grad_norm_at_the_ends_of_the_range(rfast_lib, values, norm):
     else:
         assert abs(got - norm) <= 6 * U * norm + 2.0 ** -149
         assert scale == (1.0 if norm <= 1 else pytest.approx(1 / norm, rel=1e-6))
+
+
+@pytest.mark.parametrize("clip", [1.0, 0.30078125, 0.3])
+@pytest.mark.parametrize("lead", [0, 1], ids=["aligned", "odd"])
+def test_first_moments_codes_are_those_of_the_formula_in_32_bits(rfast_lib, lead, clip):
+    """Codes and scales of the first moment equal, bit for bit, those of the formula evaluated one operation after the other in fp32.
+    A moment near a border between two codes falls on one side or the other by its last bits; over 2^24 values some twenty are that near."""
+    import paper_2307_11617_b200 as pkg
+    torch, _ = _torch()
+    n = 2 ** 24 + 77
+    torch.manual_seed(11 + lead)
+    size = torch.exp(2 * torch.randn(-(-n // 256), device="cuda") - 7).repeat_interleave(256)[:n]
+    at = lambda values: torch.cat([torch.zeros(lead, dtype=values.dtype, device="cuda"), values])  # noqa: E731
+    p, g = at(torch.randn(n, device="cuda")), at(size * torch.randn(n, device="cuda"))
+    m = at(torch.randint(0, 256, (n,), dtype=torch.uint8, device="cuda") & 0xFE)           # no code is a NaN
+    v = at(torch.randint(1, 127, (n,), dtype=torch.uint8, device="cuda"))
+    ms, vs = size[::256] * 1e-3, size[::256] * 1e-2
+    b1 = torch.tensor(B1, dtype=torch.float32, device="cuda")
+    g1 = torch.tensor(1.0 - B1, dtype=torch.float32, device="cuda")
+    scale = torch.tensor([clip], device="cuda")
+    old = m[lead:].view(torch.float8_e4m3fn).float() * ms.repeat_interleave(256)[:n]
+    want = old * b1 + (g[lead:] * scale) * g1
+    full = torch.cat([want, torch.zeros(-n % 256, device="cuda")]).view(-1, 256)
+    top = (full.abs().amax(1) * torch.tensor(1 / 448, device="cuda")).clamp_min(2.0 ** -100)
+    code = (full * (1.0 / top)[:, None]).clamp(-448, 448).to(torch.float8_e4m3fn).view(torch.uint8).view(-1)[:n]
+    a = lambda t: [t.data_ptr() + lead * t.element_size()]  # noqa: E731
+    pkg.rfast_adamw_step(a(p), a(g), a(m), a(v), [n], step=3, lr=LR, beta1=B1, beta2=B2, eps=EPS, weight_decay=WD, m_scale=[ms.data_ptr()],
+                         v_scale=[vs.data_ptr()], d_grad_scale=scale.data_ptr(), cuda_stream=torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    assert torch.equal(ms, top)
+    assert int((m[lead:] != code).sum()) == 0
