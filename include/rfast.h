@@ -502,15 +502,16 @@ int rfast_grad_norm(int32_t n_tensors, int32_t grad_type, const int64_t* numel, 
  *     v  = beta2 v + (1 - beta2) g'^2
  *     p  = p (1 - lr weight_decay) - lr m / (1 - beta1^t) / (sqrt(v / (1 - beta2^t)) + eps)
  * in 32 bits; p is rounded once to its type.
- * state_bits = 32: m and v are fp32.
+ * state_bits = 32: m and v are fp32; v, the square, is infinite where it leaves fp32, and below 2^-126 it counts as zero.
  * state_bits = 8:  m holds e4m3 codes of the first moment, v e4m3 codes of sqrt(v) (half the range in
  *   octaves, so that its small values keep their digits), one byte per value.  A block is RFAST_ADAMW_BLOCK
  *   consecutive values of a tensor, the last one shorter; its scale is max(largest magnitude / 448, 2^-100)
  *   in fp32, m_scale and v_scale hold ceil(numel / RFAST_ADAMW_BLOCK) of them per tensor, and a
  *   value is code * scale.  Codes are nearest values, ties to even; a positive sqrt(v) keeps at least the
- *   smallest positive code, so that no first moment meets a denominator of eps alone (second moments
- *   below 2^-126 count as zero).  All bytes zero are moments of zero.  A NaN or infinite gradient leaves
- *   its whole block's moments NaN or infinite.
+ *   smallest positive code, so that no first moment meets a denominator of eps alone.  The root itself is formed,
+ *   never its square: finite gradients of any size leave finite moments, and roots down to 2^-149 count.  All
+ *   bytes zero are moments of zero.  A NaN or infinite gradient leaves its whole block's moments NaN or
+ *   infinite.
  * Tensors may not overlap one another.  Addresses need to be aligned to their type only; tensors whose
  * addresses are all multiples of 16 bytes are the fast ones.  A *d_step below 1 is not seen by the call: it
  * leaves NaN or infinite parameters. */

@@ -98,6 +98,7 @@ __device__ __forceinline__ float warp_max_nan(float v) {
 __device__ __forceinline__ float block_scale(float top) {
     return max_nan(__fmul_rn(top, (float)(1.0 / 448.0)), 7.888609052210118e-31f);   // 2^-100
 }
+constexpr float kLeastNormal = 0x1p-126f, kMostFinite = 0x1.fffffep127f;
 // 1 ulp; below the least normal number 0
 __device__ __forceinline__ float root_of(float v) {
     float r;
@@ -162,13 +163,46 @@ __device__ __forceinline__ void first_moments8(const StepFactors& f, float sm, f
         m[k + 1] = __fadd_rn(a[1], b[1]);
     }
 }
-__device__ __forceinline__ void advance8(const StepFactors& f, float sm, float sv, float (&p)[8], float (&g)[8], float (&m)[8], float (&v)[8]) {
+// Roots and parameters where the second moments may leave the range of fp32: q and h are brought near 1 by a power of two first, and
+// so are numerator and denominator of the quotient where the root is large.  Any finite gradient then has a finite root, and any
+// gradient but 0 (down to where its product with sqrt(1 - beta2) is 0) a positive one.  g: scaled
+__device__ __forceinline__ void finish8_far(const StepFactors& f, float bv, float (&p)[8], const float (&g)[8], const float (&m)[8], float (&v)[8]) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const float q = bv * v[k], h = f.g2 * g[k], top = fmaxf(fabsf(q), fabsf(h));
+        const bool high = top > 0x1p60f, low = top < 0x1p-60f;
+        const float in = high ? 0x1p-70f : low ? 0x1p100f : 1.f, out = high ? 0x1p70f : low ? 0x1p-100f : 1.f;
+        const float a = q * in, b = h * in, r = root_of(fmaf(a, a, b * b)), near = high ? in : 1.f;
+        v[k] = r * out;
+        p[k] = fmaf(-f.step, m[k] * near * inverse_of(fmaf(high ? r : v[k], f.root, f.eps * near)), p[k] * f.keep);
+    }
+}
+// The roots q of before reach from 2^-109 to 2^128, and a gradient may be any fp32 value, so that q^2 + h^2 can leave fp32's range
+// where its root does not.  Lanes with such a value take the way above.  again(q): what came in v
+template <class Again>
+__device__ __forceinline__ void advance8(const StepFactors& f, float sm, float sv, float (&p)[8], float (&g)[8], float (&m)[8], float (&v)[8], Again again) {
     const float bv = sv * f.b2;
     first_moments8(f, sm, g, m);
 #pragma unroll
     for (int k = 0; k < 8; k += 2) {
         const F2 q = pair(v[k], v[k + 1]) * both(bv), h = pair(g[k], g[k + 1]) * both(f.g2);
         split(fma2(q, q, h * h), v[k], v[k + 1]);
+    }
+    float least = v[0], most = v[0];
+#pragma unroll
+    for (int k = 1; k < 8; ++k) { least = fminf(least, v[k]); most = fmaxf(most, v[k]); }
+    if (!(least >= kLeastNormal && most <= kMostFinite)) {
+        float q[8];
+        again(q);                                           // decoded once more rather than kept
+        bool far = most > kMostFinite;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) far = far || (v[k] < kLeastNormal && fabsf(bv * q[k]) + fabsf(f.g2 * g[k]) > 0.f);      // not 0, exactly
+        if (far) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = q[k];
+            finish8_far(f, bv, p, g, m, v);
+            return;
+        }
     }
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
@@ -229,7 +263,7 @@ __device__ __forceinline__ void finish(const RawBlock<PT, GT, MT>& r, const Tens
             unpack4(r.v[k], (const float*)nullptr, v + 4 * k);
         }
     }
-    if constexpr (S8) advance8(f, r.sm, r.sv, p, g, m, v);
+    if constexpr (S8) advance8(f, r.sm, r.sv, p, g, m, v, [&](float (&q)[8]) { decode4(r.v[0], q); decode4(r.v[1], q + 4); });
     else advance(f, p, g, m, v);
 #pragma unroll
     for (int k = 0; k < 2; ++k) store4((PT*)t.p + i + k * 128, p + 4 * k);
@@ -273,8 +307,12 @@ __device__ __forceinline__ void block_by_values(const TensorView& t, const StepF
             v[k] = in ? ((const float*)t.v)[j] : 0.f;
         }
     }
-    if constexpr (S8) advance8(f, t.ms[b], t.vs[b], p, g, m, v);
-    else advance(f, p, g, m, v);
+    if constexpr (S8) {
+        first_moments8(f, t.ms[b], g, m);
+        finish8_far(f, t.vs[b] * f.b2, p, g, m, v);         // right at any size
+    } else {
+        advance(f, p, g, m, v);
+    }
     float sm, sv, cm[8], cv[8];
     if constexpr (S8) to_codes(m, v, sm, sv, cm, cv);
 #pragma unroll

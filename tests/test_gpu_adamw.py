@@ -431,3 +431,48 @@ def test_first_moments_codes_are_those_of_the_formula_in_32_bits(rfast_lib, lead
     torch.cuda.synchronize()
     assert torch.equal(ms, top)
     assert int((m[lead:] != code).sum()) == 0
+
+
+@pytest.mark.parametrize("grad", ["f32", "bf16"])
+@pytest.mark.parametrize("lead", [0, 1], ids=["aligned", "odd"])
+@pytest.mark.parametrize("low,high", [(-36, -36), (-30, -30), (-25, -25), (-21, -21), (-18, -18), (17, 17), (22, 22), (30, 30), (37.9, 37.9), (-36, 37)])
+def test_roots_of_8_bit_moments_reach_as_far_as_fp32(rfast_lib, monkeypatch, low, high, lead, grad):
+    """Gradients of any finite size, alike or mixed in one block: their squares leave fp32, their roots do not.  With the least eps
+    a first moment meets its root or nothing.  The tolerances are those of the other sizes: scaling by powers of two rounds nothing,
+    and no root here is below 2^-126."""
+    torch, _ = _torch()
+    monkeypatch.setitem(globals(), "EPS", 2.0 ** -126)
+    n = 256 * 5 + 100
+    rng = np.random.default_rng(int(10 * low) + 1000)
+    g = [10.0 ** rng.uniform(low, high, n) * rng.uniform(0.5, 1, n) * rng.choice([-1, 1], n) for _ in range(3)]
+    for k in range(3):
+        g[k][rng.random(n) < 0.1] = 0
+        g[k][512:768] = 0                                    # a block that sees nothing
+    c = {"p": _Buf([rng.standard_normal(n)], torch.float32, lead), "g": _Buf([g[0]], _torch()[1][grad], lead),
+         "m": _Buf([np.zeros(n, np.uint8)], torch.uint8, lead), "v": _Buf([np.zeros(n, np.uint8)], torch.uint8, lead),
+         "ms": _Buf([np.zeros(6)], torch.float32, lead), "vs": _Buf([np.zeros(6)], torch.float32, lead)}
+    for step in (1, 2, 3):
+        c["g"].t[c["g"].at[0]:c["g"].at[0] + n] = torch.as_tensor(g[step - 1]).to(c["g"].t.dtype).cuda()
+        before = (c["p"].get(0), c["g"].get(0), _moments(c, 0, 8, n))
+        assert np.isfinite(before[1]).all()
+        _step(c, "f32", grad, 8, step)
+        torch.cuda.synchronize()
+        assert all(np.isfinite(c[k].get(0)).all() for k in ("p", "ms", "vs"))
+        _check(before, c, 0, "f32", 8, step, 1.0)
+    assert all(b.canaries_stand() for b in c.values())
+
+
+def test_an_infinite_gradient_takes_its_whole_block(rfast_lib):
+    """Every moment of the block is infinite or NaN afterwards, those of the other blocks are as without it."""
+    torch, _ = _torch()
+    n = 256 * 3
+    plain, hurt = (_case([n], "f32", "f32", 8, 0, seed=14) for _ in range(2))
+    hurt["g"].t[hurt["g"].at[0] + 300] = math.inf
+    for c in (plain, hurt):
+        _step(c, "f32", "f32", 8, 3)
+    torch.cuda.synchronize()
+    inside = np.arange(n) // 256 == 1
+    for k in ("m", "v"):
+        assert np.array_equal(plain[k].get(0)[~inside], hurt[k].get(0)[~inside])
+        with np.errstate(invalid="ignore"):
+            assert not np.isfinite(_values8(hurt[k].get(0), hurt[k + "s"].get(0), n)[inside]).any()
