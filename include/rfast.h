@@ -502,7 +502,8 @@ int rfast_grad_norm(int32_t n_tensors, int32_t grad_type, const int64_t* numel, 
  *     v  = beta2 v + (1 - beta2) g'^2
  *     p  = p (1 - lr weight_decay) - lr m / (1 - beta1^t) / (sqrt(v / (1 - beta2^t)) + eps)
  * in 32 bits; p is rounded once to its type.
- * state_bits = 32: m and v are fp32; v, the square, is infinite where it leaves fp32, and below 2^-126 it counts as zero.
+ * state_bits = 32: m and v are fp32.  v is a square: (1 - beta2) g'^2 beyond 2^128 leaves this value's v infinite, and
+ *   below 2^-149 it is zero, so that the first moment meets eps alone.
  * state_bits = 8:  m holds e4m3 codes of the first moment, v e4m3 codes of sqrt(v) (half the range in
  *   octaves, so that its small values keep their digits), one byte per value.  A block is RFAST_ADAMW_BLOCK
  *   consecutive values of a tensor, the last one shorter; its scale is max(largest magnitude / 448, 2^-100)

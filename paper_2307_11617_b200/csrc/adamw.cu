@@ -105,6 +105,12 @@ __device__ __forceinline__ float root_of(float v) {
     asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
     return r;
 }
+// 1 ulp, down to the least number of all: 32-bit second moments are held that far
+__device__ __forceinline__ float root_of_any(float v) {
+    float r;
+    asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
 // 1 ulp; the denominators are at least eps, a normal number
 __device__ __forceinline__ float inverse_of(float v) {
     float r;
@@ -141,7 +147,7 @@ __device__ __forceinline__ void advance(const StepFactors& f, float (&p)[8], con
         const float h = f.g2 * g[k];
         m[k] = fmaf(f.g1, g[k], f.b1 * m[k]);
         v[k] = fmaf(f.b2, v[k], h * h);
-        const float r = root_of(v[k]);
+        const float r = root_of_any(v[k]);
         p[k] = fmaf(-f.step, m[k] * inverse_of(fmaf(r, f.root, f.eps)), p[k] * f.keep);
     }
 }

@@ -476,3 +476,28 @@ def test_an_infinite_gradient_takes_its_whole_block(rfast_lib):
         assert np.array_equal(plain[k].get(0)[~inside], hurt[k].get(0)[~inside])
         with np.errstate(invalid="ignore"):
             assert not np.isfinite(_values8(hurt[k].get(0), hurt[k + "s"].get(0), n)[inside]).any()
+
+
+@pytest.mark.parametrize("lead", [0, 1], ids=["aligned", "odd"])
+@pytest.mark.parametrize("size", [1e-17, 1e-18, 1e-19, 1e-20])
+def test_small_second_moments_of_32_bits_count(rfast_lib, size, lead):
+    """Second moments below 2^-126, with an eps far below their roots: the quotient is that of the roots, not m / eps.
+    A square down there is held to half of 2^-149, its product with 1 - beta2 and the sum each: 2^-149 in all, which the root halves
+    relative to itself; the rest of the quotient is off by 16 u as elsewhere."""
+    torch, _ = _torch()
+    import paper_2307_11617_b200 as pkg
+    n, eps = 256 * 3 + 10, 2.0 ** -126
+    rng = np.random.default_rng(9)
+    g = size * rng.uniform(0.5, 1, n) * rng.choice([-1, 1], n)
+    c = {"p": _Buf([rng.standard_normal(n)], torch.float32, lead), "g": _Buf([g], torch.float32, lead),
+         "m": _Buf([np.zeros(n)], torch.float32, lead), "v": _Buf([np.zeros(n)], torch.float32, lead)}
+    for step in (1, 2, 3):
+        p, m, v, gg = (c[k].get(0) for k in ("p", "m", "v", "g"))
+        pkg.rfast_adamw_step(*[c[k].addresses() for k in ("p", "g", "m", "v")], [n], step=step, lr=LR, beta1=B1, beta2=B2, eps=eps, weight_decay=WD)
+        torch.cuda.synchronize()
+        m1, v1 = B1 * m + (1 - B1) * gg, B2 * v + (1 - B2) * gg * gg
+        q = LR / (1 - B1 ** step) * m1 / (np.sqrt(v1) / math.sqrt(1 - B2 ** step) + eps)
+        tol = np.abs(q) * (2.0 ** -149 / (2 * v1) * 1.01 + 16 * U) + LR / (1 - B1 ** step) * (5 * U * (np.abs(B1 * m) + np.abs((1 - B1) * gg))) / np.sqrt(v1)
+        tol += 3 * U * np.abs(p) + U * np.abs(p)
+        assert v1.max() < 2.0 ** -100 and np.all(np.abs(c["v"].get(0) - v1) <= 8 * U * v1 + 2.0 ** -149)
+        assert np.all(np.abs(c["p"].get(0) - (p * (1 - LR * WD) - q)) <= tol)
