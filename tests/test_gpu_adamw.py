@@ -501,3 +501,39 @@ def test_small_second_moments_of_32_bits_count(rfast_lib, size, lead):
         tol += 3 * U * np.abs(p) + U * np.abs(p)
         assert v1.max() < 2.0 ** -100 and np.all(np.abs(c["v"].get(0) - v1) <= 8 * U * v1 + 2.0 ** -149)
         assert np.all(np.abs(c["p"].get(0) - (p * (1 - LR * WD) - q)) <= tol)
+
+
+@pytest.mark.parametrize("step", [1, 2, 3, 100, 10 ** 6])
+@pytest.mark.parametrize("bits", [32, 8])
+def test_step_count_on_the_device_enters_the_parameters(rfast_lib, bits, step):
+    """The count that d_step points to forms both bias corrections: parameters and moments against 64 bits, beside a host count that
+    must not be read."""
+    torch, _ = _torch()
+    c = _case(SIZES["edges"], "f32", "f32", bits, 0, seed=21)
+    before = [(c["p"].get(k), c["g"].get(k), _moments(c, k, bits, n)) for k, n in enumerate(SIZES["edges"])]
+    count = torch.tensor([step], dtype=torch.int64, device="cuda")
+    _step(c, "f32", "f32", bits, step=7, d_step=count.data_ptr())
+    torch.cuda.synchronize()
+    for k, n in enumerate(SIZES["edges"]):
+        if n:
+            _check(before[k], c, k, "f32", bits, step, 1.0)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_recorded_count_moves_the_parameters_as_the_hosts(rfast_lib, bits):
+    """A recorded step with its count on the device, replayed, against 64 bits at every step."""
+    torch, _ = _torch()
+    c = _case(SIZES["long"], "f32", "f32", bits, 0, seed=22)
+    count = torch.zeros(1, dtype=torch.int64, device="cuda")
+    stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=stream):
+        count.add_(1)
+        _step(c, "f32", "f32", bits, d_step=count.data_ptr(), stream=stream.cuda_stream)
+    for step in (1, 2, 3, 4):
+        before = [(c["p"].get(k), c["g"].get(k), _moments(c, k, bits, n)) for k, n in enumerate(SIZES["long"])]
+        graph.replay()
+        torch.cuda.synchronize()
+        assert int(count) == step
+        for k in range(len(before)):
+            _check(before[k], c, k, "f32", bits, step, 1.0)
