@@ -127,16 +127,21 @@ __device__ __forceinline__ void copies_wait(int left) {
 
 template <int LEFT> __device__ __forceinline__ void copies_pending() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
 
-// 1 / (1 + exp(-u)) of a pair.  2^t and the reciprocal are the hardware's (2 ulp and 1 ulp), t and the products are rounded
-// once each: the result is good to about 2^-22.  The special function unit, with a result every other cycle where the
-// adders have eight, is what bounds a pass with this in it, so one reciprocal, of the product of both denominators, serves
-// two values (3 instead of 4 of its operations per pair).  To keep the product in range exp(-u) stops growing at 2^60: below
-// u = -41 the result is 2^-60.  A NaN gives 2^-60 as well: it must not reach its neighbour through the product, and the caller
-// multiplies by u.  e: exp(-u)
-__device__ __forceinline__ F2 sigmoid2(F2 u, F2& e) {
+// 1 / (1 + exp(-u)) of a pair.  2^t and the reciprocal are the hardware's (2 ulp and 1 ulp), t = -u log2(e) carries the roundings of
+// the constant and of the product, and the products after it one each: the result is good to 2^-22 + |u| 2^-23.  The special
+// function unit, with a result every other cycle where the adders have eight, is what bounds a pass with this in it, so one
+// reciprocal, of the product of both denominators, serves two values (3 instead of 4 of its operations per pair).  To keep the
+// product in range exp(-u) stops growing at 2^60, below u = -41.6.  u comes back bounded there as well: u / (1 + exp(-u)) and the
+// slope are then between -4e-17 and 0 however far u is, and not u 2^-60.  A NaN gives 2^-60: it must not reach its neighbour
+// through the product, and the caller multiplies by u, in which it stays.  e: exp(-u)
+__device__ __forceinline__ F2 sigmoid2(F2& u, F2& e) {
     float a, b;
+    split(u, a, b);
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(a) : "f"(-41.58883f));
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(b) : "f"(-41.58883f));
+    u = pair(a, b);
     split(u * both(-1.4426950408889634f), a, b);
-    asm("min.f32 %0, %0, %1;" : "+f"(a) : "f"(60.f));
+    asm("min.f32 %0, %0, %1;" : "+f"(a) : "f"(60.f));        // a NaN's
     asm("min.f32 %0, %0, %1;" : "+f"(b) : "f"(60.f));
     asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(a));
     asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(b));
@@ -146,7 +151,7 @@ __device__ __forceinline__ F2 sigmoid2(F2 u, F2& e) {
     asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(r));
     return pair(b, a) * both(r);
 }
-__device__ __forceinline__ F2 silu2(F2 u) { F2 e; return u * sigmoid2(u, e); }
+__device__ __forceinline__ F2 silu2(F2 u) { F2 e; const F2 q = sigmoid2(u, e); return u * q; }
 
 // cnt rows of a thread out of shared memory, R at a time: all loads of a batch go out before the first row is worked on.
 template <int R, class Row, class Load, class Use>

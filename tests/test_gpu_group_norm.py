@@ -431,3 +431,41 @@ def test_no_positions_and_foreign_addresses(rfast_lib):
     with pytest.raises(RFastError) as ei:
         pkg.rfast_group_norm(d, host.ctypes.data, d, d, d, d, samples=2, positions=3, channels=12, groups=3)
     assert ei.value.code == EINVAL and "gamma: not device memory" in str(ei.value)
+
+
+@pytest.mark.parametrize("shift", [-1e3, -1e12, -1e20, -3e38])
+@pytest.mark.parametrize("shape,kind", [("one channel a group", "f32"), ("ten a group", "f16"), ("hidden layer", "f32"), ("hidden layer", "bf16"),
+                                        ("hidden layer, wide groups", "f32"), ("long", "bf16"), ("seventeen positions", "f32"), ("wide odd group", "f16")])
+def test_values_far_below_zero_vanish(rfast_lib, shape, kind, shift):
+    """u / (1 + exp(-u)) and its slope go to 0 on the left, however far u is: a channel whose shift says "off" adds nothing."""
+    torch, _ = _torch()
+    c = _Case(SHAPES[shape], kind, seed=18)
+    ch = c.c // 2
+    c.beta[:, ch] = -100.0
+    near = c.forward("silu")
+    near_back = c.backward("silu", near[1], near[2])
+    c.beta[:, ch] = shift
+    far = c.forward("silu")
+    far_back = c.backward("silu", near[1], near[2])
+    # exp(41) = 6e17: the values are of 41.6 / (1 + exp(41.6)) = 3.6e-17 at most, their slopes likewise
+    y = _np(far[0])[:, :, ch]
+    assert np.all((y <= 0) & (y >= -4e-17))
+    for got, by in ((far_back[1], _np(c.dy) * 10), (far_back[2], _np(c.dy))):
+        assert np.all(np.abs(_np(got)[:, ch]) <= 4e-17 * np.abs(by[:, :, ch]).sum())
+    assert all(torch.equal(a, b) for a, b in zip((*near, *near_back), (*far, *far_back)))
+
+
+@pytest.mark.parametrize("shape,kind", [("ten a group", "f32"), ("hidden layer", "bf16"), ("long", "f32"), ("seventeen positions", "f16")])
+def test_huge_scales_keep_the_sign(rfast_lib, shape, kind):
+    """With a scale of 1e30 a value before the activation is far to the right or far to the left: y is itself, or nothing."""
+    c = _Case(SHAPES[shape], kind, seed=19)
+    c.gamma[:] = 1e30
+    c.beta[:] = 0
+    y, mean, rstd = (_np(t) for t in c.forward("silu"))
+    h = ((_np(c.x).reshape(c.n, c.s, c.g, -1) - mean[:, None, :, None]) * rstd[:, None, :, None]).reshape(c.n, c.s, c.c)
+    off = h < -1e-3
+    assert off.any() and np.all(np.abs(y[off]) <= 4e-17)
+    on = h > 1e-3
+    with np.errstate(over="ignore"):
+        want = h[on] * 1e30
+    assert np.all(y[on] == np.inf) if kind == "f16" else np.allclose(y[on], want, rtol=1e-2)
