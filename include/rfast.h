@@ -372,12 +372,13 @@ int rfast_snapshot_wait(rfast_ctx* ctx);
 int rfast_sync(rfast_ctx* ctx);
 
 /* Checkpoint / resume.  The blob holds the complete device state of the handle -- x, the
- * trackers, the remembered gradients, every live packet version (published v and running sums
- * rho, i.e. also the packets still in flight) and the round counter -- so that
+ * trackers, the remembered gradients, the moments of RFAST_DESCENT_ADAMW*, every live packet version (published
+ * v and running sums rho, i.e. also the packets still in flight) and the round counter -- so that
  *     create + load_schedule(same schedule) + checkpoint_load + run(K - r)
  * continues bit for bit where  run(r) + checkpoint_save  stopped.  The blob is opaque and tied
- * to the problem's shape and to the loaded schedule (a hash of its arrays is checked);
- * RFAST_ESTATE if no schedule is loaded, RFAST_EINVAL on a size or identity mismatch.
+ * to the problem's shape, to the loaded schedule (a hash of its arrays is checked) and, where there are any, to
+ * the descent and its betas and to norm_groups, norm_act and norm_eps; RFAST_ESTATE if no schedule is loaded,
+ * RFAST_EINVAL on a size or identity mismatch.
  * dst / src are caller-owned HOST buffers of rfast_checkpoint_size() bytes. */
 int64_t rfast_checkpoint_size(rfast_ctx* ctx);
 int     rfast_checkpoint_save(rfast_ctx* ctx, void* dst, size_t bytes);

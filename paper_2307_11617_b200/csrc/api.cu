@@ -1603,6 +1603,17 @@ CkptHeader make_header(rfast_ctx* c) {
     h.n = c->n; h.model = c->model; h.compensated = c->compensated + (c->rho2 ? 1 : 0); h.K = c->comp.K;
     h.n_v_slots = c->comp.n_v_slots; h.n_rho_slots = c->comp.n_rho_slots; h.round = c->round;
     h.pad = (c->buckets ? 1 : 0) | c->descent << 1 | c->norm_groups << 3;
+    // What the stored moments and remembered gradients were formed with.  Rates, eps and decay enter steps to come only and may
+    // change, as alpha may.
+    auto mix = [&](double v) {
+        uint64_t w;
+        v += 0.0;                                           // -0 is 0
+        std::memcpy(&w, &v, 8);
+        h.sched_hash = (h.sched_hash ^ w) * 0x9E3779B97F4A7C15ull;
+        h.sched_hash ^= h.sched_hash >> 29;
+    };
+    if (c->descent != RFAST_DESCENT_PLAIN) { mix(c->beta1); mix(c->beta2); }
+    if (c->norm_groups > 0) { mix(c->norm_act); mix(c->norm_eps); }
     return h;
 }
 

@@ -220,3 +220,35 @@ def test_normalised_mlp_trajectory_and_objective(rfast_lib, ov):
     xbar = x.astype(np.float64).mean(axis=0)
     want = sum(m.loss(i, xbar.astype(np.float32).astype(np.float64), np.arange(wl.rows)) for i in range(wl.n))
     assert abs(d["objective"] - want) <= 1e-4 * abs(want)
+
+
+def test_checkpoints_of_other_moments_or_layers_are_refused(rfast_lib):
+    """Moments formed with other betas, or gradients of another hidden layer, are not taken for one's own; a rate, an eps or a decay may change."""
+    import paper_2307_11617_b200 as pkg
+    from paper_2307_11617_b200 import binding as B
+    wl = _build("mlp norm", "adamw")
+    with pkg.Engine(wl) as eng:
+        eng.load_schedule(wl.schedule)
+        eng.run(4)
+        blob = eng.checkpoint()
+
+    def restored(**more):
+        descent = {"kind": "adamw", **ADAM, **more.pop("descent", {})}
+        other = _build("mlp norm", "adamw", descent=descent, **{k: v for k, v in more.items() if k != "norm_eps"})
+        if "norm_eps" in more:
+            other.dims["norm_eps"] = more["norm_eps"]
+        with pkg.Engine(other) as eng:
+            eng.load_schedule(other.schedule)
+            x = eng.read(B.STATE_X)
+            try:
+                eng.restore(blob)
+            except pkg.RFastError as e:
+                assert e.code == B.EINVAL and np.array_equal(x, eng.read(B.STATE_X))
+                return False
+            return True
+
+    assert restored()
+    assert restored(alpha=0.001) and restored(descent={"eps": 1e-4}) and restored(descent={"weight_decay": 0.0})
+    for other in ({"norm_act": "relu"}, {"norm_eps": 1e-3}, {"norm_groups": 4}, {"descent": {"beta1": 0.8}}, {"descent": {"beta2": 0.999}},
+                  {"descent": {"kind": "adamw8"}}, {"descent": {"kind": "plain"}}):
+        assert not restored(**other), other
