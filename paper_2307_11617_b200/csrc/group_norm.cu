@@ -1624,6 +1624,11 @@ bool overlaps(const GnShape& s, int64_t sn, int64_t ss) {
     return outer > 1 && far < (inner - 1) * near + s.C;
 }
 
+// Whether a result lies where an operand does, but in other strides: values would be overwritten before they are read.
+bool torn(const GnShape& s, const void* out, int64_t on, int64_t os, const void* in, int64_t sn, int64_t ss) {
+    return out == in && ((s.N > 1 && on != sn) || (s.S > 1 && os != ss));
+}
+
 }  // namespace
 
 // Partial sums of the channels: as many rows as a set's samples at most.
@@ -1677,6 +1682,7 @@ extern "C" int rfast_group_norm(const rfast_gn_shape* g, const void* d_x, const 
     GN_TRY(strides_of(y_strides, a.s, &a.on, &a.os, me, "y", err, err_len));
     if (a.s.N == 0 || a.s.S == 0) return RFAST_OK;
     if (overlaps(a.s, a.on, a.os)) return op_fail(err, err_len, RFAST_EINVAL, "%s: the strides of y make it overlap itself", me);
+    if (torn(a.s, d_y, a.on, a.os, d_x, a.xn, a.xs)) return op_fail(err, err_len, RFAST_EINVAL, "%s: y is x, but with other strides", me);
     const void* ptrs[] = {d_x, d_gamma, d_beta, d_y, d_mean, d_rstd};
     const char* names[] = {"x", "gamma", "beta", "y", "mean", "rstd"};
     const int es = type_bytes(g->type);
@@ -1710,6 +1716,8 @@ extern "C" int rfast_group_norm_backward(const rfast_gn_shape* g, const void* d_
     if (a.s.N == 0) return RFAST_OK;                        // no sets either
     const int64_t sets = a.s.N / a.s.per_set;
     if (a.s.S > 0 && overlaps(a.s, a.on, a.os)) return op_fail(err, err_len, RFAST_EINVAL, "%s: the strides of dx make it overlap itself", me);
+    if (torn(a.s, d_dx, a.on, a.os, d_x, a.xn, a.xs) || torn(a.s, d_dx, a.on, a.os, d_dy, a.dn, a.ds))
+        return op_fail(err, err_len, RFAST_EINVAL, "%s: dx is x or dy, but with other strides", me);
     const void* ptrs[] = {d_dgamma, d_dbeta, d_gamma, d_beta, d_mean, d_rstd, d_dy, d_x, d_dx};
     const char* names[] = {"dgamma", "dbeta", "gamma", "beta", "mean", "rstd", "dy", "x", "dx"};
     const int es = type_bytes(g->type);

@@ -272,3 +272,25 @@ def test_oracle_adamw_step_is_the_definition():
                 m, s = mq, sq
             assert np.allclose(orc.m[0], m, rtol=1e-12) and np.allclose(orc.s[0], s, rtol=1e-12)      # roundings of 64 bits
             m, s = orc.m[0], orc.s[0]
+
+
+@pytest.mark.parametrize("kw", [dict(x_strides=(72, 16)), dict(y_strides=(80, 12)), dict(x_strides=(0, 12)), dict(x_strides=(12, 48)), dict(positions=1, y_strides=(16, 12)),
+                                dict(samples=1, x_strides=(72, 0))])
+def test_results_in_place_want_the_operands_strides(rfast_lib, kw):
+    """y may be x, dx may be x or dy, in the same strides; in others a value would be overwritten before it is read."""
+    import paper_2307_11617_b200 as pkg
+    _refused("y is x", pkg.rfast_group_norm, **{**dict(x=A, gamma=A, beta=A, y=A, mean=A, rstd=A), **SHAPE, **kw})
+    back = {{"y_strides": "dx_strides"}.get(k, k): v for k, v in kw.items()}
+    base = dict(dy=A + 4096, x=A, gamma=A, beta=A, mean=A, rstd=A, dx=A, dgamma=A, dbeta=A, workspace=A, workspace_bytes=1 << 30)
+    _refused("dx is x or dy", pkg.rfast_group_norm_backward, **{**base, **SHAPE, **back})
+    back = {{"x_strides": "dy_strides"}.get(k, k): v for k, v in back.items()}
+    _refused("dx is x or dy", pkg.rfast_group_norm_backward, **{**base, "dy": A, "x": A + 4096, **SHAPE, **back})
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(x_strides=(72, 12)), dict(samples=1, x_strides=(5, 12)), dict(positions=1, x_strides=(12, 7))])
+def test_results_in_place_with_the_operands_strides_pass(rfast_lib, kw):
+    """Equal strides, and unlike ones along a dimension of one, go on to the next check."""
+    import paper_2307_11617_b200 as pkg
+    _refused("rstd is null", pkg.rfast_group_norm, **{**dict(x=A, gamma=A, beta=A, y=A, mean=A, rstd=0), **SHAPE, **kw})
+    base = dict(dy=A, x=A, gamma=A, beta=A, mean=A, rstd=0, dx=A, dgamma=A, dbeta=A, workspace=A, workspace_bytes=1 << 30)
+    _refused("rstd is null", pkg.rfast_group_norm_backward, **{**base, **SHAPE, **kw})
