@@ -552,7 +552,7 @@ int rfast_adamw_step(const rfast_adamw* a, void* cuda_stream, char* err, size_t 
  * Strides are those of a sample and of a position, in elements (two numbers; NULL: contiguous);
  * channels are neighbours.  Read operands may overlap themselves (a stride of 0 repeats), written
  * ones may not; y may be x, dx may be x or dy, with the same strides (others are refused).  Addresses and strides in
- * multiples of 16 bytes are the fast ones; no other operands may overlap.  A group may have 8192
+ * multiples of 16 bytes are the fast ones; an operand spans 2^56 elements at most; no other operands may overlap.  A group may have 8192
  * channels at most, there may be 2^24 channels, and 65535 runs of neighbouring groups that are at
  * least 128 bytes wide each.
  *

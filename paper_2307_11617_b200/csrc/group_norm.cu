@@ -1604,6 +1604,9 @@ int strides_of(const int64_t* given, const GnShape& s, int64_t* sn, int64_t* ss,
     *ss = given ? given[1] : s.C;
     *sn = given ? given[0] : (int64_t)s.C * s.S;
     if (*sn < 0 || *ss < 0) return op_fail(err, err_len, RFAST_EINVAL, "%s: a stride of %s is negative", me, what);
+    // addresses have 57 bits at most; sums of offsets then stay far from 64
+    const __int128 reach = (__int128)(s.N > 0 ? s.N - 1 : 0) * *sn + (__int128)(s.S > 0 ? s.S - 1 : 0) * *ss + s.C;
+    if (reach > ((__int128)1 << 56)) return op_fail(err, err_len, RFAST_EINVAL, "%s: the strides of %s reach beyond any memory", me, what);
     return RFAST_OK;
 }
 

@@ -294,3 +294,15 @@ def test_results_in_place_with_the_operands_strides_pass(rfast_lib, kw):
     _refused("rstd is null", pkg.rfast_group_norm, **{**dict(x=A, gamma=A, beta=A, y=A, mean=A, rstd=0), **SHAPE, **kw})
     base = dict(dy=A, x=A, gamma=A, beta=A, mean=A, rstd=0, dx=A, dgamma=A, dbeta=A, workspace=A, workspace_bytes=1 << 30)
     _refused("rstd is null", pkg.rfast_group_norm_backward, **{**base, **SHAPE, **kw})
+
+
+@pytest.mark.parametrize("strides", [(1 << 62, 1 << 62), (0, 1 << 61), (1 << 61, 12), (12, (1 << 63) - 1)])
+def test_strides_beyond_any_memory_are_refused(rfast_lib, strides):
+    """Offsets that leave 64 bits wrap round to small ones: the host must not take them for rows that lie apart."""
+    import paper_2307_11617_b200 as pkg
+    for which in ("x", "y"):
+        _refused(f"strides of {which} reach beyond", pkg.rfast_group_norm,
+                 **{**dict(x=A, gamma=A, beta=A, y=2 * A, mean=A, rstd=0), **SHAPE, f"{which}_strides": strides})
+    base = dict(dy=A, x=2 * A, gamma=A, beta=A, mean=A, rstd=0, dx=3 * A, dgamma=A, dbeta=A, workspace=A, workspace_bytes=1 << 30)
+    for which in ("x", "dy", "dx"):
+        _refused(f"strides of {which} reach beyond", pkg.rfast_group_norm_backward, **{**base, **SHAPE, f"{which}_strides": strides})
