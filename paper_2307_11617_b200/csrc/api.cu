@@ -1572,6 +1572,7 @@ struct CkptHeader {
     int64_t  p, stride, n_events;
     int32_t  n, model, compensated, K, n_v_slots, n_rho_slots, round, pad;
 };
+constexpr size_t kDiagSmem = 220 * 1024;                 // dynamic shared memory of a block of the diagnostics
 constexpr uint64_t kCkptMagic = 0x5246415354434B31ull;   // "RFASTCK1"
 
 // the device buffers that make up the state, in blob order
@@ -1770,7 +1771,10 @@ int rfast_diagnostics(rfast_ctx* ctx, double* out, int32_t n_out) try {
     const bool sampled = want_mf && ctx->batch > 0 && ctx->rows % ctx->batch == 0 &&
                          (ctx->model == RFAST_MODEL_SOFTMAX || ctx->model == RFAST_MODEL_MLP || ctx->model == RFAST_MODEL_LOGISTIC_SPARSE);
     const bool sampled_model = ctx->model == RFAST_MODEL_SOFTMAX || ctx->model == RFAST_MODEL_MLP || ctx->model == RFAST_MODEL_LOGISTIC_SPARSE;
-    const bool lossy = n_out == 8 && sampled_model && (ctx->model == RFAST_MODEL_LOGISTIC_SPARSE || ctx->C <= 32);
+    // a row's hidden layer in 64 bits is a warp's share of a block's 227 KB
+    const int mlp_warps = ctx->model == RFAST_MODEL_MLP ? (int)std::min<size_t>(8, kDiagSmem / (ctx->H * sizeof(double))) : 0;
+    const bool lossy = n_out == 8 && sampled_model && (ctx->model == RFAST_MODEL_LOGISTIC_SPARSE || ctx->C <= 32) &&
+                       (ctx->model != RFAST_MODEL_MLP || mlp_warps > 0);
     if (lossy && !ctx->d_diag_rowloss) CK(dev_alloc(ctx, &ctx->d_diag_rowloss, (size_t)n * ctx->rows, false));
     if ((sampled || lossy) && !ctx->d_xbar) {          // the mean iterate is wanted on the device
         CK(dev_alloc(ctx, &ctx->d_xbar, (size_t)ctx->stride, true));
@@ -1796,9 +1800,11 @@ int rfast_diagnostics(rfast_ctx* ctx, double* out, int32_t n_out) try {
         const dim3 grid((ctx->rows + 7) / 8, n);
         if (ctx->model == RFAST_MODEL_SOFTMAX)
             k_diag_loss_softmax<<<grid, 256, 0, ctx->stream>>>(ctx->feat, ctx->label, ctx->d_xbar, ctx->d_diag_rowloss, ctx->rows, ctx->F, ctx->C);
-        else if (ctx->model == RFAST_MODEL_MLP)
-            k_diag_loss_mlp<<<grid, 256, 8 * (size_t)ctx->H * sizeof(double), ctx->stream>>>(ctx->feat, ctx->label, ctx->d_xbar, ctx->d_diag_rowloss,
-                                                                                             ctx->rows, ctx->F, ctx->H, ctx->C, ctx->norm_groups, ctx->norm_act, ctx->norm_eps);
+        else if (ctx->model == RFAST_MODEL_MLP) {
+            CK(cudaFuncSetAttribute(k_diag_loss_mlp, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kDiagSmem));
+            k_diag_loss_mlp<<<dim3((ctx->rows + mlp_warps - 1) / mlp_warps, n), 32 * mlp_warps, mlp_warps * (size_t)ctx->H * sizeof(double), ctx->stream>>>(
+                ctx->feat, ctx->label, ctx->d_xbar, ctx->d_diag_rowloss, ctx->rows, ctx->F, ctx->H, ctx->C, ctx->norm_groups, ctx->norm_act, ctx->norm_eps);
+        }
         else
             k_diag_loss_logistic<<<grid, 256, 0, ctx->stream>>>(ctx->sp_ptr, ctx->sp_col, ctx->sp_val, ctx->label, ctx->d_xbar, ctx->d_diag_rowloss, ctx->rows);
         CK(cudaGetLastError());

@@ -945,14 +945,14 @@ k_diag_loss_logistic(const int64_t* __restrict__ sp_ptr, const int* __restrict__
     if (lane == 0) rowloss[r] = m > 0 ? log1p(exp(-m)) : -m + log1p(exp(m));
 }
 //   MLP: x = [W1 (H x F) | b1 (H) | W2 (C x H) | b2 (C)]; the operands of A W1^T rounded to bf16 (the
-//   matrix product the tensor cores take), everything else as it is; dynamic shared memory: 8 * H doubles.
+//   matrix product the tensor cores take), everything else as it is; a warp per row, dynamic shared memory: H doubles for each.
 //   groups > 0: x = [... | gamma (H) | beta (H)], group norm and activation in the place of relu
 __global__ void __launch_bounds__(256)
 k_diag_loss_mlp(const float* __restrict__ feat, const int* __restrict__ label, const float* __restrict__ xbar,
                 double* __restrict__ rowloss, int rows, int F, int H, int C, int groups, int act, double eps) {
     extern __shared__ double hs_all[];
     const int w = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int k = blockIdx.x * 8 + w;
+    const int k = blockIdx.x * (blockDim.x >> 5) + w;
     if (k >= rows) return;
     double* hs = hs_all + (size_t)w * H;
     const int64_t r = (int64_t)blockIdx.y * rows + k;

@@ -252,3 +252,23 @@ def test_checkpoints_of_other_moments_or_layers_are_refused(rfast_lib):
     for other in ({"norm_act": "relu"}, {"norm_eps": 1e-3}, {"norm_groups": 4}, {"descent": {"beta1": 0.8}}, {"descent": {"beta2": 0.999}},
                   {"descent": {"kind": "adamw8"}}, {"descent": {"kind": "plain"}}):
         assert not restored(**other), other
+
+
+WIDE = [dict(n=3, F=32, H=768, C=4, rows=64, K=4, batch=64), dict(n=3, F=32, H=1152, C=4, rows=72, K=4, batch=64),
+        dict(n=2, F=16, H=4096, C=3, rows=64, K=3, batch=64), dict(n=3, F=32, H=1152, C=4, rows=64, K=4, batch=64, norm_groups=6, norm_act="silu")]
+
+
+@pytest.mark.parametrize("ov", WIDE, ids=["H768", "H1152", "H4096", "H1152 G6"])
+def test_objective_of_wide_hidden_layers(rfast_lib, ov):
+    """More hidden units than eight rows of them fit 48 KB."""
+    import paper_2307_11617_b200 as pkg
+    from paper_2307_11617_b200 import binding as B
+    wl = build_config("mlp_tree64", seed=4, **ov)
+    m = make_model(wl)
+    with pkg.Engine(wl) as eng:
+        eng.load_schedule(wl.schedule)
+        eng.run()
+        x, d = eng.read(B.STATE_X), eng.diagnostics()
+    xbar = x.astype(np.float64).mean(axis=0).astype(np.float32).astype(np.float64)
+    want = sum(m.loss(i, xbar, np.arange(wl.rows)) for i in range(wl.n))
+    assert abs(d["objective"] - want) <= 1e-4 * abs(want)
