@@ -272,3 +272,17 @@ def test_objective_of_wide_hidden_layers(rfast_lib, ov):
     xbar = x.astype(np.float64).mean(axis=0).astype(np.float32).astype(np.float64)
     want = sum(m.loss(i, xbar, np.arange(wl.rows)) for i in range(wl.n))
     assert abs(d["objective"] - want) <= 1e-4 * abs(want)
+
+
+DIAG = [("mlp_tree64", dict(n=5, F=64, H=128, C=4, rows=128, K=12, batch=64, norm_groups=8, norm_act="silu")),
+        ("mlp_tree64", dict(n=4, F=32, H=256, C=3, rows=192, K=10, batch=64, norm_groups=1, norm_act="relu", l2=1e-2)),
+        ("mlp_tree64", dict(n=5, F=48, H=256, C=3, rows=128, K=12, batch=64, norm_groups=8, norm_act="none", alpha=0.003, descent={"kind": "adamw", **ADAM})),
+        ("softmax_exp16", dict(n=8, F=48, C=5, rows=64, K=30, batch=8, alpha=0.003, descent={"kind": "adamw", **ADAM}))]
+
+
+@pytest.mark.parametrize("name,ov", DIAG, ids=["silu", "relu l2", "none adamw", "softmax adamw"])
+def test_full_gradient_and_merit_of_the_options(rfast_lib, name, ov):
+    """Diagnostics in mid-run and at the end, full gradient and merit function among them, with a normalised layer and an adaptive
+    step: the checks of the plain problems."""
+    import test_gpu_aux
+    test_gpu_aux.test_diagnostics_match_the_oracle_state(rfast_lib, name, ov)
