@@ -514,6 +514,12 @@ int rfast_grad_norm(int32_t n_tensors, int32_t grad_type, const int64_t* numel, 
  *   never its square: finite gradients of any size leave finite moments, and roots down to 2^-149 count.  All
  *   bytes zero are moments of zero.  A NaN or infinite gradient leaves its whole block's moments NaN or
  *   infinite.
+ *   Nearest codes make the second moment a running average only while one step moves sqrt(v) by half a code, 2^-5 to
+ *   2^-4 of it.  Up to beta2 = 0.95 it follows the gradients within a factor of 1.7.  With beta2 = 0.99 or more a code
+ *   stays where it is unless |g'| is several times sqrt(v), and its value moves with the block's scale, that is with the
+ *   block's largest value: sqrt(v) is within a factor of 2 of the average's while gradients keep their size, but where
+ *   those of part of a block change tenfold, it can be wrong by that factor for thousands of steps.  Moments in 32 bits
+ *   have no such limit.  The first moment keeps the same rule: up to beta1 = 0.95 it follows within a tenth on average.
  * Tensors may not overlap one another.  Addresses need to be aligned to their type only; tensors whose
  * addresses are all multiples of 16 bytes are the fast ones.  A *d_step below 1 is not seen by the call: it
  * leaves NaN or infinite parameters. */

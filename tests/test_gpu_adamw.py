@@ -537,3 +537,41 @@ def test_recorded_count_moves_the_parameters_as_the_hosts(rfast_lib, bits):
         assert int(count) == step
         for k in range(len(before)):
             _check(before[k], c, k, "f32", bits, step, 1.0)
+
+
+@pytest.mark.parametrize("change", [1.0, 0.1, 10.0])
+@pytest.mark.parametrize("beta2", [0.9, 0.95, 0.99, 0.999])
+def test_8_bit_moments_beside_32_bit_ones_over_many_steps(rfast_lib, beta2, change):
+    """How far nearest codes follow the average, as the header states it: 2000 steps on four blocks, from step 500 on with half of every
+    block's gradients `change` times as large."""
+    import paper_2307_11617_b200 as pkg
+    torch, _ = _torch()
+    n, steps = 1024, 2000
+    torch.manual_seed(17)
+    factor = torch.ones(n, device="cuda")
+    factor[(torch.arange(n, device="cuda") % 256) < 128] = change
+    p, g = torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda")
+    q, m, v = (torch.zeros(n, device="cuda") for _ in range(3))
+    cm, cv = (torch.zeros(n, dtype=torch.uint8, device="cuda") for _ in range(2))
+    sm, sv = (torch.zeros(4, device="cuda") for _ in range(2))
+    a = lambda t: [t.data_ptr()]  # noqa: E731
+    stream = torch.cuda.current_stream().cuda_stream
+    steady, changed = [], []
+    for step in range(1, steps + 1):
+        g.copy_(torch.randn(n, device="cuda") * (factor if step > 500 else 1.0))
+        pkg.rfast_adamw_step(a(p), a(g), a(m), a(v), [n], step=step, beta2=beta2, cuda_stream=stream)
+        pkg.rfast_adamw_step(a(q), a(g), a(cm), a(cv), [n], step=step, beta2=beta2, m_scale=a(sm), v_scale=a(sv), cuda_stream=stream)
+        if step % 100 == 0:
+            torch.cuda.synchronize()
+            ratio = _values8(cv.cpu().numpy(), sv.cpu().numpy(), n) / np.sqrt(v.double().cpu().numpy())
+            (steady if step <= 500 or change == 1.0 else changed).append(ratio)
+            first = _values8(cm.cpu().numpy(), sm.cpu().numpy(), n)
+            assert np.abs(first - m.double().cpu().numpy()).mean() <= 0.1 * np.abs(m.double().cpu().numpy()).mean()
+    steady = np.array(steady)
+    assert np.median(steady) <= (1.2 if beta2 <= 0.95 else 1.6) and 0.5 <= steady.min() and steady.max() <= (1.6 if beta2 <= 0.95 else 2.2)
+    if changed:
+        late = np.array(changed[5:])                         # 500 steps and more after the change
+        if beta2 <= 0.95:
+            assert 0.6 <= late.min() and late.max() <= 1.7
+        else:
+            assert 0.1 <= late.min() and late.max() <= 22.0  # by the change's factor, times the two of steady gradients
