@@ -849,6 +849,7 @@ extern "C" int rfast_adamw_step(const rfast_adamw* a, void* cuda_stream, char* e
     if (!((float)a->eps >= 1.17549435e-38f) || !std::isfinite((float)a->eps)) return op_fail(err, err_len, RFAST_EINVAL, "%s: eps must be at least 2^-126", me);
     if (!std::isfinite(a->lr) || !std::isfinite(a->weight_decay)) return op_fail(err, err_len, RFAST_EINVAL, "%s: lr and weight_decay must be finite", me);
     if (!a->d_step && a->step < 1) return op_fail(err, err_len, RFAST_EINVAL, "%s: step counts from 1", me);
+    if ((uintptr_t)a->d_step % 8 || (uintptr_t)a->d_grad_scale % 4) return op_fail(err, err_len, RFAST_EINVAL, "%s: d_step or d_grad_scale is not aligned to its type", me);
     if (a->n_tensors == 0) return RFAST_OK;
     const bool s8 = a->state_bits == 8;
     if (!a->numel || !a->param || !a->grad || !a->m || !a->v || (s8 && (!a->m_scale || !a->v_scale)))

@@ -306,3 +306,9 @@ def test_strides_beyond_any_memory_are_refused(rfast_lib, strides):
     base = dict(dy=A, x=2 * A, gamma=A, beta=A, mean=A, rstd=0, dx=3 * A, dgamma=A, dbeta=A, workspace=A, workspace_bytes=1 << 30)
     for which in ("x", "dy", "dx"):
         _refused(f"strides of {which} reach beyond", pkg.rfast_group_norm_backward, **{**base, **SHAPE, f"{which}_strides": strides})
+
+
+@pytest.mark.parametrize("kw", [dict(d_step=A + 4), dict(d_step=A + 1), dict(d_grad_scale=A + 2), dict(d_step=A, d_grad_scale=A + 1)])
+def test_adamw_refuses_misaligned_scalars(rfast_lib, kw):
+    """The kernel reads 8 and 4 bytes there: off their alignment that is a fault on the device, and the host's to refuse."""
+    _refused("d_step or d_grad_scale is not aligned", _adamw, **kw)
