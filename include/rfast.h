@@ -210,6 +210,7 @@ enum {
                                      /* leaves, the neighbours' v read, x written, the remembered        */
                                      /* gradient read and the new one written (element-wise objective:   */
                                      /* its two data streams instead), the news rows read, z written, the */
+                                     /* moments of RFAST_DESCENT_ADAMW* read and written, the             */
                                      /* running sums read and written.  RFAST_Q_BYTES_* also count what   */
                                      /* only the implementation moves: re-reads between the kernels a     */
                                      /* step is split into, the low-order tracker words of compensated    */
@@ -553,7 +554,8 @@ int rfast_adamw_step(const rfast_adamw* a, void* cuda_stream, char* err, size_t 
  * share a row (all of them: one layer; a worker's rows: one layer per worker).  mean and rstd are
  * written, fp32 [samples][groups]; the backward pass wants them.  Sums and statistics are held in
  * 32 bits, y is rounded once to its type; variances come from deviations, not from a difference
- * of squares.  A NaN or infinity in x leaves NaN in its sample's group and nowhere else (backward: and
+ * of squares; where values of a group lie 2^63 and more apart their squares leave fp32, and rstd is 0.
+ * A NaN or infinity in x leaves NaN in its sample's group and nowhere else (backward: and
  * in dgamma and dbeta of the channels that it reaches).
  * Strides are those of a sample and of a position, in elements (two numbers; NULL: contiguous);
  * channels are neighbours.  Read operands may overlap themselves (a stride of 0 repeats), written

@@ -10,7 +10,8 @@
 //     blocks run at a time: one launch for the chunks' sums, one that merges them and goes over the values again, from the
 //     last position to the first, so that the L2 cache serves what it still holds (32 x 3136 x 256 bf16 backward, x and dy
 //     103 MB: the second launch reads 48 MB from memory, in the order of the first 87 MB).
-// Measured and dropped, all for 32 x 3136 x 256 bf16 and against 31 us forward and 48 us backward:
+// Measured and dropped, all for 32 x 3136 x 256 bf16 and against 31 us forward and 48 us backward (before sigmoid2 bounded its argument,
+// which costs 0.5 and 0.8 us):
 //   - spans of equal length over slabs laid end to end, which give every SM the same work: a block whose span holds the end
 //     of a slab and the start of the next sets up and sums up twice, and the launch waits for it (36 and 84 us);
 //   - a cluster of thread blocks that keep a slab in their shared memory and merge its sums there: loading, summing and
@@ -171,7 +172,7 @@ __device__ __forceinline__ void walk(int cnt, Load load, Use use) {
 // The same out of memory, through a ring of 2 PAIRS slots in shared memory that only this thread uses: `fetch(slot)` starts the
 // asynchronous copies of the next row into a slot, `held(slot)` reads one.  What is on its way costs no registers, so there can be
 // enough of it: rows fetched ahead into registers left 40 to 50 KB on their way in an SM, and 4 TB/s.  (Two pairs: backward 50 us in the
-// place of 48; four: forward 31.2 in the place of 30.8 us, see the kernels for the shape.)
+// place of 48; four: forward 31.2 in the place of 30.8 us, see the kernels for the shape, and above for what came after.)
 template <int PAIRS> struct Ring {
     int in, sent;
     template <class Fetch> __device__ __forceinline__ void send(int cnt, Fetch& fetch) {
@@ -394,11 +395,13 @@ __device__ __forceinline__ int team_size(int entries) {
 
 // ---- forward --------------------------------------------------------------------------------------
 // kWhole, kReread: grid = (items, slabs).  kSums, kApply: grid = (chunks, slabs, samples of the launch).
-// 32 x 3136 x 256 bf16 with u / (1 + exp(-u)): 31 us, 3.3 TB/s of x read and y written once; 26 us without an activation.  The
+// 32 x 3136 x 256 bf16 with u / (1 + exp(-u)): 31.7 us, 3.2 TB/s of x read and y written once; 26.9 us without an activation.  The
 // sums take 11 us of it whether x comes from memory or from the L2 cache, the second launch 20 us: its 51 MB of writes
 // alone take 14 us (a plain fill does), the special function unit is busy for 9 us, and what is in the way is that all blocks
 // merge and set up at the same time.  Registers for two blocks per SM, four where a group's channels fill accesses (2 x 16384 x
-// 320 f16, ten channels a group: 17.0 us with two, 18.6 us with three; 32 x 3136 x 256 bf16: 31.4 us with two, 30.8 us with four).
+// 320 f16, ten channels a group: 17.0 us with two, 18.6 us with three, now 17.7; 32 x 3136 x 256 bf16: 31.4 us with two, 30.8 us with
+// four).  Samples that one block takes whole wait for their one load and several barriers, with nothing on its way meanwhile:
+// 8192 x 30 x 48 fp32 62 us (135 backward) where the bytes take 15 (22), 4096 x 4 x 512 fp32 60 us (118) where they take 10 (16).
 template <class T, int V, bool WHOLE, int TASK>
 __global__ void __launch_bounds__(kT, WHOLE ? 4 : 2)
 k_gn_forward(const __grid_constant__ GnArgs a) {
@@ -758,9 +761,9 @@ k_gn_affine(const float* __restrict__ part, int64_t rows, int C, float* __restri
 // shared memory and, buffered, du in fp32 in the place of dy, so that the second pass has no exponentials.
 // kSums, kApply: grid = (chunks, slabs, samples of the launch), the last kApply with one slab more, whose blocks form dgamma and dbeta
 // meanwhile.
-// 32 x 3136 x 256 bf16: 48 us, 3.2 TB/s of x and dy read and dx written once.  Bound by the arithmetic of a row (about 100
-// instructions for 8 channels) and its latency: the sums take as long with half of x and dy in the L2 cache.  So registers for two
-// blocks per SM, in which two rows' work interleaves: 48 us against 51 us with three.
+// 32 x 3136 x 256 bf16: 49 us, 3.1 TB/s of x and dy read and dx written once, 42 us without an activation.  Bound by the arithmetic of
+// a row (about 100 instructions for 8 channels) and its latency: the sums take as long with half of x and dy in the L2 cache.  So registers for two
+// blocks per SM, in which two rows' work interleaves: 48 us against 51 us with three (before the bound of sigmoid2).
 template <class T, int V, bool WHOLE, int TASK>
 __global__ void __launch_bounds__(kT, 2)
 k_gn_backward(const __grid_constant__ GnArgs a) {
@@ -1116,12 +1119,14 @@ k_gn_backward(const __grid_constant__ GnArgs a) {
 // 4096 x 2048 fp32, 64 sets, 44 us in the place of 15).
 // A lane holds 8 channels, 4 accesses where a team of 32 lanes with 8 each does not cover the group.  4096 x 512 fp32 in 16
 // groups, 64 sets: 7.0 us forward, 7.5 us backward; the general path, whose blocks hold 32 samples and meet at five barriers for
-// them, takes 15 and 39 us.  32768 x 512, the same sets' size: 43 and 51 us, 3.1 and 4.0 TB/s, bound by the loads that the blocks
-// have on their way.  16-bit loads of the backward pass go out two turns ahead and registers are for two blocks of an SM
-// (32768 x 512 bf16, one set: 31 us; one turn and three blocks: 44 us); forward a second turn ahead gains nothing.  With 4
+// them, takes 15 and 39 us.  32768 x 512 fp32: 32 and 51 us with one set (4.2 and 3.9 TB/s), 45 and 50 us with 512; what bounds these is
+// not settled: a second turn of loads ahead gains nothing forward.  16-bit loads of the backward pass go out two turns ahead and
+// registers are for two blocks of an SM (32768 x 512 bf16, one set: 33 us; one turn and three blocks: 44 us).  With 4
 // channels per lane 4096 x 512 fp32 takes 7.2 and 7.7 us; with 16 of 16-bit types the registers spill (bf16 backward 13 us
-// in the place of 7).
-// 4096 x 2048 fp32 in 4 groups: 15.5 us, 4.3 TB/s, and 32 us backward, 3.2 TB/s; the general path takes 60 and 146 us.
+// in the place of 7).  Groups of 264 to 1024 channels of 16-bit types have 32 channels per lane, and these kernels do spill (96 bytes forward, 152
+// backward): 4096 x 4096 bf16 in 8 groups 32 and 58 us, where the bytes take 10 and 16.  Groups of 16-bit types that are no multiple
+// of 8 channels are not in rows at all: 4096 x 640 bf16 in 32 groups 78 and 62 us, the same layer in fp32 9 and 16.
+// 4096 x 2048 fp32 in 4 groups, 64 sets: 18 us, 3.7 TB/s, and 33 us backward, 3.1 TB/s; the general path takes 60 and 146 us.
 constexpr int kRowChannels = 8;
 template <int V, int K, bool BACKWARD> constexpr int kRowBlocks = BACKWARD ? K * V <= kRowChannels ? 2 : 1 : K == 1 ? 4 : K == 2 ? 3 : 2;
 struct RowPlan {
@@ -1401,9 +1406,10 @@ GnPlan make_plan(const GnShape& s, int esize, int vmax, bool backward) {
         for (int gs = unit; gs < s.G; gs += unit)
             if (gs * s.Cg * esize >= 128) { p.gs = gs; break; }
         // A narrower last slab leaves its blocks with little to do.  Where samples alone are blocks enough, a width of less than two
-        // slabs is one: 128 samples x 1881 x 96 f16 in 32 groups 36 us against 44 with two (72 and 24 channels), backward 43
-        // against 58; 5 samples 16 against 12.6 us, wide slabs of few samples having many chunks to merge.  (Three even slabs in the
-        // place of four, 200 channels in 25 groups: 128 samples x 1881 backward 111 against 94 us.)
+        // slabs is one: 128 samples x 1881 x 96 f16 in 32 groups, no activation, 32 us, backward 42 against 58 with two slabs (72 and 24
+        // channels); 5 samples 16 against 12.6 us, wide slabs of few samples having many chunks to merge.  At the border 31 samples with
+        // two slabs take 17.0 and 19.7 us, 32 with one 16.5 and 17.3.  (Three even slabs in the place of four, 200 channels in 25
+        // groups: 128 samples x 1881 backward 111 against 94 us.)
         if (s.N >= 32 && s.S > 1 && s.G % p.gs && s.C * esize < 256) p.gs = s.G;
     }
     p.W = p.gs * s.Cg;
