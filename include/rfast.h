@@ -554,7 +554,7 @@ int rfast_adamw_step(const rfast_adamw* a, void* cuda_stream, char* err, size_t 
  * share a row (all of them: one layer; a worker's rows: one layer per worker).  mean and rstd are
  * written, fp32 [samples][groups]; the backward pass wants them.  Sums and statistics are held in
  * 32 bits, y is rounded once to its type; variances come from deviations, not from a difference
- * of squares; where values of a group lie 2^63 and more apart their squares leave fp32, and rstd is 0.
+ * of squares; where values of a group lie 2^63 and more apart their squares leave fp32, and rstd is 0 or NaN.
  * A NaN or infinity in x leaves NaN in its sample's group and nowhere else (backward: and
  * in dgamma and dbeta of the channels that it reaches).
  * Strides are those of a sample and of a position, in elements (two numbers; NULL: contiguous);
