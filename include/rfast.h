@@ -549,7 +549,8 @@ int rfast_adamw_step(const rfast_adamw* a, void* cuda_stream, char* err, size_t 
  *     mean = sum x / M,  rstd = 1 / sqrt(sum (x - mean)^2 / M + eps)
  *     h = (x - mean) rstd,  u = gamma h + beta,  y = act(u)
  *     act: u | max(u, 0) | u / (1 + exp(-u))
- * (u / (1 + exp(-u)) to 2^-22 + |u| 2^-23 of itself down to u = -41, and between -4e-17 and 0 below; its slope likewise)
+ * (u / (1 + exp(-u)) to 2^-22 + |u| 2^-23 of itself down to u = -41, and between -4e-17 and 0 below; its slope
+ * to 2^-20, and below within 4e-17 of 0)
  * gamma and beta are fp32 [samples / samples_per_set][channels]: samples_per_set consecutive samples
  * share a row (all of them: one layer; a worker's rows: one layer per worker).  mean and rstd are
  * written, fp32 [samples][groups]; the backward pass wants them.  Sums and statistics are held in

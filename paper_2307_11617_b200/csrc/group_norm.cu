@@ -1725,7 +1725,7 @@ extern "C" int rfast_group_norm_backward(const rfast_gn_shape* g, const void* d_
     if (a.s.N == 0) return RFAST_OK;                        // no sets either
     const int64_t sets = a.s.N / a.s.per_set;
     if (a.s.S > 0 && overlaps(a.s, a.on, a.os)) return op_fail(err, err_len, RFAST_EINVAL, "%s: the strides of dx make it overlap itself", me);
-    if (torn(a.s, d_dx, a.on, a.os, d_x, a.xn, a.xs) || torn(a.s, d_dx, a.on, a.os, d_dy, a.dn, a.ds))
+    if (a.s.S > 0 && (torn(a.s, d_dx, a.on, a.os, d_x, a.xn, a.xs) || torn(a.s, d_dx, a.on, a.os, d_dy, a.dn, a.ds)))
         return op_fail(err, err_len, RFAST_EINVAL, "%s: dx is x or dy, but with other strides", me);
     const void* ptrs[] = {d_dgamma, d_dbeta, d_gamma, d_beta, d_mean, d_rstd, d_dy, d_x, d_dx};
     const char* names[] = {"dgamma", "dbeta", "gamma", "beta", "mean", "rstd", "dy", "x", "dx"};

@@ -312,3 +312,9 @@ def test_strides_beyond_any_memory_are_refused(rfast_lib, strides):
 def test_adamw_refuses_misaligned_scalars(rfast_lib, kw):
     """The kernel reads 8 and 4 bytes there: off their alignment that is a fault on the device, and the host's to refuse."""
     _refused("d_step or d_grad_scale is not aligned", _adamw, **kw)
+
+
+def test_strides_of_nothing_are_not_compared(rfast_lib):
+    """Without positions nothing is read or written but dgamma and dbeta: null operands in any strides are no results in place."""
+    import paper_2307_11617_b200 as pkg
+    _refused("dgamma is null", pkg.rfast_group_norm_backward, 0, 0, 0, 0, 0, 0, 0, 0, 0, x_strides=(5, 7), dx_strides=(9, 9), **{**SHAPE, "positions": 0})
