@@ -197,3 +197,34 @@ def test_chunks_of_positions_outermost_in_memory(rfast_lib, shape, kind):
     assert all(torch.equal(a, b) for a, b in zip(back, far))
     far = c.backward("silu", near[1], near[2], out=dy, dy=dy, x=x)
     assert all(torch.equal(a, b) for a, b in zip(back, far))
+
+
+EXTREME = {
+    "most runs of groups, one position": (1, 1, 32 * 65534, 65534, 1),
+    "most runs of groups": (2, 3, 32 * 65534, 65534, 2),
+    "most sets, one position": (65535, 1, 16, 2, 65535),
+    "most sets": (65535, 3, 16, 2, 65535),
+    "most channels": (1, 2, 1 << 24, 2048, 1),
+    "many rows": (300_001, 1, 24, 3, 1),
+}
+
+
+@pytest.mark.parametrize("shape", list(EXTREME))
+def test_the_largest_counts(rfast_lib, monkeypatch, shape):
+    """As many runs of groups, sets and channels as the header allows: sums and statistics as elsewhere."""
+    monkeypatch.setitem(ALL, shape, EXTREME[shape])
+    test_backward_sums_hold_every_value_once(rfast_lib, shape, "f32", 0)
+    test_statistics_hold_every_position(rfast_lib, shape, "f32")
+
+
+def test_one_more_is_refused(rfast_lib):
+    import paper_2307_11617_b200 as pkg
+    torch, _ = _torch()
+    d = torch.zeros(64, device="cuda").data_ptr()             # nothing is read: the call is refused
+    for shape, text in ((dict(samples=65536, positions=1, channels=16, groups=2, samples_per_set=1), "too many groups or sets"),
+                        (dict(samples=1, positions=2, channels=32 * 65535, groups=65535, samples_per_set=1), "too many groups or sets")):
+        need = pkg.rfast_group_norm_workspace(backward=True, **shape)
+        work = torch.empty(need, dtype=torch.uint8, device="cuda")
+        with pytest.raises(pkg.RFastError) as ei:
+            pkg.rfast_group_norm_backward(d, d, d, d, d, d, d, d, d, workspace=work.data_ptr(), workspace_bytes=need, **shape)
+        assert text in str(ei.value)
