@@ -589,6 +589,72 @@ int rfast_group_norm_backward(const rfast_gn_shape* shape, const void* d_dy, con
                               const float* d_rstd, void* d_dx, const int64_t* dx_strides, float* d_dgamma, float* d_dbeta,
                               void* workspace, size_t workspace_bytes, void* cuda_stream, char* err, size_t err_len);
 
+/* Embedding: rows of a table, looked up by token and scaled, and the gradient of the table.
+ *     out_i = scale table[token_i]                                       i < tokens
+ *     dtable_v = scale (sum of dout_i over the i whose token is v)        v < vocab;  accumulate: added to what dtable holds
+ * A token outside [0, vocab) (-1, as padding) is none: its row of out is zero, its row of dout is not read.  Tokens
+ * are 32- or 64-bit integers.  The backward pass sorts tokens and positions (stably), so that each sum runs over
+ * ascending positions in fp32, long ones over sums of 64 and 1024 sorted places; each value is rounded once to its type.
+ * Without accumulate every row of dtable is written, zeros where a token does not occur; with it those rows are left alone.
+ * A NaN or infinity of a row of dout reaches the row of its token and nothing else.
+ * Strides are those of a row in elements.  Read operands may overlap themselves (a stride of 0 repeats a row), written
+ * ones may not; no other operands may overlap.  Addresses need to be aligned to their type only; where width is a multiple
+ * of 8 and addresses and strides are multiples of 16 bytes, both operands are moved 16 bytes at a time.  At most
+ * 2^30 tokens, a vocabulary of 2^30 and a width of 2^24.
+ * workspace: rfast_embedding_workspace(shape) bytes of DEVICE memory, aligned to 16 (backward pass only). */
+typedef struct rfast_emb_shape {
+    int64_t tokens, vocab;
+    int32_t width;
+    int32_t token_bits;                /* 32 or 64 */
+    int32_t table_type;                /* RFAST_TYPE_* of table and dtable */
+    int32_t out_type;                  /* RFAST_TYPE_* of out and dout */
+} rfast_emb_shape;
+int     rfast_embedding(const rfast_emb_shape* shape, const void* d_tokens, const void* d_table, int64_t table_stride, float scale,
+                        void* d_out, int64_t out_stride, void* cuda_stream, char* err, size_t err_len);
+int64_t rfast_embedding_workspace(const rfast_emb_shape* shape);   /* bytes, or a negative status */
+int     rfast_embedding_backward(const rfast_emb_shape* shape, const void* d_tokens, const void* d_dout, int64_t dout_stride, float scale,
+                                 int accumulate, void* d_dtable, int64_t dtable_stride, void* workspace, size_t workspace_bytes,
+                                 void* cuda_stream, char* err, size_t err_len);
+
+/* Clipped policy loss with a KL term, out of logits [tokens][vocab], and its gradient in the logits:
+ *     logp = z_token / T - log(sum_v exp(z_v / T)),   r = exp(logp - old_logp)
+ *     token_loss = weight (-min(r A, clamp(r, 1 - clip_low, 1 + clip_high) A) + kl_coef (exp(d) - d - 1)),   d = ref_logp - logp
+ *     loss = sum of token_loss
+ *     dlogits_v = loss_scale d token_loss / d logp (1[v = token] - exp(z_v / T) / sum) / T
+ * (the derivative is r A's where r A <= clamp(r) A, and 0 of that term elsewhere).  Without ref_logp there is no KL
+ * term; without weight it is 1; loss_scale (DEVICE) scales the gradient only, 1 without it.
+ * A row whose weight is 0 or whose token is outside [0, vocab) does not count: its token_loss and logp are 0, its row of
+ * dlogits is zero, and neither its logits nor its other numbers are read.  Logits may be -infinity (words that may not be used):
+ * their gradient is 0.  A row of nothing but -infinity, a NaN or +infinity leave that row's results and `loss` NaN.
+ * Running sums of a row are fp32, a row's own numbers (logp, r, both terms) and `loss` 64 bits; each result is rounded
+ * once.  |z| / T below 2^126.
+ * Strides are those of a row in elements; logits may overlap themselves (a stride of 0 repeats a row), dlogits may not.
+ * dlogits may be the logits, with their stride; no other operands may overlap.  Addresses need to be aligned to their type
+ * only.  The fast case is a gradient whose rows lie as the logits' do within 16 bytes (both contiguous, or both strides
+ * multiples of 16 bytes).  Rows whose number of logits is odd are no slower. */
+typedef struct rfast_policy {
+    int64_t tokens, vocab;
+    int32_t type;                      /* RFAST_TYPE_* of logits and dlogits */
+    int32_t token_bits;                /* 32 or 64 */
+    const void*  d_logits;
+    int64_t      logits_stride;
+    const void*  d_tokens;
+    const float* d_old_logp;           /* [tokens] */
+    const float* d_ref_logp;           /* [tokens], or NULL */
+    const float* d_advantage;          /* [tokens] */
+    const float* d_weight;             /* [tokens], or NULL */
+    const float* d_loss_scale;         /* one value, or NULL */
+    double       temperature;          /* in [0.001, 1000] */
+    double       clip_low, clip_high;  /* clip_low in [0, 1], clip_high >= 0 (infinite: no bound) */
+    double       kl_coef;
+    float*       d_loss;               /* one value, or NULL; wants token_loss */
+    float*       d_token_loss;         /* [tokens], or NULL */
+    float*       d_logp;               /* [tokens], or NULL */
+    void*        d_dlogits;            /* or NULL: no gradient is formed */
+    int64_t      dlogits_stride;
+} rfast_policy;
+int rfast_policy_loss(const rfast_policy* p, void* cuda_stream, char* err, size_t err_len);
+
 void        rfast_destroy(rfast_ctx* ctx);
 const char* rfast_last_error(const rfast_ctx* ctx);   /* ctx may be NULL: last create error */
 const char* rfast_version(void);

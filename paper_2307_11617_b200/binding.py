@@ -84,6 +84,20 @@ class _GnShape(C.Structure):
                 ("samples_per_set", C.c_int64), ("type", C.c_int32), ("act", C.c_int32)]
 
 
+class _EmbShape(C.Structure):
+    _fields_ = [("tokens", C.c_int64), ("vocab", C.c_int64), ("width", C.c_int32), ("token_bits", C.c_int32), ("table_type", C.c_int32),
+                ("out_type", C.c_int32)]
+
+
+class _Policy(C.Structure):
+    _fields_ = [("tokens", C.c_int64), ("vocab", C.c_int64), ("type", C.c_int32), ("token_bits", C.c_int32),
+                ("d_logits", C.c_void_p), ("logits_stride", C.c_int64), ("d_tokens", C.c_void_p), ("d_old_logp", C.c_void_p),
+                ("d_ref_logp", C.c_void_p), ("d_advantage", C.c_void_p), ("d_weight", C.c_void_p), ("d_loss_scale", C.c_void_p),
+                ("temperature", C.c_double), ("clip_low", C.c_double), ("clip_high", C.c_double), ("kl_coef", C.c_double),
+                ("d_loss", C.c_void_p), ("d_token_loss", C.c_void_p), ("d_logp", C.c_void_p), ("d_dlogits", C.c_void_p),
+                ("dlogits_stride", C.c_int64)]
+
+
 _lib = None
 
 
@@ -136,6 +150,13 @@ def lib():
                                        C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p, C.c_char_p, C.c_size_t]
         L.rfast_group_norm_backward.argtypes = [C.POINTER(_GnShape)] + [C.c_void_p] * 13 + [C.c_size_t, C.c_void_p, C.c_char_p, C.c_size_t]
         L.rfast_adamw_step.argtypes = [C.POINTER(_AdamW), C.c_void_p, C.c_char_p, C.c_size_t]
+        L.rfast_embedding.argtypes = [C.POINTER(_EmbShape), C.c_void_p, C.c_void_p, C.c_int64, C.c_float, C.c_void_p, C.c_int64,
+                                      C.c_void_p, C.c_char_p, C.c_size_t]
+        L.rfast_embedding_workspace.argtypes = [C.POINTER(_EmbShape)]
+        L.rfast_embedding_workspace.restype = C.c_int64
+        L.rfast_embedding_backward.argtypes = [C.POINTER(_EmbShape), C.c_void_p, C.c_void_p, C.c_int64, C.c_float, C.c_int, C.c_void_p, C.c_int64,
+                                               C.c_void_p, C.c_size_t, C.c_void_p, C.c_char_p, C.c_size_t]
+        L.rfast_policy_loss.argtypes = [C.POINTER(_Policy), C.c_void_p, C.c_char_p, C.c_size_t]
         _lib = L
     return _lib
 
@@ -531,6 +552,59 @@ def rfast_group_norm_backward(dy: int, x: int, gamma: int, beta: int, mean: int,
     _op(lib().rfast_group_norm_backward(C.byref(shape), dy or None, _strides(dy_strides), x or None, _strides(x_strides), gamma or None, beta or None,
                                         mean or None, rstd or None, dx or None, _strides(dx_strides), dgamma or None, dbeta or None,
                                         workspace or None, workspace_bytes, cuda_stream or None, err, 256), err)
+
+
+def _emb_shape(tokens, vocab, width, token_bits, table_type, out_type):
+    return _EmbShape(tokens, vocab, width, token_bits, _type(table_type), _type(out_type))
+
+
+def rfast_embedding(d_tokens: int, d_table: int, d_out: int, tokens: int, vocab: int, width: int, scale: float = 1.0, token_bits: int = 64,
+                    table_type: str = "f32", out_type: str = "f32", table_stride=None, out_stride=None, cuda_stream: int = 0) -> None:
+    """out[i] = scale * table[token i]: rows of a table [vocab][width] by token, zero where the token is outside [0, vocab).
+    All addresses are DEVICE addresses; tokens are integers of token_bits (32 or 64).  Strides are those of a row in elements,
+    None for contiguous rows.  Enqueued on cuda_stream."""
+    shape = _emb_shape(tokens, vocab, width, token_bits, table_type, out_type)
+    err = C.create_string_buffer(256)
+    _op(lib().rfast_embedding(C.byref(shape), d_tokens or None, d_table or None, width if table_stride is None else table_stride, scale,
+                              d_out or None, width if out_stride is None else out_stride, cuda_stream or None, err, 256), err)
+
+
+def rfast_embedding_workspace(tokens: int, vocab: int, width: int) -> int:
+    """Bytes of DEVICE workspace that the backward pass of this shape needs."""
+    need = lib().rfast_embedding_workspace(C.byref(_emb_shape(tokens, vocab, width, 64, "f32", "f32")))
+    if need < 0:
+        raise RFastError(int(need), "rfast_embedding_workspace: the shape is not valid")
+    return int(need)
+
+
+def rfast_embedding_backward(d_tokens: int, d_dout: int, d_dtable: int, tokens: int, vocab: int, width: int, scale: float = 1.0,
+                             accumulate: bool = False, token_bits: int = 64, out_type: str = "f32", table_type: str = "f32", dout_stride=None,
+                             dtable_stride=None, workspace: int = 0, workspace_bytes: int = 0, cuda_stream: int = 0) -> None:
+    """Gradient of rfast_embedding in its table: dtable[v] = scale * sum of the rows of dout (of out_type) whose token is v, of
+    table_type; with accumulate it is added to what dtable holds.  Sums are formed in fp32 in the order of the positions.
+    workspace: rfast_embedding_workspace(...) bytes that no other running call uses.  Enqueued on cuda_stream."""
+    shape = _emb_shape(tokens, vocab, width, token_bits, table_type, out_type)
+    err = C.create_string_buffer(256)
+    _op(lib().rfast_embedding_backward(C.byref(shape), d_tokens or None, d_dout or None, width if dout_stride is None else dout_stride, scale,
+                                       1 if accumulate else 0, d_dtable or None, width if dtable_stride is None else dtable_stride,
+                                       workspace or None, workspace_bytes, cuda_stream or None, err, 256), err)
+
+
+def rfast_policy_loss(d_logits: int, d_tokens: int, d_old_logp: int, d_advantage: int, tokens: int, vocab: int, d_loss: int = 0,
+                      d_token_loss: int = 0, d_logp: int = 0, d_dlogits: int = 0, d_ref_logp: int = 0, d_weight: int = 0, d_loss_scale: int = 0,
+                      temperature: float = 1.0, clip_low: float = 0.2, clip_high: float = 0.2, kl_coef: float = 0.0, type: str = "f32",
+                      token_bits: int = 64, logits_stride=None, dlogits_stride=None, cuda_stream: int = 0) -> None:
+    """Clipped policy loss with a KL term out of logits [tokens][vocab], and its gradient: token_loss = weight (-min(r A, clamp(r, 1 -
+    clip_low, 1 + clip_high) A) + kl_coef (exp(d) - d - 1)) with r = exp(logp - old_logp), d = ref_logp - logp and logp the token's log
+    probability at `temperature`.  All addresses are DEVICE addresses: logits and dlogits have `type`, everything else is fp32 [tokens],
+    d_loss and d_loss_scale one value; 0 for what is not given or not wanted.  Rows of weight 0 or with a token outside [0, vocab) do not
+    count.  Enqueued on cuda_stream."""
+    args = _Policy(tokens, vocab, _type(type), token_bits, d_logits or None, vocab if logits_stride is None else logits_stride, d_tokens or None,
+                   d_old_logp or None, d_ref_logp or None, d_advantage or None, d_weight or None, d_loss_scale or None, temperature, clip_low,
+                   clip_high, kl_coef, d_loss or None, d_token_loss or None, d_logp or None, d_dlogits or None,
+                   vocab if dlogits_stride is None else dlogits_stride)
+    err = C.create_string_buffer(256)
+    _op(lib().rfast_policy_loss(C.byref(args), cuda_stream or None, err, 256), err)
 
 
 class Engine:
