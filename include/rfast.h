@@ -627,7 +627,7 @@ int     rfast_embedding_backward(const rfast_emb_shape* shape, const void* d_tok
  * dlogits is zero, and neither its logits nor its other numbers are read.  Logits may be -infinity (words that may not be used):
  * their gradient is 0.  A row of nothing but -infinity, a NaN or +infinity leave that row's results and `loss` NaN.
  * Running sums of a row are fp32, a row's own numbers (logp, r, both terms) and `loss` 64 bits; each result is rounded
- * once.  |z| / T below 2^126.
+ * once; exp((z - z_max) / T) below 2^-126 counts as 0.  |z| / T below 2^126.
  * Strides are those of a row in elements; logits may overlap themselves (a stride of 0 repeats a row), dlogits may not.
  * dlogits may be the logits, with their stride; no other operands may overlap.  Addresses need to be aligned to their type
  * only.  The fast case is a gradient whose rows lie as the logits' do within 16 bytes (both contiguous, or both strides

@@ -9,6 +9,8 @@ covers the relative error of a row's sum and the absolute one of logp (a power c
   logp        E + u |logp|
   token_loss  its slope's magnitude times E, u of itself:  w (|A| r + kl |e^d - 1|) E (1 + E)
   dlogits     s = scale dl/dlogp / T:  ds = scale w (|A| r + kl e^d) E / T;  ds (1[t] + p) + |s| p (2 E + 2^-22 + u R) + 3 u |s| 1[t], half a step
+A power below 2^-126 of its row's largest, the least normal number, counts as 0: p is then off by at most 2^-126 (the largest has a p of at
+least 1 / n, and p = power / sum with sum >= 1), so dlogits by |s| 2^-126 more.
 Ratios are set away from the borders of the clip, as both sides of a border are right next to it."""
 
 from __future__ import annotations
@@ -90,7 +92,7 @@ def _formula(c, kl, use_ref=True, use_w=True, use_up=True):
     tol_logp = E + U * logp.abs()
     tol_loss = size * E * (1 + E) + 2 * U * loss.abs()
     ds = up * size * E / warm
-    tol_dz = ds[:, None] * (hot + p) + s.abs()[:, None] * (p * (2 * E + 2.0 ** -22 + U * R)[:, None] + 3 * U * hot)
+    tol_dz = ds[:, None] * (hot + p) + s.abs()[:, None] * (p * (2 * E + 2.0 ** -22 + U * R)[:, None] + 3 * U * hot + 2.0 ** -126)
     tol_dz = tol_dz + HALF[c["kind"]] * (dz.abs() + tol_dz) + TINY[c["kind"]]
     return live, (loss, logp, dz), (tol_loss, torch.where(live, tol_logp, zero), torch.where(live[:, None], tol_dz, torch.zeros_like(dz)))
 
