@@ -655,6 +655,46 @@ typedef struct rfast_policy {
 } rfast_policy;
 int rfast_policy_loss(const rfast_policy* p, void* cuda_stream, char* err, size_t err_len);
 
+/* One Muon step, in place, over many matrices [rows][cols] (contiguous rows), m = min(rows, cols):
+ *     g' = scale g,  M = mu M + (1 - mu) g'                    scale = *d_grad_scale, 1 without it; mu = momentum_beta
+ *     U = nesterov ? (1 - mu) g' + mu M : M
+ *     X = U / max(||U||_F, eps), and `iterations` times
+ *         X <- a X + (b A + c A^2) X,   A = X X',   (a, b, c) = (3.4445, -4.7750, 2.0315)     (of X' where rows > cols)
+ *     p = p (1 - lr weight_decay) - lr size X
+ *     size: sqrt(max(1, rows / cols)) (RFAST_MUON_SIZE_SPECTRAL) or 0.2 sqrt(max(rows, cols)) (RFAST_MUON_SIZE_RMS)
+ * Five iterations bring the singular values of U that are not tiny next to the largest to between 0.7 and 1.2, whatever
+ * they were; those of 1e-3 of the norm and less grow 485-fold, and rounding errors in their directions with them.
+ * The momentum M is fp32, the norm 64 bits; products have fp32 sums and factors of `terms` fp16 numbers:
+ *   terms = 2: a factor is the sum of two, 22 bits; X is then within a few 1e-6 (relative, Frobenius) of exact for gradients
+ *              with a few large directions over noise
+ *   terms = 1: a factor is one, 11 bits: within 2e-3 for noise, 2e-2 with a few large directions
+ *   terms = 0: 2 for fp32 parameters, whose digits show it, 1 for 16-bit ones
+ * p is rounded once to its type.  A NaN, or an infinity, in g or M leaves its whole matrix NaN, and no other.
+ * Matrices without rows or columns are passed over.  Tensors may not overlap one another.  Addresses need to be aligned
+ * to their type only.  workspace: rfast_muon_workspace(n_tensors, rows, cols, terms) bytes of DEVICE memory (terms 1 or 2), aligned
+ * to 256; matrices go in runs of up to 128 in 8 shapes, which use it one after another.  Its first four
+ * bytes hold an int32 when the work is done: 0, or a code where a wait inside a kernel ran out (a fault of the device: the
+ * parameters are then not to be used). */
+#define RFAST_MUON_MAX_SIDE 65536
+enum { RFAST_MUON_SIZE_SPECTRAL = 0, RFAST_MUON_SIZE_RMS = 1 };
+typedef struct rfast_muon {
+    int32_t n_tensors;
+    int32_t param_type, grad_type;     /* RFAST_TYPE_* */
+    int32_t terms;                     /* 0, 1 or 2 */
+    const int32_t*     rows;           /* [n_tensors], 0 .. RFAST_MUON_MAX_SIDE */
+    const int32_t*     cols;
+    void* const*       param;
+    const void* const* grad;
+    float* const*      momentum;
+    double  lr, momentum_beta, weight_decay, eps;   /* momentum_beta in [0, 1), eps > 0 */
+    int32_t nesterov;
+    int32_t iterations;                /* 1 .. 32 */
+    int32_t size_rule;                 /* RFAST_MUON_SIZE_* */
+    const float* d_grad_scale;         /* DEVICE: factor on the gradients, or NULL */
+} rfast_muon;
+int64_t rfast_muon_workspace(int32_t n_tensors, const int32_t* rows, const int32_t* cols, int32_t terms);   /* bytes, or a negative status */
+int     rfast_muon_step(const rfast_muon* a, void* workspace, size_t workspace_bytes, void* cuda_stream, char* err, size_t err_len);
+
 void        rfast_destroy(rfast_ctx* ctx);
 const char* rfast_last_error(const rfast_ctx* ctx);   /* ctx may be NULL: last create error */
 const char* rfast_version(void);

@@ -98,6 +98,15 @@ class _Policy(C.Structure):
                 ("dlogits_stride", C.c_int64)]
 
 
+class _Muon(C.Structure):
+    _fields_ = [("n_tensors", C.c_int32), ("param_type", C.c_int32), ("grad_type", C.c_int32), ("terms", C.c_int32),
+                ("rows", C.c_void_p), ("cols", C.c_void_p), ("param", C.c_void_p), ("grad", C.c_void_p), ("momentum", C.c_void_p),
+                ("lr", C.c_double), ("momentum_beta", C.c_double), ("weight_decay", C.c_double), ("eps", C.c_double),
+                ("nesterov", C.c_int32), ("iterations", C.c_int32), ("size_rule", C.c_int32), ("d_grad_scale", C.c_void_p)]
+
+
+SIZE_RULES = {"spectral": 0, "rms": 1}
+
 _lib = None
 
 
@@ -156,6 +165,9 @@ def lib():
         L.rfast_embedding_workspace.restype = C.c_int64
         L.rfast_embedding_backward.argtypes = [C.POINTER(_EmbShape), C.c_void_p, C.c_void_p, C.c_int64, C.c_float, C.c_int, C.c_void_p, C.c_int64,
                                                C.c_void_p, C.c_size_t, C.c_void_p, C.c_char_p, C.c_size_t]
+        L.rfast_muon_workspace.argtypes = [C.c_int32, C.c_void_p, C.c_void_p, C.c_int32]
+        L.rfast_muon_workspace.restype = C.c_int64
+        L.rfast_muon_step.argtypes = [C.POINTER(_Muon), C.c_void_p, C.c_size_t, C.c_void_p, C.c_char_p, C.c_size_t]
         L.rfast_policy_loss.argtypes = [C.POINTER(_Policy), C.c_void_p, C.c_char_p, C.c_size_t]
         _lib = L
     return _lib
@@ -605,6 +617,43 @@ def rfast_policy_loss(d_logits: int, d_tokens: int, d_old_logp: int, d_advantage
                    vocab if dlogits_stride is None else dlogits_stride)
     err = C.create_string_buffer(256)
     _op(lib().rfast_policy_loss(C.byref(args), cuda_stream or None, err, 256), err)
+
+
+def _sides(rows, cols):
+    r, c = np.ascontiguousarray(rows, dtype=np.int32), np.ascontiguousarray(cols, dtype=np.int32)
+    if r.ndim != 1 or r.shape != c.shape:
+        raise ValueError("rows and cols must hold one entry per matrix")
+    return r, c
+
+
+def rfast_muon_workspace(rows, cols, param_type: str = "f32", terms: int = 0) -> int:
+    """Bytes of DEVICE workspace that a step over matrices of these rows and columns needs."""
+    r, c = _sides(rows, cols)
+    need = lib().rfast_muon_workspace(len(r), _host(r), _host(c), terms or (2 if _type(param_type) == 0 else 1))
+    if need < 0:
+        raise RFastError(int(need), "rfast_muon_workspace: rows, cols or terms are not valid")
+    return int(need)
+
+
+def rfast_muon_step(param, grad, momentum_buffer, rows, cols, lr: float = 0.02, momentum: float = 0.95, weight_decay: float = 0.0,
+                    nesterov: bool = True, eps: float = 1e-7, iterations: int = 5, size_rule: str = "spectral", terms: int = 0,
+                    param_type: str = "f32", grad_type: str = "f32", d_grad_scale: int = 0, workspace: int = 0, workspace_bytes: int = 0,
+                    cuda_stream: int = 0) -> None:
+    """One Muon step, in place, over many matrices: momentum, an update orthogonalised by `iterations` Newton-Schulz steps, decay.
+    param, grad and momentum_buffer are the matrices' DEVICE addresses, rows and cols their sizes (sequences or integer arrays);
+    momentum is fp32.  size_rule: "spectral" (sqrt(max(1, rows / cols))) or "rms" (0.2 sqrt(max(rows, cols))) times the update;
+    terms: fp16 numbers per factor of the products (0: 2 for fp32 parameters, else 1); d_grad_scale: DEVICE address of an fp32
+    factor on the gradients.  workspace: rfast_muon_workspace(...) bytes, aligned to 256, that no other running call uses.  Enqueued
+    on cuda_stream."""
+    r, c = _sides(rows, cols)
+    k = len(r)
+    lists = [_list(a, k, name) for a, name in ((param, "param"), (grad, "grad"), (momentum_buffer, "momentum_buffer"))]
+    if size_rule not in SIZE_RULES:
+        raise ValueError(f"unknown size_rule {size_rule!r}: one of {', '.join(SIZE_RULES)}")
+    args = _Muon(k, _type(param_type), _type(grad_type), terms, _host(r), _host(c), *[_host(a) for a in lists], lr, momentum, weight_decay, eps,
+                 1 if nesterov else 0, iterations, SIZE_RULES[size_rule], d_grad_scale or None)
+    err = C.create_string_buffer(256)
+    _op(lib().rfast_muon_step(C.byref(args), workspace or None, workspace_bytes, cuda_stream or None, err, 256), err)
 
 
 class Engine:

@@ -1,0 +1,823 @@
+// Muon step: momentum, an update orthogonalised by Newton-Schulz products, decay (see rfast_muon_step in rfast.h for the formulas).
+//
+// With X the update over its norm, m x n and m <= n (transposed where it is higher than wide), an iteration is three products,
+//     A = X X'            (symmetric)
+//     B = b A + c A A     (symmetric)
+//     X = a X + B X
+// and five iterations are nearly all the work: 5 (3 m^2 n + m^3) operations when only half of each symmetric product is formed.  They
+// run on the tensor cores in fp16 with fp32 sums.  A factor is one fp16 number, or (terms = 2) the sum of two, 22 bits, of which three
+// products are formed: high by high, high by low, low by high.  X lies within [-1.3, 1.3] and is held times 2^14, A and B within 3, times
+// 2^13, so that neither the range nor, for the low halves, the least normal number of fp16 is met.
+//
+// Matrices of one shape lie in one array of the workspace, so that one launch per product serves all matrices of up to eight shapes.
+// Tiles go to pairs of thread blocks, 256 x 256 per pair (one matrix instruction for both), or, where those are too few for the
+// GPU, to single ones, 128 x 64.  In a block one warp brings tiles by TMA through a ring of stages, one issues the matrix
+// instructions, eight read the sums of one tile out of tensor memory while the next is being formed.
+//
+// Every wait on a barrier is bounded: when it runs out the block leaves a code in the workspace's first word and ends.
+#include <cuda.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include <cmath>
+#include <cstdio>
+#include <new>
+#include <vector>
+
+#include "ops.h"
+#include "tensor_core.cuh"
+#include "values.cuh"
+
+namespace rfast {
+
+namespace {
+
+constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
+constexpr float kXUnit = 16384.f, kSUnit = 8192.f;           // X and A, B as they are held
+constexpr int kMats = 128, kGroups = 8;                       // matrices and shapes of one run of launches
+constexpr int kPart = 16384;                                  // values of a block of the first kernel
+constexpr int kBox = 64, kBoxBytes = kBox * kBox * 2;         // a TMA box: 64 rows of 64 values
+// The tensor cores' fp32 sums round towards zero, by up to 2^-23 of the sum with every instruction: a long sum of squares comes out
+// small.  With two terms a factor's digits are worth more than that, so X X' is summed in registers every four boxes (256 values):
+// 1 x 4096 3.7e-5 -> 1.3e-6 off.  The other products' terms have either sign, and their errors cancel.
+constexpr int kSegment = 4;
+constexpr int kEpiWarps = 8, kThreads = 64 + 32 * kEpiWarps;
+constexpr int kPairs = 74, kSms = 148;
+
+enum Product { kGram = 0, kPoly = 1, kApply = 2, kUpdate = 3 };   // A; B; X; the last X, applied to the parameters
+
+struct MuonMat {
+    void* param;
+    const void* grad;
+    float* momentum;
+    int rows, cols;
+    int group, slot;
+    float step;                        // lr * size
+    int part0;                         // first of its sums of squares
+};
+struct MuonTable {
+    MuonMat mat[kMats];
+    int part0[kMats + 1], tile0[kMats + 1];       // running counts of the first two kernels' blocks
+    int count;
+};
+struct MuonGroup {
+    int m, n, np, mp, count;
+    int mat0;                          // its first matrix in the table
+    int tile0;                         // of the launch
+    int64_t x, s;                      // byte offsets of its arrays in the workspace
+    int64_t x_plane, s_plane;          // values of [count][m][pitch]: high halves; the low ones follow, then the other buffer
+};
+struct MuonGemm {
+    CUtensorMap x[kGroups], s[kGroups];
+    MuonGroup g[kGroups];
+    int groups, tiles, in;             // `in`: the buffer of X that is read
+    int param_type;
+    float keep;                        // 1 - lr weight_decay
+    char* work;
+    const MuonMat* mats;               // in the workspace
+};
+
+struct MuonScalars {
+    float mu, omu;                     // momentum, 1 - momentum
+    int nesterov, grad_type, terms;
+    double eps;
+    const float* scale;
+};
+
+template <class T> __device__ __forceinline__ float grad_at(const void* g, int64_t i) { return value_of(((const T*)g)[i]); }
+__device__ __forceinline__ float grad_value(const void* g, int type, int64_t i) {
+    return type == RFAST_TYPE_F32 ? grad_at<float>(g, i) : type == RFAST_TYPE_BF16 ? grad_at<__nv_bfloat16>(g, i) : grad_at<__half>(g, i);
+}
+__device__ __forceinline__ int find(const int* first, int count, int at) {
+    int lo = 0, hi = count;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (first[mid] <= at) lo = mid; else hi = mid;
+    }
+    return lo;
+}
+
+// ---- momentum and norm --------------------------------------------------------------------------
+// m = mu m + (1 - mu) g; the squares of u = m, or (1 - mu) g + mu m, in 64 bits.
+template <class GT>
+__device__ __forceinline__ double momentum_part(const MuonMat& a, const MuonScalars& c, int64_t lo, int64_t hi) {
+    const float scale = c.scale ? *c.scale : 1.f;
+    const GT* g = (const GT*)a.grad;
+    double sum = 0.0;
+    const auto one = [&](float& m, float gv) {
+        gv *= scale;
+        m = fmaf(c.mu, m, c.omu * gv);
+        const float u = c.nesterov ? fmaf(c.mu, m, c.omu * gv) : m;
+        sum = fma((double)u, (double)u, sum);
+    };
+    if ((uintptr_t)g % 16 == 0 && (uintptr_t)a.momentum % 16 == 0) {
+        const int64_t end = lo + (hi - lo) / 8 * 8;
+#pragma unroll 2
+        for (int64_t i = lo + threadIdx.x * 8; i < end; i += 256 * 8) {
+            float gv[8], mv[8];
+            unpack8(load8(g + i), gv);
+            unpack8(load8(a.momentum + i), mv);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) one(mv[k], gv[k]);
+            float4* to = reinterpret_cast<float4*>(a.momentum + i);
+            to[0] = make_float4(mv[0], mv[1], mv[2], mv[3]);
+            to[1] = make_float4(mv[4], mv[5], mv[6], mv[7]);
+        }
+        lo = end;
+    }
+    for (int64_t i = lo + threadIdx.x; i < hi; i += 256) {
+        float m = a.momentum[i];
+        one(m, value_of(g[i]));
+        a.momentum[i] = m;
+    }
+    return sum;
+}
+
+__device__ __forceinline__ double block_sum(double v, double* sh) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = v;
+    __syncthreads();
+    double s = 0.0;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) s += sh[w];
+    return s;
+}
+
+__global__ void __launch_bounds__(256)
+k_muon_momentum(const __grid_constant__ MuonTable t, MuonScalars c, double* parts, MuonMat* mats, int* status) {
+    __shared__ double sh[8];
+    let_follow();
+    if (blockIdx.x == 0) {
+        if (threadIdx.x == 0 && status) *status = 0;
+        for (int k = threadIdx.x; k < t.count; k += 256) mats[k] = t.mat[k];
+    }
+    const int k = find(t.part0, t.count, blockIdx.x);
+    const MuonMat a = t.mat[k];
+    const int64_t all = (int64_t)a.rows * a.cols, lo = (int64_t)(blockIdx.x - t.part0[k]) * kPart, hi = lo + kPart < all ? lo + kPart : all;
+    double s;
+    if (c.grad_type == RFAST_TYPE_F32) s = momentum_part<float>(a, c, lo, hi);
+    else if (c.grad_type == RFAST_TYPE_BF16) s = momentum_part<__nv_bfloat16>(a, c, lo, hi);
+    else s = momentum_part<__half>(a, c, lo, hi);
+    s = block_sum(s, sh);
+    if (threadIdx.x == 0) parts[blockIdx.x] = s;
+}
+
+// X = u / max(norm, eps), m x n, as it is held: 64 x 64 values of the parameter's shape per block.
+__global__ void __launch_bounds__(256)
+k_muon_begin(const __grid_constant__ MuonTable t, MuonScalars c, const double* parts, const __grid_constant__ MuonGemm q) {
+    __shared__ double sh[8];
+    __shared__ float tile[64][65];
+    follow();
+    let_follow();
+    const int k = find(t.tile0, t.count, blockIdx.x);
+    const MuonMat a = t.mat[k];
+    double s = 0.0;
+    for (int i = t.part0[k] + threadIdx.x; i < t.part0[k + 1]; i += 256) s += parts[i];
+    const double norm = sqrt(block_sum(s, sh));
+    // a NaN goes through
+    const double unit = (double)kXUnit / (norm < c.eps ? c.eps : norm);
+    const int tiles_c = (a.cols + 63) / 64, at = blockIdx.x - t.tile0[k];
+    const int r0 = at / tiles_c * 64, c0 = at % tiles_c * 64;
+    const float scale = c.scale ? *c.scale : 1.f;
+#pragma unroll 4
+    for (int e = threadIdx.x; e < 64 * 64; e += 256) {
+        const int r = e >> 6, col = e & 63;
+        float u = 0.f;
+        if (r0 + r < a.rows && c0 + col < a.cols) {
+            const int64_t i = (int64_t)(r0 + r) * a.cols + c0 + col;
+            u = a.momentum[i];
+            if (c.nesterov) u = fmaf(c.mu, u, c.omu * (grad_value(a.grad, c.grad_type, i) * scale));
+            u = (float)((double)u * unit);
+        }
+        tile[r][col] = u;
+    }
+    __syncthreads();
+    const MuonGroup& g = q.g[a.group];
+    const bool turned = a.rows > a.cols;
+    __half* x = (__half*)(q.work + g.x) + (int64_t)a.slot * g.m * g.np;
+    const int i0 = turned ? c0 : r0, j0 = turned ? r0 : c0;
+#pragma unroll 4
+    for (int e = threadIdx.x; e < 64 * 32; e += 256) {
+        const int i = e >> 5, j = (e & 31) * 2;
+        if (i0 + i >= g.m || j0 + j >= g.n) continue;
+        const float2 v = turned ? make_float2(tile[j][i], tile[j + 1][i]) : make_float2(tile[i][j], tile[i][j + 1]);
+        const __half2 high = __floats2half2_rn(v.x, v.y);
+        __half2* to = reinterpret_cast<__half2*>(x + (int64_t)(i0 + i) * g.np + j0 + j);
+        *to = high;
+        if (c.terms == 2) {
+            const float2 f = __half22float2(high);
+            to[g.x_plane / 2] = __floats2half2_rn(v.x - f.x, v.y - f.y);
+        }
+    }
+}
+
+// ---- products -----------------------------------------------------------------------------------
+template <int CG, int TERMS>
+struct Shape {
+    static constexpr int kTM = CG == 2 ? 256 : 128, kTN = CG == 2 ? 256 : 64;
+    static constexpr int kBoxesA = 2, kBoxesB = CG == 2 ? 2 : 1;                 // of one thread block
+    static constexpr int kHalf = (kBoxesA + kBoxesB) * kBoxBytes;                // the high (or low) halves of a stage
+    static constexpr int kStage = TERMS * kHalf;
+    static constexpr int kStages = CG == 2 ? (TERMS == 2 ? 3 : 6) : 4;
+    static constexpr int kStaged = 32 * 33 * 4;                                  // a warp's 32 x 32 values
+    static constexpr int kShared = 1024 + kStages * kStage + kEpiWarps * kStaged;
+    static constexpr int kColumns = 2 * kTN;                                     // of tensor memory: two tiles' sums
+};
+
+struct Tile {
+    int g, mat, i, j;
+};
+template <int TM, int TN, bool SYM>
+__host__ __device__ inline int tiles_of(int m, int n) {
+    const int ti = (m + TM - 1) / TM;
+    if (!SYM) return ti * ((n + TN - 1) / TN);
+    // columns up to the diagonal: TM / TN tiles more in every row, the last one cut at m
+    constexpr int q = TM / TN;
+    const int last = (m + TN - 1) / TN;
+    return q * ti * (ti - 1) / 2 + (last < q * ti ? last : q * ti);
+}
+template <int TM, int TN, bool SYM>
+__device__ __forceinline__ Tile tile_at(const MuonGemm& p, int t) {
+    Tile r;
+    r.g = 0;
+    while (r.g + 1 < p.groups && p.g[r.g + 1].tile0 <= t) ++r.g;
+    const MuonGroup& g = p.g[r.g];
+    const int per = tiles_of<TM, TN, SYM>(g.m, g.n);
+    t -= g.tile0;
+    r.mat = t / per;
+    t -= r.mat * per;
+    if (SYM) {
+        constexpr int q = TM / TN;
+        int i = (int)((sqrtf(1.f + 8.f * (float)t / q) - 1.f) * 0.5f);
+        while (q * (i + 1) * (i + 2) / 2 <= t) ++i;
+        while (q * i * (i + 1) / 2 > t) --i;
+        r.i = i;
+        r.j = t - q * i * (i + 1) / 2;
+    } else {
+        const int ti = (g.m + TM - 1) / TM;
+        r.i = t % ti;
+        r.j = t / ti;
+    }
+    return r;
+}
+
+__device__ __forceinline__ float joined(__half high, __half low) { return __half2float(high) + __half2float(low); }
+
+// p = p keep - step x for 32 x 32 values of X: along the parameter's rows, so that a lane has a column of X or, where X is the
+// parameter's transpose, a row.
+template <class T>
+__device__ __forceinline__ void update_tile(T* __restrict__ param, const float (*st)[33], int row0, int col0, int m, int n, bool turned, float step, float keep) {
+    const int lane = threadIdx.x & 31;
+    T* const w = param + (turned ? (int64_t)col0 * m + row0 + lane : (int64_t)row0 * n + col0 + lane);
+    const int64_t next = turned ? m : n;
+    const int rows = turned ? (row0 + lane < m ? n - col0 : 0) : (col0 + lane < n ? m - row0 : 0);
+#pragma unroll
+    for (int part = 0; part < 32; part += 16) {
+        T old[16];
+#pragma unroll
+        for (int u = 0; u < 16; ++u)
+            if (part + u < rows) old[u] = w[(part + u) * next];
+#pragma unroll
+        for (int u = 0; u < 16; ++u)
+            if (part + u < rows) w[(part + u) * next] = rounded<T>(fmaf(-step, turned ? st[lane][part + u] : st[part + u][lane], value_of(old[u]) * keep));
+    }
+}
+
+template <int CG, int TERMS, int OP>
+__global__ void __launch_bounds__(kThreads, 1)
+k_muon_product(const __grid_constant__ MuonGemm p) {
+    using S = Shape<CG, TERMS>;
+    constexpr bool kSym = OP == kGram || OP == kPoly;
+    constexpr bool kSegmented = OP == kGram && TERMS == 2;
+    extern __shared__ uint8_t raw[];
+    uint8_t* const base = (uint8_t*)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
+    __shared__ uint64_t full[S::kStages], empty[S::kStages], acc_full[2], acc_empty[2];
+    __shared__ uint32_t tmem;
+    __shared__ volatile int bad;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = CG == 2 ? tc::cluster_rank() : 0;
+    int* const status = (int*)p.work;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < S::kStages; ++s) { tc::bar_init(&full[s], 1); tc::bar_init(&empty[s], 1); }
+        for (int b = 0; b < 2; ++b) { tc::bar_init(&acc_full[b], 1); tc::bar_init(&acc_empty[b], CG * kEpiWarps); }
+        bad = 0;
+        tc::bar_init_fence();
+    }
+    if (warp == 1) tc::tmem_alloc<CG>(&tmem, S::kColumns);
+    tc::fence_before();
+    if (CG == 2) tc::cluster_sync(); else __syncthreads();
+    tc::fence_after();
+    const uint32_t acc = tmem;
+    follow();
+    let_follow();
+    const int first = blockIdx.x / CG, stride = gridDim.x / CG;
+
+    if (warp == 0) {
+        if (lane == 0) {                                    // ---- loads
+            tc::fence_for_loads();
+            int n = 0;
+            bool ok = true;
+            for (int t = first; t < p.tiles && ok; t += stride) {
+                const Tile at = tile_at<S::kTM, S::kTN, kSym>(p, t);
+                const MuonGroup& g = p.g[at.g];
+                const int blocks = ((OP == kGram ? g.n : g.m) + kBox - 1) / kBox;
+                const int row0 = at.i * S::kTM + rank * 128, col0 = at.j * S::kTN + rank * (S::kTN / CG);
+                for (int kb = 0; kb < blocks; ++kb, ++n) {
+                    const int s = n % S::kStages;
+                    if (n >= S::kStages && !(ok = tc::bar_wait(&empty[s], ((n / S::kStages) - 1) & 1))) break;
+                    const uint32_t bar = CG == 2 ? tc::smem_of(&full[s], 0) : tc::smem(&full[s]);
+                    if (rank == 0) tc::bar_expect(&full[s], CG * S::kStage);
+#pragma unroll
+                    for (int h = 0; h < TERMS; ++h) {
+                        uint8_t* to = base + s * S::kStage + h * S::kHalf;
+#pragma unroll
+                        for (int b = 0; b < S::kBoxesA; ++b, to += kBoxBytes) {
+                            if (OP == kGram) tc::load_5d<CG>(to, &p.x[at.g], bar, kb * kBox, row0 + b * kBox, at.mat, h, p.in);
+                            else tc::load_5d<CG>(to, &p.s[at.g], bar, kb * kBox, row0 + b * kBox, at.mat, h, OP == kPoly ? 0 : 1);
+                        }
+#pragma unroll
+                        for (int b = 0; b < S::kBoxesB; ++b, to += kBoxBytes) {
+                            if (OP == kGram) tc::load_5d<CG>(to, &p.x[at.g], bar, kb * kBox, col0 + b * kBox, at.mat, h, p.in);
+                            else if (OP == kPoly) tc::load_5d<CG>(to, &p.s[at.g], bar, kb * kBox, col0 + b * kBox, at.mat, h, 0);
+                            else tc::load_5d<CG>(to, &p.x[at.g], bar, col0 + b * kBox, kb * kBox, at.mat, h, p.in);
+                        }
+                    }
+                }
+            }
+            if (!ok) { atomicExch(status, 1); bad = 1; }
+        }
+    } else if (warp == 1) {
+        if (lane == 0 && rank == 0) {                       // ---- matrix instructions, of both blocks of a pair
+            constexpr bool kAcross = !kSym;                 // X as the second operand runs along its rows
+            const uint32_t instruction = tc::instruction_f16(S::kTM, S::kTN, kAcross);
+            constexpr uint32_t kLead = kAcross ? kBoxBytes : 16, kNext = kAcross ? 2048 >> 4 : 32 >> 4;
+            int n = 0, sums = 0;                            // stages, sums begun
+            bool ok = true;
+            for (int t = first; t < p.tiles && ok; t += stride) {
+                const Tile at = tile_at<S::kTM, S::kTN, kSym>(p, t);
+                const MuonGroup& g = p.g[at.g];
+                const int blocks = ((OP == kGram ? g.n : g.m) + kBox - 1) / kBox;
+                uint32_t to = 0;
+                int buf = 0;
+                for (int kb = 0; kb < blocks; ++kb, ++n) {
+                    const bool begin = kSegmented ? kb % kSegment == 0 : kb == 0;
+                    if (begin) {
+                        buf = sums & 1;
+                        if (sums >= 2 && !(ok = tc::bar_wait(&acc_empty[buf], ((sums >> 1) - 1) & 1))) break;
+                        tc::fence_after();
+                        to = acc + buf * S::kTN;
+                        ++sums;
+                    }
+                    const int s = n % S::kStages;
+                    if (!(ok = tc::bar_wait(&full[s], (n / S::kStages) & 1))) break;
+                    tc::fence_after();
+                    const uint32_t sa = tc::smem(base + s * S::kStage), sb = sa + S::kBoxesA * kBoxBytes;
+                    const uint64_t a0 = tc::operand(sa, 16), b0 = tc::operand(sb, kLead);
+#pragma unroll
+                    for (int k = 0; k < kBox / 16; ++k) tc::mma_f16<CG>(to, a0 + 2 * k, b0 + kNext * k, instruction, begin && k == 0 ? 0u : 1u);
+                    if (TERMS == 2) {
+                        const uint64_t a1 = tc::operand(sa + S::kHalf, 16), b1 = tc::operand(sb + S::kHalf, kLead);
+#pragma unroll
+                        for (int k = 0; k < kBox / 16; ++k) {
+                            tc::mma_f16<CG>(to, a0 + 2 * k, b1 + kNext * k, instruction, 1u);
+                            tc::mma_f16<CG>(to, a1 + 2 * k, b0 + kNext * k, instruction, 1u);
+                        }
+                    }
+                    tc::commit<CG>(&empty[s]);
+                    if (kb + 1 == blocks || (kSegmented && (kb + 1) % kSegment == 0)) tc::commit<CG>(&acc_full[buf]);
+                }
+            }
+            if (!ok) { atomicExch(status, 2); bad = 1; }
+        }
+    } else {                                                // ---- sums out of tensor memory
+        const int quarter = warp & 3, half = (warp - 2) >> 2;
+        float (*const st)[33] = (float (*)[33])(base + S::kStages * S::kStage + (warp - 2) * S::kStaged);
+        constexpr int kChunks = S::kTN / 64;                // of 32 columns, of a warp
+        int sums = 0;                                       // read so far
+        const auto wait = [&] {
+            const bool ok = __all_sync(0xffffffffu, tc::bar_wait(&acc_full[sums & 1], (sums >> 1) & 1));
+            if (!ok && lane == 0) { atomicExch(status, 3); bad = 1; }
+            tc::fence_after();
+            return ok;
+        };
+        const auto release = [&] {
+            tc::fence_before();
+            __syncwarp();
+            if (lane == 0) tc::bar_arrive_cluster(tc::smem_of(&acc_empty[sums & 1], 0));
+            ++sums;
+        };
+        const auto column = [&](int ch) { return half * (S::kTN / 2) + ch * 32; };
+        const auto read = [&](int ch, float (&v)[32]) { tc::tmem_load32(acc + (sums & 1) * S::kTN + column(ch) + ((uint32_t)(quarter * 32) << 16), v); };
+        for (int t = first; t < p.tiles; t += stride) {
+            const Tile at = tile_at<S::kTM, S::kTN, kSym>(p, t);
+            const MuonGroup& g = p.g[at.g];
+            float total[kSegmented ? kChunks : 1][32];
+            if (kSegmented) {
+#pragma unroll
+                for (int ch = 0; ch < kChunks; ++ch)
+#pragma unroll
+                    for (int c = 0; c < 32; ++c) total[ch][c] = 0.f;
+                const int segments = (g.n + kBox * kSegment - 1) / (kBox * kSegment);
+                bool ok = true;
+                for (int q = 0; q < segments && (ok = wait()); ++q) {
+#pragma unroll
+                    for (int ch = 0; ch < kChunks; ++ch) {
+                        float v[32];
+                        read(ch, v);
+#pragma unroll
+                        for (int c = 0; c < 32; ++c) total[ch][c] += v[c];
+                    }
+                    release();
+                }
+                if (!ok) break;
+            } else if (!wait()) {
+                break;
+            }
+            const int row0 = at.i * S::kTM + rank * 128 + quarter * 32;
+            __half* const sx = (__half*)(p.work + g.s) + (int64_t)at.mat * g.m * g.mp;                    // A
+            __half* const x_in = (__half*)(p.work + g.x) + p.in * TERMS * g.x_plane + (int64_t)at.mat * g.m * g.np;
+            __half* const x_out = (__half*)(p.work + g.x) + (p.in ^ 1) * TERMS * g.x_plane + (int64_t)at.mat * g.m * g.np;
+#pragma unroll
+            for (int ch = 0; ch < kChunks; ++ch) {
+                const int col0 = at.j * S::kTN + column(ch);
+                if (row0 >= g.m || (kSym ? col0 > row0 + 31 : col0 >= g.n)) continue;    // nothing of it is kept
+                float v[32];
+                if (kSegmented) {
+#pragma unroll
+                    for (int c = 0; c < 32; ++c) v[c] = total[kSegmented ? ch : 0][c];
+                } else {
+                    read(ch, v);
+                }
+                if (kSym) {
+                    // lane: a row i; column j: the value is kept at (i, j) and at (j, i), j <= i
+                    const int i = row0 + lane;
+                    __half* const to = sx + (OP == kPoly ? TERMS * g.s_plane : 0);
+                    const int64_t m0 = (int64_t)col0 * g.mp + i;           // of (col0, i); a column is mp values on
+                    const int last = i < g.m ? i - col0 : -1;              // columns up to this one are kept
+                    __half a_high[32], a_low[32];
+                    if (OP == kPoly) {
+#pragma unroll
+                        for (int c = 0; c < 32; ++c) {
+                            a_high[c] = c <= last ? __ldcg(sx + m0 + (int64_t)c * g.mp) : __half(0.f);
+                            if (TERMS == 2) a_low[c] = c <= last ? __ldcg(sx + g.s_plane + m0 + (int64_t)c * g.mp) : __half(0.f);
+                        }
+                    }
+#pragma unroll
+                    for (int c = 0; c < 32; ++c) {
+                        const float f = OP == kGram ? v[c] * (kSUnit / (kXUnit * kXUnit))
+                                                    : fmaf(kB, TERMS == 2 ? joined(a_high[c], a_low[c]) : __half2float(a_high[c]), v[c] * (kC / kSUnit));
+                        if (c <= last) {
+                            const __half high = __float2half_rn(f);
+                            to[m0 + (int64_t)c * g.mp] = high;
+                            if (TERMS == 2) to[m0 + (int64_t)c * g.mp + g.s_plane] = __float2half_rn(f - __half2float(high));
+                        }
+                        st[lane][c] = f;
+                    }
+                    __syncwarp();
+#pragma unroll 4
+                    for (int s2 = 0; s2 < 16; ++s2) {
+                        const int r = 2 * s2 + (lane >> 4), c = 2 * (lane & 15), ii = row0 + r, jj = col0 + c;
+                        if (ii < g.m && jj <= ii) {
+                            const float f0 = st[r][c], f1 = st[r][c + 1];
+                            const __half2 high = __floats2half2_rn(f0, f1);
+                            __half* d = to + (int64_t)ii * g.mp + jj;
+                            const float2 f = __half22float2(high);
+                            const __half2 low = __floats2half2_rn(f0 - f.x, f1 - f.y);
+                            if (jj + 1 <= ii) {
+                                *reinterpret_cast<__half2*>(d) = high;
+                                if (TERMS == 2) *reinterpret_cast<__half2*>(d + g.s_plane) = low;
+                            } else {
+                                *d = __low2half(high);
+                                if (TERMS == 2) d[g.s_plane] = __low2half(low);
+                            }
+                        }
+                    }
+                    __syncwarp();
+                } else {
+#pragma unroll
+                    for (int c = 0; c < 32; ++c) st[lane][c] = v[c];
+                    __syncwarp();
+                    const MuonMat* mat = nullptr;
+                    bool turned = false;
+                    if (OP == kUpdate) {
+                        mat = p.mats + g.mat0 + at.mat;
+                        turned = mat->rows > mat->cols;
+                    }
+                    // lanes 0 .. 15 take a row, lanes 16 .. 31 the next, two columns each
+                    const int c = 2 * (lane & 15), jj = col0 + c, r0 = lane >> 4;
+#pragma unroll
+                    for (int part = 0; part < 2; ++part) {
+                        __half2 high[8], low[8];
+#pragma unroll
+                        for (int u = 0; u < 8; ++u) {
+                            const int ii = row0 + part * 16 + 2 * u + r0;
+                            const int64_t o = (int64_t)ii * g.np + jj;
+                            const bool in = ii < g.m && jj < g.n;
+                            high[u] = in ? __ldcg(reinterpret_cast<const __half2*>(x_in + o)) : __half2(0.f, 0.f);
+                            if (TERMS == 2) low[u] = in ? __ldcg(reinterpret_cast<const __half2*>(x_in + o + g.x_plane)) : __half2(0.f, 0.f);
+                        }
+#pragma unroll
+                        for (int u = 0; u < 8; ++u) {
+                            const int r = part * 16 + 2 * u + r0, ii = row0 + r;
+                            float2 x = __half22float2(high[u]);
+                            if (TERMS == 2) {
+                                const float2 l = __half22float2(low[u]);
+                                x.x += l.x;
+                                x.y += l.y;
+                            }
+                            const float f0 = fmaf(kA, x.x, st[r][c] * (1.f / kSUnit)), f1 = fmaf(kA, x.y, st[r][c + 1] * (1.f / kSUnit));
+                            if (OP == kUpdate) {
+                                st[r][c] = f0;
+                                st[r][c + 1] = f1;
+                            } else if (ii < g.m && jj < g.n) {
+                                const int64_t o = (int64_t)ii * g.np + jj;
+                                const __half2 h = __floats2half2_rn(f0, f1);
+                                *reinterpret_cast<__half2*>(x_out + o) = h;
+                                if (TERMS == 2) {
+                                    const float2 f = __half22float2(h);
+                                    *reinterpret_cast<__half2*>(x_out + o + g.x_plane) = __floats2half2_rn(f0 - f.x, f1 - f.y);
+                                }
+                            }
+                        }
+                    }
+                    __syncwarp();
+                    if (OP == kUpdate) {
+                        const float step = mat->step * (1.f / kXUnit);
+                        if (p.param_type == RFAST_TYPE_F32) update_tile((float*)mat->param, st, row0, col0, g.m, g.n, turned, step, p.keep);
+                        else if (p.param_type == RFAST_TYPE_BF16) update_tile((__nv_bfloat16*)mat->param, st, row0, col0, g.m, g.n, turned, step, p.keep);
+                        else update_tile((__half*)mat->param, st, row0, col0, g.m, g.n, turned, step, p.keep);
+                        __syncwarp();
+                    }
+                }
+            }
+            if (!kSegmented) release();
+        }
+    }
+    __syncwarp();
+    if (bad) {                                              // copies that are still on their way land within microseconds
+        uint64_t t0, now;
+        asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t0));
+        do asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(now)); while (now - t0 < 1000000ull);
+    }
+    __syncwarp();
+    tc::fence_before();
+    if (CG == 2) tc::cluster_sync(); else __syncthreads();
+    tc::fence_after();
+    if (warp == 1) tc::tmem_free<CG>(acc, S::kColumns);
+}
+
+// ---- host ---------------------------------------------------------------------------------------
+typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
+                             CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeFn encode_fn() {
+    static const EncodeFn fn = [] {
+        void* f = nullptr;
+        cudaDriverEntryPointQueryResult r;
+        return cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &r) == cudaSuccess && r == cudaDriverEntryPointSuccess ? (EncodeFn)f : nullptr;
+    }();
+    return fn;
+}
+// [2 buffers][terms][count][rows][pitch] fp16, rows of `width` values; boxes of 64 x 64.
+bool encode(CUtensorMap* map, void* at, int64_t width, int64_t rows, int64_t pitch, int64_t count, int terms) {
+    const cuuint64_t dims[5] = {(cuuint64_t)width, (cuuint64_t)rows, (cuuint64_t)count, (cuuint64_t)terms, 2};
+    const cuuint64_t plane = (cuuint64_t)count * rows * pitch * 2;
+    const cuuint64_t strides[4] = {(cuuint64_t)pitch * 2, (cuuint64_t)rows * pitch * 2, plane, plane * terms};
+    const cuuint32_t box[5] = {kBox, kBox, 1, 1, 1}, step[5] = {1, 1, 1, 1, 1};
+    return encode_fn()(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 5, at, dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                       CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// A run of launches: matrices of up to eight shapes, and where their arrays lie.
+struct MuonRun {
+    MuonGroup g[kGroups];
+    int groups = 0, count = 0;
+    int index[kMats];                  // of the caller's list, by group, then by slot
+    int64_t parts = 0, bytes = 0;
+};
+constexpr int64_t kHead = 256 + ((int64_t)kMats * sizeof(MuonMat) + 255) / 256 * 256;    // status word, table
+
+int64_t parts_of(int64_t rows, int64_t cols) { return (rows * cols + kPart - 1) / kPart; }
+
+// Takes matrices from `at` on that are not empty, as many as a run holds; returns where the next run begins.
+int take_run(const int32_t* rows, const int32_t* cols, int n, int at, int terms, MuonRun& r) {
+    int group_of[kMats], list[kMats];
+    r = MuonRun();
+    for (; at < n && r.count < kMats; ++at) {
+        if (rows[at] == 0 || cols[at] == 0) continue;
+        const int m = rows[at] < cols[at] ? rows[at] : cols[at], w = rows[at] < cols[at] ? cols[at] : rows[at];
+        int g = 0;
+        while (g < r.groups && (r.g[g].m != m || r.g[g].n != w)) ++g;
+        if (g == kGroups) break;
+        const int64_t parts = parts_of(rows[at], cols[at]);
+        if (r.count > 0 && r.parts + parts > (1 << 24)) break;
+        if (g == r.groups) {
+            r.g[g] = MuonGroup{};
+            r.g[g].m = m;
+            r.g[g].n = w;
+            r.g[g].mp = (m + 7) / 8 * 8;
+            r.g[g].np = (w + 7) / 8 * 8;
+            ++r.groups;
+        }
+        group_of[r.count] = g;
+        list[r.count++] = at;
+        ++r.g[g].count;
+        r.parts += parts;
+    }
+    int64_t bytes = kHead + (8 * r.parts + 255) / 256 * 256;
+    int q = 0;
+    for (int g = 0; g < r.groups; ++g) {
+        MuonGroup& a = r.g[g];
+        for (int k = 0; k < r.count; ++k)
+            if (group_of[k] == g) r.index[q++] = list[k];
+        a.x_plane = (int64_t)a.count * a.m * a.np;
+        a.s_plane = (int64_t)a.count * a.m * a.mp;
+        a.x = bytes;
+        bytes += (a.x_plane * 4 * terms + 255) / 256 * 256;
+        a.s = bytes;
+        bytes += (a.s_plane * 4 * terms + 255) / 256 * 256;
+    }
+    r.bytes = bytes;
+    return at;
+}
+
+template <int CG, int TERMS, int OP>
+cudaError_t product(MuonGemm& p, cudaStream_t st) {
+    using S = Shape<CG, TERMS>;
+    constexpr bool kSym = OP == kGram || OP == kPoly;
+    int tiles = 0;
+    for (int g = 0; g < p.groups; ++g) {
+        p.g[g].tile0 = tiles;
+        tiles += p.g[g].count * tiles_of<S::kTM, S::kTN, kSym>(p.g[g].m, p.g[g].n);
+    }
+    p.tiles = tiles;
+    const int slots = CG == 2 ? kPairs : kSms;
+    cudaError_t e = cudaFuncSetAttribute(k_muon_product<CG, TERMS, OP>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kShared);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((tiles < slots ? tiles : slots) * CG);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = S::kShared;
+    cfg.stream = st;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = CG;
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, k_muon_product<CG, TERMS, OP>, (const MuonGemm)p);
+}
+
+// Time of a product by tiles of TM x TN on `slots` places, in clocks: whole waves of the mean tile.
+template <int CG, bool SYM>
+double product_time(const MuonGemm& p, int terms, bool gram) {
+    using S = Shape<CG, 1>;
+    const double combos = terms == 2 ? 3 : 1, per = CG == 2 ? 512 : 200, set_up = CG == 2 ? 4000 : 2000;
+    const int slots = CG == 2 ? kPairs : kSms;
+    double all = 0, sum = 0;
+    for (int g = 0; g < p.groups; ++g) {
+        const double t = (double)p.g[g].count * tiles_of<S::kTM, S::kTN, SYM>(p.g[g].m, p.g[g].n);
+        all += t;
+        sum += t * (((gram ? p.g[g].n : p.g[g].m) + kBox - 1) / kBox * per * combos + set_up);
+    }
+    return std::ceil(all / slots) * (sum / all);
+}
+template <int OP>
+cudaError_t pick_product(MuonGemm& p, int terms, cudaStream_t st) {
+    constexpr bool kSym = OP == kGram || OP == kPoly;
+    const bool pair = product_time<2, kSym>(p, terms, OP == kGram) <= product_time<1, kSym>(p, terms, OP == kGram);
+    if (pair) return terms == 2 ? product<2, 2, OP>(p, st) : product<2, 1, OP>(p, st);
+    return terms == 2 ? product<1, 2, OP>(p, st) : product<1, 1, OP>(p, st);
+}
+
+int muon_terms(const rfast_muon* a) { return a->terms ? a->terms : a->param_type == RFAST_TYPE_F32 ? 2 : 1; }
+
+const char* muon_shape_fault(int n, const int32_t* rows, const int32_t* cols) {
+    if (n < 0) return "n_tensors is negative";
+    if (n > 0 && (!rows || !cols)) return "null array";
+    for (int k = 0; k < n; ++k)
+        if (rows[k] < 0 || cols[k] < 0 || rows[k] > RFAST_MUON_MAX_SIDE || cols[k] > RFAST_MUON_MAX_SIDE) return "rows and cols must be in [0, 65536]";
+    return nullptr;
+}
+
+cudaError_t muon_run(const rfast_muon* a, const MuonRun& r, char* work, bool first_run, cudaStream_t st) {
+    MuonTable t;
+    MuonGemm q{};
+    const int terms = muon_terms(a);
+    int part = 0, tile = 0;
+    t.count = r.count;
+    int at = 0;
+    for (int g = 0; g < r.groups; ++g)
+        for (int s = 0; s < r.g[g].count; ++s, ++at) {
+            const int k = r.index[at];
+            MuonMat& m = t.mat[at];
+            m.param = a->param[k];
+            m.grad = a->grad[k];
+            m.momentum = a->momentum[k];
+            m.rows = a->rows[k];
+            m.cols = a->cols[k];
+            m.group = g;
+            m.slot = s;
+            const double size = a->size_rule == RFAST_MUON_SIZE_RMS ? 0.2 * std::sqrt((double)r.g[g].n)
+                                                                    : std::sqrt(m.rows > m.cols ? (double)m.rows / m.cols : 1.0);
+            m.step = (float)(a->lr * size);
+            m.part0 = part;
+            t.part0[at] = part;
+            t.tile0[at] = tile;
+            part += (int)parts_of(m.rows, m.cols);
+            tile += (m.rows + 63) / 64 * ((m.cols + 63) / 64);
+        }
+    t.part0[at] = part;
+    t.tile0[at] = tile;
+    int first = 0;
+    for (int g = 0; g < r.groups; ++g) {
+        q.g[g] = r.g[g];
+        q.g[g].mat0 = first;
+        if (!encode(&q.x[g], work + r.g[g].x, r.g[g].n, r.g[g].m, r.g[g].np, r.g[g].count, terms)) return cudaErrorInvalidValue;
+        if (!encode(&q.s[g], work + r.g[g].s, r.g[g].m, r.g[g].m, r.g[g].mp, r.g[g].count, terms)) return cudaErrorInvalidValue;
+        first += r.g[g].count;
+    }
+    q.groups = r.groups;
+    q.param_type = a->param_type;
+    q.keep = (float)(1.0 - a->lr * a->weight_decay);
+    q.work = work;
+    MuonMat* mats = (MuonMat*)(work + 256);
+    q.mats = mats;
+    double* parts = (double*)(work + kHead);
+    const MuonScalars c{(float)a->momentum_beta, (float)(1.0 - a->momentum_beta), a->nesterov != 0, a->grad_type, terms, a->eps, a->d_grad_scale};
+    cudaError_t e = launch(k_muon_momentum, dim3((unsigned)part), 256, 0, st, false, t, c, parts, mats, first_run ? (int*)work : (int*)nullptr);
+    if (e == cudaSuccess) e = launch(k_muon_begin, dim3((unsigned)tile), 256, 0, st, true, t, c, (const double*)parts, q);
+    for (int it = 0; it < a->iterations && e == cudaSuccess; ++it) {
+        q.in = it & 1;
+        e = pick_product<kGram>(q, terms, st);
+        if (e == cudaSuccess) e = pick_product<kPoly>(q, terms, st);
+        if (e == cudaSuccess) e = it + 1 < a->iterations ? pick_product<kApply>(q, terms, st) : pick_product<kUpdate>(q, terms, st);
+    }
+    return e;
+}
+
+}  // namespace
+
+}  // namespace rfast
+
+using namespace rfast;
+
+extern "C" int64_t rfast_muon_workspace(int32_t n_tensors, const int32_t* rows, const int32_t* cols, int32_t terms) {
+    if (muon_shape_fault(n_tensors, rows, cols) || (terms != 1 && terms != 2)) return RFAST_EINVAL;
+    int64_t most = kHead;
+    MuonRun r;
+    for (int at = 0; at < n_tensors;) {
+        at = take_run(rows, cols, n_tensors, at, terms, r);
+        if (r.bytes > most) most = r.bytes;
+    }
+    return most;
+}
+
+extern "C" int rfast_muon_step(const rfast_muon* a, void* workspace, size_t workspace_bytes, void* cuda_stream, char* err, size_t err_len) {
+    const char* const me = "rfast_muon_step";
+    if (!a) return op_fail(err, err_len, RFAST_EINVAL, "%s: null arguments", me);
+    if (const char* fault = muon_shape_fault(a->n_tensors, a->rows, a->cols)) return op_fail(err, err_len, RFAST_EINVAL, "%s: %s", me, fault);
+    if (!is_type(a->param_type) || !is_type(a->grad_type)) return op_fail(err, err_len, RFAST_EINVAL, "%s: unknown type", me);
+    if (a->terms < 0 || a->terms > 2) return op_fail(err, err_len, RFAST_EINVAL, "%s: terms must be 0, 1 or 2", me);
+    // negated comparisons refuse a NaN as well
+    if (!(a->momentum_beta >= 0 && a->momentum_beta < 1)) return op_fail(err, err_len, RFAST_EINVAL, "%s: momentum must be in [0, 1)", me);
+    if (!(a->eps > 0) || !std::isfinite(a->eps)) return op_fail(err, err_len, RFAST_EINVAL, "%s: eps must be positive and finite", me);
+    if (!std::isfinite(a->lr) || !std::isfinite(a->weight_decay)) return op_fail(err, err_len, RFAST_EINVAL, "%s: lr and weight_decay must be finite", me);
+    if (a->iterations < 1 || a->iterations > 32) return op_fail(err, err_len, RFAST_EINVAL, "%s: iterations must be in [1, 32]", me);
+    if (a->size_rule != RFAST_MUON_SIZE_SPECTRAL && a->size_rule != RFAST_MUON_SIZE_RMS) return op_fail(err, err_len, RFAST_EINVAL, "%s: unknown size_rule", me);
+    if ((uintptr_t)a->d_grad_scale % 4) return op_fail(err, err_len, RFAST_EINVAL, "%s: d_grad_scale is not aligned to its type", me);
+    if (a->n_tensors == 0) return RFAST_OK;
+    if (!a->param || !a->grad || !a->momentum) return op_fail(err, err_len, RFAST_EINVAL, "%s: null array", me);
+    int some = -1;
+    for (int k = 0; k < a->n_tensors; ++k) {
+        if (a->rows[k] == 0 || a->cols[k] == 0) continue;
+        if (!a->param[k] || !a->grad[k] || !a->momentum[k]) return op_fail(err, err_len, RFAST_EINVAL, "%s: tensor %d has a null address", me, k);
+        if ((uintptr_t)a->param[k] % bytes_of(a->param_type) || (uintptr_t)a->grad[k] % bytes_of(a->grad_type) || (uintptr_t)a->momentum[k] % 4)
+            return op_fail(err, err_len, RFAST_EINVAL, "%s: an address of tensor %d is not aligned to its type", me, k);
+        if (some < 0) some = k;
+    }
+    if (some < 0) return RFAST_OK;
+    const int64_t need = rfast_muon_workspace(a->n_tensors, a->rows, a->cols, muon_terms(a));
+    if (!workspace || (uintptr_t)workspace % 256) return op_fail(err, err_len, RFAST_EINVAL, "%s: the workspace must be given, aligned to 256 bytes", me);
+    if (workspace_bytes < (size_t)need) return op_fail(err, err_len, RFAST_EINVAL, "%s: the workspace needs %lld bytes", me, (long long)need);
+    const void* first[] = {a->param[some], a->grad[some], a->momentum[some], a->d_grad_scale, workspace};
+    const char* names[] = {"rfast_muon_step: param", "rfast_muon_step: grad", "rfast_muon_step: momentum", "rfast_muon_step: d_grad_scale", "rfast_muon_step: workspace"};
+    for (int k = 0; k < 5; ++k)
+        if (first[k]) {
+            const int rc = check_device_pointer(first[k], names[k], err, err_len);
+            if (rc != RFAST_OK) return rc;
+        }
+    if (!encode_fn()) return op_fail(err, err_len, RFAST_ECUDA, "%s: the driver has no cuTensorMapEncodeTiled", me);
+    MuonRun r;
+    bool first_run = true;
+    for (int at = 0; at < a->n_tensors;) {
+        at = take_run(a->rows, a->cols, a->n_tensors, at, muon_terms(a), r);
+        if (r.count == 0) continue;
+        const cudaError_t e = muon_run(a, r, (char*)workspace, first_run, (cudaStream_t)cuda_stream);
+        first_run = false;
+        if (e != cudaSuccess) return op_fail(err, err_len, RFAST_ECUDA, "%s: %s", me, cudaGetErrorString(e));
+    }
+    return RFAST_OK;
+}

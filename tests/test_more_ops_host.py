@@ -93,3 +93,65 @@ def test_unknown_types_are_refused(rfast_lib):
     assert B.lib().rfast_policy_loss(None, None, None, 0) == B.EINVAL
     p = B._Policy(1, 1, 9, 64)
     assert B.lib().rfast_policy_loss(C.byref(p), None, err, 256) == B.EINVAL and b"unknown type" in err.value
+
+
+def _muon(**kw):
+    import paper_2307_11617_b200 as pkg
+    base = dict(param=[A, A], grad=[A, A], momentum_buffer=[A, A], rows=[5, 7], cols=[3, 9], workspace=A, workspace_bytes=1 << 40)
+    base.update(kw)
+    pkg.rfast_muon_step(**base)
+
+
+@pytest.mark.parametrize("text,kw", [
+    ("rows and cols must be", dict(rows=[5, -1])), ("rows and cols must be", dict(cols=[3, 65537])), ("terms must be", dict(terms=3)), ("terms must be", dict(terms=-1)),
+    ("momentum must be", dict(momentum=1.0)), ("momentum must be", dict(momentum=NAN)), ("momentum must be", dict(momentum=-0.1)), ("eps must be", dict(eps=0.0)),
+    ("eps must be", dict(eps=NAN)), ("eps must be", dict(eps=INF)), ("lr and weight_decay", dict(lr=INF)), ("lr and weight_decay", dict(weight_decay=NAN)),
+    ("iterations must be", dict(iterations=0)), ("iterations must be", dict(iterations=33)), ("d_grad_scale is not aligned", dict(d_grad_scale=A + 2)),
+    ("tensor 1 has a null address", dict(param=[A, 0])), ("tensor 0 has a null address", dict(grad=[0, A])), ("tensor 1 has a null address", dict(momentum_buffer=[A, 0])),
+    ("address of tensor 1 is not aligned", dict(param=[A, A + 2])), ("address of tensor 0 is not aligned", dict(grad=[A + 1, A], grad_type="bf16")),
+    ("address of tensor 0 is not aligned", dict(momentum_buffer=[A + 2, A])), ("workspace must be given", dict(workspace=0)), ("workspace must be given", dict(workspace=A + 128)),
+    ("workspace needs", dict(workspace_bytes=1000))])
+def test_muon_refuses(rfast_lib, text, kw):
+    _refused(text, _muon, **kw)
+
+
+def test_muon_c_entry_refuses(rfast_lib):
+    import ctypes as C
+    import numpy as np
+    import paper_2307_11617_b200 as pkg
+    from paper_2307_11617_b200 import binding as B
+    err = C.create_string_buffer(256)
+    assert B.lib().rfast_muon_step(None, None, 0, None, err, 256) == B.EINVAL and b"null arguments" in err.value
+    assert B.lib().rfast_muon_step(None, None, 0, None, None, 0) == B.EINVAL
+    assert B.lib().rfast_muon_workspace(1, None, None, 1) == B.EINVAL
+    one = np.ones(2, np.int32)
+    at = one.ctypes.data
+    for field, value, text in (("param_type", 4, b"unknown type"), ("grad_type", -1, b"unknown type"), ("size_rule", 2, b"unknown size_rule"), ("n_tensors", -1, b"n_tensors"),
+                               ("rows", None, b"null array"), ("grad", None, b"null array")):
+        a = B._Muon(1, 0, 0, 0, at, at, at, at, at, 0.1, 0.9, 0.0, 1e-7, 1, 5, 0, None)
+        setattr(a, field, value)
+        assert B.lib().rfast_muon_step(C.byref(a), A, 1 << 40, None, err, 256) == B.EINVAL and text in err.value, err.value
+    with pytest.raises(ValueError):
+        _muon(rows=[5])
+    with pytest.raises(ValueError):
+        _muon(grad=[A])
+    with pytest.raises(ValueError):
+        _muon(size_rule="none")
+    with pytest.raises(B.RFastError):
+        pkg.rfast_muon_workspace([1], [1], terms=3)
+
+
+def test_muon_of_nothing_needs_no_device(rfast_lib):
+    import paper_2307_11617_b200 as pkg
+    pkg.rfast_muon_step([], [], [], [], [])
+    pkg.rfast_muon_step([0], [0], [0], [0], [7])
+
+
+def test_muon_workspace_holds_its_largest_run(rfast_lib):
+    """Runs use it one after another: a second run of the same size asks for no more."""
+    import paper_2307_11617_b200 as pkg
+    one = pkg.rfast_muon_workspace([64] * 128, [96] * 128)
+    assert pkg.rfast_muon_workspace([64] * 256, [96] * 256) == one
+    assert pkg.rfast_muon_workspace([64], [96], param_type="bf16") < pkg.rfast_muon_workspace([64], [96]) < one
+    # halves of X (two buffers), A and B in 16 bits, twice for two terms
+    assert one >= 128 * (2 * 64 * 96 + 2 * 64 * 64) * 2 * 2
