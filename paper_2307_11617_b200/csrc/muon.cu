@@ -3,7 +3,7 @@
 // With X the update over its norm, m x n and m <= n (transposed where it is higher than wide), an iteration is three products,
 //     A = X X'            (symmetric)
 //     B = b A + c A A     (symmetric)
-//     X = a X + B X
+//     X = a X + B X       (B holds a on its diagonal as well: X = B X)
 // and five iterations are nearly all the work: 5 (3 m^2 n + m^3) operations when only half of each symmetric product is formed.  They
 // run on the tensor cores in fp16 with fp32 sums.  A factor is one fp16 number, or (terms = 2) the sum of two, 22 bits, of which three
 // products are formed: high by high, high by low, low by high.  X lies within [-1.3, 1.3] and is held times 2^14, A and B within 3, times
@@ -53,7 +53,7 @@ struct MuonMat {
     int rows, cols;
     int group, slot;
     float step;                        // lr * size
-    int part0;                         // first of its sums of squares
+    int wide;                          // eight parameters at a time: cols in eights, address a multiple of 16 bytes
 };
 struct MuonTable {
     MuonMat mat[kMats];
@@ -84,10 +84,6 @@ struct MuonScalars {
     const float* scale;
 };
 
-template <class T> __device__ __forceinline__ float grad_at(const void* g, int64_t i) { return value_of(((const T*)g)[i]); }
-__device__ __forceinline__ float grad_value(const void* g, int type, int64_t i) {
-    return type == RFAST_TYPE_F32 ? grad_at<float>(g, i) : type == RFAST_TYPE_BF16 ? grad_at<__nv_bfloat16>(g, i) : grad_at<__half>(g, i);
-}
 __device__ __forceinline__ int find(const int* first, int count, int at) {
     int lo = 0, hi = count;
     while (hi - lo > 1) {
@@ -163,6 +159,58 @@ k_muon_momentum(const __grid_constant__ MuonTable t, MuonScalars c, double* part
     if (threadIdx.x == 0) parts[blockIdx.x] = s;
 }
 
+// Eight values as one or two fp16 numbers each.
+template <int TERMS>
+__device__ __forceinline__ void keep8(__half* to, int64_t low_plane, const float (&v)[8]) {
+    uint32_t high[4], low[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const __half2 h = __floats2half2_rn(v[2 * k], v[2 * k + 1]);
+        high[k] = *reinterpret_cast<const uint32_t*>(&h);
+        if (TERMS == 2) {
+            const float2 f = __half22float2(h);
+            const __half2 l = __floats2half2_rn(v[2 * k] - f.x, v[2 * k + 1] - f.y);
+            low[k] = *reinterpret_cast<const uint32_t*>(&l);
+        }
+    }
+    *reinterpret_cast<uint4*>(to) = make_uint4(high[0], high[1], high[2], high[3]);
+    if (TERMS == 2) *reinterpret_cast<uint4*>(to + low_plane) = make_uint4(low[0], low[1], low[2], low[3]);
+}
+
+// 64 x 64 values of u, times f1 f2, zeros beyond the matrix.
+template <class GT>
+__device__ __forceinline__ void begin_tile(const MuonMat& a, const MuonScalars& c, int r0, int c0, float scale, float f1, float f2, float (*tile)[65]) {
+    const GT* const g = (const GT*)a.grad;
+    const bool wide = a.cols % 8 == 0 && (uintptr_t)g % 16 == 0 && (uintptr_t)a.momentum % 16 == 0;
+    const auto value = [&](float m, float gv) { return (c.nesterov ? fmaf(c.mu, m, c.omu * (gv * scale)) : m) * f1 * f2; };
+    if (wide) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int r = (threadIdx.x >> 3) + 32 * u, col = (threadIdx.x & 7) * 8;
+            float m[8] = {}, gv[8] = {};
+            if (r0 + r < a.rows && c0 + col < a.cols) {
+                const int64_t i = (int64_t)(r0 + r) * a.cols + c0 + col;
+                unpack8(load8((const float*)a.momentum + i), m);
+                if (c.nesterov) unpack8(load8(g + i), gv);
+            }
+#pragma unroll
+            for (int w = 0; w < 8; ++w) tile[r][col + w] = value(m[w], gv[w]);
+        }
+    } else {
+#pragma unroll 8
+        for (int e = threadIdx.x; e < 64 * 64; e += 256) {
+            const int r = e >> 6, col = e & 63;
+            float m = 0.f, gv = 0.f;
+            if (r0 + r < a.rows && c0 + col < a.cols) {
+                const int64_t i = (int64_t)(r0 + r) * a.cols + c0 + col;
+                m = a.momentum[i];
+                if (c.nesterov) gv = value_of(g[i]);
+            }
+            tile[r][col] = value(m, gv);
+        }
+    }
+}
+
 // X = u / max(norm, eps), m x n, as it is held: 64 x 64 values of the parameter's shape per block.
 __global__ void __launch_bounds__(256)
 k_muon_begin(const __grid_constant__ MuonTable t, MuonScalars c, const double* parts, const __grid_constant__ MuonGemm q) {
@@ -175,40 +223,32 @@ k_muon_begin(const __grid_constant__ MuonTable t, MuonScalars c, const double* p
     double s = 0.0;
     for (int i = t.part0[k] + threadIdx.x; i < t.part0[k + 1]; i += 256) s += parts[i];
     const double norm = sqrt(block_sum(s, sh));
-    // a NaN goes through
+    // a NaN goes through; the factor is split in two, so that neither it nor what it makes of a value leaves fp32 (a norm above 0 is at
+    // least 2^-149, and the factor below 2^170)
     const double unit = (double)kXUnit / (norm < c.eps ? c.eps : norm);
+    int e = 0;
+    const double digits = frexp(unit < 0x1p170 ? unit : norm > 0 || norm != norm ? unit : 0x1p170, &e);
+    const float f1 = (float)ldexp(1.0, e / 2), f2 = (float)ldexp(digits, e - e / 2);
     const int tiles_c = (a.cols + 63) / 64, at = blockIdx.x - t.tile0[k];
     const int r0 = at / tiles_c * 64, c0 = at % tiles_c * 64;
     const float scale = c.scale ? *c.scale : 1.f;
-#pragma unroll 4
-    for (int e = threadIdx.x; e < 64 * 64; e += 256) {
-        const int r = e >> 6, col = e & 63;
-        float u = 0.f;
-        if (r0 + r < a.rows && c0 + col < a.cols) {
-            const int64_t i = (int64_t)(r0 + r) * a.cols + c0 + col;
-            u = a.momentum[i];
-            if (c.nesterov) u = fmaf(c.mu, u, c.omu * (grad_value(a.grad, c.grad_type, i) * scale));
-            u = (float)((double)u * unit);
-        }
-        tile[r][col] = u;
-    }
+    if (c.grad_type == RFAST_TYPE_F32) begin_tile<float>(a, c, r0, c0, scale, f1, f2, tile);
+    else if (c.grad_type == RFAST_TYPE_BF16) begin_tile<__nv_bfloat16>(a, c, r0, c0, scale, f1, f2, tile);
+    else begin_tile<__half>(a, c, r0, c0, scale, f1, f2, tile);
     __syncthreads();
     const MuonGroup& g = q.g[a.group];
     const bool turned = a.rows > a.cols;
     __half* x = (__half*)(q.work + g.x) + (int64_t)a.slot * g.m * g.np;
     const int i0 = turned ? c0 : r0, j0 = turned ? r0 : c0;
-#pragma unroll 4
-    for (int e = threadIdx.x; e < 64 * 32; e += 256) {
-        const int i = e >> 5, j = (e & 31) * 2;
-        if (i0 + i >= g.m || j0 + j >= g.n) continue;
-        const float2 v = turned ? make_float2(tile[j][i], tile[j + 1][i]) : make_float2(tile[i][j], tile[i][j + 1]);
-        const __half2 high = __floats2half2_rn(v.x, v.y);
-        __half2* to = reinterpret_cast<__half2*>(x + (int64_t)(i0 + i) * g.np + j0 + j);
-        *to = high;
-        if (c.terms == 2) {
-            const float2 f = __half22float2(high);
-            to[g.x_plane / 2] = __floats2half2_rn(v.x - f.x, v.y - f.y);
-        }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {                           // 64 rows of X, eight values a thread
+        const int i = (threadIdx.x >> 3) + 32 * u, j = (threadIdx.x & 7) * 8;
+        if (i0 + i >= g.m || j0 + j >= g.np) continue;
+        float v[8];
+#pragma unroll
+        for (int w = 0; w < 8; ++w) v[w] = turned ? tile[j + w][i] : tile[i][j + w];
+        __half* const to = x + (int64_t)(i0 + i) * g.np + j0 + j;
+        if (c.terms == 2) keep8<2>(to, g.x_plane, v); else keep8<1>(to, 0, v);
     }
 }
 
@@ -262,12 +302,68 @@ __device__ __forceinline__ Tile tile_at(const MuonGemm& p, int t) {
     return r;
 }
 
-__device__ __forceinline__ float joined(__half high, __half low) { return __half2float(high) + __half2float(low); }
+// A warp finishes 32 x 32 sums at a time, which it has staged in shared memory: lane l takes eight neighbours, columns 8 (l & 3) on, of
+// rows (l >> 2) + 8 k, k < 4.  The same holds for the transposed block.  33 values a row put the 32 lanes on 32 banks both ways.
+__device__ __forceinline__ void staged(const float (*st)[33], int row, int col, float (&v)[8]) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = st[row][col + k];
+}
+__device__ __forceinline__ void staged_turned(const float (*st)[33], int row, int col, float (&v)[8]) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = st[col + k][row];
+}
+// of a block on the diagonal of a symmetric product: the value at or below the diagonal stands for both
+__device__ __forceinline__ void staged_lower(const float (*st)[33], int row, int col, float (&v)[8]) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = row >= col + k ? st[row][col + k] : st[col + k][row];
+}
 
-// p = p keep - step x for 32 x 32 values of X: along the parameter's rows, so that a lane has a column of X or, where X is the
-// parameter's transpose, a row.
+// What a block's finish reads from memory, fetched while the sums are formed: A for B, the parameters for the update.
+template <int OP, int TERMS>
+struct Ahead {
+    __device__ __forceinline__ void load(const MuonGemm&, const MuonGroup&, int, const MuonMat*, int, int) {}
+};
+template <int TERMS>
+struct Ahead<kPoly, TERMS> {
+    uint4 q[4 * TERMS];
+    __device__ __forceinline__ void load(const MuonGemm& p, const MuonGroup& g, int slot, const MuonMat*, int row0, int col0) {
+        const int lane = threadIdx.x & 31, col = col0 + 8 * (lane & 3);
+        const __half* a = (const __half*)(p.work + g.s) + (int64_t)slot * g.m * g.mp + col;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int row = row0 + 8 * k + (lane >> 2);
+            const bool in = row < g.m && col < g.mp;
+#pragma unroll
+            for (int h = 0; h < TERMS; ++h) q[4 * h + k] = in ? __ldcg(reinterpret_cast<const uint4*>(a + (int64_t)row * g.mp + h * g.s_plane)) : make_uint4(0, 0, 0, 0);
+        }
+    }
+};
+// the parameters eight at a time, along their rows: X's rows, or its columns where X is their transpose
+template <int TERMS>
+struct Ahead<kUpdate, TERMS> {
+    uint4 q[8];                        // fp32 takes two a group, 16-bit types one
+    __device__ __forceinline__ void load(const MuonGemm& p, const MuonGroup& g, int, const MuonMat* mat, int row0, int col0) {
+        if (!mat->wide) return;
+        const int lane = threadIdx.x & 31;
+        const bool turned = mat->rows > mat->cols;
+        const int r0 = (turned ? col0 : row0) + (lane >> 2), c = (turned ? row0 : col0) + 8 * (lane & 3);
+        const int values = p.param_type == RFAST_TYPE_F32 ? 4 : 2;
+        const char* at = (const char*)mat->param + ((int64_t)r0 * mat->cols + c) * values;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (r0 + 8 * k >= mat->rows || c >= mat->cols) continue;
+            const uint4* f = reinterpret_cast<const uint4*>(at + (int64_t)8 * k * mat->cols * values);
+            q[k] = f[0];
+            if (values == 4) q[4 + k] = f[1];
+        }
+    }
+};
+
+__device__ __forceinline__ void half8(uint4 q, float (&v)[8]) { unpack8(Raw8<__half>{q}, v); }
+
+// One value at a time: rows whose length or place does not allow for eight.
 template <class T>
-__device__ __forceinline__ void update_tile(T* __restrict__ param, const float (*st)[33], int row0, int col0, int m, int n, bool turned, float step, float keep) {
+__device__ __noinline__ void update_narrow(T* param, const float (*st)[33], int row0, int col0, int m, int n, bool turned, float step, float keep) {
     const int lane = threadIdx.x & 31;
     T* const w = param + (turned ? (int64_t)col0 * m + row0 + lane : (int64_t)row0 * n + col0 + lane);
     const int64_t next = turned ? m : n;
@@ -281,6 +377,97 @@ __device__ __forceinline__ void update_tile(T* __restrict__ param, const float (
 #pragma unroll
         for (int u = 0; u < 16; ++u)
             if (part + u < rows) w[(part + u) * next] = rounded<T>(fmaf(-step, turned ? st[lane][part + u] : st[part + u][lane], value_of(old[u]) * keep));
+    }
+}
+
+template <int OP, int TERMS>
+__device__ __forceinline__ void finish_block(const MuonGemm& p, const MuonGroup& g, int slot, const MuonMat* mat, int row0, int col0, float (*st)[33], const Ahead<OP, TERMS>& now) {
+    const int lane = threadIdx.x & 31, r = lane >> 2, c = 8 * (lane & 3);
+    if constexpr (OP == kGram || OP == kPoly) {
+        // the block and its mirror image; B holds a on the diagonal, so that B X is the next X
+        __half* const to = (__half*)(p.work + g.s) + (OP == kPoly ? TERMS * g.s_plane : 0) + (int64_t)slot * g.m * g.mp;
+        const bool diagonal = row0 == col0;
+        float v[4][8];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (diagonal) staged_lower(st, r + 8 * k, c, v[k]); else staged(st, r + 8 * k, c, v[k]);
+            if constexpr (OP == kPoly) {
+                float a[8];
+                half8(now.q[k], a);
+                if constexpr (TERMS == 2) {
+                    float low[8];
+                    half8(now.q[4 + k], low);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) a[e] += low[e];
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    v[k][e] = fmaf(kB, a[e], v[k][e] * (kC / kSUnit));
+                    if (diagonal && r + 8 * k == c + e) v[k][e] += kA * kSUnit;
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[k][e] *= kSUnit / (kXUnit * kXUnit);
+            }
+            if (row0 + r + 8 * k < g.m && col0 + c < g.mp) keep8<TERMS>(to + (int64_t)(row0 + r + 8 * k) * g.mp + col0 + c, g.s_plane, v[k]);
+        }
+        if (diagonal) return;
+        __syncwarp();
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) st[r + 8 * k][c + e] = v[k][e];
+        __syncwarp();
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            float t[8];
+            staged_turned(st, r + 8 * k, c, t);
+            if (col0 + r + 8 * k < g.m && row0 + c < g.mp) keep8<TERMS>(to + (int64_t)(col0 + r + 8 * k) * g.mp + row0 + c, g.s_plane, t);
+        }
+    } else if constexpr (OP == kApply) {
+        __half* const to = (__half*)(p.work + g.x) + (p.in ^ 1) * TERMS * g.x_plane + (int64_t)slot * g.m * g.np;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            float v[8];
+            staged(st, r + 8 * k, c, v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] *= 1.f / kSUnit;
+            if (row0 + r + 8 * k < g.m && col0 + c < g.np) keep8<TERMS>(to + (int64_t)(row0 + r + 8 * k) * g.np + col0 + c, g.x_plane, v);
+        }
+    } else {
+        const float step = mat->step * (1.f / (kSUnit * kXUnit));
+        const bool turned = mat->rows > mat->cols;
+        if (!mat->wide) {
+            if (p.param_type == RFAST_TYPE_F32) update_narrow((float*)mat->param, st, row0, col0, g.m, g.n, turned, step, p.keep);
+            else if (p.param_type == RFAST_TYPE_BF16) update_narrow((__nv_bfloat16*)mat->param, st, row0, col0, g.m, g.n, turned, step, p.keep);
+            else update_narrow((__half*)mat->param, st, row0, col0, g.m, g.n, turned, step, p.keep);
+            return;
+        }
+        const int r0 = (turned ? col0 : row0) + r, c0 = (turned ? row0 : col0) + c;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (r0 + 8 * k >= mat->rows || c0 >= mat->cols) continue;
+            float x[8], w[8];
+            if (turned) staged_turned(st, r + 8 * k, c, x); else staged(st, r + 8 * k, c, x);
+            const int64_t o = (int64_t)(r0 + 8 * k) * mat->cols + c0;
+            if (p.param_type == RFAST_TYPE_F32) {
+                const uint4 a = now.q[k], b = now.q[4 + k];
+                const uint32_t raw[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+                for (int e = 0; e < 8; ++e) w[e] = fmaf(-step, x[e], __uint_as_float(raw[e]) * p.keep);
+                store8((float*)mat->param + o, w);
+            } else if (p.param_type == RFAST_TYPE_BF16) {
+                unpack8(Raw8<__nv_bfloat16>{now.q[k]}, w);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) w[e] = fmaf(-step, x[e], w[e] * p.keep);
+                store8((__nv_bfloat16*)mat->param + o, w);
+            } else {
+                unpack8(Raw8<__half>{now.q[k]}, w);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) w[e] = fmaf(-step, x[e], w[e] * p.keep);
+                store8((__half*)mat->param + o, w);
+            }
+        }
     }
 }
 
@@ -431,124 +618,39 @@ k_muon_product(const __grid_constant__ MuonGemm p) {
                     release();
                 }
                 if (!ok) break;
-            } else if (!wait()) {
-                break;
             }
             const int row0 = at.i * S::kTM + rank * 128 + quarter * 32;
-            __half* const sx = (__half*)(p.work + g.s) + (int64_t)at.mat * g.m * g.mp;                    // A
-            __half* const x_in = (__half*)(p.work + g.x) + p.in * TERMS * g.x_plane + (int64_t)at.mat * g.m * g.np;
-            __half* const x_out = (__half*)(p.work + g.x) + (p.in ^ 1) * TERMS * g.x_plane + (int64_t)at.mat * g.m * g.np;
+            const auto kept = [&](int ch) {                 // whether anything of a chunk is
+                const int col0 = at.j * S::kTN + column(ch);
+                return row0 < g.m && (kSym ? col0 <= row0 : col0 < g.n);
+            };
+            const MuonMat* const mat = OP == kUpdate ? p.mats + g.mat0 + at.mat : nullptr;
+            Ahead<OP, TERMS> ahead;
+            const auto fetch = [&](int ch) {
+                if ((OP == kPoly || OP == kUpdate) && kept(ch)) ahead.load(p, g, at.mat, mat, row0, at.j * S::kTN + column(ch));
+            };
+            fetch(0);
+            if (!kSegmented && !wait()) break;
 #pragma unroll
             for (int ch = 0; ch < kChunks; ++ch) {
                 const int col0 = at.j * S::kTN + column(ch);
-                if (row0 >= g.m || (kSym ? col0 > row0 + 31 : col0 >= g.n)) continue;    // nothing of it is kept
-                float v[32];
-                if (kSegmented) {
+                if (kept(ch)) {
+                    float v[32];
+                    if (kSegmented) {
 #pragma unroll
-                    for (int c = 0; c < 32; ++c) v[c] = total[kSegmented ? ch : 0][c];
-                } else {
-                    read(ch, v);
-                }
-                if (kSym) {
-                    // lane: a row i; column j: the value is kept at (i, j) and at (j, i), j <= i
-                    const int i = row0 + lane;
-                    __half* const to = sx + (OP == kPoly ? TERMS * g.s_plane : 0);
-                    const int64_t m0 = (int64_t)col0 * g.mp + i;           // of (col0, i); a column is mp values on
-                    const int last = i < g.m ? i - col0 : -1;              // columns up to this one are kept
-                    __half a_high[32], a_low[32];
-                    if (OP == kPoly) {
-#pragma unroll
-                        for (int c = 0; c < 32; ++c) {
-                            a_high[c] = c <= last ? __ldcg(sx + m0 + (int64_t)c * g.mp) : __half(0.f);
-                            if (TERMS == 2) a_low[c] = c <= last ? __ldcg(sx + g.s_plane + m0 + (int64_t)c * g.mp) : __half(0.f);
-                        }
+                        for (int c = 0; c < 32; ++c) v[c] = total[kSegmented ? ch : 0][c];
+                    } else {
+                        read(ch, v);
                     }
-#pragma unroll
-                    for (int c = 0; c < 32; ++c) {
-                        const float f = OP == kGram ? v[c] * (kSUnit / (kXUnit * kXUnit))
-                                                    : fmaf(kB, TERMS == 2 ? joined(a_high[c], a_low[c]) : __half2float(a_high[c]), v[c] * (kC / kSUnit));
-                        if (c <= last) {
-                            const __half high = __float2half_rn(f);
-                            to[m0 + (int64_t)c * g.mp] = high;
-                            if (TERMS == 2) to[m0 + (int64_t)c * g.mp + g.s_plane] = __float2half_rn(f - __half2float(high));
-                        }
-                        st[lane][c] = f;
-                    }
-                    __syncwarp();
-#pragma unroll 4
-                    for (int s2 = 0; s2 < 16; ++s2) {
-                        const int r = 2 * s2 + (lane >> 4), c = 2 * (lane & 15), ii = row0 + r, jj = col0 + c;
-                        if (ii < g.m && jj <= ii) {
-                            const float f0 = st[r][c], f1 = st[r][c + 1];
-                            const __half2 high = __floats2half2_rn(f0, f1);
-                            __half* d = to + (int64_t)ii * g.mp + jj;
-                            const float2 f = __half22float2(high);
-                            const __half2 low = __floats2half2_rn(f0 - f.x, f1 - f.y);
-                            if (jj + 1 <= ii) {
-                                *reinterpret_cast<__half2*>(d) = high;
-                                if (TERMS == 2) *reinterpret_cast<__half2*>(d + g.s_plane) = low;
-                            } else {
-                                *d = __low2half(high);
-                                if (TERMS == 2) d[g.s_plane] = __low2half(low);
-                            }
-                        }
-                    }
-                    __syncwarp();
-                } else {
 #pragma unroll
                     for (int c = 0; c < 32; ++c) st[lane][c] = v[c];
                     __syncwarp();
-                    const MuonMat* mat = nullptr;
-                    bool turned = false;
-                    if (OP == kUpdate) {
-                        mat = p.mats + g.mat0 + at.mat;
-                        turned = mat->rows > mat->cols;
-                    }
-                    // lanes 0 .. 15 take a row, lanes 16 .. 31 the next, two columns each
-                    const int c = 2 * (lane & 15), jj = col0 + c, r0 = lane >> 4;
-#pragma unroll
-                    for (int part = 0; part < 2; ++part) {
-                        __half2 high[8], low[8];
-#pragma unroll
-                        for (int u = 0; u < 8; ++u) {
-                            const int ii = row0 + part * 16 + 2 * u + r0;
-                            const int64_t o = (int64_t)ii * g.np + jj;
-                            const bool in = ii < g.m && jj < g.n;
-                            high[u] = in ? __ldcg(reinterpret_cast<const __half2*>(x_in + o)) : __half2(0.f, 0.f);
-                            if (TERMS == 2) low[u] = in ? __ldcg(reinterpret_cast<const __half2*>(x_in + o + g.x_plane)) : __half2(0.f, 0.f);
-                        }
-#pragma unroll
-                        for (int u = 0; u < 8; ++u) {
-                            const int r = part * 16 + 2 * u + r0, ii = row0 + r;
-                            float2 x = __half22float2(high[u]);
-                            if (TERMS == 2) {
-                                const float2 l = __half22float2(low[u]);
-                                x.x += l.x;
-                                x.y += l.y;
-                            }
-                            const float f0 = fmaf(kA, x.x, st[r][c] * (1.f / kSUnit)), f1 = fmaf(kA, x.y, st[r][c + 1] * (1.f / kSUnit));
-                            if (OP == kUpdate) {
-                                st[r][c] = f0;
-                                st[r][c + 1] = f1;
-                            } else if (ii < g.m && jj < g.n) {
-                                const int64_t o = (int64_t)ii * g.np + jj;
-                                const __half2 h = __floats2half2_rn(f0, f1);
-                                *reinterpret_cast<__half2*>(x_out + o) = h;
-                                if (TERMS == 2) {
-                                    const float2 f = __half22float2(h);
-                                    *reinterpret_cast<__half2*>(x_out + o + g.x_plane) = __floats2half2_rn(f0 - f.x, f1 - f.y);
-                                }
-                            }
-                        }
-                    }
+                    const Ahead<OP, TERMS> now = ahead;
+                    if (ch + 1 < kChunks) fetch(ch + 1);
+                    finish_block<OP, TERMS>(p, g, at.mat, mat, row0, col0, st, now);
                     __syncwarp();
-                    if (OP == kUpdate) {
-                        const float step = mat->step * (1.f / kXUnit);
-                        if (p.param_type == RFAST_TYPE_F32) update_tile((float*)mat->param, st, row0, col0, g.m, g.n, turned, step, p.keep);
-                        else if (p.param_type == RFAST_TYPE_BF16) update_tile((__nv_bfloat16*)mat->param, st, row0, col0, g.m, g.n, turned, step, p.keep);
-                        else update_tile((__half*)mat->param, st, row0, col0, g.m, g.n, turned, step, p.keep);
-                        __syncwarp();
-                    }
+                } else if (ch + 1 < kChunks) {
+                    fetch(ch + 1);
                 }
             }
             if (!kSegmented) release();
@@ -723,7 +825,7 @@ cudaError_t muon_run(const rfast_muon* a, const MuonRun& r, char* work, bool fir
             const double size = a->size_rule == RFAST_MUON_SIZE_RMS ? 0.2 * std::sqrt((double)r.g[g].n)
                                                                     : std::sqrt(m.rows > m.cols ? (double)m.rows / m.cols : 1.0);
             m.step = (float)(a->lr * size);
-            m.part0 = part;
+            m.wide = m.cols % 8 == 0 && (uintptr_t)m.param % 16 == 0;
             t.part0[at] = part;
             t.tile0[at] = tile;
             part += (int)parts_of(m.rows, m.cols);
