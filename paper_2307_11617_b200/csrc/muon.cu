@@ -53,7 +53,7 @@ struct MuonMat {
     int rows, cols;
     int group, slot;
     float step;                        // lr * size
-    int wide;                          // eight parameters at a time: cols in eights, address a multiple of 16 bytes
+    int wide;                          // 32 bytes of a row at a time
 };
 struct MuonTable {
     MuonMat mat[kMats];
@@ -302,20 +302,31 @@ __device__ __forceinline__ Tile tile_at(const MuonGemm& p, int t) {
     return r;
 }
 
-// A warp finishes 32 x 32 sums at a time, which it has staged in shared memory: lane l takes eight neighbours, columns 8 (l & 3) on, of
-// rows (l >> 2) + 8 k, k < 4.  The same holds for the transposed block.  33 values a row put the 32 lanes on 32 banks both ways.
-__device__ __forceinline__ void staged(const float (*st)[33], int row, int col, float (&v)[8]) {
+// A warp finishes 32 x 32 sums at a time, straight from the registers that tensor memory is read into: a lane has a row of X, A or B, 32
+// neighbours, whole 32-byte sectors.  (Staging them in shared memory for longer runs was four times slower: the operands' reads
+// and the loads' writes take all of its bandwidth.)
+
+// 32 values as one or two fp16 numbers each; `values` of them are stored, in sixteens (a row's room is a multiple of that).
+template <int TERMS>
+__device__ __forceinline__ void keep32(__half* to, int64_t low_plane, const float (&v)[32], int values) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = st[row][col + k];
-}
-__device__ __forceinline__ void staged_turned(const float (*st)[33], int row, int col, float (&v)[8]) {
+    for (int q = 0; q < 2; ++q) {
+        if (q * 16 >= values) break;
+        uint32_t high[8], low[8];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = st[col + k][row];
-}
-// of a block on the diagonal of a symmetric product: the value at or below the diagonal stands for both
-__device__ __forceinline__ void staged_lower(const float (*st)[33], int row, int col, float (&v)[8]) {
-#pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = row >= col + k ? st[row][col + k] : st[col + k][row];
+        for (int k = 0; k < 8; ++k) {
+            const float a = v[16 * q + 2 * k], b = v[16 * q + 2 * k + 1];
+            const __half2 h = __floats2half2_rn(a, b);
+            high[k] = *reinterpret_cast<const uint32_t*>(&h);
+            if (TERMS == 2) {
+                const float2 f = __half22float2(h);
+                const __half2 l = __floats2half2_rn(a - f.x, b - f.y);
+                low[k] = *reinterpret_cast<const uint32_t*>(&l);
+            }
+        }
+        store32(to + 16 * q, high);
+        if (TERMS == 2) store32(to + 16 * q + low_plane, low);
+    }
 }
 
 // What a block's finish reads from memory, fetched while the sums are formed: A for B, the parameters for the update.
@@ -325,151 +336,146 @@ struct Ahead {
 };
 template <int TERMS>
 struct Ahead<kPoly, TERMS> {
-    uint4 q[4 * TERMS];
+    uint32_t q[2 * TERMS][8];
     __device__ __forceinline__ void load(const MuonGemm& p, const MuonGroup& g, int slot, const MuonMat*, int row0, int col0) {
-        const int lane = threadIdx.x & 31, col = col0 + 8 * (lane & 3);
-        const __half* a = (const __half*)(p.work + g.s) + (int64_t)slot * g.m * g.mp + col;
+        const int row = row0 + (threadIdx.x & 31);
+        const __half* a = (const __half*)(p.work + g.s) + (int64_t)slot * g.m * g.mp + (int64_t)row * g.mp + col0;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int row = row0 + 8 * k + (lane >> 2);
-            const bool in = row < g.m && col < g.mp;
+        for (int k = 0; k < 2; ++k)
+            if (row < g.m && col0 + 16 * k < g.mp)
 #pragma unroll
-            for (int h = 0; h < TERMS; ++h) q[4 * h + k] = in ? __ldcg(reinterpret_cast<const uint4*>(a + (int64_t)row * g.mp + h * g.s_plane)) : make_uint4(0, 0, 0, 0);
-        }
+                for (int h = 0; h < TERMS; ++h) load32(a + 16 * k + h * g.s_plane, q[2 * h + k]);
     }
 };
-// the parameters eight at a time, along their rows: X's rows, or its columns where X is their transpose
 template <int TERMS>
 struct Ahead<kUpdate, TERMS> {
-    uint4 q[8];                        // fp32 takes two a group, 16-bit types one
+    uint32_t q[4][8];                  // 32 parameters of a lane's row: fp32 fills all, 16-bit types half
     __device__ __forceinline__ void load(const MuonGemm& p, const MuonGroup& g, int, const MuonMat* mat, int row0, int col0) {
         if (!mat->wide) return;
-        const int lane = threadIdx.x & 31;
-        const bool turned = mat->rows > mat->cols;
-        const int r0 = (turned ? col0 : row0) + (lane >> 2), c = (turned ? row0 : col0) + 8 * (lane & 3);
-        const int values = p.param_type == RFAST_TYPE_F32 ? 4 : 2;
-        const char* at = (const char*)mat->param + ((int64_t)r0 * mat->cols + c) * values;
+        const int row = row0 + (threadIdx.x & 31), values = p.param_type == RFAST_TYPE_F32 ? 8 : 16;      // of 32 bytes
+        if (row >= g.m) return;
+        const char* at = (const char*)mat->param + ((int64_t)row * g.n + col0) * (32 / values);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            if (r0 + 8 * k >= mat->rows || c >= mat->cols) continue;
-            const uint4* f = reinterpret_cast<const uint4*>(at + (int64_t)8 * k * mat->cols * values);
-            q[k] = f[0];
-            if (values == 4) q[4 + k] = f[1];
-        }
+        for (int k = 0; k < 4; ++k)
+            if (k * values < 32 && col0 + k * values < g.n) load32(at + 32 * k, q[k]);
     }
 };
 
-__device__ __forceinline__ void half8(uint4 q, float (&v)[8]) { unpack8(Raw8<__half>{q}, v); }
-
-// One value at a time: rows whose length or place does not allow for eight.
+// Parameters one at a time, a lane a column of the parameter's: X's row, where X is its transpose, from registers ...
 template <class T>
-__device__ __noinline__ void update_narrow(T* param, const float (*st)[33], int row0, int col0, int m, int n, bool turned, float step, float keep) {
-    const int lane = threadIdx.x & 31;
-    T* const w = param + (turned ? (int64_t)col0 * m + row0 + lane : (int64_t)row0 * n + col0 + lane);
-    const int64_t next = turned ? m : n;
-    const int rows = turned ? (row0 + lane < m ? n - col0 : 0) : (col0 + lane < n ? m - row0 : 0);
+__device__ __forceinline__ void update_turned(T* __restrict__ param, const float (&v)[32], int row, int col0, int m, int n, float step, float keep) {
+    if (row >= m) return;
+    T* const w = param + (int64_t)col0 * m + row;
 #pragma unroll
     for (int part = 0; part < 32; part += 16) {
         T old[16];
 #pragma unroll
         for (int u = 0; u < 16; ++u)
-            if (part + u < rows) old[u] = w[(part + u) * next];
+            if (col0 + part + u < n) old[u] = w[(int64_t)(part + u) * m];
 #pragma unroll
         for (int u = 0; u < 16; ++u)
-            if (part + u < rows) w[(part + u) * next] = rounded<T>(fmaf(-step, turned ? st[lane][part + u] : st[part + u][lane], value_of(old[u]) * keep));
+            if (col0 + part + u < n) w[(int64_t)(part + u) * m] = rounded<T>(fmaf(-step, v[part + u], value_of(old[u]) * keep));
+    }
+}
+// ... or X's column, through shared memory: rows whose length or place does not allow for 32 bytes at a time.
+template <class T>
+__device__ __forceinline__ void update_narrow(T* param, const float (*st)[33], int row0, int col, int m, int n, float step, float keep) {
+    if (col >= n) return;
+    T* const w = param + (int64_t)row0 * n + col;
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int part = 0; part < 32; part += 8) {
+        T old[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            if (row0 + part + u < m) old[u] = w[(int64_t)(part + u) * n];
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            if (row0 + part + u < m) w[(int64_t)(part + u) * n] = rounded<T>(fmaf(-step, st[part + u][lane], value_of(old[u]) * keep));
+    }
+}
+template <class T> __device__ __forceinline__ float2 two_values(uint32_t r);
+template <> __device__ __forceinline__ float2 two_values<__half>(uint32_t r) { return __half22float2(*reinterpret_cast<const __half2*>(&r)); }
+template <> __device__ __forceinline__ float2 two_values<__nv_bfloat16>(uint32_t r) { return make_float2(__uint_as_float(r << 16), __uint_as_float(r & 0xffff0000u)); }
+
+template <class T, int TERMS>
+__device__ __forceinline__ void update_block(const MuonMat* mat, const MuonGroup& g, int row0, int col0, float (&v)[32], float (*st)[33], const Ahead<kUpdate, TERMS>& now, float keep) {
+    const int lane = threadIdx.x & 31, row = row0 + lane;
+    const float step = mat->step * (1.f / (kSUnit * kXUnit));
+    T* const param = (T*)mat->param;
+    if (mat->rows > mat->cols) {
+        update_turned(param, v, row, col0, g.m, g.n, step, keep);
+    } else if (mat->wide) {
+        if (row >= g.m) return;
+        T* const to = param + (int64_t)row * g.n + col0;
+        constexpr int kValues = 32 / (int)sizeof(T);
+#pragma unroll
+        for (int k = 0; k < 32 / kValues; ++k) {
+            if (col0 + k * kValues >= g.n) break;
+            uint32_t r[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                if constexpr (sizeof(T) == 4) {
+                    r[e] = __float_as_uint(fmaf(-step, v[k * 8 + e], __uint_as_float(now.q[k][e]) * keep));
+                } else {
+                    const float2 w = two_values<T>(now.q[k][e]);
+                    r[e] = packed(fmaf(-step, v[k * 16 + 2 * e], w.x * keep), fmaf(-step, v[k * 16 + 2 * e + 1], w.y * keep), (const T*)nullptr);
+                }
+            }
+            store32(to + k * kValues, r);
+        }
+    } else {
+#pragma unroll
+        for (int c = 0; c < 32; ++c) st[lane][c] = v[c];
+        __syncwarp();
+        update_narrow(param, st, row0, col0 + lane, g.m, g.n, step, keep);
+        __syncwarp();
     }
 }
 
 template <int OP, int TERMS>
-__device__ __forceinline__ void finish_block(const MuonGemm& p, const MuonGroup& g, int slot, const MuonMat* mat, int row0, int col0, float (*st)[33], const Ahead<OP, TERMS>& now) {
-    const int lane = threadIdx.x & 31, r = lane >> 2, c = 8 * (lane & 3);
+__device__ __forceinline__ void finish_block(const MuonGemm& p, const MuonGroup& g, int slot, const MuonMat* mat, int row0, int col0, float (&v)[32], float (*st)[33], const Ahead<OP, TERMS>& now) {
+    const int lane = threadIdx.x & 31, row = row0 + lane;
     if constexpr (OP == kGram || OP == kPoly) {
-        // the block and its mirror image; B holds a on the diagonal, so that B X is the next X
-        __half* const to = (__half*)(p.work + g.s) + (OP == kPoly ? TERMS * g.s_plane : 0) + (int64_t)slot * g.m * g.mp;
-        const bool diagonal = row0 == col0;
-        float v[4][8];
+        // B holds a on the diagonal, so that B X is the next X
+        __half* const to = (__half*)(p.work + g.s) + (OP == kPoly ? TERMS * g.s_plane : 0) + (int64_t)slot * g.m * g.mp + (int64_t)row * g.mp + col0;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            if (diagonal) staged_lower(st, r + 8 * k, c, v[k]); else staged(st, r + 8 * k, c, v[k]);
+        for (int c = 0; c < 32; c += 2) {
             if constexpr (OP == kPoly) {
-                float a[8];
-                half8(now.q[k], a);
+                float2 a = two_values<__half>(now.q[c / 16][c / 2 % 8]);
                 if constexpr (TERMS == 2) {
-                    float low[8];
-                    half8(now.q[4 + k], low);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) a[e] += low[e];
+                    const float2 low = two_values<__half>(now.q[2 + c / 16][c / 2 % 8]);
+                    a.x += low.x;
+                    a.y += low.y;
                 }
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    v[k][e] = fmaf(kB, a[e], v[k][e] * (kC / kSUnit));
-                    if (diagonal && r + 8 * k == c + e) v[k][e] += kA * kSUnit;
+                v[c] = fmaf(kB, a.x, v[c] * (kC / kSUnit));
+                v[c + 1] = fmaf(kB, a.y, v[c + 1] * (kC / kSUnit));
+                if (row0 == col0) {
+                    v[c] += lane == c ? kA * kSUnit : 0.f;
+                    v[c + 1] += lane == c + 1 ? kA * kSUnit : 0.f;
                 }
             } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[k][e] *= kSUnit / (kXUnit * kXUnit);
+                v[c] *= kSUnit / (kXUnit * kXUnit);
+                v[c + 1] *= kSUnit / (kXUnit * kXUnit);
             }
-            if (row0 + r + 8 * k < g.m && col0 + c < g.mp) keep8<TERMS>(to + (int64_t)(row0 + r + 8 * k) * g.mp + col0 + c, g.s_plane, v[k]);
         }
-        if (diagonal) return;
-        __syncwarp();
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) st[r + 8 * k][c + e] = v[k][e];
-        __syncwarp();
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            float t[8];
-            staged_turned(st, r + 8 * k, c, t);
-            if (col0 + r + 8 * k < g.m && row0 + c < g.mp) keep8<TERMS>(to + (int64_t)(col0 + r + 8 * k) * g.mp + row0 + c, g.s_plane, t);
-        }
+        if (row < g.m) keep32<TERMS>(to, g.s_plane, v, g.mp - col0);
     } else if constexpr (OP == kApply) {
-        __half* const to = (__half*)(p.work + g.x) + (p.in ^ 1) * TERMS * g.x_plane + (int64_t)slot * g.m * g.np;
+        __half* const to = (__half*)(p.work + g.x) + (p.in ^ 1) * TERMS * g.x_plane + (int64_t)slot * g.m * g.np + (int64_t)row * g.np + col0;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            float v[8];
-            staged(st, r + 8 * k, c, v);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] *= 1.f / kSUnit;
-            if (row0 + r + 8 * k < g.m && col0 + c < g.np) keep8<TERMS>(to + (int64_t)(row0 + r + 8 * k) * g.np + col0 + c, g.x_plane, v);
-        }
+        for (int c = 0; c < 32; ++c) v[c] *= 1.f / kSUnit;
+        if (row < g.m) keep32<TERMS>(to, g.x_plane, v, g.np - col0);
     } else {
-        const float step = mat->step * (1.f / (kSUnit * kXUnit));
-        const bool turned = mat->rows > mat->cols;
-        if (!mat->wide) {
-            if (p.param_type == RFAST_TYPE_F32) update_narrow((float*)mat->param, st, row0, col0, g.m, g.n, turned, step, p.keep);
-            else if (p.param_type == RFAST_TYPE_BF16) update_narrow((__nv_bfloat16*)mat->param, st, row0, col0, g.m, g.n, turned, step, p.keep);
-            else update_narrow((__half*)mat->param, st, row0, col0, g.m, g.n, turned, step, p.keep);
-            return;
-        }
-        const int r0 = (turned ? col0 : row0) + r, c0 = (turned ? row0 : col0) + c;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            if (r0 + 8 * k >= mat->rows || c0 >= mat->cols) continue;
-            float x[8], w[8];
-            if (turned) staged_turned(st, r + 8 * k, c, x); else staged(st, r + 8 * k, c, x);
-            const int64_t o = (int64_t)(r0 + 8 * k) * mat->cols + c0;
-            if (p.param_type == RFAST_TYPE_F32) {
-                const uint4 a = now.q[k], b = now.q[4 + k];
-                const uint32_t raw[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-                for (int e = 0; e < 8; ++e) w[e] = fmaf(-step, x[e], __uint_as_float(raw[e]) * p.keep);
-                store8((float*)mat->param + o, w);
-            } else if (p.param_type == RFAST_TYPE_BF16) {
-                unpack8(Raw8<__nv_bfloat16>{now.q[k]}, w);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) w[e] = fmaf(-step, x[e], w[e] * p.keep);
-                store8((__nv_bfloat16*)mat->param + o, w);
-            } else {
-                unpack8(Raw8<__half>{now.q[k]}, w);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) w[e] = fmaf(-step, x[e], w[e] * p.keep);
-                store8((__half*)mat->param + o, w);
-            }
-        }
+        if (p.param_type == RFAST_TYPE_F32) update_block<float, TERMS>(mat, g, row0, col0, v, st, now, p.keep);
+        else if (p.param_type == RFAST_TYPE_BF16) update_block<__nv_bfloat16, TERMS>(mat, g, row0, col0, v, st, now, p.keep);
+        else update_block<__half, TERMS>(mat, g, row0, col0, v, st, now, p.keep);
     }
 }
+
+// A and B are stored up to this column in the row tile of `row`: only tiles up to the diagonal are formed.  All products of a run use tiles
+// of one shape, so that an operand's rows lie in one row tile.
+template <class S>
+__device__ __forceinline__ int stored_up_to(int row) { return (row / S::kTM + 1) * S::kTM; }
 
 template <int CG, int TERMS, int OP>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -478,11 +484,11 @@ k_muon_product(const __grid_constant__ MuonGemm p) {
     constexpr bool kSym = OP == kGram || OP == kPoly;
     constexpr bool kSegmented = OP == kGram && TERMS == 2;
     extern __shared__ uint8_t raw[];
-    uint8_t* const base = (uint8_t*)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
+    uint8_t* const base = raw + (0u - tc::smem(raw) & 1023u);      // by an offset: the compiler goes on knowing that this is shared memory
     __shared__ uint64_t full[S::kStages], empty[S::kStages], acc_full[2], acc_empty[2];
     __shared__ uint32_t tmem;
     __shared__ volatile int bad;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const uint32_t rank = CG == 2 ? tc::cluster_rank() : 0;
     int* const status = (int*)p.work;
     if (threadIdx.x == 0) {
@@ -500,86 +506,96 @@ k_muon_product(const __grid_constant__ MuonGemm p) {
     let_follow();
     const int first = blockIdx.x / CG, stride = gridDim.x / CG;
 
-    if (warp == 0) {
-        if (lane == 0) {                                    // ---- loads
-            tc::fence_for_loads();
-            int n = 0;
-            bool ok = true;
-            for (int t = first; t < p.tiles && ok; t += stride) {
-                const Tile at = tile_at<S::kTM, S::kTN, kSym>(p, t);
-                const MuonGroup& g = p.g[at.g];
-                const int blocks = ((OP == kGram ? g.n : g.m) + kBox - 1) / kBox;
-                const int row0 = at.i * S::kTM + rank * 128, col0 = at.j * S::kTN + rank * (S::kTN / CG);
-                for (int kb = 0; kb < blocks; ++kb, ++n) {
-                    const int s = n % S::kStages;
-                    if (n >= S::kStages && !(ok = tc::bar_wait(&empty[s], ((n / S::kStages) - 1) & 1))) break;
-                    const uint32_t bar = CG == 2 ? tc::smem_of(&full[s], 0) : tc::smem(&full[s]);
+    if (warp == 0) {                                        // ---- loads
+        tc::fence_for_loads();
+        const uint32_t bar0 = CG == 2 ? tc::smem_of(full, 0) : tc::smem(full), to0 = tc::smem(base);
+        int s = 0;
+        uint32_t turn = 1;                                  // of the ring: the first goes through without a wait
+        bool ok = true;
+        for (int t = first; t < p.tiles && ok; t += stride) {
+            const Tile at = tile_at<S::kTM, S::kTN, kSym>(p, t);
+            const MuonGroup& g = p.g[at.g];
+            const int blocks = ((OP == kGram ? g.n : g.m) + kBox - 1) / kBox;
+            const int row0 = at.i * S::kTM + rank * 128, col0 = at.j * S::kTN + rank * (S::kTN / CG);
+            const CUtensorMap* const map_a = OP == kGram ? &p.x[at.g] : &p.s[at.g];
+            const CUtensorMap* const map_b = OP == kPoly ? &p.s[at.g] : &p.x[at.g];
+            // which matrix of an array: [buffer][terms][count]
+            const int in_a = at.mat + g.count * TERMS * (OP == kGram ? p.in : OP == kPoly ? 0 : 1);
+            const int in_b = at.mat + g.count * TERMS * (OP == kPoly ? 0 : p.in);
+            const int limit_a = stored_up_to<S>(row0), limit_b = stored_up_to<S>(col0);
+            for (int kb = 0; kb < blocks; ++kb) {
+                if (!(ok = tc::bar_wait(&empty[s], turn))) break;
+                const int k0 = kb * kBox;
+                // A and B above their stored tiles are read as the transposed ones below, rows along the other dimension
+                const bool across_a = OP != kGram && k0 >= limit_a, across_b = OP == kPoly ? k0 >= limit_b : OP != kGram;
+                if (tc::elect()) {
                     if (rank == 0) tc::bar_expect(&full[s], CG * S::kStage);
+                    const uint32_t bar = bar0 + s * 8;
 #pragma unroll
                     for (int h = 0; h < TERMS; ++h) {
-                        uint8_t* to = base + s * S::kStage + h * S::kHalf;
+                        const uint32_t to = to0 + s * S::kStage + h * S::kHalf;
 #pragma unroll
-                        for (int b = 0; b < S::kBoxesA; ++b, to += kBoxBytes) {
-                            if (OP == kGram) tc::load_5d<CG>(to, &p.x[at.g], bar, kb * kBox, row0 + b * kBox, at.mat, h, p.in);
-                            else tc::load_5d<CG>(to, &p.s[at.g], bar, kb * kBox, row0 + b * kBox, at.mat, h, OP == kPoly ? 0 : 1);
-                        }
+                        for (int b = 0; b < S::kBoxesA; ++b)
+                            tc::load_3d<CG>(to + b * kBoxBytes, map_a, bar, across_a ? row0 + b * kBox : k0, across_a ? k0 : row0 + b * kBox, in_a + h * g.count);
 #pragma unroll
-                        for (int b = 0; b < S::kBoxesB; ++b, to += kBoxBytes) {
-                            if (OP == kGram) tc::load_5d<CG>(to, &p.x[at.g], bar, kb * kBox, col0 + b * kBox, at.mat, h, p.in);
-                            else if (OP == kPoly) tc::load_5d<CG>(to, &p.s[at.g], bar, kb * kBox, col0 + b * kBox, at.mat, h, 0);
-                            else tc::load_5d<CG>(to, &p.x[at.g], bar, col0 + b * kBox, kb * kBox, at.mat, h, p.in);
-                        }
+                        for (int b = 0; b < S::kBoxesB; ++b)
+                            tc::load_3d<CG>(to + (S::kBoxesA + b) * kBoxBytes, map_b, bar, across_b ? col0 + b * kBox : k0, across_b ? k0 : col0 + b * kBox, in_b + h * g.count);
                     }
                 }
+                __syncwarp();
+                if (++s == S::kStages) { s = 0; turn ^= 1; }
             }
-            if (!ok) { atomicExch(status, 1); bad = 1; }
         }
+        if (!ok && lane == 0) { atomicExch(status, 1); bad = 1; }
     } else if (warp == 1) {
-        if (lane == 0 && rank == 0) {                       // ---- matrix instructions, of both blocks of a pair
-            constexpr bool kAcross = !kSym;                 // X as the second operand runs along its rows
-            const uint32_t instruction = tc::instruction_f16(S::kTM, S::kTN, kAcross);
-            constexpr uint32_t kLead = kAcross ? kBoxBytes : 16, kNext = kAcross ? 2048 >> 4 : 32 >> 4;
-            int n = 0, sums = 0;                            // stages, sums begun
+        if (rank == 0) {                                    // ---- matrix instructions, of both blocks of a pair
+            constexpr uint32_t kAlong = 32 >> 4, kAcross = 2048 >> 4;                   // 16 steps of the sum, by the rows' direction
+            const uint64_t a_first = tc::operand(tc::smem(base), kBoxBytes), b_first = tc::operand(tc::smem(base) + S::kBoxesA * kBoxBytes, kBoxBytes);
+            int s = 0, sums = 0;                            // stage, sums begun
+            uint32_t turn = 0;
             bool ok = true;
             for (int t = first; t < p.tiles && ok; t += stride) {
                 const Tile at = tile_at<S::kTM, S::kTN, kSym>(p, t);
-                const MuonGroup& g = p.g[at.g];
-                const int blocks = ((OP == kGram ? g.n : g.m) + kBox - 1) / kBox;
-                uint32_t to = 0;
-                int buf = 0;
-                for (int kb = 0; kb < blocks; ++kb, ++n) {
+                const int blocks = ((OP == kGram ? p.g[at.g].n : p.g[at.g].m) + kBox - 1) / kBox;
+                const int limit_a = stored_up_to<S>(at.i * S::kTM), limit_b = stored_up_to<S>(at.j * S::kTN);
+                uint32_t to = 0, buf = 0;
+                for (int kb = 0; kb < blocks; ++kb) {
                     const bool begin = kSegmented ? kb % kSegment == 0 : kb == 0;
                     if (begin) {
                         buf = sums & 1;
-                        if (sums >= 2 && !(ok = tc::bar_wait(&acc_empty[buf], ((sums >> 1) - 1) & 1))) break;
-                        tc::fence_after();
+                        if (!(ok = tc::bar_wait(&acc_empty[buf], ~(sums >> 1) & 1))) break;
                         to = acc + buf * S::kTN;
                         ++sums;
                     }
-                    const int s = n % S::kStages;
-                    if (!(ok = tc::bar_wait(&full[s], (n / S::kStages) & 1))) break;
+                    if (!(ok = tc::bar_wait(&full[s], turn))) break;
                     tc::fence_after();
-                    const uint32_t sa = tc::smem(base + s * S::kStage), sb = sa + S::kBoxesA * kBoxBytes;
-                    const uint64_t a0 = tc::operand(sa, 16), b0 = tc::operand(sb, kLead);
+                    const bool across_a = OP != kGram && kb * kBox >= limit_a, across_b = OP == kPoly ? kb * kBox >= limit_b : OP != kGram;
+                    const uint32_t instruction = tc::instruction_f16(S::kTM, S::kTN) | (across_a ? tc::kAcrossA : 0u) | (across_b ? tc::kAcrossB : 0u);
+                    const uint32_t next_a = across_a ? kAcross : kAlong, next_b = across_b ? kAcross : kAlong;
+                    if (tc::elect()) {
+                        const uint64_t a0 = a_first + s * (S::kStage >> 4), b0 = b_first + s * (S::kStage >> 4);
 #pragma unroll
-                    for (int k = 0; k < kBox / 16; ++k) tc::mma_f16<CG>(to, a0 + 2 * k, b0 + kNext * k, instruction, begin && k == 0 ? 0u : 1u);
-                    if (TERMS == 2) {
-                        const uint64_t a1 = tc::operand(sa + S::kHalf, 16), b1 = tc::operand(sb + S::kHalf, kLead);
+                        for (int k = 0; k < kBox / 16; ++k) tc::mma_f16<CG>(to, a0 + next_a * k, b0 + next_b * k, instruction, begin && k == 0 ? 0u : 1u);
+                        if (TERMS == 2) {
+                            const uint64_t a1 = a0 + (S::kHalf >> 4), b1 = b0 + (S::kHalf >> 4);
 #pragma unroll
-                        for (int k = 0; k < kBox / 16; ++k) {
-                            tc::mma_f16<CG>(to, a0 + 2 * k, b1 + kNext * k, instruction, 1u);
-                            tc::mma_f16<CG>(to, a1 + 2 * k, b0 + kNext * k, instruction, 1u);
+                            for (int k = 0; k < kBox / 16; ++k) {
+                                tc::mma_f16<CG>(to, a0 + next_a * k, b1 + next_b * k, instruction, 1u);
+                                tc::mma_f16<CG>(to, a1 + next_a * k, b0 + next_b * k, instruction, 1u);
+                            }
                         }
+                        tc::commit<CG>(&empty[s]);
+                        if (kb + 1 == blocks || (kSegmented && (kb + 1) % kSegment == 0)) tc::commit<CG>(&acc_full[buf]);
                     }
-                    tc::commit<CG>(&empty[s]);
-                    if (kb + 1 == blocks || (kSegmented && (kb + 1) % kSegment == 0)) tc::commit<CG>(&acc_full[buf]);
+                    __syncwarp();
+                    if (++s == S::kStages) { s = 0; turn ^= 1; }
                 }
             }
-            if (!ok) { atomicExch(status, 2); bad = 1; }
+            if (!ok && lane == 0) { atomicExch(status, 2); bad = 1; }
         }
     } else {                                                // ---- sums out of tensor memory
         const int quarter = warp & 3, half = (warp - 2) >> 2;
-        float (*const st)[33] = (float (*)[33])(base + S::kStages * S::kStage + (warp - 2) * S::kStaged);
+        float (*const st)[33] = (float (*)[33])(base + S::kStages * S::kStage + (warp - 2) * S::kStaged);     // update_narrow's
         constexpr int kChunks = S::kTN / 64;                // of 32 columns, of a warp
         int sums = 0;                                       // read so far
         const auto wait = [&] {
@@ -622,7 +638,7 @@ k_muon_product(const __grid_constant__ MuonGemm p) {
             const int row0 = at.i * S::kTM + rank * 128 + quarter * 32;
             const auto kept = [&](int ch) {                 // whether anything of a chunk is
                 const int col0 = at.j * S::kTN + column(ch);
-                return row0 < g.m && (kSym ? col0 <= row0 : col0 < g.n);
+                return row0 < g.m && col0 < (kSym ? g.m : g.n);
             };
             const MuonMat* const mat = OP == kUpdate ? p.mats + g.mat0 + at.mat : nullptr;
             Ahead<OP, TERMS> ahead;
@@ -642,13 +658,9 @@ k_muon_product(const __grid_constant__ MuonGemm p) {
                     } else {
                         read(ch, v);
                     }
-#pragma unroll
-                    for (int c = 0; c < 32; ++c) st[lane][c] = v[c];
-                    __syncwarp();
                     const Ahead<OP, TERMS> now = ahead;
                     if (ch + 1 < kChunks) fetch(ch + 1);
-                    finish_block<OP, TERMS>(p, g, at.mat, mat, row0, col0, st, now);
-                    __syncwarp();
+                    finish_block<OP, TERMS>(p, g, at.mat, mat, row0, col0, v, st, now);
                 } else if (ch + 1 < kChunks) {
                     fetch(ch + 1);
                 }
@@ -680,13 +692,12 @@ EncodeFn encode_fn() {
     }();
     return fn;
 }
-// [2 buffers][terms][count][rows][pitch] fp16, rows of `width` values; boxes of 64 x 64.
+// [2 buffers x terms x count][rows][pitch] fp16, rows of `width` values; boxes of 64 x 64.
 bool encode(CUtensorMap* map, void* at, int64_t width, int64_t rows, int64_t pitch, int64_t count, int terms) {
-    const cuuint64_t dims[5] = {(cuuint64_t)width, (cuuint64_t)rows, (cuuint64_t)count, (cuuint64_t)terms, 2};
-    const cuuint64_t plane = (cuuint64_t)count * rows * pitch * 2;
-    const cuuint64_t strides[4] = {(cuuint64_t)pitch * 2, (cuuint64_t)rows * pitch * 2, plane, plane * terms};
-    const cuuint32_t box[5] = {kBox, kBox, 1, 1, 1}, step[5] = {1, 1, 1, 1, 1};
-    return encode_fn()(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 5, at, dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+    const cuuint64_t dims[3] = {(cuuint64_t)width, (cuuint64_t)rows, (cuuint64_t)count * terms * 2};
+    const cuuint64_t strides[2] = {(cuuint64_t)pitch * 2, (cuuint64_t)rows * pitch * 2};
+    const cuuint32_t box[3] = {kBox, kBox, 1}, step[3] = {1, 1, 1};
+    return encode_fn()(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, at, dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -717,8 +728,8 @@ int take_run(const int32_t* rows, const int32_t* cols, int n, int at, int terms,
             r.g[g] = MuonGroup{};
             r.g[g].m = m;
             r.g[g].n = w;
-            r.g[g].mp = (m + 7) / 8 * 8;
-            r.g[g].np = (w + 7) / 8 * 8;
+            r.g[g].mp = (m + 15) / 16 * 16;
+            r.g[g].np = (w + 15) / 16 * 16;
             ++r.groups;
         }
         group_of[r.count] = g;
@@ -786,12 +797,13 @@ double product_time(const MuonGemm& p, int terms, bool gram) {
     }
     return std::ceil(all / slots) * (sum / all);
 }
+template <int CG, int OP>
+cudaError_t product_terms(MuonGemm& p, int terms, cudaStream_t st) { return terms == 2 ? product<CG, 2, OP>(p, st) : product<CG, 1, OP>(p, st); }
 template <int OP>
-cudaError_t pick_product(MuonGemm& p, int terms, cudaStream_t st) {
-    constexpr bool kSym = OP == kGram || OP == kPoly;
-    const bool pair = product_time<2, kSym>(p, terms, OP == kGram) <= product_time<1, kSym>(p, terms, OP == kGram);
-    if (pair) return terms == 2 ? product<2, 2, OP>(p, st) : product<2, 1, OP>(p, st);
-    return terms == 2 ? product<1, 2, OP>(p, st) : product<1, 1, OP>(p, st);
+cudaError_t product_of(MuonGemm& p, int terms, bool pairs, cudaStream_t st) { return pairs ? product_terms<2, OP>(p, terms, st) : product_terms<1, OP>(p, terms, st); }
+template <int CG>
+double iteration_time(const MuonGemm& p, int terms) {
+    return product_time<CG, true>(p, terms, true) + product_time<CG, true>(p, terms, false) + product_time<CG, false>(p, terms, false);
 }
 
 int muon_terms(const rfast_muon* a) { return a->terms ? a->terms : a->param_type == RFAST_TYPE_F32 ? 2 : 1; }
@@ -825,7 +837,7 @@ cudaError_t muon_run(const rfast_muon* a, const MuonRun& r, char* work, bool fir
             const double size = a->size_rule == RFAST_MUON_SIZE_RMS ? 0.2 * std::sqrt((double)r.g[g].n)
                                                                     : std::sqrt(m.rows > m.cols ? (double)m.rows / m.cols : 1.0);
             m.step = (float)(a->lr * size);
-            m.wide = m.cols % 8 == 0 && (uintptr_t)m.param % 16 == 0;
+            m.wide = m.rows <= m.cols && m.cols * (int64_t)bytes_of(a->param_type) % 32 == 0 && (uintptr_t)m.param % 32 == 0;
             t.part0[at] = part;
             t.tile0[at] = tile;
             part += (int)parts_of(m.rows, m.cols);
@@ -851,11 +863,12 @@ cudaError_t muon_run(const rfast_muon* a, const MuonRun& r, char* work, bool fir
     const MuonScalars c{(float)a->momentum_beta, (float)(1.0 - a->momentum_beta), a->nesterov != 0, a->grad_type, terms, a->eps, a->d_grad_scale};
     cudaError_t e = launch(k_muon_momentum, dim3((unsigned)part), 256, 0, st, false, t, c, parts, mats, first_run ? (int*)work : (int*)nullptr);
     if (e == cudaSuccess) e = launch(k_muon_begin, dim3((unsigned)tile), 256, 0, st, true, t, c, (const double*)parts, q);
+    const bool pairs = iteration_time<2>(q, terms) <= iteration_time<1>(q, terms);
     for (int it = 0; it < a->iterations && e == cudaSuccess; ++it) {
         q.in = it & 1;
-        e = pick_product<kGram>(q, terms, st);
-        if (e == cudaSuccess) e = pick_product<kPoly>(q, terms, st);
-        if (e == cudaSuccess) e = it + 1 < a->iterations ? pick_product<kApply>(q, terms, st) : pick_product<kUpdate>(q, terms, st);
+        e = product_of<kGram>(q, terms, pairs, st);
+        if (e == cudaSuccess) e = product_of<kPoly>(q, terms, pairs, st);
+        if (e == cudaSuccess) e = it + 1 < a->iterations ? product_of<kApply>(q, terms, pairs, st) : product_of<kUpdate>(q, terms, pairs, st);
     }
     return e;
 }

@@ -10,7 +10,7 @@
 namespace rfast {
 namespace tc {
 
-constexpr uint64_t kWaitNs = 2000000000ull;      // every wait on a barrier gives up after 2 s
+constexpr int64_t kWaitClocks = 4000000000ll;    // every wait on a barrier gives up after these, 2 s and more
 
 __device__ __forceinline__ uint32_t smem(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 // The same variable in thread block `rank` of the cluster.
@@ -42,34 +42,39 @@ __device__ __forceinline__ void bar_arrive_cluster(uint32_t addr) {
 // False when the limit ran out: the caller records it and bails out.
 __device__ __forceinline__ bool bar_wait(uint64_t* bar, uint32_t parity) {
     const uint32_t addr = smem(bar);
-    uint64_t t0 = 0;
+    int64_t t0 = 0;
     for (uint32_t it = 0;; ++it) {
         uint32_t ok;
         asm volatile(
             "{\n.reg .pred p;\n"
-            "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
+            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
             "selp.u32 %0, 1, 0, p;\n}\n"
             : "=r"(ok) : "r"(addr), "r"(parity) : "memory");
         if (ok) return true;
-        uint64_t now;
-        asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(now));
+        const int64_t now = clock64();
         if (it == 0) t0 = now;
-        else if (now - t0 > kWaitNs) return false;
+        else if (now - t0 > kWaitClocks) return false;
     }
 }
 
-// A box of a five-dimensional array into this block's shared memory; the bytes are counted at the barrier `bar`, an address in
+// One thread of a converged warp.  The warp runs its loop as a whole and this picks who issues, so that what the instructions take stays in
+// uniform registers; a loop that only lane 0 runs pays 300 clocks more for four matrix instructions and as many loads.
+__device__ __forceinline__ bool elect() {
+    uint32_t one;
+    asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}\n" : "=r"(one));
+    return one != 0;
+}
+
+// A box of a three-dimensional array into this block's shared memory; the bytes are counted at the barrier `bar`, an address in
 // the cluster's shared memory (CG = 2: of either block of the pair).
 template <int CG>
-__device__ __forceinline__ void load_5d(void* dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2, int c3, int c4) {
+__device__ __forceinline__ void load_3d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2) {
     if (CG == 2)
-        asm volatile(
-            "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%3, %4, %5, %6, %7}], [%2];"
-            ::"r"(smem(dst)), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4) : "memory");
+        asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%3, %4, %5}], [%2];"
+                     ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2) : "memory");
     else
-        asm volatile(
-            "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];"
-            ::"r"(smem(dst)), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4) : "memory");
+        asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+                     ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2) : "memory");
 }
 // what kernels before this one wrote by plain stores, for the loads above
 __device__ __forceinline__ void fence_for_loads() { asm volatile("fence.proxy.async.global;" ::: "memory"); }
@@ -93,15 +98,14 @@ __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::be
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 
 // Operand descriptor of a tile that TMA wrote with the 128-byte swizzle, base a multiple of 1024 bytes.
-//   rows of 64 values along the summed dimension: `stride` is 1024, eight rows
-//   rows of 64 values along the other dimension:  `stride` is 1024, eight steps of the sum; `lead` the next 64 values
+//   rows of 64 values along the summed dimension: eight rows are 1024 bytes; `lead` is not used
+//   rows of 64 values along the other dimension:  eight steps of the sum are 1024 bytes; `lead` to the next 64 values
 __device__ __forceinline__ uint64_t operand(uint32_t addr, uint32_t lead) {
     return (uint64_t)((addr & 0x3FFFF) >> 4) | (uint64_t)((lead >> 4) & 0x3FFF) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
 }
-// fp16 operands, fp32 sums, M x N; `across`: the second operand's rows run along N.
-__host__ __device__ constexpr uint32_t instruction_f16(int M, int N, bool across) {
-    return 1u << 4 | (across ? 1u << 16 : 0u) | (uint32_t)(N >> 3) << 17 | (uint32_t)(M >> 4) << 24;
-}
+// fp16 operands, fp32 sums, M x N; kAcrossA, kAcrossB are added where the first operand's rows run along M, the second's along N.
+__host__ __device__ constexpr uint32_t instruction_f16(int M, int N) { return 1u << 4 | (uint32_t)(N >> 3) << 17 | (uint32_t)(M >> 4) << 24; }
+constexpr uint32_t kAcrossA = 1u << 15, kAcrossB = 1u << 16;
 template <int CG>
 __device__ __forceinline__ void mma_f16(uint32_t acc, uint64_t a, uint64_t b, uint32_t instruction, uint32_t add) {
     if (CG == 2)

@@ -69,6 +69,16 @@ __device__ __forceinline__ void store8(T* p, const float (&v)[8]) {
     __stcs(reinterpret_cast<uint4*>(p), make_uint4(packed(v[0], v[1], p), packed(v[2], v[3], p), packed(v[4], v[5], p), packed(v[6], v[7], p)));
 }
 
+// 32 bytes at a multiple of 32, past the first-level cache.
+__device__ __forceinline__ void load32(const void* p, uint32_t (&r)[8]) {
+    asm volatile("ld.global.L1::no_allocate.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "l"(p));
+}
+__device__ __forceinline__ void store32(void* p, const uint32_t (&r)[8]) {
+    asm volatile("st.global.v8.b32 [%8], {%0,%1,%2,%3,%4,%5,%6,%7};"
+                 ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "l"(p) : "memory");
+}
+
 inline size_t bytes_of(int type) { return type == RFAST_TYPE_F32 ? 4 : 2; }
 inline bool is_type(int type) { return type == RFAST_TYPE_F32 || type == RFAST_TYPE_BF16 || type == RFAST_TYPE_F16; }
 
