@@ -62,6 +62,7 @@ struct MuonTable {
 };
 struct MuonGroup {
     int m, n, np, mp, count;
+    int turned;                        // parameters are n x m: X is their update's transpose
     int mat0;                          // its first matrix in the table
     int tile0;                         // of the launch
     int64_t x, s;                      // byte offsets of its arrays in the workspace
@@ -71,7 +72,7 @@ struct MuonGemm {
     CUtensorMap x[kGroups], s[kGroups];
     MuonGroup g[kGroups];
     int groups, tiles, in;             // `in`: the buffer of X that is read
-    int param_type;
+    int back;                          // tiles from the last to the first
     float keep;                        // 1 - lr weight_decay
     char* work;
     const MuonMat* mats;               // in the workspace
@@ -268,6 +269,7 @@ struct Shape {
 struct Tile {
     int g, mat, i, j;
 };
+// Tiles of a matrix's product: m x n, up to the diagonal where SYM.
 template <int TM, int TN, bool SYM>
 __host__ __device__ inline int tiles_of(int m, int n) {
     const int ti = (m + TM - 1) / TM;
@@ -277,13 +279,18 @@ __host__ __device__ inline int tiles_of(int m, int n) {
     const int last = (m + TN - 1) / TN;
     return q * ti * (ti - 1) / 2 + (last < q * ti ? last : q * ti);
 }
-template <int TM, int TN, bool SYM>
+// What a product's result has for rows and columns: the update has the parameter's.
+template <int OP> __host__ __device__ inline int result_rows(const MuonGroup& g) { return OP == kUpdate && g.turned ? g.n : g.m; }
+template <int OP> __host__ __device__ inline int result_cols(const MuonGroup& g) { return OP == kGram || OP == kPoly || (OP == kUpdate && g.turned) ? g.m : g.n; }
+template <int TM, int TN, int OP>
 __device__ __forceinline__ Tile tile_at(const MuonGemm& p, int t) {
+    constexpr bool SYM = OP == kGram || OP == kPoly;
+    if (p.back) t = p.tiles - 1 - t;
     Tile r;
     r.g = 0;
     while (r.g + 1 < p.groups && p.g[r.g + 1].tile0 <= t) ++r.g;
     const MuonGroup& g = p.g[r.g];
-    const int per = tiles_of<TM, TN, SYM>(g.m, g.n);
+    const int per = tiles_of<TM, TN, SYM>(result_rows<OP>(g), result_cols<OP>(g));
     t -= g.tile0;
     r.mat = t / per;
     t -= r.mat * per;
@@ -295,7 +302,7 @@ __device__ __forceinline__ Tile tile_at(const MuonGemm& p, int t) {
         r.i = i;
         r.j = t - q * i * (i + 1) / 2;
     } else {
-        const int ti = (g.m + TM - 1) / TM;
+        const int ti = (result_rows<OP>(g) + TM - 1) / TM;
         r.i = t % ti;
         r.j = t / ti;
     }
@@ -330,12 +337,12 @@ __device__ __forceinline__ void keep32(__half* to, int64_t low_plane, const floa
 }
 
 // What a block's finish reads from memory, fetched while the sums are formed: A for B, the parameters for the update.
-template <int OP, int TERMS>
+template <int OP, int TERMS, class T>
 struct Ahead {
     __device__ __forceinline__ void load(const MuonGemm&, const MuonGroup&, int, const MuonMat*, int, int) {}
 };
-template <int TERMS>
-struct Ahead<kPoly, TERMS> {
+template <int TERMS, class T>
+struct Ahead<kPoly, TERMS, T> {
     uint32_t q[2 * TERMS][8];
     __device__ __forceinline__ void load(const MuonGemm& p, const MuonGroup& g, int slot, const MuonMat*, int row0, int col0) {
         const int row = row0 + (threadIdx.x & 31);
@@ -347,94 +354,82 @@ struct Ahead<kPoly, TERMS> {
                 for (int h = 0; h < TERMS; ++h) load32(a + 16 * k + h * g.s_plane, q[2 * h + k]);
     }
 };
-template <int TERMS>
-struct Ahead<kUpdate, TERMS> {
-    uint32_t q[4][8];                  // 32 parameters of a lane's row: fp32 fills all, 16-bit types half
-    __device__ __forceinline__ void load(const MuonGemm& p, const MuonGroup& g, int, const MuonMat* mat, int row0, int col0) {
-        if (!mat->wide) return;
-        const int row = row0 + (threadIdx.x & 31), values = p.param_type == RFAST_TYPE_F32 ? 8 : 16;      // of 32 bytes
-        if (row >= g.m) return;
-        const char* at = (const char*)mat->param + ((int64_t)row * g.n + col0) * (32 / values);
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-            if (k * values < 32 && col0 + k * values < g.n) load32(at + 32 * k, q[k]);
-    }
-};
-
-// Parameters one at a time, a lane a column of the parameter's: X's row, where X is its transpose, from registers ...
-template <class T>
-__device__ __forceinline__ void update_turned(T* __restrict__ param, const float (&v)[32], int row, int col0, int m, int n, float step, float keep) {
-    if (row >= m) return;
-    T* const w = param + (int64_t)col0 * m + row;
-#pragma unroll
-    for (int part = 0; part < 32; part += 16) {
-        T old[16];
-#pragma unroll
-        for (int u = 0; u < 16; ++u)
-            if (col0 + part + u < n) old[u] = w[(int64_t)(part + u) * m];
-#pragma unroll
-        for (int u = 0; u < 16; ++u)
-            if (col0 + part + u < n) w[(int64_t)(part + u) * m] = rounded<T>(fmaf(-step, v[part + u], value_of(old[u]) * keep));
-    }
+// Parameters, two ways: 32 neighbours of a lane's row, 32 bytes at a time (wide), or 32 rows of a lane's column, the sums brought there
+// through shared memory (rows whose length or place does not allow for the first way).
+template <class T> __device__ __forceinline__ uint32_t raw_of(const T* p) {
+    if constexpr (sizeof(T) == 4) return *reinterpret_cast<const uint32_t*>(p);
+    else return *reinterpret_cast<const uint16_t*>(p);
 }
-// ... or X's column, through shared memory: rows whose length or place does not allow for 32 bytes at a time.
-template <class T>
-__device__ __forceinline__ void update_narrow(T* param, const float (*st)[33], int row0, int col, int m, int n, float step, float keep) {
-    if (col >= n) return;
-    T* const w = param + (int64_t)row0 * n + col;
-    const int lane = threadIdx.x & 31;
-#pragma unroll
-    for (int part = 0; part < 32; part += 8) {
-        T old[8];
-#pragma unroll
-        for (int u = 0; u < 8; ++u)
-            if (row0 + part + u < m) old[u] = w[(int64_t)(part + u) * n];
-#pragma unroll
-        for (int u = 0; u < 8; ++u)
-            if (row0 + part + u < m) w[(int64_t)(part + u) * n] = rounded<T>(fmaf(-step, st[part + u][lane], value_of(old[u]) * keep));
-    }
-}
+template <class T> __device__ __forceinline__ float value_of_raw(uint32_t r);
+template <> __device__ __forceinline__ float value_of_raw<float>(uint32_t r) { return __uint_as_float(r); }
+template <> __device__ __forceinline__ float value_of_raw<__nv_bfloat16>(uint32_t r) { return __uint_as_float(r << 16); }
+template <> __device__ __forceinline__ float value_of_raw<__half>(uint32_t r) { return __half2float(__ushort_as_half((unsigned short)r)); }
 template <class T> __device__ __forceinline__ float2 two_values(uint32_t r);
 template <> __device__ __forceinline__ float2 two_values<__half>(uint32_t r) { return __half22float2(*reinterpret_cast<const __half2*>(&r)); }
 template <> __device__ __forceinline__ float2 two_values<__nv_bfloat16>(uint32_t r) { return make_float2(__uint_as_float(r << 16), __uint_as_float(r & 0xffff0000u)); }
 
-template <class T, int TERMS>
-__device__ __forceinline__ void update_block(const MuonMat* mat, const MuonGroup& g, int row0, int col0, float (&v)[32], float (*st)[33], const Ahead<kUpdate, TERMS>& now, float keep) {
-    const int lane = threadIdx.x & 31, row = row0 + lane;
+template <int TERMS, class T>
+struct Ahead<kUpdate, TERMS, T> {
+    uint32_t q[32];
+    __device__ __forceinline__ void load(const MuonGemm&, const MuonGroup&, int, const MuonMat* mat, int row0, int col0) {
+        const int lane = threadIdx.x & 31;
+        const T* const param = (const T*)mat->param;
+        if (mat->wide) {
+            constexpr int kValues = 32 / (int)sizeof(T);
+            const T* w = param + (int64_t)(row0 + lane) * mat->cols + col0;
+            const int n = row0 + lane < mat->rows ? mat->cols - col0 : 0;
+#pragma unroll
+            for (int k = 0; k < 32 / kValues; ++k)
+                if (k * kValues < n) load32(w + k * kValues, *reinterpret_cast<uint32_t(*)[8]>(q + 8 * k));
+        } else {
+            const T* w = param + (int64_t)row0 * mat->cols + col0 + lane;
+            const int m = col0 + lane < mat->cols ? mat->rows - row0 : 0;
+#pragma unroll
+            for (int k = 0; k < 32; ++k)
+                if (k < m) q[k] = raw_of(w + (int64_t)k * mat->cols);
+        }
+    }
+};
+
+template <int TERMS, class T>
+__device__ __forceinline__ void update_block(const MuonMat* mat, int row0, int col0, float (&v)[32], float (*st)[33], const Ahead<kUpdate, TERMS, T>& now, float keep) {
+    const int lane = threadIdx.x & 31;
     const float step = mat->step * (1.f / (kSUnit * kXUnit));
     T* const param = (T*)mat->param;
-    if (mat->rows > mat->cols) {
-        update_turned(param, v, row, col0, g.m, g.n, step, keep);
-    } else if (mat->wide) {
-        if (row >= g.m) return;
-        T* const to = param + (int64_t)row * g.n + col0;
+    if (mat->wide) {
         constexpr int kValues = 32 / (int)sizeof(T);
+        T* const w = param + (int64_t)(row0 + lane) * mat->cols + col0;
+        const int n = row0 + lane < mat->rows ? mat->cols - col0 : 0;
 #pragma unroll
         for (int k = 0; k < 32 / kValues; ++k) {
-            if (col0 + k * kValues >= g.n) break;
+            if (k * kValues >= n) break;
             uint32_t r[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 if constexpr (sizeof(T) == 4) {
-                    r[e] = __float_as_uint(fmaf(-step, v[k * 8 + e], __uint_as_float(now.q[k][e]) * keep));
+                    r[e] = __float_as_uint(fmaf(-step, v[k * 8 + e], __uint_as_float(now.q[k * 8 + e]) * keep));
                 } else {
-                    const float2 w = two_values<T>(now.q[k][e]);
-                    r[e] = packed(fmaf(-step, v[k * 16 + 2 * e], w.x * keep), fmaf(-step, v[k * 16 + 2 * e + 1], w.y * keep), (const T*)nullptr);
+                    const float2 o = two_values<T>(now.q[k * 8 + e]);
+                    r[e] = packed(fmaf(-step, v[k * 16 + 2 * e], o.x * keep), fmaf(-step, v[k * 16 + 2 * e + 1], o.y * keep), (const T*)nullptr);
                 }
             }
-            store32(to + k * kValues, r);
+            store32(w + k * kValues, r);
         }
     } else {
 #pragma unroll
         for (int c = 0; c < 32; ++c) st[lane][c] = v[c];
         __syncwarp();
-        update_narrow(param, st, row0, col0 + lane, g.m, g.n, step, keep);
+        T* const w = param + (int64_t)row0 * mat->cols + col0 + lane;
+        const int m = col0 + lane < mat->cols ? mat->rows - row0 : 0;
+#pragma unroll
+        for (int k = 0; k < 32; ++k)
+            if (k < m) w[(int64_t)k * mat->cols] = rounded<T>(fmaf(-step, st[k][lane], value_of_raw<T>(now.q[k]) * keep));
         __syncwarp();
     }
 }
 
-template <int OP, int TERMS>
-__device__ __forceinline__ void finish_block(const MuonGemm& p, const MuonGroup& g, int slot, const MuonMat* mat, int row0, int col0, float (&v)[32], float (*st)[33], const Ahead<OP, TERMS>& now) {
+template <int OP, int TERMS, class T>
+__device__ __forceinline__ void finish_block(const MuonGemm& p, const MuonGroup& g, int slot, const MuonMat* mat, int row0, int col0, float (&v)[32], float (*st)[33], const Ahead<OP, TERMS, T>& now) {
     const int lane = threadIdx.x & 31, row = row0 + lane;
     if constexpr (OP == kGram || OP == kPoly) {
         // B holds a on the diagonal, so that B X is the next X
@@ -466,18 +461,19 @@ __device__ __forceinline__ void finish_block(const MuonGemm& p, const MuonGroup&
         for (int c = 0; c < 32; ++c) v[c] *= 1.f / kSUnit;
         if (row < g.m) keep32<TERMS>(to, g.x_plane, v, g.np - col0);
     } else {
-        if (p.param_type == RFAST_TYPE_F32) update_block<float, TERMS>(mat, g, row0, col0, v, st, now, p.keep);
-        else if (p.param_type == RFAST_TYPE_BF16) update_block<__nv_bfloat16, TERMS>(mat, g, row0, col0, v, st, now, p.keep);
-        else update_block<__half, TERMS>(mat, g, row0, col0, v, st, now, p.keep);
+        update_block<TERMS, T>(mat, row0, col0, v, st, now, p.keep);
     }
 }
 
 // A and B are stored up to this column in the row tile of `row`: only tiles up to the diagonal are formed.  All products of a run use tiles
 // of one shape, so that an operand's rows lie in one row tile.
+// Whether an operand is read with rows along the other dimension than the sum's: X but for X X', A and B above what is stored of them.
+template <int OP>
+__device__ __forceinline__ bool across(bool x, bool above) { return x ? OP != kGram : above; }
 template <class S>
 __device__ __forceinline__ int stored_up_to(int row) { return (row / S::kTM + 1) * S::kTM; }
 
-template <int CG, int TERMS, int OP>
+template <int CG, int TERMS, int OP, class T>         // T: of the parameters, for kUpdate
 __global__ void __launch_bounds__(kThreads, 1)
 k_muon_product(const __grid_constant__ MuonGemm p) {
     using S = Shape<CG, TERMS>;
@@ -497,6 +493,10 @@ k_muon_product(const __grid_constant__ MuonGemm p) {
         bad = 0;
         tc::bar_init_fence();
     }
+    if (warp == 0 && lane < p.groups) {
+        tc::map_ahead(&p.x[lane]);
+        tc::map_ahead(&p.s[lane]);
+    }
     if (warp == 1) tc::tmem_alloc<CG>(&tmem, S::kColumns);
     tc::fence_before();
     if (CG == 2) tc::cluster_sync(); else __syncthreads();
@@ -513,21 +513,23 @@ k_muon_product(const __grid_constant__ MuonGemm p) {
         uint32_t turn = 1;                                  // of the ring: the first goes through without a wait
         bool ok = true;
         for (int t = first; t < p.tiles && ok; t += stride) {
-            const Tile at = tile_at<S::kTM, S::kTN, kSym>(p, t);
+            const Tile at = tile_at<S::kTM, S::kTN, OP>(p, t);
             const MuonGroup& g = p.g[at.g];
             const int blocks = ((OP == kGram ? g.n : g.m) + kBox - 1) / kBox;
             const int row0 = at.i * S::kTM + rank * 128, col0 = at.j * S::kTN + rank * (S::kTN / CG);
-            const CUtensorMap* const map_a = OP == kGram ? &p.x[at.g] : &p.s[at.g];
-            const CUtensorMap* const map_b = OP == kPoly ? &p.s[at.g] : &p.x[at.g];
+            // X X' and A A have one factor twice, B X and (B X)' = X' B two
+            const bool x_first = OP == kGram || (OP == kUpdate && g.turned), x_second = OP == kGram || (OP >= kApply && !x_first);
+            const CUtensorMap* const map_a = x_first ? &p.x[at.g] : &p.s[at.g];
+            const CUtensorMap* const map_b = x_second ? &p.x[at.g] : &p.s[at.g];
             // which matrix of an array: [buffer][terms][count]
-            const int in_a = at.mat + g.count * TERMS * (OP == kGram ? p.in : OP == kPoly ? 0 : 1);
-            const int in_b = at.mat + g.count * TERMS * (OP == kPoly ? 0 : p.in);
+            const int in_x = at.mat + g.count * TERMS * p.in, in_s = at.mat + g.count * TERMS * (OP == kPoly ? 0 : 1);
+            const int in_a = x_first ? in_x : in_s, in_b = x_second ? in_x : in_s;
             const int limit_a = stored_up_to<S>(row0), limit_b = stored_up_to<S>(col0);
             for (int kb = 0; kb < blocks; ++kb) {
                 if (!(ok = tc::bar_wait(&empty[s], turn))) break;
                 const int k0 = kb * kBox;
                 // A and B above their stored tiles are read as the transposed ones below, rows along the other dimension
-                const bool across_a = OP != kGram && k0 >= limit_a, across_b = OP == kPoly ? k0 >= limit_b : OP != kGram;
+                const bool across_a = across<OP>(x_first, k0 >= limit_a), across_b = across<OP>(x_second, k0 >= limit_b);
                 if (tc::elect()) {
                     if (rank == 0) tc::bar_expect(&full[s], CG * S::kStage);
                     const uint32_t bar = bar0 + s * 8;
@@ -555,8 +557,9 @@ k_muon_product(const __grid_constant__ MuonGemm p) {
             uint32_t turn = 0;
             bool ok = true;
             for (int t = first; t < p.tiles && ok; t += stride) {
-                const Tile at = tile_at<S::kTM, S::kTN, kSym>(p, t);
+                const Tile at = tile_at<S::kTM, S::kTN, OP>(p, t);
                 const int blocks = ((OP == kGram ? p.g[at.g].n : p.g[at.g].m) + kBox - 1) / kBox;
+                const bool x_first = OP == kGram || (OP == kUpdate && p.g[at.g].turned), x_second = OP == kGram || (OP >= kApply && !x_first);
                 const int limit_a = stored_up_to<S>(at.i * S::kTM), limit_b = stored_up_to<S>(at.j * S::kTN);
                 uint32_t to = 0, buf = 0;
                 for (int kb = 0; kb < blocks; ++kb) {
@@ -569,7 +572,7 @@ k_muon_product(const __grid_constant__ MuonGemm p) {
                     }
                     if (!(ok = tc::bar_wait(&full[s], turn))) break;
                     tc::fence_after();
-                    const bool across_a = OP != kGram && kb * kBox >= limit_a, across_b = OP == kPoly ? kb * kBox >= limit_b : OP != kGram;
+                    const bool across_a = across<OP>(x_first, kb * kBox >= limit_a), across_b = across<OP>(x_second, kb * kBox >= limit_b);
                     const uint32_t instruction = tc::instruction_f16(S::kTM, S::kTN) | (across_a ? tc::kAcrossA : 0u) | (across_b ? tc::kAcrossB : 0u);
                     const uint32_t next_a = across_a ? kAcross : kAlong, next_b = across_b ? kAcross : kAlong;
                     if (tc::elect()) {
@@ -613,7 +616,7 @@ k_muon_product(const __grid_constant__ MuonGemm p) {
         const auto column = [&](int ch) { return half * (S::kTN / 2) + ch * 32; };
         const auto read = [&](int ch, float (&v)[32]) { tc::tmem_load32(acc + (sums & 1) * S::kTN + column(ch) + ((uint32_t)(quarter * 32) << 16), v); };
         for (int t = first; t < p.tiles; t += stride) {
-            const Tile at = tile_at<S::kTM, S::kTN, kSym>(p, t);
+            const Tile at = tile_at<S::kTM, S::kTN, OP>(p, t);
             const MuonGroup& g = p.g[at.g];
             float total[kSegmented ? kChunks : 1][32];
             if (kSegmented) {
@@ -638,10 +641,10 @@ k_muon_product(const __grid_constant__ MuonGemm p) {
             const int row0 = at.i * S::kTM + rank * 128 + quarter * 32;
             const auto kept = [&](int ch) {                 // whether anything of a chunk is
                 const int col0 = at.j * S::kTN + column(ch);
-                return row0 < g.m && col0 < (kSym ? g.m : g.n);
+                return row0 < result_rows<OP>(g) && col0 < result_cols<OP>(g);
             };
             const MuonMat* const mat = OP == kUpdate ? p.mats + g.mat0 + at.mat : nullptr;
-            Ahead<OP, TERMS> ahead;
+            Ahead<OP, TERMS, T> ahead;
             const auto fetch = [&](int ch) {
                 if ((OP == kPoly || OP == kUpdate) && kept(ch)) ahead.load(p, g, at.mat, mat, row0, at.j * S::kTN + column(ch));
             };
@@ -658,9 +661,9 @@ k_muon_product(const __grid_constant__ MuonGemm p) {
                     } else {
                         read(ch, v);
                     }
-                    const Ahead<OP, TERMS> now = ahead;
+                    const Ahead<OP, TERMS, T> now = ahead;
                     if (ch + 1 < kChunks) fetch(ch + 1);
-                    finish_block<OP, TERMS>(p, g, at.mat, mat, row0, col0, v, st, now);
+                    finish_block<OP, TERMS, T>(p, g, at.mat, mat, row0, col0, v, st, now);
                 } else if (ch + 1 < kChunks) {
                     fetch(ch + 1);
                 }
@@ -720,7 +723,8 @@ int take_run(const int32_t* rows, const int32_t* cols, int n, int at, int terms,
         if (rows[at] == 0 || cols[at] == 0) continue;
         const int m = rows[at] < cols[at] ? rows[at] : cols[at], w = rows[at] < cols[at] ? cols[at] : rows[at];
         int g = 0;
-        while (g < r.groups && (r.g[g].m != m || r.g[g].n != w)) ++g;
+        const int turned = rows[at] > cols[at];
+        while (g < r.groups && (r.g[g].m != m || r.g[g].n != w || r.g[g].turned != turned)) ++g;
         if (g == kGroups) break;
         const int64_t parts = parts_of(rows[at], cols[at]);
         if (r.count > 0 && r.parts + parts > (1 << 24)) break;
@@ -728,6 +732,7 @@ int take_run(const int32_t* rows, const int32_t* cols, int n, int at, int terms,
             r.g[g] = MuonGroup{};
             r.g[g].m = m;
             r.g[g].n = w;
+            r.g[g].turned = turned;
             r.g[g].mp = (m + 15) / 16 * 16;
             r.g[g].np = (w + 15) / 16 * 16;
             ++r.groups;
@@ -754,18 +759,19 @@ int take_run(const int32_t* rows, const int32_t* cols, int n, int at, int terms,
     return at;
 }
 
-template <int CG, int TERMS, int OP>
+template <int CG, int TERMS, int OP, class T = float>
 cudaError_t product(MuonGemm& p, cudaStream_t st) {
     using S = Shape<CG, TERMS>;
     constexpr bool kSym = OP == kGram || OP == kPoly;
     int tiles = 0;
     for (int g = 0; g < p.groups; ++g) {
         p.g[g].tile0 = tiles;
-        tiles += p.g[g].count * tiles_of<S::kTM, S::kTN, kSym>(p.g[g].m, p.g[g].n);
+        tiles += p.g[g].count * tiles_of<S::kTM, S::kTN, kSym>(result_rows<OP>(p.g[g]), result_cols<OP>(p.g[g]));
     }
     p.tiles = tiles;
+    p.back ^= 1;                       // what the product before wrote last is read first, while the L2 cache holds it
     const int slots = CG == 2 ? kPairs : kSms;
-    cudaError_t e = cudaFuncSetAttribute(k_muon_product<CG, TERMS, OP>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kShared);
+    cudaError_t e = cudaFuncSetAttribute(k_muon_product<CG, TERMS, OP, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kShared);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((tiles < slots ? tiles : slots) * CG);
@@ -780,7 +786,7 @@ cudaError_t product(MuonGemm& p, cudaStream_t st) {
     at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, k_muon_product<CG, TERMS, OP>, (const MuonGemm)p);
+    return cudaLaunchKernelEx(&cfg, k_muon_product<CG, TERMS, OP, T>, (const MuonGemm)p);
 }
 
 // Time of a product by tiles of TM x TN on `slots` places, in clocks: whole waves of the mean tile.
@@ -797,10 +803,16 @@ double product_time(const MuonGemm& p, int terms, bool gram) {
     }
     return std::ceil(all / slots) * (sum / all);
 }
+template <int CG, int TERMS, int OP>
+cudaError_t product_type(MuonGemm& p, int type, cudaStream_t st) {
+    if (OP != kUpdate || type == RFAST_TYPE_F32) return product<CG, TERMS, OP, float>(p, st);
+    if constexpr (OP == kUpdate) return type == RFAST_TYPE_BF16 ? product<CG, TERMS, OP, __nv_bfloat16>(p, st) : product<CG, TERMS, OP, __half>(p, st);
+    return cudaErrorInvalidValue;
+}
 template <int CG, int OP>
-cudaError_t product_terms(MuonGemm& p, int terms, cudaStream_t st) { return terms == 2 ? product<CG, 2, OP>(p, st) : product<CG, 1, OP>(p, st); }
+cudaError_t product_terms(MuonGemm& p, int terms, int type, cudaStream_t st) { return terms == 2 ? product_type<CG, 2, OP>(p, type, st) : product_type<CG, 1, OP>(p, type, st); }
 template <int OP>
-cudaError_t product_of(MuonGemm& p, int terms, bool pairs, cudaStream_t st) { return pairs ? product_terms<2, OP>(p, terms, st) : product_terms<1, OP>(p, terms, st); }
+cudaError_t product_of(MuonGemm& p, int terms, bool pairs, int type, cudaStream_t st) { return pairs ? product_terms<2, OP>(p, terms, type, st) : product_terms<1, OP>(p, terms, type, st); }
 template <int CG>
 double iteration_time(const MuonGemm& p, int terms) {
     return product_time<CG, true>(p, terms, true) + product_time<CG, true>(p, terms, false) + product_time<CG, false>(p, terms, false);
@@ -837,7 +849,7 @@ cudaError_t muon_run(const rfast_muon* a, const MuonRun& r, char* work, bool fir
             const double size = a->size_rule == RFAST_MUON_SIZE_RMS ? 0.2 * std::sqrt((double)r.g[g].n)
                                                                     : std::sqrt(m.rows > m.cols ? (double)m.rows / m.cols : 1.0);
             m.step = (float)(a->lr * size);
-            m.wide = m.rows <= m.cols && m.cols * (int64_t)bytes_of(a->param_type) % 32 == 0 && (uintptr_t)m.param % 32 == 0;
+            m.wide = m.cols * (int64_t)bytes_of(a->param_type) % 32 == 0 && (uintptr_t)m.param % 32 == 0;
             t.part0[at] = part;
             t.tile0[at] = tile;
             part += (int)parts_of(m.rows, m.cols);
@@ -854,7 +866,6 @@ cudaError_t muon_run(const rfast_muon* a, const MuonRun& r, char* work, bool fir
         first += r.g[g].count;
     }
     q.groups = r.groups;
-    q.param_type = a->param_type;
     q.keep = (float)(1.0 - a->lr * a->weight_decay);
     q.work = work;
     MuonMat* mats = (MuonMat*)(work + 256);
@@ -866,9 +877,9 @@ cudaError_t muon_run(const rfast_muon* a, const MuonRun& r, char* work, bool fir
     const bool pairs = iteration_time<2>(q, terms) <= iteration_time<1>(q, terms);
     for (int it = 0; it < a->iterations && e == cudaSuccess; ++it) {
         q.in = it & 1;
-        e = product_of<kGram>(q, terms, pairs, st);
-        if (e == cudaSuccess) e = product_of<kPoly>(q, terms, pairs, st);
-        if (e == cudaSuccess) e = it + 1 < a->iterations ? product_of<kApply>(q, terms, pairs, st) : product_of<kUpdate>(q, terms, pairs, st);
+        e = product_of<kGram>(q, terms, pairs, a->param_type, st);
+        if (e == cudaSuccess) e = product_of<kPoly>(q, terms, pairs, a->param_type, st);
+        if (e == cudaSuccess) e = it + 1 < a->iterations ? product_of<kApply>(q, terms, pairs, a->param_type, st) : product_of<kUpdate>(q, terms, pairs, a->param_type, st);
     }
     return e;
 }

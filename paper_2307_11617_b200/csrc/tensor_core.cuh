@@ -76,6 +76,7 @@ __device__ __forceinline__ void load_3d(uint32_t dst, const CUtensorMap* map, ui
         asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
                      ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2) : "memory");
 }
+__device__ __forceinline__ void map_ahead(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
 // what kernels before this one wrote by plain stores, for the loads above
 __device__ __forceinline__ void fence_for_loads() { asm volatile("fence.proxy.async.global;" ::: "memory"); }
 
