@@ -594,14 +594,14 @@ int rfast_group_norm_backward(const rfast_gn_shape* shape, const void* d_dy, con
  *     dtable_v = scale (sum of dout_i over the i whose token is v)        v < vocab;  accumulate: added to what dtable holds
  * A token outside [0, vocab) (-1, as padding) is none: its row of out is zero, its row of dout is not read.  Tokens
  * are 32- or 64-bit integers.  The backward pass sorts tokens and positions (stably), so that each sum runs over
- * ascending positions in fp32, long ones over sums of 64 and 1024 sorted places; each value is rounded once to its type.
+ * ascending positions in fp32, long ones over sums of up to 16 and of 256 sorted places; each value is rounded once to its type.
  * Without accumulate every row of dtable is written, zeros where a token does not occur; with it those rows are left alone.
  * A NaN or infinity of a row of dout reaches the row of its token and nothing else.
  * Strides are those of a row in elements.  Read operands may overlap themselves (a stride of 0 repeats a row), written
  * ones may not; no other operands may overlap.  Addresses need to be aligned to their type only; where width is a multiple
- * of 8 and addresses and strides are multiples of 16 bytes, both operands are moved 16 bytes at a time.  At most
+ * of 8, strides are, and addresses are multiples of eight values' size, both operands are moved eight values at a time.  At most
  * 2^30 tokens, a vocabulary of 2^30 and a width of 2^24.
- * workspace: rfast_embedding_workspace(shape) bytes of DEVICE memory, aligned to 16 (backward pass only). */
+ * workspace: rfast_embedding_workspace(shape) bytes of DEVICE memory, aligned to 32 (backward pass only). */
 typedef struct rfast_emb_shape {
     int64_t tokens, vocab;
     int32_t width;
@@ -630,8 +630,8 @@ int     rfast_embedding_backward(const rfast_emb_shape* shape, const void* d_tok
  * once; exp((z - z_max) / T) below 2^-126 counts as 0.  |z| / T below 2^126.
  * Strides are those of a row in elements; logits may overlap themselves (a stride of 0 repeats a row), dlogits may not.
  * dlogits may be the logits, with their stride; no other operands may overlap.  Addresses need to be aligned to their type
- * only.  The fast case is a gradient whose rows lie as the logits' do within 16 bytes (both contiguous, or both strides
- * multiples of 16 bytes).  Rows whose number of logits is odd are no slower. */
+ * only.  The fast case is a gradient whose rows begin at the same place within eight values as the logits' do (both contiguous,
+ * or strides that differ by a multiple of 8).  Rows whose number of logits is odd are no slower. */
 typedef struct rfast_policy {
     int64_t tokens, vocab;
     int32_t type;                      /* RFAST_TYPE_* of logits and dlogits */

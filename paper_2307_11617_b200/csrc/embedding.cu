@@ -2,13 +2,14 @@
 //
 // The gradient of a table row is the sum of the rows of dout that carry its token.  Tokens are sorted first (a stable radix
 // sort of token and position), so that every sum runs over neighbours in the sorted order, in the order of the positions,
-// without atomics: the same inputs give the same bits.  Then a warp owns some rows of the table and 256 columns, finds its
-// rows' runs in `start`, adds up in fp32 and writes each value once, zeros of unused rows among them.  What bounds it is
-// memory: dout is read once and the table's gradient written once.
+// without atomics: the same inputs give the same bits.  What bounds it is memory: dout is read once and the table's gradient
+// written once.
 //
-// Text uses some tokens thousands of times.  A run longer than a chunk (64 sorted places) is therefore cut at multiples of 64:
-// chunks that lie wholly in one run are summed beforehand, by a warp each, and sixteen whole neighbours to one sum again, so
-// that the row's owner adds at most 64 + 16 + tokens / 1024 + 16 + 64 rows one after the other.
+// Text uses some tokens thousands of times and most of a table's never, so work is shared out by sorted places, not by rows:
+// a warp takes a chunk of 16 places and 256 columns, adds up in fp32 with eight rows on their way, and writes the rows whose
+// run lies in its chunk.  Of a run that crosses a chunk's border it leaves the piece's sum, and the sum of sixteen chunks that lie in one
+// run.  A last kernel writes zeros where a token does not occur and adds up the pieces of the runs that cross: two, and the
+// chunks between them, at most 15 + tokens / 256 + 15.
 #include <cuda_runtime.h>
 
 #include <cstdio>
@@ -25,8 +26,9 @@ constexpr int kSortThreads = 256, kSortWarps = 8, kSortItems = 4;
 constexpr int kSortTile = kSortThreads * kSortItems;
 constexpr int kDigitBits = 10, kDigits = 1 << kDigitBits;
 constexpr int kSortBlocks = 64;              // every block reads the counts of all blocks: 64 keep that below 256 KB
-constexpr int64_t kSortOne = 2048;           // up to so many tokens one block sorts in one launch
-constexpr int kChunk = 64, kChunksPerSum = 16, kSpan = kChunk * kChunksPerSum;
+constexpr int64_t kSortOne = 2048;           // up to so many tokens one block sorts in shared memory, in one launch
+constexpr int kChunk = 16, kChunksPerSum = 16, kSpan = kChunk * kChunksPerSum;
+constexpr int kFlight = 8;                   // rows of dout on their way at once
 constexpr int64_t kMaxTokens = (int64_t)1 << 30, kMaxVocab = (int64_t)1 << 30;
 constexpr int64_t kMaxWidth = (int64_t)1 << 24;
 
@@ -85,9 +87,10 @@ struct SortPass {
     const int* pos_in;
     uint32_t* keys_out;
     int* pos_out;
-    int* counts;                       // [digit][block]
+    int* counts;                       // [block][digit]
+    int2* range;                       // [vocab] of sorted places, cleared beside the first pass
     int64_t n, per_block, vocab;
-    int wide_tokens, shift, bits;
+    int wide_tokens, shift, bits, blocks;
 };
 __device__ __forceinline__ uint32_t sort_key(const SortPass& a, int64_t i) {
     if (!a.tokens) return a.keys_in[i];
@@ -103,18 +106,26 @@ __device__ __forceinline__ void sort_count(const SortPass& a, int64_t lo, int64_
     __syncthreads();
 }
 
+// Thread blocks from `first` on clear the ranges.
+__device__ __forceinline__ void clear_ranges(const SortPass& a, int first) {
+    const int64_t step = (int64_t)(gridDim.x - first) * kSortThreads;
+    for (int64_t v = (int64_t)(blockIdx.x - first) * kSortThreads + threadIdx.x; v < a.vocab; v += step) a.range[v] = make_int2(0, 0);
+}
+
 __global__ void __launch_bounds__(kSortThreads)
 k_sort_count(SortPass a) {
     __shared__ int sh[kDigits];
     follow();
     let_follow();
+    if ((int)blockIdx.x >= a.blocks) { clear_ranges(a, a.blocks); return; }
     const int64_t lo = blockIdx.x * a.per_block, hi = lo + a.per_block < a.n ? lo + a.per_block : a.n;
     sort_count(a, lo, hi, sh);
-    for (int d = threadIdx.x; d < 1 << a.bits; d += kSortThreads) a.counts[d * gridDim.x + blockIdx.x] = sh[d];
+    for (int d = threadIdx.x; d < 1 << a.bits; d += kSortThreads) a.counts[(blockIdx.x << a.bits) + d] = sh[d];
 }
 
 struct SortShared {
     int at[kDigits];                   // where a digit's next token goes
+    int before[kDigits];
     int warp[kSortWarps][kDigits];
     int sums[kSortWarps];
 };
@@ -198,43 +209,63 @@ k_sort_place(SortPass a) {
     __shared__ SortShared sh;
     follow();
     let_follow();
-    const int digits = 1 << a.bits, blocks = gridDim.x;
-    int before[4] = {0, 0, 0, 0};
+    // the counts of all blocks, and of those before this one: four digits a thread, the blocks shared out among threads
+    const int digits = 1 << a.bits, quads = digits / 4;      // two bits at least
+    for (int d = threadIdx.x; d < digits; d += kSortThreads) sh.at[d] = sh.before[d] = 0;
+    __syncthreads();
+    {
+        const int q = threadIdx.x % quads, share = threadIdx.x / quads, shares = kSortThreads / quads;
+        int all[4] = {0, 0, 0, 0}, ahead[4] = {0, 0, 0, 0};
+        for (int b0 = share; b0 < a.blocks; b0 += 16 * shares) {
+            int4 c[16];                                     // on their way together
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int d = threadIdx.x * 4 + j;
-        if (d >= digits) continue;
-        int all = 0;
-        for (int b = 0; b < blocks; ++b) {
-            const int c = a.counts[d * blocks + b];
-            all += c;
-            if (b < (int)blockIdx.x) before[j] += c;
+            for (int u = 0; u < 16; ++u) {
+                const int b = b0 + u * shares;
+                c[u] = b < a.blocks ? *reinterpret_cast<const int4*>(a.counts + (b << a.bits) + q * 4) : make_int4(0, 0, 0, 0);
+            }
+#pragma unroll
+            for (int u = 0; u < 16; ++u) {
+                all[0] += c[u].x; all[1] += c[u].y; all[2] += c[u].z; all[3] += c[u].w;
+                if (b0 + u * shares < (int)blockIdx.x) { ahead[0] += c[u].x; ahead[1] += c[u].y; ahead[2] += c[u].z; ahead[3] += c[u].w; }
+            }
         }
-        sh.at[d] = all;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (all[j]) atomicAdd(&sh.at[q * 4 + j], all[j]);
+            if (ahead[j]) atomicAdd(&sh.before[q * 4 + j], ahead[j]);
+        }
     }
+    __syncthreads();
+    int before[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) before[j] = threadIdx.x * 4 + j < digits ? sh.before[threadIdx.x * 4 + j] : 0;
     __syncthreads();
     sort_starts(sh, before, digits);
     const int64_t lo = blockIdx.x * a.per_block, hi = lo + a.per_block < a.n ? lo + a.per_block : a.n;
     sort_place(a, lo, hi, sh);
 }
 
-// All passes in one block.  keys / pos: two buffers each; the sorted ones end in buffer (passes - 1) & 1.
+// All passes in one block, keys and positions in shared memory in between (generic addresses serve both).
+struct SortOne {
+    SortShared sh;
+    uint32_t keys[2][kSortOne];
+    int pos[2][kSortOne];
+};
 __global__ void __launch_bounds__(kSortThreads)
-k_sort_one(SortPass a, uint32_t* keys1, int* pos1, int passes) {
-    __shared__ SortShared sh;
-    uint32_t* const keys[2] = {a.keys_out, keys1};
-    int* const pos[2] = {a.pos_out, pos1};
+k_sort_one(SortPass a, int passes) {
+    extern __shared__ __align__(16) uint8_t raw[];
+    SortOne& s = *reinterpret_cast<SortOne*>(raw);
     let_follow();
+    if (blockIdx.x > 0) { clear_ranges(a, 1); return; }
     for (int p = 0; p < passes; ++p) {
         SortPass b = a;
         b.shift = p * a.bits;
-        if (p) { b.tokens = nullptr; b.keys_in = keys[(p - 1) & 1]; b.pos_in = pos[(p - 1) & 1]; }
-        b.keys_out = keys[p & 1];
-        b.pos_out = pos[p & 1];
-        sort_count(b, 0, b.n, sh.at);
+        if (p) { b.tokens = nullptr; b.keys_in = s.keys[(p - 1) & 1]; b.pos_in = s.pos[(p - 1) & 1]; }
+        if (p + 1 < passes) { b.keys_out = s.keys[p & 1]; b.pos_out = s.pos[p & 1]; }
+        sort_count(b, 0, b.n, s.sh.at);
         const int before[4] = {0, 0, 0, 0};
-        sort_starts(sh, before, 1 << b.bits);
-        sort_place(b, 0, b.n, sh);
+        sort_starts(s.sh, before, 1 << b.bits);
+        sort_place(b, 0, b.n, s.sh);
     }
 }
 
@@ -242,52 +273,49 @@ k_sort_one(SortPass a, uint32_t* keys1, int* pos1, int passes) {
 struct EmbSums {
     const uint32_t* keys;              // sorted
     const int* order;                  // their positions
-    int* start;                        // [vocab + 1] first sorted place of a token
-    float *chunk, *span;               // sums of whole chunks and of sixteen of them, [..][pitch]
+    int2* range;                       // [vocab] sorted places of a token, none: {0, 0}
+    float *chunk, *tail, *span;        // [..][pitch] sums of chunks: of the first run, if it began before (all of the chunk, perhaps); of the
+                                       // last, if it goes on; of sixteen chunks in one run
     int64_t n, vocab, dout_stride, table_stride;
-    int width, pitch, col_tiles, rows_per_warp, bound_blocks, accumulate;
+    int width, pitch, col_tiles, rows_per_warp, accumulate;
     float scale;
 };
 
-// Eight columns of a lane, of the rows order[i .. j) of dout, added in order: neighbours where WIDE, 32 apart elsewhere.
+// Eight columns of a lane, of `take` <= kFlight rows of dout: neighbours where WIDE, 32 apart elsewhere.  The position of row k is in
+// lane (first + k) of `mine`.
 template <class DT, bool WIDE>
-__device__ __forceinline__ void add_rows(const EmbSums& a, const DT* __restrict__ dout, int64_t i, int64_t j, int c0, float (&acc)[8]) {
-    const int lane = threadIdx.x & 31;
-    for (; i < j; i += 32) {
-        const int take = j - i < 32 ? (int)(j - i) : 32;
-        const int mine = lane < take ? a.order[i + lane] : 0;
-        for (int k = 0; k < take; k += 4) {
-            const DT* p[4];
+struct Flight {
+    Raw8<DT> r[kFlight];
+    __device__ __forceinline__ void load(const EmbSums& a, const DT* __restrict__ dout, int mine, int first, int take, int c0) {
 #pragma unroll
-            for (int u = 0; u < 4; ++u) p[u] = dout + (int64_t)__shfl_sync(0xffffffffu, mine, (k + u) & 31) * a.dout_stride;
-            if (WIDE) {
-                Raw8<DT> r[4];
-#pragma unroll
-                for (int u = 0; u < 4; ++u)
-                    if (k + u < take && c0 < a.width) r[u] = load8(p[u] + c0);
-#pragma unroll
-                for (int u = 0; u < 4; ++u)
-                    if (k + u < take && c0 < a.width) {
-                        float v[8];
-                        unpack8(r[u], v);
-#pragma unroll
-                        for (int q = 0; q < 8; ++q) acc[q] += v[q];
-                    }
-            } else {
-                float v[4][8];
-#pragma unroll
-                for (int u = 0; u < 4; ++u)
-#pragma unroll
-                    for (int q = 0; q < 8; ++q) v[u][q] = k + u < take && c0 + 32 * q < a.width ? value_of(p[u][c0 + 32 * q]) : 0.f;
-#pragma unroll
-                for (int u = 0; u < 4; ++u)
-                    if (k + u < take)
-#pragma unroll
-                        for (int q = 0; q < 8; ++q) acc[q] += v[u][q];
-            }
+        for (int k = 0; k < kFlight; ++k) {
+            const DT* p = dout + (int64_t)__shfl_sync(0xffffffffu, mine, (first + k) & 31) * a.dout_stride;
+            if (k < take && c0 < a.width) r[k] = load8(p + c0);
         }
     }
-}
+    __device__ __forceinline__ void add(int k, float (&acc)[8]) const {
+        float v[8];
+        unpack8(r[k], v);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) acc[q] += v[q];
+    }
+};
+template <class DT>
+struct Flight<DT, false> {
+    DT r[kFlight][8];
+    __device__ __forceinline__ void load(const EmbSums& a, const DT* __restrict__ dout, int mine, int first, int take, int c0) {
+#pragma unroll
+        for (int k = 0; k < kFlight; ++k) {
+            const DT* p = dout + (int64_t)__shfl_sync(0xffffffffu, mine, (first + k) & 31) * a.dout_stride;
+#pragma unroll
+            for (int q = 0; q < 8; ++q) r[k][q] = k < take && c0 + 32 * q < a.width ? p[c0 + 32 * q] : rounded<DT>(0.f);
+        }
+    }
+    __device__ __forceinline__ void add(int k, float (&acc)[8]) const {
+#pragma unroll
+        for (int q = 0; q < 8; ++q) acc[q] += value_of(r[k][q]);
+    }
+};
 template <bool WIDE>
 __device__ __forceinline__ void add_sums(const EmbSums& a, const float* __restrict__ from, int64_t i, int64_t j, int c0, float (&acc)[8]) {
 #pragma unroll 4
@@ -307,60 +335,121 @@ __device__ __forceinline__ void add_sums(const EmbSums& a, const float* __restri
     }
 }
 
-// The first blocks find `start`, one token per thread; the others sum whole chunks, a warp each, and whole spans.
-template <class DT, bool WIDE>
-__global__ void __launch_bounds__(512)
-k_emb_chunks(EmbSums a, const DT* __restrict__ dout) {
-    __shared__ float sh[kChunksPerSum][kCols];
+// One row of the gradient: scale acc, on top of what is there if that is wanted.
+template <class TT, bool WIDE>
+__device__ __forceinline__ void put_row(const EmbSums& a, TT* __restrict__ to, int c0, const float (&acc)[8]) {
+    if (WIDE) {
+        if (c0 >= a.width) return;
+        float v[8];
+        if (a.accumulate) {
+            unpack8(load8(to + c0), v);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) v[q] = fmaf(acc[q], a.scale, v[q]);
+        } else {
+#pragma unroll
+            for (int q = 0; q < 8; ++q) v[q] = acc[q] * a.scale;
+        }
+        store8(to + c0, v);
+    } else {
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            const int col = c0 + 32 * q;
+            if (col < a.width) to[col] = rounded<TT>(a.accumulate ? fmaf(acc[q], a.scale, value_of(to[col])) : acc[q] * a.scale);
+        }
+    }
+}
+
+template <bool WIDE>
+__device__ __forceinline__ void put_sum(const EmbSums& a, float* __restrict__ to, int c0, const float (&acc)[8]) {
+    if (WIDE) {
+        if (c0 >= a.width) return;
+        uint32_t r[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) r[q] = __float_as_uint(acc[q]);
+        store32(to + c0, r);
+    } else {
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+            if (c0 + 32 * q < a.width) to[c0 + 32 * q] = acc[q];
+    }
+}
+
+// What lies before and behind the chunk decides what becomes of its first and last run.
+template <class DT, class TT, bool WIDE>
+__global__ void __launch_bounds__(256, sizeof(DT) == 4 || !WIDE ? 2 : 3)
+k_emb_chunks(EmbSums a, const DT* __restrict__ dout, TT* __restrict__ dtable) {
+    __shared__ float sh[kChunksPerSum / 2][kCols];
     follow();
     let_follow();
-    if ((int)blockIdx.x < a.bound_blocks) {
-        const int64_t v = (int64_t)blockIdx.x * 512 + threadIdx.x;
-        if (v > a.vocab) return;
-        int64_t lo = 0, hi = a.n;                           // the first place whose key is not below v
-        while (lo < hi) {
-            const int64_t mid = (lo + hi) >> 1;
-            if (a.keys[mid] < (uint32_t)v) lo = mid + 1; else hi = mid;
-        }
-        a.start[v] = (int)lo;
-        return;
-    }
-    const int64_t job = blockIdx.x - a.bound_blocks;
-    const int64_t s = job / a.col_tiles;
-    const int tile = (int)(job - s * a.col_tiles), warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int64_t s = blockIdx.x / a.col_tiles;
+    const int tile = (int)(blockIdx.x - s * a.col_tiles), warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int c0 = tile * kCols + (WIDE ? lane * 8 : lane);
-    const int64_t c = s * kChunksPerSum + warp, i = c * kChunk;
-    float acc[8] = {};
-    if (i + kChunk <= a.n) {
-        const uint32_t key = a.keys[i];
-        if (key == a.keys[i + kChunk - 1] && key < (uint32_t)a.vocab) {
-            add_rows<DT, WIDE>(a, dout, i, i + kChunk, c0, acc);
-            float* to = a.chunk + c * a.pitch;
+    const uint32_t none = (uint32_t)a.vocab;
+    float both[8] = {};                                     // of two whole chunks, for the span
+    for (int h = 0; h < 2; ++h) {
+        const int64_t c = s * kChunksPerSum + warp * 2 + h, i = c * kChunk;
+        if (i >= a.n) break;
+        const bool in = lane < kChunk && i + lane < a.n;
+        const uint32_t key = in ? a.keys[i + lane] : none;
+        const int mine = in ? a.order[i + lane] : 0;
+        uint32_t before = __shfl_up_sync(0xffffffffu, key, 1), after = __shfl_down_sync(0xffffffffu, key, 1);
+        if (lane == 0) before = i > 0 ? a.keys[i - 1] : none;
+        if (lane == kChunk - 1) after = i + kChunk < a.n ? a.keys[i + kChunk] : none;
+        const int places = __popc(__ballot_sync(0xffffffffu, key < none));               // those without a token come last
+        const unsigned ends = __ballot_sync(0xffffffffu, key < none && after != key);     // last places of runs
+        const bool goes_on = __shfl_sync(0xffffffffu, before == key, 0);                  // the first run began before the chunk
+        if (tile == 0 && key < none) {
+            if (before != key) a.range[key].x = (int)(i + lane);
+            if (after != key) a.range[key].y = (int)(i + lane) + 1;
+        }
+        if (places == 0) break;
+        float acc[8] = {};
+        bool first = goes_on;                               // the run at hand is the rest of an earlier one
+#pragma unroll 1
+        for (int k = 0; k < places; k += kFlight) {
+            const int take = places - k < kFlight ? places - k : kFlight;
+            Flight<DT, WIDE> f;
+            f.load(a, dout, mine, k, take, c0);
 #pragma unroll
-            for (int q = 0; q < 8; ++q) {
-                const int col = WIDE ? c0 + q : c0 + 32 * q;
-                if (col < a.width) to[col] = acc[q];
+            for (int u = 0; u < kFlight; ++u) {
+                if (u >= take) break;
+                f.add(u, acc);
+                if (ends >> (k + u) & 1) {
+                    const int64_t row = __shfl_sync(0xffffffffu, key, k + u);
+                    if (first) put_sum<WIDE>(a, a.chunk + c * a.pitch, c0, acc);
+                    else put_row<TT, WIDE>(a, dtable + row * a.table_stride, c0, acc);
+                    first = false;
+                    if (ends == 1u << (kChunk - 1)) break;            // a whole chunk: the span wants its sum
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) acc[q] = 0.f;
+                }
             }
         }
+        if (!(ends >> (places - 1) & 1)) {                  // the last run goes on: all of the chunk, or its tail
+            put_sum<WIDE>(a, (first || !ends ? a.chunk : a.tail) + c * a.pitch, c0, acc);
+        }
+#pragma unroll
+        for (int q = 0; q < 8; ++q) both[q] += acc[q];
     }
     const int64_t s0 = s * kSpan;
     if (s0 + kSpan > a.n) return;
     const uint32_t key = a.keys[s0];
-    if (key != a.keys[s0 + kSpan - 1] || key >= (uint32_t)a.vocab) return;      // the whole block alike
+    if (key != a.keys[s0 + kSpan - 1] || key >= none) return;                            // the whole block alike
 #pragma unroll
-    for (int q = 0; q < 8; ++q) sh[warp][WIDE ? lane * 8 + q : lane + 32 * q] = acc[q];
+    for (int q = 0; q < 8; ++q) sh[warp][WIDE ? lane * 8 + q : lane + 32 * q] = both[q];
     __syncthreads();
-    if (threadIdx.x < kCols && tile * kCols + (int)threadIdx.x < a.width) {
+    if (tile * kCols + (int)threadIdx.x < a.width) {
         float sum = 0.f;
 #pragma unroll
-        for (int w = 0; w < kChunksPerSum; ++w) sum += sh[w][threadIdx.x];
+        for (int w = 0; w < kChunksPerSum / 2; ++w) sum += sh[w][threadIdx.x];
         a.span[s * a.pitch + tile * kCols + threadIdx.x] = sum;
     }
 }
 
-template <class DT, class TT, bool WIDE>
+// Zeros for tokens that do not occur, sums of the pieces of runs that cross a chunk's border.
+template <class TT, bool WIDE>
 __global__ void __launch_bounds__(256)
-k_emb_rows(EmbSums a, const DT* __restrict__ dout, TT* __restrict__ dtable) {
+k_emb_rows(EmbSums a, TT* __restrict__ dtable) {
     follow();
     const int lane = threadIdx.x & 31;
     const int64_t w = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
@@ -369,56 +458,37 @@ k_emb_rows(EmbSums a, const DT* __restrict__ dout, TT* __restrict__ dtable) {
     const int64_t v0 = group * a.rows_per_warp;
     if (v0 >= a.vocab) return;
     const int rows = a.vocab - v0 < a.rows_per_warp ? (int)(a.vocab - v0) : a.rows_per_warp;
-    const int mine = lane <= rows ? a.start[v0 + lane] : 0;
+    const int2 mine = lane < rows ? a.range[v0 + lane] : make_int2(0, 0);
     const int c0 = tile * kCols + (WIDE ? lane * 8 : lane);
-    for (int r = 0; r < rows; ++r) {
-        int64_t i = __shfl_sync(0xffffffffu, mine, r);
-        const int64_t j = __shfl_sync(0xffffffffu, mine, r + 1);
-        if (a.accumulate && i == j) continue;
+    const unsigned some = __ballot_sync(0xffffffffu, mine.x < mine.y);
+    if (!a.accumulate) {
+        const float zero[8] = {};
+        for (int r = 0; r < rows; ++r)
+            if (!(some >> r & 1)) put_row<TT, WIDE>(a, dtable + (v0 + r) * a.table_stride, c0, zero);
+    }
+    unsigned cross = __ballot_sync(0xffffffffu, mine.x < mine.y && mine.x / kChunk != (mine.y - 1) / kChunk);
+    for (; cross; cross &= cross - 1) {
+        const int r = __ffs(cross) - 1;
+        const int begin = __shfl_sync(0xffffffffu, mine.x, r), end = __shfl_sync(0xffffffffu, mine.y, r);
         float acc[8] = {};
-        if (j - i > kChunk) {
-            const int64_t head = (i + kChunk - 1) / kChunk * kChunk;
-            add_rows<DT, WIDE>(a, dout, i, head, c0, acc);
-            const int64_t c1 = j / kChunk;
-            int64_t c = head / kChunk;
-            // whole chunks up to a whole span, whole spans, the chunks behind them
-            const int64_t s = (c + kChunksPerSum - 1) / kChunksPerSum, s1 = c1 / kChunksPerSum;
-            if (s < s1) {
-                add_sums<WIDE>(a, a.chunk, c, s * kChunksPerSum, c0, acc);
-                add_sums<WIDE>(a, a.span, s, s1, c0, acc);
-                c = s1 * kChunksPerSum;
-            }
-            add_sums<WIDE>(a, a.chunk, c, c1, c0, acc);
-            i = c1 > head / kChunk ? c1 * kChunk : head;
+        int64_t c = begin / kChunk;
+        if (begin % kChunk) { add_sums<WIDE>(a, a.tail, c, c + 1, c0, acc); ++c; }
+        const int64_t whole = end / kChunk, all = (end + kChunk - 1) / kChunk;           // chunks that the run fills end before `whole`
+        const int64_t s = (c + kChunksPerSum - 1) / kChunksPerSum;
+        const int64_t s1 = whole / kChunksPerSum;
+        if (s < s1) {
+            add_sums<WIDE>(a, a.chunk, c, s * kChunksPerSum, c0, acc);
+            add_sums<WIDE>(a, a.span, s, s1, c0, acc);
+            c = s1 * kChunksPerSum;
         }
-        add_rows<DT, WIDE>(a, dout, i, j, c0, acc);
-        TT* to = dtable + (v0 + r) * a.table_stride;
-        if (WIDE) {
-            if (c0 < a.width) {
-                float v[8];
-                if (a.accumulate) {
-                    unpack8(load8(to + c0), v);
-#pragma unroll
-                    for (int q = 0; q < 8; ++q) v[q] = fmaf(acc[q], a.scale, v[q]);
-                } else {
-#pragma unroll
-                    for (int q = 0; q < 8; ++q) v[q] = acc[q] * a.scale;
-                }
-                store8(to + c0, v);
-            }
-        } else {
-#pragma unroll
-            for (int q = 0; q < 8; ++q) {
-                const int col = c0 + 32 * q;
-                if (col < a.width) to[col] = rounded<TT>(a.accumulate ? fmaf(acc[q], a.scale, value_of(to[col])) : acc[q] * a.scale);
-            }
-        }
+        add_sums<WIDE>(a, a.chunk, c, all, c0, acc);
+        put_row<TT, WIDE>(a, dtable + (v0 + r) * a.table_stride, c0, acc);
     }
 }
 
 // ---- host ---------------------------------------------------------------------------------------
 struct EmbRoom {
-    int64_t keys[2], pos[2], counts, start, chunk, span, total;      // offsets in bytes
+    int64_t keys[2], pos[2], counts, range, chunk, tail, span, total;      // offsets in bytes
     int pitch;
 };
 EmbRoom emb_room(const rfast_emb_shape& s) {
@@ -428,8 +498,10 @@ EmbRoom emb_room(const rfast_emb_shape& s) {
     r.pitch = (s.width + 7) / 8 * 8;
     for (int k = 0; k < 2; ++k) { r.keys[k] = take(4 * s.tokens); r.pos[k] = take(4 * s.tokens); }
     r.counts = take(4 * (int64_t)kDigits * kSortBlocks);
-    r.start = take(4 * (s.vocab + 1));
-    r.chunk = take(4 * (s.tokens / kChunk) * r.pitch);
+    r.range = take(8 * s.vocab);
+    const int64_t chunks = (s.tokens + kChunk - 1) / kChunk;
+    r.chunk = take(4 * chunks * r.pitch);
+    r.tail = take(4 * chunks * r.pitch);
     r.span = take(4 * (s.tokens / kSpan) * r.pitch);
     r.total = at;
     return r;
@@ -454,7 +526,8 @@ const char* emb_rows_fault(const void* p, int type, int64_t stride, int64_t rows
     return nullptr;
 }
 bool emb_wide(const void* p, int type, int64_t stride, int width) {
-    return width % 8 == 0 && (uintptr_t)p % 16 == 0 && stride * (int64_t)bytes_of(type) % 16 == 0;
+    const int64_t b = (int64_t)bytes_of(type);
+    return width % 8 == 0 && (uintptr_t)p % (8 * b) == 0 && stride % 8 == 0;
 }
 
 struct EmbCall {
@@ -484,17 +557,18 @@ cudaError_t look_up_types(const EmbCall& c) {
 }
 
 template <class DT, class TT, bool WIDE>
-cudaError_t sums(const EmbSums& a, const void* dout, void* dtable, cudaStream_t st, bool after) {
-    const int64_t spans = a.n / kChunk > 0 ? (a.n + kSpan - 1) / kSpan : 0;
-    const int64_t blocks = a.bound_blocks + spans * a.col_tiles;
-    cudaError_t e = launch(k_emb_chunks<DT, WIDE>, dim3((unsigned)blocks), 512, 0, st, after, a, (const DT*)dout);
-    if (e != cudaSuccess) return e;
+cudaError_t sums(const EmbSums& a, const void* dout, void* dtable, cudaStream_t st) {
+    const int64_t blocks = (a.n + kSpan - 1) / kSpan * a.col_tiles;
+    if (blocks > 0) {
+        const cudaError_t e = launch(k_emb_chunks<DT, TT, WIDE>, dim3((unsigned)blocks), 256, 0, st, true, a, (const DT*)dout, (TT*)dtable);
+        if (e != cudaSuccess) return e;
+    }
     const int64_t groups = (a.vocab + a.rows_per_warp - 1) / a.rows_per_warp;
-    return launch(k_emb_rows<DT, TT, WIDE>, dim3((unsigned)((groups * a.col_tiles + 7) / 8)), 256, 0, st, true, a, (const DT*)dout, (TT*)dtable);
+    return launch(k_emb_rows<TT, WIDE>, dim3((unsigned)((groups * a.col_tiles + 7) / 8)), 256, 0, st, true, a, (TT*)dtable);
 }
 template <class DT, class TT>
-cudaError_t sums_types(const EmbSums& a, const void* dout, void* dtable, bool wide, cudaStream_t st, bool after) {
-    return wide ? sums<DT, TT, true>(a, dout, dtable, st, after) : sums<DT, TT, false>(a, dout, dtable, st, after);
+cudaError_t sums_types(const EmbSums& a, const void* dout, void* dtable, bool wide, cudaStream_t st) {
+    return wide ? sums<DT, TT, true>(a, dout, dtable, st) : sums<DT, TT, false>(a, dout, dtable, st);
 }
 
 }  // namespace
@@ -556,14 +630,13 @@ extern "C" int rfast_embedding_backward(const rfast_emb_shape* shape, const void
     if ((fault = emb_rows_fault(d_dtable, shape->table_type, dtable_stride, shape->vocab, shape->width, true)))
         return op_fail(err, err_len, RFAST_EINVAL, "%s: dtable %s", me, fault);
     const EmbRoom room = emb_room(*shape);
-    if (!workspace || (uintptr_t)workspace % 16) return op_fail(err, err_len, RFAST_EINVAL, "%s: the workspace must be given, aligned to 16 bytes", me);
+    if (!workspace || (uintptr_t)workspace % 32) return op_fail(err, err_len, RFAST_EINVAL, "%s: the workspace must be given, aligned to 32 bytes", me);
     if (workspace_bytes < (size_t)room.total)
         return op_fail(err, err_len, RFAST_EINVAL, "%s: the workspace needs %lld bytes", me, (long long)room.total);
     if (n == 0 && accumulate) return RFAST_OK;
     const int64_t col_tiles = (shape->width + kCols - 1) / kCols;
     const int rows_per_warp = shape->vocab * col_tiles >= (int64_t)8 * 148 * 32 ? 8 : 1;    // few rows: a warp each
-    const int64_t bound_blocks = (shape->vocab + 1 + 511) / 512;
-    if ((shape->vocab / rows_per_warp + 1) * col_tiles / 8 >= 0x7fffffff || bound_blocks + (n / kSpan + 1) * col_tiles >= 0x7fffffff)
+    if ((shape->vocab / rows_per_warp + 1) * col_tiles / 8 >= 0x7fffffff || (n / kSpan + 1) * col_tiles >= 0x7fffffff)
         return op_fail(err, err_len, RFAST_EINVAL, "%s: more thread blocks than a launch takes", me);
     const void* ptrs[] = {n > 0 ? d_tokens : nullptr, n > 0 ? d_dout : nullptr, d_dtable, workspace};
     const char* names[] = {"rfast_embedding_backward: tokens", "rfast_embedding_backward: dout", "rfast_embedding_backward: dtable", "rfast_embedding_backward: workspace"};
@@ -585,19 +658,25 @@ extern "C" int rfast_embedding_backward(const rfast_emb_shape* shape, const void
     p.vocab = shape->vocab;
     p.wide_tokens = shape->token_bits == 64;
     p.bits = (bits + passes - 1) / passes;
+    if (p.bits < 2) p.bits = 2;
     p.counts = (int*)(base + room.counts);
+    p.range = (int2*)(base + room.range);
+    // blocks that clear the ranges: 2048 of them each, up to two per SM
+    const int64_t clear = (shape->vocab + 2047) / 2048, clear_blocks = clear < 296 ? clear : 296;
     cudaError_t e = cudaSuccess;
-    if (n > 0 && n <= kSortOne) {
+    if (n <= kSortOne) {                                    // no tokens: the ranges are cleared all the same
         p.tokens = d_tokens;
-        p.keys_out = keys[0];
-        p.pos_out = pos[0];
+        p.keys_out = keys[(passes - 1) & 1];
+        p.pos_out = pos[(passes - 1) & 1];
         p.per_block = n;
-        e = launch(k_sort_one, dim3(1), kSortThreads, 0, st, false, p, keys[1], pos[1], passes);
-    } else if (n > 0) {
-        const int64_t want = (n + kSortOne - 1) / kSortOne;
+        p.blocks = 1;
+        e = cudaFuncSetAttribute(k_sort_one, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(SortOne));
+        if (e == cudaSuccess) e = launch(k_sort_one, dim3(1 + (unsigned)clear_blocks), kSortThreads, sizeof(SortOne), st, false, p, passes);
+    } else {
+        const int64_t want = (n + kSortTile - 1) / kSortTile;
         const int64_t blocks = want < kSortBlocks ? want : kSortBlocks;
         p.per_block = (n + blocks - 1) / blocks;
-        const int64_t used = (n + p.per_block - 1) / p.per_block;
+        p.blocks = (int)((n + p.per_block - 1) / p.per_block);
         for (int k = 0; k < passes && e == cudaSuccess; ++k) {
             p.shift = k * p.bits;
             p.tokens = k ? nullptr : d_tokens;
@@ -605,16 +684,17 @@ extern "C" int rfast_embedding_backward(const rfast_emb_shape* shape, const void
             p.pos_in = k ? pos[(k - 1) & 1] : nullptr;
             p.keys_out = keys[k & 1];
             p.pos_out = pos[k & 1];
-            e = launch(k_sort_count, dim3((unsigned)used), kSortThreads, 0, st, k > 0, p);
-            if (e == cudaSuccess) e = launch(k_sort_place, dim3((unsigned)used), kSortThreads, 0, st, true, p);
+            e = launch(k_sort_count, dim3((unsigned)(p.blocks + (k ? 0 : clear_blocks))), kSortThreads, 0, st, k > 0, p);
+            if (e == cudaSuccess) e = launch(k_sort_place, dim3((unsigned)p.blocks), kSortThreads, 0, st, true, p);
         }
     }
     if (e == cudaSuccess) {
         EmbSums a{};
         a.keys = keys[(passes - 1) & 1];
         a.order = pos[(passes - 1) & 1];
-        a.start = (int*)(base + room.start);
+        a.range = (int2*)(base + room.range);
         a.chunk = (float*)(base + room.chunk);
+        a.tail = (float*)(base + room.tail);
         a.span = (float*)(base + room.span);
         a.n = n;
         a.vocab = shape->vocab;
@@ -624,11 +704,10 @@ extern "C" int rfast_embedding_backward(const rfast_emb_shape* shape, const void
         a.pitch = room.pitch;
         a.col_tiles = (int)col_tiles;
         a.rows_per_warp = rows_per_warp;
-        a.bound_blocks = (int)bound_blocks;
         a.accumulate = accumulate != 0;
         a.scale = scale;
         const bool wide = emb_wide(d_dtable, shape->table_type, dtable_stride, shape->width) && (n == 0 || emb_wide(d_dout, shape->out_type, dout_stride, shape->width));
-        e = RFAST_TWO_TYPES(sums_types, shape->out_type, shape->table_type, a, d_dout, d_dtable, wide, st, n > 0);
+        e = RFAST_TWO_TYPES(sums_types, shape->out_type, shape->table_type, a, d_dout, d_dtable, wide, st);
     }
     if (e != cudaSuccess) return op_fail(err, err_len, RFAST_ECUDA, "%s: kernel launch: %s", me, cudaGetErrorString(e));
     return RFAST_OK;

@@ -107,7 +107,7 @@ __device__ __forceinline__ double momentum_part(const MuonMat& a, const MuonScal
         const float u = c.nesterov ? fmaf(c.mu, m, c.omu * gv) : m;
         sum = fma((double)u, (double)u, sum);
     };
-    if ((uintptr_t)g % 16 == 0 && (uintptr_t)a.momentum % 16 == 0) {
+    if ((uintptr_t)g % (8 * sizeof(GT)) == 0 && (uintptr_t)a.momentum % 32 == 0) {
         const int64_t end = lo + (hi - lo) / 8 * 8;
 #pragma unroll 2
         for (int64_t i = lo + threadIdx.x * 8; i < end; i += 256 * 8) {
@@ -116,9 +116,7 @@ __device__ __forceinline__ double momentum_part(const MuonMat& a, const MuonScal
             unpack8(load8(a.momentum + i), mv);
 #pragma unroll
             for (int k = 0; k < 8; ++k) one(mv[k], gv[k]);
-            float4* to = reinterpret_cast<float4*>(a.momentum + i);
-            to[0] = make_float4(mv[0], mv[1], mv[2], mv[3]);
-            to[1] = make_float4(mv[4], mv[5], mv[6], mv[7]);
+            store8(a.momentum + i, mv);
         }
         lo = end;
     }
@@ -182,7 +180,7 @@ __device__ __forceinline__ void keep8(__half* to, int64_t low_plane, const float
 template <class GT>
 __device__ __forceinline__ void begin_tile(const MuonMat& a, const MuonScalars& c, int r0, int c0, float scale, float f1, float f2, float (*tile)[65]) {
     const GT* const g = (const GT*)a.grad;
-    const bool wide = a.cols % 8 == 0 && (uintptr_t)g % 16 == 0 && (uintptr_t)a.momentum % 16 == 0;
+    const bool wide = a.cols % 8 == 0 && (uintptr_t)g % (8 * sizeof(GT)) == 0 && (uintptr_t)a.momentum % 32 == 0;
     const auto value = [&](float m, float gv) { return (c.nesterov ? fmaf(c.mu, m, c.omu * (gv * scale)) : m) * f1 * f2; };
     if (wide) {
 #pragma unroll

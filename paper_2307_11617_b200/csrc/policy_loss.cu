@@ -20,6 +20,7 @@ namespace rfast {
 namespace {
 
 constexpr int kBlockTeam = 1024;             // threads of a long row's block
+constexpr int kAhead = 4;                    // groups of eight logits that a thread has on their way
 constexpr int64_t kShortRow = 2048;          // up to so many logits a warp does the row
 
 struct Policy {
@@ -103,10 +104,11 @@ __device__ __forceinline__ RowOut row_numbers(const Policy& a, int64_t row, Run 
     return o;
 }
 
-// A row cut at multiples of 16 bytes: `head` values, then groups of eight, then the rest.  ALIGN: the byte offset of logits and
-// gradients within 16 bytes is the same, so that the groups are whole in both.
+// A row cut at multiples of eight values' size: `head` values, then groups of eight, then the rest.  ALIGN: logits and gradients
+// begin at the same place within a group, so that the groups are whole in both.
 template <class T> __device__ __forceinline__ int head_of(const T* p, int64_t n) {
-    const int h = (int)(((16 - ((uintptr_t)p & 15)) & 15) / sizeof(T));
+    constexpr uintptr_t kGroup = 8 * sizeof(T);
+    const int h = (int)(((kGroup - ((uintptr_t)p & (kGroup - 1))) & (kGroup - 1)) / sizeof(T));
     return h < n ? h : (int)n;
 }
 
@@ -138,22 +140,18 @@ __device__ __forceinline__ void policy_row(const Policy& a, int64_t row, int tid
     Run r{-INFINITY, 0.f};
     {
         const T* g0 = z + head;
-        int64_t g = tid;
-        for (; g + 3 * TEAM < groups; g += 4 * TEAM) {
-            Raw8<T> q[4];
+        for (int64_t g = tid; g < groups; g += kAhead * TEAM) {
+            Raw8<T> q[kAhead];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) q[u] = load8(g0 + (g + u * TEAM) * 8);
+            for (int u = 0; u < kAhead; ++u)
+                if (g + u * TEAM < groups) q[u] = load8(g0 + (g + u * TEAM) * 8);
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                float v[8];
-                unpack8(q[u], v);
-                take(r, v, k);
-            }
-        }
-        for (; g < groups; g += TEAM) {
-            float v[8];
-            unpack8(load8(g0 + g * 8), v);
-            take(r, v, k);
+            for (int u = 0; u < kAhead; ++u)
+                if (g + u * TEAM < groups) {
+                    float v[8];
+                    unpack8(q[u], v);
+                    take(r, v, k);
+                }
         }
         if (tid < head) { const float v[1] = {value_of(z[tid])}; take(r, v, k); }
         for (int64_t i = head + groups * 8 + tid; i < n; i += TEAM) { const float v[1] = {value_of(z[i])}; take(r, v, k); }
@@ -196,33 +194,25 @@ __device__ __forceinline__ void policy_row(const Policy& a, int64_t row, int tid
     if (ALIGN) {
         const T* g0 = z + head;
         T* d0 = dz + head;
-        // back to front: the last logits read are the surest to be near
-        int64_t g = tid;
-        for (; g + 3 * TEAM < groups; g += 4 * TEAM) {
-            Raw8<T> q[4];
+        for (int64_t g = tid; g < groups; g += kAhead * TEAM) {
+            Raw8<T> q[kAhead];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) q[u] = load8(g0 + (g + u * TEAM) * 8);
+            for (int u = 0; u < kAhead; ++u)
+                if (g + u * TEAM < groups) q[u] = load8(g0 + (g + u * TEAM) * 8);
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                float v[8];
-                unpack8(q[u], v);
-                const int64_t i0 = head + (g + u * TEAM) * 8;
+            for (int u = 0; u < kAhead; ++u)
+                if (g + u * TEAM < groups) {
+                    float v[8];
+                    unpack8(q[u], v);
+                    const int64_t i0 = head + (g + u * TEAM) * 8;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = out.p * two_to(fmaf(v[j], k, -out.base));
-                if ((uint64_t)(t - i0) < 8) {
+                    for (int j = 0; j < 8; ++j) v[j] = out.p * two_to(fmaf(v[j], k, -out.base));
+                    if ((uint64_t)(t - i0) < 8) {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) v[j] += i0 + j == t ? out.slope : 0.f;
+                        for (int j = 0; j < 8; ++j) v[j] += i0 + j == t ? out.slope : 0.f;
+                    }
+                    store8(d0 + (g + u * TEAM) * 8, v);
                 }
-                store8(d0 + (g + u * TEAM) * 8, v);
-            }
-        }
-        for (; g < groups; g += TEAM) {
-            float v[8];
-            unpack8(load8(g0 + g * 8), v);
-            const int64_t i0 = head + g * 8;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = slope_of(v[j], i0 + j);
-            store8(d0 + g * 8, v);
         }
         if (tid < head) dz[tid] = rounded<T>(slope_of(value_of(z[tid]), tid));
         for (int64_t i = head + groups * 8 + tid; i < n; i += TEAM) dz[i] = rounded<T>(slope_of(value_of(z[i]), i));
@@ -341,10 +331,10 @@ extern "C" int rfast_policy_loss(const rfast_policy* p, void* cuda_stream, char*
     cudaStream_t st = (cudaStream_t)cuda_stream;
     cudaError_t e = cudaSuccess;
     if (p->tokens > 0) {
-        // the offset within 16 bytes is the same in every row of both
+        // the offset within eight values is the same in every row of both
         const int64_t b = (int64_t)bytes_of(p->type);
-        const bool align = !p->d_dlogits || (((uintptr_t)p->d_logits ^ (uintptr_t)p->d_dlogits) % 16 == 0 &&
-                                             (p->logits_stride * b - p->dlogits_stride * b) % 16 == 0);
+        const bool align = !p->d_dlogits || (((uintptr_t)p->d_logits ^ (uintptr_t)p->d_dlogits) % (8 * b) == 0 &&
+                                             (p->logits_stride - p->dlogits_stride) % 8 == 0);
         switch (p->type) {
             case RFAST_TYPE_F32: e = policy_types<float>(a, align, st); break;
             case RFAST_TYPE_BF16: e = policy_types<__nv_bfloat16>(a, align, st); break;

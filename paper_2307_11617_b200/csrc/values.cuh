@@ -1,5 +1,5 @@
-// Values of the operators' types in registers: eight at a time where addresses are multiples of 16 bytes, one at a
-// time elsewhere.  Launches that follow one another inside one call.
+// Values of the operators' types in registers: eight at a time where addresses are multiples of their size (32 bytes of fp32, 16 of
+// the others), one at a time elsewhere.  Launches that follow one another inside one call.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -20,19 +20,30 @@ template <> __device__ __forceinline__ float rounded<float>(float v) { return v;
 template <> __device__ __forceinline__ __nv_bfloat16 rounded<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 template <> __device__ __forceinline__ __half rounded<__half>(float v) { return __float2half_rn(v); }
 
-// Eight neighbouring values as they lie in memory.
+// 32 bytes at a multiple of 32: a whole sector per lane.
+__device__ __forceinline__ void load32(const void* p, uint32_t (&r)[8]) {
+    asm volatile("ld.global.L1::no_allocate.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "l"(p));
+}
+__device__ __forceinline__ void store32(void* p, const uint32_t (&r)[8]) {
+    asm volatile("st.global.v8.b32 [%8], {%0,%1,%2,%3,%4,%5,%6,%7};"
+                 ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "l"(p) : "memory");
+}
+
+// Eight neighbouring values as they lie in memory, from a multiple of their size in bytes.
 template <class T> struct Raw8 { uint4 q; };
-template <> struct Raw8<float> { float4 a, b; };
+template <> struct Raw8<float> { uint32_t q[8]; };
 
 __device__ __forceinline__ Raw8<float> load8(const float* p) {
-    const float4* q = reinterpret_cast<const float4*>(p);
-    return {q[0], q[1]};
+    Raw8<float> r;
+    load32(p, r.q);
+    return r;
 }
 template <class T> __device__ __forceinline__ Raw8<T> load8(const T* p) { return {*reinterpret_cast<const uint4*>(p)}; }
 
 __device__ __forceinline__ void unpack8(const Raw8<float>& r, float (&v)[8]) {
-    v[0] = r.a.x; v[1] = r.a.y; v[2] = r.a.z; v[3] = r.a.w;
-    v[4] = r.b.x; v[5] = r.b.y; v[6] = r.b.z; v[7] = r.b.w;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r.q[i]);
 }
 __device__ __forceinline__ void unpack8(const Raw8<__nv_bfloat16>& r, float (&v)[8]) {
     const uint32_t w[4] = {r.q.x, r.q.y, r.q.z, r.q.w};
@@ -53,8 +64,10 @@ __device__ __forceinline__ void unpack8(const Raw8<__half>& r, float (&v)[8]) {
 }
 
 __device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
-    __stcs(reinterpret_cast<float4*>(p), make_float4(v[0], v[1], v[2], v[3]));
-    __stcs(reinterpret_cast<float4*>(p) + 1, make_float4(v[4], v[5], v[6], v[7]));
+    uint32_t r[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = __float_as_uint(v[i]);
+    store32(p, r);
 }
 __device__ __forceinline__ uint32_t packed(float a, float b, const __nv_bfloat16*) {
     const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
@@ -67,16 +80,6 @@ __device__ __forceinline__ uint32_t packed(float a, float b, const __half*) {
 template <class T>
 __device__ __forceinline__ void store8(T* p, const float (&v)[8]) {
     __stcs(reinterpret_cast<uint4*>(p), make_uint4(packed(v[0], v[1], p), packed(v[2], v[3], p), packed(v[4], v[5], p), packed(v[6], v[7], p)));
-}
-
-// 32 bytes at a multiple of 32, past the first-level cache.
-__device__ __forceinline__ void load32(const void* p, uint32_t (&r)[8]) {
-    asm volatile("ld.global.L1::no_allocate.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "l"(p));
-}
-__device__ __forceinline__ void store32(void* p, const uint32_t (&r)[8]) {
-    asm volatile("st.global.v8.b32 [%8], {%0,%1,%2,%3,%4,%5,%6,%7};"
-                 ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "l"(p) : "memory");
 }
 
 inline size_t bytes_of(int type) { return type == RFAST_TYPE_F32 ? 4 : 2; }

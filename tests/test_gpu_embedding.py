@@ -1,9 +1,9 @@
 """Embedding look-up and its gradient against plain restatements in 64 bits.
 
 u = 2^-24 is half a step of fp32.  A look-up is one fp32 product rounded once to its type, and so is the restatement: equal bits.
-A gradient is a sum in fp32 whose longest chain has at most 64 + 16 + spans + 16 + 64 additions after sums of 64 and of 16 terms, each off
-by at most u of the sum of magnitudes: (chain) u sum|x| with chain = min(count, 240 + n / 1024), 2 u for the scale's product (and the sum
-with what was there, u of that), then half a step of the gradient's type."""
+A gradient is a sum in fp32: chunks of up to 16 terms, sixteen of those to a span of 256, and of a run at most two pieces, 15 chunks before and
+15 behind its n / 256 spans.  Each addition is off by at most u of the sum of magnitudes: (chain) u sum|x| with chain = min(count, 16 + 16 +
+32 + n / 256), 2 u for the scale's product (and the sum with what was there, u of that), then half a step of the gradient's type."""
 
 from __future__ import annotations
 
@@ -45,10 +45,10 @@ def _tokens(n, vocab, how, rng):
         t = (np.exp(rng.random(n) * math.log(vocab + 1.0)) - 1.0).astype(np.int64).clip(0, vocab - 1) * 7919 % vocab
     elif how == "one":
         t = np.full(n, vocab // 2)
-    elif how == "runs":                     # runs that begin and end at, before and behind multiples of 64 and 1024
+    elif how == "runs":                     # runs that begin and end at, before and behind multiples of 16 and 256
         t = np.zeros(n, np.int64)
         at, k = 0, 0
-        for size in [64, 1, 63, 65, 1024, 1, 1023, 128, 2, 62, 2048, 1000, 1048, 3000] * (n // 10000 + 1):
+        for size in [64, 1, 63, 65, 1024, 1, 1023, 128, 2, 62, 2048, 1000, 1048, 3000, 16, 15, 1, 17, 255, 256, 257, 32, 240] * (n // 10000 + 1):
             t[at:at + size] = k % vocab
             at, k = at + size, k + 1
         t = t[rng.permutation(n)]
@@ -103,7 +103,7 @@ def _check_gradient(got, t, dout, vocab, scale, kind, before=None):
     import torch
     total, size, count = _gradient(t, dout, vocab, scale)
     n = dout.shape[0]
-    chain = torch.clamp(count, max=240 + n / 1024)[:, None]
+    chain = torch.clamp(count, max=64 + n / 256)[:, None]
     tol = (chain + 2) * U * size
     if before is not None:
         tol = tol + U * (before.abs() + total.abs())
