@@ -524,7 +524,7 @@ k_muon_product(const __grid_constant__ MuonGemm p) {
             const int in_a = x_first ? in_x : in_s, in_b = x_second ? in_x : in_s;
             const int limit_a = stored_up_to<S>(row0), limit_b = stored_up_to<S>(col0);
             for (int kb = 0; kb < blocks; ++kb) {
-                if (!(ok = tc::bar_wait(&empty[s], turn))) break;
+                if (!(ok = tc::bar_wait_warp(&empty[s], turn))) break;
                 const int k0 = kb * kBox;
                 // A and B above their stored tiles are read as the transposed ones below, rows along the other dimension
                 const bool across_a = across<OP>(x_first, k0 >= limit_a), across_b = across<OP>(x_second, k0 >= limit_b);
@@ -564,11 +564,11 @@ k_muon_product(const __grid_constant__ MuonGemm p) {
                     const bool begin = kSegmented ? kb % kSegment == 0 : kb == 0;
                     if (begin) {
                         buf = sums & 1;
-                        if (!(ok = tc::bar_wait(&acc_empty[buf], ~(sums >> 1) & 1))) break;
+                        if (!(ok = tc::bar_wait_warp(&acc_empty[buf], ~(sums >> 1) & 1))) break;
                         to = acc + buf * S::kTN;
                         ++sums;
                     }
-                    if (!(ok = tc::bar_wait(&full[s], turn))) break;
+                    if (!(ok = tc::bar_wait_warp(&full[s], turn))) break;
                     tc::fence_after();
                     const bool across_a = across<OP>(x_first, kb * kBox >= limit_a), across_b = across<OP>(x_second, kb * kBox >= limit_b);
                     const uint32_t instruction = tc::instruction_f16(S::kTM, S::kTN) | (across_a ? tc::kAcrossA : 0u) | (across_b ? tc::kAcrossB : 0u);
@@ -600,7 +600,7 @@ k_muon_product(const __grid_constant__ MuonGemm p) {
         constexpr int kChunks = S::kTN / 64;                // of 32 columns, of a warp
         int sums = 0;                                       // read so far
         const auto wait = [&] {
-            const bool ok = __all_sync(0xffffffffu, tc::bar_wait(&acc_full[sums & 1], (sums >> 1) & 1));
+            const bool ok = tc::bar_wait_warp(&acc_full[sums & 1], (sums >> 1) & 1);
             if (!ok && lane == 0) { atomicExch(status, 3); bad = 1; }
             tc::fence_after();
             return ok;

@@ -1,27 +1,35 @@
 // Clipped policy loss with a KL term, out of logits, and its gradient (see rfast_policy_loss in rfast.h for the formulas).
 //
-// A row of logits is a team's work: a warp's for short rows, a thread block's for long ones.  The first pass holds a running
-// maximum and sum of each thread's values (one pass, rescaled where the maximum grows), which are merged in a fixed order; one
-// thread forms the row's numbers in 64 bits; the second pass writes the gradient, reading the logits again.  That second read
-// finds them in the L2 cache, so that memory sees each logit once in and each gradient once out, which is what bounds it.
+// What bounds it is memory, where a logit has to come in once and its gradient to leave once.  The first pass over a row holds a running
+// maximum and sum of each thread's values, which are merged in a fixed order; one warp forms the row's numbers in 64 bits; the
+// second pass writes the gradient out of the logits again.  A warp does a row of up to 1024 logits, a block of 128 threads one of
+// up to 8192, a block of 512 longer ones, or, where rows are few, a cluster of up to eight blocks.  A thread of these keeps the first
+// logits that it reads in shared memory, 96 KB a block; the rest it reads again, the last first.  Without that the rows under way,
+// 296 of 256 KB, are too much for the L2 cache: 4096 x 128256 bf16 read 1.72 GB instead of 0.93, 445 us.  (Bringing rows through a ring
+// in shared memory by bulk copies, a cluster to a row and the next row's sum before this one's gradient, read every logit
+// once and took 510 us: with 20 instructions a logit in the place of 13 the issue slots were the bound.)
 //
 // Powers are taken of two: exp((z - c) / T) = 2^(z k - c') with k = log2(e) / T in fp32 and c' the rounded z_max k.  k is the only
 // constant that both passes and the row's numbers share, so rounding it is a change of T by 2^-25 of itself and nothing else.
 #include <cuda_runtime.h>
 
+#include <climits>
 #include <cmath>
 #include <cstdio>
 
 #include "ops.h"
+#include "tensor_core.cuh"
 #include "values.cuh"
 
 namespace rfast {
 
 namespace {
 
-constexpr int kBlockTeam = 1024;             // threads of a long row's block
-constexpr int kAhead = 4;                    // groups of eight logits that a thread has on their way
-constexpr int64_t kShortRow = 2048;          // up to so many logits a warp does the row
+constexpr int kBlockTeam = 512, kMidTeam = 128;
+constexpr int kPlaces = 240;                 // blocks of 512 threads that run at once, less what clusters cannot use
+constexpr int kAhead = 4;                    // groups of eight logits that a thread has on their way (four more, fetched while it works: no gain)
+constexpr int64_t kShortRow = 1024, kMidRow = 8192;          // logits of a row up to which a warp, a small block does it
+constexpr int kKept = 96 * 1024;             // bytes of a row that a long row's block keeps; two blocks share an SM
 
 struct Policy {
     const void* logits;
@@ -43,64 +51,85 @@ __device__ __forceinline__ float two_to(float x) {
     return r;
 }
 
-// Running maximum and sum of 2^(z k - max k) over what a thread has seen.
+// Sum of 2^(z k - c) over what a thread has seen.  The reference c is the rounded product of k and an earlier maximum (never one exact in a
+// multiply-add): it follows the maximum only where that is 2^kSlack ahead, so that sums are seldom rescaled, and terms below
+// 2^-126 at the reference are 2^-126 of the largest term and less.  No logit but -infinity and NaN so far: c is -infinity.
 struct Run {
-    float top, sum;
+    float c, sum;
 };
-// The reference of exponents: the rounded product of the maximum and k (never one exact in a multiply-add), 0 where there is no
-// maximum yet.
-__device__ __forceinline__ float base_of(float top, float k) { return top == -INFINITY ? 0.f : __fmul_rn(top, k); }
-// The factor that takes a sum to the reference c.  A run that saw nothing but -infinity and NaN keeps its sum, 0 or NaN.
-__device__ __forceinline__ float rescale(float top, float c, float k) { return top == -INFINITY ? 1.f : two_to(__fmul_rn(top, k) - c); }
-__device__ __forceinline__ Run merged(Run a, Run b, float k) {
-    Run r;
-    r.top = fmaxf(a.top, b.top);
-    const float c = base_of(r.top, k);
-    r.sum = a.sum * rescale(a.top, c, k) + b.sum * rescale(b.top, c, k);
-    return r;
+constexpr float kSlack = 40.f;
+// what is subtracted: 0 where there is no reference yet (-infinity less 0 is -infinity)
+__device__ __forceinline__ float base_of(float c) { return c == -INFINITY ? 0.f : c; }
+// the factor that takes a sum to the reference `to`; a run without one keeps its sum, 0 or NaN
+__device__ __forceinline__ float rescale(float c, float to) { return c == -INFINITY ? 1.f : two_to(c - to); }
+// Merged over a warp: the largest reference first, so that each sum is taken to it once.
+__device__ __forceinline__ Run merged_warp(Run r) {
+    float c = r.c;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) c = fmaxf(c, __shfl_xor_sync(0xffffffffu, c, o));
+    float sum = r.sum * rescale(r.c, base_of(c));
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    return {c, sum};
+}
+__device__ __forceinline__ void follow_top(Run& r, float top, float k) {
+    const float to = __fmul_rn(top, k);
+    if (to > r.c + kSlack) {
+        r.sum *= rescale(r.c, to);
+        r.c = to;
+    }
 }
 template <int N>
 __device__ __forceinline__ void take(Run& r, const float (&v)[N], float k) {
-    float top = r.top;
+    float top = v[0];
 #pragma unroll
-    for (int i = 0; i < N; ++i) top = fmaxf(top, v[i]);
-    const float c = base_of(top, k);
-    float sum = top > r.top ? r.sum * rescale(r.top, c, k) : r.sum;
+    for (int i = 1; i < N; ++i) top = fmaxf(top, v[i]);
+    follow_top(r, top, k);
+    const float c = base_of(r.c);
 #pragma unroll
-    for (int i = 0; i < N; ++i) sum += two_to(fmaf(v[i], k, -c));
-    r.top = top;
-    r.sum = sum;
+    for (int i = 0; i < N; ++i) r.sum += two_to(fmaf(v[i], k, -c));
 }
 
 // What the second pass needs of a row: the gradient is p * 2^(z k - base), at the token plus `slope`.
 struct RowOut {
     float base, p, slope;
-    int live;
 };
 
-// One thread: the row's loss and slope, in 64 bits, from the merged run and the token's logit.
-__device__ __forceinline__ RowOut row_numbers(const Policy& a, int64_t row, Run r, float zt) {
-    const double base = (double)base_of(r.top, a.k);
+// A warp: the row's loss and slope, in 64 bits, from the merged run, the token's logit and what belongs to the row (lane 0's).  Lanes
+// 0 and 1 take the two exponentials side by side.
+struct RowIn {
+    float zt, adv, w, old, ref, scale;
+};
+template <class T>
+__device__ __forceinline__ RowIn row_in(const Policy& a, int64_t row, const T* z, int64_t t) {
+    return {value_of(z[t]), a.advantage[row], a.weight ? a.weight[row] : 1.f, a.old_logp[row], a.ref_logp ? a.ref_logp[row] : 0.f, a.scale ? *a.scale : 1.f};
+}
+__device__ __forceinline__ RowOut row_numbers(const Policy& a, int64_t row, Run r, const RowIn& in, bool keep) {
+    const int lane = threadIdx.x & 31;
+    const double base = (double)base_of(r.c);
+    const float zt = __shfl_sync(0xffffffffu, in.zt, 0), ref = __shfl_sync(0xffffffffu, in.ref, 0), old = __shfl_sync(0xffffffffu, in.old, 0);
     const double logp = a.ln2k * ((double)zt * (double)a.k - base - log2((double)r.sum));
-    const double adv = a.advantage[row], w = a.weight ? (double)a.weight[row] : 1.0;
-    const double ratio = exp(logp - (double)a.old_logp[row]);
-    const double held = ratio < a.clip_lo ? a.clip_lo : ratio > a.clip_hi ? a.clip_hi : ratio;
-    const double one = ratio * adv, two = held * adv;
-    const bool pass = !(one > two);                         // a NaN passes
-    double loss = pass ? -one : -two, slope = pass ? -one : 0.0;
-    if (a.ref_logp) {
-        const double d = (double)a.ref_logp[row] - logp, e = expm1(d);
-        loss += a.kl * (e - d);
-        slope -= a.kl * e;
+    const double d = (double)ref - logp;
+    const double e = lane < 2 ? expm1(lane ? d : logp - (double)old) : 0.0;
+    const double e1 = __shfl_sync(0xffffffffu, e, 1);
+    RowOut o{};
+    if (lane == 0) {
+        const double ratio = e + 1.0, adv = in.adv, w = in.w;
+        const double held = ratio < a.clip_lo ? a.clip_lo : ratio > a.clip_hi ? a.clip_hi : ratio;
+        const double one = ratio * adv, two = held * adv;
+        const bool pass = !(one > two);                     // a NaN passes
+        double loss = pass ? -one : -two, slope = pass ? -one : 0.0;
+        if (a.ref_logp) {
+            loss += a.kl * (e1 - d);
+            slope -= a.kl * e1;
+        }
+        if (keep && a.token_loss) a.token_loss[row] = (float)(w * loss);
+        if (keep && a.logp) a.logp[row] = (float)logp;
+        slope *= w * (double)in.scale * (double)a.inv_t;
+        o.base = (float)base;
+        o.slope = (float)slope;
+        o.p = -o.slope / r.sum;
     }
-    if (a.token_loss) a.token_loss[row] = (float)(w * loss);
-    if (a.logp) a.logp[row] = (float)logp;
-    slope *= w * (a.scale ? (double)*a.scale : 1.0) * (double)a.inv_t;
-    RowOut o;
-    o.base = (float)base;
-    o.p = (float)(-slope / (double)r.sum);
-    o.slope = (float)slope;
-    o.live = 1;
     return o;
 }
 
@@ -112,76 +141,78 @@ template <class T> __device__ __forceinline__ int head_of(const T* p, int64_t n)
     return h < n ? h : (int)n;
 }
 
-template <class T, int TEAM, bool ALIGN>
-__device__ __forceinline__ void policy_row(const Policy& a, int64_t row, int tid, Run* sh_run, RowOut* sh_out) {
+// KEEP: iterations of the block's threads over a row whose logits stay in shared memory, a thread's own.  A cluster's blocks share the
+// groups out; the first has what lies before and behind them.
+template <class T, int TEAM, bool ALIGN, int KEEP>
+__device__ __forceinline__ void policy_row(const Policy& a, int64_t row, int tid, int rank, int blocks, Run* sh_run, Run* sh_all, RowOut* sh_out, Raw8<T>* kept) {
     const T* z = (const T*)a.logits + row * a.in_stride;
     T* dz = a.dlogits ? (T*)a.dlogits + row * a.out_stride : nullptr;
     const int64_t t = a.wide_tokens ? ((const int64_t*)a.tokens)[row] : (int64_t)((const int*)a.tokens)[row];
     const int64_t n = a.vocab;
     const bool live = t >= 0 && t < n && !(a.weight && a.weight[row] == 0.f);
     const float k = a.k;
+    const int head = head_of(live ? z : dz, n);
+    const int all = (int)((n - head) / 8), per = (all + blocks - 1) / blocks;
+    const int g0 = per * rank < all ? per * rank : all, groups = (all - g0 < per ? all - g0 : per);      // this block's
+    const int64_t rest0 = head + (int64_t)all * 8;
+    // one value before or behind the groups, fewer than eight each
+    const int64_t edge = rank ? -1 : tid < head ? tid : tid >= 16 && tid < 32 && rest0 + tid - 16 < n ? rest0 + tid - 16 : -1;
     if (!live) {
-        if (tid == 0) {
+        if (tid == 0 && rank == 0) {
             if (a.token_loss) a.token_loss[row] = 0.f;
             if (a.logp) a.logp[row] = 0.f;
         }
-        if (!dz) return;
-        const int head = head_of(dz, n);
-        const int64_t groups = (n - head) / 8;
-        const float zero[8] = {};
-        if (tid < head) dz[tid] = rounded<T>(0.f);
-        for (int64_t g = tid; g < groups; g += TEAM) store8(dz + head + g * 8, zero);
-        for (int64_t i = head + groups * 8 + tid; i < n; i += TEAM) dz[i] = rounded<T>(0.f);
+        if (dz) {
+            const float zero[8] = {};
+            T* d = dz + head + (int64_t)g0 * 8;
+            for (int g = tid; g < groups; g += TEAM) store8(d + (int64_t)g * 8, zero);
+            if (edge >= 0) dz[edge] = rounded<T>(0.f);
+        }
         return;
     }
-    const int head = head_of(z, n);
-    const int64_t groups = (n - head) / 8;
-    const float zt = tid == 0 ? value_of(z[t]) : 0.f;
+    RowIn in{};
+    if (tid == 0) in = row_in(a, row, z, t);
     Run r{-INFINITY, 0.f};
-    {
-        const T* g0 = z + head;
-        for (int64_t g = tid; g < groups; g += kAhead * TEAM) {
-            Raw8<T> q[kAhead];
+    const T* zg = z + head + (int64_t)g0 * 8;
+    const int its = (groups - tid + TEAM - 1) / TEAM;       // groups of this thread: tid + it TEAM
+    for (int it = 0; it < its; it += kAhead) {
+        Raw8<T> q[kAhead];
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u)
-                if (g + u * TEAM < groups) q[u] = load8(g0 + (g + u * TEAM) * 8);
+        for (int u = 0; u < kAhead; ++u)
+            if (it + u < its) q[u] = load8(zg + (int64_t)(tid + (it + u) * TEAM) * 8);
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u)
-                if (g + u * TEAM < groups) {
-                    float v[8];
-                    unpack8(q[u], v);
-                    take(r, v, k);
-                }
-        }
-        if (tid < head) { const float v[1] = {value_of(z[tid])}; take(r, v, k); }
-        for (int64_t i = head + groups * 8 + tid; i < n; i += TEAM) { const float v[1] = {value_of(z[i])}; take(r, v, k); }
+        for (int u = 0; u < kAhead; ++u)
+            if (it + u < its) {
+                if (KEEP > 0 && it + u < KEEP) kept[(it + u) * TEAM + tid] = q[u];
+                float v[8];
+                unpack8(q[u], v);
+                take(r, v, k);
+            }
     }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        Run b;
-        b.top = __shfl_xor_sync(0xffffffffu, r.top, o);
-        b.sum = __shfl_xor_sync(0xffffffffu, r.sum, o);
-        r = merged(r, b, k);
-    }
+    if (edge >= 0) { const float v[1] = {value_of(z[edge])}; take(r, v, k); }
+    r = merged_warp(r);
     RowOut out;
     if (TEAM == 32) {
-        if (tid == 0) out = row_numbers(a, row, r, zt);
+        out = row_numbers(a, row, r, in, true);
         out.base = __shfl_sync(0xffffffffu, out.base, 0);
         out.p = __shfl_sync(0xffffffffu, out.p, 0);
         out.slope = __shfl_sync(0xffffffffu, out.slope, 0);
     } else {
         if ((tid & 31) == 0) sh_run[tid >> 5] = r;
         __syncthreads();
-        if (tid < 32) {
-            r = tid < TEAM / 32 ? sh_run[tid] : Run{-INFINITY, 0.f};
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) {
-                Run b;
-                b.top = __shfl_xor_sync(0xffffffffu, r.top, o);
-                b.sum = __shfl_xor_sync(0xffffffffu, r.sum, o);
-                r = merged(r, b, k);
+        if (tid < 32) r = merged_warp(tid < TEAM / 32 ? sh_run[tid] : Run{-INFINITY, 0.f});
+        if (blocks > 1) {                                   // every block sends its sum to all, and merges them in the same order
+            if (tid < blocks) {
+                const uint32_t at = tc::smem_of(&sh_all[rank], tid);
+                asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(at), "f"(r.c), "f"(r.sum) : "memory");
             }
-            if (tid == 0) *sh_out = row_numbers(a, row, r, zt);
+            __syncwarp();
+            tc::cluster_sync();
+            if (tid < 32) r = merged_warp(tid < blocks ? sh_all[tid] : Run{-INFINITY, 0.f});
+        }
+        if (tid < 32) {
+            const RowOut o = row_numbers(a, row, r, in, rank == 0);
+            if (tid == 0) *sh_out = o;
         }
         __syncthreads();
         out = *sh_out;
@@ -192,30 +223,37 @@ __device__ __forceinline__ void policy_row(const Policy& a, int64_t row, int tid
         return i == t ? out.slope + p : p;
     };
     if (ALIGN) {
-        const T* g0 = z + head;
-        T* d0 = dz + head;
-        for (int64_t g = tid; g < groups; g += kAhead * TEAM) {
+        T* dg = dz + head + (int64_t)g0 * 8;
+        // of the token, counted from this block's first group; beyond any where it is none of its
+        const int64_t from = t - head - (int64_t)g0 * 8;
+        const int token_at = from >= 0 && from < (int64_t)groups * 8 ? (int)from : INT_MAX;
+        const auto put = [&](int g, const Raw8<T>& q) {
+            float v[8];
+            unpack8(q, v);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = out.p * two_to(fmaf(v[j], k, -out.base));
+            const unsigned at = (unsigned)(token_at - g * 8);
+            if (at < 8) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] += at == j ? out.slope : 0.f;
+            }
+            store8(dg + (int64_t)g * 8, v);
+        };
+        for (int it = its - 1; it >= KEEP; it -= kAhead) {  // those from KEEP on are read again, the last first
             Raw8<T> q[kAhead];
 #pragma unroll
             for (int u = 0; u < kAhead; ++u)
-                if (g + u * TEAM < groups) q[u] = load8(g0 + (g + u * TEAM) * 8);
+                if (it - u >= KEEP) q[u] = load8(zg + (int64_t)(tid + (it - u) * TEAM) * 8);
 #pragma unroll
             for (int u = 0; u < kAhead; ++u)
-                if (g + u * TEAM < groups) {
-                    float v[8];
-                    unpack8(q[u], v);
-                    const int64_t i0 = head + (g + u * TEAM) * 8;
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) v[j] = out.p * two_to(fmaf(v[j], k, -out.base));
-                    if ((uint64_t)(t - i0) < 8) {
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) v[j] += i0 + j == t ? out.slope : 0.f;
-                    }
-                    store8(d0 + (g + u * TEAM) * 8, v);
-                }
+                if (it - u >= KEEP) put(tid + (it - u) * TEAM, q[u]);
         }
-        if (tid < head) dz[tid] = rounded<T>(slope_of(value_of(z[tid]), tid));
-        for (int64_t i = head + groups * 8 + tid; i < n; i += TEAM) dz[i] = rounded<T>(slope_of(value_of(z[i]), i));
+        if (KEEP > 0) {
+            const int last = its < KEEP ? its : KEEP;
+#pragma unroll 4
+            for (int it = 0; it < last; ++it) put(tid + it * TEAM, kept[it * TEAM + tid]);
+        }
+        if (edge >= 0) dz[edge] = rounded<T>(slope_of(value_of(z[edge]), edge));
     } else {
         for (int64_t i = tid; i < n; i += TEAM) dz[i] = rounded<T>(slope_of(value_of(z[i]), i));
     }
@@ -226,16 +264,23 @@ __global__ void __launch_bounds__(256)
 k_policy_warp(const __grid_constant__ Policy a) {
     let_follow();
     for (int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); row < a.rows; row += (int64_t)gridDim.x * 8)
-        policy_row<T, 32, ALIGN>(a, row, threadIdx.x & 31, nullptr, nullptr);
+        policy_row<T, 32, ALIGN, 0>(a, row, threadIdx.x & 31, 0, 1, nullptr, nullptr, nullptr, nullptr);
 }
 
-template <class T, bool ALIGN>
-__global__ void __launch_bounds__(kBlockTeam, 2)
+template <class T, int TEAM, bool ALIGN, int KEEP>
+__global__ void __launch_bounds__(TEAM, 1024 / TEAM)
 k_policy_block(const __grid_constant__ Policy a) {
-    __shared__ Run sh_run[kBlockTeam / 32];
+    extern __shared__ __align__(32) uint8_t kept[];
+    __shared__ Run sh_run[TEAM / 32], sh_all[8];
     __shared__ RowOut sh_out;
     let_follow();
-    policy_row<T, kBlockTeam, ALIGN>(a, blockIdx.x, threadIdx.x, sh_run, &sh_out);
+    uint32_t blocks = 1, rank = 0;
+    if (TEAM == kBlockTeam) {
+        asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(blocks));
+        rank = tc::cluster_rank();
+        if (blocks > 1) tc::cluster_sync();                 // all have begun: their shared memory is there
+    }
+    policy_row<T, TEAM, ALIGN, KEEP>(a, blockIdx.x / blocks, threadIdx.x, rank, blocks, sh_run, sh_all, &sh_out, (Raw8<T>*)kept);
 }
 
 // The sum of the tokens' losses, in 64 bits and a fixed order.
@@ -262,7 +307,30 @@ cudaError_t policy_launch(const Policy& a, cudaStream_t st) {
         const int64_t blocks = (a.rows + 7) / 8;
         return launch(k_policy_warp<T, ALIGN>, dim3((unsigned)(blocks < 0x7fffffff ? blocks : 0x7fffffff)), 256, 0, st, false, a);
     }
-    return launch(k_policy_block<T, ALIGN>, dim3((unsigned)a.rows), kBlockTeam, 0, st, false, a);
+    if (a.vocab <= kMidRow) return launch(k_policy_block<T, kMidTeam, ALIGN, 0>, dim3((unsigned)a.rows), kMidTeam, 0, st, false, a);
+    if constexpr (ALIGN) {
+        constexpr int kKeep = kKept / (kBlockTeam * 8 * (int)sizeof(T));
+        // few rows: blocks share one out while all fit the GPU at once and each has two iterations of its threads left
+        int c = 1;
+        while (c < 8 && a.rows * c * 2 <= kPlaces && a.vocab / (c * 2) >= 2 * kBlockTeam * 8) c *= 2;
+        const auto kernel = k_policy_block<T, kBlockTeam, true, kKeep>;
+        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kKept);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+        if (e != cudaSuccess) return e;
+        cudaLaunchConfig_t cfg{};
+        cfg.gridDim = dim3((unsigned)(a.rows * c));
+        cfg.blockDim = dim3(kBlockTeam);
+        cfg.dynamicSmemBytes = kKept;
+        cfg.stream = st;
+        cudaLaunchAttribute at{};
+        at.id = cudaLaunchAttributeClusterDimension;
+        at.val.clusterDim.x = c;
+        at.val.clusterDim.y = at.val.clusterDim.z = 1;
+        cfg.attrs = &at;
+        cfg.numAttrs = c > 1 ? 1 : 0;
+        return cudaLaunchKernelEx(&cfg, kernel, (const Policy)a);
+    }
+    return launch(k_policy_block<T, kBlockTeam, false, 0>, dim3((unsigned)a.rows), kBlockTeam, 0, st, false, a);
 }
 template <class T>
 cudaError_t policy_types(const Policy& a, bool align, cudaStream_t st) {
