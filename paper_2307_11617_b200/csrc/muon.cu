@@ -508,12 +508,10 @@ k_muon_product(const __grid_constant__ MuonGemm p) {
     if (CG == 2) tc::cluster_sync(); else __syncthreads();
     tc::fence_after();
     const uint32_t acc = tmem;
-    follow();
-    let_follow();
+    let_follow();                                           // each warp follows (waits) itself, once it knows its first tile
     const int first = blockIdx.x / CG, stride = gridDim.x / CG;
 
     if (warp == 0) {                                        // ---- loads
-        tc::fence_for_loads();
         const uint32_t bar0 = CG == 2 ? tc::smem_of(full, 0) : tc::smem(full), to0 = tc::smem(base);
         int s = 0;
         uint32_t turn = 1;                                  // of the ring: the first goes through without a wait
@@ -532,6 +530,10 @@ k_muon_product(const __grid_constant__ MuonGemm p) {
             const int in_a = x_first ? in_x : in_s, in_b = x_second ? in_x : in_s;
             const int limit_a = stored_up_to<S>(row0), limit_b = stored_up_to<S>(col0);
             const int start = first_box<S, OP, TERMS>(at, g.turned, blocks);
+            if (t == first) {
+                follow();
+                tc::fence_for_loads();
+            }
             for (int box = 0; box < blocks; ++box) {
                 if (!(ok = tc::bar_wait_warp(&empty[s], turn))) break;
                 const int k0 = (box + start < blocks ? box + start : box + start - blocks) * kBox;
@@ -653,6 +655,7 @@ k_muon_product(const __grid_constant__ MuonGemm p) {
                 return row0 < result_rows<OP>(g) && col0 < result_cols<OP>(g);
             };
             const MuonMat* const mat = OP == kUpdate ? p.mats + g.mat0 + at.mat : nullptr;
+            if (!kSegmented && t == first) follow();
             Ahead<OP, TERMS, T> ahead;
             const auto fetch = [&](int ch) {
                 if ((OP == kPoly || OP == kUpdate) && kept(ch)) ahead.load(p, g, at.mat, mat, row0, at.j * S::kTN + column(ch));
