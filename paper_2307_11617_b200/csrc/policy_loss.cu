@@ -2,12 +2,13 @@
 //
 // What bounds it is memory, where a logit has to come in once and its gradient to leave once.  The first pass over a row holds a running
 // maximum and sum of each thread's values, which are merged in a fixed order; one warp forms the row's numbers in 64 bits; the
-// second pass writes the gradient out of the logits again.  A warp does a row of up to 1024 logits, a block of 128 threads one of
-// up to 8192, a block of 512 longer ones, or, where rows are few, a cluster of up to eight blocks.  A thread of these keeps the first
-// logits that it reads in shared memory, 96 KB a block; the rest it reads again, the last first.  Without that the rows under way,
-// 296 of 256 KB, are too much for the L2 cache: 4096 x 128256 bf16 read 1.72 GB instead of 0.93, 445 us.  (Bringing rows through a ring
-// in shared memory by bulk copies, a cluster to a row and the next row's sum before this one's gradient, read every logit
-// once and took 510 us: with 20 instructions a logit in the place of 13 the issue slots were the bound.)
+// second pass writes the gradient out of the logits again.  A warp does a row of up to 1024 logits, a block of 128 threads one of up to
+// 40 KB (in the L2 cache between the passes), a block of 256 one of up to 128 KB, a block of 512 longer ones; a cluster of up to eight
+// blocks where rows are few.  A thread of the latter two keeps the first logits that it reads in shared memory, 48 or 96 KB a block; the rest
+// it reads again, the last first.  Without that the rows under way, 296 of 256 KB, are too much for the L2 cache: 4096 x 128256 bf16 read
+// 1.72 GB instead of 0.93, 445 us; with it 1.03 GB, 414 us, 4.7 TB/s and half of the issue slots and of the special function unit.
+// (Bringing rows through a ring in shared memory by bulk copies, a cluster to a row and the next row's sum before this one's
+// gradient, read every logit once and took 510 us: with 20 instructions a logit in the place of 13 the issue slots were the bound.)
 //
 // Powers are taken of two: exp((z - c) / T) = 2^(z k - c') with k = log2(e) / T in fp32 and c' the rounded z_max k.  k is the only
 // constant that both passes and the row's numbers share, so rounding it is a change of T by 2^-25 of itself and nothing else.
@@ -25,11 +26,13 @@ namespace rfast {
 
 namespace {
 
-constexpr int kBlockTeam = 512, kMidTeam = 128;
+constexpr int kBlockTeam = 512, kHalfTeam = 256, kMidTeam = 128;
 constexpr int kPlaces = 240;                 // blocks of 512 threads that run at once, less what clusters cannot use
 constexpr int kAhead = 4;                    // groups of eight logits that a thread has on their way (four more, fetched while it works: no gain)
-constexpr int64_t kShortRow = 1024, kMidRow = 8192;          // logits of a row up to which a warp, a small block does it
+constexpr int64_t kShortRow = 1024;          // logits of a row up to which a warp does it
 constexpr int kKept = 96 * 1024;             // bytes of a row that a long row's block keeps; two blocks share an SM
+constexpr int64_t kReadAgain = 56ll << 20;   // bytes (4096 x 128256 bf16 leave 47 MB: 414 us, 452 by pairs of blocks; 2000 x 100000 f32 90 MB: 362, 336 by pairs)
+constexpr int64_t kHalfRow = 128 * 1024, kQuarterRow = 40 * 1024;     // bytes of a row up to which it is a block of half, of a quarter of the threads
 
 struct Policy {
     const void* logits;
@@ -275,7 +278,7 @@ k_policy_block(const __grid_constant__ Policy a) {
     __shared__ RowOut sh_out;
     let_follow();
     uint32_t blocks = 1, rank = 0;
-    if (TEAM == kBlockTeam) {
+    if (KEEP > 0) {
         asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(blocks));
         rank = tc::cluster_rank();
         if (blocks > 1) tc::cluster_sync();                 // all have begun: their shared memory is there
@@ -301,35 +304,43 @@ k_policy_total(const float* __restrict__ token_loss, int64_t rows, float* __rest
     }
 }
 
+template <class T, int TEAM>
+cudaError_t keeping_launch(const Policy& a, cudaStream_t st) {
+    constexpr int kBytes = kKept / kBlockTeam * TEAM, kKeep = kBytes / (TEAM * 8 * (int)sizeof(T));
+    // few rows: blocks share one out while all fit the GPU at once and each has two iterations of its threads left
+    int c = 1;
+    while (c < 8 && a.rows * c * 2 <= kPlaces * (kBlockTeam / TEAM) && a.vocab / (c * 2) >= 2 * TEAM * 8) c *= 2;
+    // long rows: as many blocks to a row as leave what is read again of the rows under way to the L2 cache
+    const int64_t row = a.vocab * (int64_t)sizeof(T);
+    while (c < 8 && 296 / c * (kBlockTeam / TEAM) * (row - (int64_t)c * kBytes) > kReadAgain) c *= 2;
+    const auto kernel = k_policy_block<T, TEAM, true, kKeep>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(a.rows * c));
+    cfg.blockDim = dim3(TEAM);
+    cfg.dynamicSmemBytes = kBytes;
+    cfg.stream = st;
+    cudaLaunchAttribute at{};
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim.x = c;
+    at.val.clusterDim.y = at.val.clusterDim.z = 1;
+    cfg.attrs = &at;
+    cfg.numAttrs = c > 1 ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, kernel, (const Policy)a);
+}
 template <class T, bool ALIGN>
 cudaError_t policy_launch(const Policy& a, cudaStream_t st) {
     if (a.vocab <= kShortRow) {
         const int64_t blocks = (a.rows + 7) / 8;
         return launch(k_policy_warp<T, ALIGN>, dim3((unsigned)(blocks < 0x7fffffff ? blocks : 0x7fffffff)), 256, 0, st, false, a);
     }
-    if (a.vocab <= kMidRow) return launch(k_policy_block<T, kMidTeam, ALIGN, 0>, dim3((unsigned)a.rows), kMidTeam, 0, st, false, a);
     if constexpr (ALIGN) {
-        constexpr int kKeep = kKept / (kBlockTeam * 8 * (int)sizeof(T));
-        // few rows: blocks share one out while all fit the GPU at once and each has two iterations of its threads left
-        int c = 1;
-        while (c < 8 && a.rows * c * 2 <= kPlaces && a.vocab / (c * 2) >= 2 * kBlockTeam * 8) c *= 2;
-        const auto kernel = k_policy_block<T, kBlockTeam, true, kKeep>;
-        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kKept);
-        if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
-        if (e != cudaSuccess) return e;
-        cudaLaunchConfig_t cfg{};
-        cfg.gridDim = dim3((unsigned)(a.rows * c));
-        cfg.blockDim = dim3(kBlockTeam);
-        cfg.dynamicSmemBytes = kKept;
-        cfg.stream = st;
-        cudaLaunchAttribute at{};
-        at.id = cudaLaunchAttributeClusterDimension;
-        at.val.clusterDim.x = c;
-        at.val.clusterDim.y = at.val.clusterDim.z = 1;
-        cfg.attrs = &at;
-        cfg.numAttrs = c > 1 ? 1 : 0;
-        return cudaLaunchKernelEx(&cfg, kernel, (const Policy)a);
+        const int64_t row = a.vocab * (int64_t)sizeof(T);
+        if (row > kQuarterRow) return row <= kHalfRow ? keeping_launch<T, kHalfTeam>(a, st) : keeping_launch<T, kBlockTeam>(a, st);
     }
+    if (a.vocab * (int64_t)sizeof(T) <= kQuarterRow) return launch(k_policy_block<T, kMidTeam, ALIGN, 0>, dim3((unsigned)a.rows), kMidTeam, 0, st, false, a);
     return launch(k_policy_block<T, kBlockTeam, false, 0>, dim3((unsigned)a.rows), kBlockTeam, 0, st, false, a);
 }
 template <class T>
