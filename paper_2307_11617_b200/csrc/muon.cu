@@ -21,8 +21,6 @@
 
 #include <cmath>
 #include <cstdio>
-#include <new>
-#include <vector>
 
 #include "ops.h"
 #include "tensor_core.cuh"
@@ -947,6 +945,11 @@ extern "C" int rfast_muon_step(const rfast_muon* a, void* workspace, size_t work
             if (rc != RFAST_OK) return rc;
         }
     if (!encode_fn()) return op_fail(err, err_len, RFAST_ECUDA, "%s: the driver has no cuTensorMapEncodeTiled", me);
+    // a thread whose first call this is has no context yet, which the encoding of tensor maps wants
+    int dev = 0;
+    cudaError_t bound = cudaGetDevice(&dev);
+    if (bound == cudaSuccess) bound = cudaSetDevice(dev);
+    if (bound != cudaSuccess) return op_fail(err, err_len, RFAST_ECUDA, "%s: %s", me, cudaGetErrorString(bound));
     MuonRun r;
     bool first_run = true;
     for (int at = 0; at < a->n_tensors;) {

@@ -251,3 +251,38 @@ def test_gradient_against_differences():
     a, b = (dout.double() * out.double()).sum(), (grad.double() * e.double()).sum()
     size = (grad.double() * e.double()).abs().sum() + (dout.double() * out.double()).abs().sum()
     assert abs(a - b) <= 260 * U * size
+
+
+def test_offsets_beyond_32_bits():
+    """A table of 2.3e9 values: its last rows lie beyond 2^31 values and 2^32 bytes."""
+    import torch
+    import paper_2307_11617_b200 as pkg
+    vocab, width, n = 70_000, 32_768, 300
+    table = torch.zeros(vocab, width, dtype=torch.bfloat16, device="cuda")
+    t = torch.arange(vocab - n, vocab, device="cuda")[torch.randperm(n, device="cuda")]
+    t[::7] = torch.arange(0, (n + 6) // 7, device="cuda")
+    table[t] = torch.randn(n, width, device="cuda").bfloat16()
+    out = torch.empty(n, width, dtype=torch.bfloat16, device="cuda")
+    st = torch.cuda.current_stream().cuda_stream
+    pkg.rfast_embedding(t.data_ptr(), table.data_ptr(), out.data_ptr(), n, vocab, width, scale=0.5, table_type="bf16", out_type="bf16", cuda_stream=st)
+    assert torch.equal(out, table[t] * 0.5)
+    need = pkg.rfast_embedding_workspace(n, vocab, width)
+    work = torch.empty(need, dtype=torch.uint8, device="cuda")
+    grad = torch.full((vocab, width), 3.0, dtype=torch.bfloat16, device="cuda")
+    pkg.rfast_embedding_backward(t.data_ptr(), out.data_ptr(), grad.data_ptr(), n, vocab, width, scale=2.0, out_type="bf16", table_type="bf16", workspace=work.data_ptr(),
+                                 workspace_bytes=need, cuda_stream=st)
+    assert torch.equal(grad[t], table[t])                      # every token once: exact
+    assert int((grad != 0).any(1).sum()) == len(t.unique())
+
+
+def test_rows_read_over_one_another():
+    """A table whose rows overlap (a stride below its width), as sliding windows of one sequence."""
+    import torch
+    import paper_2307_11617_b200 as pkg
+    flat = torch.randn(4096, device="cuda")
+    for stride, width in ((8, 64), (3, 17), (0, 40)):
+        vocab, n = 200, 333
+        t = torch.randint(0, vocab, (n,), device="cuda")
+        out = torch.empty(n, width, device="cuda")
+        pkg.rfast_embedding(t.data_ptr(), flat.data_ptr(), out.data_ptr(), n, vocab, width, table_stride=stride, cuda_stream=torch.cuda.current_stream().cuda_stream)
+        assert torch.equal(out, flat.as_strided((vocab, width), (stride, 1))[t])

@@ -272,3 +272,46 @@ def test_update_is_nearly_orthogonal():
     d = -torch.diagonal(inner)[keep]
     assert bool(((d > 0.6) & (d < 1.3)).all())
     assert float((inner - torch.diag(torch.diagonal(inner))).abs().max()) < 1e-3
+
+
+@pytest.mark.parametrize("rows,cols", [(65536, 1), (3, 65536), (40_001, 70)])
+def test_the_longest_sides(rows, cols):
+    c = _step([(rows, cols)], sizes=[1.0], low=True, lr=0.5)
+    _check(c, [(rows, cols)], "f32", lr=0.5)
+
+
+def test_calls_from_several_threads():
+    """Two host threads, a stream, matrices and a workspace each."""
+    import threading
+    import torch
+    lists = [[(200, 300)] * 5, [(64, 500), (500, 64), (33, 7)]]
+    cs = [_step(s, sizes=[1.0] * len(s), seed=10 + k) for k, s in enumerate(lists)]
+    start = [{k: c[k].t.clone() for k in "pm"} for c in cs]
+    want = []
+    for c in cs:
+        for _ in range(5):
+            c["call"](torch.cuda.current_stream().cuda_stream)
+        torch.cuda.synchronize()
+        want.append(c["p"].t.clone())
+    for c, s in zip(cs, start):
+        for k in "pm":
+            c[k].t.copy_(s[k])
+    torch.cuda.synchronize()
+    streams, failed = [torch.cuda.Stream() for _ in cs], []
+
+    def work(c, s):
+        try:
+            for _ in range(5):
+                c["call"](s.cuda_stream)
+        except Exception as e:  # noqa: BLE001
+            failed.append(e)
+
+    threads = [threading.Thread(target=work, args=a) for a in zip(cs, streams)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not failed
+    for c, w in zip(cs, want):
+        assert torch.equal(c["p"].t, w)

@@ -270,3 +270,60 @@ def test_no_rows():
     loss = torch.full((1,), 4.0, device="cuda")
     pkg.rfast_policy_loss(0, 0, 0, 0, 0, 50, d_loss=loss.data_ptr(), d_token_loss=loss.data_ptr(), cuda_stream=torch.cuda.current_stream().cuda_stream)
     assert float(loss) == 0.0
+
+
+def test_offsets_beyond_32_bits():
+    """Logits of 2.3e9 values: the last rows lie beyond 2^31 values and 2^32 bytes."""
+    import torch
+    import paper_2307_11617_b200 as pkg
+    n, v, k = 18_000, 128_256, 4
+    z = torch.zeros(n, v, dtype=torch.bfloat16, device="cuda")
+    c = _case(k, v, "bf16", 1.0, 40)
+    z[-k:] = c["z"]
+    t = torch.full((n,), -1, dtype=torch.int64, device="cuda")
+    t[-k:] = c["t"]
+    dz = torch.full((n, v), 3.0, dtype=torch.bfloat16, device="cuda")
+    full = {}
+    for name in ("old", "ref", "adv", "w"):
+        full[name] = torch.full((n,), math.nan, device="cuda")
+        full[name][-k:] = c[name]
+    small = torch.empty(2 * n + 1, device="cuda")
+    pkg.rfast_policy_loss(z.data_ptr(), t.data_ptr(), full["old"].data_ptr(), full["adv"].data_ptr(), n, v, d_loss=small[2 * n:].data_ptr(), d_token_loss=small.data_ptr(),
+                          d_logp=small[n:].data_ptr(), d_dlogits=dz.data_ptr(), d_ref_logp=full["ref"].data_ptr(), d_weight=full["w"].data_ptr(), d_loss_scale=c["up"].data_ptr(),
+                          clip_low=LO, clip_high=HI, kl_coef=0.1, type="bf16", cuda_stream=torch.cuda.current_stream().cuda_stream)
+    _check(c, (small[2 * n], small[n - k:n], small[2 * n - k:2 * n], dz[-k:], None), 0.1)
+    assert bool((dz[:-k] == 0).all()) and bool((small[:n - k] == 0).all())
+
+
+@pytest.mark.parametrize("v", [300, 3001, 20_001, 90_000])
+def test_single_results(v):
+    """Each result alone is what it is among the others."""
+    import torch
+    import paper_2307_11617_b200 as pkg
+    c = _case(9, v, "f16", 1.0, v)
+    got = _run(c, 0.1)
+    for which in ("d_token_loss", "d_logp", "d_dlogits"):
+        out = torch.full_like(got[3], 7.0) if which == "d_dlogits" else torch.full((9,), 7.0, device="cuda")
+        pkg.rfast_policy_loss(c["z"].data_ptr(), c["t"].data_ptr(), c["old"].data_ptr(), c["adv"].data_ptr(), 9, v, d_ref_logp=c["ref"].data_ptr(), d_weight=c["w"].data_ptr(),
+                              d_loss_scale=c["up"].data_ptr(), clip_low=LO, clip_high=HI, kl_coef=0.1, type="f16", cuda_stream=torch.cuda.current_stream().cuda_stream,
+                              **{which: out.data_ptr()})
+        assert torch.equal(out, got[{"d_token_loss": 1, "d_logp": 2, "d_dlogits": 3}[which]]), which
+
+
+def test_logits_of_one_row_for_all():
+    """A stride of 0: many tokens scored by the same logits."""
+    import torch
+    for v in (700, 40_001):
+        c = _case(1, v, "f32", 1.0, 50)
+        n = 30
+        one = dict(c, n=n, stride=v, z=c["z"].expand(n, v), t=torch.arange(n, device="cuda"), adv=torch.ones(n, device="cuda"), w=torch.ones(n, device="cuda"))
+        logp = torch.log_softmax(c["z"].double(), 1)[0, :n]
+        one["old"], one["ref"] = (logp - 0.1).float(), (logp + 0.2).float()
+        import paper_2307_11617_b200 as pkg
+        small = torch.empty(2 * n + 1, device="cuda")
+        dz = torch.empty(n, v, device="cuda")
+        pkg.rfast_policy_loss(c["z"].data_ptr(), one["t"].data_ptr(), one["old"].data_ptr(), one["adv"].data_ptr(), n, v, d_loss=small[2 * n:].data_ptr(),
+                              d_token_loss=small.data_ptr(), d_logp=small[n:].data_ptr(), d_dlogits=dz.data_ptr(), d_ref_logp=one["ref"].data_ptr(), d_weight=one["w"].data_ptr(),
+                              d_loss_scale=c["up"].data_ptr(), clip_low=LO, clip_high=HI, kl_coef=0.1, logits_stride=0,
+                              cuda_stream=torch.cuda.current_stream().cuda_stream)
+        _check(one, (small[2 * n], small[:n], small[n:2 * n], dz, None), 0.1)
