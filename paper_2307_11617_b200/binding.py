@@ -629,7 +629,8 @@ def _sides(rows, cols):
 def rfast_muon_workspace(rows, cols, param_type: str = "f32", terms: int = 0) -> int:
     """Bytes of DEVICE workspace that a step over matrices of these rows and columns needs."""
     r, c = _sides(rows, cols)
-    need = lib().rfast_muon_workspace(len(r), _host(r), _host(c), terms or (2 if _type(param_type) == 0 else 1))
+    _type(param_type)
+    need = lib().rfast_muon_workspace(len(r), _host(r), _host(c), terms or (1 if param_type == "bf16" else 2))
     if need < 0:
         raise RFastError(int(need), "rfast_muon_workspace: rows, cols or terms are not valid")
     return int(need)
@@ -642,7 +643,7 @@ def rfast_muon_step(param, grad, momentum_buffer, rows, cols, lr: float = 0.02, 
     """One Muon step, in place, over many matrices: momentum, an update orthogonalised by `iterations` Newton-Schulz steps, decay.
     param, grad and momentum_buffer are the matrices' DEVICE addresses, rows and cols their sizes (sequences or integer arrays);
     momentum is fp32.  size_rule: "spectral" (sqrt(max(1, rows / cols))) or "rms" (0.2 sqrt(max(rows, cols))) times the update;
-    terms: fp16 numbers per factor of the products (0: 2 for fp32 parameters, else 1); d_grad_scale: DEVICE address of an fp32
+    terms: fp16 numbers per factor of the products (0: 1 for bf16 parameters, else 2); d_grad_scale: DEVICE address of an fp32
     factor on the gradients.  workspace: rfast_muon_workspace(...) bytes, aligned to 256, that no other running call uses.  Enqueued
     on cuda_stream."""
     r, c = _sides(rows, cols)

@@ -827,7 +827,7 @@ double iteration_time(const MuonGemm& p, int terms) {
     return product_time<CG, true>(p, terms, true) + product_time<CG, true>(p, terms, false) + product_time<CG, false>(p, terms, false);
 }
 
-int muon_terms(const rfast_muon* a) { return a->terms ? a->terms : a->param_type == RFAST_TYPE_F32 ? 2 : 1; }
+int muon_terms(const rfast_muon* a) { return a->terms ? a->terms : a->param_type == RFAST_TYPE_BF16 ? 1 : 2; }
 
 const char* muon_shape_fault(int n, const int32_t* rows, const int32_t* cols) {
     if (n < 0) return "n_tensors is negative";

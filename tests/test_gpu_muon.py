@@ -122,7 +122,7 @@ def _step(shapes, param="f32", grad="f32", terms=0, lead=0, low=False, seed=0, s
     torch.cuda.synchronize()
     assert int(c["work"][:4].view(torch.int32)) == 0
     assert bool((c["work"][need:] == 255).all())
-    c["terms"] = terms or (2 if param == "f32" else 1)
+    c["terms"] = terms or (1 if param == "bf16" else 2)
     return c
 
 
