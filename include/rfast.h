@@ -596,7 +596,7 @@ int rfast_group_norm_backward(const rfast_gn_shape* shape, const void* d_dy, con
  * are 32- or 64-bit integers.  The backward pass sorts tokens and positions (stably), so that each sum runs over
  * ascending positions in fp32, long ones over sums of up to 16 and of 256 sorted places; each value is rounded once to its type.
  * Without accumulate every row of dtable is written, zeros where a token does not occur; with it those rows are left alone.
- * A NaN or infinity of a row of dout reaches the row of its token and nothing else.
+ * A NaN or infinity of a row of dout reaches the row of its token and nothing else.  scale is finite.
  * Strides are those of a row in elements.  Read operands may overlap themselves (a stride of 0 repeats a row), written
  * ones may not; no other operands may overlap.  Addresses need to be aligned to their type only; where width is a multiple
  * of 8, strides are, and addresses are multiples of eight values' size, both operands are moved eight values at a time.  At most
@@ -625,7 +625,8 @@ int     rfast_embedding_backward(const rfast_emb_shape* shape, const void* d_tok
  * term; without weight it is 1; loss_scale (DEVICE) scales the gradient only, 1 without it.
  * A row whose weight is 0 or whose token is outside [0, vocab) does not count: its token_loss and logp are 0, its row of
  * dlogits is zero, and neither its logits nor its other numbers are read.  Logits may be -infinity (words that may not be used):
- * their gradient is 0.  A row of nothing but -infinity, a NaN or +infinity leave that row's results and `loss` NaN.
+ * their gradient is 0; a token whose own logit is -infinity has logp = -infinity and r = 0, and with a KL term a loss and a
+ * gradient of NaN.  A row of nothing but -infinity, a NaN or +infinity leave that row's results and `loss` NaN.
  * Running sums of a row are fp32, a row's own numbers (logp, r, both terms) and `loss` 64 bits; each result is rounded
  * once; exp((z - z_max) / T) below 2^-126 counts as 0.  |z| / T below 2^126.
  * Strides are those of a row in elements; logits may overlap themselves (a stride of 0 repeats a row), dlogits may not.

@@ -12,6 +12,7 @@
 // chunks between them, at most 15 + tokens / 256 + 15.
 #include <cuda_runtime.h>
 
+#include <cmath>
 #include <cstdio>
 
 #include "ops.h"
@@ -594,6 +595,7 @@ extern "C" int rfast_embedding(const rfast_emb_shape* shape, const void* d_token
     const char* const me = "rfast_embedding";
     const char* fault = emb_shape_fault(shape);
     if (fault) return op_fail(err, err_len, RFAST_EINVAL, "%s: %s", me, fault);
+    if (!std::isfinite(scale)) return op_fail(err, err_len, RFAST_EINVAL, "%s: scale must be finite", me);
     if (shape->tokens == 0) return RFAST_OK;
     if (!d_tokens || (uintptr_t)d_tokens % (shape->token_bits / 8)) return op_fail(err, err_len, RFAST_EINVAL, "%s: tokens are null or not aligned to their type", me);
     if ((fault = emb_rows_fault(d_table, shape->table_type, table_stride, shape->vocab, shape->width, false)))
@@ -622,6 +624,7 @@ extern "C" int rfast_embedding_backward(const rfast_emb_shape* shape, const void
     const char* const me = "rfast_embedding_backward";
     const char* fault = emb_shape_fault(shape);
     if (fault) return op_fail(err, err_len, RFAST_EINVAL, "%s: %s", me, fault);
+    if (!std::isfinite(scale)) return op_fail(err, err_len, RFAST_EINVAL, "%s: scale must be finite", me);
     const int64_t n = shape->tokens;
     if (n > 0 && (!d_tokens || (uintptr_t)d_tokens % (shape->token_bits / 8)))
         return op_fail(err, err_len, RFAST_EINVAL, "%s: tokens are null or not aligned to their type", me);

@@ -327,3 +327,20 @@ def test_logits_of_one_row_for_all():
                               d_loss_scale=c["up"].data_ptr(), clip_low=LO, clip_high=HI, kl_coef=0.1, logits_stride=0,
                               cuda_stream=torch.cuda.current_stream().cuda_stream)
         _check(one, (small[2 * n], small[:n], small[n:2 * n], dz, None), 0.1)
+
+
+@pytest.mark.parametrize("v", [64, 5000, 70_000])
+def test_a_token_that_may_not_be_used(v):
+    """Its own logit is -infinity: logp = -infinity, a ratio of 0, no gradient; NaN where a KL term asks for more."""
+    import torch
+    c = _case(6, v, "f32", 1.0, 61)
+    c["w"].fill_(1.0)
+    c["t"].copy_(torch.arange(6))
+    c["z"][2, 2] = -math.inf
+    c["old"].fill_(-4.0)
+    c["ref"].fill_(-4.0)
+    c["adv"].fill_(1.0)
+    total, loss, logp, dz, _ = _run(c, 0.0, use_ref=False)
+    assert float(logp[2]) == -math.inf and float(loss[2]) == 0.0 and bool((dz[2] == 0).all()) and bool(torch.isfinite(total))
+    total, loss, logp, dz, _ = _run(c, 0.1)
+    assert math.isnan(float(loss[2])) and bool(torch.isfinite(loss[[0, 1, 3, 4, 5]]).all()) and bool(torch.isfinite(dz[[0, 1, 3, 4, 5]]).all())

@@ -37,7 +37,7 @@ def test_embedding_refuses_shapes(rfast_lib, text, kw):
     ("tokens are null or not aligned", dict(d_tokens=A + 2, token_bits=32)), ("table is null", dict(d_table=0)), ("table is not aligned", dict(d_table=A + 2)),
     ("table has rows that overlap", dict(table_stride=-1)), ("table spans", dict(table_stride=1 << 55)), ("out is null", dict(d_out=0)),
     ("out is not aligned", dict(d_out=A + 1, out_type="bf16")), ("out has rows that overlap", dict(out_stride=7)), ("out has rows that overlap", dict(out_stride=0)),
-    ("out spans", dict(out_stride=1 << 55))])
+    ("out spans", dict(out_stride=1 << 55)), ("scale must be finite", dict(scale=NAN)), ("scale must be finite", dict(scale=INF))])
 def test_embedding_refuses_operands(rfast_lib, text, kw):
     import paper_2307_11617_b200 as pkg
     _refused(text, pkg.rfast_embedding, **{**dict(d_tokens=A, d_table=A, d_out=A), **SHAPE, **kw})
@@ -47,7 +47,7 @@ def test_embedding_refuses_operands(rfast_lib, text, kw):
     ("token_bits", dict(token_bits=8)), ("tokens are null", dict(d_tokens=0)), ("dout is null", dict(d_dout=0)), ("dout is not aligned", dict(d_dout=A + 2)),
     ("dout has rows that overlap", dict(dout_stride=-8)), ("dtable is null", dict(d_dtable=0)), ("dtable is not aligned", dict(d_dtable=A + 1, table_type="f16")),
     ("dtable has rows that overlap", dict(dtable_stride=7)), ("dtable spans", dict(dtable_stride=1 << 55)), ("workspace must be given", dict(workspace=0)),
-    ("workspace must be given", dict(workspace=A + 8)), ("workspace needs", dict(workspace_bytes=100))])
+    ("workspace must be given", dict(workspace=A + 8)), ("workspace needs", dict(workspace_bytes=100)), ("scale must be finite", dict(scale=-INF))])
 def test_embedding_backward_refuses(rfast_lib, text, kw):
     import paper_2307_11617_b200 as pkg
     _refused(text, pkg.rfast_embedding_backward, **{**dict(d_tokens=A, d_dout=A, d_dtable=A, workspace=A, workspace_bytes=1 << 30), **SHAPE, **kw})
