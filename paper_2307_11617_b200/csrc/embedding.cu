@@ -3,7 +3,7 @@
 // The gradient of a table row is the sum of the rows of dout that carry its token.  Tokens are sorted first (a stable radix
 // sort of token and position), so that every sum runs over neighbours in the sorted order, in the order of the positions,
 // without atomics: the same inputs give the same bits.  What bounds it is memory: dout is read once and the table's gradient
-// written once.
+// written once (65536 of 131072 x 2048 bf16: 169 us, sums and zeros at 5.2 and 5.4 TB/s behind 25 us of sorting).
 //
 // Text uses some tokens thousands of times and most of a table's never, so work is shared out by sorted places, not by rows:
 // a warp takes a chunk of 16 places and 256 columns, adds up in fp32 with eight rows on their way, and writes the rows whose
@@ -23,6 +23,8 @@ namespace rfast {
 namespace {
 
 constexpr int kCols = 256;                   // columns of a warp: eight per lane
+constexpr int kShort = 256;                  // columns up to which a look-up's rows are not a warp's each (90000 x 64 f32 to bf16: 31 -> 8 us); a
+                                             // quarter of it where values go one at a time
 constexpr int kSortThreads = 256, kSortWarps = 8, kSortItems = 4;
 constexpr int kSortTile = kSortThreads * kSortItems;
 constexpr int kDigitBits = 10, kDigits = 1 << kDigitBits;
@@ -76,6 +78,57 @@ k_embedding(const I* __restrict__ tokens, const TT* __restrict__ table, int64_t 
 #pragma unroll
             for (int k = 0; k < 8; ++k)
                 if (c0 + 32 * k < width) dst[c0 + 32 * k] = rounded<OT>(v[k]);
+        }
+    }
+}
+
+// Short rows: lanes go from one to the next, four values (WIDE: groups of eight) of a thread on their way.  L: 32 bits where all are counted
+// in them.
+template <class I, class TT, class OT, bool WIDE, class L>
+__global__ void __launch_bounds__(256)
+k_embedding_short(const I* __restrict__ tokens, const TT* __restrict__ table, int64_t table_stride, OT* __restrict__ out, int64_t out_stride, L all, int64_t vocab,
+                  unsigned per, float scale) {
+    constexpr int kOf = WIDE ? 8 : 1;
+    const L step = (L)gridDim.x * 256;
+    for (L at = (L)blockIdx.x * 1024 + threadIdx.x; at < all; at += step * 4) {
+        const TT* src[4];
+        OT* dst[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const L v = at + (L)u * 256;
+            src[u] = nullptr;
+            dst[u] = nullptr;
+            if (v < all) {
+                const L row = v / per;
+                const int c = (int)(v - row * per) * kOf;
+                const int64_t t = (int64_t)tokens[row];
+                if (t >= 0 && t < vocab) src[u] = table + t * table_stride + c;
+                dst[u] = out + (int64_t)row * out_stride + c;
+            }
+        }
+        if constexpr (WIDE) {
+            Raw8<TT> r[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (src[u]) r[u] = load8(src[u]);
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (dst[u]) {
+                    float v[8] = {};
+                    if (src[u]) {
+                        unpack8(r[u], v);
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) v[k] *= scale;
+                    }
+                    store8(dst[u], v);
+                }
+        } else {
+            float v[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) v[u] = src[u] ? value_of(*src[u]) * scale : 0.f;
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (dst[u]) *dst[u] = rounded<OT>(v[u]);
         }
     }
 }
@@ -317,6 +370,8 @@ struct Flight<DT, false> {
         for (int q = 0; q < 8; ++q) acc[q] += value_of(r[k][q]);
     }
 };
+// Few registers: they would be taken from the warps that write zeros (four or eight sums fetched together: 65536 of 131072 x 2048 bf16 169 ->
+// 262 us).
 template <bool WIDE>
 __device__ __forceinline__ void add_sums(const EmbSums& a, const float* __restrict__ from, int64_t i, int64_t j, int c0, float (&acc)[8]) {
 #pragma unroll 4
@@ -545,6 +600,17 @@ struct EmbCall {
 
 template <class I, class TT, class OT, bool WIDE>
 cudaError_t look_up(const EmbCall& c) {
+    if (c.s->width <= (WIDE ? kShort : kShort / 4)) {
+        const int of = WIDE ? 8 : 1;
+        const unsigned in_row = (unsigned)(c.s->width / of);
+        const int64_t all = c.s->tokens * in_row, blocks = (all + 1023) / 1024;
+        const dim3 grid((unsigned)(blocks < 0x7fffffff ? blocks : 0x7fffffff));
+        if (all < (int64_t)1 << 31)
+            return launch(k_embedding_short<I, TT, OT, WIDE, uint32_t>, grid, 256, 0, c.st, false, (const I*)c.tokens, (const TT*)c.in, c.in_stride, (OT*)c.out, c.out_stride,
+                          (uint32_t)all, c.s->vocab, in_row, c.scale);
+        return launch(k_embedding_short<I, TT, OT, WIDE, uint64_t>, grid, 256, 0, c.st, false, (const I*)c.tokens, (const TT*)c.in, c.in_stride, (OT*)c.out, c.out_stride,
+                      (uint64_t)all, c.s->vocab, in_row, c.scale);
+    }
     const int per = WIDE ? 1024 : kCols;
     const int parts = (c.s->width + per - 1) / per;
     const int64_t blocks = (c.s->tokens * parts + 7) / 8;

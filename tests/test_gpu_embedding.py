@@ -286,3 +286,36 @@ def test_rows_read_over_one_another():
         out = torch.empty(n, width, device="cuda")
         pkg.rfast_embedding(t.data_ptr(), flat.data_ptr(), out.data_ptr(), n, vocab, width, table_stride=stride, cuda_stream=torch.cuda.current_stream().cuda_stream)
         assert torch.equal(out, flat.as_strided((vocab, width), (stride, 1))[t])
+
+
+@pytest.mark.parametrize("width", [1, 2, 8, 16, 63, 64, 65, 128, 248, 256, 264])
+@pytest.mark.parametrize("lead,pad", [(0, 0), (8, 8), (1, 2)])
+def test_short_rows(width, lead, pad):
+    """Rows of fewer columns than a warp takes, many of them."""
+    import torch
+    import paper_2307_11617_b200 as pkg
+    n, vocab = 5003, 700
+    rng = np.random.default_rng(width)
+    t = torch.as_tensor(_tokens(n, vocab, "even", rng)).cuda()
+    ft, tab = _strided(vocab, width, width + pad, "bf16", lead)
+    tab.copy_(torch.as_tensor(rng.standard_normal((vocab, width)).astype(np.float32)))
+    fo, got = _strided(n, width, width + 2 * pad, "f32", lead)
+    pkg.rfast_embedding(t.data_ptr(), tab.data_ptr(), got.data_ptr(), n, vocab, width, scale=1.5, table_type="bf16", out_type="f32", table_stride=width + pad,
+                        out_stride=width + 2 * pad, cuda_stream=torch.cuda.current_stream().cuda_stream)
+    some = (t >= 0) & (t < vocab)
+    want = torch.where(some[:, None], tab[t.clamp(0, vocab - 1)].float() * 1.5, torch.zeros((), device="cuda"))
+    assert torch.equal(got, want)
+    assert _marks_stand(fo, got, lead, n, width, width + 2 * pad)
+
+
+def test_more_short_rows_than_32_bits_count():
+    import torch
+    import paper_2307_11617_b200 as pkg
+    n, vocab, width = 65_100_000, 10, 33                       # 2.15e9 values
+    t = torch.randint(0, vocab, (n,), dtype=torch.int32, device="cuda")
+    table = torch.randn(vocab, width, device="cuda").bfloat16()
+    out = torch.empty(n, width, dtype=torch.bfloat16, device="cuda")
+    pkg.rfast_embedding(t.data_ptr(), table.data_ptr(), out.data_ptr(), n, vocab, width, token_bits=32, table_type="bf16", out_type="bf16",
+                        cuda_stream=torch.cuda.current_stream().cuda_stream)
+    for part in (slice(0, 1000), slice(n // 2, n // 2 + 1000), slice(n - 2_000_000, n)):
+        assert torch.equal(out[part], table[t[part].long()])
