@@ -628,7 +628,7 @@ int     rfast_embedding_backward(const rfast_emb_shape* shape, const void* d_tok
  * their gradient is 0; a token whose own logit is -infinity has logp = -infinity and r = 0, and with a KL term a loss and a
  * gradient of NaN.  A row of nothing but -infinity, a NaN or +infinity leave that row's results and `loss` NaN.
  * Running sums of a row are fp32, a row's own numbers (logp, r, both terms) and `loss` 64 bits; each result is rounded
- * once; exp((z - z_max) / T) below 2^-126 counts as 0.  |z| / T below 2^126.
+ * once; exp((z - z_max) / T) below 2^-126 may count as 0.  |z| / T below 2^126.
  * Strides are those of a row in elements; logits may overlap themselves (a stride of 0 repeats a row), dlogits may not.
  * dlogits may be the logits, with their stride; no other operands may overlap.  Addresses need to be aligned to their type
  * only.  The fast case is a gradient whose rows begin at the same place within eight values as the logits' do (both contiguous,

@@ -36,7 +36,6 @@ __device__ __forceinline__ void bar_init_fence() { asm volatile("fence.mbarrier_
 __device__ __forceinline__ void bar_expect(uint64_t* bar, uint32_t bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem(bar)), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ void bar_arrive(uint64_t* bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem(bar)) : "memory"); }
 // An arrival at a barrier of this or of another thread block of the cluster.
 __device__ __forceinline__ void bar_arrive_cluster(uint32_t addr) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
@@ -61,24 +60,6 @@ __device__ __forceinline__ bool bar_wait(uint64_t* bar, uint32_t parity) {
 
 // For a whole warp, which decides as one.
 __device__ __forceinline__ bool bar_wait_warp(uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, bar_wait(bar, parity)); }
-// The same for arrivals of other blocks of the cluster: what they wrote before is seen.
-__device__ __forceinline__ bool bar_wait_cluster(uint64_t* bar, uint32_t parity) {
-    const uint32_t addr = smem(bar);
-    int64_t t0 = 0;
-    for (uint32_t it = 0;; ++it) {
-        uint32_t ok;
-        asm volatile(
-            "{\n.reg .pred p;\n"
-            "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n"
-            "selp.u32 %0, 1, 0, p;\n}\n"
-            : "=r"(ok) : "r"(addr), "r"(parity), "r"(kSleepNs) : "memory");
-        if (ok) return true;
-        const int64_t now = clock64();
-        if (it == 0) t0 = now;
-        else if (now - t0 > kWaitClocks) return false;
-    }
-}
-
 // One thread of a converged warp.  The warp runs its loop as a whole and this picks who issues, so that what the instructions take stays in
 // uniform registers; a loop that only lane 0 runs pays 300 clocks more for four matrix instructions and as many loads.
 __device__ __forceinline__ bool elect() {
