@@ -370,23 +370,44 @@ struct Flight<DT, false> {
         for (int q = 0; q < 8; ++q) acc[q] += value_of(r[k][q]);
     }
 };
-// Few registers: they would be taken from the warps that write zeros (four or eight sums fetched together: 65536 of 131072 x 2048 bf16 169 ->
-// 262 us).
-template <bool WIDE>
+// Sums [i, j) of a list of them, one after the other.  MANY: eight are fetched at once, for long runs (90000 tokens of 3, 64 columns: the
+// gradient in 28 us, not 39).  Elsewhere the registers would be missed by the warps that write zeros (65536 of 131072 x 2048 bf16: 262 us, not 169).
+template <bool WIDE, bool MANY>
 __device__ __forceinline__ void add_sums(const EmbSums& a, const float* __restrict__ from, int64_t i, int64_t j, int c0, float (&acc)[8]) {
-#pragma unroll 4
-    for (; i < j; ++i) {
-        const float* p = from + i * a.pitch;
-        if (WIDE) {
-            if (c0 < a.width) {
-                float v[8];
-                unpack8(load8(p + c0), v);
+    if constexpr (MANY) {
+        for (; i < j; i += 8) {
+            float r[8][8];
 #pragma unroll
-                for (int q = 0; q < 8; ++q) acc[q] += v[q];
+            for (int u = 0; u < 8; ++u) {
+                const float* p = from + (i + u) * a.pitch;
+                if (WIDE) {
+                    if (i + u < j && c0 < a.width) unpack8(load8(p + c0), r[u]);
+                } else {
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) r[u][q] = i + u < j && c0 + 32 * q < a.width ? p[c0 + 32 * q] : 0.f;
+                }
             }
-        } else {
 #pragma unroll
-            for (int q = 0; q < 8; ++q) acc[q] += c0 + 32 * q < a.width ? p[c0 + 32 * q] : 0.f;
+            for (int u = 0; u < 8; ++u)
+                if (i + u < j && c0 < a.width)
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) acc[q] += r[u][q];
+        }
+    } else {
+#pragma unroll 4
+        for (; i < j; ++i) {
+            const float* p = from + i * a.pitch;
+            if (WIDE) {
+                if (c0 < a.width) {
+                    float v[8];
+                    unpack8(load8(p + c0), v);
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) acc[q] += v[q];
+                }
+            } else {
+#pragma unroll
+                for (int q = 0; q < 8; ++q) acc[q] += c0 + 32 * q < a.width ? p[c0 + 32 * q] : 0.f;
+            }
         }
     }
 }
@@ -503,7 +524,7 @@ k_emb_chunks(EmbSums a, const DT* __restrict__ dout, TT* __restrict__ dtable) {
 }
 
 // Zeros for tokens that do not occur, sums of the pieces of runs that cross a chunk's border.
-template <class TT, bool WIDE>
+template <class TT, bool WIDE, bool MANY>
 __global__ void __launch_bounds__(256)
 k_emb_rows(EmbSums a, TT* __restrict__ dtable) {
     follow();
@@ -528,16 +549,16 @@ k_emb_rows(EmbSums a, TT* __restrict__ dtable) {
         const int begin = __shfl_sync(0xffffffffu, mine.x, r), end = __shfl_sync(0xffffffffu, mine.y, r);
         float acc[8] = {};
         int64_t c = begin / kChunk;
-        if (begin % kChunk) { add_sums<WIDE>(a, a.tail, c, c + 1, c0, acc); ++c; }
+        if (begin % kChunk) { add_sums<WIDE, MANY>(a, a.tail, c, c + 1, c0, acc); ++c; }
         const int64_t whole = end / kChunk, all = (end + kChunk - 1) / kChunk;           // chunks that the run fills end before `whole`
         const int64_t s = (c + kChunksPerSum - 1) / kChunksPerSum;
         const int64_t s1 = whole / kChunksPerSum;
         if (s < s1) {
-            add_sums<WIDE>(a, a.chunk, c, s * kChunksPerSum, c0, acc);
-            add_sums<WIDE>(a, a.span, s, s1, c0, acc);
+            add_sums<WIDE, MANY>(a, a.chunk, c, s * kChunksPerSum, c0, acc);
+            add_sums<WIDE, MANY>(a, a.span, s, s1, c0, acc);
             c = s1 * kChunksPerSum;
         }
-        add_sums<WIDE>(a, a.chunk, c, all, c0, acc);
+        add_sums<WIDE, MANY>(a, a.chunk, c, all, c0, acc);
         put_row<TT, WIDE>(a, dtable + (v0 + r) * a.table_stride, c0, acc);
     }
 }
@@ -631,7 +652,10 @@ cudaError_t sums(const EmbSums& a, const void* dout, void* dtable, cudaStream_t 
         if (e != cudaSuccess) return e;
     }
     const int64_t groups = (a.vocab + a.rows_per_warp - 1) / a.rows_per_warp;
-    return launch(k_emb_rows<TT, WIDE>, dim3((unsigned)((groups * a.col_tiles + 7) / 8)), 256, 0, st, true, a, (TT*)dtable);
+    const dim3 grid((unsigned)((groups * a.col_tiles + 7) / 8));
+    // a token has eight places on average: long runs and few zeros
+    if (a.n >= 8 * a.vocab) return launch(k_emb_rows<TT, WIDE, true>, grid, 256, 0, st, true, a, (TT*)dtable);
+    return launch(k_emb_rows<TT, WIDE, false>, grid, 256, 0, st, true, a, (TT*)dtable);
 }
 template <class DT, class TT>
 cudaError_t sums_types(const EmbSums& a, const void* dout, void* dtable, bool wide, cudaStream_t st) {
