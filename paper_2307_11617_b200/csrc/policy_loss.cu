@@ -312,7 +312,8 @@ cudaError_t keeping_launch(const Policy& a, cudaStream_t st) {
     while (c < 8 && a.rows * c * 2 <= kPlaces * (kBlockTeam / TEAM) && a.vocab / (c * 2) >= 2 * TEAM * 8) c *= 2;
     // long rows: as many blocks to a row as leave what is read again of the rows under way to the L2 cache
     const int64_t row = a.vocab * (int64_t)sizeof(T);
-    while (c < 8 && 296 / c * (kBlockTeam / TEAM) * (row - (int64_t)c * kBytes) > kReadAgain) c *= 2;
+    // (and a grid holds: repeated rows, their stride 0, can be 2^31 - 1)
+    while (c < 8 && a.rows * c * 2 <= INT_MAX && 296 / c * (kBlockTeam / TEAM) * (row - (int64_t)c * kBytes) > kReadAgain) c *= 2;
     const auto kernel = k_policy_block<T, TEAM, true, kKeep>;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);

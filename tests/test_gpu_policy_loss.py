@@ -329,6 +329,27 @@ def test_logits_of_one_row_for_all():
         _check(one, (small[2 * n], small[:n], small[n:2 * n], dz, None), 0.1)
 
 
+def test_more_rows_than_a_grid_has_groups_of_blocks():
+    """2^29 + 1 rows of one long row of zeros: eight blocks to a row would be more than a launch takes.  Three rows count."""
+    import torch
+    import paper_2307_11617_b200 as pkg
+    n, v = (1 << 29) + 1, 600_000
+    z = torch.zeros(v, device="cuda")
+    t = torch.full((n,), -1, dtype=torch.int32, device="cuda")
+    old, adv = torch.full((n,), -math.log(v), device="cuda"), torch.ones(n, device="cuda")
+    loss = torch.full((n,), 3.0, device="cuda")
+    rows = [0, n // 2, n - 1]
+    for k in rows:
+        t[k] = k % v
+    pkg.rfast_policy_loss(z.data_ptr(), t.data_ptr(), old.data_ptr(), adv.data_ptr(), n, v, d_token_loss=loss.data_ptr(), logits_stride=0, token_bits=32,
+                          cuda_stream=torch.cuda.current_stream().cuda_stream)
+    # the sum of v powers of zero is exact; old_logp, 13.3, is rounded by at most 2^-21, the ratio next to 1 moves by as much; then the result's 2^-24
+    for k in rows:
+        assert abs(float(loss[k]) + 1.0) < 2.0 ** -21 + 2.0 ** -23, k
+        loss[k] = 0.0
+    assert not bool(loss.any())
+
+
 @pytest.mark.parametrize("v", [64, 5000, 70_000])
 def test_a_token_that_may_not_be_used(v):
     """Its own logit is -infinity: logp = -infinity, a ratio of 0, no gradient; NaN where a KL term asks for more."""
