@@ -666,10 +666,12 @@ int rfast_policy_loss(const rfast_policy* p, void* cuda_stream, char* err, size_
  * Five iterations bring the singular values of U that are not tiny next to the largest to between 0.7 and 1.2, whatever
  * they were; those of 1e-3 of the norm and less grow 485-fold, and rounding errors in their directions with them.
  * The momentum M is fp32, the norm 64 bits; products have fp32 sums and factors of `terms` fp16 numbers:
- *   terms = 2: a factor is the sum of two, 22 bits; X is then within 1e-5 (relative, Frobenius) of exact for sides of up to 300,
- *              3e-5 up to 4096, for gradients with a few large directions over noise
- *   terms = 1: a factor is one, 11 bits: within 2e-3 for noise, 2e-2 with a few large directions
- *   terms = 0: 2 for fp32 and fp16 parameters, whose digits show it, 1 for bf16 ones
+ *   terms = 2: a factor is the sum of two, 22 bits, the product of the two low halves left out; X is then within 1e-5 (relative,
+ *              Frobenius) of exact for sides of up to 300, 3e-5 up to 4096, for noise, or a few large directions over noise of a seventh of
+ *              their values (standard deviations); within 3e-5 and 3e-4 over noise of a seventieth
+ *   terms = 1: a factor is one, 11 bits: within 2e-3 for noise, 2e-2 with a few large directions, over noise of a seventieth at least
+ *   terms = 0: 2 for fp32 and fp16 parameters; 1 for bf16 ones, whose own rounding is larger (6 of 4096 x 1024, weights of 0.04, steps of
+ *              0.02 X: 1.658e-3 off the exact result with one term as with two; with one a value in 80 falls to the next number)
  * p is rounded once to its type.  A NaN, or an infinity, in g or M leaves its whole matrix NaN, and no other.
  * Matrices without rows or columns are passed over.  Tensors may not overlap one another.  Addresses need to be aligned
  * to their type only.  workspace: rfast_muon_workspace(n_tensors, rows, cols, terms) bytes of DEVICE memory (terms 1 or 2), aligned
