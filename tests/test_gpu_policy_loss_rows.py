@@ -1,0 +1,76 @@
+"""Policy loss: rows at the borders between the ways that rows are done.
+
+What the sums of a row are off by, u = 2^-24, R = log2(e) / T times the spread of the row's logits:
+  * a power of two is off by 2^-22 of itself (what the instruction promises), its exponent, of at most R + 40 either way (the reference may lie
+    2^40 below the maximum), by u of that, which is ln 2 u (R + 40) of the power;
+  * a sum is taken to another reference at most R / 40 + 1 times while a thread reads and once at each of three merges (2^-22 for the factor, u for
+    the product);
+  * a thread adds up its logits one after the other, and at most 15 additions merge the threads' sums (a warp's, a block's, a cluster's): u each.
+    A row of up to 1024 logits is a warp's, one of up to 40 KB 128 threads', one of up to 128 KB 256 threads' where its gradient lies as it does,
+    512 threads' elsewhere; a thread takes groups of eight and one value beside them.
+    E = 2^-22 (5 + R / 40) + u (ln 2 (R + 40) + chain + 15 + 4 + R / 40)
+is the relative error of a sum and the absolute one of logp.  log2(e) / T is rounded to fp32, a change of T by u of itself at most, which moves logp
+by u ln 2 R more.  The results' tolerances follow:
+  logp        L = E + u ln 2 R, and u |logp| for its rounding
+  token_loss  w (|A| r + kl (e^d + 1)) L (1 + L) and 2 u of itself
+  dlogits     s = scale dl/dlogp / T, p = softmax:  scale w (|A| r + kl (e^d + 1)) L / T (1[t] + p) + |s| p (2 E + 2^-22 + u ln 2 (R + 40) + 2 u) + 3 u |s| 1[t],
+              2^-126 |s| (a power below counts as 0), half a step of the type."""
+
+from __future__ import annotations
+
+import math
+
+import pytest
+
+from test_gpu_policy_loss import HALF, HI, LO, TINY, U, _case, _formula, _run
+
+pytestmark = pytest.mark.gpu
+
+LN2 = math.log(2.0)
+BYTES = {"f32": 4, "bf16": 2, "f16": 2}
+
+
+def _chain(v, kind, align):
+    size = v * BYTES[kind]
+    team = 32 if v <= 1024 else 128 if size <= 40 * 1024 else 256 if align and size <= 128 * 1024 else 512
+    return 8 * -(-(v // 8) // team) + 1
+
+
+def _sums(c, align):
+    """Of every row: R, E, the bound of logp before its rounding, and the exact logp."""
+    import torch
+    z = c["z"].double() / c["warm"]
+    t = c["t"].long().clamp(0, c["v"] - 1)[:, None]
+    R = (z.amax(1) - z.amin(1)) / LN2
+    E = 2.0 ** -22 * (5 + R / 40) + U * (LN2 * (R + 40) + _chain(c["v"], c["kind"], align) + 19 + R / 40)
+    return R, E, E + U * LN2 * R, z.gather(1, t)[:, 0] - torch.logsumexp(z, 1)
+
+
+def _within(c, got, kl, align=True):
+    import torch
+    live, (loss0, logp0, dz0), _ = _formula(c, kl)
+    _, loss, logp, dz, _ = got
+    R, E, L, lp = _sums(c, align)
+    size = c["w"].double() * (c["adv"].double().abs() * torch.exp(lp - c["old"].double()) + kl * (torch.exp(c["ref"].double() - lp) + 1))
+    p = torch.softmax(c["z"].double() / c["warm"], 1)
+    hot = torch.zeros_like(p).scatter_(1, c["t"].long().clamp(0, c["v"] - 1)[:, None], 1.0)
+    # |s|, out of the formula's gradient: dz = s (1[t] - p)
+    s = dz0.abs().sum(1) / (hot - p).abs().sum(1).clamp_min(1e-300)
+    tol = (float(c["up"]) * size * L / c["warm"])[:, None] * (hot + p) + s[:, None] * (p * (2 * E + 2.0 ** -22 + U * (LN2 * (R + 40) + 2))[:, None] + 3 * U * hot + 2.0 ** -126)
+    tol = tol + HALF[c["kind"]] * (dz0.abs() + tol) + TINY[c["kind"]]
+    for name, g, x, e in (("logp", logp, logp0, L + U * logp0.abs()), ("loss", loss, loss0, size * L * (1 + L) + 2 * U * loss0.abs()), ("dz", dz, dz0, tol)):
+        off = (g.double() - x).abs()[live] / e[live]
+        assert bool((off <= 1).all()), (name, int((off > 1).sum()), float(off.max()))
+        assert not bool(g[~live].any()), name
+
+
+BORDERS = [("f32", v) for v in (1023, 1024, 1025, 10_240, 10_241, 32_768, 32_769)] + [(k, v) for k in ("bf16", "f16") for v in (1024, 1025, 20_480, 20_481, 65_536, 65_537)]
+
+
+@pytest.mark.parametrize("kind,v", BORDERS)
+@pytest.mark.parametrize("n", [5, 400])
+def test_rows_at_the_borders_of_their_teams(kind, v, n):
+    """Few rows (shared out over clusters where they are long) and many, gradients that lie as the logits do and otherwise."""
+    c = _case(n, v, kind, 0.8, v + n)
+    _within(c, _run(c, 0.1), 0.1)
+    _within(c, _run(c, 0.1, out_stride=v + 3, out_lead=1), 0.1, align=False)
