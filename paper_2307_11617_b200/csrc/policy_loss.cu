@@ -411,10 +411,10 @@ extern "C" int rfast_policy_loss(const rfast_policy* p, void* cuda_stream, char*
     cudaStream_t st = (cudaStream_t)cuda_stream;
     cudaError_t e = cudaSuccess;
     if (p->tokens > 0) {
-        // the offset within eight values is the same in every row of both
+        // the offset within eight values is the same in every row of both (one row has no stride)
         const int64_t b = (int64_t)bytes_of(p->type);
         const bool align = !p->d_dlogits || (((uintptr_t)p->d_logits ^ (uintptr_t)p->d_dlogits) % (8 * b) == 0 &&
-                                             (p->logits_stride - p->dlogits_stride) % 8 == 0);
+                                             (p->tokens == 1 || (p->logits_stride - p->dlogits_stride) % 8 == 0));
         switch (p->type) {
             case RFAST_TYPE_F32: e = policy_types<float>(a, align, st); break;
             case RFAST_TYPE_BF16: e = policy_types<__nv_bfloat16>(a, align, st); break;

@@ -1,4 +1,4 @@
-"""Policy loss: rows at the borders between the ways that rows are done.
+"""Policy loss: rows at the borders between the ways that rows are done, single rows.
 
 What the sums of a row are off by, u = 2^-24, R = log2(e) / T times the spread of the row's logits:
   * a power of two is off by 2^-22 of itself (what the instruction promises), its exponent, of at most R + 40 either way (the reference may lie
@@ -74,3 +74,18 @@ def test_rows_at_the_borders_of_their_teams(kind, v, n):
     c = _case(n, v, kind, 0.8, v + n)
     _within(c, _run(c, 0.1), 0.1)
     _within(c, _run(c, 0.1, out_stride=v + 3, out_lead=1), 0.1, align=False)
+
+
+@pytest.mark.parametrize("kind,v,stride", [("f32", 10_300, 10_301), ("f32", 50_257, 50_304), ("bf16", 50_257, 50_304), ("bf16", 128_256, 128_259), ("f16", 30_001, 30_007), ("f32", 700, 701)])
+def test_one_row_has_no_stride(kind, v, stride):
+    """What a row would be away from the next one does not matter where there is one: the same results, bit for bit, whatever the strides say."""
+    import torch
+    c = _case(1, v, kind, 1.0, v, stride=stride)
+    c["w"].fill_(0.7)
+    c["t"].fill_(v // 3)
+    want = _run(c, 0.1, out_stride=stride)
+    for out_stride in (v, v + 5, 0):
+        got = _run(c, 0.1, out_stride=max(out_stride, v)) if out_stride else _run(dict(c, stride=0), 0.1, out_stride=v)
+        for a, b in zip(got[:4], want[:4]):
+            assert torch.equal(a.reshape(-1), b.reshape(-1)), out_stride
+    _within(c, want, 0.1)
