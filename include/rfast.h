@@ -623,6 +623,7 @@ int     rfast_embedding_backward(const rfast_emb_shape* shape, const void* d_tok
  *     dlogits_v = loss_scale d token_loss / d logp (1[v = token] - exp(z_v / T) / sum) / T
  * (the derivative is r A's where r A <= clamp(r) A, and 0 of that term elsewhere).  Without ref_logp there is no KL
  * term; without weight it is 1; loss_scale (DEVICE) scales the gradient only, 1 without it.
+ * Where d_logp alone is wanted (log probabilities, of which old_logp and ref_logp are made), old_logp and advantage may be NULL.
  * A row whose weight is 0 or whose token is outside [0, vocab) does not count: its token_loss and logp are 0, its row of
  * dlogits is zero, and neither its logits nor its other numbers are read.  Logits may be -infinity (words that may not be used):
  * their gradient is 0; a token whose own logit is -infinity has logp = -infinity and r = 0, and with a KL term a loss and a
@@ -640,9 +641,9 @@ typedef struct rfast_policy {
     const void*  d_logits;
     int64_t      logits_stride;
     const void*  d_tokens;
-    const float* d_old_logp;           /* [tokens] */
+    const float* d_old_logp;           /* [tokens]; NULL where d_logp alone is wanted */
     const float* d_ref_logp;           /* [tokens], or NULL */
-    const float* d_advantage;          /* [tokens] */
+    const float* d_advantage;          /* [tokens]; likewise */
     const float* d_weight;             /* [tokens], or NULL */
     const float* d_loss_scale;         /* one value, or NULL */
     double       temperature;          /* in [0.001, 1000] */

@@ -609,8 +609,8 @@ def rfast_policy_loss(d_logits: int, d_tokens: int, d_old_logp: int, d_advantage
     """Clipped policy loss with a KL term out of logits [tokens][vocab], and its gradient: token_loss = weight (-min(r A, clamp(r, 1 -
     clip_low, 1 + clip_high) A) + kl_coef (exp(d) - d - 1)) with r = exp(logp - old_logp), d = ref_logp - logp and logp the token's log
     probability at `temperature`.  All addresses are DEVICE addresses: logits and dlogits have `type`, everything else is fp32 [tokens],
-    d_loss and d_loss_scale one value; 0 for what is not given or not wanted.  Rows of weight 0 or with a token outside [0, vocab) do not
-    count.  Enqueued on cuda_stream."""
+    d_loss and d_loss_scale one value; 0 for what is not given or not wanted (d_old_logp and d_advantage too where d_logp is the only result).
+    Rows of weight 0 or with a token outside [0, vocab) do not count.  Enqueued on cuda_stream."""
     args = _Policy(tokens, vocab, _type(type), token_bits, d_logits or None, vocab if logits_stride is None else logits_stride, d_tokens or None,
                    d_old_logp or None, d_ref_logp or None, d_advantage or None, d_weight or None, d_loss_scale or None, temperature, clip_low,
                    clip_high, kl_coef, d_loss or None, d_token_loss or None, d_logp or None, d_dlogits or None,

@@ -105,7 +105,8 @@ struct RowIn {
 };
 template <class T>
 __device__ __forceinline__ RowIn row_in(const Policy& a, int64_t row, const T* z, int64_t t) {
-    return {value_of(z[t]), a.advantage[row], a.weight ? a.weight[row] : 1.f, a.old_logp[row], a.ref_logp ? a.ref_logp[row] : 0.f, a.scale ? *a.scale : 1.f};
+    return {value_of(z[t]), a.advantage ? a.advantage[row] : 0.f, a.weight ? a.weight[row] : 1.f, a.old_logp ? a.old_logp[row] : 0.f,
+            a.ref_logp ? a.ref_logp[row] : 0.f, a.scale ? *a.scale : 1.f};
 }
 __device__ __forceinline__ RowOut row_numbers(const Policy& a, int64_t row, Run r, const RowIn& in, bool keep) {
     const int lane = threadIdx.x & 31;
@@ -373,7 +374,9 @@ extern "C" int rfast_policy_loss(const rfast_policy* p, void* cuda_stream, char*
         if (!p->d_logits || (uintptr_t)p->d_logits % b) return op_fail(err, err_len, RFAST_EINVAL, "%s: logits are null or not aligned to their type", me);
         if ((uintptr_t)p->d_dlogits % b) return op_fail(err, err_len, RFAST_EINVAL, "%s: dlogits are not aligned to their type", me);
         if (!p->d_tokens || (uintptr_t)p->d_tokens % (p->token_bits / 8)) return op_fail(err, err_len, RFAST_EINVAL, "%s: tokens are null or not aligned to their type", me);
-        if (!p->d_old_logp || !p->d_advantage) return op_fail(err, err_len, RFAST_EINVAL, "%s: old_logp or advantage is null", me);
+        // log probabilities by themselves, from which old_logp and ref_logp come, have no use for either
+        if ((p->d_token_loss || p->d_dlogits) && (!p->d_old_logp || !p->d_advantage))
+            return op_fail(err, err_len, RFAST_EINVAL, "%s: old_logp or advantage is null", me);
         const int64_t most = ((int64_t)1 << 56) / p->tokens;
         if (p->logits_stride < 0 || p->logits_stride > most) return op_fail(err, err_len, RFAST_EINVAL, "%s: the stride of logits is negative or spans more than 2^56 elements", me);
         if (p->d_dlogits && ((p->tokens > 1 && p->dlogits_stride < p->vocab) || p->dlogits_stride < 0 || p->dlogits_stride > most))

@@ -1,4 +1,4 @@
-"""Policy loss: rows at the borders between the ways that rows are done, single rows.
+"""Policy loss: rows at the borders between the ways that rows are done, single rows, log probabilities by themselves.
 
 What the sums of a row are off by, u = 2^-24, R = log2(e) / T times the spread of the row's logits:
   * a power of two is off by 2^-22 of itself (what the instruction promises), its exponent, of at most R + 40 either way (the reference may lie
@@ -89,3 +89,23 @@ def test_one_row_has_no_stride(kind, v, stride):
         for a, b in zip(got[:4], want[:4]):
             assert torch.equal(a.reshape(-1), b.reshape(-1)), out_stride
     _within(c, want, 0.1)
+
+
+@pytest.mark.parametrize("n,v,kind,bits", [(1, 1, "f32", 64), (7, 1000, "bf16", 32), (30, 5003, "f32", 64), (9, 50_257, "f16", 64), (3, 400_000, "f32", 32)])
+def test_log_probabilities_by_themselves(n, v, kind, bits):
+    """They need no policy to compare with and no advantage; the bits are those of a call that has them."""
+    import torch
+    import paper_2307_11617_b200 as pkg
+    c = _case(n, v, kind, 0.7, n + v, bits=bits)
+    want = _run(c, 0.1)[2]
+    for w in (c["w"].data_ptr(), 0):
+        out = torch.full((n,), 7.0, device="cuda")
+        pkg.rfast_policy_loss(c["z"].data_ptr(), c["t"].data_ptr(), 0, 0, n, v, d_logp=out.data_ptr(), d_weight=w, temperature=0.7, type=kind, token_bits=bits,
+                              cuda_stream=torch.cuda.current_stream().cuda_stream)
+        if w:
+            assert torch.equal(out, want)
+            continue
+        on = (c["t"].long() >= 0) & (c["t"].long() < v)      # rows without a weight count as well
+        _, _, bound, logp = _sums(c, True)
+        assert torch.equal(out[c["w"] != 0], want[c["w"] != 0]) and not bool(out[~on].any())
+        assert bool(((out.double() - logp).abs() <= bound + U * logp.abs())[on].all())
