@@ -634,8 +634,9 @@ k_grad_norm(const __grid_constant__ NormTable<T> a) {
     if (threadIdx.x == 0) a.part[blockIdx.x] = s;
 }
 
+// The parts are still being written when this kernel is set up: no __restrict__, which would say that nobody writes them while it runs.
 __global__ void __launch_bounds__(kThreadsOp)
-k_grad_norm_end(const double* __restrict__ part, int parts, float max_norm, float* norm, float* scale) {
+k_grad_norm_end(const double* part, int parts, float max_norm, float* norm, float* scale) {
     __shared__ double sh[kWarps];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     double sum = 0.0;

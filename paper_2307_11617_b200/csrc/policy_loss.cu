@@ -287,9 +287,10 @@ k_policy_block(const __grid_constant__ Policy a) {
     policy_row<T, TEAM, ALIGN, KEEP>(a, blockIdx.x / blocks, threadIdx.x, rank, blocks, sh_run, sh_all, &sh_out, (Raw8<T>*)kept);
 }
 
-// The sum of the tokens' losses, in 64 bits and a fixed order.
+// The sum of the tokens' losses, in 64 bits and a fixed order.  They are still being written when this kernel is set up: no __restrict__, which would
+// say that nobody writes them while it runs.
 __global__ void __launch_bounds__(1024)
-k_policy_total(const float* __restrict__ token_loss, int64_t rows, float* __restrict__ loss) {
+k_policy_total(const float* token_loss, int64_t rows, float* loss) {
     __shared__ double sh[32];
     follow();
     double s = 0.0;
