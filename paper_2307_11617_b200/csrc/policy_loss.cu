@@ -57,12 +57,17 @@ __device__ __forceinline__ float two_to(float x) {
 // Sum of 2^(z k - c) over what a thread has seen.  The reference c is the rounded product of k and an earlier maximum (never one exact in a
 // multiply-add): it follows the maximum only where that is 2^kSlack ahead, so that sums are seldom rescaled, and terms below
 // 2^-126 at the reference are 2^-126 of the largest term and less.  No logit but -infinity and NaN so far: c is -infinity.
+// Beyond kNear the rounding of c would be an exponent of its own, up to 2^-24 |c|, without bound (masks of -1e10 or of the type's lowest value, rows
+// that share such an offset).  Nothing is subtracted there: far below zero all powers are 0, which is what they are next to any reference that is near,
+// and a row that has no such reference is done again by far_row.
 struct Run {
     float c, sum;
 };
 constexpr float kSlack = 40.f;
-// what is subtracted: 0 where there is no reference yet (-infinity less 0 is -infinity)
-__device__ __forceinline__ float base_of(float c) { return c == -INFINITY ? 0.f : c; }
+constexpr float kNear = 1048576.f;           // c's rounding is up to 2^-4
+__device__ __forceinline__ bool is_near(float c) { return fabsf(c) < kNear; }
+// what is subtracted: 0 where there is no reference yet, or a far one (-infinity less 0 is -infinity)
+__device__ __forceinline__ float base_of(float c) { return is_near(c) ? c : 0.f; }
 // the factor that takes a sum to the reference `to`; a run without one keeps its sum, 0 or NaN
 __device__ __forceinline__ float rescale(float c, float to) { return c == -INFINITY ? 1.f : two_to(c - to); }
 // Merged over a warp: the largest reference first, so that each sum is taken to it once.
@@ -108,11 +113,10 @@ __device__ __forceinline__ RowIn row_in(const Policy& a, int64_t row, const T* z
     return {value_of(z[t]), a.advantage ? a.advantage[row] : 0.f, a.weight ? a.weight[row] : 1.f, a.old_logp ? a.old_logp[row] : 0.f,
             a.ref_logp ? a.ref_logp[row] : 0.f, a.scale ? *a.scale : 1.f};
 }
-__device__ __forceinline__ RowOut row_numbers(const Policy& a, int64_t row, Run r, const RowIn& in, bool keep) {
+__device__ __forceinline__ RowOut row_numbers(const Policy& a, int64_t row, double base, float sum, const RowIn& in, bool keep) {
     const int lane = threadIdx.x & 31;
-    const double base = (double)base_of(r.c);
     const float zt = __shfl_sync(0xffffffffu, in.zt, 0), ref = __shfl_sync(0xffffffffu, in.ref, 0), old = __shfl_sync(0xffffffffu, in.old, 0);
-    const double logp = a.ln2k * ((double)zt * (double)a.k - base - log2((double)r.sum));
+    const double logp = a.ln2k * ((double)zt * (double)a.k - base - log2((double)sum));
     const double d = (double)ref - logp;
     const double e = lane < 2 ? expm1(lane ? d : logp - (double)old) : 0.0;
     const double e1 = __shfl_sync(0xffffffffu, e, 1);
@@ -132,7 +136,7 @@ __device__ __forceinline__ RowOut row_numbers(const Policy& a, int64_t row, Run 
         slope *= w * (double)in.scale * (double)a.inv_t;
         o.base = (float)base;
         o.slope = (float)slope;
-        o.p = -o.slope / r.sum;
+        o.p = -o.slope / sum;
     }
     return o;
 }
@@ -145,10 +149,84 @@ template <class T> __device__ __forceinline__ int head_of(const T* p, int64_t n)
     return h < n ? h : (int)n;
 }
 
+__device__ __forceinline__ uint32_t cluster_blocks() {
+    uint32_t n;
+    asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(n));
+    return n;
+}
+
+// A row whose logits are all far from zero (or -infinity, or one of which is +infinity): its maximum m, sum and gradient by 2^((z - m) k), where the
+// difference of neighbours is exact.  One value at a time: such rows are rare.  It finds out anew where it is, so that nothing is kept for it.
+template <class T, int TEAM>
+__device__ __noinline__ void far_row(const Policy& a, int64_t row, Run* sh_run, Run* sh_all, RowOut* sh_out) {
+    const int tid = threadIdx.x % TEAM, blocks = TEAM == 32 ? 1 : cluster_blocks(), rank = TEAM == 32 ? 0 : tc::cluster_rank();
+    if (TEAM > 32) row = blockIdx.x / blocks;
+    const T* z = (const T*)a.logits + row * a.in_stride;
+    T* dz = a.dlogits ? (T*)a.dlogits + row * a.out_stride : nullptr;
+    const int64_t t = a.wide_tokens ? ((const int64_t*)a.tokens)[row] : (int64_t)((const int*)a.tokens)[row];
+    const int64_t per = (a.vocab + blocks - 1) / blocks, lo = per * rank < a.vocab ? per * rank : a.vocab, hi = lo + per < a.vocab ? lo + per : a.vocab;     // this block's
+    RowIn in{};
+    if (tid == 0) in = row_in(a, row, z, t);
+    const float k = a.k;
+    float m = -INFINITY, sum = 0.f;
+    for (int pass = 0; pass < 2; ++pass) {                  // the maximum (in c), then the sum
+        const float from = m == -INFINITY ? 0.f : m;
+        if (pass) {
+            for (int64_t i = lo + tid; i < hi; i += TEAM) sum += two_to((value_of(z[i]) - from) * k);
+        } else {
+            for (int64_t i = lo + tid; i < hi; i += TEAM) m = fmaxf(m, value_of(z[i]));
+        }
+        const auto merged = [&](Run r) {
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) {
+                r.c = fmaxf(r.c, __shfl_xor_sync(0xffffffffu, r.c, o));
+                r.sum += __shfl_xor_sync(0xffffffffu, r.sum, o);
+            }
+            return r;
+        };
+        Run r = merged({m, sum});
+        if (TEAM > 32) {
+            __syncthreads();                                // what is in shared memory has been read
+            if ((tid & 31) == 0) sh_run[tid >> 5] = r;
+            __syncthreads();
+            r = merged((tid & 31) < TEAM / 32 ? sh_run[tid & 31] : Run{-INFINITY, 0.f});
+            if (blocks > 1) {
+                tc::cluster_sync();
+                if (tid < blocks) {
+                    const uint32_t at = tc::smem_of(&sh_all[rank], tid);
+                    asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(at), "f"(r.c), "f"(r.sum) : "memory");
+                }
+                __syncwarp();
+                tc::cluster_sync();
+                r = merged((tid & 31) < blocks ? sh_all[tid & 31] : Run{-INFINITY, 0.f});
+            }
+        }
+        m = r.c;
+        sum = r.sum;
+    }
+    const float from = m == -INFINITY ? 0.f : m;
+    RowOut out;
+    if (TEAM == 32 || tid < 32) out = row_numbers(a, row, (double)from * (double)k, sum, in, rank == 0);
+    if (TEAM == 32) {
+        out.p = __shfl_sync(0xffffffffu, out.p, 0);
+        out.slope = __shfl_sync(0xffffffffu, out.slope, 0);
+    } else {
+        if (tid == 0) *sh_out = out;
+        __syncthreads();
+        out = *sh_out;
+    }
+    if (!dz) return;
+    for (int64_t i = lo + tid; i < hi; i += TEAM) {
+        const float p = out.p * two_to((value_of(z[i]) - from) * k);
+        dz[i] = rounded<T>(i == t ? out.slope + p : p);
+    }
+}
+
 // KEEP: iterations of the block's threads over a row whose logits stay in shared memory, a thread's own.  A cluster's blocks share the
 // groups out; the first has what lies before and behind them.
+// True: a row that far_row has to do.
 template <class T, int TEAM, bool ALIGN, int KEEP>
-__device__ __forceinline__ void policy_row(const Policy& a, int64_t row, int tid, int rank, int blocks, Run* sh_run, Run* sh_all, RowOut* sh_out, Raw8<T>* kept) {
+__device__ __forceinline__ bool policy_row(const Policy& a, int64_t row, int tid, int rank, int blocks, Run* sh_run, Run* sh_all, RowOut* sh_out, Raw8<T>* kept) {
     const T* z = (const T*)a.logits + row * a.in_stride;
     T* dz = a.dlogits ? (T*)a.dlogits + row * a.out_stride : nullptr;
     const int64_t t = a.wide_tokens ? ((const int64_t*)a.tokens)[row] : (int64_t)((const int*)a.tokens)[row];
@@ -172,7 +250,7 @@ __device__ __forceinline__ void policy_row(const Policy& a, int64_t row, int tid
             for (int g = tid; g < groups; g += TEAM) store8(d + (int64_t)g * 8, zero);
             if (edge >= 0) dz[edge] = rounded<T>(0.f);
         }
-        return;
+        return false;
     }
     RowIn in{};
     if (tid == 0) in = row_in(a, row, z, t);
@@ -197,7 +275,7 @@ __device__ __forceinline__ void policy_row(const Policy& a, int64_t row, int tid
     r = merged_warp(r);
     RowOut out;
     if (TEAM == 32) {
-        out = row_numbers(a, row, r, in, true);
+        out = row_numbers(a, row, r.c, r.sum, in, true);
         out.base = __shfl_sync(0xffffffffu, out.base, 0);
         out.p = __shfl_sync(0xffffffffu, out.p, 0);
         out.slope = __shfl_sync(0xffffffffu, out.slope, 0);
@@ -215,13 +293,14 @@ __device__ __forceinline__ void policy_row(const Policy& a, int64_t row, int tid
             if (tid < 32) r = merged_warp(tid < blocks ? sh_all[tid] : Run{-INFINITY, 0.f});
         }
         if (tid < 32) {
-            const RowOut o = row_numbers(a, row, r, in, rank == 0);
+            const RowOut o = row_numbers(a, row, r.c, r.sum, in, rank == 0);
             if (tid == 0) *sh_out = o;
         }
         __syncthreads();
         out = *sh_out;
     }
-    if (!dz) return;
+    if (!is_near(out.base)) return true;                    // far_row forms the row's numbers again
+    if (!dz) return false;
     const auto slope_of = [&](float v, int64_t i) {
         const float p = out.p * two_to(fmaf(v, k, -out.base));
         return i == t ? out.slope + p : p;
@@ -261,6 +340,7 @@ __device__ __forceinline__ void policy_row(const Policy& a, int64_t row, int tid
     } else {
         for (int64_t i = tid; i < n; i += TEAM) dz[i] = rounded<T>(slope_of(value_of(z[i]), i));
     }
+    return false;
 }
 
 template <class T, bool ALIGN>
@@ -268,11 +348,12 @@ __global__ void __launch_bounds__(256)
 k_policy_warp(const __grid_constant__ Policy a) {
     let_follow();
     for (int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); row < a.rows; row += (int64_t)gridDim.x * 8)
-        policy_row<T, 32, ALIGN, 0>(a, row, threadIdx.x & 31, 0, 1, nullptr, nullptr, nullptr, nullptr);
+        if (policy_row<T, 32, ALIGN, 0>(a, row, threadIdx.x & 31, 0, 1, nullptr, nullptr, nullptr, nullptr)) far_row<T, 32>(a, row, nullptr, nullptr, nullptr);
 }
 
+// Nine blocks of 128 threads to an SM, for which far_row has to spill registers (8192 x 9000 bf16: 67 us, 70 with eight, 66 without far_row).
 template <class T, int TEAM, bool ALIGN, int KEEP>
-__global__ void __launch_bounds__(TEAM, 1024 / TEAM)
+__global__ void __launch_bounds__(TEAM, TEAM == kMidTeam && sizeof(T) == 2 ? 9 : 1024 / TEAM)
 k_policy_block(const __grid_constant__ Policy a) {
     extern __shared__ __align__(32) uint8_t kept[];
     __shared__ Run sh_run[TEAM / 32], sh_all[8];
@@ -280,11 +361,12 @@ k_policy_block(const __grid_constant__ Policy a) {
     let_follow();
     uint32_t blocks = 1, rank = 0;
     if (KEEP > 0) {
-        asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(blocks));
+        blocks = cluster_blocks();
         rank = tc::cluster_rank();
         if (blocks > 1) tc::cluster_sync();                 // all have begun: their shared memory is there
     }
-    policy_row<T, TEAM, ALIGN, KEEP>(a, blockIdx.x / blocks, threadIdx.x, rank, blocks, sh_run, sh_all, &sh_out, (Raw8<T>*)kept);
+    if (policy_row<T, TEAM, ALIGN, KEEP>(a, blockIdx.x / blocks, threadIdx.x, rank, blocks, sh_run, sh_all, &sh_out, (Raw8<T>*)kept))
+        far_row<T, TEAM>(a, 0, sh_run, sh_all, &sh_out);
 }
 
 // The sum of the tokens' losses, in 64 bits and a fixed order.  They are still being written when this kernel is set up: no __restrict__, which would

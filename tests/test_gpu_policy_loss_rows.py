@@ -41,7 +41,7 @@ def _sums(c, align):
     import torch
     z = c["z"].double() / c["warm"]
     t = c["t"].long().clamp(0, c["v"] - 1)[:, None]
-    R = (z.amax(1) - z.amin(1)) / LN2
+    R = (z.amax(1) - torch.where(torch.isfinite(z), z, math.inf).amin(1)) / LN2
     E = 2.0 ** -22 * (5 + R / 40) + U * (LN2 * (R + 40) + _chain(c["v"], c["kind"], align) + 19 + R / 40)
     return R, E, E + U * LN2 * R, z.gather(1, t)[:, 0] - torch.logsumexp(z, 1)
 
