@@ -116,7 +116,8 @@ __device__ __forceinline__ RowIn row_in(const Policy& a, int64_t row, const T* z
 __device__ __forceinline__ RowOut row_numbers(const Policy& a, int64_t row, double base, float sum, const RowIn& in, bool keep) {
     const int lane = threadIdx.x & 31;
     const float zt = __shfl_sync(0xffffffffu, in.zt, 0), ref = __shfl_sync(0xffffffffu, in.ref, 0), old = __shfl_sync(0xffffffffu, in.old, 0);
-    const double logp = a.ln2k * ((double)zt * (double)a.k - base - log2((double)sum));
+    const double up_to = a.ln2k * ((double)zt * (double)a.k - base - log2((double)sum));
+    const double logp = up_to > 0.0 ? 0.0 : up_to;          // a word that has all of the probability, and a sum that is off; NaN stays
     const double d = (double)ref - logp;
     const double e = lane < 2 ? expm1(lane ? d : logp - (double)old) : 0.0;
     const double e1 = __shfl_sync(0xffffffffu, e, 1);

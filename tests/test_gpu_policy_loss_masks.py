@@ -104,3 +104,24 @@ def test_two_values_far_from_zero(base, v):
     got = _run(c, 0.1)
     _within(plain, got, 0.1)
     assert not bool(got[3][:, :100].any()) and not bool(got[3][:, 108:].any())
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("warm", [0.7, 1.0, 1.3])
+@pytest.mark.parametrize("v", [64, 3000, 50_001])
+def test_no_log_probability_is_above_zero(kind, warm, v):
+    """Words that have all, or nearly all, of a row: their powers are off either way, their log probabilities are not above that of certainty."""
+    import torch
+    n = 200
+    c = _case(n, v, kind, warm, v)
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(v)
+    c["t"].copy_(torch.randint(0, v, (n,), generator=gen, device="cuda"))
+    c["w"].fill_(1.0)
+    top = 40.0 + 20.0 * torch.rand(n, 1, generator=gen, device="cuda")
+    c["z"].scatter_(1, c["t"].long()[:, None], top.to(c["z"].dtype))
+    logp = torch.log_softmax(c["z"].double() / warm, 1).gather(1, c["t"].long()[:, None])[:, 0]
+    c["old"], c["ref"] = (logp - 0.1).float(), (logp + 0.1).float()
+    got = _run(c, 0.1)
+    assert bool((got[2] <= 0).all())
+    _within(c, got, 0.1)
