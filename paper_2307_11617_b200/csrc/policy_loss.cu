@@ -10,8 +10,10 @@
 // (Bringing rows through a ring in shared memory by bulk copies, a cluster to a row and the next row's sum before this one's
 // gradient, read every logit once and took 510 us: with 20 instructions a logit in the place of 13 the issue slots were the bound.)
 //
-// Powers are taken of two: exp((z - c) / T) = 2^(z k - c') with k = log2(e) / T in fp32 and c' the rounded z_max k.  k is the only
-// constant that both passes and the row's numbers share, so rounding it is a change of T by 2^-25 of itself and nothing else.
+// Powers are taken of two: exp((z - m) / T) = 2^(z k - c) with k = log2(e) / T and c near m k (see Run).  k in fp32 would be another T, by up to 2^-24 of
+// itself, which moves all token losses of a call one way; the sums take it in two parts, one multiply-add more (2047 x 50257 f16 94.2 -> 94.5 us, 4096 x
+// 128256 bf16 without a gradient 197.5 -> 201), the row's numbers in 64 bits.  The gradient's powers have it in fp32: it matters to their distance
+// from c only, c's own share is made up for in p.
 #include <cuda_runtime.h>
 
 #include <climits>
@@ -31,7 +33,9 @@ constexpr int kPlaces = 240;                 // blocks of 512 threads that run a
 constexpr int kAhead = 4;                    // groups of eight logits that a thread has on their way (four more, fetched while it works: no gain)
 constexpr int64_t kShortRow = 1024;          // logits of a row up to which a warp does it
 constexpr int kKept = 96 * 1024;             // bytes of a row that a long row's block keeps; two blocks share an SM
-constexpr int64_t kReadAgain = 56ll << 20;   // bytes (4096 x 128256 bf16 leave 47 MB: 414 us, 452 by pairs of blocks; 2000 x 100000 f32 90 MB: 362, 336 by pairs)
+// Bytes read again above which pairs of blocks do a row (one block, pairs; us): 4096 rows bf16 at 47 MB 418, 456; 53 MB 466, 496; 61 MB 522, 528; 68 MB 564,
+// 545; 77 MB 634, 597.  2000 rows f32 at 48 MB 225, 227; 54 MB 247, 245; 60 MB 270, 256; 90 MB 366, 339.
+constexpr int64_t kReadAgain = 56ll << 20;
 constexpr int64_t kHalfRow = 128 * 1024, kQuarterRow = 40 * 1024;     // bytes of a row up to which it is a block of half, of a quarter of the threads
 
 struct Policy {
@@ -42,8 +46,9 @@ struct Policy {
     void* dlogits;
     int64_t rows, vocab, in_stride, out_stride;
     int wide_tokens;
-    float k;                           // log2(e) / T
-    double ln2k;                       // ln 2, of which k makes 1 / T
+    double exact_k;                    // log2(e) / T
+    float k, high, low;                // rounded; its first 12 bits (or the number below), so that the rest is above 0 and takes -infinity as it should
+    float beyond;                      // exact_k / k - 1
     float inv_t;
     double clip_lo, clip_hi, kl;       // 1 - clip_low, 1 + clip_high
 };
@@ -88,14 +93,14 @@ __device__ __forceinline__ void follow_top(Run& r, float top, float k) {
     }
 }
 template <int N>
-__device__ __forceinline__ void take(Run& r, const float (&v)[N], float k) {
+__device__ __forceinline__ void take(Run& r, const float (&v)[N], const Policy& a) {
     float top = v[0];
 #pragma unroll
     for (int i = 1; i < N; ++i) top = fmaxf(top, v[i]);
-    follow_top(r, top, k);
+    follow_top(r, top, a.k);
     const float c = base_of(r.c);
 #pragma unroll
-    for (int i = 0; i < N; ++i) r.sum += two_to(fmaf(v[i], k, -c));
+    for (int i = 0; i < N; ++i) r.sum += two_to(fmaf(v[i], a.low, fmaf(v[i], a.high, -c)));
 }
 
 // What the second pass needs of a row: the gradient is p * 2^(z k - base), at the token plus `slope`.
@@ -113,10 +118,10 @@ __device__ __forceinline__ RowIn row_in(const Policy& a, int64_t row, const T* z
     return {value_of(z[t]), a.advantage ? a.advantage[row] : 0.f, a.weight ? a.weight[row] : 1.f, a.old_logp ? a.old_logp[row] : 0.f,
             a.ref_logp ? a.ref_logp[row] : 0.f, a.scale ? *a.scale : 1.f};
 }
-__device__ __forceinline__ RowOut row_numbers(const Policy& a, int64_t row, double base, float sum, const RowIn& in, bool keep) {
+__device__ __forceinline__ RowOut row_numbers(const Policy& a, int64_t row, float from, float c, float sum, const RowIn& in, bool keep) {
     const int lane = threadIdx.x & 31;
     const float zt = __shfl_sync(0xffffffffu, in.zt, 0), ref = __shfl_sync(0xffffffffu, in.ref, 0), old = __shfl_sync(0xffffffffu, in.old, 0);
-    const double up_to = a.ln2k * ((double)zt * (double)a.k - base - log2((double)sum));
+    const double up_to = 0.6931471805599453 * (((double)zt - (double)from) * a.exact_k - (double)c - log2((double)sum));
     const double logp = up_to > 0.0 ? 0.0 : up_to;          // a word that has all of the probability, and a sum that is off; NaN stays
     const double d = (double)ref - logp;
     const double e = lane < 2 ? expm1(lane ? d : logp - (double)old) : 0.0;
@@ -135,9 +140,9 @@ __device__ __forceinline__ RowOut row_numbers(const Policy& a, int64_t row, doub
         if (keep && a.token_loss) a.token_loss[row] = (float)(w * loss);
         if (keep && a.logp) a.logp[row] = (float)logp;
         slope *= w * (double)in.scale * (double)a.inv_t;
-        o.base = (float)base;
+        o.base = c;
         o.slope = (float)slope;
-        o.p = -o.slope / sum;
+        o.p = -o.slope / sum * two_to(c * a.beyond);        // in 32 bits: off by 2^-22, as much as a power is
     }
     return o;
 }
@@ -207,7 +212,7 @@ __device__ __noinline__ void far_row(const Policy& a, int64_t row, Run* sh_run, 
     }
     const float from = m == -INFINITY ? 0.f : m;
     RowOut out;
-    if (TEAM == 32 || tid < 32) out = row_numbers(a, row, (double)from * (double)k, sum, in, rank == 0);
+    if (TEAM == 32 || tid < 32) out = row_numbers(a, row, from, 0.f, sum, in, rank == 0);
     if (TEAM == 32) {
         out.p = __shfl_sync(0xffffffffu, out.p, 0);
         out.slope = __shfl_sync(0xffffffffu, out.slope, 0);
@@ -269,14 +274,14 @@ __device__ __forceinline__ bool policy_row(const Policy& a, int64_t row, int tid
                 if (KEEP > 0 && it + u < KEEP) kept[(it + u) * TEAM + tid] = q[u];
                 float v[8];
                 unpack8(q[u], v);
-                take(r, v, k);
+                take(r, v, a);
             }
     }
-    if (edge >= 0) { const float v[1] = {value_of(z[edge])}; take(r, v, k); }
+    if (edge >= 0) { const float v[1] = {value_of(z[edge])}; take(r, v, a); }
     r = merged_warp(r);
     RowOut out;
     if (TEAM == 32) {
-        out = row_numbers(a, row, r.c, r.sum, in, true);
+        out = row_numbers(a, row, 0.f, r.c, r.sum, in, true);
         out.base = __shfl_sync(0xffffffffu, out.base, 0);
         out.p = __shfl_sync(0xffffffffu, out.p, 0);
         out.slope = __shfl_sync(0xffffffffu, out.slope, 0);
@@ -294,7 +299,7 @@ __device__ __forceinline__ bool policy_row(const Policy& a, int64_t row, int tid
             if (tid < 32) r = merged_warp(tid < blocks ? sh_all[tid] : Run{-INFINITY, 0.f});
         }
         if (tid < 32) {
-            const RowOut o = row_numbers(a, row, r.c, r.sum, in, rank == 0);
+            const RowOut o = row_numbers(a, row, 0.f, r.c, r.sum, in, rank == 0);
             if (tid == 0) *sh_out = o;
         }
         __syncthreads();
@@ -491,8 +496,13 @@ extern "C" int rfast_policy_loss(const rfast_policy* p, void* cuda_stream, char*
     a.token_loss = p->d_token_loss; a.logp = p->d_logp; a.dlogits = p->d_dlogits;
     a.rows = p->tokens; a.vocab = p->vocab; a.in_stride = p->logits_stride; a.out_stride = p->dlogits_stride;
     a.wide_tokens = p->token_bits == 64;
-    a.k = (float)(1.4426950408889634 / p->temperature);
-    a.ln2k = 0.6931471805599453;
+    a.exact_k = 1.4426950408889634 / p->temperature;
+    a.k = (float)a.exact_k;
+    int binary = 0;
+    const double digits = std::frexp(a.exact_k, &binary);
+    a.high = (float)std::ldexp(std::ceil(digits * 4096) - 1, binary - 12);
+    a.low = (float)(a.exact_k - a.high);
+    a.beyond = (float)(a.exact_k / a.k - 1.0);
     a.inv_t = (float)(1.0 / p->temperature);
     a.clip_lo = 1.0 - p->clip_low; a.clip_hi = 1.0 + p->clip_high; a.kl = p->kl_coef;
     cudaStream_t st = (cudaStream_t)cuda_stream;
