@@ -596,7 +596,8 @@ int rfast_group_norm_backward(const rfast_gn_shape* shape, const void* d_dy, con
  * are 32- or 64-bit integers.  The backward pass sorts tokens and positions (stably), so that each sum runs over
  * ascending positions in fp32, long ones over sums of up to 16 and of 256 sorted places; each value is rounded once to its type.
  * Without accumulate every row of dtable is written, zeros where a token does not occur; with it those rows are left alone.
- * A NaN or infinity of a row of dout reaches the row of its token and nothing else.  scale is finite.
+ * A NaN or infinity of a row of dout reaches the row of its token and nothing else.  scale is finite.  The same call gives the
+ * same bits; the last bits of a row also depend on where its token lies among the sorted ones.
  * Strides are those of a row in elements.  Read operands may overlap themselves (a stride of 0 repeats a row), written
  * ones may not; no other operands may overlap.  Addresses need to be aligned to their type only; where width is a multiple
  * of 8, strides are, and addresses are multiples of eight values' size, both operands are moved eight values at a time.  At most
@@ -628,8 +629,11 @@ int     rfast_embedding_backward(const rfast_emb_shape* shape, const void* d_tok
  * dlogits is zero, and neither its logits nor its other numbers are read.  Logits may be -infinity (words that may not be used):
  * their gradient is 0; a token whose own logit is -infinity has logp = -infinity and r = 0, and with a KL term a loss and a
  * gradient of NaN.  A row of nothing but -infinity, a NaN or +infinity leave that row's results and `loss` NaN.
- * Running sums of a row are fp32, a row's own numbers (logp, r, both terms) and `loss` 64 bits; each result is rounded
- * once; exp((z - z_max) / T) below 2^-126 may count as 0.  |z| / T below 2^126.
+ * Running sums of a row are fp32; a row's own numbers (logp, r, both terms) are formed from them in 64 bits.  token_loss and logp (never above
+ * 0) are rounded once; `loss` is the 64-bit sum of token_loss as it is rounded, rounded once more; dlogits are products of two fp32 numbers, off by at most 2^-18 + 2^-24 |z - z_max| / T of
+ * themselves and what the row's sum is off by (at the token: added to an fp32 number), rounded once to their type; exp((z - z_max) / T) below
+ * 2^-126 may count as 0.  Words may as well be masked by a large negative logit, down to the lowest of the type.  The same call gives the same bits.
+ * In another call a row may differ in its last bits: its sum is shared out by the number of rows and by where its gradient lies.
  * Strides are those of a row in elements; logits may overlap themselves (a stride of 0 repeats a row), dlogits may not.
  * dlogits may be the logits, with their stride; no other operands may overlap.  Addresses need to be aligned to their type
  * only.  The fast case is a gradient whose rows begin at the same place within eight values as the logits' do (both contiguous,
@@ -678,7 +682,8 @@ int rfast_policy_loss(const rfast_policy* p, void* cuda_stream, char* err, size_
  * to their type only.  workspace: rfast_muon_workspace(n_tensors, rows, cols, terms) bytes of DEVICE memory (terms 1 or 2), aligned
  * to 256; matrices go in runs of up to 128 in 8 shapes, which use it one after another.  Its first four
  * bytes hold an int32 when the work is done: 0, or a code where a wait inside a kernel ran out (a fault of the device: the
- * parameters are then not to be used). */
+ * parameters are then not to be used); where no matrix has rows and columns it is not touched.  The same call gives the same bits; a matrix
+ * may differ in its last bits where the list around it has other tiles chosen for its products. */
 #define RFAST_MUON_MAX_SIDE 65536
 enum { RFAST_MUON_SIZE_SPECTRAL = 0, RFAST_MUON_SIZE_RMS = 1 };
 typedef struct rfast_muon {

@@ -212,7 +212,8 @@ __device__ __forceinline__ void begin_tile(const MuonMat& a, const MuonScalars& 
     }
 }
 
-// X = u / max(norm, eps), m x n, as it is held: 64 x 64 values of the parameter's shape per block.
+// X = u / max(norm, eps), m x n, as it is held: 64 x 64 values of the parameter's shape per block.  Every block adds up its matrix's
+// squares from the first kernel's sums by itself: 34 MB out of the L2 cache at 4096 x 4096, 8.6 GB (of 79 ms) at 16384 x 16384.
 __global__ void __launch_bounds__(256)
 k_muon_begin(const __grid_constant__ MuonTable t, MuonScalars c, const double* parts, const __grid_constant__ MuonGemm q) {
     __shared__ double sh[8];
