@@ -8,7 +8,7 @@
 // it reads again, the last first.  Without that the rows under way, 296 of 256 KB, are too much for the L2 cache: 4096 x 128256 bf16 read
 // 1.72 GB instead of 0.93, 445 us; with it 1.03 GB, 414 us, 4.7 TB/s and half of the issue slots and of the special function unit.
 // (Bringing rows through a ring in shared memory by bulk copies, a cluster to a row and the next row's sum before this one's
-// gradient, read every logit once and took 510 us: with 20 instructions a logit in the place of 13 the issue slots were the bound.)
+// gradient, read every logit once and took 510 us: with 20 instructions a logit in the place of then 13 the issue slots were the bound.)
 //
 // Powers are taken of two: exp((z - m) / T) = 2^(z k - c) with k = log2(e) / T and c near m k (see Run).  k in fp32 would be another T, by up to 2^-24 of
 // itself, which moves all token losses of a call one way; the sums take it in two parts, one multiply-add more (2047 x 50257 f16 94.2 -> 94.5 us, 4096 x
