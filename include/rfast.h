@@ -629,10 +629,11 @@ int     rfast_embedding_backward(const rfast_emb_shape* shape, const void* d_tok
  * dlogits is zero, and neither its logits nor its other numbers are read.  Logits may be -infinity (words that may not be used):
  * their gradient is 0; a token whose own logit is -infinity has logp = -infinity and r = 0, and with a KL term a loss and a
  * gradient of NaN.  A row of nothing but -infinity, a NaN or +infinity leave that row's results and `loss` NaN.
- * Running sums of a row are fp32; a row's own numbers (logp, r, both terms) are formed from them in 64 bits.  token_loss and logp (never above
- * 0) are rounded once; `loss` is the 64-bit sum of token_loss as it is rounded, rounded once more; dlogits are products of two fp32 numbers, off by at most 2^-18 + 2^-24 |z - z_max| / T of
- * themselves and what the row's sum is off by (at the token: added to an fp32 number), rounded once to their type; exp((z - z_max) / T) below
- * 2^-126 may count as 0.  Words may as well be masked by a large negative logit, down to the lowest of the type.  The same call gives the same bits.
+ * Running sums of a row are fp32; a row's own numbers (logp, r, both terms) are formed from them in 64 bits.  token_loss and logp (never
+ * above 0) are rounded once; `loss` is the 64-bit sum of token_loss as it is rounded, rounded once more; dlogits are products of two fp32
+ * numbers, off by at most 2^-18 + 2^-24 |z - z_max| / T of themselves and what the row's sum is off by (at the token: added to an fp32
+ * number), rounded once to their type; exp((z - z_max) / T) below 2^-126 may count as 0.  Words may as well be masked by a large negative
+ * logit, down to the lowest of the type.  The same call gives the same bits.
  * In another call a row may differ in its last bits: its sum is shared out by the number of rows and by where its gradient lies.
  * Strides are those of a row in elements; logits may overlap themselves (a stride of 0 repeats a row), dlogits may not.
  * dlogits may be the logits, with their stride; no other operands may overlap.  Addresses need to be aligned to their type
